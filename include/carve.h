@@ -275,8 +275,137 @@ int carve_rmsnorm_bwd(const carve_dims_t* d, const void* o, const float* weight,
 int carve_rmsnorm_bwd_noalloc(const carve_dims_t* d, const void* o, const float* weight, float eps,
                               const void* dy, void* d_o, float* dweight, hipStream_t stream);
 
+/* ---- the gated delta rule (scalar decay) ------------------------------------
+ *
+ * The scalar-gated delta rule that the CARVE layer is compared with, per
+ * sequence and value head (key head hv / (Hv / Hk); S in R^{Dv x Dk}, f32):
+ *     S~ = exp(g_t) S_{t-1},  u_t = beta_t (v_t - S~ k_t),
+ *     S_t = S~ + u_t k_t^T,   o_t = scale S_t q_t
+ * with one log decay g_t <= 0 and one write strength beta_t per token and
+ * value head, and the decay before the prediction.  carve_gdr_chunk_fwd and
+ * carve_gdr_chunk_bwd evaluate it in chunks of 64 tokens (any T; no padding),
+ * carve_gdr_step token by token on a pool of states.
+ *
+ *   - q, k are [B, T, Hk, Dk] and v is [B, T, Hv, Dv] with the strides of
+ *     carve_gdr_dims_t (in elements; the last dimension is contiguous), so that
+ *     they may be slices of a fused projection.  beta [B, T, Hv] (token dtype),
+ *     g [B, T, Hv] (f32), o and dO [B, T, Hv, Dv] and every gradient are dense.
+ *     The strides may not be negative; a stride of 0 is a broadcast input, whose
+ *     gradient is still written per element.
+ *   - Packed sequences: with N > 0, B must be 1 and the T rows hold N sequences,
+ *     sequence n being rows [offsets[n], offsets[n + 1]); offsets is a device
+ *     array of N + 1 ints, non-decreasing from >= 0 to <= T.  Sequences may be
+ *     empty or of one token.  Rows of o and of the gradients that belong to no
+ *     sequence are left as they were.  Offsets are not read on the host: values
+ *     outside this contract stay within the tensors, with unspecified results.
+ *     With N = 0, offsets must be NULL and every batch element is a sequence.
+ *   - S0, S_T, dS_T, dS0: [sequences, Hv, Dv, Dk] f32.  The state of an empty
+ *     sequence passes through.  S_chunks: [carve_gdr_chunk_count(d), Hv, Dv, Dk]
+ *     f32, the state at the start of every chunk, written by carve_gdr_chunk_fwd for
+ *     carve_gdr_chunk_bwd (slots of no chunk are left as they were).
+ *   - Supported: Dk in {32, 64, 128}; Dv in {32, 64, 128, 256}; Hv a multiple of
+ *     Hk, at most 65535; dtype f32 or bf16.  scale is finite.  q, k, v and their
+ *     strides are 16-byte aligned, like every other pointer.
+ *   - Inputs are finite with g <= 0; g = -inf is a reset (decay 0).  With bf16
+ *     tokens the chunk form carries f32 intermediates through the matrix cores as
+ *     sums of two bf16 values (errors of states and of dg of some 1e-6 of their
+ *     size); with f32 tokens all products are f32.
+ */
+typedef struct {
+  int B, T;            /* dense: B sequences of T tokens; packed: B = 1, T rows */
+  int N;               /* packed: number of sequences; dense: 0 */
+  int Hk, Hv, Dk, Dv;
+  carve_dtype_t dtype;
+  float scale;
+  long long q_batch, q_token, q_head;   /* strides in elements */
+  long long k_batch, k_token, k_head;
+  long long v_batch, v_token, v_head;
+} carve_gdr_dims_t;
+
+/* Chunks that S_chunks has room for (the same as a program needs to allocate;
+ * dense: B ceil(T / 64); packed: floor(T / 64) + N); 0 for invalid dims. */
+size_t carve_gdr_chunk_count(const carve_gdr_dims_t* d);
+
+/* Bytes of device workspace of carve_gdr_chunk_fwd (for_backward = 0) and
+ * carve_gdr_chunk_bwd (1); 0 for invalid dims.  Nothing in it is kept between calls;
+ * calls that overlap in time need workspaces of their own, and so do captured
+ * graphs that may run at once. */
+size_t carve_gdr_workspace_size(const carve_gdr_dims_t* d, int for_backward);
+
+/* Forward.  S0, S_T, S_chunks may be NULL (zeros; not wanted).  Two launches.
+ * The strides of q, k, v are those of d. */
+int carve_gdr_chunk_fwd(const carve_gdr_dims_t* d, const void* q, const void* k, const void* v, const float* g,
+                        const void* beta, const float* S0, const int* offsets, void* o, float* S_T,
+                        float* S_chunks, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Backward for loss <dO, o> + <dS_T, S_T>.  In: the forward's inputs (S0 only
+ * through S_chunks), S_chunks as carve_gdr_chunk_fwd wrote it, dO, dS_T or NULL (zeros).
+ * Out: dq, dk [B,T,Hk,Dk], dv [B,T,Hv,Dv], dbeta [B,T,Hv] (token dtype), dg
+ * [B,T,Hv] f32, dS0 or NULL.  dq and dk are summed over the value heads of their
+ * key head in order: reruns are bitwise identical.  Three launches. */
+int carve_gdr_chunk_bwd(const carve_gdr_dims_t* d, const void* q, const void* k, const void* v, const float* g,
+                        const void* beta, const float* S_chunks, const int* offsets, const void* dO,
+                        const float* dS_T, void* dq, void* dk, void* dv, float* dg, void* dbeta, float* dS0,
+                        void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* T tokens for each of B sequences (d->N = 0), token by token in f32: state is a
+ * pool of `pool` states [pool, Hv, Dv, Dk] f32, updated in place; sequence b's
+ * state is state[slots[b]] (slots: [B] device ints), or state[b] with slots NULL
+ * (then pool >= B).  A sequence whose slot is outside [0, pool) is a padding
+ * entry: its state and its rows of o are left as they were.  Two sequences of one
+ * call may not have the same slot (their results are then unspecified).  B is at
+ * most 65535.  One launch, no workspace. */
+int carve_gdr_step(const carve_gdr_dims_t* d, const void* q, const void* k, const void* v, const float* g,
+                   const void* beta, const int* slots, int pool, float* state, void* o, hipStream_t stream);
+
+/* ---- the norms around a block, with its gate and residual scale ---------------
+ *
+ * Rows of N values, statistics and parameters in f32 (see also carve_rmsnorm_fwd,
+ * the plain norm of the layer's output):
+ *     n = y / sqrt(mean(y^2 over its group) + eps) * weight
+ *     t = n * act(gate)                    (gate given; act: SiLU or sigmoid)
+ *     x = alpha * residual + scale * t     (residual, scale given)
+ *     h = x / sqrt(mean(x^2) + eps) * next_weight       (next_weight given)
+ * y is a block's output; n its norm over `groups` equal groups of a row (1: the
+ * row; H: per head, with N = H Dv); x the residual stream; h the next block's
+ * input.  One pass: h is formed from x before x is rounded to its dtype.
+ * weight, scale, next_weight: [N] f32.  y, gate, residual have row strides (in
+ * elements, >= 0, 16-byte aligned), every other tensor is dense.
+ * Supported: N a multiple of 8 (bf16) or 4 (f32), at most 8192; with groups > 1,
+ * N / groups must be 16 bytes times a power of two up to 64; eps finite and >= 0,
+ * alpha finite. */
+enum { CARVE_GATE_SILU = 1, CARVE_GATE_SIGMOID = 2 };
+typedef struct {
+  long long rows;
+  int N, groups;
+  carve_dtype_t dtype;
+  int gate_act;        /* CARVE_GATE_*, read where gate is given */
+  float eps, alpha;    /* alpha is read where residual is given */
+  long long y_stride, gate_stride, residual_stride;
+} carve_block_norm_dims_t;
+
+/* gate, residual, scale may be NULL (left out); next_weight and h are both given
+ * or both NULL.  One launch. */
+int carve_block_norm_fwd(const carve_block_norm_dims_t* d, const void* y, const float* weight, const void* gate,
+                         const void* residual, const float* scale, const float* next_weight, void* x, void* h,
+                         hipStream_t stream);
+
+/* Bytes of device workspace of carve_block_norm_bwd; 0 for invalid dims. */
+size_t carve_block_norm_workspace_size(const carve_block_norm_dims_t* d);
+
+/* Backward for loss <dx, x> + <dh, h>: in the forward's inputs (x is formed again,
+ * unrounded) and dx, dh (dx may be NULL, zeros, where dh is given; dh is given
+ * exactly where next_weight is).  Out: dy, dgate and dresidual (exactly where gate
+ * and residual are given) in the token dtype; dweight, dscale, dnext_weight [N]
+ * f32 (exactly where their inputs are given), summed over the rows in a fixed
+ * order (reruns are bitwise identical).  Two launches. */
+int carve_block_norm_bwd(const carve_block_norm_dims_t* d, const void* y, const float* weight, const void* gate,
+                         const void* residual, const float* scale, const float* next_weight, const void* dx,
+                         const void* dh, void* dy, void* dgate, void* dresidual, float* dweight, float* dscale,
+                         float* dnext_weight, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
 /* Measurement hook (not part of the computation).  Arms the next
- * carve_chunk_* or carve_rmsnorm_* call made on the calling thread to record
+ * carve_chunk_*, carve_rmsnorm_*, carve_gdr_* or carve_block_norm_* call made on the calling thread to record
  * events[0] on its stream before its first kernel launch and events[i] after
  * its i-th launch (the forward makes 1 launch; the backward 4: clear of the
  * chunk ready flags, chunk recompute fused with the adjoint, the partials of

@@ -9,6 +9,7 @@ tensor of the right dtype, the call raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -21,12 +22,28 @@ SYMBOLS = ("carve_chunk_fwd", "carve_chunk_bwd", "carve_chunk_fwd_gated", "carve
            "carve_chunk_fwd_sw", "carve_chunk_bwd_sw", "carve_chunk_fwd_act", "carve_chunk_bwd_act",
            "carve_rmsnorm_fwd", "carve_rmsnorm_bwd", "carve_rmsnorm_workspace_size", "carve_rmsnorm_bwd_noalloc",
            "carve_workspace_size", "carve_status_string", "carve_profile_events", "carve_bwd_wait_status",
-           "carve_set_ready_wait_limit")
+           "carve_set_ready_wait_limit",
+           "carve_gdr_chunk_fwd", "carve_gdr_chunk_bwd", "carve_gdr_step", "carve_gdr_chunk_count",
+           "carve_gdr_workspace_size", "carve_block_norm_fwd", "carve_block_norm_bwd",
+           "carve_block_norm_workspace_size")
 
 
 class Dims(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int), ("T", ctypes.c_int), ("H", ctypes.c_int), ("Dk", ctypes.c_int),
                 ("Dv", ctypes.c_int), ("R", ctypes.c_int), ("L", ctypes.c_int), ("dtype", ctypes.c_int)]
+
+
+class GdrDims(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int) for n in ("B", "T", "N", "Hk", "Hv", "Dk", "Dv", "dtype")]
+                + [("scale", ctypes.c_float)]
+                + [(n, ctypes.c_longlong) for n in ("q_batch", "q_token", "q_head", "k_batch", "k_token", "k_head",
+                                                    "v_batch", "v_token", "v_head")])
+
+
+class BlockNormDims(ctypes.Structure):
+    _fields_ = ([("rows", ctypes.c_longlong)] + [(n, ctypes.c_int) for n in ("N", "groups", "dtype", "gate_act")]
+                + [("eps", ctypes.c_float), ("alpha", ctypes.c_float)]
+                + [(n, ctypes.c_longlong) for n in ("y_stride", "gate_stride", "residual_stride")])
 
 
 class CarveError(RuntimeError):
@@ -84,6 +101,23 @@ def load_library(path: str = LIB_PATH):
     lib.carve_bwd_wait_status.restype = ctypes.c_int
     lib.carve_set_ready_wait_limit.argtypes = [ctypes.c_int]
     lib.carve_set_ready_wait_limit.restype = ctypes.c_int
+    G, N = ctypes.POINTER(GdrDims), ctypes.POINTER(BlockNormDims)
+    lib.carve_gdr_chunk_count.argtypes = [G]
+    lib.carve_gdr_chunk_count.restype = sz
+    lib.carve_gdr_workspace_size.argtypes = [G, ctypes.c_int]
+    lib.carve_gdr_workspace_size.restype = sz
+    lib.carve_gdr_chunk_fwd.argtypes = [G] + [vp] * 11 + [sz, vp]
+    lib.carve_gdr_chunk_fwd.restype = ctypes.c_int
+    lib.carve_gdr_chunk_bwd.argtypes = [G] + [vp] * 16 + [sz, vp]
+    lib.carve_gdr_chunk_bwd.restype = ctypes.c_int
+    lib.carve_gdr_step.argtypes = [G] + [vp] * 6 + [ctypes.c_int] + [vp] * 3
+    lib.carve_gdr_step.restype = ctypes.c_int
+    lib.carve_block_norm_fwd.argtypes = [N] + [vp] * 9
+    lib.carve_block_norm_fwd.restype = ctypes.c_int
+    lib.carve_block_norm_workspace_size.argtypes = [N]
+    lib.carve_block_norm_workspace_size.restype = sz
+    lib.carve_block_norm_bwd.argtypes = [N] + [vp] * 15 + [sz, vp]
+    lib.carve_block_norm_bwd.restype = ctypes.c_int
     if path == LIB_PATH:
         _lib = lib
     return lib
@@ -443,3 +477,277 @@ def rmsnorm_bwd_noalloc(o, weight, dy, d_o, dweight, *, eps=RMSNORM_EPS, stream=
                                        _ptr(dweight, "dweight", torch.float32, (H * Dv,)), _stream(stream))
     _check("carve_rmsnorm_bwd_noalloc", st)
     return d_o, dweight
+
+
+# ---- the gated delta rule and the norms around a block ------------------------
+
+
+def _same_device(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} is on {t.device}, expected {device}")
+
+
+def _on_stream(call, device, stream):
+    """call(stream handle) with the tensors' device current and, with ``stream``
+    given, that stream current too, so that what the call allocates belongs to it."""
+    if stream is None and device.index == torch.cuda.current_device():
+        return call(torch.cuda.current_stream().cuda_stream)
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    if stream.device != device:
+        raise ValueError(f"stream is on {stream.device}, the tensors are on {device}")
+    with torch.cuda.stream(stream):
+        return call(stream.cuda_stream)
+
+
+def _out(res, name, shape, dtype, device):
+    if res.get(name) is None:
+        res[name] = torch.empty(shape, dtype=dtype, device=device)
+    return _ptr(res[name], name, dtype, shape)
+
+
+def _scratch(workspace, nbytes, device):
+    if workspace is None:
+        workspace = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
+    return workspace, _ptr(workspace, "workspace"), workspace.numel() * workspace.element_size()
+
+
+@functools.lru_cache(maxsize=256)
+def _gdr_dims(B, T, N, Hk, Hv, Dk, Dv, dtype, scale, *strides):
+    """The C dims of a call (by sizes and strides alone), its chunk count and the
+    workspace sizes of its forward and backward."""
+    lib = load_library()
+    d = GdrDims(B, T, N, Hk, Hv, Dk, Dv, CARVE_BF16 if dtype == torch.bfloat16 else CARVE_F32, scale, *strides)
+    r = ctypes.byref(d)
+    return d, int(lib.carve_gdr_chunk_count(r)), int(lib.carve_gdr_workspace_size(r, 0)), int(lib.carve_gdr_workspace_size(r, 1))
+
+
+def _strides(t):
+    # (a dimension of one element may have any stride; none is taken)
+    return tuple(s if n > 1 else 0 for n, s in zip(t.shape[:3], t.stride()[:3]))
+
+
+def _gdr_call(q, k, v, g, beta, scale, offsets):
+    """Checks what every entry point takes; returns (dims, chunks, workspace sizes,
+    sequences, the pointers of q, k, v, g, beta)."""
+    for name, t, dims in (("q", q, 4), ("k", k, 4), ("v", v, 4), ("g", g, 3), ("beta", beta, 3)):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise TypeError(f"{name} must be a GPU tensor")
+        if t.dim() != dims:
+            raise ValueError(f"{name} has {t.dim()} dimensions, expected {dims}")
+    dt, device = q.dtype, q.device
+    if dt not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"q must be bfloat16 or float32, got {dt}")
+    B, T, Hk, Dk = q.shape
+    Hv, Dv = v.shape[2:]
+    for name, t, shape in (("k", k, (B, T, Hk, Dk)), ("v", v, (B, T, Hv, Dv))):
+        if t.dtype != dt:
+            raise TypeError(f"{name} must be {dt}, got {t.dtype}")
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+    for name, t in (("q", q), ("k", k), ("v", v)):
+        if t.stride(3) != 1 and t.shape[3] > 1:
+            raise ValueError(f"{name} must be contiguous in its last dimension")
+    _same_device(device, k=k, v=v, g=g, beta=beta, offsets=offsets)
+    seqs = B
+    if offsets is not None:
+        if offsets.dim() != 1 or offsets.numel() < 2:
+            raise ValueError("offsets must be one-dimensional, the number of sequences and one")
+        seqs = offsets.numel() - 1
+    if scale is None:
+        scale = Dk ** -0.5
+    dims = _gdr_dims(B, T, seqs if offsets is not None else 0, Hk, Hv, Dk, Dv, dt, float(scale), *_strides(q),
+                     *_strides(k), *_strides(v))
+    ptrs = (q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(g, "g", torch.float32, (B, T, Hv)),
+            _ptr(beta, "beta", dt, (B, T, Hv)))
+    return dims, seqs, ptrs
+
+
+def gdr_chunk_fwd(q, k, v, g, beta, S0=None, *, scale=None, offsets=None, want_chunks=True, want_state=True, out=None,
+                  workspace=None, stream=None):
+    """Forward of the gated delta rule with a scalar decay, in chunks of 64 tokens:
+
+        S~ = e^g_t S;  u_t = beta_t (v_t - S~ k_t);  S = S~ + u_t k_t^T;  o_t = scale S q_t
+
+    q, k [B,T,Hk,Dk], v [B,T,Hv,Dv] (last dimension contiguous, any strides that are
+    multiples of 16 bytes), g [B,T,Hv] f32 (<= 0), beta [B,T,Hv]; value head h reads
+    key head h // (Hv // Hk); S0 [B,Hv,Dv,Dk] f32 or None; scale: Dk**-0.5 if None.
+    offsets (int32 [n + 1]): the T rows of B = 1 hold n packed sequences, rows
+    offsets[i] to offsets[i + 1] each, and states are [n,Hv,Dv,Dk]; rows of no
+    sequence are left as they were in a given ``out["o"]``.
+    Returns (o, S_T, S_chunks); S_chunks is what ``gdr_chunk_bwd`` needs.  ``out`` may
+    hold preallocated {"o", "S_T", "S_chunks"}.
+    """
+    lib = load_library()
+    (dims, chunks, ws_bytes, _), seqs, ptrs = _gdr_call(q, k, v, g, beta, scale, offsets)
+    B, T, Hv, Dv = v.shape
+    Dk, dt, f32, dev = q.shape[3], q.dtype, torch.float32, q.device
+    res = dict(out or {})
+    _same_device(dev, S0=S0, workspace=workspace, **res)
+
+    def call(s):
+        o = _out(res, "o", (B, T, Hv, Dv), dt, dev)
+        S_T = _out(res, "S_T", (seqs, Hv, Dv, Dk), f32, dev) if want_state or res.get("S_T") is not None else None
+        S_c = _out(res, "S_chunks", (chunks, Hv, Dv, Dk), f32, dev) if want_chunks or res.get("S_chunks") is not None else None
+        ws, ws_ptr, ws_len = _scratch(workspace, ws_bytes, dev)
+        return lib.carve_gdr_chunk_fwd(
+            ctypes.byref(dims), *ptrs, _ptr(S0, "S0", f32, (seqs, Hv, Dv, Dk)), _ptr(offsets, "offsets", torch.int32),
+            o, S_T, S_c, ws_ptr, ws_len, s)
+
+    _check("carve_gdr_chunk_fwd", _on_stream(call, dev, stream))
+    return res["o"], res.get("S_T"), res.get("S_chunks")
+
+
+def gdr_chunk_bwd(q, k, v, g, beta, S_chunks, dO, dS_T=None, *, scale=None, offsets=None, want_dS0=True, out=None,
+                  workspace=None, stream=None):
+    """Backward of ``gdr_chunk_fwd`` for loss <dO, o> + <dS_T, S_T>: a dict with dq,
+    dk, dv, dg (f32), dbeta and, with want_dS0, dS0.  dq and dk are sums over the
+    value heads of a key head."""
+    lib = load_library()
+    (dims, chunks, _, ws_bytes), seqs, ptrs = _gdr_call(q, k, v, g, beta, scale, offsets)
+    B, T, Hv, Dv = v.shape
+    Hk, Dk = q.shape[2:]
+    dt, f32, dev = q.dtype, torch.float32, q.device
+    res = dict(out or {})
+    _same_device(dev, S_chunks=S_chunks, dO=dO, dS_T=dS_T, workspace=workspace, **res)
+
+    def call(s):
+        outs = [_out(res, name, shape, t, dev)
+                for name, shape, t in (("dq", (B, T, Hk, Dk), dt), ("dk", (B, T, Hk, Dk), dt), ("dv", (B, T, Hv, Dv), dt),
+                                       ("dg", (B, T, Hv), f32), ("dbeta", (B, T, Hv), dt))]
+        dS0 = _out(res, "dS0", (seqs, Hv, Dv, Dk), f32, dev) if want_dS0 or res.get("dS0") is not None else None
+        ws, ws_ptr, ws_len = _scratch(workspace, ws_bytes, dev)
+        return lib.carve_gdr_chunk_bwd(
+            ctypes.byref(dims), *ptrs, _ptr(S_chunks, "S_chunks", f32, (chunks, Hv, Dv, Dk)),
+            _ptr(offsets, "offsets", torch.int32), _ptr(dO, "dO", dt, (B, T, Hv, Dv)),
+            _ptr(dS_T, "dS_T", f32, (seqs, Hv, Dv, Dk)), *outs, dS0, ws_ptr, ws_len, s)
+
+    _check("carve_gdr_chunk_bwd", _on_stream(call, dev, stream))
+    return res
+
+
+def gdr_step(q, k, v, g, beta, state, slots=None, *, scale=None, out=None, stream=None):
+    """The gated delta rule token by token, for decoding: T tokens (one, or a few
+    drafted ones) for each of B sequences, whose states in the pool ``state``
+    [pool,Hv,Dv,Dk] f32 are updated in place.  Sequence b's state is
+    state[slots[b]] (int32 [B]), or state[b] without slots.  A slot outside the
+    pool (-1) marks a padding entry, whose output rows are left as they were.  No
+    slot may appear twice.  The other arguments are those of ``gdr_chunk_fwd``.
+    Returns o [B,T,Hv,Dv] (``out`` if given)."""
+    lib = load_library()
+    (dims, *_), _, ptrs = _gdr_call(q, k, v, g, beta, scale, None)
+    B, T, Hv, Dv = v.shape
+    dt, dev = q.dtype, q.device
+    if not isinstance(state, torch.Tensor) or state.dim() != 4:
+        raise ValueError("state must be [pool, Hv, Dv, Dk]")
+    pool = state.shape[0]
+    _same_device(dev, state=state, slots=slots, out=out)
+    res = {"o": out}
+
+    def call(s):
+        o = _out(res, "o", (B, T, Hv, Dv), dt, dev)
+        return lib.carve_gdr_step(ctypes.byref(dims), *ptrs, _ptr(slots, "slots", torch.int32, (B,)), pool,
+                                  _ptr(state, "state", torch.float32, (pool, Hv, Dv, q.shape[3])), o, s)
+
+    _check("carve_gdr_step", _on_stream(call, dev, stream))
+    return res["o"]
+
+
+GATE_ACTS = {"silu": 1, "sigmoid": 2}
+
+
+@functools.lru_cache(maxsize=256)
+def _block_norm_dims(rows, N, groups, dtype, act, eps, alpha, *strides):
+    d = BlockNormDims(rows, N, groups, CARVE_BF16 if dtype == torch.bfloat16 else CARVE_F32, act, eps, alpha, *strides)
+    return d, int(load_library().carve_block_norm_workspace_size(ctypes.byref(d)))
+
+
+def _rows(t, name, like=None):
+    """t as [rows, N] without a copy, and its row stride."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a GPU tensor")
+    if like is not None:
+        if t.dtype != like.dtype:
+            raise TypeError(f"{name} must be {like.dtype}, got {t.dtype}")
+        if t.shape != like.shape:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(like.shape)}")
+        if t.device != like.device:
+            raise ValueError(f"{name} is on {t.device}, expected {like.device}")
+    if t.dim() < 1 or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name} must be contiguous in its last dimension")
+    if t.dim() != 2:
+        try:
+            t = t.view(-1, t.shape[-1]) if t.numel() else t.reshape(0, t.shape[-1])
+        except RuntimeError:
+            raise ValueError(f"{name}'s rows must have one stride") from None
+    return t, (t.stride(0) if t.shape[0] > 1 else 0)
+
+
+def _block_norm_call(y, weight, groups, gate, gate_act, residual, alpha, scale, next_weight, eps):
+    yr, ys = _rows(y, "y")
+    if y.dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"y must be bfloat16 or float32, got {y.dtype}")
+    if gate is not None and gate_act not in GATE_ACTS:
+        raise ValueError(f"gate_act must be one of {sorted(GATE_ACTS)}, got {gate_act!r}")
+    zr, zs = (None, 0) if gate is None else _rows(gate, "gate", y)
+    rr, rs = (None, 0) if residual is None else _rows(residual, "residual", y)
+    _same_device(y.device, weight=weight, scale=scale, next_weight=next_weight)
+    rows, N = yr.shape
+    dims, ws_bytes = _block_norm_dims(rows, N, int(groups), y.dtype, GATE_ACTS[gate_act] if gate is not None else 0,
+                                      float(eps), float(alpha), ys, zs, rs)
+    ptrs = (yr.data_ptr(), _ptr(weight, "weight", torch.float32, (N,)), None if gate is None else zr.data_ptr(),
+            None if residual is None else rr.data_ptr(), _ptr(scale, "scale", torch.float32, (N,)),
+            _ptr(next_weight, "next_weight", torch.float32, (N,)))
+    if weight is None:
+        raise TypeError("weight must be a GPU tensor")
+    return dims, ws_bytes, ptrs
+
+
+def block_norm_fwd(y, weight, *, groups=1, gate=None, gate_act="silu", residual=None, alpha=1.0, scale=None,
+                   next_weight=None, eps=RMSNORM_EPS, out=None, stream=None):
+    """The norm after a block, its gate, its scaled addition to the residual stream
+    and the norm before the next block, in one pass over rows y [..., N]:
+
+        n = y / sqrt(mean(y^2) + eps) * weight      (mean over each of ``groups`` groups)
+        x = alpha * residual + scale * n * act(gate),   act: "silu" or "sigmoid"
+        h = x / sqrt(mean(x^2) + eps) * next_weight
+
+    gate, residual (shape and dtype of y), scale, next_weight (f32 [N]) may be left
+    out.  y, gate and residual may be slices of wider rows.  Returns (x, h), h None
+    without next_weight.  ``out`` may hold preallocated {"x", "h"}."""
+    lib = load_library()
+    dims, _, ptrs = _block_norm_call(y, weight, groups, gate, gate_act, residual, alpha, scale, next_weight, eps)
+    res = dict(out or {})
+    _same_device(y.device, **res)
+
+    def call(s):
+        x = _out(res, "x", tuple(y.shape), y.dtype, y.device)
+        h = _out(res, "h", tuple(y.shape), y.dtype, y.device) if next_weight is not None else _ptr(res.get("h"), "h")
+        return lib.carve_block_norm_fwd(ctypes.byref(dims), *ptrs, x, h, s)
+
+    _check("carve_block_norm_fwd", _on_stream(call, y.device, stream))
+    return res["x"], res.get("h")
+
+
+def block_norm_bwd(y, weight, dx, dh=None, *, groups=1, gate=None, gate_act="silu", residual=None, alpha=1.0, scale=None,
+                   next_weight=None, eps=RMSNORM_EPS, out=None, workspace=None, stream=None):
+    """Backward of ``block_norm_fwd`` for loss <dx, x> + <dh, h> (dx may be None where
+    dh is given): a dict with dy, dweight and, for each input given, dgate,
+    dresidual, dscale, dnext_weight."""
+    lib = load_library()
+    dims, ws_bytes, ptrs = _block_norm_call(y, weight, groups, gate, gate_act, residual, alpha, scale, next_weight, eps)
+    res = dict(out or {})
+    dev, shape, N, f32 = y.device, tuple(y.shape), y.shape[-1], torch.float32
+    _same_device(dev, dx=dx, dh=dh, workspace=workspace, **res)
+    wanted = [("dy", y, shape, y.dtype), ("dgate", gate, shape, y.dtype), ("dresidual", residual, shape, y.dtype),
+              ("dweight", weight, (N,), f32), ("dscale", scale, (N,), f32), ("dnext_weight", next_weight, (N,), f32)]
+
+    def call(s):
+        outs = [_out(res, name, sh, t, dev) if of is not None else _ptr(res.get(name), name) for name, of, sh, t in wanted]
+        ws, ws_ptr, ws_len = _scratch(workspace, ws_bytes, dev)
+        return lib.carve_block_norm_bwd(ctypes.byref(dims), *ptrs, _ptr(dx, "dx", y.dtype, shape),
+                                        _ptr(dh, "dh", y.dtype, shape), *outs, ws_ptr, ws_len, s)
+
+    _check("carve_block_norm_bwd", _on_stream(call, dev, stream))
+    return res

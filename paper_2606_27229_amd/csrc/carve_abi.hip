@@ -2,6 +2,7 @@
 // sizing, kernel selection and launch.  No allocation, no synchronisation.
 #include <stdint.h>
 
+#include "carve_gdr.h"
 #include "carve_kernels.h"
 
 using namespace carve;
@@ -572,6 +573,304 @@ int carve_rmsnorm_bwd(const carve_dims_t* d, const void* o, const float* weight,
                           stream, prof_mark);
   prof_mark(stream);
   return st;
+}
+
+}  // extern "C"
+
+// ---- the gated delta rule ----------------------------------------------------
+
+namespace {
+
+// largest offset + 1 of a strided [B, T, H, D] tensor, in bytes
+size_t span(long long sb, long long st, long long sh, int B, int T, int H, int D, size_t es) {
+  return ((size_t)(B - 1) * sb + (size_t)(T - 1) * st + (size_t)(H - 1) * sh + D) * es;
+}
+
+int check_gdr(const carve_gdr_dims_t* d) {
+  if (!d) return CARVE_ERR_NULL;
+  if (d->B <= 0 || d->T <= 0 || d->N < 0 || d->Hk <= 0 || d->Hv <= 0 || d->Dk <= 0 || d->Dv <= 0) return CARVE_ERR_SHAPE;
+  if (d->N > 0 && d->B != 1) return CARVE_ERR_SHAPE;
+  if (d->dtype != CARVE_F32 && d->dtype != CARVE_BF16) return CARVE_ERR_UNSUPPORTED;
+  if (d->Dk != 32 && d->Dk != 64 && d->Dk != 128) return CARVE_ERR_UNSUPPORTED;
+  if (d->Dv != 32 && d->Dv != 64 && d->Dv != 128 && d->Dv != 256) return CARVE_ERR_UNSUPPORTED;
+  if (d->Hv % d->Hk || d->Hv > 65535) return CARVE_ERR_UNSUPPORTED;
+  if (!(d->scale >= -3.0e38f && d->scale <= 3.0e38f)) return CARVE_ERR_ARG;
+  const long long strides[] = {d->q_batch, d->q_token, d->q_head, d->k_batch, d->k_token,
+                               d->k_head,  d->v_batch, d->v_token, d->v_head};
+  const long long vec = 16 / (long long)esize(d->dtype);
+  for (const long long s : strides) {
+    if (s < 0) return CARVE_ERR_ARG;
+    if (s % vec) return CARVE_ERR_ALIGN;
+  }
+  // (no tensor reaches 2^45 elements: the spans below stay within 64 bits)
+  const int counts[] = {d->B, d->T, d->Hk, d->B, d->T, d->Hk, d->B, d->T, d->Hv};
+  for (int i = 0; i < 9; ++i)
+    if ((double)strides[i] * (counts[i] - 1) >= 3.5e13) return CARVE_ERR_UNSUPPORTED;
+  // grids and row counts: B T rows, chunk slots and (sequence, head, slice) workgroups below 2^31
+  if ((long long)d->B * d->T >= (1LL << 31)) return CARVE_ERR_UNSUPPORTED;
+  if ((long long)d->B * ((d->T + kGdrC - 1) / kGdrC) + d->N >= (1LL << 31)) return CARVE_ERR_UNSUPPORTED;
+  const long long seqs = d->N ? d->N : d->B;
+  if (seqs * d->Hv * (d->Dv / 32) >= (1LL << 30)) return CARVE_ERR_UNSUPPORTED;
+  return CARVE_OK;
+}
+
+size_t gdr_chunks(const carve_gdr_dims_t* d) {
+  return d->N ? (size_t)(d->T / kGdrC) + d->N : (size_t)d->B * ((d->T + kGdrC - 1) / kGdrC);
+}
+size_t gdr_per(bool bwd) { return (size_t)(bwd ? 3 : 2) * kGdrImg + kGdrScal; }
+size_t gdr_state(const carve_gdr_dims_t* d) { return (size_t)d->Hv * d->Dv * d->Dk * 4; }   // bytes, all heads
+
+void gdr_args(GdrArgs& a, const carve_gdr_dims_t* d, const void* q, const void* k, const void* v, const float* g,
+              const void* beta, const int* offsets, void* ws, bool bwd) {
+  a = GdrArgs{};
+  a.q = q, a.k = k, a.v = v, a.g = g, a.beta = beta, a.offsets = offsets;
+  a.qs[0] = d->q_batch, a.qs[1] = d->q_token, a.qs[2] = d->q_head;
+  a.ks[0] = d->k_batch, a.ks[1] = d->k_token, a.ks[2] = d->k_head;
+  a.vs[0] = d->v_batch, a.vs[1] = d->v_token, a.vs[2] = d->v_head;
+  a.T = d->T, a.Hk = d->Hk, a.Hv = d->Hv, a.Dk = d->Dk, a.Dv = d->Dv;
+  a.nseq = d->N ? d->N : d->B;
+  a.nslots = (int)gdr_chunks(d);
+  a.scale = d->scale;
+  a.ws = static_cast<char*>(ws);
+  a.per = (int)gdr_per(bwd);
+}
+
+// the input ranges that every entry point has
+int gdr_inputs(const carve_gdr_dims_t* d, const void* q, const void* k, const void* v, const float* g,
+               const void* beta, Range* r) {
+  const size_t es = esize(d->dtype), rows = (size_t)d->B * d->T;
+  r[0] = {q, span(d->q_batch, d->q_token, d->q_head, d->B, d->T, d->Hk, d->Dk, es)};
+  r[1] = {k, span(d->k_batch, d->k_token, d->k_head, d->B, d->T, d->Hk, d->Dk, es)};
+  r[2] = {v, span(d->v_batch, d->v_token, d->v_head, d->B, d->T, d->Hv, d->Dv, es)};
+  r[3] = {g, rows * d->Hv * 4};
+  r[4] = {beta, rows * d->Hv * es};
+  return 5;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t carve_gdr_chunk_count(const carve_gdr_dims_t* d) { return check_gdr(d) == CARVE_OK ? gdr_chunks(d) : 0; }
+
+size_t carve_gdr_workspace_size(const carve_gdr_dims_t* d, int for_backward) {
+  if (check_gdr(d) != CARVE_OK) return 0;
+  const size_t n = gdr_chunks(d);
+  const size_t images = align256(n * d->Hv * gdr_per(for_backward != 0));
+  return for_backward ? images + n * gdr_state(d) : images;
+}
+
+int carve_gdr_chunk_fwd(const carve_gdr_dims_t* d, const void* q, const void* k, const void* v, const float* g,
+                  const void* beta, const float* S0, const int* offsets, void* o, float* S_T, float* S_chunks,
+                  void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  ProfClear pc;
+  int st = check_gdr(d);
+  if (st) return st;
+  if (!q || !k || !v || !g || !beta || !o || (d->N > 0 && !offsets)) return CARVE_ERR_NULL;
+  if (d->N == 0 && offsets) return CARVE_ERR_ARG;
+  const void* ptrs[] = {q, k, v, g, beta, S0, offsets, o, S_T, S_chunks, workspace};
+  for (const void* p : ptrs)
+    if (p && !aligned16(p)) return CARVE_ERR_ALIGN;
+  const size_t need = carve_gdr_workspace_size(d, 0);
+  if (!workspace || workspace_bytes < need) return CARVE_ERR_WORKSPACE;
+  const size_t seqs = d->N ? d->N : d->B, state = gdr_state(d);
+  Range ins[7];
+  int nin = gdr_inputs(d, q, k, v, g, beta, ins);
+  ins[nin++] = {S0, seqs * state};
+  ins[nin++] = {offsets, (size_t)(d->N + 1) * 4};
+  const Range outs[] = {{o, (size_t)d->B * d->T * d->Hv * d->Dv * esize(d->dtype)},
+                        {S_T, seqs * state},
+                        {S_chunks, gdr_chunks(d) * state},
+                        {workspace, need}};
+  if (any_overlap(outs, 4, ins, nin)) return CARVE_ERR_UNSUPPORTED;
+  GdrArgs a;
+  gdr_args(a, d, q, k, v, g, beta, offsets, workspace, false);
+  a.S0 = S0, a.o = o, a.S_T = S_T, a.S_chunks = S_chunks;
+  prof_mark(stream);
+  return launch_gdr_fwd(a, d->dtype, stream, prof_mark);
+}
+
+int carve_gdr_chunk_bwd(const carve_gdr_dims_t* d, const void* q, const void* k, const void* v, const float* g,
+                  const void* beta, const float* S_chunks, const int* offsets, const void* dO, const float* dS_T,
+                  void* dq, void* dk, void* dv, float* dg, void* dbeta, float* dS0, void* workspace,
+                  size_t workspace_bytes, hipStream_t stream) {
+  ProfClear pc;
+  int st = check_gdr(d);
+  if (st) return st;
+  if (!q || !k || !v || !g || !beta || !S_chunks || !dO || !dq || !dk || !dv || !dg || !dbeta ||
+      (d->N > 0 && !offsets))
+    return CARVE_ERR_NULL;
+  if (d->N == 0 && offsets) return CARVE_ERR_ARG;
+  const void* ptrs[] = {q, k, v, g, beta, S_chunks, offsets, dO, dS_T, dq, dk, dv, dg, dbeta, dS0, workspace};
+  for (const void* p : ptrs)
+    if (p && !aligned16(p)) return CARVE_ERR_ALIGN;
+  const size_t need = carve_gdr_workspace_size(d, 1);
+  if (!workspace || workspace_bytes < need) return CARVE_ERR_WORKSPACE;
+  const size_t es = esize(d->dtype), rows = (size_t)d->B * d->T;
+  const size_t seqs = d->N ? d->N : d->B, state = gdr_state(d);
+  Range ins[9];
+  int nin = gdr_inputs(d, q, k, v, g, beta, ins);
+  ins[nin++] = {S_chunks, gdr_chunks(d) * state};
+  ins[nin++] = {offsets, (size_t)(d->N + 1) * 4};
+  ins[nin++] = {dO, rows * d->Hv * d->Dv * es};
+  ins[nin++] = {dS_T, seqs * state};
+  const Range outs[] = {{dq, rows * d->Hk * d->Dk * es}, {dk, rows * d->Hk * d->Dk * es},
+                        {dv, rows * d->Hv * d->Dv * es}, {dg, rows * d->Hv * 4},
+                        {dbeta, rows * d->Hv * es},      {dS0, seqs * state},
+                        {workspace, need}};
+  if (any_overlap(outs, 7, ins, nin)) return CARVE_ERR_UNSUPPORTED;
+  GdrArgs a;
+  gdr_args(a, d, q, k, v, g, beta, offsets, workspace, true);
+  a.S_chunks = const_cast<float*>(S_chunks);   // (read only)
+  a.dS_chunks = reinterpret_cast<float*>(a.ws + align256(gdr_chunks(d) * d->Hv * gdr_per(true)));
+  a.dO = dO, a.dS_T = dS_T, a.dq = dq, a.dk = dk, a.dv = dv, a.dg = dg, a.dbeta = dbeta, a.dS0 = dS0;
+  prof_mark(stream);
+  return launch_gdr_bwd(a, d->dtype, stream, prof_mark);
+}
+
+int carve_gdr_step(const carve_gdr_dims_t* d, const void* q, const void* k, const void* v, const float* g,
+                   const void* beta, const int* slots, int pool, float* state, void* o, hipStream_t stream) {
+  ProfClear pc;
+  int st = check_gdr(d);
+  if (st) return st;
+  if (d->N != 0 || pool <= 0 || (!slots && pool < d->B)) return CARVE_ERR_SHAPE;
+  if (d->B > 65535) return CARVE_ERR_UNSUPPORTED;
+  if (!q || !k || !v || !g || !beta || !state || !o) return CARVE_ERR_NULL;
+  const void* ptrs[] = {q, k, v, g, beta, state, o};
+  for (const void* p : ptrs)
+    if (!aligned16(p)) return CARVE_ERR_ALIGN;
+  if (slots && ((uintptr_t)slots & 3u)) return CARVE_ERR_ALIGN;
+  Range ins[6];
+  int nin = gdr_inputs(d, q, k, v, g, beta, ins);
+  ins[nin++] = {slots, (size_t)d->B * 4};
+  const Range outs[] = {{o, (size_t)d->B * d->T * d->Hv * d->Dv * esize(d->dtype)}, {state, (size_t)pool * gdr_state(d)}};
+  if (any_overlap(outs, 2, ins, nin)) return CARVE_ERR_UNSUPPORTED;
+  GdrStepArgs a = {};
+  a.q = q, a.k = k, a.v = v, a.g = g, a.beta = beta, a.slots = slots, a.state = state, a.o = o;
+  a.qs[0] = d->q_batch, a.qs[1] = d->q_token, a.qs[2] = d->q_head;
+  a.ks[0] = d->k_batch, a.ks[1] = d->k_token, a.ks[2] = d->k_head;
+  a.vs[0] = d->v_batch, a.vs[1] = d->v_token, a.vs[2] = d->v_head;
+  a.B = d->B, a.T = d->T, a.Hk = d->Hk, a.Hv = d->Hv, a.Dv = d->Dv, a.nslots = pool, a.scale = d->scale;
+  prof_mark(stream);
+  st = launch_gdr_step(a, d->Dk, d->dtype, stream);
+  prof_mark(stream);
+  return st;
+}
+
+}  // extern "C"
+
+// ---- the norms around a block ---------------------------------------------------
+
+namespace {
+
+int check_block_norm(const carve_block_norm_dims_t* d) {
+  if (!d) return CARVE_ERR_NULL;
+  if (d->rows <= 0 || d->N <= 0 || d->groups <= 0 || d->N % d->groups) return CARVE_ERR_SHAPE;
+  if (d->dtype != CARVE_F32 && d->dtype != CARVE_BF16) return CARVE_ERR_UNSUPPORTED;
+  const int vec = 16 / (int)esize(d->dtype);
+  if (d->N % vec || d->N > kBlockNormMaxN || d->rows >= (1LL << 31)) return CARVE_ERR_UNSUPPORTED;
+  const int size = d->N / d->groups;
+  if (d->groups > 1 && (size % vec || size / vec > 64 || ((size / vec) & (size / vec - 1)))) return CARVE_ERR_UNSUPPORTED;
+  if (!eps_ok(d->eps)) return CARVE_ERR_ARG;
+  return CARVE_OK;
+}
+
+// what the forward and the backward check alike; fills the arguments and the input ranges
+int block_norm_args(const carve_block_norm_dims_t* d, const void* y, const float* weight, const void* gate,
+                    const void* residual, const float* scale, const float* next_weight, BlockNormArgs& a, Range* ins) {
+  if (!y || !weight) return CARVE_ERR_NULL;
+  if (gate && d->gate_act != CARVE_GATE_SILU && d->gate_act != CARVE_GATE_SIGMOID) return CARVE_ERR_ARG;
+  if (residual && !(d->alpha >= -3.0e38f && d->alpha <= 3.0e38f)) return CARVE_ERR_ARG;
+  const void* ptrs[] = {y, weight, gate, residual, scale, next_weight};
+  for (const void* p : ptrs)
+    if (p && !aligned16(p)) return CARVE_ERR_ALIGN;
+  const size_t es = esize(d->dtype);
+  const long long vec = 16 / (long long)es;
+  const struct {
+    const void* p;
+    long long stride;
+  } rows[] = {{y, d->y_stride}, {gate, d->gate_stride}, {residual, d->residual_stride}};
+  for (int i = 0; i < 3; ++i) {
+    ins[i] = {nullptr, 0};
+    if (!rows[i].p) continue;
+    if (rows[i].stride < 0) return CARVE_ERR_ARG;
+    if (rows[i].stride % vec) return CARVE_ERR_ALIGN;
+    if ((double)rows[i].stride * (d->rows - 1) >= 3.5e13) return CARVE_ERR_UNSUPPORTED;   // (no tensor reaches that)
+    ins[i] = {rows[i].p, ((size_t)(d->rows - 1) * rows[i].stride + d->N) * es};
+  }
+  ins[3] = {weight, (size_t)d->N * 4};
+  ins[4] = {scale, (size_t)d->N * 4};
+  ins[5] = {next_weight, (size_t)d->N * 4};
+  a = BlockNormArgs{};
+  a.y = y, a.gate = gate, a.residual = residual, a.weight = weight, a.scale = scale, a.next_weight = next_weight;
+  a.rows = d->rows, a.N = d->N, a.groups = d->groups, a.lanes = (int)(d->N / d->groups / vec), a.act = d->gate_act;
+  a.y_stride = d->y_stride, a.gate_stride = d->gate_stride, a.residual_stride = d->residual_stride;
+  a.eps = d->eps, a.alpha = d->alpha;
+  return CARVE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t carve_block_norm_workspace_size(const carve_block_norm_dims_t* d) {
+  if (check_block_norm(d) != CARVE_OK) return 0;
+  return align256((size_t)block_norm_groups(d->rows, d->N, d->dtype) * 3 * d->N * 4);
+}
+
+int carve_block_norm_fwd(const carve_block_norm_dims_t* d, const void* y, const float* weight, const void* gate,
+                         const void* residual, const float* scale, const float* next_weight, void* x, void* h,
+                         hipStream_t stream) {
+  ProfClear pc;
+  int st = check_block_norm(d);
+  if (st) return st;
+  if (!x) return CARVE_ERR_NULL;
+  if (!next_weight != !h) return CARVE_ERR_ARG;
+  BlockNormArgs a;
+  Range ins[6];
+  st = block_norm_args(d, y, weight, gate, residual, scale, next_weight, a, ins);
+  if (st) return st;
+  if (!aligned16(x) || !aligned16(h)) return CARVE_ERR_ALIGN;
+  const size_t nx = (size_t)d->rows * d->N * esize(d->dtype);
+  const Range outs[] = {{x, nx}, {h, nx}};
+  if (any_overlap(outs, 2, ins, 6)) return CARVE_ERR_UNSUPPORTED;
+  a.x = x, a.h = h;
+  prof_mark(stream);
+  st = launch_block_norm_fwd(a, d->dtype, stream);
+  prof_mark(stream);
+  return st;
+}
+
+int carve_block_norm_bwd(const carve_block_norm_dims_t* d, const void* y, const float* weight, const void* gate,
+                         const void* residual, const float* scale, const float* next_weight, const void* dx,
+                         const void* dh, void* dy, void* dgate, void* dresidual, float* dweight, float* dscale,
+                         float* dnext_weight, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  ProfClear pc;
+  int st = check_block_norm(d);
+  if (st) return st;
+  if (!dy || !dweight || (!dx && !dh)) return CARVE_ERR_NULL;
+  if (!next_weight != !dh || !next_weight != !dnext_weight || !gate != !dgate || !residual != !dresidual ||
+      !scale != !dscale)
+    return CARVE_ERR_ARG;
+  BlockNormArgs a;
+  Range ins[8];
+  st = block_norm_args(d, y, weight, gate, residual, scale, next_weight, a, ins);
+  if (st) return st;
+  const void* ptrs[] = {dx, dh, dy, dgate, dresidual, dweight, dscale, dnext_weight, workspace};
+  for (const void* p : ptrs)
+    if (!aligned16(p)) return CARVE_ERR_ALIGN;
+  const size_t need = carve_block_norm_workspace_size(d);
+  if (!workspace || workspace_bytes < need) return CARVE_ERR_WORKSPACE;
+  const size_t nx = (size_t)d->rows * d->N * esize(d->dtype), np = (size_t)d->N * 4;
+  ins[6] = {dx, nx};
+  ins[7] = {dh, nx};
+  const Range outs[] = {{dy, nx}, {dgate, nx}, {dresidual, nx}, {dweight, np}, {dscale, np}, {dnext_weight, np}, {workspace, need}};
+  if (any_overlap(outs, 7, ins, 8)) return CARVE_ERR_UNSUPPORTED;
+  a.dx = dx, a.dh = dh, a.dy = dy, a.dgate = dgate, a.dresidual = dresidual;
+  a.dweight = dweight, a.dscale = dscale, a.dnext_weight = dnext_weight;
+  a.partial = static_cast<float*>(workspace);
+  prof_mark(stream);
+  return launch_block_norm_bwd(a, d->dtype, stream, prof_mark);
 }
 
 }  // extern "C"

@@ -1,0 +1,412 @@
+// carve_block_norm.hip -- the norms before and after a block, fused with the
+// block's gate and its scaled addition to the residual stream (rows of N):
+//   n = y rsqrt(mean_group(y^2) + eps) weight        (groups of N / groups values)
+//   t = n act(gate),  x = alpha residual + scale t
+//   h = x rsqrt(mean(x^2) + eps) next_weight         (the next block's input)
+// and backward for loss <dx, x> + <dh, h>, with everything formed again from y,
+// gate and residual:
+//   dX = dx + r2 (m - x r2^2 mean(m x)),  m = dh next_weight
+//   dresidual = alpha dX,  dt = scale dX,  dgate = dt n act'(gate),  dn = dt act(gate)
+//   dy = r1 (dn weight - y r1 mean_group(dn weight y r1))
+//   dweight = sum dn y r1,  dscale = sum dX t,  dnext_weight = sum dh x r2
+//
+// Bound by HBM: every row tensor is read once and written once.  NT threads (one
+// wave, or four) hold a row in registers, NCH 16-byte chunks each; sums run over a
+// group's lanes by DPP and over the waves through LDS.  Statistics, x and the
+// gradients are f32 until they are stored; h comes from the unrounded x, and so
+// does the backward, which forms x again instead of reading the rounded one.
+#include "carve_kernels.h"
+
+namespace carve {
+namespace {
+
+template <typename T>
+struct Vec;
+template <>
+struct Vec<bf16_t> {
+  static constexpr int n = 8;
+};
+template <>
+struct Vec<float> {
+  static constexpr int n = 4;
+};
+
+template <typename T>
+__device__ __forceinline__ void ld_vec(const T* p, float* f) {
+  Chunk16<T>::unpack(*reinterpret_cast<const u32x4_t*>(p), f);
+}
+template <typename T>
+__device__ __forceinline__ void st_vec(T* p, const float* f) {
+  *reinterpret_cast<u32x4_t*>(p) = Chunk16<T>::pack(f);
+}
+__device__ __forceinline__ void ld_f32(const float* p, float* f, int n) {
+  for (int i = 0; i < n; i += 4) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(p + i);
+    for (int e = 0; e < 4; ++e) f[i + e] = v[e];
+  }
+}
+
+// sum over aligned groups of n lanes (n a power of two up to 64, uniform)
+__device__ __forceinline__ float lanes_sum(float x, int n) {
+  for (int m = 1; m < n; m <<= 1) x += __shfl_xor(x, m);
+  return x;
+}
+// sums over the row of two values at once, in every thread of the row
+template <int NT>
+__device__ __forceinline__ void row_sums(float& a, float& b, float* red) {
+  a = group_sum<64>(a);
+  b = group_sum<64>(b);
+  if constexpr (NT > 64) {
+    const int w = threadIdx.x >> 6;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) {
+      red[2 * w] = a;
+      red[2 * w + 1] = b;
+    }
+    __syncthreads();
+    a = red[0];
+    b = red[1];
+    for (int i = 1; i < NT / 64; ++i) {
+      a += red[2 * i];
+      b += red[2 * i + 1];
+    }
+  }
+}
+
+__device__ __forceinline__ float sigmoid_x(float z) { return 1.0f / (1.0f + expf(-z)); }
+
+// r1 of every chunk: over the whole row, or over the lanes of the chunk's group
+template <typename T, int NT, int NCH>
+__device__ __forceinline__ void group_rstd(const float (*y)[Vec<T>::n], float* r1, const BlockNormArgs& a, float* red) {
+  constexpr int V = Vec<T>::n;
+  float part[NCH];
+#pragma unroll
+  for (int ch = 0; ch < NCH; ++ch) {
+    part[ch] = 0.0f;
+#pragma unroll
+    for (int e = 0; e < V; ++e) part[ch] += y[ch][e] * y[ch][e];
+  }
+  const float inv = 1.0f / (float)(a.N / a.groups);
+  if (a.groups == 1) {
+    float s = 0.0f, z = 0.0f;
+#pragma unroll
+    for (int ch = 0; ch < NCH; ++ch) s += part[ch];
+    row_sums<NT>(s, z, red);
+#pragma unroll
+    for (int ch = 0; ch < NCH; ++ch) r1[ch] = 1.0f / sqrtf(s * inv + a.eps);
+  } else {
+#pragma unroll
+    for (int ch = 0; ch < NCH; ++ch) r1[ch] = 1.0f / sqrtf(lanes_sum(part[ch], a.lanes) * inv + a.eps);
+  }
+}
+
+template <typename T, int NT, int NCH>
+__global__ void __launch_bounds__(256) carve_block_norm_fwd_kernel(BlockNormArgs a) {
+  constexpr int V = Vec<T>::n;
+  __shared__ float red[8];
+  const int tid = threadIdx.x % NT;
+  const long long row = (long long)blockIdx.x * (256 / NT) + threadIdx.x / NT;
+  if (row >= a.rows) return;   // (whole waves; with NT = 256 there is no such row)
+  const T* yp = reinterpret_cast<const T*>(a.y) + row * a.y_stride;
+  const T* zp = reinterpret_cast<const T*>(a.gate) + row * a.gate_stride;
+  const T* rp = reinterpret_cast<const T*>(a.residual) + row * a.residual_stride;
+  float y[NCH][V], z[NCH][V], rs[NCH][V];
+#pragma unroll
+  for (int ch = 0; ch < NCH; ++ch) {
+    const int c0 = (ch * NT + tid) * V;
+#pragma unroll
+    for (int e = 0; e < V; ++e) y[ch][e] = z[ch][e] = rs[ch][e] = 0.0f;
+    if (c0 < a.N) {
+      ld_vec(yp + c0, y[ch]);
+      if (a.gate) ld_vec(zp + c0, z[ch]);
+      if (a.residual) ld_vec(rp + c0, rs[ch]);
+    }
+  }
+  float r1[NCH];
+  group_rstd<T, NT, NCH>(y, r1, a, red);
+  float ss = 0.0f, none = 0.0f;
+#pragma unroll
+  for (int ch = 0; ch < NCH; ++ch) {
+    const int c0 = (ch * NT + tid) * V;
+    if (c0 >= a.N) continue;
+    float wt[V], sc[V];
+    ld_f32(a.weight + c0, wt, V);
+    if (a.scale) ld_f32(a.scale + c0, sc, V);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      float t = y[ch][e] * r1[ch] * wt[e];
+      if (a.gate) t *= a.act == CARVE_GATE_SILU ? z[ch][e] * sigmoid_x(z[ch][e]) : sigmoid_x(z[ch][e]);
+      if (a.scale) t *= sc[e];
+      y[ch][e] = a.residual ? a.alpha * rs[ch][e] + t : t;
+      ss += y[ch][e] * y[ch][e];
+    }
+    st_vec(reinterpret_cast<T*>(a.x) + row * a.N + c0, y[ch]);
+  }
+  if (!a.next_weight) return;   // (uniform)
+  row_sums<NT>(ss, none, red);
+  const float r2 = 1.0f / sqrtf(ss / (float)a.N + a.eps);
+#pragma unroll
+  for (int ch = 0; ch < NCH; ++ch) {
+    const int c0 = (ch * NT + tid) * V;
+    if (c0 >= a.N) continue;
+    float wt[V];
+    ld_f32(a.next_weight + c0, wt, V);
+#pragma unroll
+    for (int e = 0; e < V; ++e) y[ch][e] *= r2 * wt[e];
+    st_vec(reinterpret_cast<T*>(a.h) + row * a.N + c0, y[ch]);
+  }
+}
+
+// Workgroups take rows in turn and keep their share of the parameter gradients in
+// registers; their partial rows, [group][3][N] (dweight, dscale, dnext_weight), are
+// summed in order by the second launch, so reruns are bitwise identical.
+template <typename T, int NT, int NCH>
+__global__ void __launch_bounds__(256) carve_block_norm_bwd_kernel(BlockNormArgs a) {
+  constexpr int V = Vec<T>::n;
+  __shared__ float red[8];
+  extern __shared__ __attribute__((aligned(16))) float sacc[];   // NT = 64: [3][4][N] in turn
+  const int tid = threadIdx.x % NT, rw = threadIdx.x / NT;
+  float aw[NCH][V], as[NCH][V], an[NCH][V];
+#pragma unroll
+  for (int ch = 0; ch < NCH; ++ch)
+#pragma unroll
+    for (int e = 0; e < V; ++e) aw[ch][e] = as[ch][e] = an[ch][e] = 0.0f;
+  const float invN = 1.0f / (float)a.N, invG = 1.0f / (float)(a.N / a.groups);
+  for (long long row = (long long)blockIdx.x * (256 / NT) + rw; row < a.rows; row += (long long)gridDim.x * (256 / NT)) {
+    const T* yp = reinterpret_cast<const T*>(a.y) + row * a.y_stride;
+    const T* zp = reinterpret_cast<const T*>(a.gate) + row * a.gate_stride;
+    const T* rp = reinterpret_cast<const T*>(a.residual) + row * a.residual_stride;
+    float y[NCH][V], z[NCH][V], x[NCH][V], dX[NCH][V], dh[NCH][V];
+#pragma unroll
+    for (int ch = 0; ch < NCH; ++ch) {
+      const int c0 = (ch * NT + tid) * V;
+#pragma unroll
+      for (int e = 0; e < V; ++e) y[ch][e] = z[ch][e] = x[ch][e] = dX[ch][e] = dh[ch][e] = 0.0f;
+      if (c0 < a.N) {
+        ld_vec(yp + c0, y[ch]);
+        if (a.gate) ld_vec(zp + c0, z[ch]);
+        if (a.residual && a.next_weight) ld_vec(rp + c0, x[ch]);
+        if (a.dx) ld_vec(reinterpret_cast<const T*>(a.dx) + row * a.N + c0, dX[ch]);
+        if (a.dh) ld_vec(reinterpret_cast<const T*>(a.dh) + row * a.N + c0, dh[ch]);
+      }
+    }
+    float r1[NCH];
+    group_rstd<T, NT, NCH>(y, r1, a, red);
+    // through the next block's norm
+    if (a.next_weight) {
+      float ss = 0.0f, mx = 0.0f;
+#pragma unroll
+      for (int ch = 0; ch < NCH; ++ch) {
+        const int c0 = (ch * NT + tid) * V;
+        if (c0 >= a.N) continue;
+        float wt[V], sc[V], wn[V];
+        ld_f32(a.weight + c0, wt, V);
+        ld_f32(a.next_weight + c0, wn, V);
+        if (a.scale) ld_f32(a.scale + c0, sc, V);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          float t = y[ch][e] * r1[ch] * wt[e];
+          if (a.gate) t *= a.act == CARVE_GATE_SILU ? z[ch][e] * sigmoid_x(z[ch][e]) : sigmoid_x(z[ch][e]);
+          if (a.scale) t *= sc[e];
+          x[ch][e] = a.residual ? a.alpha * x[ch][e] + t : t;
+          ss += x[ch][e] * x[ch][e];
+          mx += dh[ch][e] * wn[e] * x[ch][e];
+        }
+      }
+      row_sums<NT>(ss, mx, red);
+      const float r2 = 1.0f / sqrtf(ss * invN + a.eps), m2 = r2 * r2 * (mx * invN);
+#pragma unroll
+      for (int ch = 0; ch < NCH; ++ch) {
+        const int c0 = (ch * NT + tid) * V;
+        if (c0 >= a.N) continue;
+        float wn[V];
+        ld_f32(a.next_weight + c0, wn, V);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          dX[ch][e] += r2 * (dh[ch][e] * wn[e] - x[ch][e] * m2);
+          an[ch][e] += dh[ch][e] * (x[ch][e] * r2);
+        }
+      }
+    }
+    float dot[NCH];
+#pragma unroll
+    for (int ch = 0; ch < NCH; ++ch) {
+      const int c0 = (ch * NT + tid) * V;
+      dot[ch] = 0.0f;
+      if (c0 >= a.N) continue;
+      if (a.dresidual) {
+        float o[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] = a.alpha * dX[ch][e];
+        st_vec(reinterpret_cast<T*>(a.dresidual) + row * a.N + c0, o);
+      }
+      float wt[V], sc[V];
+      ld_f32(a.weight + c0, wt, V);
+      if (a.scale) ld_f32(a.scale + c0, sc, V);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float yh = y[ch][e] * r1[ch], nv = yh * wt[e];
+        float act = 1.0f, slope = 0.0f;
+        if (a.gate) {
+          const float s = sigmoid_x(z[ch][e]);
+          act = a.act == CARVE_GATE_SILU ? z[ch][e] * s : s;
+          slope = a.act == CARVE_GATE_SILU ? s * (1.0f + z[ch][e] * (1.0f - s)) : s * (1.0f - s);
+        }
+        as[ch][e] += dX[ch][e] * (nv * act);
+        const float dt = a.scale ? dX[ch][e] * sc[e] : dX[ch][e];
+        z[ch][e] = dt * nv * slope;      // dgate
+        const float dn = dt * act;
+        aw[ch][e] += dn * yh;
+        dX[ch][e] = dn * wt[e];          // through the weight
+        dot[ch] += dX[ch][e] * yh;
+      }
+      if (a.dgate) st_vec(reinterpret_cast<T*>(a.dgate) + row * a.N + c0, z[ch]);
+    }
+    if (a.groups == 1) {
+      float s = 0.0f, none = 0.0f;
+#pragma unroll
+      for (int ch = 0; ch < NCH; ++ch) s += dot[ch];
+      row_sums<NT>(s, none, red);
+#pragma unroll
+      for (int ch = 0; ch < NCH; ++ch) dot[ch] = s * invG;
+    } else {
+#pragma unroll
+      for (int ch = 0; ch < NCH; ++ch) dot[ch] = lanes_sum(dot[ch], a.lanes) * invG;
+    }
+#pragma unroll
+    for (int ch = 0; ch < NCH; ++ch) {
+      const int c0 = (ch * NT + tid) * V;
+      if (c0 >= a.N) continue;
+#pragma unroll
+      for (int e = 0; e < V; ++e) dX[ch][e] = r1[ch] * (dX[ch][e] - y[ch][e] * r1[ch] * dot[ch]);
+      st_vec(reinterpret_cast<T*>(a.dy) + row * a.N + c0, dX[ch]);
+    }
+  }
+  // the workgroup's partial rows: one row of threads writes its share, four waves
+  // with a row each are summed in wave order
+  float* part = a.partial + (size_t)blockIdx.x * 3 * a.N;
+  const auto put = [&](const float (*acc)[V], int which) {
+    float* dst = part + (size_t)which * a.N;
+    if constexpr (NT == 256) {
+#pragma unroll
+      for (int ch = 0; ch < NCH; ++ch) {
+        const int c0 = (ch * NT + tid) * V;
+        if (c0 < a.N)
+#pragma unroll
+          for (int e = 0; e < V; ++e) dst[c0 + e] = acc[ch][e];
+      }
+    } else {
+      __syncthreads();
+#pragma unroll
+      for (int ch = 0; ch < NCH; ++ch) {
+        const int c0 = (ch * NT + tid) * V;
+        if (c0 < a.N)
+#pragma unroll
+          for (int e = 0; e < V; ++e) sacc[rw * a.N + c0 + e] = acc[ch][e];
+      }
+      __syncthreads();
+      for (int col = threadIdx.x; col < a.N; col += 256) {
+        float s = sacc[col];
+        for (int i = 1; i < 256 / NT; ++i) s += sacc[i * a.N + col];
+        dst[col] = s;
+      }
+    }
+  };
+  put(aw, 0);
+  if (a.dscale) put(as, 1);
+  if (a.dnext_weight) put(an, 2);
+}
+
+// dweight, dscale, dnext_weight: the partial rows of every workgroup in order, as
+// sixteen interleaved sums of a column that are added in order
+constexpr int kReduceRows = 16;
+__global__ void __launch_bounds__(64 * kReduceRows) carve_block_norm_reduce_kernel(BlockNormArgs a, int nparts) {
+  __shared__ float red[kReduceRows][64];
+  float* out = blockIdx.y == 0 ? a.dweight : blockIdx.y == 1 ? a.dscale : a.dnext_weight;
+  if (!out) return;   // (uniform)
+  const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
+  const int col = blockIdx.x * 64 + tx;
+  const size_t step = 3 * (size_t)a.N;
+  float s = 0.0f;
+  if (col < a.N) {
+    const float* p = a.partial + (size_t)blockIdx.y * a.N + col;
+    int i = ty;
+    for (; i + 3 * kReduceRows < nparts; i += 4 * kReduceRows) {
+      const float a0 = p[i * step], a1 = p[(i + kReduceRows) * step];
+      const float a2 = p[(i + 2 * kReduceRows) * step], a3 = p[(i + 3 * kReduceRows) * step];
+      s += a0;
+      s += a1;
+      s += a2;
+      s += a3;
+    }
+    for (; i < nparts; i += kReduceRows) s += p[i * step];
+  }
+  red[ty][tx] = s;
+  __syncthreads();
+  if (ty == 0 && col < a.N) {
+    float t = red[0][tx];
+    for (int y = 1; y < kReduceRows; ++y) t += red[y][tx];
+    out[col] = t;
+  }
+}
+
+// threads of a row and 16-byte chunks of a thread: one wave up to two chunks a lane
+template <typename T>
+bool wave_rows(int N) { return N <= 2 * 64 * Vec<T>::n; }
+
+template <typename T, int NT, int NCH>
+int fwd_t(const BlockNormArgs& a, hipStream_t s) {
+  const long long nwg = (a.rows + 256 / NT - 1) / (256 / NT);
+  hipLaunchKernelGGL((carve_block_norm_fwd_kernel<T, NT, NCH>), dim3((unsigned)nwg), dim3(256), 0, s, a);
+  return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
+}
+template <typename T, int NT, int NCH>
+int bwd_t(const BlockNormArgs& a, int nwg, hipStream_t s) {
+  const size_t lds = NT == 64 ? (size_t)4 * a.N * sizeof(float) : 0;
+  hipLaunchKernelGGL((carve_block_norm_bwd_kernel<T, NT, NCH>), dim3((unsigned)nwg), dim3(256), lds, s, a);
+  return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
+}
+template <typename T>
+int fwd_d(const BlockNormArgs& a, hipStream_t s) {
+  const int nch = (a.N + 256 * Vec<T>::n - 1) / (256 * Vec<T>::n);
+  if (wave_rows<T>(a.N)) return a.N <= 64 * Vec<T>::n ? fwd_t<T, 64, 1>(a, s) : fwd_t<T, 64, 2>(a, s);
+  if (nch <= 1) return fwd_t<T, 256, 1>(a, s);
+  if (nch <= 2) return fwd_t<T, 256, 2>(a, s);
+  if constexpr (sizeof(T) == 4)
+    if (nch > 4) return fwd_t<T, 256, 8>(a, s);
+  return fwd_t<T, 256, 4>(a, s);
+}
+template <typename T>
+int bwd_d(const BlockNormArgs& a, int nwg, hipStream_t s) {
+  const int nch = (a.N + 256 * Vec<T>::n - 1) / (256 * Vec<T>::n);
+  if (wave_rows<T>(a.N)) return a.N <= 64 * Vec<T>::n ? bwd_t<T, 64, 1>(a, nwg, s) : bwd_t<T, 64, 2>(a, nwg, s);
+  if (nch <= 1) return bwd_t<T, 256, 1>(a, nwg, s);
+  if (nch <= 2) return bwd_t<T, 256, 2>(a, nwg, s);
+  if constexpr (sizeof(T) == 4)
+    if (nch > 4) return bwd_t<T, 256, 8>(a, nwg, s);
+  return bwd_t<T, 256, 4>(a, nwg, s);
+}
+
+}  // namespace
+
+int block_norm_groups(long long rows, int N, int dtype) {
+  const bool wave = dtype == CARVE_BF16 ? wave_rows<bf16_t>(N) : wave_rows<float>(N);
+  const long long need = wave ? (rows + 3) / 4 : rows;
+  return (int)(need < kBlockNormGroups ? need : kBlockNormGroups);
+}
+
+int launch_block_norm_fwd(const BlockNormArgs& a, int dtype, hipStream_t s) {
+  return dtype == CARVE_BF16 ? fwd_d<bf16_t>(a, s) : fwd_d<float>(a, s);
+}
+
+int launch_block_norm_bwd(const BlockNormArgs& a, int dtype, hipStream_t s, void (*mark)(hipStream_t)) {
+  const int nwg = block_norm_groups(a.rows, a.N, dtype);
+  const int st = dtype == CARVE_BF16 ? bwd_d<bf16_t>(a, nwg, s) : bwd_d<float>(a, nwg, s);
+  if (st) return st;
+  mark(s);
+  hipLaunchKernelGGL(carve_block_norm_reduce_kernel, dim3((a.N + 63) / 64, 3), dim3(64 * kReduceRows), 0, s, a, nwg);
+  mark(s);
+  return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
+}
+
+}  // namespace carve

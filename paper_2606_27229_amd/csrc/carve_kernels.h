@@ -492,6 +492,24 @@ int launch_rmsnorm_fwd(const void* x, const float* wt, void* y, long rows, int N
 int launch_rmsnorm_bwd(const void* x, const float* wt, const void* dy, void* dx, float* partial, float* dw, long rows,
                        int N, float eps, int dtype, hipStream_t s, void (*mark)(hipStream_t));
 
+// The norms around a block (carve_block_norm.hip): rows of N values.  The backward's
+// workgroups (at most kBlockNormGroups) each write three f32 partial rows, summed in
+// order by a second launch; mark is called after each.
+constexpr int kBlockNormGroups = 1024;
+constexpr int kBlockNormMaxN = 8192;
+struct BlockNormArgs {
+  const void *y, *gate, *residual, *dx, *dh;
+  const float *weight, *scale, *next_weight;
+  void *x, *h, *dy, *dgate, *dresidual;
+  float *dweight, *dscale, *dnext_weight, *partial;
+  long long rows, y_stride, gate_stride, residual_stride;
+  int N, groups, lanes, act;   // lanes: 16-byte chunks of a group (groups > 1)
+  float eps, alpha;
+};
+int block_norm_groups(long long rows, int N, int dtype);
+int launch_block_norm_fwd(const BlockNormArgs& a, int dtype, hipStream_t s);
+int launch_block_norm_bwd(const BlockNormArgs& a, int dtype, hipStream_t s, void (*mark)(hipStream_t));
+
 // floats of one partial-gradient record: d[Ub; Uw] ([R][D] twice) or dVb, dVw ([D][R] twice)
 __host__ __device__ constexpr size_t part_floats(int R, int D) { return (size_t)2 * R * D; }
 
