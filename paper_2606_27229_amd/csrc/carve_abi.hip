@@ -606,6 +606,9 @@ int check_gdr(const carve_gdr_dims_t* d) {
   const int counts[] = {d->B, d->T, d->Hk, d->B, d->T, d->Hk, d->B, d->T, d->Hv};
   for (int i = 0; i < 9; ++i)
     if ((double)strides[i] * (counts[i] - 1) >= 3.5e13) return CARVE_ERR_UNSUPPORTED;
+  // (a chunk's rows are addressed with 32 bits)
+  for (const long long s : {d->q_token, d->k_token, d->v_token, (long long)d->Hv * d->Dv})
+    if (s >= (1LL << 24) / (long long)esize(d->dtype)) return CARVE_ERR_UNSUPPORTED;
   // grids and row counts: B T rows, chunk slots and (sequence, head, slice) workgroups below 2^31
   if ((long long)d->B * d->T >= (1LL << 31)) return CARVE_ERR_UNSUPPORTED;
   if ((long long)d->B * ((d->T + kGdrC - 1) / kGdrC) + d->N >= (1LL << 31)) return CARVE_ERR_UNSUPPORTED;
@@ -617,7 +620,11 @@ int check_gdr(const carve_gdr_dims_t* d) {
 size_t gdr_chunks(const carve_gdr_dims_t* d) {
   return d->N ? (size_t)(d->T / kGdrC) + d->N : (size_t)d->B * ((d->T + kGdrC - 1) / kGdrC);
 }
-size_t gdr_per(bool bwd) { return (size_t)(bwd ? 3 : 2) * kGdrImg + kGdrScal; }
+// workspace bytes of one (chunk slot, value head)
+size_t gdr_per(const carve_gdr_dims_t* d, bool bwd) {
+  if (d->dtype == CARVE_BF16) return bwd ? GdrWs<bf16_t>::bBytes : GdrWs<bf16_t>::fBytes;
+  return bwd ? GdrWs<float>::bBytes : GdrWs<float>::fBytes;
+}
 size_t gdr_state(const carve_gdr_dims_t* d) { return (size_t)d->Hv * d->Dv * d->Dk * 4; }   // bytes, all heads
 
 void gdr_args(GdrArgs& a, const carve_gdr_dims_t* d, const void* q, const void* k, const void* v, const float* g,
@@ -632,7 +639,7 @@ void gdr_args(GdrArgs& a, const carve_gdr_dims_t* d, const void* q, const void* 
   a.nslots = (int)gdr_chunks(d);
   a.scale = d->scale;
   a.ws = static_cast<char*>(ws);
-  a.per = (int)gdr_per(bwd);
+  a.per = (int)gdr_per(d, bwd);
 }
 
 // the input ranges that every entry point has
@@ -656,7 +663,7 @@ size_t carve_gdr_chunk_count(const carve_gdr_dims_t* d) { return check_gdr(d) ==
 size_t carve_gdr_workspace_size(const carve_gdr_dims_t* d, int for_backward) {
   if (check_gdr(d) != CARVE_OK) return 0;
   const size_t n = gdr_chunks(d);
-  const size_t images = align256(n * d->Hv * gdr_per(for_backward != 0));
+  const size_t images = align256(n * d->Hv * gdr_per(d, for_backward != 0));
   return for_backward ? images + n * gdr_state(d) : images;
 }
 
@@ -722,7 +729,7 @@ int carve_gdr_chunk_bwd(const carve_gdr_dims_t* d, const void* q, const void* k,
   GdrArgs a;
   gdr_args(a, d, q, k, v, g, beta, offsets, workspace, true);
   a.S_chunks = const_cast<float*>(S_chunks);   // (read only)
-  a.dS_chunks = reinterpret_cast<float*>(a.ws + align256(gdr_chunks(d) * d->Hv * gdr_per(true)));
+  a.dS_chunks = reinterpret_cast<float*>(a.ws + align256(gdr_chunks(d) * d->Hv * gdr_per(d, true)));
   a.dO = dO, a.dS_T = dS_T, a.dq = dq, a.dk = dk, a.dv = dv, a.dg = dg, a.dbeta = dbeta, a.dS0 = dS0;
   prof_mark(stream);
   return launch_gdr_bwd(a, d->dtype, stream, prof_mark);

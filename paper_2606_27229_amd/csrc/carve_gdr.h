@@ -10,11 +10,13 @@
 //
 // Precision.  Every decay factor scales rows of f32 results, never an operand, so
 // q, k, v and dO enter the matrix cores as they are.  With bf16 tokens the f32
-// intermediates (S, T, P, R, U and their adjoints) enter as the sum of two bf16
-// values (Fi): what that leaves out is 2^-18 of a value, and the product of two
-// such operands leaves out their low parts' product, 2^-18 again.  One bf16 value
-// would leave out 2^-9, which states and decay gradients (f32 outputs) do not
-// bear.  With f32 tokens every product is an f32 matrix-core product.
+// intermediates (S, T, R, U and their adjoints) enter as sums of bf16 values (Fi):
+// three of them hold 24 bits, as f32 does; what only reaches bf16 results is taken
+// as two (16 bits: what is left out is 2^-18 of a value, far below the rounding of
+// the result).  Products of two such operands leave out the pairs of pieces that lie
+// below the last piece.  One bf16 value would leave out 2^-9, which states and decay
+// gradients (f32 outputs) do not bear; two left 4e-6 of a state and 1e-5 of dg.  With
+// f32 tokens every product is an f32 matrix-core product.
 #pragma once
 #include "../../include/carve.h"
 #include "carve_dev.h"
@@ -22,8 +24,7 @@
 namespace carve {
 
 constexpr int kGdrC = 64;                 // tokens of a chunk
-constexpr int kGdrImg = 6 * 2 * 1024;     // bytes of a triangular operand image (6 fragments of 2 planes)
-constexpr int kGdrScal = 5 * kGdrC * 4;   // bytes of a chunk's scalars
+constexpr int kGdrScal = 2048;            // bytes of a chunk's scalars ([5][64] floats, to whole KB)
 constexpr float kGdrMinG = -1e4f;         // e^-1e4 is 0 in f32: a decay of -inf is taken as this
 
 struct GdrArgs {
@@ -90,52 +91,66 @@ template <typename T>
 struct Fr {
   typename Quad<T>::q a, b;
 };
-// An f32 intermediate as an operand: two bf16 values whose sum it is, or f32.
-template <typename T>
-struct Fi;
-template <>
-struct Fi<bf16_t> {
-  Fr<bf16_t> hi, lo;
+// An f32 intermediate as an operand: N bf16 values whose sum it is, or f32.
+template <typename T, int N>
+struct Fi {
+  Fr<T> x[sizeof(T) == 2 ? N : 1];
 };
-template <>
-struct Fi<float> {
-  Fr<float> x;
-};
+constexpr int kExact = 3, kNear = 2;   // pieces towards f32 and towards bf16 results
 
-__device__ __forceinline__ void split4(f32x4 x, bf16x4& hi, bf16x4& lo) {
-  hi = Quad<bf16_t>::cvt(x);
-  lo = Quad<bf16_t>::cvt(x - Quad<bf16_t>::f32(hi));
-}
-template <typename T>
-__device__ __forceinline__ Fi<T> to_fi(f32x4 a, f32x4 b) {
-  Fi<T> f;
+template <typename T, int N>
+__device__ __forceinline__ Fi<T, N> to_fi(f32x4 a, f32x4 b) {
+  Fi<T, N> f;
   if constexpr (sizeof(T) == 2) {
-    split4(a, f.hi.a, f.lo.a);
-    split4(b, f.hi.b, f.lo.b);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      f.x[i].a = Quad<T>::cvt(a);
+      f.x[i].b = Quad<T>::cvt(b);
+      if (i + 1 < N) {
+        a -= Quad<T>::f32(f.x[i].a);
+        b -= Quad<T>::f32(f.x[i].b);
+      }
+    }
   } else {
-    f.x.a = a;
-    f.x.b = b;
+    f.x[0].a = a;
+    f.x[0].b = b;
   }
   return f;
+}
+// the first M pieces
+template <int M, typename T, int N>
+__device__ __forceinline__ Fi<T, M> first(const Fi<T, N>& f) {
+  Fi<T, M> r;
+  if constexpr (sizeof(T) == 2)
+    for (int i = 0; i < M; ++i) r.x[i] = f.x[i];
+  else r.x[0] = f.x[0];
+  return r;
 }
 template <typename T>
 __device__ __forceinline__ f32x4 mma(Fr<T> a, Fr<T> b, f32x4 c) {
   return Quad<T>::mma32(a.a, a.b, b.a, b.b, c);
 }
-template <typename T>
-__device__ __forceinline__ f32x4 mma(const Fi<T>& a, Fr<T> b, f32x4 c) {
-  if constexpr (sizeof(T) == 2) return mma<T>(a.hi, b, mma<T>(a.lo, b, c));
-  else return mma<T>(a.x, b, c);
+// (small pieces first)
+template <typename T, int N>
+__device__ __forceinline__ f32x4 mma(const Fi<T, N>& a, Fr<T> b, f32x4 c) {
+#pragma unroll
+  for (int i = (sizeof(T) == 2 ? N : 1) - 1; i >= 0; --i) c = mma<T>(a.x[i], b, c);
+  return c;
 }
-template <typename T>
-__device__ __forceinline__ f32x4 mma(Fr<T> a, const Fi<T>& b, f32x4 c) {
-  if constexpr (sizeof(T) == 2) return mma<T>(a, b.hi, mma<T>(a, b.lo, c));
-  else return mma<T>(a, b.x, c);
+template <typename T, int N>
+__device__ __forceinline__ f32x4 mma(Fr<T> a, const Fi<T, N>& b, f32x4 c) {
+#pragma unroll
+  for (int i = (sizeof(T) == 2 ? N : 1) - 1; i >= 0; --i) c = mma<T>(a, b.x[i], c);
+  return c;
 }
-template <typename T>
-__device__ __forceinline__ f32x4 mma(const Fi<T>& a, const Fi<T>& b, f32x4 c) {
-  if constexpr (sizeof(T) == 2) return mma<T>(a.hi, b.hi, mma<T>(a.hi, b.lo, mma<T>(a.lo, b.hi, c)));
-  else return mma<T>(a.x, b.x, c);
+template <typename T, int N>
+__device__ __forceinline__ f32x4 mma(const Fi<T, N>& a, const Fi<T, N>& b, f32x4 c) {
+  constexpr int P = sizeof(T) == 2 ? N : 1;
+#pragma unroll
+  for (int s = P - 1; s >= 0; --s)
+#pragma unroll
+    for (int i = s; i >= 0; --i) c = mma<T>(a.x[i], b.x[s - i], c);
+  return c;
 }
 
 // eight consecutive elements of a token row (16-byte aligned), zeros if !ok
@@ -175,83 +190,138 @@ __device__ __forceinline__ Fr<T> ld_fr16(const T* p, bool ok) {
 // and 32 s + 16 + 4 g + e of row 16 i + c.  Lower: s <= i / 2; upper: s >= i / 2.
 __host__ __device__ constexpr int img_lower(int i, int s) { return i < 2 ? i : 2 + 2 * (i - 2) + s; }
 __host__ __device__ constexpr int img_upper(int i, int s) { return i < 2 ? 2 * i + s : i + 2; }
+// bytes of an image of N pieces: planes of 1 KB a fragment, a piece each (bf16) or the
+// two quads of a lane (f32)
 template <typename T>
-__device__ __forceinline__ Fi<T> ld_img(const char* img, int f, int lane) {
-  const char* p = img + f * 2048 + lane * 16;
-  Fi<T> x;
+__host__ __device__ constexpr int img_planes(int N) { return sizeof(T) == 2 ? N : 2; }
+template <typename T>
+__host__ __device__ constexpr int img_bytes(int N) { return 6 * 1024 * img_planes<T>(N); }
+template <typename T, int N>
+__device__ __forceinline__ Fi<T, N> ld_img(const char* img, int f, int lane) {
+  const char* p = img + f * 1024 * img_planes<T>(N) + lane * 16;
+  Fi<T, N> x;
   if constexpr (sizeof(T) == 2) {
-    const bf16x8 h = *reinterpret_cast<const bf16x8*>(p), l = *reinterpret_cast<const bf16x8*>(p + 1024);
-    x.hi.a = __builtin_shufflevector(h, h, 0, 1, 2, 3);
-    x.hi.b = __builtin_shufflevector(h, h, 4, 5, 6, 7);
-    x.lo.a = __builtin_shufflevector(l, l, 0, 1, 2, 3);
-    x.lo.b = __builtin_shufflevector(l, l, 4, 5, 6, 7);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const bf16x8 h = *reinterpret_cast<const bf16x8*>(p + 1024 * i);
+      x.x[i].a = __builtin_shufflevector(h, h, 0, 1, 2, 3);
+      x.x[i].b = __builtin_shufflevector(h, h, 4, 5, 6, 7);
+    }
   } else {
-    x.x.a = *reinterpret_cast<const f32x4*>(p);
-    x.x.b = *reinterpret_cast<const f32x4*>(p + 1024);
+    x.x[0].a = *reinterpret_cast<const f32x4*>(p);
+    x.x[0].b = *reinterpret_cast<const f32x4*>(p + 1024);
   }
   return x;
 }
-template <typename T>
+template <typename T, int N>
 __device__ __forceinline__ void st_img(char* img, int f, int lane, f32x4 a, f32x4 b) {
-  char* p = img + f * 2048 + lane * 16;
-  const Fi<T> x = to_fi<T>(a, b);
+  char* p = img + f * 1024 * img_planes<T>(N) + lane * 16;
+  const Fi<T, N> x = to_fi<T, N>(a, b);
   if constexpr (sizeof(T) == 2) {
-    *reinterpret_cast<bf16x8*>(p) = __builtin_shufflevector(x.hi.a, x.hi.b, 0, 1, 2, 3, 4, 5, 6, 7);
-    *reinterpret_cast<bf16x8*>(p + 1024) = __builtin_shufflevector(x.lo.a, x.lo.b, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      *reinterpret_cast<bf16x8*>(p + 1024 * i) = __builtin_shufflevector(x.x[i].a, x.x[i].b, 0, 1, 2, 3, 4, 5, 6, 7);
   } else {
-    *reinterpret_cast<f32x4*>(p) = x.x.a;
-    *reinterpret_cast<f32x4*>(p + 1024) = x.x.b;
+    *reinterpret_cast<f32x4*>(p) = x.x[0].a;
+    *reinterpret_cast<f32x4*>(p + 1024) = x.x[0].b;
   }
 }
+// one (slot, head) of the workspace.  Forward: T, P (towards o), scalars; backward: T,
+// P^T, T^T, scalars
+template <typename T>
+struct GdrWs {
+  static constexpr int I3 = img_bytes<T>(kExact), I2 = img_bytes<T>(kNear);
+  static constexpr int fT = 0, fP = I3, fScal = I3 + I2, fBytes = I3 + I2 + kGdrScal;
+  static constexpr int bT = 0, bPt = I3, bTt = 2 * I3, bScal = 3 * I3, bBytes = 3 * I3 + kGdrScal;
+};
 
-// one (slot, head) of the workspace: images, then scalars [5][64]: e^G, e^{G_C - G},
-// beta, and G as a sum of two floats
+// scalars [5][64] of a chunk: e^G, e^{G_C - G}, beta, and G as a sum of two floats
 enum : int { kScGam = 0, kScEnd = 1, kScBeta = 2, kScGh = 3, kScGl = 4 };
 
-// ---- token rows in LDS for reads across rows --------------------------------------------
-// A [64][DK] token tile whose 16-column tiles (p, h) = columns 32 p + 8 q + 4 h + i
-// (q, i = 0..3) are read transposed: as A operands K^T[j][t].  bf16: quad (p, q, h)
-// of row r sits at quad 8 p + 4 h + (q ^ ((r >> 2) & 3)), rows 16 (mod 32) elements
-// apart, which keeps the transposing reads free of bank conflicts.  f32: as it is,
-// rows padded by 16 bytes.
-template <typename T, int DK>
+// ---- token rows in LDS ------------------------------------------------------------------
+// A [64][COLS] token tile loaded straight into LDS (16 bytes a lane, no registers):
+// 16-byte piece x of row r sits at piece x ^ swz(r) of the row, so that both kinds of
+// bf16 operand reads are free of bank conflicts: along a row (16 rows x 2 neighbouring
+// quads at a time) and across rows (8 rows x 4 neighbouring quads).
+template <typename T, int COLS>
 struct GdrRows {
-  static constexpr int LD = sizeof(T) == 2 ? DK + 16 : DK + 4;
-  static constexpr int bytes = kGdrC * LD * (int)sizeof(T);
-  // the row's eight elements 32 p + 8 q ..
-  static __device__ __forceinline__ void put(T* t, int r, int p, int q, Fr<T> f) {
-    if constexpr (sizeof(T) == 2) {
-      T* d = t + r * LD + 32 * p + 4 * (q ^ ((r >> 2) & 3));
-      Quad<T>::st(d, f.a);
-      Quad<T>::st(d + 16, f.b);
-    } else {
-      T* d = t + r * LD + 32 * p + 8 * q;
-      Quad<T>::st(d, f.a);
-      Quad<T>::st(d + 4, f.b);
+  static constexpr int RB = COLS * (int)sizeof(T);     // bytes of a row
+  static constexpr int NCH = RB / 16;
+  static constexpr int bytes = kGdrC * RB;
+  static constexpr int PER = RB < 256 ? 256 / RB : 1;  // rows of a turn over the banks
+  static constexpr int MASK = NCH / 2 - 1 < 7 ? NCH / 2 - 1 : 7;
+  static_assert(NCH >= 4 && 1024 % RB == 0, "rows of 64 bytes to 1 KB");
+  static __device__ __forceinline__ int swz(int r) { return (((r / PER) & MASK) * 2) ^ ((r >> 3) & 1); }
+
+  // wave w of nw takes its share of the 1 KB pieces; rows behind the last of `len`
+  // repeat it.  base: the first row; stride in bytes, below 2^24
+  static __device__ __forceinline__ void dma(char* lds, const T* base, int stride, int len, int w, int nw, int lane) {
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<void*>(reinterpret_cast<const void*>(base)), 0, (len - 1) * stride + RB, 0x00027000);
+    constexpr int RPI = 1024 / RB;   // rows of a piece
+#pragma unroll
+    for (int i = 0; i < bytes / 1024; ++i) {
+      if (i % nw != w) continue;     // (uniform)
+      const int row = i * RPI + lane / NCH, x = (lane % NCH) ^ swz(row);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + 1024 * i), 16,
+                                               (int)__umul24(min(row, len - 1), stride) + 16 * x, 0, 0, 0);
     }
   }
-  // lane (g, c): column c of tile (p, h), rows r0 + 4 g + e
-  static __device__ __forceinline__ typename Quad<T>::q tr(const T* t, int r0, int p, int h, int g, int c) {
+  // lane (g, c): row 16 i + c, columns 32 p + 4 g + e and 32 p + 16 + 4 g + e
+  static __device__ __forceinline__ Fr<T> nat(const char* lds, int i, int p, int g, int c) {
+    Fr<T> f;
     if constexpr (sizeof(T) == 2) {
-      return Quad<T>::ld_tr_at(t + (r0 + 4 * g + (c >> 2)) * LD + 32 * p + 16 * h + 4 * ((c & 3) ^ g));
+      const int o = (((4 * p + (g >> 1)) ^ swz(c)) << 4) + ((g & 1) << 3);
+      f.a = Quad<T>::ld(reinterpret_cast<const T*>(lds + (16 * i + c) * RB + o));
+      f.b = Quad<T>::ld(reinterpret_cast<const T*>(lds + (16 * i + c) * RB + (o ^ 32)));
     } else {
-      const T* d = t + (r0 + 4 * g) * LD + 32 * p + 8 * (c >> 2) + 4 * h + (c & 3);
-      typename Quad<T>::q o = {d[0], d[LD], d[2 * LD], d[3 * LD]};
+      f.a = Quad<T>::ld(reinterpret_cast<const T*>(lds + (16 * i + c) * RB + (((8 * p + g) ^ swz(c)) << 4)));
+      f.b = Quad<T>::ld(reinterpret_cast<const T*>(lds + (16 * i + c) * RB + (((8 * p + 4 + g) ^ swz(c)) << 4)));
+    }
+    return f;
+  }
+  // lane (g, c): column 16 j + c, rows r0 + 4 g + e (r0 a multiple of 16)
+  static __device__ __forceinline__ typename Quad<T>::q tr(const char* lds, int r0, int j, int g, int c) {
+    if constexpr (sizeof(T) == 2) {
+      const int r = 4 * g + (c >> 2);
+      const int o = (((2 * j + ((c >> 1) & 1)) ^ swz(r)) << 4) + ((c & 1) << 3);
+      return Quad<T>::ld_tr_at(reinterpret_cast<const T*>(lds + (r0 + r) * RB + o));
+    } else {
+      typename Quad<T>::q o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = r0 + 4 * g + e;
+        o[e] = *reinterpret_cast<const T*>(lds + r * RB + (((4 * j + (c >> 2)) ^ swz(r)) << 4) + ((c & 3) << 2));
+      }
       return o;
     }
   }
-  static __device__ __forceinline__ Fr<T> frag(const T* t, int s, int p, int h, int g, int c) {
+  // both for the 32 tokens from 32 s
+  static __device__ __forceinline__ Fr<T> tr32(const char* lds, int s, int j, int g, int c) {
     Fr<T> f;
-    f.a = tr(t, 32 * s, p, h, g, c);
-    f.b = tr(t, 32 * s + 16, p, h, g, c);
+    f.a = tr(lds, 32 * s, j, g, c);
+    f.b = tr(lds, 32 * s + 16, j, g, c);
     return f;
   }
 };
+// `bytes` (whole KB) of global memory, as they are
+__device__ __forceinline__ void dma_flat(char* lds, const char* src, int bytes, int w, int nw, int lane) {
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(src), 0, bytes, 0x00027000);
+#pragma unroll
+  for (int i = 0; i < bytes / 1024; ++i) {
+    if (i % nw != w) continue;   // (uniform)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + 1024 * i), 16,
+                                             1024 * i + 16 * lane, 0, 0, 0);
+  }
+}
 
 // launches (carve_gdr_*.hip); mark: called after every launch
 int launch_gdr_fwd(const GdrArgs& a, int dtype, hipStream_t s, void (*mark)(hipStream_t));
 int launch_gdr_bwd(const GdrArgs& a, int dtype, hipStream_t s, void (*mark)(hipStream_t));
 int launch_gdr_prep(const GdrArgs& a, int dtype, bool bwd, hipStream_t s);
+// waves of a workgroup of the chains: two value tiles' worth fills every compute unit
+// up to 512 waves, beyond that four share a chunk's rows
+inline int gdr_chain_waves(const GdrArgs& a) { return a.Dv % 64 == 0 && (long long)a.nseq * a.Hv * a.Dv > 16 * 512 ? 4 : 2; }
 
 struct GdrStepArgs {
   const void *q, *k, *v, *beta;

@@ -18,127 +18,130 @@ namespace carve {
 namespace {
 
 // ---------------------------------------------------------------------------------
-// The chain of state gradients, the mirror of the forward's: a wave keeps dS^T[j][v]
-// of 16 value columns in registers and runs the chunks from the last to the first;
-// dS of every chunk's end goes to dS_chunks.
-template <typename T, int DK>
-__global__ void __launch_bounds__(128, 1) carve_gdr_bchain_kernel(GdrArgs a) {
+// The chain of state gradients, the mirror of the forward's (carve_gdr_chain_kernel): a
+// wave keeps dS^T[j][v] of 16 value columns in registers and runs the chunks from the
+// last to the first; dS of every chunk's end goes to dS_chunks.
+template <typename T, int DK, int NW>
+struct BChainLds {
+  typedef GdrRows<T, DK> KR;
+  typedef GdrRows<T, 16 * NW> VR;
+  static constexpr int img = GdrWs<T>::bBytes - GdrWs<T>::bPt;   // P^T, T^T, scalars
+  static constexpr int K = 0, Q = K + KR::bytes, O = Q + KR::bytes, I = O + VR::bytes;
+  static constexpr int one = I + img;
+  static constexpr int nbuf = 2 * one <= 160 * 1024 ? 2 : 1;
+  static constexpr int total = nbuf * one;
+};
+
+template <typename T, int DK, int NW>
+__global__ void __launch_bounds__(64 * NW, 1) carve_gdr_bchain_kernel(GdrArgs a) {
   constexpr int NP = DK / 32;
-  typedef GdrRows<T, DK> Rows;
-  constexpr int NBUF = 4 * Rows::bytes <= 160 * 1024 ? 2 : 1;
+  typedef BChainLds<T, DK, NW> L;
+  typedef typename L::KR KR;
+  typedef typename L::VR VR;
+  typedef GdrWs<T> WS;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, c = lane & 15;
-  const int ns = a.Dv / 32, idx = blockIdx.x;
+  const int ns = a.Dv / (16 * NW), idx = blockIdx.x;
   const int head = idx / (8 * ns) * 8 + idx % 8, slice = idx / 8 % ns;
   if (head >= a.nseq * a.Hv) return;
   const int n = head / a.Hv, hv = head % a.Hv, hk = hv / (a.Hv / a.Hk);
-  const int v0 = 32 * slice + 16 * w;
+  const int vs = 16 * NW * slice, v0 = vs + 16 * w;
   const GdrSeq sq = gdr_seq(a, n);
   const T* q = reinterpret_cast<const T*>(a.q) + sq.batch * a.qs[0] + sq.t0 * a.qs[1] + hk * a.qs[2];
   const T* k = reinterpret_cast<const T*>(a.k) + sq.batch * a.ks[0] + sq.t0 * a.ks[1] + hk * a.ks[2];
-  const T* dO = reinterpret_cast<const T*>(a.dO) + (((size_t)sq.batch * a.T + sq.t0) * a.Hv + hv) * a.Dv + v0;
-  const size_t sm = (size_t)a.Dv * DK, soff = (size_t)(v0 + c) * DK + 8 * g;
+  const T* dO = reinterpret_cast<const T*>(a.dO) + (((size_t)sq.batch * a.T + sq.t0) * a.Hv + hv) * a.Dv + vs;
   const size_t ors = (size_t)a.Hv * a.Dv;
+  const size_t sm = (size_t)a.Dv * DK, soff = (size_t)(v0 + c) * DK + 4 * g;
+  const int nch = (sq.len + kGdrC - 1) / kGdrC;
+
+  const auto load = [&](int ch) {
+    char* buf = smem + (L::nbuf == 2 ? (ch & 1) * L::one : 0);
+    const int t0 = ch * kGdrC, len = min(kGdrC, sq.len - t0);
+    KR::dma(buf + L::K, k + t0 * a.ks[1], (int)(a.ks[1] * sizeof(T)), len, w, NW, lane);
+    dma_flat(buf + L::I, a.ws + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * a.per + WS::bPt, L::img, w, NW, lane);
+    VR::dma(buf + L::O, dO + t0 * ors, (int)(ors * sizeof(T)), len, w, NW, lane);
+    KR::dma(buf + L::Q, q + t0 * a.qs[1], (int)(a.qs[1] * sizeof(T)), len, w, NW, lane);
+  };
+  if (L::nbuf == 2 && nch > 0) load(nch - 1);
 
   f32x4 S[2 * NP];
 #pragma unroll
-  for (int p = 0; p < NP; ++p) {
-    S[2 * p] = S[2 * p + 1] = zero4();
-    if (a.dS_T) {
-      const float* s = a.dS_T + (size_t)head * sm + soff + 32 * p;
-      S[2 * p] = *reinterpret_cast<const f32x4*>(s);
-      S[2 * p + 1] = *reinterpret_cast<const f32x4*>(s + 4);
-    }
-  }
-  const int nch = (sq.len + kGdrC - 1) / kGdrC;
+  for (int j = 0; j < 2 * NP; ++j)
+    S[j] = a.dS_T ? *reinterpret_cast<const f32x4*>(a.dS_T + (size_t)head * sm + soff + 16 * j) : zero4();
   for (int ch = nch - 1; ch >= 0; --ch) {
-    const int t0 = ch * kGdrC, len = min(kGdrC, sq.len - t0);
-    const size_t sh = (size_t)(sq.slot0 + ch) * a.Hv + hv;
-    const char* ws = a.ws + sh * a.per;
-    const float* scal = reinterpret_cast<const float*>(ws + 3 * kGdrImg);
-    T* sK = reinterpret_cast<T*>(smem + (NBUF == 2 ? 2 * (ch & 1) * Rows::bytes : 0));
-    T* sQ = reinterpret_cast<T*>(reinterpret_cast<char*>(sK) + Rows::bytes);
+    const char* buf = smem + (L::nbuf == 2 ? (ch & 1) * L::one : 0);
+    if constexpr (L::nbuf == 1) {
+      __syncthreads();
+      load(ch);
+    }
+    vm_wait_all();
+    __syncthreads();
+    if (L::nbuf == 2 && ch > 0) load(ch - 1);
     {
-      float* s = a.dS_chunks + sh * sm + soff;
+      float* s = a.dS_chunks + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * sm + soff;
 #pragma unroll
-      for (int p = 0; p < NP; ++p) {
-        *reinterpret_cast<f32x4*>(s + 32 * p) = S[2 * p];
-        *reinterpret_cast<f32x4*>(s + 32 * p + 4) = S[2 * p + 1];
-      }
+      for (int j = 0; j < 2 * NP; ++j) *reinterpret_cast<f32x4*>(s + 16 * j) = S[j];
     }
-    if (NBUF == 1 && ch < nch - 1) __syncthreads();
-    for (int x = tid; x < kGdrC * NP * 4; x += 128) {
-      const int r = x / (NP * 4), pq = x % (NP * 4);
-      Rows::put(sK, r, pq >> 2, pq & 3, ld_fr<T>(k + (size_t)(t0 + r) * a.ks[1] + 8 * pq, r < len));
-      Rows::put(sQ, r, pq >> 2, pq & 3, ld_fr<T>(q + (size_t)(t0 + r) * a.qs[1] + 8 * pq, r < len));
-    }
-    // dO[t][v] of this wave's columns, tokens as rows
-    f32x4 od[4];
+    const char* img = buf + L::I;
+    const float* scal = reinterpret_cast<const float*>(img + (WS::bScal - WS::bPt));
+    const int len = sq.len - ch * kGdrC;
+    // dO[t][v] of this wave's columns, zeros behind the last token
+    Fr<T> of[2] = {VR::tr32(buf + L::O, 0, w, g, c), VR::tr32(buf + L::O, 1, w, g, c)};
+    if (len < kGdrC)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+      for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int t = 16 * i + 4 * g + e;
-        od[i][e] = t < len ? (float)dO[(size_t)(t0 + t) * ors + c] : 0.0f;
-      }
-    Fr<T> of[2];
+        for (int e = 0; e < 4; ++e) {
+          if (32 * s + 4 * g + e >= len) of[s].a[e] = (T)0.0f;
+          if (32 * s + 16 + 4 * g + e >= len) of[s].b[e] = (T)0.0f;
+        }
+    Fi<T, kExact> Sf[NP];
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      of[s].a = Quad<T>::cvt(od[2 * s]);
-      of[s].b = Quad<T>::cvt(od[2 * s + 1]);
-    }
-    Fi<T> Sf[NP];
-#pragma unroll
-    for (int p = 0; p < NP; ++p) Sf[p] = to_fi<T>(S[2 * p], S[2 * p + 1]);
+    for (int p = 0; p < NP; ++p) Sf[p] = to_fi<T, kExact>(S[2 * p], S[2 * p + 1]);
     // dU = P^T dO' + E K dS^T
     f32x4 U[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int r = 16 * i + c;
       f32x4 x = zero4(), y = zero4();
 #pragma unroll
-      for (int p = 0; p < NP; ++p)
-        y = mma<T>(ld_fr<T>(k + (size_t)(t0 + r) * a.ks[1] + 32 * p + 8 * g, r < len), Sf[p], y);
+      for (int p = 0; p < NP; ++p) y = mma<T>(KR::nat(buf + L::K, i, p, g, c), Sf[p], y);
 #pragma unroll
-      for (int s = i / 2; s < 2; ++s) x = mma<T>(ld_img<T>(ws + kGdrImg, img_upper(i, s), lane), of[s], x);
+      for (int s = i / 2; s < 2; ++s) x = mma<T>(ld_img<T, kExact>(img, img_upper(i, s), lane), of[s], x);
       const f32x4 end = *reinterpret_cast<const f32x4*>(scal + kScEnd * kGdrC + 16 * i + 4 * g);
       U[i] = x * a.scale + y * end;
     }
-    const Fi<T> Uf[2] = {to_fi<T>(U[0], U[1]), to_fi<T>(U[2], U[3])};
+    const Fi<T, kExact> Uf[2] = {to_fi<T, kExact>(U[0], U[1]), to_fi<T, kExact>(U[2], U[3])};
     // - beta e^G dR, dR = T^T dU, and e^G dO'
-    f32x4 R[4];
+    f32x4 R[4], od[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       f32x4 x = zero4();
 #pragma unroll
-      for (int s = i / 2; s < 2; ++s) x = mma<T>(ld_img<T>(ws + 2 * kGdrImg, img_upper(i, s), lane), Uf[s], x);
+      for (int s = i / 2; s < 2; ++s)
+        x = mma<T>(ld_img<T, kExact>(img + (WS::bTt - WS::bPt), img_upper(i, s), lane), Uf[s], x);
       const f32x4 gam = *reinterpret_cast<const f32x4*>(scal + kScGam * kGdrC + 16 * i + 4 * g);
       const f32x4 be = *reinterpret_cast<const f32x4*>(scal + kScBeta * kGdrC + 16 * i + 4 * g);
       R[i] = -(x * gam * be);
-      od[i] *= gam * a.scale;
+      od[i] = Quad<T>::f32(i % 2 ? of[i / 2].b : of[i / 2].a) * (gam * a.scale);
     }
-    const Fi<T> Rf[2] = {to_fi<T>(R[0], R[1]), to_fi<T>(R[2], R[3])};
-    const Fi<T> Of[2] = {to_fi<T>(od[0], od[1]), to_fi<T>(od[2], od[3])};
-    __syncthreads();
+    const Fi<T, kExact> Rf[2] = {to_fi<T, kExact>(R[0], R[1]), to_fi<T, kExact>(R[2], R[3])};
+    const Fi<T, kExact> Of[2] = {to_fi<T, kExact>(od[0], od[1]), to_fi<T, kExact>(od[2], od[3])};
     const float gend = scal[kScGam * kGdrC + kGdrC - 1];
 #pragma unroll
     for (int j = 0; j < 2 * NP; ++j) {
       S[j] *= gend;
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        S[j] = mma<T>(Rows::frag(sQ, s, j >> 1, j & 1, g, c), Of[s], S[j]);
-        S[j] = mma<T>(Rows::frag(sK, s, j >> 1, j & 1, g, c), Rf[s], S[j]);
+        S[j] = mma<T>(KR::tr32(buf + L::Q, s, j, g, c), Of[s], S[j]);
+        S[j] = mma<T>(KR::tr32(buf + L::K, s, j, g, c), Rf[s], S[j]);
       }
     }
   }
   if (a.dS0) {
     float* s = a.dS0 + (size_t)head * sm + soff;
 #pragma unroll
-    for (int p = 0; p < NP; ++p) {
-      *reinterpret_cast<f32x4*>(s + 32 * p) = S[2 * p];
-      *reinterpret_cast<f32x4*>(s + 32 * p + 4) = S[2 * p + 1];
-    }
+    for (int j = 0; j < 2 * NP; ++j) *reinterpret_cast<f32x4*>(s + 16 * j) = S[j];
   }
 }
 
@@ -156,47 +159,43 @@ constexpr int kVB = 128;   // value columns of a block
 template <typename T>
 struct InterT {
   static constexpr int LD = sizeof(T) == 2 ? kGdrC + 16 : kGdrC + 4;
-  static __host__ __device__ constexpr int bytes(int cols) { return cols * LD * 4; }   // bf16: two planes
-  // the four tokens 16 i + 4 g .. of column col
+  static __host__ __device__ constexpr int bytes(int cols, int n) { return cols * LD * (sizeof(T) == 2 ? 2 * n : 4); }
+  // the four tokens 16 i + 4 g .. of column col, in N pieces
+  template <int N>
   static __device__ __forceinline__ void put(char* m, int cols, int col, int i, int g, f32x4 x) {
     T* p = reinterpret_cast<T*>(m) + col * LD + 16 * i;
     if constexpr (sizeof(T) == 2) {
-      bf16x4 hi, lo;
-      split4(x, hi, lo);
-      Quad<T>::st(p + ((4 * g) ^ qswz<T>(col)), hi);
-      Quad<T>::st(p + cols * LD + ((4 * g) ^ qswz<T>(col)), lo);
+#pragma unroll
+      for (int y = 0; y < N; ++y) {
+        const typename Quad<T>::q h = Quad<T>::cvt(x);
+        Quad<T>::st(p + y * cols * LD + ((4 * g) ^ qswz<T>(col)), h);
+        x -= Quad<T>::f32(h);
+      }
     } else {
       Quad<T>::st(p + 4 * g, x);
     }
   }
   // lane (g, c): token 16 i + c, columns col0 + 4 g + e and col0 + 16 + 4 g + e
-  static __device__ __forceinline__ Fi<T> tok(const char* m, int cols, int i, int col0, int g, int c) {
+  template <int N>
+  static __device__ __forceinline__ Fi<T, N> tok(const char* m, int cols, int i, int col0, int g, int c) {
     const T* p = reinterpret_cast<const T*>(m);
-    Fi<T> f;
-    if constexpr (sizeof(T) == 2) {
-      f.hi.a = Quad<T>::ld_tr_sw(p, LD, col0, 16 * i, g, c);
-      f.hi.b = Quad<T>::ld_tr_sw(p, LD, col0 + 16, 16 * i, g, c);
-      f.lo.a = Quad<T>::ld_tr_sw(p + cols * LD, LD, col0, 16 * i, g, c);
-      f.lo.b = Quad<T>::ld_tr_sw(p + cols * LD, LD, col0 + 16, 16 * i, g, c);
-    } else {
-      f.x.a = Quad<T>::ld_tr(p, LD, col0, 16 * i, g, c);
-      f.x.b = Quad<T>::ld_tr(p, LD, col0 + 16, 16 * i, g, c);
+    Fi<T, N> f;
+#pragma unroll
+    for (int y = 0; y < (sizeof(T) == 2 ? N : 1); ++y) {
+      f.x[y].a = Quad<T>::ld_tr_sw(p + y * cols * LD, LD, col0, 16 * i, g, c);
+      f.x[y].b = Quad<T>::ld_tr_sw(p + y * cols * LD, LD, col0 + 16, 16 * i, g, c);
     }
     return f;
   }
   // lane (g, c): column col0 + c, tokens 32 s + 4 g + e and 32 s + 16 + 4 g + e
-  static __device__ __forceinline__ Fi<T> col(const char* m, int cols, int col0, int s, int g, int c) {
-    const T* p = reinterpret_cast<const T*>(m) + (col0 + c) * LD + 32 * s;
-    Fi<T> f;
-    if constexpr (sizeof(T) == 2) {
-      const int o = (4 * g) ^ qswz<T>(col0 + c);
-      f.hi.a = Quad<T>::ld(p + o);
-      f.hi.b = Quad<T>::ld(p + o + 16);
-      f.lo.a = Quad<T>::ld(p + cols * LD + o);
-      f.lo.b = Quad<T>::ld(p + cols * LD + o + 16);
-    } else {
-      f.x.a = Quad<T>::ld(p + 4 * g);
-      f.x.b = Quad<T>::ld(p + 4 * g + 16);
+  template <int N>
+  static __device__ __forceinline__ Fi<T, N> col(const char* m, int cols, int col0, int s, int g, int c) {
+    const T* p = reinterpret_cast<const T*>(m) + (col0 + c) * LD + 32 * s + ((4 * g) ^ qswz<T>(col0 + c));
+    Fi<T, N> f;
+#pragma unroll
+    for (int y = 0; y < (sizeof(T) == 2 ? N : 1); ++y) {
+      f.x[y].a = Quad<T>::ld(p + y * cols * LD);
+      f.x[y].b = Quad<T>::ld(p + y * cols * LD + 16);
     }
     return f;
   }
@@ -205,10 +204,10 @@ struct InterT {
 template <typename T>
 struct GradLds {
   static constexpr int U = 0;
-  static constexpr int R = U + InterT<T>::bytes(kVB);
-  static constexpr int W = R + InterT<T>::bytes(kVB);      // (D dP)^T: [j][i]
-  static constexpr int M = W + InterT<T>::bytes(kGdrC);    // M^T: [j][i]
-  static constexpr int red = M + InterT<T>::bytes(kGdrC);
+  static constexpr int R = U + InterT<T>::bytes(kVB, kExact);
+  static constexpr int red = R + InterT<T>::bytes(kVB, kExact);
+  static constexpr int W = 0;                                      // (D dP)^T: [j][i], over U
+  static constexpr int M = W + InterT<T>::bytes(kGdrC, kNear);     // M^T: [j][i]
   // sums over values or keys: [wave][64] of dR.V, q.(dO' S), k.(U dS), k.(dR S), then
   // <dS, S> per wave; sums over tiles: [4][64] of rows of dP P + dA A, rows of dA A /
   // beta, columns of dP P + dA A; decays and beta
@@ -254,16 +253,10 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
   f32x4 dQ[NI], dK[NI];
 #pragma unroll
   for (int i = 0; i < NI; ++i) dQ[i] = dK[i] = zero4();
-  // the upper tiles (0, 1) and (2, 3) of W and M, which the fragments reach: zeros
-  for (int x = tid; x < 4 * 64; x += 512) {
-    const int y = x >> 6;
-    IT::put(smem + (y & 1 ? L::M : L::W), kGdrC, 16 * (y < 2 ? 1 : 3) + c, y < 2 ? 0 : 2, g, zero4());
-  }
-
   for (int hv = hk * grp; hv < (hk + 1) * grp; ++hv) {
     const size_t sh = (size_t)slot * a.Hv + hv;
     const char* ws = a.ws + sh * a.per;
-    const float* scal = reinterpret_cast<const float*>(ws + 3 * kGdrImg);
+    const float* scal = reinterpret_cast<const float*>(ws + GdrWs<T>::bScal);
     const T* v = reinterpret_cast<const T*>(a.v) + sq.batch * a.vs[0] + t0 * a.vs[1] + hv * a.vs[2];
     const T* dO = reinterpret_cast<const T*>(a.dO) + (row0 * a.Hv + hv) * a.Dv;
     T* dV = reinterpret_cast<T*>(a.dv) + (row0 * a.Hv + hv) * a.Dv;
@@ -291,15 +284,15 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
       // ---- 1. U, dR of columns vb + 16 w ..
       if (16 * w < cols) {
         const int v0 = vb + 16 * w;
-        Fi<T> Sf[NP], Df[NP];
+        Fi<T, kExact> Sf[NP], Df[NP];
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
           const size_t at = (size_t)(v0 + c) * DK + 32 * p + 8 * g;
           const f32x4 s0 = *reinterpret_cast<const f32x4*>(S + at), s1 = *reinterpret_cast<const f32x4*>(S + at + 4);
           const f32x4 d0 = *reinterpret_cast<const f32x4*>(dS + at), d1 = *reinterpret_cast<const f32x4*>(dS + at + 4);
           for (int e = 0; e < 4; ++e) ss += s0[e] * d0[e] + s1[e] * d1[e];
-          Sf[p] = to_fi<T>(s0, s1);
-          Df[p] = to_fi<T>(d0, d1);
+          Sf[p] = to_fi<T, kExact>(s0, s1);
+          Df[p] = to_fi<T, kExact>(d0, d1);
         }
         f32x4 R[4], U[4], vt[4], od[4];
 #pragma unroll
@@ -327,24 +320,24 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
             y = mma<T>(fk, Df[p], y);
           }
 #pragma unroll
-          for (int s = i / 2; s < 2; ++s) z = mma<T>(ld_img<T>(ws + kGdrImg, img_upper(i, s), lane), of[s], z);
+          for (int s = i / 2; s < 2; ++s) z = mma<T>(ld_img<T, kExact>(ws + GdrWs<T>::bPt, img_upper(i, s), lane), of[s], z);
           const f32x4 gam = *reinterpret_cast<const f32x4*>(scal + kScGam * kGdrC + 16 * i + 4 * g);
           const f32x4 end = *reinterpret_cast<const f32x4*>(scal + kScEnd * kGdrC + 16 * i + 4 * g);
           const f32x4 be = *reinterpret_cast<const f32x4*>(scal + kScBeta * kGdrC + 16 * i + 4 * g);
           R[i] = be * (vt[i] - gam * x);
           U[i] = z * a.scale + y * end;      // dU
         }
-        const Fi<T> Rf[2] = {to_fi<T>(R[0], R[1]), to_fi<T>(R[2], R[3])};
-        const Fi<T> Uf[2] = {to_fi<T>(U[0], U[1]), to_fi<T>(U[2], U[3])};
+        const Fi<T, kExact> Rf[2] = {to_fi<T, kExact>(R[0], R[1]), to_fi<T, kExact>(R[2], R[3])};
+        const Fi<T, kExact> Uf[2] = {to_fi<T, kExact>(U[0], U[1]), to_fi<T, kExact>(U[2], U[3])};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           f32x4 x = zero4(), y = zero4();
 #pragma unroll
-          for (int s = 0; s <= i / 2; ++s) x = mma<T>(ld_img<T>(ws, img_lower(i, s), lane), Rf[s], x);
+          for (int s = 0; s <= i / 2; ++s) x = mma<T>(ld_img<T, kExact>(ws, img_lower(i, s), lane), Rf[s], x);
 #pragma unroll
-          for (int s = i / 2; s < 2; ++s) y = mma<T>(ld_img<T>(ws + 2 * kGdrImg, img_upper(i, s), lane), Uf[s], y);
-          IT::put(smem + L::U, kVB, 16 * w + c, i, g, x);
-          IT::put(smem + L::R, kVB, 16 * w + c, i, g, y);
+          for (int s = i / 2; s < 2; ++s) y = mma<T>(ld_img<T, kExact>(ws + GdrWs<T>::bTt, img_upper(i, s), lane), Uf[s], y);
+          IT::template put<kExact>(smem + L::U, kVB, 16 * w + c, i, g, x);
+          IT::template put<kExact>(smem + L::R, kVB, 16 * w + c, i, g, y);
           const f32x4 be = *reinterpret_cast<const f32x4*>(scal + kScBeta * kGdrC + 16 * i + 4 * g);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -362,9 +355,9 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
         if (y < 10) {
           const int i = tri_row_of(y, false), j = tri_col_of(y, false), r = 16 * i + c;
           for (int p = 0; p < cols / 32; ++p) {
-            const Fi<T> fu = IT::tok(smem + L::U, kVB, j, 32 * p, g, c);
+            const Fi<T, kExact> fu = IT::template tok<kExact>(smem + L::U, kVB, j, 32 * p, g, c);
             aP[x] = mma<T>(ld_fr16<T>(dO + (size_t)r * ors + vb + 32 * p + 4 * g, r < len), fu, aP[x]);
-            aA[x] = mma<T>(IT::tok(smem + L::R, kVB, i, 32 * p, g, c), fu, aA[x]);
+            aA[x] = mma<T>(IT::template tok<kExact>(smem + L::R, kVB, i, 32 * p, g, c), fu, aA[x]);
           }
         }
       }
@@ -378,13 +371,13 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
             s[h][e] = S[at];
             d[h][e] = dS[at];
           }
-        const Fi<T> fs = to_fi<T>(s[0], s[1]), fd = to_fi<T>(d[0], d[1]);
+        const Fi<T, kExact> fs = to_fi<T, kExact>(s[0], s[1]), fd = to_fi<T, kExact>(d[0], d[1]);
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
           const int r = 16 * (i0 + i) + c;
           a1[i] = mma<T>(ld_fr16<T>(dO + (size_t)r * ors + vb + 32 * p + 4 * g, r < len), fs, a1[i]);
-          a2[i] = mma<T>(IT::tok(smem + L::U, kVB, i0 + i, 32 * p, g, c), fd, a2[i]);
-          a3[i] = mma<T>(IT::tok(smem + L::R, kVB, i0 + i, 32 * p, g, c), fs, a3[i]);
+          a2[i] = mma<T>(IT::template tok<kExact>(smem + L::U, kVB, i0 + i, 32 * p, g, c), fd, a2[i]);
+          a3[i] = mma<T>(IT::template tok<kExact>(smem + L::R, kVB, i0 + i, 32 * p, g, c), fs, a3[i]);
         }
       }
       __syncthreads();
@@ -401,7 +394,12 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
     ss = group_sum<64>(ss);
     if (lane == 0) rSS[w] = ss;
 
-    // ---- D dP and M of this wave's tiles, with their row and column sums
+    // ---- D dP and M of this wave's tiles, with their row and column sums; zeros in the
+    // upper tiles (0, 1) and (2, 3), which the fragments reach
+    if (w >= 4) {
+      const int y = w - 4;
+      IT::template put<kNear>(smem + (y & 1 ? L::M : L::W), kGdrC, 16 * (y < 2 ? 1 : 3) + c, y < 2 ? 0 : 2, g, zero4());
+    }
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       const int y = w + 8 * x;
@@ -435,8 +433,8 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
         col += __shfl_xor(col, 16);
         col += __shfl_xor(col, 32);
         if (g == 0) rCol[i * kGdrC + rj] = col;
-        IT::put(smem + L::W, kGdrC, 16 * j + c, i, g, W);
-        IT::put(smem + L::M, kGdrC, 16 * j + c, i, g, M);
+        IT::template put<kNear>(smem + L::W, kGdrC, 16 * j + c, i, g, W);
+        IT::template put<kNear>(smem + L::M, kGdrC, 16 * j + c, i, g, M);
       }
     }
     __syncthreads();
@@ -481,12 +479,12 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
         dQ[ii] += x1;
         dK[ii] += x2 - be * x3;
         for (int s = 0; s <= i / 2; ++s) {
-          dQ[ii] = mma<T>(IT::tok(smem + L::W, kGdrC, i, 32 * s, g, c), fk[s], dQ[ii]);
-          dK[ii] = mma<T>(IT::tok(smem + L::M, kGdrC, i, 32 * s, g, c), fk[s], dK[ii]);
+          dQ[ii] = mma<T>(IT::template tok<kNear>(smem + L::W, kGdrC, i, 32 * s, g, c), fk[s], dQ[ii]);
+          dK[ii] = mma<T>(IT::template tok<kNear>(smem + L::M, kGdrC, i, 32 * s, g, c), fk[s], dK[ii]);
         }
         for (int s = i / 2; s < 2; ++s) {
-          dK[ii] = mma<T>(IT::col(smem + L::W, kGdrC, 16 * i, s, g, c), fq[s], dK[ii]);
-          dK[ii] = mma<T>(IT::col(smem + L::M, kGdrC, 16 * i, s, g, c), fk[s], dK[ii]);
+          dK[ii] = mma<T>(IT::template col<kNear>(smem + L::W, kGdrC, 16 * i, s, g, c), fq[s], dK[ii]);
+          dK[ii] = mma<T>(IT::template col<kNear>(smem + L::M, kGdrC, 16 * i, s, g, c), fk[s], dK[ii]);
         }
       }
     }
@@ -553,21 +551,28 @@ int allow_lds(K kern, int bytes) {
              : CARVE_ERR_HIP;
 }
 
+template <typename T, int DK, int NW>
+int launch_bchain_t(const GdrArgs& a, hipStream_t s) {
+  constexpr int lds = BChainLds<T, DK, NW>::total;
+  static_assert(lds <= 160 * 1024, "LDS");
+  const auto kern = carve_gdr_bchain_kernel<T, DK, NW>;
+  const int st = allow_lds(kern, lds);
+  if (st) return st;
+  const unsigned heads = (unsigned)a.nseq * a.Hv;
+  hipLaunchKernelGGL(kern, dim3((heads + 7) / 8 * 8 * (a.Dv / (16 * NW))), dim3(64 * NW), lds, s, a);
+  return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
+}
 template <typename T, int DK>
 int launch_bwd_t(const GdrArgs& a, hipStream_t s, void (*mark)(hipStream_t)) {
-  constexpr int rows = GdrRows<T, DK>::bytes;
-  constexpr int chain_lds = (4 * rows <= 160 * 1024 ? 4 : 2) * rows;
-  static_assert(chain_lds <= 160 * 1024 && GradLds<T>::total <= 160 * 1024, "LDS");
-  int st = allow_lds(carve_gdr_bchain_kernel<T, DK>, chain_lds);
-  if (!st) st = allow_lds(carve_gdr_grad_kernel<T, DK>, GradLds<T>::total);
-  if (!st) st = launch_gdr_prep(a, sizeof(T) == 2 ? CARVE_BF16 : CARVE_F32, true, s);
+  static_assert(GradLds<T>::total <= 160 * 1024, "LDS");
+  int st = launch_gdr_prep(a, sizeof(T) == 2 ? CARVE_BF16 : CARVE_F32, true, s);
   if (st) return st;
   mark(s);
-  const unsigned heads = (unsigned)a.nseq * a.Hv;
-  hipLaunchKernelGGL((carve_gdr_bchain_kernel<T, DK>), dim3((heads + 7) / 8 * 8 * (a.Dv / 32)), dim3(128), chain_lds, s,
-                     a);
-  if (hipGetLastError() != hipSuccess) return CARVE_ERR_HIP;
+  st = gdr_chain_waves(a) == 4 ? launch_bchain_t<T, DK, 4>(a, s) : launch_bchain_t<T, DK, 2>(a, s);
+  if (st) return st;
   mark(s);
+  st = allow_lds(carve_gdr_grad_kernel<T, DK>, GradLds<T>::total);
+  if (st) return st;
   hipLaunchKernelGGL((carve_gdr_grad_kernel<T, DK>), dim3(a.nslots, a.Hk), dim3(512), GradLds<T>::total, s, a);
   mark(s);
   return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;

@@ -33,7 +33,8 @@ __global__ void __launch_bounds__(256) carve_gdr_prep_kernel(GdrArgs a) {
   const T* k = reinterpret_cast<const T*>(a.k) + sq.batch * a.ks[0] + t0 * a.ks[1] + hk * a.ks[2];
   const size_t row0 = ((size_t)sq.batch * a.T + t0) * a.Hv + hv;
   char* ws = a.ws + ((size_t)slot * a.Hv + hv) * a.per;
-  float* scal = reinterpret_cast<float*>(ws + (BWD ? 3 : 2) * kGdrImg);
+  typedef GdrWs<T> WS;
+  float* scal = reinterpret_cast<float*>(ws + (BWD ? WS::bScal : WS::fScal));
 
   // row tile w against the column tiles up to it
   f32x4 kk[4], qk[4];
@@ -99,20 +100,20 @@ __global__ void __launch_bounds__(256) carve_gdr_prep_kernel(GdrArgs a) {
     }
   __syncthreads();
   // P image by waves 1 - 3, the diagonal inverses by wave 0
-  char* imgP = ws + kGdrImg;
+  char* imgP = ws + (BWD ? WS::bPt : WS::fP);
   if (w > 0) {
     for (int x = tid - 64; x < 6 * 64; x += 192) {
       const int f = x >> 6, l = x & 63, lg = l >> 4, lc = l & 15;
       if constexpr (!BWD) {
         const int i = f < 2 ? f : 2 + (f - 2) / 2, s = f < 2 ? 0 : (f - 2) % 2;
         const float* r = sP + (16 * i + lc) * LD + 32 * s + 4 * lg;
-        st_img<T>(imgP, f, l, *reinterpret_cast<const f32x4*>(r), *reinterpret_cast<const f32x4*>(r + 16));
+        st_img<T, kNear>(imgP, f, l, *reinterpret_cast<const f32x4*>(r), *reinterpret_cast<const f32x4*>(r + 16));
       } else {
         const int i = f < 4 ? f / 2 : f - 2, s = f < 4 ? f % 2 : 1;
         const float* r = sP + (32 * s + 4 * lg) * LD + 16 * i + lc;
         const f32x4 x0 = {r[0], r[LD], r[2 * LD], r[3 * LD]};
         const f32x4 x1 = {r[16 * LD], r[17 * LD], r[18 * LD], r[19 * LD]};
-        st_img<T>(imgP, f, l, x0, x1);
+        st_img<T, kExact>(imgP, f, l, x0, x1);
       }
     }
   } else {
@@ -165,145 +166,158 @@ __global__ void __launch_bounds__(256) carve_gdr_prep_kernel(GdrArgs a) {
     {
       const int i = f < 2 ? f : 2 + (f - 2) / 2, s = f < 2 ? 0 : (f - 2) % 2;
       const float* r = sT + (16 * i + lc) * LD + 32 * s + 4 * lg;
-      st_img<T>(ws, f, l, *reinterpret_cast<const f32x4*>(r), *reinterpret_cast<const f32x4*>(r + 16));
+      st_img<T, kExact>(ws, f, l, *reinterpret_cast<const f32x4*>(r), *reinterpret_cast<const f32x4*>(r + 16));
     }
     if constexpr (BWD) {
       const int i = f < 4 ? f / 2 : f - 2, s = f < 4 ? f % 2 : 1;
       const float* r = sT + (32 * s + 4 * lg) * LD + 16 * i + lc;
       const f32x4 x0 = {r[0], r[LD], r[2 * LD], r[3 * LD]};
       const f32x4 x1 = {r[16 * LD], r[17 * LD], r[18 * LD], r[19 * LD]};
-      st_img<T>(ws + 2 * kGdrImg, f, l, x0, x1);
+      st_img<T, kExact>(ws + WS::bTt, f, l, x0, x1);
     }
   }
 }
 
 // ---------------------------------------------------------------------------------
-// The chain of states.  A workgroup of two waves runs one sequence and value head
-// for 32 value columns, a wave for 16 of them: value rows of S are independent, so
-// nothing but the chunk's keys (read across rows, in LDS) is shared and one barrier
-// a chunk is left.  A wave keeps S^T[j][v] in the matrix-core result layout, where
-// it is at once the B operand of K S^T and the A operand of (Q S^T)^T: no state
-// passes through LDS.  Tile (p, h) of it holds the keys j = 32 p + 8 (m / 4) + 4 h +
-// m mod 4 of row m, so that a lane's keys of the tiles (p, 0), (p, 1) are eight
-// consecutive ones and the token rows are read in 16-byte pieces.
-template <typename T, int DK>
-__global__ void __launch_bounds__(128, 1) carve_gdr_chain_kernel(GdrArgs a) {
+// The chain of states.  A workgroup of NW waves runs one sequence and value head for
+// 16 NW value columns, a wave for 16 of them: value rows of S are independent, so the
+// waves share nothing but the chunk's rows.  A wave keeps S^T[j][v] in the matrix-core
+// result layout, where it is at once the B operand of K S^T and the A operand of
+// (Q S^T)^T: no state passes through LDS.  The next chunk's keys, queries, values and
+// images are loaded straight into the other half of the LDS while this one runs; one
+// wait for memory and one barrier a chunk, and the outputs of a chunk are stored behind
+// the next one's wait, so that no wait covers a store that was just issued.
+template <typename T, int DK, int NW>
+struct ChainLds {
+  typedef GdrRows<T, DK> KR;
+  typedef GdrRows<T, 16 * NW> VR;
+  static constexpr int K = 0, Q = K + KR::bytes, V = Q + KR::bytes, I = V + VR::bytes;
+  static constexpr int one = I + GdrWs<T>::fBytes;
+  static constexpr int nbuf = 2 * one <= 160 * 1024 ? 2 : 1;   // (f32 rows of 128: one)
+  static constexpr int total = nbuf * one;
+};
+
+template <typename T, int DK, int NW>
+__global__ void __launch_bounds__(64 * NW, 1) carve_gdr_chain_kernel(GdrArgs a) {
   constexpr int NP = DK / 32;
-  typedef GdrRows<T, DK> Rows;
-  // two buffers where they fit 64 KB (all but f32 rows of 128): one barrier a chunk
-  constexpr int NBUF = 2 * Rows::bytes <= 65536 ? 2 : 1;
-  __shared__ __attribute__((aligned(16))) char smem[NBUF * Rows::bytes];
+  typedef ChainLds<T, DK, NW> L;
+  typedef typename L::KR KR;
+  typedef typename L::VR VR;
+  typedef GdrWs<T> WS;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, c = lane & 15;
   // blocks 8 apart share an XCD: the slices of a (sequence, head) follow each other there
-  const int ns = a.Dv / 32, idx = blockIdx.x;
+  const int ns = a.Dv / (16 * NW), idx = blockIdx.x;
   const int head = idx / (8 * ns) * 8 + idx % 8, slice = idx / 8 % ns;
   if (head >= a.nseq * a.Hv) return;
   const int n = head / a.Hv, hv = head % a.Hv, hk = hv / (a.Hv / a.Hk);
-  const int v0 = 32 * slice + 16 * w;
+  const int vs = 16 * NW * slice, v0 = vs + 16 * w;
   const GdrSeq sq = gdr_seq(a, n);
   const T* q = reinterpret_cast<const T*>(a.q) + sq.batch * a.qs[0] + sq.t0 * a.qs[1] + hk * a.qs[2];
   const T* k = reinterpret_cast<const T*>(a.k) + sq.batch * a.ks[0] + sq.t0 * a.ks[1] + hk * a.ks[2];
-  const T* v = reinterpret_cast<const T*>(a.v) + sq.batch * a.vs[0] + sq.t0 * a.vs[1] + hv * a.vs[2] + v0;
+  const T* v = reinterpret_cast<const T*>(a.v) + sq.batch * a.vs[0] + sq.t0 * a.vs[1] + hv * a.vs[2] + vs;
   T* o = reinterpret_cast<T*>(a.o) + (((size_t)sq.batch * a.T + sq.t0) * a.Hv + hv) * a.Dv + v0;
+  const size_t ors = (size_t)a.Hv * a.Dv;
   const size_t sm = (size_t)a.Dv * DK;   // elements of a state
-  const size_t soff = (size_t)(v0 + c) * DK + 8 * g;
+  const size_t soff = (size_t)(v0 + c) * DK + 4 * g;
+  const int nch = (sq.len + kGdrC - 1) / kGdrC;
+
+  const auto load = [&](int ch) {
+    char* buf = smem + (L::nbuf == 2 ? (ch & 1) * L::one : 0);
+    const int t0 = ch * kGdrC, len = min(kGdrC, sq.len - t0);
+    KR::dma(buf + L::K, k + t0 * a.ks[1], (int)(a.ks[1] * sizeof(T)), len, w, NW, lane);
+    dma_flat(buf + L::I, a.ws + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * a.per, WS::fBytes, w, NW, lane);
+    VR::dma(buf + L::V, v + t0 * a.vs[1], (int)(a.vs[1] * sizeof(T)), len, w, NW, lane);
+    KR::dma(buf + L::Q, q + t0 * a.qs[1], (int)(a.qs[1] * sizeof(T)), len, w, NW, lane);
+  };
+  if (L::nbuf == 2 && nch > 0) load(0);
 
   f32x4 S[2 * NP];
 #pragma unroll
-  for (int p = 0; p < NP; ++p) {
-    S[2 * p] = S[2 * p + 1] = zero4();
-    if (a.S0) {
-      const float* s = a.S0 + (size_t)head * sm + soff + 32 * p;
-      S[2 * p] = *reinterpret_cast<const f32x4*>(s);
-      S[2 * p + 1] = *reinterpret_cast<const f32x4*>(s + 4);
-    }
-  }
-  const int nch = (sq.len + kGdrC - 1) / kGdrC;
+  for (int j = 0; j < 2 * NP; ++j)
+    S[j] = a.S0 ? *reinterpret_cast<const f32x4*>(a.S0 + (size_t)head * sm + soff + 16 * j) : zero4();
+  typename Quad<T>::q oq[4];   // o^T of the last chunk: four values of token 16 i + c
+  const auto store_o = [&](int ch) {
+    const int t0 = ch * kGdrC, len = sq.len - t0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (16 * i + c < len) Quad<T>::st(o + (size_t)(t0 + 16 * i + c) * ors + 4 * g, oq[i]);
+  };
   for (int ch = 0; ch < nch; ++ch) {
-    const int t0 = ch * kGdrC, len = min(kGdrC, sq.len - t0);
-    const size_t sh = (size_t)(sq.slot0 + ch) * a.Hv + hv;
-    const char* ws = a.ws + sh * a.per;
-    const float* scal = reinterpret_cast<const float*>(ws + 2 * kGdrImg);
-    T* sK = reinterpret_cast<T*>(smem + (NBUF == 2 ? (ch & 1) * Rows::bytes : 0));
+    const char* buf = smem + (L::nbuf == 2 ? (ch & 1) * L::one : 0);
+    if constexpr (L::nbuf == 1) {
+      __syncthreads();
+      load(ch);
+    }
+    vm_wait_all();
+    __syncthreads();
+    if (L::nbuf == 2 && ch + 1 < nch) load(ch + 1);
+    if (ch > 0) store_o(ch - 1);
     if (a.S_chunks) {
-      float* s = a.S_chunks + sh * sm + soff;
+      float* s = a.S_chunks + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * sm + soff;
 #pragma unroll
-      for (int p = 0; p < NP; ++p) {
-        *reinterpret_cast<f32x4*>(s + 32 * p) = S[2 * p];
-        *reinterpret_cast<f32x4*>(s + 32 * p + 4) = S[2 * p + 1];
-      }
+      for (int j = 0; j < 2 * NP; ++j) *reinterpret_cast<f32x4*>(s + 16 * j) = S[j];
     }
-    // keys into LDS, for the state update
-    if (NBUF == 1 && ch > 0) __syncthreads();
-    for (int x = tid; x < kGdrC * NP * 4; x += 128) {
-      const int r = x / (NP * 4), pq = x % (NP * 4);
-      Rows::put(sK, r, pq >> 2, pq & 3, ld_fr<T>(k + (size_t)(t0 + r) * a.ks[1] + 8 * pq, r < len));
-    }
-    Fi<T> Sf[NP];
+    const char* img = buf + L::I;
+    const float* scal = reinterpret_cast<const float*>(img + WS::fScal);
+    Fi<T, kExact> Sf[NP];
 #pragma unroll
-    for (int p = 0; p < NP; ++p) Sf[p] = to_fi<T>(S[2 * p], S[2 * p + 1]);
+    for (int p = 0; p < NP; ++p) Sf[p] = to_fi<T, kExact>(S[2 * p], S[2 * p + 1]);
     // R = beta (V - e^G K S^T), tile by tile of 16 tokens
     f32x4 R[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int r = 16 * i + c;
       f32x4 acc = zero4();
 #pragma unroll
-      for (int p = 0; p < NP; ++p)
-        acc = mma<T>(ld_fr<T>(k + (size_t)(t0 + r) * a.ks[1] + 32 * p + 8 * g, r < len), Sf[p], acc);
+      for (int p = 0; p < NP; ++p) acc = mma<T>(KR::nat(buf + L::K, i, p, g, c), Sf[p], acc);
       const f32x4 gam = *reinterpret_cast<const f32x4*>(scal + kScGam * kGdrC + 16 * i + 4 * g);
       const f32x4 be = *reinterpret_cast<const f32x4*>(scal + kScBeta * kGdrC + 16 * i + 4 * g);
+      R[i] = be * (Quad<T>::f32(VR::tr(buf + L::V, 16 * i, w, g, c)) - gam * acc);
+    }
+    f32x4 U[4];
+    {
+      const Fi<T, kExact> Rf[2] = {to_fi<T, kExact>(R[0], R[1]), to_fi<T, kExact>(R[2], R[3])};
+      // U = T R
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int t = 16 * i + 4 * g + e;
-        const float vt = t < len ? (float)v[(size_t)(t0 + t) * a.vs[1] + c] : 0.0f;
-        R[i][e] = be[e] * (vt - gam[e] * acc[e]);
+      for (int i = 0; i < 4; ++i) {
+        U[i] = zero4();
+#pragma unroll
+        for (int s = 0; s <= i / 2; ++s)
+          U[i] = mma<T>(ld_img<T, kExact>(img + WS::fT, img_lower(i, s), lane), Rf[s], U[i]);
       }
     }
-    const Fi<T> Rf[2] = {to_fi<T>(R[0], R[1]), to_fi<T>(R[2], R[3])};
-    // U = T R
-    f32x4 U[4];
+    // O^T = scale (e^G (Q S^T)^T + U^T P^T)
+    {
+      const Fi<T, kNear> Uf[2] = {to_fi<T, kNear>(U[0], U[1]), to_fi<T, kNear>(U[2], U[3])};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      U[i] = zero4();
+      for (int i = 0; i < 4; ++i) {
+        f32x4 x = zero4(), y = zero4();
 #pragma unroll
-      for (int s = 0; s <= i / 2; ++s) U[i] = mma<T>(ld_img<T>(ws, img_lower(i, s), lane), Rf[s], U[i]);
-    }
-    const Fi<T> Uf[2] = {to_fi<T>(U[0], U[1]), to_fi<T>(U[2], U[3])};
-    // O^T = scale (e^G (Q S^T)^T + U^T P^T): a lane holds four values of token 16 i + c
+        for (int p = 0; p < NP; ++p) x = mma<T>(first<kNear>(Sf[p]), KR::nat(buf + L::Q, i, p, g, c), x);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = 16 * i + c;
-      f32x4 x = zero4(), y = zero4();
-#pragma unroll
-      for (int p = 0; p < NP; ++p)
-        x = mma<T>(Sf[p], ld_fr<T>(q + (size_t)(t0 + r) * a.qs[1] + 32 * p + 8 * g, r < len), x);
-#pragma unroll
-      for (int s = 0; s <= i / 2; ++s) y = mma<T>(Uf[s], ld_img<T>(ws + kGdrImg, img_lower(i, s), lane), y);
-      const float gam = scal[kScGam * kGdrC + r];
-      if (r < len) Quad<T>::st(o + (size_t)(t0 + r) * a.Hv * a.Dv + 4 * g, Quad<T>::cvt((x * gam + y) * a.scale));
+        for (int s = 0; s <= i / 2; ++s)
+          y = mma<T>(Uf[s], ld_img<T, kNear>(img + WS::fP, img_lower(i, s), lane), y);
+        oq[i] = Quad<T>::cvt((x * scal[kScGam * kGdrC + 16 * i + c] + y) * a.scale);
+      }
     }
     // S^T <- e^{G_C} S^T + K^T (e^{G_C - G} U)
-    __syncthreads();
     const float gend = scal[kScGam * kGdrC + kGdrC - 1];
 #pragma unroll
     for (int i = 0; i < 4; ++i) U[i] *= *reinterpret_cast<const f32x4*>(scal + kScEnd * kGdrC + 16 * i + 4 * g);
-    const Fi<T> Ue[2] = {to_fi<T>(U[0], U[1]), to_fi<T>(U[2], U[3])};
+    const Fi<T, kExact> Ue[2] = {to_fi<T, kExact>(U[0], U[1]), to_fi<T, kExact>(U[2], U[3])};
 #pragma unroll
     for (int j = 0; j < 2 * NP; ++j) {
       S[j] *= gend;
 #pragma unroll
-      for (int s = 0; s < 2; ++s) S[j] = mma<T>(Rows::frag(sK, s, j >> 1, j & 1, g, c), Ue[s], S[j]);
+      for (int s = 0; s < 2; ++s) S[j] = mma<T>(KR::tr32(buf + L::K, s, j, g, c), Ue[s], S[j]);
     }
   }
+  if (nch > 0) store_o(nch - 1);
   if (a.S_T) {
     float* s = a.S_T + (size_t)head * sm + soff;
 #pragma unroll
-    for (int p = 0; p < NP; ++p) {
-      *reinterpret_cast<f32x4*>(s + 32 * p) = S[2 * p];
-      *reinterpret_cast<f32x4*>(s + 32 * p + 4) = S[2 * p + 1];
-    }
+    for (int j = 0; j < 2 * NP; ++j) *reinterpret_cast<f32x4*>(s + 16 * j) = S[j];
   }
 }
 
@@ -314,15 +328,25 @@ int launch_prep_t(const GdrArgs& a, bool bwd, hipStream_t s) {
   else hipLaunchKernelGGL((carve_gdr_prep_kernel<T, DK, false>), grid, dim3(256), 0, s, a);
   return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
 }
+template <typename T, int DK, int NW>
+int launch_chain_t(const GdrArgs& a, hipStream_t s) {
+  constexpr int lds = ChainLds<T, DK, NW>::total;
+  static_assert(lds <= 160 * 1024, "LDS");
+  const auto kern = carve_gdr_chain_kernel<T, DK, NW>;
+  if (hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
+    return CARVE_ERR_HIP;
+  const unsigned heads = (unsigned)a.nseq * a.Hv;
+  hipLaunchKernelGGL(kern, dim3((heads + 7) / 8 * 8 * (a.Dv / (16 * NW))), dim3(64 * NW), lds, s, a);
+  return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
+}
 template <typename T, int DK>
 int launch_fwd_t(const GdrArgs& a, hipStream_t s, void (*mark)(hipStream_t)) {
-  const int st = launch_prep_t<T, DK>(a, false, s);
+  int st = launch_prep_t<T, DK>(a, false, s);
   if (st) return st;
   mark(s);
-  const unsigned heads = (unsigned)a.nseq * a.Hv;
-  hipLaunchKernelGGL((carve_gdr_chain_kernel<T, DK>), dim3((heads + 7) / 8 * 8 * (a.Dv / 32)), dim3(128), 0, s, a);
+  st = gdr_chain_waves(a) == 4 ? launch_chain_t<T, DK, 4>(a, s) : launch_chain_t<T, DK, 2>(a, s);
   mark(s);
-  return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
+  return st;
 }
 
 }  // namespace
