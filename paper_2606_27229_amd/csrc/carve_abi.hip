@@ -664,7 +664,7 @@ size_t carve_gdr_workspace_size(const carve_gdr_dims_t* d, int for_backward) {
   if (check_gdr(d) != CARVE_OK) return 0;
   const size_t n = gdr_chunks(d);
   const size_t images = align256(n * d->Hv * gdr_per(d, for_backward != 0));
-  return for_backward ? images + n * gdr_state(d) : images;
+  return for_backward ? images + n * gdr_state(d) + n * d->Hv * d->Dv * kGdrC * 4 : images;
 }
 
 int carve_gdr_chunk_fwd(const carve_gdr_dims_t* d, const void* q, const void* k, const void* v, const float* g,
@@ -730,6 +730,7 @@ int carve_gdr_chunk_bwd(const carve_gdr_dims_t* d, const void* q, const void* k,
   gdr_args(a, d, q, k, v, g, beta, offsets, workspace, true);
   a.S_chunks = const_cast<float*>(S_chunks);   // (read only)
   a.dS_chunks = reinterpret_cast<float*>(a.ws + align256(gdr_chunks(d) * d->Hv * gdr_per(d, true)));
+  a.dR = a.dS_chunks + gdr_chunks(d) * (gdr_state(d) / 4);
   a.dO = dO, a.dS_T = dS_T, a.dq = dq, a.dk = dk, a.dv = dv, a.dg = dg, a.dbeta = dbeta, a.dS0 = dS0;
   prof_mark(stream);
   return launch_gdr_bwd(a, d->dtype, stream, prof_mark);

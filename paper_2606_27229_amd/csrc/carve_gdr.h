@@ -35,6 +35,7 @@ struct GdrArgs {
   float *S_T, *S_chunks, *dg, *dS0;
   char* ws;                // images and scalars of every (chunk slot, value head)
   float* dS_chunks;        // [nslots][Hv][Dv][Dk]: the state gradients at chunk ends (backward)
+  float* dR;               // [nslots][Hv][Dv / 16][4][64][4]: dR as result tiles (backward)
   long long qs[3], ks[3], vs[3];   // strides of batch, token, head
   int T, Hk, Hv, Dk, Dv, nseq, nslots, per;   // per: bytes of one (slot, head) in ws
   float scale;
@@ -227,16 +228,24 @@ __device__ __forceinline__ void st_img(char* img, int f, int lane, f32x4 a, f32x
   }
 }
 // one (slot, head) of the workspace.  Forward: T, P (towards o), scalars; backward: T,
-// P^T, T^T, scalars
+// scalars, P^T, T^T
 template <typename T>
 struct GdrWs {
   static constexpr int I3 = img_bytes<T>(kExact), I2 = img_bytes<T>(kNear);
   static constexpr int fT = 0, fP = I3, fScal = I3 + I2, fBytes = I3 + I2 + kGdrScal;
-  static constexpr int bT = 0, bPt = I3, bTt = 2 * I3, bScal = 3 * I3, bBytes = 3 * I3 + kGdrScal;
+  static constexpr int bT = 0, bScal = I3, bPt = bScal + kGdrScal, bTt = bPt + I3, bBytes = bTt + I3;
 };
 
 // scalars [5][64] of a chunk: e^G, e^{G_C - G}, beta, and G as a sum of two floats
 enum : int { kScGam = 0, kScEnd = 1, kScBeta = 2, kScGh = 3, kScGl = 4 };
+
+// lane coordinates the compiler takes as new: what is computed from them is computed
+// where it is used, not ahead of a loop and kept
+__device__ __forceinline__ void renew(int& g, int& c) { asm volatile("" : "+v"(g), "+v"(c)); }
+
+// an LDS address as the direct loads take it (the low half of the generic address)
+typedef __attribute__((address_space(3))) void* lds_ptr;
+__device__ __forceinline__ lds_ptr lds_at(const char* p) { return (lds_ptr)(uintptr_t)(unsigned)(uintptr_t)p; }
 
 // ---- token rows in LDS ------------------------------------------------------------------
 // A [64][COLS] token tile loaded straight into LDS (16 bytes a lane, no registers):
@@ -263,7 +272,7 @@ struct GdrRows {
     for (int i = 0; i < bytes / 1024; ++i) {
       if (i % nw != w) continue;     // (uniform)
       const int row = i * RPI + lane / NCH, x = (lane % NCH) ^ swz(row);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + 1024 * i), 16,
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, lds_at(lds + 1024 * i), 16,
                                                (int)__umul24(min(row, len - 1), stride) + 16 * x, 0, 0, 0);
     }
   }
@@ -310,7 +319,7 @@ __device__ __forceinline__ void dma_flat(char* lds, const char* src, int bytes, 
 #pragma unroll
   for (int i = 0; i < bytes / 1024; ++i) {
     if (i % nw != w) continue;   // (uniform)
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + 1024 * i), 16,
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, lds_at(lds + 1024 * i), 16,
                                              1024 * i + 16 * lane, 0, 0, 0);
   }
 }

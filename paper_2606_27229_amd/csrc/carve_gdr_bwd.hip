@@ -25,7 +25,7 @@ template <typename T, int DK, int NW>
 struct BChainLds {
   typedef GdrRows<T, DK> KR;
   typedef GdrRows<T, 16 * NW> VR;
-  static constexpr int img = GdrWs<T>::bBytes - GdrWs<T>::bPt;   // P^T, T^T, scalars
+  static constexpr int img = GdrWs<T>::bBytes - GdrWs<T>::bScal;   // scalars, P^T, T^T
   static constexpr int K = 0, Q = K + KR::bytes, O = Q + KR::bytes, I = O + VR::bytes;
   static constexpr int one = I + img;
   static constexpr int nbuf = 2 * one <= 160 * 1024 ? 2 : 1;
@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(64 * NW, 1) carve_gdr_bchain_kernel(GdrArgs a)
     char* buf = smem + (L::nbuf == 2 ? (ch & 1) * L::one : 0);
     const int t0 = ch * kGdrC, len = min(kGdrC, sq.len - t0);
     KR::dma(buf + L::K, k + t0 * a.ks[1], (int)(a.ks[1] * sizeof(T)), len, w, NW, lane);
-    dma_flat(buf + L::I, a.ws + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * a.per + WS::bPt, L::img, w, NW, lane);
+    dma_flat(buf + L::I, a.ws + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * a.per + WS::bScal, L::img, w, NW, lane);
     VR::dma(buf + L::O, dO + t0 * ors, (int)(ors * sizeof(T)), len, w, NW, lane);
     KR::dma(buf + L::Q, q + t0 * a.qs[1], (int)(a.qs[1] * sizeof(T)), len, w, NW, lane);
   };
@@ -84,7 +84,7 @@ __global__ void __launch_bounds__(64 * NW, 1) carve_gdr_bchain_kernel(GdrArgs a)
       for (int j = 0; j < 2 * NP; ++j) *reinterpret_cast<f32x4*>(s + 16 * j) = S[j];
     }
     const char* img = buf + L::I;
-    const float* scal = reinterpret_cast<const float*>(img + (WS::bScal - WS::bPt));
+    const float* scal = reinterpret_cast<const float*>(img);
     const int len = sq.len - ch * kGdrC;
     // dO[t][v] of this wave's columns, zeros behind the last token
     Fr<T> of[2] = {VR::tr32(buf + L::O, 0, w, g, c), VR::tr32(buf + L::O, 1, w, g, c)};
@@ -107,21 +107,23 @@ __global__ void __launch_bounds__(64 * NW, 1) carve_gdr_bchain_kernel(GdrArgs a)
 #pragma unroll
       for (int p = 0; p < NP; ++p) y = mma<T>(KR::nat(buf + L::K, i, p, g, c), Sf[p], y);
 #pragma unroll
-      for (int s = i / 2; s < 2; ++s) x = mma<T>(ld_img<T, kExact>(img, img_upper(i, s), lane), of[s], x);
+      for (int s = i / 2; s < 2; ++s) x = mma<T>(ld_img<T, kExact>(img + (WS::bPt - WS::bScal), img_upper(i, s), lane), of[s], x);
       const f32x4 end = *reinterpret_cast<const f32x4*>(scal + kScEnd * kGdrC + 16 * i + 4 * g);
       U[i] = x * a.scale + y * end;
     }
     const Fi<T, kExact> Uf[2] = {to_fi<T, kExact>(U[0], U[1]), to_fi<T, kExact>(U[2], U[3])};
-    // - beta e^G dR, dR = T^T dU, and e^G dO'
+    // - beta e^G dR, dR = T^T dU (kept for the chunk's gradients), and e^G dO'
     f32x4 R[4], od[4];
+    float* keep = a.dR + (((size_t)(sq.slot0 + ch) * a.Hv + hv) * (a.Dv / 16) + v0 / 16) * 1024 + 4 * lane;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       f32x4 x = zero4();
 #pragma unroll
       for (int s = i / 2; s < 2; ++s)
-        x = mma<T>(ld_img<T, kExact>(img + (WS::bTt - WS::bPt), img_upper(i, s), lane), Uf[s], x);
+        x = mma<T>(ld_img<T, kExact>(img + (WS::bTt - WS::bScal), img_upper(i, s), lane), Uf[s], x);
       const f32x4 gam = *reinterpret_cast<const f32x4*>(scal + kScGam * kGdrC + 16 * i + 4 * g);
       const f32x4 be = *reinterpret_cast<const f32x4*>(scal + kScBeta * kGdrC + 16 * i + 4 * g);
+      *reinterpret_cast<f32x4*>(keep + 256 * i) = x;
       R[i] = -(x * gam * be);
       od[i] = Quad<T>::f32(i % 2 ? of[i / 2].b : of[i / 2].a) * (gam * a.scale);
     }
@@ -147,250 +149,286 @@ __global__ void __launch_bounds__(64 * NW, 1) carve_gdr_bchain_kernel(GdrArgs a)
 
 // ---------------------------------------------------------------------------------
 // Gradients of one chunk and key head (its value heads one after another, dq and dk
-// summed in registers).  Eight waves, per value head and block of 128 value columns:
-//   1. wave w: value columns 16 w ..: U and dR again from S and dS (both read here
-//      once as B operands), into LDS transposed; dV; <dS, S>; dR.V
+// summed in registers).  Eight waves, per value head and block of VB value columns:
+//   1. wave w: value columns 16 w ..: U again from S, beside dR from the chain; both
+//      into LDS as pieces, transposed; sums over the value columns
 //   2. products over the value columns: dP and dA, tile by tile (lower tiles only),
 //      and dO' S, U dS, dR S for the wave's key columns
 // then, all columns done, D dP and M through LDS into dQ and dK.
-constexpr int kVB = 128;   // value columns of a block
+// dg is an f32 result: what reaches it (dP, dA, dO' S and U dS by their sums with q
+// and k) is taken in three pieces; k.(dR S) is dR.(S k), summed where S k is at hand,
+// so that dR S itself only reaches dk and is taken in two.
+// LDS: U and dR in three pieces fill 96 KB at 128 columns, so the rest shares places:
+// the values lie where U goes, the queries where T was.
 
-// [columns][tokens] tiles of an f32 intermediate in LDS
-template <typename T>
+// [VB columns][64 tokens] of an f32 intermediate in LDS
+template <typename T, int VB>
 struct InterT {
-  static constexpr int LD = sizeof(T) == 2 ? kGdrC + 16 : kGdrC + 4;
-  static __host__ __device__ constexpr int bytes(int cols, int n) { return cols * LD * (sizeof(T) == 2 ? 2 * n : 4); }
+  static constexpr int LD = sizeof(T) == 2 ? kGdrC : kGdrC + 4;
+  static constexpr int plane = VB * LD;
+  static __host__ __device__ constexpr int bytes(int n) { return plane * (sizeof(T) == 2 ? 2 * n : 4); }
+  // bf16 rows of 64 elements: quad y of column r at quad y ^ sw(r), which spreads the
+  // 16 columns of a quad write or read, and the 8 columns x 4 quads of a read across
+  // columns, over all banks
+  static __device__ __forceinline__ int sw(int r) { return (((r >> 1) & 3) << 2) | (((r >> 3) & 1) << 1) | (r & 1); }
   // the four tokens 16 i + 4 g .. of column col, in N pieces
   template <int N>
-  static __device__ __forceinline__ void put(char* m, int cols, int col, int i, int g, f32x4 x) {
-    T* p = reinterpret_cast<T*>(m) + col * LD + 16 * i;
+  static __device__ __forceinline__ void put(char* m, int col, int i, int g, f32x4 x) {
+    T* p = reinterpret_cast<T*>(m) + col * LD;
     if constexpr (sizeof(T) == 2) {
+      p += 4 * ((4 * i + g) ^ sw(col));
 #pragma unroll
       for (int y = 0; y < N; ++y) {
         const typename Quad<T>::q h = Quad<T>::cvt(x);
-        Quad<T>::st(p + y * cols * LD + ((4 * g) ^ qswz<T>(col)), h);
-        x -= Quad<T>::f32(h);
+        Quad<T>::st(p + y * plane, h);
+        if (y + 1 < N) x -= Quad<T>::f32(h);
       }
     } else {
-      Quad<T>::st(p + 4 * g, x);
+      Quad<T>::st(p + 16 * i + 4 * g, x);
     }
   }
   // lane (g, c): token 16 i + c, columns col0 + 4 g + e and col0 + 16 + 4 g + e
   template <int N>
-  static __device__ __forceinline__ Fi<T, N> tok(const char* m, int cols, int i, int col0, int g, int c) {
+  static __device__ __forceinline__ Fi<T, N> tok(const char* m, int i, int col0, int g, int c) {
     const T* p = reinterpret_cast<const T*>(m);
     Fi<T, N> f;
+    if constexpr (sizeof(T) == 2) {
+      const int r = 4 * g + (c >> 2);
+      p += (col0 + r) * LD + 4 * ((4 * i + (c & 3)) ^ sw(r));
 #pragma unroll
-    for (int y = 0; y < (sizeof(T) == 2 ? N : 1); ++y) {
-      f.x[y].a = Quad<T>::ld_tr_sw(p + y * cols * LD, LD, col0, 16 * i, g, c);
-      f.x[y].b = Quad<T>::ld_tr_sw(p + y * cols * LD, LD, col0 + 16, 16 * i, g, c);
+      for (int y = 0; y < N; ++y) {
+        f.x[y].a = Quad<T>::ld_tr_at(p + y * plane);
+        f.x[y].b = Quad<T>::ld_tr_at(p + y * plane + 16 * LD);
+      }
+    } else {
+      f.x[0].a = Quad<T>::ld_tr(p, LD, col0, 16 * i, g, c);
+      f.x[0].b = Quad<T>::ld_tr(p, LD, col0 + 16, 16 * i, g, c);
     }
     return f;
   }
   // lane (g, c): column col0 + c, tokens 32 s + 4 g + e and 32 s + 16 + 4 g + e
   template <int N>
-  static __device__ __forceinline__ Fi<T, N> col(const char* m, int cols, int col0, int s, int g, int c) {
-    const T* p = reinterpret_cast<const T*>(m) + (col0 + c) * LD + 32 * s + ((4 * g) ^ qswz<T>(col0 + c));
+  static __device__ __forceinline__ Fi<T, N> col(const char* m, int col0, int s, int g, int c) {
+    const T* p = reinterpret_cast<const T*>(m) + (col0 + c) * LD;
     Fi<T, N> f;
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int y = 0; y < (sizeof(T) == 2 ? N : 1); ++y) {
-      f.x[y].a = Quad<T>::ld(p + y * cols * LD);
-      f.x[y].b = Quad<T>::ld(p + y * cols * LD + 16);
+      for (int y = 0; y < N; ++y) {
+        f.x[y].a = Quad<T>::ld(p + y * plane + 4 * ((8 * s + g) ^ sw(c)));
+        f.x[y].b = Quad<T>::ld(p + y * plane + 4 * ((8 * s + 4 + g) ^ sw(c)));
+      }
+    } else {
+      f.x[0].a = Quad<T>::ld(p + 32 * s + 4 * g);
+      f.x[0].b = Quad<T>::ld(p + 32 * s + 16 + 4 * g);
     }
     return f;
   }
 };
 
-template <typename T>
+template <typename T, int DK, int VB>
 struct GradLds {
-  static constexpr int U = 0;
-  static constexpr int R = U + InterT<T>::bytes(kVB, kExact);
-  static constexpr int red = R + InterT<T>::bytes(kVB, kExact);
-  static constexpr int W = 0;                                      // (D dP)^T: [j][i], over U
-  static constexpr int M = W + InterT<T>::bytes(kGdrC, kNear);     // M^T: [j][i]
-  // sums over values or keys: [wave][64] of dR.V, q.(dO' S), k.(U dS), k.(dR S), then
-  // <dS, S> per wave; sums over tiles: [4][64] of rows of dP P + dA A, rows of dA A /
-  // beta, columns of dP P + dA A; decays and beta
-  static constexpr int floats = 4 * 8 * kGdrC + 8 + 3 * 4 * kGdrC + 3 * kGdrC;
+  typedef GdrRows<T, DK> KR;
+  typedef GdrRows<T, VB> VR;
+  typedef InterT<T, VB> UT;
+  typedef InterT<T, kGdrC> WT;
+  static constexpr int U = 0, R = U + UT::bytes(kExact), V = U;
+  static constexpr int W = U, M = W + WT::bytes(kNear);       // (D dP)^T, M^T: [j][i], over U and dR
+  static constexpr int ur = 2 * UT::bytes(kExact) > 2 * WT::bytes(kNear) ? 2 * UT::bytes(kExact) : 2 * WT::bytes(kNear);
+  static constexpr int K = ur > VR::bytes ? ur : VR::bytes;
+  static constexpr int O = K + KR::bytes;
+  static constexpr int scal = O + VR::bytes;
+  static constexpr int Z = scal + kGdrScal;                    // T, then Q
+  static constexpr int red = Z + (KR::bytes > GdrWs<T>::I3 ? KR::bytes : GdrWs<T>::I3);
+  // sums over values, [wave][64]: dR.(V - e^G S k), dR.(e^G S k); over keys, [key tile]
+  // [64]: q.(dO' S), k.(U dS); <dS, S> per wave; over tiles, [4][64]: rows of dP P + dA
+  // A, rows of dA A / beta, columns of dP P + dA A
+  static constexpr int floats = 4 * 8 * kGdrC + 8 + 3 * 4 * kGdrC;
   static constexpr int total = red + floats * 4;
 };
 
-template <typename T, int DK>
+template <typename T, int DK, int VB>
 __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
-  typedef InterT<T> IT;
-  typedef GradLds<T> L;
+  typedef GradLds<T, DK, VB> L;
+  typedef typename L::KR KR;
+  typedef typename L::VR VR;
+  typedef typename L::UT UT;
+  typedef typename L::WT WT;
   constexpr int NP = DK / 32;
   constexpr int NJ = DK / 16;      // key tiles
   constexpr int NI = NJ / 2;       // row tiles of a wave in the products over key columns
+  constexpr int NV = VB / 32;
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  float* red = reinterpret_cast<float*>(smem + L::red);
-  float* rRV = red;                        // [8][64]
-  float* rQ = rRV + 8 * kGdrC;             // [8][64]
+  const float* scal = reinterpret_cast<const float*>(smem + L::scal);
+  float* rRV = reinterpret_cast<float*>(smem + L::red);   // [8][64]
+  float* rRK = rRV + 8 * kGdrC;            // [8][64]
+  float* rQ = rRK + 8 * kGdrC;             // [8][64]
   float* rUK = rQ + 8 * kGdrC;             // [8][64]
-  float* rRK = rUK + 8 * kGdrC;            // [8][64]
-  float* rSS = rRK + 8 * kGdrC;            // [8]
+  float* rSS = rUK + 8 * kGdrC;            // [8]
   float* rRow = rSS + 8;                   // [4][64]
   float* rBeta = rRow + 4 * kGdrC;         // [4][64]
   float* rCol = rBeta + 4 * kGdrC;         // [4][64]
-  float* sGh = rCol + 4 * kGdrC;           // [64]
-  float* sGl = sGh + kGdrC;
-  float* sBe = sGl + kGdrC;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int g = lane >> 4, c = lane & 15;
+  int g = lane >> 4, c = lane & 15;
   const int slot = blockIdx.x, hk = blockIdx.y, grp = a.Hv / a.Hk;
   GdrSeq sq;
   int n, chunk;
   if (!gdr_find(a, slot, sq, n, chunk)) return;   // (uniform)
   const int t0 = sq.t0 + chunk * kGdrC, len = min(kGdrC, sq.len - chunk * kGdrC);
-  const T* q = reinterpret_cast<const T*>(a.q) + sq.batch * a.qs[0] + t0 * a.qs[1] + hk * a.qs[2];
-  const T* k = reinterpret_cast<const T*>(a.k) + sq.batch * a.ks[0] + t0 * a.ks[1] + hk * a.ks[2];
   const size_t row0 = (size_t)sq.batch * a.T + t0;
   const size_t sm = (size_t)a.Dv * DK;
   const size_t ors = (size_t)a.Hv * a.Dv;
+  const T* q = reinterpret_cast<const T*>(a.q) + sq.batch * a.qs[0] + t0 * a.qs[1] + hk * a.qs[2];
+  KR::dma(smem + L::K, reinterpret_cast<const T*>(a.k) + sq.batch * a.ks[0] + t0 * a.ks[1] + hk * a.ks[2],
+          (int)(a.ks[1] * sizeof(T)), len, w, 8, lane);
 
   // this wave's key tile and row tiles
   const int jt = w % NJ, i0 = NI * (w / NJ);
   f32x4 dQ[NI], dK[NI];
 #pragma unroll
   for (int i = 0; i < NI; ++i) dQ[i] = dK[i] = zero4();
+
   for (int hv = hk * grp; hv < (hk + 1) * grp; ++hv) {
     const size_t sh = (size_t)slot * a.Hv + hv;
-    const char* ws = a.ws + sh * a.per;
-    const float* scal = reinterpret_cast<const float*>(ws + GdrWs<T>::bScal);
-    const T* v = reinterpret_cast<const T*>(a.v) + sq.batch * a.vs[0] + t0 * a.vs[1] + hv * a.vs[2];
-    const T* dO = reinterpret_cast<const T*>(a.dO) + (row0 * a.Hv + hv) * a.Dv;
-    T* dV = reinterpret_cast<T*>(a.dv) + (row0 * a.Hv + hv) * a.Dv;
-    const float* S = a.S_chunks + sh * sm;
-    const float* dS = a.dS_chunks + sh * sm;
-    if (tid < kGdrC) {
-      sGh[tid] = scal[kScGh * kGdrC + tid];
-      sGl[tid] = scal[kScGl * kGdrC + tid];
-      sBe[tid] = scal[kScBeta * kGdrC + tid];
-    }
     f32x4 aP[2], aA[2];                     // tile tasks w and w + 8 (of ten)
     f32x4 a1[NI], a2[NI], a3[NI];           // dO S, U dS, dR S
 #pragma unroll
     for (int x = 0; x < 2; ++x) aP[x] = aA[x] = zero4();
 #pragma unroll
     for (int i = 0; i < NI; ++i) a1[i] = a2[i] = a3[i] = zero4();
-    float rv[4][4], ss = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) rv[i][e] = 0.0f;
+    float ss = 0.0f;
 
-    for (int vb = 0; vb < a.Dv; vb += kVB) {
-      const int cols = min(kVB, a.Dv - vb);
-      // ---- 1. U, dR of columns vb + 16 w ..
-      if (16 * w < cols) {
-        const int v0 = vb + 16 * w;
-        Fi<T, kExact> Sf[NP], Df[NP];
+#pragma unroll 1
+    for (int vb = 0; vb < a.Dv; vb += VB) {
+      // ---- 1. U and dR of columns vb + 16 w ..
+      renew(g, c);
+      const T* dO = reinterpret_cast<const T*>(a.dO) + (row0 * a.Hv + hv) * a.Dv + vb;
+      VR::dma(smem + L::V, reinterpret_cast<const T*>(a.v) + sq.batch * a.vs[0] + t0 * a.vs[1] + hv * a.vs[2] + vb,
+              (int)(a.vs[1] * sizeof(T)), len, w, 8, lane);
+      VR::dma(smem + L::O, dO, (int)(ors * sizeof(T)), len, w, 8, lane);
+      const char* ws = a.ws + sh * a.per;
+      dma_flat(smem + L::Z, ws + GdrWs<T>::bT, GdrWs<T>::I3, w, 8, lane);
+      dma_flat(smem + L::scal, ws + GdrWs<T>::bScal, kGdrScal, w, 8, lane);
+      const bool mine = 16 * w < VB;   // (uniform)
+      const float* S = a.S_chunks + sh * sm + (size_t)vb * DK;
+      const float* dS = a.dS_chunks + sh * sm + (size_t)vb * DK;
+      f32x4 s[2 * NP], R[4], vt[4];
+      if (mine) {
+        const float* kept = a.dR + (sh * (a.Dv / 16) + vb / 16 + w) * 1024 + 4 * lane;
 #pragma unroll
-        for (int p = 0; p < NP; ++p) {
-          const size_t at = (size_t)(v0 + c) * DK + 32 * p + 8 * g;
-          const f32x4 s0 = *reinterpret_cast<const f32x4*>(S + at), s1 = *reinterpret_cast<const f32x4*>(S + at + 4);
-          const f32x4 d0 = *reinterpret_cast<const f32x4*>(dS + at), d1 = *reinterpret_cast<const f32x4*>(dS + at + 4);
-          for (int e = 0; e < 4; ++e) ss += s0[e] * d0[e] + s1[e] * d1[e];
-          Sf[p] = to_fi<T, kExact>(s0, s1);
-          Df[p] = to_fi<T, kExact>(d0, d1);
-        }
-        f32x4 R[4], U[4], vt[4], od[4];
+        for (int j = 0; j < 2 * NP; ++j) s[j] = *reinterpret_cast<const f32x4*>(S + (16 * w + c) * DK + 16 * j + 4 * g);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i) R[i] = *reinterpret_cast<const f32x4*>(kept + 256 * i);
+      }
+      vm_wait_all();
+      __syncthreads();
+      if (mine) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int t = 16 * i + 4 * g + e;
-            vt[i][e] = t < len ? (float)v[(size_t)t * a.vs[1] + v0 + c] : 0.0f;
-            od[i][e] = t < len ? (float)dO[(size_t)t * ors + v0 + c] : 0.0f;
-          }
-        Fr<T> of[2];
+        for (int i = 0; i < 4; ++i) vt[i] = Quad<T>::f32(VR::tr(smem + L::V, 16 * i, w, g, c));
+      }
+      __syncthreads();   // (U goes where the values were)
+      if (mine) {
+        Fi<T, kExact> Sf[NP];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          of[s].a = Quad<T>::cvt(od[2 * s]);
-          of[s].b = Quad<T>::cvt(od[2 * s + 1]);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = 16 * i + c;
-          f32x4 x = zero4(), y = zero4(), z = zero4();
-#pragma unroll
-          for (int p = 0; p < NP; ++p) {
-            const Fr<T> fk = ld_fr<T>(k + (size_t)r * a.ks[1] + 32 * p + 8 * g, r < len);
-            x = mma<T>(fk, Sf[p], x);
-            y = mma<T>(fk, Df[p], y);
-          }
-#pragma unroll
-          for (int s = i / 2; s < 2; ++s) z = mma<T>(ld_img<T, kExact>(ws + GdrWs<T>::bPt, img_upper(i, s), lane), of[s], z);
-          const f32x4 gam = *reinterpret_cast<const f32x4*>(scal + kScGam * kGdrC + 16 * i + 4 * g);
-          const f32x4 end = *reinterpret_cast<const f32x4*>(scal + kScEnd * kGdrC + 16 * i + 4 * g);
-          const f32x4 be = *reinterpret_cast<const f32x4*>(scal + kScBeta * kGdrC + 16 * i + 4 * g);
-          R[i] = be * (vt[i] - gam * x);
-          U[i] = z * a.scale + y * end;      // dU
-        }
-        const Fi<T, kExact> Rf[2] = {to_fi<T, kExact>(R[0], R[1]), to_fi<T, kExact>(R[2], R[3])};
-        const Fi<T, kExact> Uf[2] = {to_fi<T, kExact>(U[0], U[1]), to_fi<T, kExact>(U[2], U[3])};
+        for (int p = 0; p < NP; ++p) Sf[p] = to_fi<T, kExact>(s[2 * p], s[2 * p + 1]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          f32x4 x = zero4(), y = zero4();
+          f32x4 x = zero4();
 #pragma unroll
-          for (int s = 0; s <= i / 2; ++s) x = mma<T>(ld_img<T, kExact>(ws, img_lower(i, s), lane), Rf[s], x);
-#pragma unroll
-          for (int s = i / 2; s < 2; ++s) y = mma<T>(ld_img<T, kExact>(ws + GdrWs<T>::bTt, img_upper(i, s), lane), Uf[s], y);
-          IT::template put<kExact>(smem + L::U, kVB, 16 * w + c, i, g, x);
-          IT::template put<kExact>(smem + L::R, kVB, 16 * w + c, i, g, y);
+          for (int p = 0; p < NP; ++p) x = mma<T>(KR::nat(smem + L::K, i, p, g, c), Sf[p], x);
+          x *= *reinterpret_cast<const f32x4*>(scal + kScGam * kGdrC + 16 * i + 4 * g);
           const f32x4 be = *reinterpret_cast<const f32x4*>(scal + kScBeta * kGdrC + 16 * i + 4 * g);
+          vt[i] -= x;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int t = 16 * i + 4 * g + e;
-            rv[i][e] += y[e] * vt[i][e];
-            if (t < len) dV[(size_t)t * ors + v0 + c] = (T)(be[e] * y[e]);
+            const int at = w * kGdrC + 16 * i + 4 * g + e;
+            const float s1 = group_sum<16>(R[i][e] * vt[i][e]), s2 = group_sum<16>(R[i][e] * x[e]);
+            if (c == 0) {
+              rRV[at] = vb ? rRV[at] + s1 : s1;
+              rRK[at] = vb ? rRK[at] + s2 : s2;
+            }
           }
+          vt[i] *= be;
+          UT::template put<kExact>(smem + L::R, 16 * w + c, i, g, R[i]);
+        }
+        const Fi<T, kExact> Rf[2] = {to_fi<T, kExact>(vt[0], vt[1]), to_fi<T, kExact>(vt[2], vt[3])};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          f32x4 x = zero4();
+#pragma unroll
+          for (int y = 0; y <= i / 2; ++y)
+            x = mma<T>(ld_img<T, kExact>(smem + L::Z, img_lower(i, y), lane), Rf[y], x);
+          UT::template put<kExact>(smem + L::U, 16 * w + c, i, g, x);
         }
       }
       __syncthreads();
-      // ---- 2. products over these columns
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int y = w + 8 * x;
-        if (y < 10) {
-          const int i = tri_row_of(y, false), j = tri_col_of(y, false), r = 16 * i + c;
-          for (int p = 0; p < cols / 32; ++p) {
-            const Fi<T, kExact> fu = IT::template tok<kExact>(smem + L::U, kVB, j, 32 * p, g, c);
-            aP[x] = mma<T>(ld_fr16<T>(dO + (size_t)r * ors + vb + 32 * p + 4 * g, r < len), fu, aP[x]);
-            aA[x] = mma<T>(IT::template tok<kExact>(smem + L::R, kVB, i, 32 * p, g, c), fu, aA[x]);
-          }
-        }
-      }
-      for (int p = 0; p < cols / 32; ++p) {
-        f32x4 s[2], d[2];
+      // ---- 2. products over these columns (queries on their way)
+      renew(g, c);
+      if (vb + VB >= a.Dv) KR::dma(smem + L::Z, q, (int)(a.qs[1] * sizeof(T)), len, w, 8, lane);
+      f32x4 sn[2], dn[2];   // S, dS of the next 32 value columns
+      const auto columns = [&](int p) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const size_t at = (size_t)(vb + 32 * p + 16 * h + 4 * g + e) * DK + 16 * jt + c;
-            s[h][e] = S[at];
-            d[h][e] = dS[at];
+            const int at = (32 * p + 16 * h + 4 * g + e) * DK + 16 * jt + c;
+            sn[h][e] = S[at];
+            dn[h][e] = dS[at];
           }
-        const Fi<T, kExact> fs = to_fi<T, kExact>(s[0], s[1]), fd = to_fi<T, kExact>(d[0], d[1]);
+      };
+      columns(0);
+#pragma unroll 1
+      for (int p = 0; p < NV; ++p) {
+        const Fi<T, kExact> fs = to_fi<T, kExact>(sn[0], sn[1]), fd = to_fi<T, kExact>(dn[0], dn[1]);
+        if (w < NJ)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) ss += sn[h][e] * dn[h][e];
+        if (p + 1 < NV) columns(p + 1);
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-          const int r = 16 * (i0 + i) + c;
-          a1[i] = mma<T>(ld_fr16<T>(dO + (size_t)r * ors + vb + 32 * p + 4 * g, r < len), fs, a1[i]);
-          a2[i] = mma<T>(IT::template tok<kExact>(smem + L::U, kVB, i0 + i, 32 * p, g, c), fd, a2[i]);
-          a3[i] = mma<T>(IT::template tok<kExact>(smem + L::R, kVB, i0 + i, 32 * p, g, c), fs, a3[i]);
+          a1[i] = mma<T>(VR::nat(smem + L::O, i0 + i, p, g, c), fs, a1[i]);
+          a2[i] = mma<T>(UT::template tok<kExact>(smem + L::U, i0 + i, 32 * p, g, c), fd, a2[i]);
+          a3[i] = mma<T>(UT::template tok<kNear>(smem + L::R, i0 + i, 32 * p, g, c), first<kNear>(fs), a3[i]);
         }
       }
+      renew(g, c);
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int y = w + 8 * x;
+        if (y < 10) {
+          const int i = tri_row_of(y, false), j = tri_col_of(y, false);
+#pragma unroll 1
+          for (int p = 0; p < NV; ++p) {
+            const Fi<T, kExact> fu = UT::template tok<kExact>(smem + L::U, j, 32 * p, g, c);
+            aP[x] = mma<T>(VR::nat(smem + L::O, i, p, g, c), fu, aP[x]);
+            aA[x] = mma<T>(UT::template tok<kExact>(smem + L::R, i, 32 * p, g, c), fu, aA[x]);
+          }
+        }
+      }
+      // dV = beta dR, four values of a token a lane
+      for (int x = w; x < 4 * NV; x += 8) {
+        const int i = x & 3, p = x >> 2, t = 16 * i + c;
+        const Fi<T, kExact> f = UT::template tok<kExact>(smem + L::R, i, 32 * p, g, c);
+        f32x4 lo = zero4(), hi = zero4();
+#pragma unroll
+        for (int y = (sizeof(T) == 2 ? kExact : 1) - 1; y >= 0; --y) {
+          lo += Quad<T>::f32(f.x[y].a);
+          hi += Quad<T>::f32(f.x[y].b);
+        }
+        if (t < len) {
+          const float be = scal[kScBeta * kGdrC + t];
+          T* d = reinterpret_cast<T*>(a.dv) + ((row0 + t) * a.Hv + hv) * a.Dv + vb + 32 * p + 4 * g;
+          Quad<T>::st(d, Quad<T>::cvt(lo * be));
+          Quad<T>::st(d + 16, Quad<T>::cvt(hi * be));
+        }
+      }
+      if (vb + VB >= a.Dv) vm_wait_all();
       __syncthreads();
     }
 
-    // ---- sums over the value columns and <dS, S>
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float x = group_sum<16>(rv[i][e]);
-        if (c == 0) rRV[w * kGdrC + 16 * i + 4 * g + e] = x;
-      }
+    // ---- <dS, S>
+    renew(g, c);
     ss = group_sum<64>(ss);
     if (lane == 0) rSS[w] = ss;
 
@@ -398,33 +436,35 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
     // upper tiles (0, 1) and (2, 3), which the fragments reach
     if (w >= 4) {
       const int y = w - 4;
-      IT::template put<kNear>(smem + (y & 1 ? L::M : L::W), kGdrC, 16 * (y < 2 ? 1 : 3) + c, y < 2 ? 0 : 2, g, zero4());
+      WT::template put<kNear>(smem + (y & 1 ? L::M : L::W), 16 * (y < 2 ? 1 : 3) + c, y < 2 ? 0 : 2, g, zero4());
     }
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       const int y = w + 8 * x;
       if (y < 10) {
-        const int i = tri_row_of(y, false), j = tri_col_of(y, false), r = 16 * i + c, rj = 16 * j + c;
+        const int i = tri_row_of(y, false), j = tri_col_of(y, false), tj = 16 * j + c;
         f32x4 qk = zero4(), kk = zero4();
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
-          const Fr<T> fb = ld_fr<T>(k + (size_t)rj * a.ks[1] + 32 * p + 8 * g, rj < len);
-          qk = mma<T>(ld_fr<T>(q + (size_t)r * a.qs[1] + 32 * p + 8 * g, r < len), fb, qk);
-          kk = mma<T>(ld_fr<T>(k + (size_t)r * a.ks[1] + 32 * p + 8 * g, r < len), fb, kk);
+          const Fr<T> fb = KR::nat(smem + L::K, j, p, g, c);
+          qk = mma<T>(KR::nat(smem + L::Z, i, p, g, c), fb, qk);
+          kk = mma<T>(KR::nat(smem + L::K, i, p, g, c), fb, kk);
         }
+        const float Ghj = scal[kScGh * kGdrC + tj], Glj = scal[kScGl * kGdrC + tj];
         f32x4 W, M;
         float col = 0.0f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int ti = 16 * i + 4 * g + e, tj = 16 * j + c;
+          const int ti = 16 * i + 4 * g + e;
           float D = 0.0f;
-          if (tj <= ti) D = expf((sGh[ti] - sGh[tj]) + (sGl[ti] - sGl[tj]));
-          const float be = sBe[ti], dA = tj < ti ? -aA[x][e] : 0.0f;
+          if (tj <= ti && ti < len) D = expf((scal[kScGh * kGdrC + ti] - Ghj) + (scal[kScGl * kGdrC + ti] - Glj));
+          const float be = scal[kScBeta * kGdrC + ti], dA = tj < ti ? -aA[x][e] : 0.0f;
           W[e] = a.scale * (D * aP[x][e]);
           M[e] = be * (D * dA);
-          const float pp = W[e] * qk[e], ab = D * dA * kk[e], s = pp + be * ab;
-          col += s;
-          const float rs = group_sum<16>(s), rb = group_sum<16>(ab);
+          // (a token's product with itself is a row and a column term of one G: no change)
+          const float pp = tj < ti ? W[e] * qk[e] : 0.0f, ab = D * dA * kk[e], sum = pp + be * ab;
+          col += sum;
+          const float rs = group_sum<16>(sum), rb = group_sum<16>(ab);
           if (c == 0) {
             rRow[j * kGdrC + ti] = rs;
             rBeta[j * kGdrC + ti] = rb;
@@ -432,59 +472,44 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
         }
         col += __shfl_xor(col, 16);
         col += __shfl_xor(col, 32);
-        if (g == 0) rCol[i * kGdrC + rj] = col;
-        IT::template put<kNear>(smem + L::W, kGdrC, 16 * j + c, i, g, W);
-        IT::template put<kNear>(smem + L::M, kGdrC, 16 * j + c, i, g, M);
+        if (g == 0) rCol[i * kGdrC + tj] = col;
+        WT::template put<kNear>(smem + L::W, 16 * j + c, i, g, W);
+        WT::template put<kNear>(smem + L::M, 16 * j + c, i, g, M);
       }
     }
     __syncthreads();
 
     // ---- dQ, dK of this wave's tiles
-    {
-      // K and Q as B operands: tokens 32 s + 4 g + e and + 16, column 16 jt + c
-      Fr<T> fk[2], fq[2];
+    renew(g, c);
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
+    for (int ii = 0; ii < NI; ++ii) {
+      const int i = i0 + ii;
+      const f32x4 gam = *reinterpret_cast<const f32x4*>(scal + kScGam * kGdrC + 16 * i + 4 * g);
+      const f32x4 end = *reinterpret_cast<const f32x4*>(scal + kScEnd * kGdrC + 16 * i + 4 * g);
+      const f32x4 be = *reinterpret_cast<const f32x4*>(scal + kScBeta * kGdrC + 16 * i + 4 * g);
+      const f32x4 x1 = a1[ii] * gam * a.scale, x2 = a2[ii] * end, x3 = a3[ii] * gam;
+      const f32x4 kt = Quad<T>::f32(KR::tr(smem + L::K, 16 * i, jt, g, c));
+      const f32x4 qt = Quad<T>::f32(KR::tr(smem + L::Z, 16 * i, jt, g, c));
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          typename Quad<T>::q xk, xq;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int t = 32 * s + 16 * h + 4 * g + e;
-            xk[e] = t < len ? k[(size_t)t * a.ks[1] + 16 * jt + c] : (T)0.0f;
-            xq[e] = t < len ? q[(size_t)t * a.qs[1] + 16 * jt + c] : (T)0.0f;
-          }
-          if (h == 0) fk[s].a = xk, fq[s].a = xq;
-          else fk[s].b = xk, fq[s].b = xq;
+      for (int e = 0; e < 4; ++e) {
+        const float s1 = group_sum<16>(qt[e] * x1[e]), s2 = group_sum<16>(kt[e] * x2[e]);
+        if (c == 0) {
+          rQ[jt * kGdrC + 16 * i + 4 * g + e] = s1;
+          rUK[jt * kGdrC + 16 * i + 4 * g + e] = s2;
         }
+      }
+      dQ[ii] += x1;
+      dK[ii] += x2 - be * x3;
 #pragma unroll
-      for (int ii = 0; ii < NI; ++ii) {
-        const int i = i0 + ii;
-        const f32x4 gam = *reinterpret_cast<const f32x4*>(scal + kScGam * kGdrC + 16 * i + 4 * g);
-        const f32x4 end = *reinterpret_cast<const f32x4*>(scal + kScEnd * kGdrC + 16 * i + 4 * g);
-        const f32x4 be = *reinterpret_cast<const f32x4*>(scal + kScBeta * kGdrC + 16 * i + 4 * g);
-        const f32x4 x1 = a1[ii] * gam * a.scale, x2 = a2[ii] * end, x3 = a3[ii] * gam;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int t = 16 * i + 4 * g + e;
-          const float kt = t < len ? (float)k[(size_t)t * a.ks[1] + 16 * jt + c] : 0.0f;
-          const float qt = t < len ? (float)q[(size_t)t * a.qs[1] + 16 * jt + c] : 0.0f;
-          const float s1 = group_sum<16>(qt * x1[e]), s2 = group_sum<16>(kt * x2[e]), s3 = group_sum<16>(kt * x3[e]);
-          if (c == 0) {
-            rQ[jt * kGdrC + t] = s1;
-            rUK[jt * kGdrC + t] = s2;
-            rRK[jt * kGdrC + t] = s3;
-          }
+      for (int y = 0; y < 2; ++y) {
+        const Fr<T> fk = KR::tr32(smem + L::K, y, jt, g, c);
+        if (2 * y <= i) {    // (uniform)
+          dQ[ii] = mma<T>(WT::template tok<kNear>(smem + L::W, i, 32 * y, g, c), fk, dQ[ii]);
+          dK[ii] = mma<T>(WT::template tok<kNear>(smem + L::M, i, 32 * y, g, c), fk, dK[ii]);
         }
-        dQ[ii] += x1;
-        dK[ii] += x2 - be * x3;
-        for (int s = 0; s <= i / 2; ++s) {
-          dQ[ii] = mma<T>(IT::template tok<kNear>(smem + L::W, kGdrC, i, 32 * s, g, c), fk[s], dQ[ii]);
-          dK[ii] = mma<T>(IT::template tok<kNear>(smem + L::M, kGdrC, i, 32 * s, g, c), fk[s], dK[ii]);
-        }
-        for (int s = i / 2; s < 2; ++s) {
-          dK[ii] = mma<T>(IT::template col<kNear>(smem + L::W, kGdrC, 16 * i, s, g, c), fq[s], dK[ii]);
-          dK[ii] = mma<T>(IT::template col<kNear>(smem + L::M, kGdrC, 16 * i, s, g, c), fk[s], dK[ii]);
+        if (2 * y + 1 >= i) {
+          dK[ii] = mma<T>(WT::template col<kNear>(smem + L::W, 16 * i, y, g, c), KR::tr32(smem + L::Z, y, jt, g, c), dK[ii]);
+          dK[ii] = mma<T>(WT::template col<kNear>(smem + L::M, 16 * i, y, g, c), fk, dK[ii]);
         }
       }
     }
@@ -493,15 +518,15 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
     // ---- dbeta, dg
     if (w == 0) {
       const int t = lane;
-      float rv1 = 0.0f, s1 = 0.0f, s2 = 0.0f, s3 = 0.0f, sss = 0.0f, row = 0.0f, rb = 0.0f, col = 0.0f;
-      for (int x = 0; x < 8; ++x) {
+      float rv1 = 0.0f, rk1 = 0.0f, s1 = 0.0f, s2 = 0.0f, sss = 0.0f, row = 0.0f, rb = 0.0f, col = 0.0f;
+      for (int x = 0; x < VB / 16; ++x) {
         rv1 += rRV[x * kGdrC + t];
-        sss += rSS[x];
+        rk1 += rRK[x * kGdrC + t];
       }
+      for (int x = 0; x < 8; ++x) sss += rSS[x];
       for (int x = 0; x < NJ; ++x) {
         s1 += rQ[x * kGdrC + t];
         s2 += rUK[x * kGdrC + t];
-        s3 += rRK[x * kGdrC + t];
       }
       for (int x = 0; x < 4; ++x) {
         if (x <= t / 16) {
@@ -510,9 +535,11 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
         }
         if (x >= t / 16) col += rCol[x * kGdrC + t];
       }
-      const float be = sBe[t];
-      float dG = s1 - be * s3 - s2 + row - col;
-      float ends = group_sum<64>(s2);
+      const float be = scal[kScBeta * kGdrC + t];
+      float dG = s1 - be * rk1 - s2 + row - col;
+      float ends = t < len ? s2 : 0.0f;
+      if (t >= len) dG = 0.0f;
+      ends = group_sum<64>(ends);
       ends += scal[kScGam * kGdrC + kGdrC - 1] * sss;
       // suffix sums
 #pragma unroll
@@ -522,7 +549,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
       }
       if (t < len) {
         a.dg[(row0 + t) * a.Hv + hv] = dG + ends;
-        reinterpret_cast<T*>(a.dbeta)[(row0 + t) * a.Hv + hv] = (T)(rv1 - s3 + rb);
+        reinterpret_cast<T*>(a.dbeta)[(row0 + t) * a.Hv + hv] = (T)(rv1 + rb);
       }
     }
     __syncthreads();
@@ -562,20 +589,29 @@ int launch_bchain_t(const GdrArgs& a, hipStream_t s) {
   hipLaunchKernelGGL(kern, dim3((heads + 7) / 8 * 8 * (a.Dv / (16 * NW))), dim3(64 * NW), lds, s, a);
   return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
 }
+template <typename T, int DK, int VB>
+int launch_grad_t(const GdrArgs& a, hipStream_t s) {
+  constexpr int lds = GradLds<T, DK, VB>::total;
+  static_assert(lds <= 160 * 1024, "LDS");
+  const auto kern = carve_gdr_grad_kernel<T, DK, VB>;
+  const int st = allow_lds(kern, lds);
+  if (st) return st;
+  hipLaunchKernelGGL(kern, dim3(a.nslots, a.Hk), dim3(512), lds, s, a);
+  return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
+}
 template <typename T, int DK>
 int launch_bwd_t(const GdrArgs& a, hipStream_t s, void (*mark)(hipStream_t)) {
-  static_assert(GradLds<T>::total <= 160 * 1024, "LDS");
   int st = launch_gdr_prep(a, sizeof(T) == 2 ? CARVE_BF16 : CARVE_F32, true, s);
   if (st) return st;
   mark(s);
   st = gdr_chain_waves(a) == 4 ? launch_bchain_t<T, DK, 4>(a, s) : launch_bchain_t<T, DK, 2>(a, s);
   if (st) return st;
   mark(s);
-  st = allow_lds(carve_gdr_grad_kernel<T, DK>, GradLds<T>::total);
-  if (st) return st;
-  hipLaunchKernelGGL((carve_gdr_grad_kernel<T, DK>), dim3(a.nslots, a.Hk), dim3(512), GradLds<T>::total, s, a);
+  if (a.Dv == 32) st = launch_grad_t<T, DK, 32>(a, s);
+  else if (a.Dv == 64 || sizeof(T) == 4) st = launch_grad_t<T, DK, 64>(a, s);   // (f32 at 128 columns: 177 KB)
+  else st = launch_grad_t<T, DK, sizeof(T) == 4 ? 64 : 128>(a, s);
   mark(s);
-  return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
+  return st;
 }
 
 }  // namespace
