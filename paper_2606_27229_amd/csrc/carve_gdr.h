@@ -99,6 +99,20 @@ struct Fi {
 };
 constexpr int kExact = 3, kNear = 2;   // pieces towards f32 and towards bf16 results
 
+// x minus its bf16 rounding h, exactly: one two-term product a value, which also
+// widens h (a shift or mask and a subtraction otherwise; the constants are the pairs
+// (-1, 0) and (0, -1), set up here because as literals the assembler takes the pair's
+// low half for an f32 constant)
+__device__ __forceinline__ f32x4 bf16_rest(f32x4 x, bf16x4 h) {
+  unsigned c0, c1;
+  asm("s_mov_b32 %0, 0xbf80" : "=s"(c0));
+  asm("s_mov_b32 %0, 0xbf800000" : "=s"(c1));
+  const bf16x2 m0 = __builtin_bit_cast(bf16x2, c0), m1 = __builtin_bit_cast(bf16x2, c1);
+  const bf16x2 lo = __builtin_shufflevector(h, h, 0, 1), hi = __builtin_shufflevector(h, h, 2, 3);
+  const f32x4 r = {__builtin_amdgcn_fdot2_f32_bf16(lo, m0, x[0], false), __builtin_amdgcn_fdot2_f32_bf16(lo, m1, x[1], false),
+                   __builtin_amdgcn_fdot2_f32_bf16(hi, m0, x[2], false), __builtin_amdgcn_fdot2_f32_bf16(hi, m1, x[3], false)};
+  return r;
+}
 template <typename T, int N>
 __device__ __forceinline__ Fi<T, N> to_fi(f32x4 a, f32x4 b) {
   Fi<T, N> f;
@@ -108,8 +122,8 @@ __device__ __forceinline__ Fi<T, N> to_fi(f32x4 a, f32x4 b) {
       f.x[i].a = Quad<T>::cvt(a);
       f.x[i].b = Quad<T>::cvt(b);
       if (i + 1 < N) {
-        a -= Quad<T>::f32(f.x[i].a);
-        b -= Quad<T>::f32(f.x[i].b);
+        a = bf16_rest(a, f.x[i].a);
+        b = bf16_rest(b, f.x[i].b);
       }
     }
   } else {
@@ -227,12 +241,12 @@ __device__ __forceinline__ void st_img(char* img, int f, int lane, f32x4 a, f32x
     *reinterpret_cast<f32x4*>(p + 1024) = x.x[0].b;
   }
 }
-// one (slot, head) of the workspace.  Forward: T, P (towards o), scalars; backward: T,
+// one (slot, head) of the workspace.  Forward: T, scalars, P (towards o); backward: T,
 // scalars, P^T, T^T
 template <typename T>
 struct GdrWs {
   static constexpr int I3 = img_bytes<T>(kExact), I2 = img_bytes<T>(kNear);
-  static constexpr int fT = 0, fP = I3, fScal = I3 + I2, fBytes = I3 + I2 + kGdrScal;
+  static constexpr int fT = 0, fScal = I3, fP = I3 + kGdrScal, fBytes = fP + I2;
   static constexpr int bT = 0, bScal = I3, bPt = bScal + kGdrScal, bTt = bPt + I3, bBytes = bTt + I3;
 };
 
@@ -328,9 +342,12 @@ __device__ __forceinline__ void dma_flat(char* lds, const char* src, int bytes, 
 int launch_gdr_fwd(const GdrArgs& a, int dtype, hipStream_t s, void (*mark)(hipStream_t));
 int launch_gdr_bwd(const GdrArgs& a, int dtype, hipStream_t s, void (*mark)(hipStream_t));
 int launch_gdr_prep(const GdrArgs& a, int dtype, bool bwd, hipStream_t s);
-// waves of a workgroup of the chains: two value tiles' worth fills every compute unit
-// up to 512 waves, beyond that four share a chunk's rows
-inline int gdr_chain_waves(const GdrArgs& a) { return a.Dv % 64 == 0 && (long long)a.nseq * a.Hv * a.Dv > 16 * 512 ? 4 : 2; }
+// value tiles of a workgroup of the chains: two up to 512 tiles in all, which gives every
+// compute unit one workgroup; beyond that four tiles share a chunk's rows where their
+// LDS fits (f32 rows of 128 do not)
+inline int gdr_chain_tiles(const GdrArgs& a, bool f32) {
+  return a.Dv % 64 == 0 && (long long)a.nseq * a.Hv * (a.Dv / 16) > 512 && !(f32 && a.Dk == 128) ? 4 : 2;
+}
 
 struct GdrStepArgs {
   const void *q, *k, *v, *beta;

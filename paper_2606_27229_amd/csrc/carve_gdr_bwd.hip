@@ -18,132 +18,218 @@ namespace carve {
 namespace {
 
 // ---------------------------------------------------------------------------------
-// The chain of state gradients, the mirror of the forward's (carve_gdr_chain_kernel): a
-// wave keeps dS^T[j][v] of 16 value columns in registers and runs the chunks from the
-// last to the first; dS of every chunk's end goes to dS_chunks.
+// The chain of state gradients, the mirror of the forward's (carve_gdr_chain_kernel), from
+// the last chunk to the first.  Two waves a tile of 16 value columns:
+//   chain   dU = z + E K dS^T, dR = T^T dU, dS^T <- e^{G_C} dS^T + Y - K^T (beta e^G dR);
+//           dS of every chunk's end and dR go out
+//   helper  what does not need dS, one chunk ahead: z = P^T dO' and Y = Q^T (e^G dO');
+//           it loads the next chunk's rows
+// z and Y pass through LDS as they lie in registers.  Barriers, two a chunk: (1) z, Y and
+// the chunk's rows are there; (2) the chain has taken z and Y.
 template <typename T, int DK, int NW>
 struct BChainLds {
   typedef GdrRows<T, DK> KR;
-  typedef GdrRows<T, 16 * NW> VR;
-  static constexpr int img = GdrWs<T>::bBytes - GdrWs<T>::bScal;   // scalars, P^T, T^T
-  static constexpr int K = 0, Q = K + KR::bytes, O = Q + KR::bytes, I = O + VR::bytes;
-  static constexpr int one = I + img;
-  static constexpr int nbuf = 2 * one <= 160 * 1024 ? 2 : 1;
-  static constexpr int total = nbuf * one;
+  static constexpr bool q_lds = sizeof(T) == 2 || DK < 128;       // (f32 queries of 128: from memory)
+  static constexpr int K0 = 0, I = KR::bytes;                     // I: scalars, then T^T
+  static constexpr int one = I + kGdrScal + GdrWs<T>::I3;
+  static constexpr int Q = 2 * one, qone = q_lds ? KR::bytes : 0;
+  static constexpr int xz = Q + 2 * qone, xY = xz + NW * 4 * 1024;
+  static constexpr int total = xY + NW * (DK / 16) * 1024;
 };
 
 template <typename T, int DK, int NW>
-__global__ void __launch_bounds__(64 * NW, 1) carve_gdr_bchain_kernel(GdrArgs a) {
+__global__ void __launch_bounds__(128 * NW, 1) carve_gdr_bchain_kernel(GdrArgs a) {
   constexpr int NP = DK / 32;
   typedef BChainLds<T, DK, NW> L;
   typedef typename L::KR KR;
-  typedef typename L::VR VR;
   typedef GdrWs<T> WS;
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const bool helper = wave >= NW;
+  const int w = helper ? wave - NW : wave;
   const int g = lane >> 4, c = lane & 15;
   const int ns = a.Dv / (16 * NW), idx = blockIdx.x;
   const int head = idx / (8 * ns) * 8 + idx % 8, slice = idx / 8 % ns;
   if (head >= a.nseq * a.Hv) return;
   const int n = head / a.Hv, hv = head % a.Hv, hk = hv / (a.Hv / a.Hk);
-  const int vs = 16 * NW * slice, v0 = vs + 16 * w;
+  const int v0 = 16 * (NW * slice + w);
   const GdrSeq sq = gdr_seq(a, n);
-  const T* q = reinterpret_cast<const T*>(a.q) + sq.batch * a.qs[0] + sq.t0 * a.qs[1] + hk * a.qs[2];
-  const T* k = reinterpret_cast<const T*>(a.k) + sq.batch * a.ks[0] + sq.t0 * a.ks[1] + hk * a.ks[2];
-  const T* dO = reinterpret_cast<const T*>(a.dO) + (((size_t)sq.batch * a.T + sq.t0) * a.Hv + hv) * a.Dv + vs;
-  const size_t ors = (size_t)a.Hv * a.Dv;
   const size_t sm = (size_t)a.Dv * DK, soff = (size_t)(v0 + c) * DK + 4 * g;
   const int nch = (sq.len + kGdrC - 1) / kGdrC;
+  f32x4* xz = reinterpret_cast<f32x4*>(smem + L::xz + w * 4 * 1024) + lane;
+  f32x4* xY = reinterpret_cast<f32x4*>(smem + L::xY + w * (DK / 16) * 1024) + lane;
 
-  const auto load = [&](int ch) {
-    char* buf = smem + (L::nbuf == 2 ? (ch & 1) * L::one : 0);
-    const int t0 = ch * kGdrC, len = min(kGdrC, sq.len - t0);
-    KR::dma(buf + L::K, k + t0 * a.ks[1], (int)(a.ks[1] * sizeof(T)), len, w, NW, lane);
-    dma_flat(buf + L::I, a.ws + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * a.per + WS::bScal, L::img, w, NW, lane);
-    VR::dma(buf + L::O, dO + t0 * ors, (int)(ors * sizeof(T)), len, w, NW, lane);
-    KR::dma(buf + L::Q, q + t0 * a.qs[1], (int)(a.qs[1] * sizeof(T)), len, w, NW, lane);
-  };
-  if (L::nbuf == 2 && nch > 0) load(nch - 1);
-
-  f32x4 S[2 * NP];
+  if (!helper) {
+    f32x4 S[2 * NP];
 #pragma unroll
-  for (int j = 0; j < 2 * NP; ++j)
-    S[j] = a.dS_T ? *reinterpret_cast<const f32x4*>(a.dS_T + (size_t)head * sm + soff + 16 * j) : zero4();
-  for (int ch = nch - 1; ch >= 0; --ch) {
-    const char* buf = smem + (L::nbuf == 2 ? (ch & 1) * L::one : 0);
-    if constexpr (L::nbuf == 1) {
-      __syncthreads();
-      load(ch);
+    for (int j = 0; j < 2 * NP; ++j)
+      S[j] = a.dS_T ? *reinterpret_cast<const f32x4*>(a.dS_T + (size_t)head * sm + soff + 16 * j) : zero4();
+    if (nch > 0) __syncthreads();   // (0)
+#pragma unroll 1
+    for (int ch = nch - 1; ch >= 0; --ch) {
+      const char* buf = smem + (ch & 1) * L::one;
+      const float* scal = reinterpret_cast<const float*>(buf + L::I);
+      const size_t sh = (size_t)(sq.slot0 + ch) * a.Hv + hv;
+      __syncthreads();   // (1)
+      f32x4 U[4];
+      Fi<T, kExact> Sf[NP];
+      const float gend = scal[kScGam * kGdrC + kGdrC - 1];
+      float* out = a.dS_chunks + sh * sm + soff;
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        Sf[p] = to_fi<T, kExact>(S[2 * p], S[2 * p + 1]);
+#pragma unroll
+        for (int j = 2 * p; j < 2 * p + 2; ++j) {
+          *reinterpret_cast<f32x4*>(out + 16 * j) = S[j];
+          S[j] = S[j] * gend + xY[64 * j];
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) U[i] = xz[64 * i];
+      __syncthreads();   // (2)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f32x4 y = zero4();
+#pragma unroll
+        for (int p = 0; p < NP; ++p) y = mma<T>(KR::nat(buf + L::K0, i, p, g, c), Sf[p], y);
+        U[i] += y * *reinterpret_cast<const f32x4*>(scal + kScEnd * kGdrC + 16 * i + 4 * g);
+      }
+      const Fi<T, kExact> Uf[2] = {to_fi<T, kExact>(U[0], U[1]), to_fi<T, kExact>(U[2], U[3])};
+      f32x4 R[4];
+      float* keep = a.dR + (sh * (a.Dv / 16) + v0 / 16) * 1024 + 4 * lane;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f32x4 x = zero4();
+#pragma unroll
+        for (int s = i / 2; s < 2; ++s)
+          x = mma<T>(ld_img<T, kExact>(buf + L::I + kGdrScal, img_upper(i, s), lane), Uf[s], x);
+        *reinterpret_cast<f32x4*>(keep + 256 * i) = x;
+        const f32x4 gam = *reinterpret_cast<const f32x4*>(scal + kScGam * kGdrC + 16 * i + 4 * g);
+        const f32x4 be = *reinterpret_cast<const f32x4*>(scal + kScBeta * kGdrC + 16 * i + 4 * g);
+        R[i] = -(x * (gam * be));
+      }
+      const Fi<T, kExact> Rf[2] = {to_fi<T, kExact>(R[0], R[1]), to_fi<T, kExact>(R[2], R[3])};
+#pragma unroll
+      for (int j = 0; j < 2 * NP; ++j)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) S[j] = mma<T>(KR::tr32(buf + L::K0, s, j, g, c), Rf[s], S[j]);
     }
-    vm_wait_all();
-    __syncthreads();
-    if (L::nbuf == 2 && ch > 0) load(ch - 1);
-    {
-      float* s = a.dS_chunks + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * sm + soff;
+    if (a.dS0) {
+      float* s = a.dS0 + (size_t)head * sm + soff;
 #pragma unroll
       for (int j = 0; j < 2 * NP; ++j) *reinterpret_cast<f32x4*>(s + 16 * j) = S[j];
     }
-    const char* img = buf + L::I;
-    const float* scal = reinterpret_cast<const float*>(img);
-    const int len = sq.len - ch * kGdrC;
-    // dO[t][v] of this wave's columns, zeros behind the last token
-    Fr<T> of[2] = {VR::tr32(buf + L::O, 0, w, g, c), VR::tr32(buf + L::O, 1, w, g, c)};
-    if (len < kGdrC)
+    return;
+  }
+
+  // ---- helper
+  if (nch == 0) return;   // (no barriers then)
+  const T* q = reinterpret_cast<const T*>(a.q) + sq.batch * a.qs[0] + sq.t0 * a.qs[1] + hk * a.qs[2];
+  const T* k = reinterpret_cast<const T*>(a.k) + sq.batch * a.ks[0] + sq.t0 * a.ks[1] + hk * a.ks[2];
+  const T* dO = reinterpret_cast<const T*>(a.dO) + (((size_t)sq.batch * a.T + sq.t0) * a.Hv + hv) * a.Dv + v0 + c;
+  const size_t ors = (size_t)a.Hv * a.Dv;
+  const auto ws_of = [&](int ch) { return a.ws + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * a.per; };
+  const auto load = [&](int ch) {
+    char* buf = smem + (ch & 1) * L::one;
+    const int t0 = ch * kGdrC, len = min(kGdrC, sq.len - t0);
+    KR::dma(buf + L::K0, k + t0 * a.ks[1], (int)(a.ks[1] * sizeof(T)), len, w, NW, lane);
+    dma_flat(buf + L::I, ws_of(ch) + WS::bScal, kGdrScal, w, NW, lane);
+    dma_flat(buf + L::I + kGdrScal, ws_of(ch) + WS::bTt, WS::I3, w, NW, lane);
+  };
+  const auto load_q = [&](int ch) {
+    if constexpr (L::q_lds) {
+      const int t0 = ch * kGdrC, len = min(kGdrC, sq.len - t0);
+      KR::dma(smem + L::Q + (ch & 1) * L::qone, q + t0 * a.qs[1], (int)(a.qs[1] * sizeof(T)), len, w, NW, lane);
+    }
+  };
+  struct Mine {
+    typename Quad<T>::q od[4];   // dO[t][v]: tokens 16 i + 4 g + e of column c
+    Fi<T, kExact> Pt[6];
+    f32x4 gam[4];
+  };
+  const auto load_m = [&](Mine& m, int ch) {
+    const char* ws = ws_of(ch);
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (32 * s + 4 * g + e >= len) of[s].a[e] = (T)0.0f;
-          if (32 * s + 16 + 4 * g + e >= len) of[s].b[e] = (T)0.0f;
-        }
-    Fi<T, kExact> Sf[NP];
-#pragma unroll
-    for (int p = 0; p < NP; ++p) Sf[p] = to_fi<T, kExact>(S[2 * p], S[2 * p + 1]);
-    // dU = P^T dO' + E K dS^T
-    f32x4 U[4];
+    for (int f = 0; f < 6; ++f) m.Pt[f] = ld_img<T, kExact>(ws + WS::bPt, f, lane);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      f32x4 x = zero4(), y = zero4();
+      m.gam[i] = *reinterpret_cast<const f32x4*>(ws + WS::bScal + 4 * (kScGam * kGdrC + 16 * i + 4 * g));
 #pragma unroll
-      for (int p = 0; p < NP; ++p) y = mma<T>(KR::nat(buf + L::K, i, p, g, c), Sf[p], y);
-#pragma unroll
-      for (int s = i / 2; s < 2; ++s) x = mma<T>(ld_img<T, kExact>(img + (WS::bPt - WS::bScal), img_upper(i, s), lane), of[s], x);
-      const f32x4 end = *reinterpret_cast<const f32x4*>(scal + kScEnd * kGdrC + 16 * i + 4 * g);
-      U[i] = x * a.scale + y * end;
+      for (int e = 0; e < 4; ++e) {
+        // (past the end: the last token, zeroed where it is used)
+        m.od[i][e] = dO[(size_t)min(ch * kGdrC + 16 * i + 4 * g + e, sq.len - 1) * ors];
+      }
     }
-    const Fi<T, kExact> Uf[2] = {to_fi<T, kExact>(U[0], U[1]), to_fi<T, kExact>(U[2], U[3])};
-    // - beta e^G dR, dR = T^T dU (kept for the chunk's gradients), and e^G dO'
-    f32x4 R[4], od[4];
-    float* keep = a.dR + (((size_t)(sq.slot0 + ch) * a.Hv + hv) * (a.Dv / 16) + v0 / 16) * 1024 + 4 * lane;
+  };
+  // z and Y of a chunk into LDS
+  const auto work = [&](Mine& m, int ch) {
+    const int len = sq.len - ch * kGdrC;
+    f32x4 od[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (len < kGdrC)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (16 * i + 4 * g + e >= len) m.od[i][e] = (T)0.0f;
+      od[i] = Quad<T>::f32(m.od[i]) * (m.gam[i] * a.scale);
+    }
+    const Fr<T> of[2] = {{m.od[0], m.od[1]}, {m.od[2], m.od[3]}};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       f32x4 x = zero4();
 #pragma unroll
-      for (int s = i / 2; s < 2; ++s)
-        x = mma<T>(ld_img<T, kExact>(img + (WS::bTt - WS::bScal), img_upper(i, s), lane), Uf[s], x);
-      const f32x4 gam = *reinterpret_cast<const f32x4*>(scal + kScGam * kGdrC + 16 * i + 4 * g);
-      const f32x4 be = *reinterpret_cast<const f32x4*>(scal + kScBeta * kGdrC + 16 * i + 4 * g);
-      *reinterpret_cast<f32x4*>(keep + 256 * i) = x;
-      R[i] = -(x * gam * be);
-      od[i] = Quad<T>::f32(i % 2 ? of[i / 2].b : of[i / 2].a) * (gam * a.scale);
+      for (int s = i / 2; s < 2; ++s) x = mma<T>(m.Pt[img_upper(i, s)], of[s], x);
+      xz[64 * i] = x * a.scale;
     }
-    const Fi<T, kExact> Rf[2] = {to_fi<T, kExact>(R[0], R[1]), to_fi<T, kExact>(R[2], R[3])};
     const Fi<T, kExact> Of[2] = {to_fi<T, kExact>(od[0], od[1]), to_fi<T, kExact>(od[2], od[3])};
-    const float gend = scal[kScGam * kGdrC + kGdrC - 1];
 #pragma unroll
     for (int j = 0; j < 2 * NP; ++j) {
-      S[j] *= gend;
+      f32x4 x = zero4();
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        S[j] = mma<T>(KR::tr32(buf + L::Q, s, j, g, c), Of[s], S[j]);
-        S[j] = mma<T>(KR::tr32(buf + L::K, s, j, g, c), Rf[s], S[j]);
-      }
-    }
-  }
-  if (a.dS0) {
-    float* s = a.dS0 + (size_t)head * sm + soff;
+        Fr<T> f;
+        if constexpr (L::q_lds) {
+          f = KR::tr32(smem + L::Q + (ch & 1) * L::qone, s, j, g, c);
+        } else {
 #pragma unroll
-    for (int j = 0; j < 2 * NP; ++j) *reinterpret_cast<f32x4*>(s + 16 * j) = S[j];
+          for (int e = 0; e < 4; ++e) {
+            const int t = ch * kGdrC + 32 * s + 4 * g + e;
+            f.a[e] = q[(size_t)min(t, sq.len - 1) * a.qs[1] + 16 * j + c];
+            f.b[e] = q[(size_t)min(t + 16, sq.len - 1) * a.qs[1] + 16 * j + c];
+          }
+        }
+        x = mma<T>(f, Of[s], x);
+      }
+      xY[64 * j] = x;
+    }
+  };
+  constexpr bool AHEAD = NW == 2 && sizeof(T) == 2;
+  Mine cur, nxt;
+  load(nch - 1);
+  load_q(nch - 1);
+  load_m(cur, nch - 1);
+  vm_wait_all();
+  __syncthreads();   // (0) the helpers' shares of the queries
+  work(cur, nch - 1);
+  if (nch > 1) {
+    load_q(nch - 2);
+    if constexpr (AHEAD) load_m(nxt, nch - 2);
+  }
+#pragma unroll 1
+  for (int ch = nch - 1; ch >= 0; --ch) {
+    vm_wait_all();
+    __syncthreads();   // (1)
+    __syncthreads();   // (2)
+    if (ch == 0) break;
+    load(ch - 1);
+    if (ch > 1) load_q(ch - 2);
+    if constexpr (AHEAD) {
+      cur = nxt;
+      if (ch > 1) load_m(nxt, ch - 2);
+    } else {
+      load_m(cur, ch - 1);
+    }
+    work(cur, ch - 1);
   }
 }
 
@@ -181,7 +267,7 @@ struct InterT {
       for (int y = 0; y < N; ++y) {
         const typename Quad<T>::q h = Quad<T>::cvt(x);
         Quad<T>::st(p + y * plane, h);
-        if (y + 1 < N) x -= Quad<T>::f32(h);
+        if (y + 1 < N) x = bf16_rest(x, h);
       }
     } else {
       Quad<T>::st(p + 16 * i + 4 * g, x);
@@ -586,7 +672,7 @@ int launch_bchain_t(const GdrArgs& a, hipStream_t s) {
   const int st = allow_lds(kern, lds);
   if (st) return st;
   const unsigned heads = (unsigned)a.nseq * a.Hv;
-  hipLaunchKernelGGL(kern, dim3((heads + 7) / 8 * 8 * (a.Dv / (16 * NW))), dim3(64 * NW), lds, s, a);
+  hipLaunchKernelGGL(kern, dim3((heads + 7) / 8 * 8 * (a.Dv / (16 * NW))), dim3(128 * NW), lds, s, a);
   return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
 }
 template <typename T, int DK, int VB>
@@ -604,7 +690,8 @@ int launch_bwd_t(const GdrArgs& a, hipStream_t s, void (*mark)(hipStream_t)) {
   int st = launch_gdr_prep(a, sizeof(T) == 2 ? CARVE_BF16 : CARVE_F32, true, s);
   if (st) return st;
   mark(s);
-  st = gdr_chain_waves(a) == 4 ? launch_bchain_t<T, DK, 4>(a, s) : launch_bchain_t<T, DK, 2>(a, s);
+  if constexpr (sizeof(T) == 4 && DK == 128) st = launch_bchain_t<T, DK, 2>(a, s);
+  else st = gdr_chain_tiles(a, sizeof(T) == 4) == 4 ? launch_bchain_t<T, DK, 4>(a, s) : launch_bchain_t<T, DK, 2>(a, s);
   if (st) return st;
   mark(s);
   if (a.Dv == 32) st = launch_grad_t<T, DK, 32>(a, s);

@@ -179,33 +179,41 @@ __global__ void __launch_bounds__(256) carve_gdr_prep_kernel(GdrArgs a) {
 }
 
 // ---------------------------------------------------------------------------------
-// The chain of states.  A workgroup of NW waves runs one sequence and value head for
-// 16 NW value columns, a wave for 16 of them: value rows of S are independent, so the
-// waves share nothing but the chunk's rows.  A wave keeps S^T[j][v] in the matrix-core
-// result layout, where it is at once the B operand of K S^T and the A operand of
-// (Q S^T)^T: no state passes through LDS.  The next chunk's keys, queries, values and
-// images are loaded straight into the other half of the LDS while this one runs; one
-// wait for memory and one barrier a chunk, and the outputs of a chunk are stored behind
-// the next one's wait, so that no wait covers a store that was just issued.
+// The chain of states.  A workgroup runs one sequence and value head for 16 NW value
+// columns, NW tiles of 16: value rows of S are independent, so the tiles share nothing
+// but the chunk's rows.  Two waves a tile:
+//   chain   R = beta (V - e^G K S^T), U = T R, S^T <- e^{G_C} S^T + K^T (e^{G_C - G} U)
+//   helper  o = scale (e^G Q S^T + P U), one chunk behind, and all global memory: the
+//           next chunk's keys, values, T and decays straight into LDS, its own queries
+//           and P into registers, outputs and chunk start states out
+// The chain is what the call takes (chunks follow each other), so the helper takes from
+// it whatever it can; the two run on different SIMDs.  The chain's S^T[j][v] stays in the
+// matrix-core result layout, where it is at once the B operand of K S^T (chain) and the
+// A operand of (Q S^T)^T (helper): it needs no transposition, and U neither.  S and U
+// pass to the helper through LDS as they lie in registers.  Barriers, two a chunk: (1)
+// the chunk's rows are there and the chain has left S(ch), U(ch - 1); (2) the helper has
+// taken them.
 template <typename T, int DK, int NW>
 struct ChainLds {
   typedef GdrRows<T, DK> KR;
   typedef GdrRows<T, 16 * NW> VR;
-  static constexpr int K = 0, Q = K + KR::bytes, V = Q + KR::bytes, I = V + VR::bytes;
-  static constexpr int one = I + GdrWs<T>::fBytes;
-  static constexpr int nbuf = 2 * one <= 160 * 1024 ? 2 : 1;   // (f32 rows of 128: one)
-  static constexpr int total = nbuf * one;
+  static constexpr int K = 0, V = K + KR::bytes, I = V + VR::bytes;   // I: T, scalars
+  static constexpr int one = I + GdrWs<T>::fP;
+  static constexpr int xS = 2 * one, xU = xS + NW * (DK / 16) * 1024;
+  static constexpr int total = xU + NW * 4 * 1024;
 };
 
 template <typename T, int DK, int NW>
-__global__ void __launch_bounds__(64 * NW, 1) carve_gdr_chain_kernel(GdrArgs a) {
+__global__ void __launch_bounds__(128 * NW, 1) carve_gdr_chain_kernel(GdrArgs a) {
   constexpr int NP = DK / 32;
   typedef ChainLds<T, DK, NW> L;
   typedef typename L::KR KR;
   typedef typename L::VR VR;
   typedef GdrWs<T> WS;
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const bool helper = wave >= NW;
+  const int w = helper ? wave - NW : wave;   // tile
   const int g = lane >> 4, c = lane & 15;
   // blocks 8 apart share an XCD: the slices of a (sequence, head) follow each other there
   const int ns = a.Dv / (16 * NW), idx = blockIdx.x;
@@ -214,110 +222,170 @@ __global__ void __launch_bounds__(64 * NW, 1) carve_gdr_chain_kernel(GdrArgs a) 
   const int n = head / a.Hv, hv = head % a.Hv, hk = hv / (a.Hv / a.Hk);
   const int vs = 16 * NW * slice, v0 = vs + 16 * w;
   const GdrSeq sq = gdr_seq(a, n);
-  const T* q = reinterpret_cast<const T*>(a.q) + sq.batch * a.qs[0] + sq.t0 * a.qs[1] + hk * a.qs[2];
-  const T* k = reinterpret_cast<const T*>(a.k) + sq.batch * a.ks[0] + sq.t0 * a.ks[1] + hk * a.ks[2];
-  const T* v = reinterpret_cast<const T*>(a.v) + sq.batch * a.vs[0] + sq.t0 * a.vs[1] + hv * a.vs[2] + vs;
-  T* o = reinterpret_cast<T*>(a.o) + (((size_t)sq.batch * a.T + sq.t0) * a.Hv + hv) * a.Dv + v0;
-  const size_t ors = (size_t)a.Hv * a.Dv;
   const size_t sm = (size_t)a.Dv * DK;   // elements of a state
   const size_t soff = (size_t)(v0 + c) * DK + 4 * g;
   const int nch = (sq.len + kGdrC - 1) / kGdrC;
+  f32x4* xS = reinterpret_cast<f32x4*>(smem + L::xS + w * (DK / 16) * 1024) + lane;
+  f32x4* xU = reinterpret_cast<f32x4*>(smem + L::xU + w * 4 * 1024) + lane;
 
-  const auto load = [&](int ch) {
-    char* buf = smem + (L::nbuf == 2 ? (ch & 1) * L::one : 0);
-    const int t0 = ch * kGdrC, len = min(kGdrC, sq.len - t0);
-    KR::dma(buf + L::K, k + t0 * a.ks[1], (int)(a.ks[1] * sizeof(T)), len, w, NW, lane);
-    dma_flat(buf + L::I, a.ws + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * a.per, WS::fBytes, w, NW, lane);
-    VR::dma(buf + L::V, v + t0 * a.vs[1], (int)(a.vs[1] * sizeof(T)), len, w, NW, lane);
-    KR::dma(buf + L::Q, q + t0 * a.qs[1], (int)(a.qs[1] * sizeof(T)), len, w, NW, lane);
-  };
-  if (L::nbuf == 2 && nch > 0) load(0);
-
-  f32x4 S[2 * NP];
+  if (!helper) {
+    f32x4 S[2 * NP];
 #pragma unroll
-  for (int j = 0; j < 2 * NP; ++j)
-    S[j] = a.S0 ? *reinterpret_cast<const f32x4*>(a.S0 + (size_t)head * sm + soff + 16 * j) : zero4();
-  typename Quad<T>::q oq[4];   // o^T of the last chunk: four values of token 16 i + c
-  const auto store_o = [&](int ch) {
-    const int t0 = ch * kGdrC, len = sq.len - t0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (16 * i + c < len) Quad<T>::st(o + (size_t)(t0 + 16 * i + c) * ors + 4 * g, oq[i]);
-  };
-  for (int ch = 0; ch < nch; ++ch) {
-    const char* buf = smem + (L::nbuf == 2 ? (ch & 1) * L::one : 0);
-    if constexpr (L::nbuf == 1) {
-      __syncthreads();
-      load(ch);
+    for (int j = 0; j < 2 * NP; ++j) {
+      S[j] = a.S0 ? *reinterpret_cast<const f32x4*>(a.S0 + (size_t)head * sm + soff + 16 * j) : zero4();
+      xS[64 * j] = S[j];
     }
-    vm_wait_all();
-    __syncthreads();
-    if (L::nbuf == 2 && ch + 1 < nch) load(ch + 1);
-    if (ch > 0) store_o(ch - 1);
-    if (a.S_chunks) {
-      float* s = a.S_chunks + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * sm + soff;
+#pragma unroll 1
+    for (int ch = 0; ch < nch; ++ch) {
+      const char* buf = smem + (ch & 1) * L::one;
+      const float* scal = reinterpret_cast<const float*>(buf + L::I + WS::fScal);
+      __syncthreads();   // (1)
+      Fi<T, kExact> Sf[NP];
 #pragma unroll
-      for (int j = 0; j < 2 * NP; ++j) *reinterpret_cast<f32x4*>(s + 16 * j) = S[j];
-    }
-    const char* img = buf + L::I;
-    const float* scal = reinterpret_cast<const float*>(img + WS::fScal);
-    Fi<T, kExact> Sf[NP];
+      for (int p = 0; p < NP; ++p) Sf[p] = to_fi<T, kExact>(S[2 * p], S[2 * p + 1]);
+      __syncthreads();   // (2)
+      f32x4 R[4];
 #pragma unroll
-    for (int p = 0; p < NP; ++p) Sf[p] = to_fi<T, kExact>(S[2 * p], S[2 * p + 1]);
-    // R = beta (V - e^G K S^T), tile by tile of 16 tokens
-    f32x4 R[4];
+      for (int i = 0; i < 4; ++i) {
+        f32x4 acc = zero4();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f32x4 acc = zero4();
-#pragma unroll
-      for (int p = 0; p < NP; ++p) acc = mma<T>(KR::nat(buf + L::K, i, p, g, c), Sf[p], acc);
-      const f32x4 gam = *reinterpret_cast<const f32x4*>(scal + kScGam * kGdrC + 16 * i + 4 * g);
-      const f32x4 be = *reinterpret_cast<const f32x4*>(scal + kScBeta * kGdrC + 16 * i + 4 * g);
-      R[i] = be * (Quad<T>::f32(VR::tr(buf + L::V, 16 * i, w, g, c)) - gam * acc);
-    }
-    f32x4 U[4];
-    {
+        for (int p = 0; p < NP; ++p) acc = mma<T>(KR::nat(buf + L::K, i, p, g, c), Sf[p], acc);
+        const f32x4 gam = *reinterpret_cast<const f32x4*>(scal + kScGam * kGdrC + 16 * i + 4 * g);
+        const f32x4 be = *reinterpret_cast<const f32x4*>(scal + kScBeta * kGdrC + 16 * i + 4 * g);
+        R[i] = be * (Quad<T>::f32(VR::tr(buf + L::V, 16 * i, w, g, c)) - gam * acc);
+      }
       const Fi<T, kExact> Rf[2] = {to_fi<T, kExact>(R[0], R[1]), to_fi<T, kExact>(R[2], R[3])};
-      // U = T R
+      f32x4 U[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         U[i] = zero4();
 #pragma unroll
         for (int s = 0; s <= i / 2; ++s)
-          U[i] = mma<T>(ld_img<T, kExact>(img + WS::fT, img_lower(i, s), lane), Rf[s], U[i]);
+          U[i] = mma<T>(ld_img<T, kExact>(buf + L::I + WS::fT, img_lower(i, s), lane), Rf[s], U[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        xU[64 * i] = U[i];
+        U[i] *= *reinterpret_cast<const f32x4*>(scal + kScEnd * kGdrC + 16 * i + 4 * g);
+      }
+      const float gend = scal[kScGam * kGdrC + kGdrC - 1];
+      const Fi<T, kExact> Ue[2] = {to_fi<T, kExact>(U[0], U[1]), to_fi<T, kExact>(U[2], U[3])};
+#pragma unroll
+      for (int j = 0; j < 2 * NP; ++j) {
+        S[j] *= gend;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) S[j] = mma<T>(KR::tr32(buf + L::K, s, j, g, c), Ue[s], S[j]);
+        xS[64 * j] = S[j];
       }
     }
-    // O^T = scale (e^G (Q S^T)^T + U^T P^T)
-    {
+    __syncthreads();
+    if (a.S_T) {
+      float* s = a.S_T + (size_t)head * sm + soff;
+#pragma unroll
+      for (int j = 0; j < 2 * NP; ++j) *reinterpret_cast<f32x4*>(s + 16 * j) = S[j];
+    }
+    return;
+  }
+
+  // ---- helper
+  const T* q = reinterpret_cast<const T*>(a.q) + sq.batch * a.qs[0] + sq.t0 * a.qs[1] + hk * a.qs[2];
+  const T* k = reinterpret_cast<const T*>(a.k) + sq.batch * a.ks[0] + sq.t0 * a.ks[1] + hk * a.ks[2];
+  const T* v = reinterpret_cast<const T*>(a.v) + sq.batch * a.vs[0] + sq.t0 * a.vs[1] + hv * a.vs[2] + vs;
+  T* o = reinterpret_cast<T*>(a.o) + (((size_t)sq.batch * a.T + sq.t0) * a.Hv + hv) * a.Dv + v0;
+  const size_t ors = (size_t)a.Hv * a.Dv;
+  const auto load = [&](int ch) {
+    char* buf = smem + (ch & 1) * L::one;
+    const int t0 = ch * kGdrC, len = min(kGdrC, sq.len - t0);
+    KR::dma(buf + L::K, k + t0 * a.ks[1], (int)(a.ks[1] * sizeof(T)), len, w, NW, lane);
+    dma_flat(buf + L::I, a.ws + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * a.per, WS::fP, w, NW, lane);
+    VR::dma(buf + L::V, v + t0 * a.vs[1], (int)(a.vs[1] * sizeof(T)), len, w, NW, lane);
+  };
+  // queries of a chunk (any row behind the last token repeats it) and P with e^G
+  struct Mine {
+    Fr<T> q[4][NP];
+    Fi<T, kNear> P[6];
+    float gam[4];
+  };
+  const auto load_q = [&](Mine& m, int ch) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const T* r = q + (size_t)min(ch * kGdrC + 16 * i + c, sq.len - 1) * a.qs[1] + 4 * g;
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        m.q[i][p].a = Quad<T>::ld(r + 32 * p);
+        m.q[i][p].b = Quad<T>::ld(r + 32 * p + 16);
+      }
+    }
+  };
+  const auto load_p = [&](Mine& m, int ch) {
+    const char* img = a.ws + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * a.per;
+#pragma unroll
+    for (int f = 0; f < 6; ++f) m.P[f] = ld_img<T, kNear>(img + WS::fP, f, lane);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      m.gam[i] = reinterpret_cast<const float*>(img + WS::fScal)[kScGam * kGdrC + 16 * i + c];
+  };
+  // with the registers for it (one wave a SIMD, bf16), loaded a chunk ahead
+  constexpr bool AHEAD = NW == 2 && sizeof(T) == 2;
+  Mine cur, nxt;
+  f32x4 x[4];
+  if (nch > 0) {
+    load(0);
+    if constexpr (AHEAD) load_q(nxt, 0);
+  }
+#pragma unroll 1
+  for (int ch = 0; ch <= nch; ++ch) {
+    vm_wait_all();
+    __syncthreads();   // (1)
+    f32x4 S[2 * NP], U[4];
+#pragma unroll
+    for (int j = 0; j < 2 * NP; ++j) S[j] = xS[64 * j];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) U[i] = xU[64 * i];
+    if (ch < nch) __syncthreads();   // (2)
+    if (ch + 1 < nch) load(ch + 1);
+    if constexpr (AHEAD) {
+      // (the queries of this chunk and P of the last one)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int p = 0; p < NP; ++p) cur.q[i][p] = nxt.q[i][p];
+#pragma unroll
+      for (int f = 0; f < 6; ++f) cur.P[f] = nxt.P[f];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) cur.gam[i] = nxt.gam[i];
+      if (ch + 1 < nch) load_q(nxt, ch + 1);
+      if (ch < nch) load_p(nxt, ch);
+    }
+    if (a.S_chunks && ch < nch) {
+      float* s = a.S_chunks + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * sm + soff;
+#pragma unroll
+      for (int j = 0; j < 2 * NP; ++j) *reinterpret_cast<f32x4*>(s + 16 * j) = S[j];
+    }
+    if (ch > 0) {   // o of the last chunk
+      if constexpr (!AHEAD) load_p(cur, ch - 1);
       const Fi<T, kNear> Uf[2] = {to_fi<T, kNear>(U[0], U[1]), to_fi<T, kNear>(U[2], U[3])};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        f32x4 x = zero4(), y = zero4();
+        f32x4 y = zero4();
 #pragma unroll
-        for (int p = 0; p < NP; ++p) x = mma<T>(first<kNear>(Sf[p]), KR::nat(buf + L::Q, i, p, g, c), x);
-#pragma unroll
-        for (int s = 0; s <= i / 2; ++s)
-          y = mma<T>(Uf[s], ld_img<T, kNear>(img + WS::fP, img_lower(i, s), lane), y);
-        oq[i] = Quad<T>::cvt((x * scal[kScGam * kGdrC + 16 * i + c] + y) * a.scale);
+        for (int s = 0; s <= i / 2; ++s) y = mma<T>(Uf[s], cur.P[img_lower(i, s)], y);
+        const int t = (ch - 1) * kGdrC + 16 * i + c;
+        if (t < sq.len) Quad<T>::st(o + (size_t)t * ors + 4 * g, Quad<T>::cvt((x[i] * cur.gam[i] + y) * a.scale));
       }
     }
-    // S^T <- e^{G_C} S^T + K^T (e^{G_C - G} U)
-    const float gend = scal[kScGam * kGdrC + kGdrC - 1];
+    if (ch < nch) {   // (Q S^T)^T: a lane holds four values of token 16 i + c
+      if constexpr (!AHEAD) load_q(cur, ch);
+      Fi<T, kNear> Sf[NP];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) U[i] *= *reinterpret_cast<const f32x4*>(scal + kScEnd * kGdrC + 16 * i + 4 * g);
-    const Fi<T, kExact> Ue[2] = {to_fi<T, kExact>(U[0], U[1]), to_fi<T, kExact>(U[2], U[3])};
+      for (int p = 0; p < NP; ++p) Sf[p] = to_fi<T, kNear>(S[2 * p], S[2 * p + 1]);
 #pragma unroll
-    for (int j = 0; j < 2 * NP; ++j) {
-      S[j] *= gend;
+      for (int i = 0; i < 4; ++i) {
+        x[i] = zero4();
 #pragma unroll
-      for (int s = 0; s < 2; ++s) S[j] = mma<T>(KR::tr32(buf + L::K, s, j, g, c), Ue[s], S[j]);
+        for (int p = 0; p < NP; ++p) x[i] = mma<T>(Sf[p], cur.q[i][p], x[i]);
+      }
     }
-  }
-  if (nch > 0) store_o(nch - 1);
-  if (a.S_T) {
-    float* s = a.S_T + (size_t)head * sm + soff;
-#pragma unroll
-    for (int j = 0; j < 2 * NP; ++j) *reinterpret_cast<f32x4*>(s + 16 * j) = S[j];
   }
 }
 
@@ -336,7 +404,7 @@ int launch_chain_t(const GdrArgs& a, hipStream_t s) {
   if (hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
     return CARVE_ERR_HIP;
   const unsigned heads = (unsigned)a.nseq * a.Hv;
-  hipLaunchKernelGGL(kern, dim3((heads + 7) / 8 * 8 * (a.Dv / (16 * NW))), dim3(64 * NW), lds, s, a);
+  hipLaunchKernelGGL(kern, dim3((heads + 7) / 8 * 8 * (a.Dv / (16 * NW))), dim3(128 * NW), lds, s, a);
   return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
 }
 template <typename T, int DK>
@@ -344,7 +412,8 @@ int launch_fwd_t(const GdrArgs& a, hipStream_t s, void (*mark)(hipStream_t)) {
   int st = launch_prep_t<T, DK>(a, false, s);
   if (st) return st;
   mark(s);
-  st = gdr_chain_waves(a) == 4 ? launch_chain_t<T, DK, 4>(a, s) : launch_chain_t<T, DK, 2>(a, s);
+  if constexpr (sizeof(T) == 4 && DK == 128) st = launch_chain_t<T, DK, 2>(a, s);
+  else st = gdr_chain_tiles(a, sizeof(T) == 4) == 4 ? launch_chain_t<T, DK, 4>(a, s) : launch_chain_t<T, DK, 2>(a, s);
   mark(s);
   return st;
 }
