@@ -48,17 +48,25 @@ __device__ __forceinline__ void ld_f32(const float* p, float* f, int n) {
 
 // sum over aligned groups of n lanes (n a power of two up to 64, uniform)
 __device__ __forceinline__ float lanes_sum(float x, int n) {
-  for (int m = 1; m < n; m <<= 1) x += __shfl_xor(x, m);
-  return x;
+  switch (n) {
+    case 1: return x;
+    case 2: return group_sum<2>(x);
+    case 4: return group_sum<4>(x);
+    case 8: return group_sum<8>(x);
+    case 16: return group_sum<16>(x);
+    case 32: return group_sum<32>(x);
+    default: return group_sum<64>(x);
+  }
 }
-// sums over the row of two values at once, in every thread of the row
+// Sums over the row of two values at once, in every thread of the row.  One barrier: a
+// buffer is written again only behind another of these sums' (the caller passes each
+// sum of a row its own, and alternates where a row has one alone).
 template <int NT>
 __device__ __forceinline__ void row_sums(float& a, float& b, float* red) {
   a = group_sum<64>(a);
   b = group_sum<64>(b);
   if constexpr (NT > 64) {
     const int w = threadIdx.x >> 6;
-    __syncthreads();
     if ((threadIdx.x & 63) == 0) {
       red[2 * w] = a;
       red[2 * w + 1] = b;
@@ -103,7 +111,7 @@ __device__ __forceinline__ void group_rstd(const float (*y)[Vec<T>::n], float* r
 template <typename T, int NT, int NCH>
 __global__ void __launch_bounds__(256) carve_block_norm_fwd_kernel(BlockNormArgs a) {
   constexpr int V = Vec<T>::n;
-  __shared__ float red[8];
+  __shared__ float red[16];
   const int tid = threadIdx.x % NT;
   const long long row = (long long)blockIdx.x * (256 / NT) + threadIdx.x / NT;
   if (row >= a.rows) return;   // (whole waves; with NT = 256 there is no such row)
@@ -143,7 +151,7 @@ __global__ void __launch_bounds__(256) carve_block_norm_fwd_kernel(BlockNormArgs
     st_vec(reinterpret_cast<T*>(a.x) + row * a.N + c0, y[ch]);
   }
   if (!a.next_weight) return;   // (uniform)
-  row_sums<NT>(ss, none, red);
+  row_sums<NT>(ss, none, red + 8);
   const float r2 = 1.0f / sqrtf(ss / (float)a.N + a.eps);
 #pragma unroll
   for (int ch = 0; ch < NCH; ++ch) {
@@ -159,39 +167,91 @@ __global__ void __launch_bounds__(256) carve_block_norm_fwd_kernel(BlockNormArgs
 
 // Workgroups take rows in turn and keep their share of the parameter gradients in
 // registers; their partial rows, [group][3][N] (dweight, dscale, dnext_weight), are
-// summed in order by the second launch, so reruns are bitwise identical.
+// summed in order by the second launch, so reruns are bitwise identical.  With up to
+// eight columns a thread the parameters stay in registers and the next row is on its way
+// while this one's sums run (AHEAD).
 template <typename T, int NT, int NCH>
 __global__ void __launch_bounds__(256) carve_block_norm_bwd_kernel(BlockNormArgs a) {
   constexpr int V = Vec<T>::n;
-  __shared__ float red[8];
-  extern __shared__ __attribute__((aligned(16))) float sacc[];   // NT = 64: [3][4][N] in turn
+  constexpr bool AHEAD = NCH * V <= 8;
+  __shared__ float red[2][24];
+  extern __shared__ __attribute__((aligned(16))) float sacc[];   // NT = 64: [4][N], a gradient at a time
   const int tid = threadIdx.x % NT, rw = threadIdx.x / NT;
   float aw[NCH][V], as[NCH][V], an[NCH][V];
+  float pw[AHEAD ? NCH : 1][V], ps[AHEAD ? NCH : 1][V], pn[AHEAD ? NCH : 1][V];
 #pragma unroll
-  for (int ch = 0; ch < NCH; ++ch)
+  for (int ch = 0; ch < NCH; ++ch) {
+    const int c0 = (ch * NT + tid) * V;
 #pragma unroll
-    for (int e = 0; e < V; ++e) aw[ch][e] = as[ch][e] = an[ch][e] = 0.0f;
-  const float invN = 1.0f / (float)a.N, invG = 1.0f / (float)(a.N / a.groups);
-  for (long long row = (long long)blockIdx.x * (256 / NT) + rw; row < a.rows; row += (long long)gridDim.x * (256 / NT)) {
-    const T* yp = reinterpret_cast<const T*>(a.y) + row * a.y_stride;
-    const T* zp = reinterpret_cast<const T*>(a.gate) + row * a.gate_stride;
-    const T* rp = reinterpret_cast<const T*>(a.residual) + row * a.residual_stride;
-    float y[NCH][V], z[NCH][V], x[NCH][V], dX[NCH][V], dh[NCH][V];
+    for (int e = 0; e < V; ++e) {
+      aw[ch][e] = as[ch][e] = an[ch][e] = 0.0f;
+      if (AHEAD) pw[AHEAD ? ch : 0][e] = pn[AHEAD ? ch : 0][e] = 0.0f, ps[AHEAD ? ch : 0][e] = 1.0f;
+    }
+    if (AHEAD && c0 < a.N) {
+      ld_f32(a.weight + c0, pw[AHEAD ? ch : 0], V);
+      if (a.scale) ld_f32(a.scale + c0, ps[AHEAD ? ch : 0], V);
+      if (a.next_weight) ld_f32(a.next_weight + c0, pn[AHEAD ? ch : 0], V);
+    }
+  }
+  const auto weight = [&](int ch, float* f) {
+    if constexpr (AHEAD) for (int e = 0; e < V; ++e) f[e] = pw[ch][e];
+    else ld_f32(a.weight + (ch * NT + tid) * V, f, V);
+  };
+  const auto scale = [&](int ch, float* f) {   // (1 where there is none)
+    if constexpr (AHEAD) {
+      for (int e = 0; e < V; ++e) f[e] = ps[ch][e];
+    } else if (a.scale) {
+      ld_f32(a.scale + (ch * NT + tid) * V, f, V);
+    } else {
+      for (int e = 0; e < V; ++e) f[e] = 1.0f;
+    }
+  };
+  const auto next_weight = [&](int ch, float* f) {
+    if constexpr (AHEAD) for (int e = 0; e < V; ++e) f[e] = pn[ch][e];
+    else ld_f32(a.next_weight + (ch * NT + tid) * V, f, V);
+  };
+  // the row's chunks as they are in memory
+  u32x4_t qy[NCH], qz[NCH], qr[NCH], qx[NCH], qh[NCH];
+  const auto load = [&](long long row) {
 #pragma unroll
     for (int ch = 0; ch < NCH; ++ch) {
       const int c0 = (ch * NT + tid) * V;
-#pragma unroll
-      for (int e = 0; e < V; ++e) y[ch][e] = z[ch][e] = x[ch][e] = dX[ch][e] = dh[ch][e] = 0.0f;
+      qy[ch] = qz[ch] = qr[ch] = qx[ch] = qh[ch] = u32x4_t{0, 0, 0, 0};
       if (c0 < a.N) {
-        ld_vec(yp + c0, y[ch]);
-        if (a.gate) ld_vec(zp + c0, z[ch]);
-        if (a.residual && a.next_weight) ld_vec(rp + c0, x[ch]);
-        if (a.dx) ld_vec(reinterpret_cast<const T*>(a.dx) + row * a.N + c0, dX[ch]);
-        if (a.dh) ld_vec(reinterpret_cast<const T*>(a.dh) + row * a.N + c0, dh[ch]);
+        const auto at = [&](const void* p, long long stride) {
+          return *reinterpret_cast<const u32x4_t*>(reinterpret_cast<const T*>(p) + row * stride + c0);
+        };
+        qy[ch] = at(a.y, a.y_stride);
+        if (a.gate) qz[ch] = at(a.gate, a.gate_stride);
+        if (a.residual && a.next_weight) qr[ch] = at(a.residual, a.residual_stride);
+        if (a.dx) qx[ch] = at(a.dx, a.N);
+        if (a.dh) qh[ch] = at(a.dh, a.N);
       }
     }
+  };
+  const float invN = 1.0f / (float)a.N, invG = 1.0f / (float)(a.N / a.groups);
+  const long long step = (long long)gridDim.x * (256 / NT), row0 = (long long)blockIdx.x * (256 / NT) + rw;
+  if (AHEAD && row0 < a.rows) load(row0);
+  int turn = 0;
+  for (long long row = row0; row < a.rows; row += step, turn ^= 1) {
+    if (!AHEAD) load(row);
+    float y[NCH][V], z[NCH][V], x[NCH][V], dX[NCH][V], dh[NCH][V], sg[NCH][V];
+#pragma unroll
+    for (int ch = 0; ch < NCH; ++ch) {
+      Chunk16<T>::unpack(qy[ch], y[ch]);
+      Chunk16<T>::unpack(qz[ch], z[ch]);
+      Chunk16<T>::unpack(qr[ch], x[ch]);
+      Chunk16<T>::unpack(qx[ch], dX[ch]);
+      Chunk16<T>::unpack(qh[ch], dh[ch]);
+    }
+    if (AHEAD && row + step < a.rows) load(row + step);
+    if (a.gate)
+#pragma unroll
+      for (int ch = 0; ch < NCH; ++ch)
+#pragma unroll
+        for (int e = 0; e < V; ++e) sg[ch][e] = sigmoid_x(z[ch][e]);
     float r1[NCH];
-    group_rstd<T, NT, NCH>(y, r1, a, red);
+    group_rstd<T, NT, NCH>(y, r1, a, red[turn]);
     // through the next block's norm
     if (a.next_weight) {
       float ss = 0.0f, mx = 0.0f;
@@ -200,27 +260,27 @@ __global__ void __launch_bounds__(256) carve_block_norm_bwd_kernel(BlockNormArgs
         const int c0 = (ch * NT + tid) * V;
         if (c0 >= a.N) continue;
         float wt[V], sc[V], wn[V];
-        ld_f32(a.weight + c0, wt, V);
-        ld_f32(a.next_weight + c0, wn, V);
-        if (a.scale) ld_f32(a.scale + c0, sc, V);
+        weight(ch, wt);
+        scale(ch, sc);
+        next_weight(ch, wn);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           float t = y[ch][e] * r1[ch] * wt[e];
-          if (a.gate) t *= a.act == CARVE_GATE_SILU ? z[ch][e] * sigmoid_x(z[ch][e]) : sigmoid_x(z[ch][e]);
-          if (a.scale) t *= sc[e];
+          if (a.gate) t *= a.act == CARVE_GATE_SILU ? z[ch][e] * sg[ch][e] : sg[ch][e];
+          t *= sc[e];
           x[ch][e] = a.residual ? a.alpha * x[ch][e] + t : t;
           ss += x[ch][e] * x[ch][e];
           mx += dh[ch][e] * wn[e] * x[ch][e];
         }
       }
-      row_sums<NT>(ss, mx, red);
+      row_sums<NT>(ss, mx, red[turn] + 8);
       const float r2 = 1.0f / sqrtf(ss * invN + a.eps), m2 = r2 * r2 * (mx * invN);
 #pragma unroll
       for (int ch = 0; ch < NCH; ++ch) {
         const int c0 = (ch * NT + tid) * V;
         if (c0 >= a.N) continue;
         float wn[V];
-        ld_f32(a.next_weight + c0, wn, V);
+        next_weight(ch, wn);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           dX[ch][e] += r2 * (dh[ch][e] * wn[e] - x[ch][e] * m2);
@@ -241,19 +301,19 @@ __global__ void __launch_bounds__(256) carve_block_norm_bwd_kernel(BlockNormArgs
         st_vec(reinterpret_cast<T*>(a.dresidual) + row * a.N + c0, o);
       }
       float wt[V], sc[V];
-      ld_f32(a.weight + c0, wt, V);
-      if (a.scale) ld_f32(a.scale + c0, sc, V);
+      weight(ch, wt);
+      scale(ch, sc);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         const float yh = y[ch][e] * r1[ch], nv = yh * wt[e];
         float act = 1.0f, slope = 0.0f;
         if (a.gate) {
-          const float s = sigmoid_x(z[ch][e]);
+          const float s = sg[ch][e];
           act = a.act == CARVE_GATE_SILU ? z[ch][e] * s : s;
           slope = a.act == CARVE_GATE_SILU ? s * (1.0f + z[ch][e] * (1.0f - s)) : s * (1.0f - s);
         }
         as[ch][e] += dX[ch][e] * (nv * act);
-        const float dt = a.scale ? dX[ch][e] * sc[e] : dX[ch][e];
+        const float dt = dX[ch][e] * sc[e];
         z[ch][e] = dt * nv * slope;      // dgate
         const float dn = dt * act;
         aw[ch][e] += dn * yh;
@@ -266,7 +326,7 @@ __global__ void __launch_bounds__(256) carve_block_norm_bwd_kernel(BlockNormArgs
       float s = 0.0f, none = 0.0f;
 #pragma unroll
       for (int ch = 0; ch < NCH; ++ch) s += dot[ch];
-      row_sums<NT>(s, none, red);
+      row_sums<NT>(s, none, red[turn] + 16);
 #pragma unroll
       for (int ch = 0; ch < NCH; ++ch) dot[ch] = s * invG;
     } else {

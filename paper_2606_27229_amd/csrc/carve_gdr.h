@@ -168,33 +168,17 @@ __device__ __forceinline__ f32x4 mma(const Fi<T, N>& a, const Fi<T, N>& b, f32x4
   return c;
 }
 
-// eight consecutive elements of a token row (16-byte aligned), zeros if !ok
+// eight consecutive elements of a token row (16-byte aligned)
 template <typename T>
-__device__ __forceinline__ Fr<T> ld_fr(const T* p, bool ok) {
+__device__ __forceinline__ Fr<T> ld_fr(const T* p) {
   Fr<T> f;
   if constexpr (sizeof(T) == 2) {
-    u32x4_t v = {0, 0, 0, 0};
-    if (ok) v = *reinterpret_cast<const u32x4_t*>(p);
-    const bf16x8 b = __builtin_bit_cast(bf16x8, v);
+    const bf16x8 b = *reinterpret_cast<const bf16x8*>(p);
     f.a = __builtin_shufflevector(b, b, 0, 1, 2, 3);
     f.b = __builtin_shufflevector(b, b, 4, 5, 6, 7);
   } else {
-    f.a = f.b = zero4();
-    if (ok) {
-      f.a = *reinterpret_cast<const f32x4*>(p);
-      f.b = *reinterpret_cast<const f32x4*>(p + 4);
-    }
-  }
-  return f;
-}
-// four consecutive elements at p and four 16 further on
-template <typename T>
-__device__ __forceinline__ Fr<T> ld_fr16(const T* p, bool ok) {
-  Fr<T> f;
-  f.a = f.b = Quad<T>::cvt(zero4());
-  if (ok) {
-    f.a = Quad<T>::ld(p);
-    f.b = Quad<T>::ld(p + 16);
+    f.a = *reinterpret_cast<const f32x4*>(p);
+    f.b = *reinterpret_cast<const f32x4*>(p + 4);
   }
   return f;
 }
@@ -250,6 +234,10 @@ struct GdrWs {
   static constexpr int bT = 0, bScal = I3, bPt = bScal + kGdrScal, bTt = bPt + I3, bBytes = bTt + I3;
 };
 
+// e^x of a decay (x <= 0): one hardware exp2.  The product's rounding moves e^x by
+// |x| 2^-24 of itself, at most 0.4 * 2^-24 in all
+__device__ __forceinline__ float decay_exp(float x) { return exp2_f(x * kLog2e); }
+
 // scalars [5][64] of a chunk: e^G, e^{G_C - G}, beta, and G as a sum of two floats
 enum : int { kScGam = 0, kScEnd = 1, kScBeta = 2, kScGh = 3, kScGl = 4 };
 
@@ -276,15 +264,17 @@ struct GdrRows {
   static_assert(NCH >= 4 && 1024 % RB == 0, "rows of 64 bytes to 1 KB");
   static __device__ __forceinline__ int swz(int r) { return (((r / PER) & MASK) * 2) ^ ((r >> 3) & 1); }
 
-  // wave w of nw takes its share of the 1 KB pieces; rows behind the last of `len`
+  // wave w of NW takes its share of the 1 KB pieces; rows behind the last of `len`
   // repeat it.  base: the first row; stride in bytes, below 2^24
-  static __device__ __forceinline__ void dma(char* lds, const T* base, int stride, int len, int w, int nw, int lane) {
+  template <int NW>
+  static __device__ __forceinline__ void dma(char* lds, const T* base, int stride, int len, int w, int lane) {
     const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<void*>(reinterpret_cast<const void*>(base)), 0, (len - 1) * stride + RB, 0x00027000);
     constexpr int RPI = 1024 / RB;   // rows of a piece
 #pragma unroll
-    for (int i = 0; i < bytes / 1024; ++i) {
-      if (i % nw != w) continue;     // (uniform)
+    for (int u = 0; u < (bytes / 1024 + NW - 1) / NW; ++u) {
+      const int i = w + NW * u;
+      if ((bytes / 1024) % NW != 0 && i >= bytes / 1024) break;   // (uniform)
       const int row = i * RPI + lane / NCH, x = (lane % NCH) ^ swz(row);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(r, lds_at(lds + 1024 * i), 16,
                                                (int)__umul24(min(row, len - 1), stride) + 16 * x, 0, 0, 0);
@@ -327,14 +317,15 @@ struct GdrRows {
     return f;
   }
 };
-// `bytes` (whole KB) of global memory, as they are
-__device__ __forceinline__ void dma_flat(char* lds, const char* src, int bytes, int w, int nw, int lane) {
-  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(src), 0, bytes, 0x00027000);
+// KB * 1024 bytes of global memory as they are, wave w of NW its share
+template <int NW, int KB>
+__device__ __forceinline__ void dma_flat(char* lds, const char* src, int w, int lane) {
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(src), 0, 1024 * KB, 0x00027000);
 #pragma unroll
-  for (int i = 0; i < bytes / 1024; ++i) {
-    if (i % nw != w) continue;   // (uniform)
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, lds_at(lds + 1024 * i), 16,
-                                             1024 * i + 16 * lane, 0, 0, 0);
+  for (int u = 0; u < (KB + NW - 1) / NW; ++u) {
+    const int i = w + NW * u;
+    if (KB % NW != 0 && i >= KB) break;   // (uniform)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, lds_at(lds + 1024 * i), 16, 16 * lane, 1024 * i, 0, 0);
   }
 }
 
@@ -342,12 +333,10 @@ __device__ __forceinline__ void dma_flat(char* lds, const char* src, int bytes, 
 int launch_gdr_fwd(const GdrArgs& a, int dtype, hipStream_t s, void (*mark)(hipStream_t));
 int launch_gdr_bwd(const GdrArgs& a, int dtype, hipStream_t s, void (*mark)(hipStream_t));
 int launch_gdr_prep(const GdrArgs& a, int dtype, bool bwd, hipStream_t s);
-// value tiles of a workgroup of the chains: two up to 512 tiles in all, which gives every
-// compute unit one workgroup; beyond that four tiles share a chunk's rows where their
-// LDS fits (f32 rows of 128 do not)
-inline int gdr_chain_tiles(const GdrArgs& a, bool f32) {
-  return a.Dv % 64 == 0 && (long long)a.nseq * a.Hv * (a.Dv / 16) > 512 && !(f32 && a.Dk == 128) ? 4 : 2;
-}
+// Whether a call has more value tiles than the chains' workgroups of two can run at once
+// (512): then four tiles a workgroup, one chain wave each, give more per compute unit;
+// below it two chain waves a tile run a chunk faster.
+inline bool gdr_many_tiles(const GdrArgs& a) { return a.Dv % 64 == 0 && (long long)a.nseq * a.Hv * (a.Dv / 16) > 512; }
 
 struct GdrStepArgs {
   const void *q, *k, *v, *beta;

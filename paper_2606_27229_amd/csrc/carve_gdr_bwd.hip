@@ -132,14 +132,14 @@ __global__ void __launch_bounds__(128 * NW, 1) carve_gdr_bchain_kernel(GdrArgs a
   const auto load = [&](int ch) {
     char* buf = smem + (ch & 1) * L::one;
     const int t0 = ch * kGdrC, len = min(kGdrC, sq.len - t0);
-    KR::dma(buf + L::K0, k + t0 * a.ks[1], (int)(a.ks[1] * sizeof(T)), len, w, NW, lane);
-    dma_flat(buf + L::I, ws_of(ch) + WS::bScal, kGdrScal, w, NW, lane);
-    dma_flat(buf + L::I + kGdrScal, ws_of(ch) + WS::bTt, WS::I3, w, NW, lane);
+    KR::template dma<NW>(buf + L::K0, k + t0 * a.ks[1], (int)(a.ks[1] * sizeof(T)), len, w, lane);
+    dma_flat<NW, kGdrScal / 1024>(buf + L::I, ws_of(ch) + WS::bScal, w, lane);
+    dma_flat<NW, WS::I3 / 1024>(buf + L::I + kGdrScal, ws_of(ch) + WS::bTt, w, lane);
   };
   const auto load_q = [&](int ch) {
     if constexpr (L::q_lds) {
       const int t0 = ch * kGdrC, len = min(kGdrC, sq.len - t0);
-      KR::dma(smem + L::Q + (ch & 1) * L::qone, q + t0 * a.qs[1], (int)(a.qs[1] * sizeof(T)), len, w, NW, lane);
+      KR::template dma<NW>(smem + L::Q + (ch & 1) * L::qone, q + t0 * a.qs[1], (int)(a.qs[1] * sizeof(T)), len, w, lane);
     }
   };
   struct Mine {
@@ -230,6 +230,252 @@ __global__ void __launch_bounds__(128 * NW, 1) carve_gdr_bchain_kernel(GdrArgs a
       load_m(cur, ch - 1);
     }
     work(cur, ch - 1);
+  }
+}
+
+// ---------------------------------------------------------------------------------
+// The same chain with two waves a tile on it and two helpers, the mirror of
+// carve_gdr_pair_kernel.  Chain wave h keeps dS of the keys' half h, finishes dU of the
+// token tiles 2 h, 2 h + 1 and multiplies by T^T's columns of these tokens.  Helper wave
+// h forms z of the same token tiles and Y of the same keys.
+// Barriers, four a chunk: (1), (2) as above; (3) the halves of K dS^T are there; (4) the
+// parts of dR.
+template <typename T, int DK>
+struct BPairLds {
+  static constexpr int NW = 2;
+  typedef GdrRows<T, DK> KR;
+  static constexpr bool q_lds = sizeof(T) == 2 || DK < 128;       // (f32 queries of 128: from memory)
+  static constexpr int K0 = 0, I = KR::bytes;                     // I: scalars, then T^T
+  static constexpr int one = I + kGdrScal + GdrWs<T>::I3;
+  static constexpr int Q = 2 * one, qone = q_lds ? KR::bytes : 0;
+  // KB of a tile: z, Y, the halves of K dS^T that the other wave takes, dR of wave 1 (its
+  // first two tiles without wave 0's part), that part
+  static constexpr int xz = 0, xY = 4, xP = xY + DK / 16, xU = xP + 4, xV = xU + 4, kb = xV + 2;
+  static constexpr int x = Q + 2 * qone, total = x + NW * kb * 1024;
+};
+
+template <typename T, int DK>
+__global__ void __launch_bounds__(512, 1) carve_gdr_bpair_kernel(GdrArgs a) {
+  constexpr int NP = DK / 32, NW = 2;
+  typedef BPairLds<T, DK> L;
+  typedef typename L::KR KR;
+  typedef GdrWs<T> WS;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const bool helper = wave >= 2 * NW;
+  const int w = (wave >> 1) & (NW - 1), h = wave & 1;
+  const int g = lane >> 4, c = lane & 15;
+  const int ns = a.Dv / (16 * NW), idx = blockIdx.x;
+  const int head = idx / (8 * ns) * 8 + idx % 8, slice = idx / 8 % ns;
+  if (head >= a.nseq * a.Hv) return;
+  const int n = head / a.Hv, hv = head % a.Hv, hk = hv / (a.Hv / a.Hk);
+  const int v0 = 16 * (NW * slice + w);
+  const GdrSeq sq = gdr_seq(a, n);
+  const size_t sm = (size_t)a.Dv * DK, soff = (size_t)(v0 + c) * DK + 16 * NP * h + 4 * g;
+  const int nch = (sq.len + kGdrC - 1) / kGdrC;
+  f32x4* x = reinterpret_cast<f32x4*>(smem + L::x + w * L::kb * 1024) + lane;
+
+  if (!helper) {
+    f32x4 S[NP];   // key tiles NP h ..
+#pragma unroll
+    for (int j = 0; j < NP; ++j)
+      S[j] = a.dS_T ? *reinterpret_cast<const f32x4*>(a.dS_T + (size_t)head * sm + soff + 16 * j) : zero4();
+    if (nch > 0) __syncthreads();   // (0)
+#pragma unroll 1
+    for (int ch = nch - 1; ch >= 0; --ch) {
+      const char* buf = smem + (ch & 1) * L::one;
+      const float* scal = reinterpret_cast<const float*>(buf + L::I);
+      const size_t sh = (size_t)(sq.slot0 + ch) * a.Hv + hv;
+      __syncthreads();   // (1)
+      const float gend = scal[kScGam * kGdrC + kGdrC - 1];
+      float* out = a.dS_chunks + sh * sm + soff;
+      Fi<T, kExact> Sf[NP / 2];
+#pragma unroll
+      for (int p = 0; p < NP / 2; ++p) {
+        Sf[p] = to_fi<T, kExact>(S[2 * p], S[2 * p + 1]);
+#pragma unroll
+        for (int j = 2 * p; j < 2 * p + 2; ++j) {
+          *reinterpret_cast<f32x4*>(out + 16 * j) = S[j];
+          S[j] = S[j] * gend + x[64 * (L::xY + NP * h + j)];
+        }
+      }
+      f32x4 U[2] = {x[64 * (L::xz + 2 * h)], x[64 * (L::xz + 2 * h + 1)]};
+      __syncthreads();   // (2)
+      f32x4 acc[4];      // the other wave's two token tiles, then this one's
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const int i = (2 * (1 - h) + y) & 3;
+        acc[y] = zero4();
+#pragma unroll
+        for (int p = 0; p < NP / 2; ++p) acc[y] = mma<T>(KR::nat(buf + L::K0, i, NP / 2 * h + p, g, c), Sf[p], acc[y]);
+        if (y < 2) x[64 * (L::xP + 2 * h + y)] = acc[y];
+      }
+      __syncthreads();   // (3)
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+        U[y] += (acc[2 + y] + x[64 * (L::xP + 2 * (1 - h) + y)]) *
+                *reinterpret_cast<const f32x4*>(scal + kScEnd * kGdrC + 16 * (2 * h + y) + 4 * g);
+      const Fi<T, kExact> Uf = to_fi<T, kExact>(U[0], U[1]);
+      f32x4 R[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (i >= 2 && !h) continue;   // (uniform)
+        R[i] = mma<T>(ld_img<T, kExact>(buf + L::I + kGdrScal, img_upper(i, h), lane), Uf, zero4());
+        x[64 * (h ? L::xU + i : L::xV + i)] = R[i];
+      }
+      __syncthreads();   // (4)
+      // dR whole; tiles 2 h, 2 h + 1 of it go out
+      float* keep = a.dR + (sh * (a.Dv / 16) + v0 / 16) * 1024 + 4 * lane + 512 * h;
+      if (h) {
+        R[0] += x[64 * L::xV];
+        R[1] += x[64 * (L::xV + 1)];
+        *reinterpret_cast<f32x4*>(keep) = R[2];
+        *reinterpret_cast<f32x4*>(keep + 256) = R[3];
+      } else {
+        R[0] += x[64 * L::xU];
+        R[1] += x[64 * (L::xU + 1)];
+        R[2] = x[64 * (L::xU + 2)];
+        R[3] = x[64 * (L::xU + 3)];
+        *reinterpret_cast<f32x4*>(keep) = R[0];
+        *reinterpret_cast<f32x4*>(keep + 256) = R[1];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        R[i] *= -(*reinterpret_cast<const f32x4*>(scal + kScGam * kGdrC + 16 * i + 4 * g) *
+                  *reinterpret_cast<const f32x4*>(scal + kScBeta * kGdrC + 16 * i + 4 * g));
+      const Fi<T, kExact> Rf[2] = {to_fi<T, kExact>(R[0], R[1]), to_fi<T, kExact>(R[2], R[3])};
+#pragma unroll
+      for (int j = 0; j < NP; ++j)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) S[j] = mma<T>(KR::tr32(buf + L::K0, s, NP * h + j, g, c), Rf[s], S[j]);
+    }
+    if (a.dS0) {
+      float* s = a.dS0 + (size_t)head * sm + soff;
+#pragma unroll
+      for (int j = 0; j < NP; ++j) *reinterpret_cast<f32x4*>(s + 16 * j) = S[j];
+    }
+    return;
+  }
+
+  // ---- helper
+  if (nch == 0) return;   // (no barriers then)
+  const T* q = reinterpret_cast<const T*>(a.q) + sq.batch * a.qs[0] + sq.t0 * a.qs[1] + hk * a.qs[2];
+  const T* k = reinterpret_cast<const T*>(a.k) + sq.batch * a.ks[0] + sq.t0 * a.ks[1] + hk * a.ks[2];
+  const T* dO = reinterpret_cast<const T*>(a.dO) + (((size_t)sq.batch * a.T + sq.t0) * a.Hv + hv) * a.Dv + v0 + c;
+  const size_t ors = (size_t)a.Hv * a.Dv;
+  const int part = wave - 2 * NW;
+  const auto ws_of = [&](int ch) { return a.ws + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * a.per; };
+  const auto load = [&](int ch) {
+    char* buf = smem + (ch & 1) * L::one;
+    const int t0 = ch * kGdrC, len = min(kGdrC, sq.len - t0);
+    KR::template dma<2 * NW>(buf + L::K0, k + t0 * a.ks[1], (int)(a.ks[1] * sizeof(T)), len, part, lane);
+    dma_flat<2 * NW, kGdrScal / 1024>(buf + L::I, ws_of(ch) + WS::bScal, part, lane);
+    dma_flat<2 * NW, WS::I3 / 1024>(buf + L::I + kGdrScal, ws_of(ch) + WS::bTt, part, lane);
+  };
+  const auto load_q = [&](int ch) {
+    if constexpr (L::q_lds) {
+      const int t0 = ch * kGdrC, len = min(kGdrC, sq.len - t0);
+      KR::template dma<2 * NW>(smem + L::Q + (ch & 1) * L::qone, q + t0 * a.qs[1], (int)(a.qs[1] * sizeof(T)), len, part,
+                               lane);
+    }
+  };
+  struct Mine {
+    typename Quad<T>::q od[4];   // dO[t][v]: tokens 16 i + 4 g + e of column c
+    Fi<T, kExact> Pt[2][2];      // (the second of a pair: only tiles 0 and 1)
+    f32x4 gam[4];
+  };
+  const auto load_m = [&](Mine& m, int ch) {
+    const char* ws = ws_of(ch);
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const int i = 2 * h + y;
+      m.Pt[y][0] = ld_img<T, kExact>(ws + WS::bPt, img_upper(i, h ? 1 : 0), lane);
+      if (!h) m.Pt[y][1] = ld_img<T, kExact>(ws + WS::bPt, img_upper(i, 1), lane);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      m.gam[i] = *reinterpret_cast<const f32x4*>(ws + WS::bScal + 4 * (kScGam * kGdrC + 16 * i + 4 * g));
+#pragma unroll
+      for (int e = 0; e < 4; ++e)   // (past the end: the last token, zeroed where it is used)
+        m.od[i][e] = dO[(size_t)min(ch * kGdrC + 16 * i + 4 * g + e, sq.len - 1) * ors];
+    }
+  };
+  const auto work_z = [&](Mine& m, int ch) {
+    const int len = sq.len - ch * kGdrC;
+    if (len < kGdrC)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (16 * i + 4 * g + e >= len) m.od[i][e] = (T)0.0f;
+    const Fr<T> of[2] = {{m.od[0], m.od[1]}, {m.od[2], m.od[3]}};
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      f32x4 z = zero4();
+      if (h) {
+        z = mma<T>(m.Pt[y][0], of[1], z);
+      } else {
+        z = mma<T>(m.Pt[y][0], of[0], z);
+        z = mma<T>(m.Pt[y][1], of[1], z);
+      }
+      x[64 * (L::xz + 2 * h + y)] = z * a.scale;
+    }
+  };
+  const auto work_Y = [&](Mine& m, int ch) {
+    f32x4 od[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) od[i] = Quad<T>::f32(m.od[i]) * (m.gam[i] * a.scale);
+    const Fi<T, kExact> Of[2] = {to_fi<T, kExact>(od[0], od[1]), to_fi<T, kExact>(od[2], od[3])};
+#pragma unroll
+    for (int j = 0; j < NP; ++j) {
+      f32x4 y = zero4();
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        Fr<T> f;
+        if constexpr (L::q_lds) {
+          f = KR::tr32(smem + L::Q + (ch & 1) * L::qone, s, NP * h + j, g, c);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int t = ch * kGdrC + 32 * s + 4 * g + e;
+            f.a[e] = q[(size_t)min(t, sq.len - 1) * a.qs[1] + 16 * (NP * h + j) + c];
+            f.b[e] = q[(size_t)min(t + 16, sq.len - 1) * a.qs[1] + 16 * (NP * h + j) + c];
+          }
+        }
+        y = mma<T>(f, Of[s], y);
+      }
+      x[64 * (L::xY + NP * h + j)] = y;
+    }
+  };
+  Mine cur, nxt;
+  load(nch - 1);
+  load_q(nch - 1);
+  load_m(cur, nch - 1);
+  vm_wait_all();
+  __syncthreads();   // (0) the helpers' shares of the queries
+  work_z(cur, nch - 1);
+  work_Y(cur, nch - 1);
+  if (nch > 1) {
+    load_q(nch - 2);
+    load_m(nxt, nch - 2);
+  }
+#pragma unroll 1
+  for (int ch = nch - 1; ch >= 0; --ch) {
+    vm_wait_all();
+    __syncthreads();   // (1)
+    __syncthreads();   // (2)
+    if (ch > 0) {
+      load(ch - 1);
+      cur = nxt;
+      if (ch > 1) {
+        load_q(ch - 2);
+        load_m(nxt, ch - 2);
+      }
+    }
+    __syncthreads();   // (3)
+    if (ch > 0) work_z(cur, ch - 1);
+    __syncthreads();   // (4)
+    if (ch > 0) work_Y(cur, ch - 1);
   }
 }
 
@@ -364,8 +610,8 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
   const size_t sm = (size_t)a.Dv * DK;
   const size_t ors = (size_t)a.Hv * a.Dv;
   const T* q = reinterpret_cast<const T*>(a.q) + sq.batch * a.qs[0] + t0 * a.qs[1] + hk * a.qs[2];
-  KR::dma(smem + L::K, reinterpret_cast<const T*>(a.k) + sq.batch * a.ks[0] + t0 * a.ks[1] + hk * a.ks[2],
-          (int)(a.ks[1] * sizeof(T)), len, w, 8, lane);
+  KR::template dma<8>(smem + L::K, reinterpret_cast<const T*>(a.k) + sq.batch * a.ks[0] + t0 * a.ks[1] + hk * a.ks[2],
+          (int)(a.ks[1] * sizeof(T)), len, w, lane);
 
   // this wave's key tile and row tiles
   const int jt = w % NJ, i0 = NI * (w / NJ);
@@ -388,12 +634,12 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
       // ---- 1. U and dR of columns vb + 16 w ..
       renew(g, c);
       const T* dO = reinterpret_cast<const T*>(a.dO) + (row0 * a.Hv + hv) * a.Dv + vb;
-      VR::dma(smem + L::V, reinterpret_cast<const T*>(a.v) + sq.batch * a.vs[0] + t0 * a.vs[1] + hv * a.vs[2] + vb,
-              (int)(a.vs[1] * sizeof(T)), len, w, 8, lane);
-      VR::dma(smem + L::O, dO, (int)(ors * sizeof(T)), len, w, 8, lane);
+      VR::template dma<8>(smem + L::V, reinterpret_cast<const T*>(a.v) + sq.batch * a.vs[0] + t0 * a.vs[1] + hv * a.vs[2] + vb,
+              (int)(a.vs[1] * sizeof(T)), len, w, lane);
+      VR::template dma<8>(smem + L::O, dO, (int)(ors * sizeof(T)), len, w, lane);
       const char* ws = a.ws + sh * a.per;
-      dma_flat(smem + L::Z, ws + GdrWs<T>::bT, GdrWs<T>::I3, w, 8, lane);
-      dma_flat(smem + L::scal, ws + GdrWs<T>::bScal, kGdrScal, w, 8, lane);
+      dma_flat<8, GdrWs<T>::I3 / 1024>(smem + L::Z, ws + GdrWs<T>::bT, w, lane);
+      dma_flat<8, kGdrScal / 1024>(smem + L::scal, ws + GdrWs<T>::bScal, w, lane);
       const bool mine = 16 * w < VB;   // (uniform)
       const float* S = a.S_chunks + sh * sm + (size_t)vb * DK;
       const float* dS = a.dS_chunks + sh * sm + (size_t)vb * DK;
@@ -449,7 +695,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
       __syncthreads();
       // ---- 2. products over these columns (queries on their way)
       renew(g, c);
-      if (vb + VB >= a.Dv) KR::dma(smem + L::Z, q, (int)(a.qs[1] * sizeof(T)), len, w, 8, lane);
+      if (vb + VB >= a.Dv) KR::template dma<8>(smem + L::Z, q, (int)(a.qs[1] * sizeof(T)), len, w, lane);
       f32x4 sn[2], dn[2];   // S, dS of the next 32 value columns
       const auto columns = [&](int p) {
 #pragma unroll
@@ -543,7 +789,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
         for (int e = 0; e < 4; ++e) {
           const int ti = 16 * i + 4 * g + e;
           float D = 0.0f;
-          if (tj <= ti && ti < len) D = expf((scal[kScGh * kGdrC + ti] - Ghj) + (scal[kScGl * kGdrC + ti] - Glj));
+          if (tj <= ti && ti < len) D = decay_exp((scal[kScGh * kGdrC + ti] - Ghj) + (scal[kScGl * kGdrC + ti] - Glj));
           const float be = scal[kScBeta * kGdrC + ti], dA = tj < ti ? -aA[x][e] : 0.0f;
           W[e] = a.scale * (D * aP[x][e]);
           M[e] = be * (D * dA);
@@ -675,6 +921,17 @@ int launch_bchain_t(const GdrArgs& a, hipStream_t s) {
   hipLaunchKernelGGL(kern, dim3((heads + 7) / 8 * 8 * (a.Dv / (16 * NW))), dim3(128 * NW), lds, s, a);
   return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
 }
+template <typename T, int DK>
+int launch_bpair_t(const GdrArgs& a, hipStream_t s) {
+  constexpr int lds = BPairLds<T, DK>::total;
+  static_assert(lds <= 160 * 1024, "LDS");
+  const auto kern = carve_gdr_bpair_kernel<T, DK>;
+  const int st = allow_lds(kern, lds);
+  if (st) return st;
+  const unsigned heads = (unsigned)a.nseq * a.Hv;
+  hipLaunchKernelGGL(kern, dim3((heads + 7) / 8 * 8 * (a.Dv / 32)), dim3(512), lds, s, a);
+  return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
+}
 template <typename T, int DK, int VB>
 int launch_grad_t(const GdrArgs& a, hipStream_t s) {
   constexpr int lds = GradLds<T, DK, VB>::total;
@@ -690,8 +947,13 @@ int launch_bwd_t(const GdrArgs& a, hipStream_t s, void (*mark)(hipStream_t)) {
   int st = launch_gdr_prep(a, sizeof(T) == 2 ? CARVE_BF16 : CARVE_F32, true, s);
   if (st) return st;
   mark(s);
-  if constexpr (sizeof(T) == 4 && DK == 128) st = launch_bchain_t<T, DK, 2>(a, s);
-  else st = gdr_chain_tiles(a, sizeof(T) == 4) == 4 ? launch_bchain_t<T, DK, 4>(a, s) : launch_bchain_t<T, DK, 2>(a, s);
+  if constexpr (DK == 32) {
+    st = launch_bchain_t<T, DK, 2>(a, s);
+  } else {
+    constexpr bool four = sizeof(T) == 2 || DK < 128;   // (f32 rows of 128: four tiles' LDS does not fit)
+    if (!four || !gdr_many_tiles(a)) st = launch_bpair_t<T, DK>(a, s);
+    else if constexpr (four) st = launch_bchain_t<T, DK, 4>(a, s);
+  }
   if (st) return st;
   mark(s);
   if (a.Dv == 32) st = launch_grad_t<T, DK, 32>(a, s);

@@ -7,21 +7,23 @@ namespace {
 
 // ---------------------------------------------------------------------------------
 // Chunk-local part: T = (I + A)^-1 and P of every (chunk slot, value head), as
-// operand images, with the chunk's decay factors.  One workgroup of four waves each;
-// wave w forms the row tile w of K K^T and Q K^T.  The diagonal 16 x 16 blocks are
-// inverted by substitution (one lane a column, all four blocks in one wave), the
-// blocks below by T21 = -T22 A21 T11 with f32 matrix-core products, twice.  f32
-// throughout: T multiplies every value of the chunk.
+// operand images, with the chunk's decay factors.  One workgroup of four waves each.
+// Wave w forms the products of token tile w (as columns of the result, so that a lane
+// holds four consecutive entries of a row of A and P: P's image needs no transposition).
+// The diagonal 16 x 16 blocks are inverted by substitution (one lane a column, all four
+// blocks in one wave), the blocks below by T21 = -T22 A21 T11 with f32 matrix-core
+// products, twice.  f32 throughout: T multiplies every value of the chunk.  Bound by the
+// latency of these steps, so what counts is how many workgroups a compute unit holds:
+// A (below the diagonal) and T (transposed, above it) share 17 KB of LDS.
 // G is summed in 64 bits and kept as two floats, so that a decay between two tokens
 // keeps its digits however strongly the tokens before them decay.
 template <typename T, int DK, bool BWD>
-__global__ void __launch_bounds__(256) carve_gdr_prep_kernel(GdrArgs a) {
+__global__ void __launch_bounds__(256, 4) carve_gdr_prep_kernel(GdrArgs a) {
   constexpr int NP = DK / 32;
   constexpr int LD = kGdrC + 4;
-  __shared__ __attribute__((aligned(16))) float sA[kGdrC * LD];
-  __shared__ __attribute__((aligned(16))) float sT[kGdrC * LD];
-  __shared__ __attribute__((aligned(16))) float sP[kGdrC * LD];
-  __shared__ float sGh[kGdrC], sGl[kGdrC], sB[kGdrC];
+  typedef GdrWs<T> WS;
+  __shared__ __attribute__((aligned(16))) float sM[kGdrC * LD];
+  __shared__ __attribute__((aligned(16))) float sGh[kGdrC], sGl[kGdrC], sB[kGdrC];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, c = lane & 15;
   const int slot = blockIdx.x, hv = blockIdx.y, hk = hv / (a.Hv / a.Hk);
@@ -29,22 +31,24 @@ __global__ void __launch_bounds__(256) carve_gdr_prep_kernel(GdrArgs a) {
   int n, chunk;
   if (!gdr_find(a, slot, sq, n, chunk)) return;   // (uniform)
   const int t0 = sq.t0 + chunk * kGdrC, len = min(kGdrC, sq.len - chunk * kGdrC);
-  const T* q = reinterpret_cast<const T*>(a.q) + sq.batch * a.qs[0] + t0 * a.qs[1] + hk * a.qs[2];
-  const T* k = reinterpret_cast<const T*>(a.k) + sq.batch * a.ks[0] + t0 * a.ks[1] + hk * a.ks[2];
+  const T* q = reinterpret_cast<const T*>(a.q) + sq.batch * a.qs[0] + t0 * a.qs[1] + hk * a.qs[2] + 8 * g;
+  const T* k = reinterpret_cast<const T*>(a.k) + sq.batch * a.ks[0] + t0 * a.ks[1] + hk * a.ks[2] + 8 * g;
   const size_t row0 = ((size_t)sq.batch * a.T + t0) * a.Hv + hv;
   char* ws = a.ws + ((size_t)slot * a.Hv + hv) * a.per;
-  typedef GdrWs<T> WS;
   float* scal = reinterpret_cast<float*>(ws + (BWD ? WS::bScal : WS::fScal));
 
-  // row tile w against the column tiles up to it
-  f32x4 kk[4], qk[4];
+  // KK[j]: tokens 16 j + 4 g + e against token 16 w + c; QK[j] the same with the queries
+  // of token 16 w + c (forward), or queries 16 j + 4 g + e against key 16 w + c (backward)
+  f32x4 KK[4], QK[4];
   {
     Fr<T> fk[NP], fq[NP];
-    const int r = 16 * w + c;
+    // (rows behind the last token repeat it: beta is 0 there, and no token before them
+    // sees them)
+    const int r = min(16 * w + c, len - 1);
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      fk[p] = ld_fr<T>(k + r * a.ks[1] + 32 * p + 8 * g, r < len);
-      fq[p] = ld_fr<T>(q + r * a.qs[1] + 32 * p + 8 * g, r < len);
+      fk[p] = ld_fr<T>(k + r * a.ks[1] + 32 * p);
+      if (!BWD) fq[p] = ld_fr<T>(q + r * a.qs[1] + 32 * p);
     }
     if (w == 0) {   // decays: prefix sums over the wave's lanes
       const size_t at = row0 + (size_t)lane * a.Hv;
@@ -62,62 +66,57 @@ __global__ void __launch_bounds__(256) carve_gdr_prep_kernel(GdrArgs a) {
       sGh[lane] = Gh;
       sGl[lane] = Gl;
       sB[lane] = be;
-      scal[kScGam * kGdrC + lane] = expf(Gh) * (1.0f + Gl);
-      scal[kScEnd * kGdrC + lane] = expf((float)(Ge - G));
+      scal[kScGam * kGdrC + lane] = decay_exp(Gh) * (1.0f + Gl);
+      scal[kScEnd * kGdrC + lane] = decay_exp((float)(Ge - G));
       scal[kScBeta * kGdrC + lane] = be;
       scal[kScGh * kGdrC + lane] = Gh;
       scal[kScGl * kGdrC + lane] = Gl;
     }
+    // (all four tiles for every wave, masked below: branches by wave cost more than the
+    // products they save)
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      kk[s] = qk[s] = zero4();
-      if (s <= w) {
-        const int rb = 16 * s + c;
+    for (int j = 0; j < 4; ++j) {
+      KK[j] = QK[j] = zero4();
+      const int ra = min(16 * j + c, len - 1);
 #pragma unroll
-        for (int p = 0; p < NP; ++p) {
-          const Fr<T> fb = ld_fr<T>(k + rb * a.ks[1] + 32 * p + 8 * g, rb < len);
-          kk[s] = mma<T>(fk[p], fb, kk[s]);
-          qk[s] = mma<T>(fq[p], fb, qk[s]);
-        }
+      for (int p = 0; p < NP; ++p) {
+        const Fr<T> fa = ld_fr<T>(k + ra * a.ks[1] + 32 * p);
+        KK[j] = mma<T>(fa, fk[p], KK[j]);
+        if constexpr (BWD) QK[j] = mma<T>(ld_fr<T>(q + ra * a.qs[1] + 32 * p), fk[p], QK[j]);
+        else QK[j] = mma<T>(fa, fq[p], QK[j]);
       }
     }
   }
   __syncthreads();
+  {
+    const int t = 16 * w + c;
+    const float Gh = sGh[t], Gl = sGl[t], be = sB[t];
 #pragma unroll
-  for (int s = 0; s < 4; ++s)
+    for (int j = 0; j < 4; ++j) {
+      const f32x4 gh = *reinterpret_cast<const f32x4*>(sGh + 16 * j + 4 * g);
+      const f32x4 gl = *reinterpret_cast<const f32x4*>(sGl + 16 * j + 4 * g);
+      f32x4 A;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int i = 16 * w + 4 * g + e, j = 16 * s + c;
-      float Av = 0.0f, Pv = 0.0f;
-      if (j <= i) {
-        const float D = expf((sGh[i] - sGh[j]) + (sGl[i] - sGl[j]));
-        Pv = D * qk[s][e];
-        if (j < i) Av = sB[i] * (D * kk[s][e]);
+      for (int e = 0; e < 4; ++e) {
+        const int s = 16 * j + 4 * g + e;
+        // one exponential serves both: of the decay from s to t, or from t to s
+        const float x = (Gh - gh[e]) + (Gl - gl[e]), D = decay_exp(s <= t ? x : -x);
+        A[e] = s < t ? be * (D * KK[j][e]) : 0.0f;
+        QK[j][e] = (BWD ? s >= t : s <= t) ? D * QK[j][e] : 0.0f;
       }
-      sA[i * LD + j] = Av;
-      sP[i * LD + j] = Pv;
-      sT[i * LD + j] = 0.0f;
+      if (j <= w) *reinterpret_cast<f32x4*>(sM + t * LD + 16 * j + 4 * g) = A;   // (uniform)
     }
+    // P's rows, or P^T's, of this wave's tile
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      if (!BWD && s <= w / 2) st_img<T, kNear>(ws + WS::fP, img_lower(w, s), lane, QK[2 * s], QK[2 * s + 1]);
+      if (BWD && s >= w / 2) st_img<T, kExact>(ws + WS::bPt, img_upper(w, s), lane, QK[2 * s], QK[2 * s + 1]);
+    }
+  }
   __syncthreads();
-  // P image by waves 1 - 3, the diagonal inverses by wave 0
-  char* imgP = ws + (BWD ? WS::bPt : WS::fP);
-  if (w > 0) {
-    for (int x = tid - 64; x < 6 * 64; x += 192) {
-      const int f = x >> 6, l = x & 63, lg = l >> 4, lc = l & 15;
-      if constexpr (!BWD) {
-        const int i = f < 2 ? f : 2 + (f - 2) / 2, s = f < 2 ? 0 : (f - 2) % 2;
-        const float* r = sP + (16 * i + lc) * LD + 32 * s + 4 * lg;
-        st_img<T, kNear>(imgP, f, l, *reinterpret_cast<const f32x4*>(r), *reinterpret_cast<const f32x4*>(r + 16));
-      } else {
-        const int i = f < 4 ? f / 2 : f - 2, s = f < 4 ? f % 2 : 1;
-        const float* r = sP + (32 * s + 4 * lg) * LD + 16 * i + lc;
-        const f32x4 x0 = {r[0], r[LD], r[2 * LD], r[3 * LD]};
-        const f32x4 x1 = {r[16 * LD], r[17 * LD], r[18 * LD], r[19 * LD]};
-        st_img<T, kExact>(imgP, f, l, x0, x1);
-      }
-    }
-  } else {
-    const float* A = sA + 16 * g * LD + 16 * g;
+  if (w == 0) {   // diagonal blocks: lane (g, c) column c of block g
+    const float* A = sM + 16 * g * LD + 16 * g;
+    float* Tt = sM + (16 * g + c) * LD + 16 * g;
     float col[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -125,27 +124,34 @@ __global__ void __launch_bounds__(256) carve_gdr_prep_kernel(GdrArgs a) {
 #pragma unroll
       for (int j = 0; j < i; ++j) x -= A[i * LD + j] * col[j];
       col[i] = x;
-      sT[(16 * g + i) * LD + 16 * g + c] = x;
     }
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (i >= c) Tt[i] = col[i];   // (above the diagonal and on it: A's entries stay)
   }
   __syncthreads();
-  // 16 x 16 operands in LDS: A operand rows, B operand columns
-  const auto opA = [&](const float* m, int i, int j) {
-    return *reinterpret_cast<const f32x4*>(m + (16 * i + c) * LD + 16 * j + 4 * g);
-  };
-  const auto opB = [&](const float* m, int i, int j) {
-    const float* r = m + (16 * i + 4 * g) * LD + 16 * j + c;
-    const f32x4 x = {r[0], r[LD], r[2 * LD], r[3 * LD]};
+  // 16 x 16 operands: A's rows; T's rows and columns, zero above T's diagonal
+  const auto opA = [&](int i, int j) { return *reinterpret_cast<const f32x4*>(sM + (16 * i + c) * LD + 16 * j + 4 * g); };
+  const auto rowT = [&](int i, int j) {
+    const float* r = sM + (16 * j + 4 * g) * LD + 16 * i + c;
+    f32x4 x = {r[0], r[LD], r[2 * LD], r[3 * LD]};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (i < j || (i == j && 4 * g + e > c)) x[e] = 0.0f;
     return x;
   };
-  const auto put = [&](int i, int j, f32x4 x) {
+  const auto colT = [&](int i, int j) {
+    f32x4 x = *reinterpret_cast<const f32x4*>(sM + (16 * j + c) * LD + 16 * i + 4 * g);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sT[(16 * i + 4 * g + e) * LD + 16 * j + c] = -x[e];
+    for (int e = 0; e < 4; ++e)
+      if (i < j || (i == j && 4 * g + e < c)) x[e] = 0.0f;
+    return x;
   };
+  const auto put = [&](int i, int j, f32x4 x) { *reinterpret_cast<f32x4*>(sM + (16 * j + c) * LD + 16 * i + 4 * g) = -x; };
   typedef Quad<float> QF;
   if (w < 2) {
-    const f32x4 y = QF::mma16(opA(sA, 2 * w + 1, 2 * w), opB(sT, 2 * w, 2 * w), zero4());
-    put(2 * w + 1, 2 * w, QF::mma16(opA(sT, 2 * w + 1, 2 * w + 1), y, zero4()));
+    const f32x4 y = QF::mma16(opA(2 * w + 1, 2 * w), colT(2 * w, 2 * w), zero4());
+    put(2 * w + 1, 2 * w, QF::mma16(rowT(2 * w + 1, 2 * w + 1), y, zero4()));
   }
   __syncthreads();
   {
@@ -154,27 +160,17 @@ __global__ void __launch_bounds__(256) carve_gdr_prep_kernel(GdrArgs a) {
 #pragma unroll
     for (int kb = 2; kb < 4; ++kb) {
       if (kb > i) continue;
-      f32x4 y = QF::mma16(opA(sA, kb, 1), opB(sT, 1, j), zero4());
-      if (j == 0) y = QF::mma16(opA(sA, kb, 0), opB(sT, 0, 0), y);
-      r = QF::mma16(opA(sT, i, kb), y, r);
+      f32x4 y = QF::mma16(opA(kb, 1), colT(1, j), zero4());
+      if (j == 0) y = QF::mma16(opA(kb, 0), colT(0, 0), y);
+      r = QF::mma16(rowT(i, kb), y, r);
     }
     put(i, j, r);
   }
   __syncthreads();
-  for (int x = tid; x < 6 * 64; x += 256) {
-    const int f = x >> 6, l = x & 63, lg = l >> 4, lc = l & 15;
-    {
-      const int i = f < 2 ? f : 2 + (f - 2) / 2, s = f < 2 ? 0 : (f - 2) % 2;
-      const float* r = sT + (16 * i + lc) * LD + 32 * s + 4 * lg;
-      st_img<T, kExact>(ws, f, l, *reinterpret_cast<const f32x4*>(r), *reinterpret_cast<const f32x4*>(r + 16));
-    }
-    if constexpr (BWD) {
-      const int i = f < 4 ? f / 2 : f - 2, s = f < 4 ? f % 2 : 1;
-      const float* r = sT + (32 * s + 4 * lg) * LD + 16 * i + lc;
-      const f32x4 x0 = {r[0], r[LD], r[2 * LD], r[3 * LD]};
-      const f32x4 x1 = {r[16 * LD], r[17 * LD], r[18 * LD], r[19 * LD]};
-      st_img<T, kExact>(ws + WS::bTt, f, l, x0, x1);
-    }
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    if (s <= w / 2) st_img<T, kExact>(ws, img_lower(w, s), lane, rowT(w, 2 * s), rowT(w, 2 * s + 1));
+    if (BWD && s >= w / 2) st_img<T, kExact>(ws + WS::bTt, img_upper(w, s), lane, colT(2 * s, w), colT(2 * s + 1, w));
   }
 }
 
@@ -296,9 +292,9 @@ __global__ void __launch_bounds__(128 * NW, 1) carve_gdr_chain_kernel(GdrArgs a)
   const auto load = [&](int ch) {
     char* buf = smem + (ch & 1) * L::one;
     const int t0 = ch * kGdrC, len = min(kGdrC, sq.len - t0);
-    KR::dma(buf + L::K, k + t0 * a.ks[1], (int)(a.ks[1] * sizeof(T)), len, w, NW, lane);
-    dma_flat(buf + L::I, a.ws + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * a.per, WS::fP, w, NW, lane);
-    VR::dma(buf + L::V, v + t0 * a.vs[1], (int)(a.vs[1] * sizeof(T)), len, w, NW, lane);
+    KR::template dma<NW>(buf + L::K, k + t0 * a.ks[1], (int)(a.ks[1] * sizeof(T)), len, w, lane);
+    dma_flat<NW, WS::fP / 1024>(buf + L::I, a.ws + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * a.per, w, lane);
+    VR::template dma<NW>(buf + L::V, v + t0 * a.vs[1], (int)(a.vs[1] * sizeof(T)), len, w, lane);
   };
   // queries of a chunk (any row behind the last token repeats it) and P with e^G
   struct Mine {
@@ -389,6 +385,219 @@ __global__ void __launch_bounds__(128 * NW, 1) carve_gdr_chain_kernel(GdrArgs a)
   }
 }
 
+// ---------------------------------------------------------------------------------
+// The same chain with two waves a tile on it and two helpers (keys of 64 and 128), for
+// calls of few tiles, which wait for each chunk's chain: a wave issues an instruction
+// every 7 to 8 cycles on its own, so that the number of instructions between chunk and
+// chunk is what takes the time.  Chain wave h keeps the state of the keys' half h.  K S^T
+// is the sum of both halves' products; each wave finishes two token tiles of it, makes
+// their R and multiplies by T's columns of these tokens; both then add up U and update
+// their half of the state.  Helper wave h takes the outputs of two token tiles.
+// Barriers, four a chunk: (1), (2) as above; (3) the halves of K S^T are there; (4) the
+// parts of U.
+template <typename T, int DK>
+struct PairLds {
+  static constexpr int NW = 2;   // tiles
+  typedef GdrRows<T, DK> KR;
+  typedef GdrRows<T, 16 * NW> VR;
+  static constexpr int K = 0, V = K + KR::bytes, I = V + VR::bytes;   // I: T, scalars
+  static constexpr int one = I + GdrWs<T>::fP;
+  // KB of a tile: S, the halves of K S^T that the other wave takes, U (its last two
+  // tiles without the other wave's part), that part, U's last two tiles
+  static constexpr int xS = 0, xP = DK / 16, xU = xP + 4, xV = xU + 4, xW = xV + 2, kb = xW + 2;
+  static constexpr int x = 2 * one, total = x + NW * kb * 1024;
+};
+
+template <typename T, int DK>
+__global__ void __launch_bounds__(512, 1) carve_gdr_pair_kernel(GdrArgs a) {
+  constexpr int NP = DK / 32, NW = 2;
+  typedef PairLds<T, DK> L;
+  typedef typename L::KR KR;
+  typedef typename L::VR VR;
+  typedef GdrWs<T> WS;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const bool helper = wave >= 2 * NW;
+  const int w = (wave >> 1) & (NW - 1), h = wave & 1;   // tile, half
+  const int g = lane >> 4, c = lane & 15;
+  const int ns = a.Dv / (16 * NW), idx = blockIdx.x;
+  const int head = idx / (8 * ns) * 8 + idx % 8, slice = idx / 8 % ns;
+  if (head >= a.nseq * a.Hv) return;
+  const int n = head / a.Hv, hv = head % a.Hv, hk = hv / (a.Hv / a.Hk);
+  const int vs = 16 * NW * slice, v0 = vs + 16 * w;
+  const GdrSeq sq = gdr_seq(a, n);
+  const size_t sm = (size_t)a.Dv * DK;
+  const size_t soff = (size_t)(v0 + c) * DK + 4 * g;
+  const int nch = (sq.len + kGdrC - 1) / kGdrC;
+  // KB number i of the tile's exchange area, this lane's 16 bytes
+  f32x4* x = reinterpret_cast<f32x4*>(smem + L::x + w * L::kb * 1024) + lane;
+
+  if (!helper) {
+    f32x4 S[NP];   // key tiles NP h ..
+#pragma unroll
+    for (int j = 0; j < NP; ++j) {
+      S[j] = a.S0 ? *reinterpret_cast<const f32x4*>(a.S0 + (size_t)head * sm + soff + 16 * (NP * h + j)) : zero4();
+      x[64 * (L::xS + NP * h + j)] = S[j];
+    }
+#pragma unroll 1
+    for (int ch = 0; ch < nch; ++ch) {
+      const char* buf = smem + (ch & 1) * L::one;
+      const float* scal = reinterpret_cast<const float*>(buf + L::I + WS::fScal);
+      __syncthreads();   // (1)
+      Fi<T, kExact> Sf[NP / 2];
+#pragma unroll
+      for (int p = 0; p < NP / 2; ++p) Sf[p] = to_fi<T, kExact>(S[2 * p], S[2 * p + 1]);
+      __syncthreads();   // (2)
+      f32x4 acc[4];      // the other wave's two token tiles, then this one's
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const int i = (2 * (1 - h) + y) & 3;
+        acc[y] = zero4();
+#pragma unroll
+        for (int p = 0; p < NP / 2; ++p) acc[y] = mma<T>(KR::nat(buf + L::K, i, NP / 2 * h + p, g, c), Sf[p], acc[y]);
+        if (y < 2) x[64 * (L::xP + 2 * h + y)] = acc[y];
+      }
+      const float gend = scal[kScGam * kGdrC + kGdrC - 1];
+#pragma unroll
+      for (int j = 0; j < NP; ++j) S[j] *= gend;
+      __syncthreads();   // (3)
+      f32x4 R[2], U[4];
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const int i = 2 * h + y;
+        const f32x4 gam = *reinterpret_cast<const f32x4*>(scal + kScGam * kGdrC + 16 * i + 4 * g);
+        const f32x4 be = *reinterpret_cast<const f32x4*>(scal + kScBeta * kGdrC + 16 * i + 4 * g);
+        R[y] = be * (Quad<T>::f32(VR::tr(buf + L::V, 16 * i, w, g, c)) - gam * (acc[2 + y] + x[64 * (L::xP + 2 * (1 - h) + y)]));
+      }
+      const Fi<T, kExact> Rf = to_fi<T, kExact>(R[0], R[1]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (i < 2 && h) continue;   // (uniform)
+        U[i] = mma<T>(ld_img<T, kExact>(buf + L::I + WS::fT, img_lower(i, h), lane), Rf, zero4());
+        x[64 * (h ? L::xV + i - 2 : L::xU + i)] = U[i];
+      }
+      __syncthreads();   // (4)
+      if (h == 0) {
+        U[2] += x[64 * L::xV];
+        U[3] += x[64 * (L::xV + 1)];
+      } else {
+        U[0] = x[64 * L::xU];
+        U[1] = x[64 * (L::xU + 1)];
+        U[2] += x[64 * (L::xU + 2)];
+        U[3] += x[64 * (L::xU + 3)];
+        x[64 * L::xW] = U[2];
+        x[64 * (L::xW + 1)] = U[3];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) U[i] *= *reinterpret_cast<const f32x4*>(scal + kScEnd * kGdrC + 16 * i + 4 * g);
+      const Fi<T, kExact> Ue[2] = {to_fi<T, kExact>(U[0], U[1]), to_fi<T, kExact>(U[2], U[3])};
+#pragma unroll
+      for (int j = 0; j < NP; ++j) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) S[j] = mma<T>(KR::tr32(buf + L::K, s, NP * h + j, g, c), Ue[s], S[j]);
+        x[64 * (L::xS + NP * h + j)] = S[j];
+      }
+    }
+    __syncthreads();
+    if (a.S_T) {
+      float* s = a.S_T + (size_t)head * sm + soff + 16 * NP * h;
+#pragma unroll
+      for (int j = 0; j < NP; ++j) *reinterpret_cast<f32x4*>(s + 16 * j) = S[j];
+    }
+    return;
+  }
+
+  // ---- helper: token tiles 2 h, 2 h + 1
+  const T* q = reinterpret_cast<const T*>(a.q) + sq.batch * a.qs[0] + sq.t0 * a.qs[1] + hk * a.qs[2];
+  const T* k = reinterpret_cast<const T*>(a.k) + sq.batch * a.ks[0] + sq.t0 * a.ks[1] + hk * a.ks[2];
+  const T* v = reinterpret_cast<const T*>(a.v) + sq.batch * a.vs[0] + sq.t0 * a.vs[1] + hv * a.vs[2] + vs;
+  T* o = reinterpret_cast<T*>(a.o) + (((size_t)sq.batch * a.T + sq.t0) * a.Hv + hv) * a.Dv + v0;
+  const size_t ors = (size_t)a.Hv * a.Dv;
+  const auto load = [&](int ch) {
+    char* buf = smem + (ch & 1) * L::one;
+    const int t0 = ch * kGdrC, len = min(kGdrC, sq.len - t0), part = wave - 2 * NW;
+    KR::template dma<2 * NW>(buf + L::K, k + t0 * a.ks[1], (int)(a.ks[1] * sizeof(T)), len, part, lane);
+    dma_flat<2 * NW, WS::fP / 1024>(buf + L::I, a.ws + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * a.per, part, lane);
+    VR::template dma<2 * NW>(buf + L::V, v + t0 * a.vs[1], (int)(a.vs[1] * sizeof(T)), len, part, lane);
+  };
+  struct Mine {
+    Fr<T> q[2][NP];
+    Fi<T, kNear> P[2][2];   // (the second of a pair: only tiles 2 and 3)
+    float gam[2];
+  };
+  const auto load_q = [&](Mine& m, int ch) {
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const T* r = q + (size_t)min(ch * kGdrC + 16 * (2 * h + y) + c, sq.len - 1) * a.qs[1] + 4 * g;
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        m.q[y][p].a = Quad<T>::ld(r + 32 * p);
+        m.q[y][p].b = Quad<T>::ld(r + 32 * p + 16);
+      }
+    }
+  };
+  const auto load_p = [&](Mine& m, int ch) {
+    const char* img = a.ws + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * a.per;
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const int i = 2 * h + y;
+      m.P[y][0] = ld_img<T, kNear>(img + WS::fP, img_lower(i, 0), lane);
+      if (h) m.P[y][1] = ld_img<T, kNear>(img + WS::fP, img_lower(i, 1), lane);
+      m.gam[y] = reinterpret_cast<const float*>(img + WS::fScal)[kScGam * kGdrC + 16 * i + c];
+    }
+  };
+  Mine cur, nxt;
+  f32x4 xo[2];
+  if (nch > 0) {
+    load(0);
+    load_q(nxt, 0);
+  }
+#pragma unroll 1
+  for (int ch = 0; ch <= nch; ++ch) {
+    vm_wait_all();
+    __syncthreads();   // (1)
+    f32x4 S[2 * NP], U[4];
+#pragma unroll
+    for (int j = 0; j < 2 * NP; ++j) S[j] = x[64 * (L::xS + j)];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) U[i] = x[64 * (i < 2 ? L::xU + i : L::xW + i - 2)];
+    if (ch < nch) __syncthreads();   // (2)
+    if (ch + 1 < nch) load(ch + 1);
+    cur = nxt;   // (this chunk's queries, the last one's P)
+    if (ch + 1 < nch) load_q(nxt, ch + 1);
+    if (ch < nch) load_p(nxt, ch);
+    if (a.S_chunks && ch < nch) {
+      float* s = a.S_chunks + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * sm + soff;
+#pragma unroll
+      for (int j = 0; j < 2 * NP; ++j)
+        if (j / NP == h) *reinterpret_cast<f32x4*>(s + 16 * j) = S[j];
+    }
+    if (ch < nch) __syncthreads();   // (3)
+    if (ch > 0) {   // o of the last chunk
+      const Fi<T, kNear> Uf[2] = {to_fi<T, kNear>(U[0], U[1]), to_fi<T, kNear>(U[2], U[3])};
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        f32x4 z = mma<T>(Uf[0], cur.P[y][0], zero4());
+        if (h) z = mma<T>(Uf[1], cur.P[y][1], z);
+        const int t = (ch - 1) * kGdrC + 16 * (2 * h + y) + c;
+        if (t < sq.len) Quad<T>::st(o + (size_t)t * ors + 4 * g, Quad<T>::cvt((xo[y] * cur.gam[y] + z) * a.scale));
+      }
+    }
+    if (ch < nch) {
+      __syncthreads();   // (4)
+      Fi<T, kNear> Sf[NP];
+#pragma unroll
+      for (int p = 0; p < NP; ++p) Sf[p] = to_fi<T, kNear>(S[2 * p], S[2 * p + 1]);
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        xo[y] = zero4();
+#pragma unroll
+        for (int p = 0; p < NP; ++p) xo[y] = mma<T>(Sf[p], cur.q[y][p], xo[y]);
+      }
+    }
+  }
+}
+
 template <typename T, int DK>
 int launch_prep_t(const GdrArgs& a, bool bwd, hipStream_t s) {
   const dim3 grid(a.nslots, a.Hv);
@@ -408,12 +617,28 @@ int launch_chain_t(const GdrArgs& a, hipStream_t s) {
   return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
 }
 template <typename T, int DK>
+int launch_pair_t(const GdrArgs& a, hipStream_t s) {
+  constexpr int lds = PairLds<T, DK>::total;
+  static_assert(lds <= 160 * 1024, "LDS");
+  const auto kern = carve_gdr_pair_kernel<T, DK>;
+  if (hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
+    return CARVE_ERR_HIP;
+  const unsigned heads = (unsigned)a.nseq * a.Hv;
+  hipLaunchKernelGGL(kern, dim3((heads + 7) / 8 * 8 * (a.Dv / 32)), dim3(512), lds, s, a);
+  return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
+}
+template <typename T, int DK>
 int launch_fwd_t(const GdrArgs& a, hipStream_t s, void (*mark)(hipStream_t)) {
   int st = launch_prep_t<T, DK>(a, false, s);
   if (st) return st;
   mark(s);
-  if constexpr (sizeof(T) == 4 && DK == 128) st = launch_chain_t<T, DK, 2>(a, s);
-  else st = gdr_chain_tiles(a, sizeof(T) == 4) == 4 ? launch_chain_t<T, DK, 4>(a, s) : launch_chain_t<T, DK, 2>(a, s);
+  if constexpr (DK == 32) {
+    st = launch_chain_t<T, DK, 2>(a, s);
+  } else {
+    constexpr bool four = sizeof(T) == 2 || DK < 128;   // (f32 rows of 128: four tiles' LDS does not fit)
+    if (!four || !gdr_many_tiles(a)) st = launch_pair_t<T, DK>(a, s);
+    else if constexpr (four) st = launch_chain_t<T, DK, 4>(a, s);
+  }
   mark(s);
   return st;
 }
