@@ -329,6 +329,18 @@ __device__ __forceinline__ void dma_flat(char* lds, const char* src, int w, int 
   }
 }
 
+// ---- workgroups of the chains ---------------------------------------------------------
+// Workgroup -> (sequence, value head) and value slice (of ns).  Blocks 8 apart share an
+// XCD; each XCD takes a run of consecutive heads, all slices of a head one after another,
+// so that the slices, and the value heads of a key head, read the same rows from one L2.
+__host__ __device__ inline unsigned gdr_chain_grid(unsigned heads, int ns) { return (heads + 7) / 8 * 8 * ns; }
+__device__ __forceinline__ bool gdr_chain_block(const GdrArgs& a, int ns, int& head, int& slice) {
+  const int heads = a.nseq * a.Hv, run = (heads + 7) / 8, at = blockIdx.x / 8;
+  head = (int)(blockIdx.x % 8) * run + at / ns;
+  slice = at % ns;
+  return at / ns < run && head < heads;
+}
+
 // launches (carve_gdr_*.hip); mark: called after every launch
 int launch_gdr_fwd(const GdrArgs& a, int dtype, hipStream_t s, void (*mark)(hipStream_t));
 int launch_gdr_bwd(const GdrArgs& a, int dtype, hipStream_t s, void (*mark)(hipStream_t));

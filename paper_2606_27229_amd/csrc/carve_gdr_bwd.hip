@@ -48,9 +48,8 @@ __global__ void __launch_bounds__(128 * NW, 1) carve_gdr_bchain_kernel(GdrArgs a
   const bool helper = wave >= NW;
   const int w = helper ? wave - NW : wave;
   const int g = lane >> 4, c = lane & 15;
-  const int ns = a.Dv / (16 * NW), idx = blockIdx.x;
-  const int head = idx / (8 * ns) * 8 + idx % 8, slice = idx / 8 % ns;
-  if (head >= a.nseq * a.Hv) return;
+  int head, slice;
+  if (!gdr_chain_block(a, a.Dv / (16 * NW), head, slice)) return;
   const int n = head / a.Hv, hv = head % a.Hv, hk = hv / (a.Hv / a.Hk);
   const int v0 = 16 * (NW * slice + w);
   const GdrSeq sq = gdr_seq(a, n);
@@ -244,6 +243,7 @@ template <typename T, int DK>
 struct BPairLds {
   static constexpr int NW = 2;
   typedef GdrRows<T, DK> KR;
+  typedef GdrRows<T, 16 * NW> VR;
   static constexpr bool q_lds = sizeof(T) == 2 || DK < 128;       // (f32 queries of 128: from memory)
   static constexpr int K0 = 0, I = KR::bytes;                     // I: scalars, then T^T
   static constexpr int one = I + kGdrScal + GdrWs<T>::I3;
@@ -251,7 +251,8 @@ struct BPairLds {
   // KB of a tile: z, Y, the halves of K dS^T that the other wave takes, dR of wave 1 (its
   // first two tiles without wave 0's part), that part
   static constexpr int xz = 0, xY = 4, xP = xY + DK / 16, xU = xP + 4, xV = xU + 4, kb = xV + 2;
-  static constexpr int x = Q + 2 * qone, total = x + NW * kb * 1024;
+  static constexpr int O = Q + 2 * qone;                          // dO of the workgroup's columns
+  static constexpr int x = O + 2 * VR::bytes, total = x + NW * kb * 1024;
 };
 
 template <typename T, int DK>
@@ -259,15 +260,15 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_bpair_kernel(GdrArgs a) {
   constexpr int NP = DK / 32, NW = 2;
   typedef BPairLds<T, DK> L;
   typedef typename L::KR KR;
+  typedef typename L::VR VR;
   typedef GdrWs<T> WS;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const bool helper = wave >= 2 * NW;
   const int w = (wave >> 1) & (NW - 1), h = wave & 1;
   const int g = lane >> 4, c = lane & 15;
-  const int ns = a.Dv / (16 * NW), idx = blockIdx.x;
-  const int head = idx / (8 * ns) * 8 + idx % 8, slice = idx / 8 % ns;
-  if (head >= a.nseq * a.Hv) return;
+  int head, slice;
+  if (!gdr_chain_block(a, a.Dv / (16 * NW), head, slice)) return;
   const int n = head / a.Hv, hv = head % a.Hv, hk = hv / (a.Hv / a.Hk);
   const int v0 = 16 * (NW * slice + w);
   const GdrSeq sq = gdr_seq(a, n);
@@ -361,7 +362,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_bpair_kernel(GdrArgs a) {
   if (nch == 0) return;   // (no barriers then)
   const T* q = reinterpret_cast<const T*>(a.q) + sq.batch * a.qs[0] + sq.t0 * a.qs[1] + hk * a.qs[2];
   const T* k = reinterpret_cast<const T*>(a.k) + sq.batch * a.ks[0] + sq.t0 * a.ks[1] + hk * a.ks[2];
-  const T* dO = reinterpret_cast<const T*>(a.dO) + (((size_t)sq.batch * a.T + sq.t0) * a.Hv + hv) * a.Dv + v0 + c;
+  const T* dO = reinterpret_cast<const T*>(a.dO) + (((size_t)sq.batch * a.T + sq.t0) * a.Hv + hv) * a.Dv + 16 * NW * slice;
   const size_t ors = (size_t)a.Hv * a.Dv;
   const int part = wave - 2 * NW;
   const auto ws_of = [&](int ch) { return a.ws + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * a.per; };
@@ -372,15 +373,15 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_bpair_kernel(GdrArgs a) {
     dma_flat<2 * NW, kGdrScal / 1024>(buf + L::I, ws_of(ch) + WS::bScal, part, lane);
     dma_flat<2 * NW, WS::I3 / 1024>(buf + L::I + kGdrScal, ws_of(ch) + WS::bTt, part, lane);
   };
-  const auto load_q = [&](int ch) {
+  const auto load_q = [&](int ch) {   // and dO
+    const int t0 = ch * kGdrC, len = min(kGdrC, sq.len - t0);
+    VR::template dma<2 * NW>(smem + L::O + (ch & 1) * VR::bytes, dO + t0 * ors, (int)(ors * sizeof(T)), len, part, lane);
     if constexpr (L::q_lds) {
-      const int t0 = ch * kGdrC, len = min(kGdrC, sq.len - t0);
       KR::template dma<2 * NW>(smem + L::Q + (ch & 1) * L::qone, q + t0 * a.qs[1], (int)(a.qs[1] * sizeof(T)), len, part,
                                lane);
     }
   };
   struct Mine {
-    typename Quad<T>::q od[4];   // dO[t][v]: tokens 16 i + 4 g + e of column c
     Fi<T, kExact> Pt[2][2];      // (the second of a pair: only tiles 0 and 1)
     f32x4 gam[4];
   };
@@ -393,22 +394,21 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_bpair_kernel(GdrArgs a) {
       if (!h) m.Pt[y][1] = ld_img<T, kExact>(ws + WS::bPt, img_upper(i, 1), lane);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 4; ++i)
       m.gam[i] = *reinterpret_cast<const f32x4*>(ws + WS::bScal + 4 * (kScGam * kGdrC + 16 * i + 4 * g));
-#pragma unroll
-      for (int e = 0; e < 4; ++e)   // (past the end: the last token, zeroed where it is used)
-        m.od[i][e] = dO[(size_t)min(ch * kGdrC + 16 * i + 4 * g + e, sq.len - 1) * ors];
-    }
   };
+  typename Quad<T>::q od[4];   // dO[t][v]: tokens 16 i + 4 g + e of column c, zeros behind the last
   const auto work_z = [&](Mine& m, int ch) {
     const int len = sq.len - ch * kGdrC;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) od[i] = VR::tr(smem + L::O + (ch & 1) * VR::bytes, 16 * i, w, g, c);
     if (len < kGdrC)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (16 * i + 4 * g + e >= len) m.od[i][e] = (T)0.0f;
-    const Fr<T> of[2] = {{m.od[0], m.od[1]}, {m.od[2], m.od[3]}};
+          if (16 * i + 4 * g + e >= len) od[i][e] = (T)0.0f;
+    const Fr<T> of[2] = {{od[0], od[1]}, {od[2], od[3]}};
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
       f32x4 z = zero4();
@@ -422,10 +422,10 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_bpair_kernel(GdrArgs a) {
     }
   };
   const auto work_Y = [&](Mine& m, int ch) {
-    f32x4 od[4];
+    f32x4 og[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) od[i] = Quad<T>::f32(m.od[i]) * (m.gam[i] * a.scale);
-    const Fi<T, kExact> Of[2] = {to_fi<T, kExact>(od[0], od[1]), to_fi<T, kExact>(od[2], od[3])};
+    for (int i = 0; i < 4; ++i) og[i] = Quad<T>::f32(od[i]) * (m.gam[i] * a.scale);
+    const Fi<T, kExact> Of[2] = {to_fi<T, kExact>(og[0], og[1]), to_fi<T, kExact>(og[2], og[3])};
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
       f32x4 y = zero4();
@@ -918,7 +918,7 @@ int launch_bchain_t(const GdrArgs& a, hipStream_t s) {
   const int st = allow_lds(kern, lds);
   if (st) return st;
   const unsigned heads = (unsigned)a.nseq * a.Hv;
-  hipLaunchKernelGGL(kern, dim3((heads + 7) / 8 * 8 * (a.Dv / (16 * NW))), dim3(128 * NW), lds, s, a);
+  hipLaunchKernelGGL(kern, dim3(gdr_chain_grid(heads, a.Dv / (16 * NW))), dim3(128 * NW), lds, s, a);
   return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
 }
 template <typename T, int DK>
@@ -929,7 +929,7 @@ int launch_bpair_t(const GdrArgs& a, hipStream_t s) {
   const int st = allow_lds(kern, lds);
   if (st) return st;
   const unsigned heads = (unsigned)a.nseq * a.Hv;
-  hipLaunchKernelGGL(kern, dim3((heads + 7) / 8 * 8 * (a.Dv / 32)), dim3(512), lds, s, a);
+  hipLaunchKernelGGL(kern, dim3(gdr_chain_grid(heads, a.Dv / 32)), dim3(512), lds, s, a);
   return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
 }
 template <typename T, int DK, int VB>

@@ -211,10 +211,8 @@ __global__ void __launch_bounds__(128 * NW, 1) carve_gdr_chain_kernel(GdrArgs a)
   const bool helper = wave >= NW;
   const int w = helper ? wave - NW : wave;   // tile
   const int g = lane >> 4, c = lane & 15;
-  // blocks 8 apart share an XCD: the slices of a (sequence, head) follow each other there
-  const int ns = a.Dv / (16 * NW), idx = blockIdx.x;
-  const int head = idx / (8 * ns) * 8 + idx % 8, slice = idx / 8 % ns;
-  if (head >= a.nseq * a.Hv) return;
+  int head, slice;
+  if (!gdr_chain_block(a, a.Dv / (16 * NW), head, slice)) return;
   const int n = head / a.Hv, hv = head % a.Hv, hk = hv / (a.Hv / a.Hk);
   const int vs = 16 * NW * slice, v0 = vs + 16 * w;
   const GdrSeq sq = gdr_seq(a, n);
@@ -405,7 +403,9 @@ struct PairLds {
   // KB of a tile: S, the halves of K S^T that the other wave takes, U (its last two
   // tiles without the other wave's part), that part, U's last two tiles
   static constexpr int xS = 0, xP = DK / 16, xU = xP + 4, xV = xU + 4, xW = xV + 2, kb = xW + 2;
-  static constexpr int x = 2 * one, total = x + NW * kb * 1024;
+  static constexpr bool q_lds = sizeof(T) == 2 || DK < 128;           // (f32 queries of 128: from memory)
+  static constexpr int Q = 2 * one, qone = q_lds ? KR::bytes : 0;
+  static constexpr int x = Q + 2 * qone, total = x + NW * kb * 1024;
 };
 
 template <typename T, int DK>
@@ -420,9 +420,8 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_pair_kernel(GdrArgs a) {
   const bool helper = wave >= 2 * NW;
   const int w = (wave >> 1) & (NW - 1), h = wave & 1;   // tile, half
   const int g = lane >> 4, c = lane & 15;
-  const int ns = a.Dv / (16 * NW), idx = blockIdx.x;
-  const int head = idx / (8 * ns) * 8 + idx % 8, slice = idx / 8 % ns;
-  if (head >= a.nseq * a.Hv) return;
+  int head, slice;
+  if (!gdr_chain_block(a, a.Dv / (16 * NW), head, slice)) return;
   const int n = head / a.Hv, hv = head % a.Hv, hk = hv / (a.Hv / a.Hk);
   const int vs = 16 * NW * slice, v0 = vs + 16 * w;
   const GdrSeq sq = gdr_seq(a, n);
@@ -513,27 +512,35 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_pair_kernel(GdrArgs a) {
   const T* v = reinterpret_cast<const T*>(a.v) + sq.batch * a.vs[0] + sq.t0 * a.vs[1] + hv * a.vs[2] + vs;
   T* o = reinterpret_cast<T*>(a.o) + (((size_t)sq.batch * a.T + sq.t0) * a.Hv + hv) * a.Dv + v0;
   const size_t ors = (size_t)a.Hv * a.Dv;
-  const auto load = [&](int ch) {
+  const int part = wave - 2 * NW;
+  const auto load_k = [&](int ch) {
+    const int t0 = ch * kGdrC, len = min(kGdrC, sq.len - t0);
+    KR::template dma<2 * NW>(smem + (ch & 1) * L::one + L::K, k + t0 * a.ks[1], (int)(a.ks[1] * sizeof(T)), len, part, lane);
+  };
+  const auto load_t = [&](int ch) {   // T, decays, values
     char* buf = smem + (ch & 1) * L::one;
-    const int t0 = ch * kGdrC, len = min(kGdrC, sq.len - t0), part = wave - 2 * NW;
-    KR::template dma<2 * NW>(buf + L::K, k + t0 * a.ks[1], (int)(a.ks[1] * sizeof(T)), len, part, lane);
+    const int t0 = ch * kGdrC, len = min(kGdrC, sq.len - t0);
     dma_flat<2 * NW, WS::fP / 1024>(buf + L::I, a.ws + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * a.per, part, lane);
     VR::template dma<2 * NW>(buf + L::V, v + t0 * a.vs[1], (int)(a.vs[1] * sizeof(T)), len, part, lane);
   };
   struct Mine {
-    Fr<T> q[2][NP];
     Fi<T, kNear> P[2][2];   // (the second of a pair: only tiles 2 and 3)
     float gam[2];
   };
-  const auto load_q = [&](Mine& m, int ch) {
-#pragma unroll
-    for (int y = 0; y < 2; ++y) {
-      const T* r = q + (size_t)min(ch * kGdrC + 16 * (2 * h + y) + c, sq.len - 1) * a.qs[1] + 4 * g;
-#pragma unroll
-      for (int p = 0; p < NP; ++p) {
-        m.q[y][p].a = Quad<T>::ld(r + 32 * p);
-        m.q[y][p].b = Quad<T>::ld(r + 32 * p + 16);
-      }
+  // queries go through LDS like the keys: a wave that loads 16 rows' pieces of 8 bytes
+  // itself takes as long as all else together (63 cycles an instruction)
+  const auto load_q = [&](int ch) {
+    if constexpr (L::q_lds) {
+      const int t0 = ch * kGdrC, len = min(kGdrC, sq.len - t0);
+      KR::template dma<2 * NW>(smem + L::Q + (ch & 1) * L::qone, q + t0 * a.qs[1], (int)(a.qs[1] * sizeof(T)), len, part, lane);
+    }
+  };
+  const auto query = [&](int ch, int y, int p) {
+    if constexpr (L::q_lds) {
+      return KR::nat(smem + L::Q + (ch & 1) * L::qone, 2 * h + y, p, g, c);
+    } else {
+      const T* r = q + (size_t)min(ch * kGdrC + 16 * (2 * h + y) + c, sq.len - 1) * a.qs[1] + 32 * p + 4 * g;
+      return Fr<T>{Quad<T>::ld(r), Quad<T>::ld(r + 16)};
     }
   };
   const auto load_p = [&](Mine& m, int ch) {
@@ -548,9 +555,20 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_pair_kernel(GdrArgs a) {
   };
   Mine cur, nxt;
   f32x4 xo[2];
+  // (o^T of a chunk goes out an iteration later, before the loads: the wait at (1) covers
+  // stores too)
+  typename Quad<T>::q oq[2];
+  const auto store_o = [&](int ch) {
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const int t = ch * kGdrC + 16 * (2 * h + y) + c;
+      if (t < sq.len) Quad<T>::st(o + (size_t)t * ors + 4 * g, oq[y]);
+    }
+  };
   if (nch > 0) {
-    load(0);
-    load_q(nxt, 0);
+    load_k(0);
+    load_t(0);
+    load_q(0);
   }
 #pragma unroll 1
   for (int ch = 0; ch <= nch; ++ch) {
@@ -562,10 +580,11 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_pair_kernel(GdrArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) U[i] = x[64 * (i < 2 ? L::xU + i : L::xW + i - 2)];
     if (ch < nch) __syncthreads();   // (2)
-    if (ch + 1 < nch) load(ch + 1);
-    cur = nxt;   // (this chunk's queries, the last one's P)
-    if (ch + 1 < nch) load_q(nxt, ch + 1);
-    if (ch < nch) load_p(nxt, ch);
+    // memory instructions wait for each other (a KB of rows takes some 40 cycles), and the
+    // chain waits for the helpers at each barrier, so they are spread over its steps
+    if (ch > 1) store_o(ch - 2);
+    if (ch + 1 < nch) load_k(ch + 1);
+    cur = nxt;   // (the last chunk's P)
     if (a.S_chunks && ch < nch) {
       float* s = a.S_chunks + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * sm + soff;
 #pragma unroll
@@ -573,18 +592,20 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_pair_kernel(GdrArgs a) {
         if (j / NP == h) *reinterpret_cast<f32x4*>(s + 16 * j) = S[j];
     }
     if (ch < nch) __syncthreads();   // (3)
+    if (ch + 1 < nch) load_t(ch + 1);
     if (ch > 0) {   // o of the last chunk
       const Fi<T, kNear> Uf[2] = {to_fi<T, kNear>(U[0], U[1]), to_fi<T, kNear>(U[2], U[3])};
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
         f32x4 z = mma<T>(Uf[0], cur.P[y][0], zero4());
         if (h) z = mma<T>(Uf[1], cur.P[y][1], z);
-        const int t = (ch - 1) * kGdrC + 16 * (2 * h + y) + c;
-        if (t < sq.len) Quad<T>::st(o + (size_t)t * ors + 4 * g, Quad<T>::cvt((xo[y] * cur.gam[y] + z) * a.scale));
+        oq[y] = Quad<T>::cvt((xo[y] * cur.gam[y] + z) * a.scale);
       }
     }
     if (ch < nch) {
       __syncthreads();   // (4)
+      if (ch + 1 < nch) load_q(ch + 1);
+      load_p(nxt, ch);
       Fi<T, kNear> Sf[NP];
 #pragma unroll
       for (int p = 0; p < NP; ++p) Sf[p] = to_fi<T, kNear>(S[2 * p], S[2 * p + 1]);
@@ -592,10 +613,11 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_pair_kernel(GdrArgs a) {
       for (int y = 0; y < 2; ++y) {
         xo[y] = zero4();
 #pragma unroll
-        for (int p = 0; p < NP; ++p) xo[y] = mma<T>(Sf[p], cur.q[y][p], xo[y]);
+        for (int p = 0; p < NP; ++p) xo[y] = mma<T>(Sf[p], query(ch, y, p), xo[y]);
       }
     }
   }
+  if (nch > 0) store_o(nch - 1);
 }
 
 template <typename T, int DK>
@@ -613,7 +635,7 @@ int launch_chain_t(const GdrArgs& a, hipStream_t s) {
   if (hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
     return CARVE_ERR_HIP;
   const unsigned heads = (unsigned)a.nseq * a.Hv;
-  hipLaunchKernelGGL(kern, dim3((heads + 7) / 8 * 8 * (a.Dv / (16 * NW))), dim3(128 * NW), lds, s, a);
+  hipLaunchKernelGGL(kern, dim3(gdr_chain_grid(heads, a.Dv / (16 * NW))), dim3(128 * NW), lds, s, a);
   return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
 }
 template <typename T, int DK>
@@ -624,7 +646,7 @@ int launch_pair_t(const GdrArgs& a, hipStream_t s) {
   if (hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
     return CARVE_ERR_HIP;
   const unsigned heads = (unsigned)a.nseq * a.Hv;
-  hipLaunchKernelGGL(kern, dim3((heads + 7) / 8 * 8 * (a.Dv / 32)), dim3(512), lds, s, a);
+  hipLaunchKernelGGL(kern, dim3(gdr_chain_grid(heads, a.Dv / 32)), dim3(512), lds, s, a);
   return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
 }
 template <typename T, int DK>
