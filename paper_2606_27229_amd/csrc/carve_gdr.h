@@ -329,6 +329,20 @@ __device__ __forceinline__ void dma_flat(char* lds, const char* src, int w, int 
   }
 }
 
+// ---- two waves of a workgroup meeting ---------------------------------------------------
+// Wave `me` (0 or 1) tells the other that its LDS writes so far are done and waits for the
+// same word of it.  A wave's LDS accesses are carried out in order, so the flag (the
+// `turn`-th meeting, counted from 1) follows the data.  Both waves belong to one workgroup
+// and meet equally often, so the wait ends; it costs the other waves nothing, where a
+// barrier would hold them to these two waves' pace.
+__device__ __forceinline__ void pair_meet(volatile int* flags, int me, int turn) {
+  asm volatile("" ::: "memory");
+  flags[me] = turn;
+  while (__builtin_amdgcn_readfirstlane(flags[1 - me]) < turn) {
+  }
+  asm volatile("" ::: "memory");
+}
+
 // ---- workgroups of the chains ---------------------------------------------------------
 // Workgroup -> (sequence, value head) and value slice (of ns).  Blocks 8 apart share an
 // XCD; each XCD takes a run of consecutive heads, all slices of a head one after another,

@@ -237,8 +237,8 @@ __global__ void __launch_bounds__(128 * NW, 1) carve_gdr_bchain_kernel(GdrArgs a
 // carve_gdr_pair_kernel.  Chain wave h keeps dS of the keys' half h, finishes dU of the
 // token tiles 2 h, 2 h + 1 and multiplies by T^T's columns of these tokens.  Helper wave
 // h forms z of the same token tiles and Y of the same keys.
-// Barriers, four a chunk: (1), (2) as above; (3) the halves of K dS^T are there; (4) the
-// parts of dR.
+// Two barriers a chunk, (1) and (2) as above; the chain waves of a tile meet by flags: (3)
+// the halves of K dS^T are there; (4) the parts of dR.
 template <typename T, int DK>
 struct BPairLds {
   static constexpr int NW = 2;
@@ -252,7 +252,7 @@ struct BPairLds {
   // first two tiles without wave 0's part), that part
   static constexpr int xz = 0, xY = 4, xP = xY + DK / 16, xU = xP + 4, xV = xU + 4, kb = xV + 2;
   static constexpr int O = Q + 2 * qone;                          // dO of the workgroup's columns
-  static constexpr int x = O + 2 * VR::bytes, total = x + NW * kb * 1024;
+  static constexpr int x = O + 2 * VR::bytes, flags = x + NW * kb * 1024, total = flags + NW * 16;
 };
 
 template <typename T, int DK>
@@ -276,7 +276,10 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_bpair_kernel(GdrArgs a) {
   const int nch = (sq.len + kGdrC - 1) / kGdrC;
   f32x4* x = reinterpret_cast<f32x4*>(smem + L::x + w * L::kb * 1024) + lane;
 
+  volatile int* flags = reinterpret_cast<volatile int*>(smem + L::flags + 16 * w);
+
   if (!helper) {
+    flags[h] = 0;   // (seen by the other wave behind the first barrier)
     f32x4 S[NP];   // key tiles NP h ..
 #pragma unroll
     for (int j = 0; j < NP; ++j)
@@ -311,7 +314,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_bpair_kernel(GdrArgs a) {
         for (int p = 0; p < NP / 2; ++p) acc[y] = mma<T>(KR::nat(buf + L::K0, i, NP / 2 * h + p, g, c), Sf[p], acc[y]);
         if (y < 2) x[64 * (L::xP + 2 * h + y)] = acc[y];
       }
-      __syncthreads();   // (3)
+      pair_meet(flags, h, 2 * (nch - 1 - ch) + 1);   // (3)
 #pragma unroll
       for (int y = 0; y < 2; ++y)
         U[y] += (acc[2 + y] + x[64 * (L::xP + 2 * (1 - h) + y)]) *
@@ -324,7 +327,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_bpair_kernel(GdrArgs a) {
         R[i] = mma<T>(ld_img<T, kExact>(buf + L::I + kGdrScal, img_upper(i, h), lane), Uf, zero4());
         x[64 * (h ? L::xU + i : L::xV + i)] = R[i];
       }
-      __syncthreads();   // (4)
+      pair_meet(flags, h, 2 * (nch - 1 - ch) + 2);   // (4)
       // dR whole; tiles 2 h, 2 h + 1 of it go out
       float* keep = a.dR + (sh * (a.Dv / 16) + v0 / 16) * 1024 + 4 * lane + 512 * h;
       if (h) {
@@ -472,10 +475,10 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_bpair_kernel(GdrArgs a) {
         load_m(nxt, ch - 2);
       }
     }
-    __syncthreads();   // (3)
-    if (ch > 0) work_z(cur, ch - 1);
-    __syncthreads();   // (4)
-    if (ch > 0) work_Y(cur, ch - 1);
+    if (ch > 0) {
+      work_z(cur, ch - 1);
+      work_Y(cur, ch - 1);
+    }
   }
 }
 

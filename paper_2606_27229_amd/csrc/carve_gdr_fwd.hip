@@ -391,8 +391,10 @@ __global__ void __launch_bounds__(128 * NW, 1) carve_gdr_chain_kernel(GdrArgs a)
 // is the sum of both halves' products; each wave finishes two token tiles of it, makes
 // their R and multiplies by T's columns of these tokens; both then add up U and update
 // their half of the state.  Helper wave h takes the outputs of two token tiles.
-// Barriers, four a chunk: (1), (2) as above; (3) the halves of K S^T are there; (4) the
-// parts of U.
+// Two barriers a chunk, (1) and (2) as above; the chain waves of a tile meet twice more,
+// by flags in LDS: (3) the halves of K S^T are there; (4) the parts of U.  With barriers
+// for these too the helpers, whose memory instructions wait for each other (some 45 cycles
+// a KB), held the chain up: 214 us a call of 64 chunks of 64 heads.
 template <typename T, int DK>
 struct PairLds {
   static constexpr int NW = 2;   // tiles
@@ -405,7 +407,7 @@ struct PairLds {
   static constexpr int xS = 0, xP = DK / 16, xU = xP + 4, xV = xU + 4, xW = xV + 2, kb = xW + 2;
   static constexpr bool q_lds = sizeof(T) == 2 || DK < 128;           // (f32 queries of 128: from memory)
   static constexpr int Q = 2 * one, qone = q_lds ? KR::bytes : 0;
-  static constexpr int x = Q + 2 * qone, total = x + NW * kb * 1024;
+  static constexpr int x = Q + 2 * qone, flags = x + NW * kb * 1024, total = flags + NW * 16;
 };
 
 template <typename T, int DK>
@@ -431,7 +433,10 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_pair_kernel(GdrArgs a) {
   // KB number i of the tile's exchange area, this lane's 16 bytes
   f32x4* x = reinterpret_cast<f32x4*>(smem + L::x + w * L::kb * 1024) + lane;
 
+  volatile int* flags = reinterpret_cast<volatile int*>(smem + L::flags + 16 * w);
+
   if (!helper) {
+    flags[h] = 0;   // (seen by the other wave behind the first barrier)
     f32x4 S[NP];   // key tiles NP h ..
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
@@ -459,7 +464,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_pair_kernel(GdrArgs a) {
       const float gend = scal[kScGam * kGdrC + kGdrC - 1];
 #pragma unroll
       for (int j = 0; j < NP; ++j) S[j] *= gend;
-      __syncthreads();   // (3)
+      pair_meet(flags, h, 2 * ch + 1);   // (3)
       f32x4 R[2], U[4];
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
@@ -475,7 +480,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_pair_kernel(GdrArgs a) {
         U[i] = mma<T>(ld_img<T, kExact>(buf + L::I + WS::fT, img_lower(i, h), lane), Rf, zero4());
         x[64 * (h ? L::xV + i - 2 : L::xU + i)] = U[i];
       }
-      __syncthreads();   // (4)
+      pair_meet(flags, h, 2 * ch + 2);   // (4)
       if (h == 0) {
         U[2] += x[64 * L::xV];
         U[3] += x[64 * (L::xV + 1)];
@@ -580,19 +585,20 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_pair_kernel(GdrArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) U[i] = x[64 * (i < 2 ? L::xU + i : L::xW + i - 2)];
     if (ch < nch) __syncthreads();   // (2)
-    // memory instructions wait for each other (a KB of rows takes some 40 cycles), and the
-    // chain waits for the helpers at each barrier, so they are spread over its steps
     if (ch > 1) store_o(ch - 2);
-    if (ch + 1 < nch) load_k(ch + 1);
+    if (ch + 1 < nch) {
+      load_k(ch + 1);
+      load_t(ch + 1);
+      load_q(ch + 1);
+    }
     cur = nxt;   // (the last chunk's P)
+    if (ch < nch) load_p(nxt, ch);
     if (a.S_chunks && ch < nch) {
       float* s = a.S_chunks + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * sm + soff;
 #pragma unroll
       for (int j = 0; j < 2 * NP; ++j)
         if (j / NP == h) *reinterpret_cast<f32x4*>(s + 16 * j) = S[j];
     }
-    if (ch < nch) __syncthreads();   // (3)
-    if (ch + 1 < nch) load_t(ch + 1);
     if (ch > 0) {   // o of the last chunk
       const Fi<T, kNear> Uf[2] = {to_fi<T, kNear>(U[0], U[1]), to_fi<T, kNear>(U[2], U[3])};
 #pragma unroll
@@ -603,9 +609,6 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_pair_kernel(GdrArgs a) {
       }
     }
     if (ch < nch) {
-      __syncthreads();   // (4)
-      if (ch + 1 < nch) load_q(ch + 1);
-      load_p(nxt, ch);
       Fi<T, kNear> Sf[NP];
 #pragma unroll
       for (int p = 0; p < NP; ++p) Sf[p] = to_fi<T, kNear>(S[2 * p], S[2 * p + 1]);
