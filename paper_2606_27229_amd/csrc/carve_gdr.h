@@ -335,7 +335,8 @@ __device__ __forceinline__ void dma_flat(char* lds, const char* src, int w, int 
 // `turn`-th meeting, counted from 1) follows the data.  Both waves belong to one workgroup
 // and meet equally often, so the wait ends; it costs the other waves nothing, where a
 // barrier would hold them to these two waves' pace.
-__device__ __forceinline__ void pair_meet(volatile int* flags, int me, int turn) {
+typedef volatile __attribute__((address_space(3))) int lds_flag;
+__device__ __forceinline__ void pair_meet(lds_flag* flags, int me, int turn) {
   asm volatile("" ::: "memory");
   flags[me] = turn;
   while (__builtin_amdgcn_readfirstlane(flags[1 - me]) < turn) {

@@ -276,7 +276,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_bpair_kernel(GdrArgs a) {
   const int nch = (sq.len + kGdrC - 1) / kGdrC;
   f32x4* x = reinterpret_cast<f32x4*>(smem + L::x + w * L::kb * 1024) + lane;
 
-  volatile int* flags = reinterpret_cast<volatile int*>(smem + L::flags + 16 * w);
+  lds_flag* flags = (lds_flag*)lds_at(smem + L::flags + 16 * w);
 
   if (!helper) {
     flags[h] = 0;   // (seen by the other wave behind the first barrier)
