@@ -183,6 +183,17 @@ __device__ __forceinline__ Fr<T> ld_fr(const T* p) {
   return f;
 }
 
+template <typename T>
+__device__ __forceinline__ void st_eight(T* p, f32x4 lo, f32x4 hi) {
+  if constexpr (sizeof(T) == 2) {
+    const bf16x4 a = Quad<T>::cvt(lo), b = Quad<T>::cvt(hi);
+    *reinterpret_cast<bf16x8*>(p) = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+  } else {
+    *reinterpret_cast<f32x4*>(p) = lo;
+    *reinterpret_cast<f32x4*>(p + 4) = hi;
+  }
+}
+
 // ---- triangular operand images ----------------------------------------------------------
 // A 64 x 64 triangle as A operands of depth 32 over its columns: fragment (i, s)
 // holds rows 16 i .. and columns 32 s .. + 31, lane (g, c) the columns 32 s + 4 g + e
@@ -240,6 +251,16 @@ __device__ __forceinline__ float decay_exp(float x) { return exp2_f(x * kLog2e);
 
 // scalars [5][64] of a chunk: e^G, e^{G_C - G}, beta, and G as a sum of two floats
 enum : int { kScGam = 0, kScEnd = 1, kScBeta = 2, kScGh = 3, kScGl = 4 };
+
+// sum over the 16 lanes of a row, in every lane (group_sum<16> in forms that fold into the
+// additions: every lane has a source, so the bound control changes nothing)
+__device__ __forceinline__ float row_sum(float x) {
+  x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0xB1, 0xf, 0xf, true));
+  x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x4E, 0xf, 0xf, true));
+  x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x141, 0xf, 0xf, true));
+  x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x140, 0xf, 0xf, true));
+  return x;
+}
 
 // lane coordinates the compiler takes as new: what is computed from them is computed
 // where it is used, not ahead of a loop and kept

@@ -541,6 +541,27 @@ struct InterT {
     }
     return f;
   }
+  // lane (g, c): token 16 i + c, the eight columns col0 + 8 g .., as f32 sums of N pieces
+  template <int N>
+  static __device__ __forceinline__ void eight(const char* m, int i, int col0, int g, int c, f32x4& lo, f32x4& hi) {
+    const T* p = reinterpret_cast<const T*>(m);
+    lo = hi = zero4();
+    if constexpr (sizeof(T) == 2) {
+      const int r = col0 + 8 * g + (c >> 2);
+#pragma unroll
+      for (int y = N - 1; y >= 0; --y) {
+        lo += Quad<T>::f32(Quad<T>::ld_tr_at(p + y * plane + r * LD + 4 * ((4 * i + (c & 3)) ^ sw(r))));
+        hi += Quad<T>::f32(Quad<T>::ld_tr_at(p + y * plane + (r + 4) * LD + 4 * ((4 * i + (c & 3)) ^ sw(r + 4))));
+      }
+    } else {
+      const T* q = p + (col0 + 8 * g) * LD + 16 * i + c;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        lo[e] = q[e * LD];
+        hi[e] = q[(4 + e) * LD];
+      }
+    }
+  }
   // lane (g, c): column col0 + c, tokens 32 s + 4 g + e and 32 s + 16 + 4 g + e
   template <int N>
   static __device__ __forceinline__ Fi<T, N> col(const char* m, int col0, int s, int g, int c) {
@@ -676,7 +697,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int at = w * kGdrC + 16 * i + 4 * g + e;
-            const float s1 = group_sum<16>(R[i][e] * vt[i][e]), s2 = group_sum<16>(R[i][e] * x[e]);
+            const float s1 = row_sum(R[i][e] * vt[i][e]), s2 = row_sum(R[i][e] * x[e]);
             if (c == 0) {
               rRV[at] = vb ? rRV[at] + s1 : s1;
               rRK[at] = vb ? rRK[at] + s2 : s2;
@@ -741,22 +762,13 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
           }
         }
       }
-      // dV = beta dR, four values of a token a lane
+      // dV = beta dR, eight values of a token a lane
       for (int x = w; x < 4 * NV; x += 8) {
         const int i = x & 3, p = x >> 2, t = 16 * i + c;
-        const Fi<T, kExact> f = UT::template tok<kExact>(smem + L::R, i, 32 * p, g, c);
-        f32x4 lo = zero4(), hi = zero4();
-#pragma unroll
-        for (int y = (sizeof(T) == 2 ? kExact : 1) - 1; y >= 0; --y) {
-          lo += Quad<T>::f32(f.x[y].a);
-          hi += Quad<T>::f32(f.x[y].b);
-        }
-        if (t < len) {
-          const float be = scal[kScBeta * kGdrC + t];
-          T* d = reinterpret_cast<T*>(a.dv) + ((row0 + t) * a.Hv + hv) * a.Dv + vb + 32 * p + 4 * g;
-          Quad<T>::st(d, Quad<T>::cvt(lo * be));
-          Quad<T>::st(d + 16, Quad<T>::cvt(hi * be));
-        }
+        f32x4 lo, hi;
+        UT::template eight<kExact>(smem + L::R, i, 32 * p, g, c, lo, hi);
+        const float be = scal[kScBeta * kGdrC + t];
+        if (t < len) st_eight(reinterpret_cast<T*>(a.dv) + ((row0 + t) * a.Hv + hv) * a.Dv + vb + 32 * p + 8 * g, lo * be, hi * be);
       }
       if (vb + VB >= a.Dv) vm_wait_all();
       __syncthreads();
@@ -799,7 +811,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
           // (a token's product with itself is a row and a column term of one G: no change)
           const float pp = tj < ti ? W[e] * qk[e] : 0.0f, ab = D * dA * kk[e], sum = pp + be * ab;
           col += sum;
-          const float rs = group_sum<16>(sum), rb = group_sum<16>(ab);
+          const float rs = row_sum(sum), rb = row_sum(ab);
           if (c == 0) {
             rRow[j * kGdrC + ti] = rs;
             rBeta[j * kGdrC + ti] = rb;
@@ -827,7 +839,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
       const f32x4 qt = Quad<T>::f32(KR::tr(smem + L::Z, 16 * i, jt, g, c));
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float s1 = group_sum<16>(qt[e] * x1[e]), s2 = group_sum<16>(kt[e] * x2[e]);
+        const float s1 = row_sum(qt[e] * x1[e]), s2 = row_sum(kt[e] * x2[e]);
         if (c == 0) {
           rQ[jt * kGdrC + 16 * i + 4 * g + e] = s1;
           rUK[jt * kGdrC + 16 * i + 4 * g + e] = s2;
@@ -890,18 +902,24 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
     __syncthreads();
   }
 
-  T* dq = reinterpret_cast<T*>(a.dq) + (row0 * a.Hk + hk) * DK + 16 * jt + c;
-  T* dk = reinterpret_cast<T*>(a.dk) + (row0 * a.Hk + hk) * DK + 16 * jt + c;
+  // out through LDS, 16 bytes a lane (from the results' layout a store would cover 32
+  // bytes of each of 4 rows)
+  typedef InterT<T, DK> DT;
+  static_assert(2 * DT::bytes(1) <= L::total, "over what is no longer needed");
 #pragma unroll
-  for (int ii = 0; ii < NI; ++ii)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int t = 16 * (i0 + ii) + 4 * g + e;
-      if (t < len) {
-        dq[(size_t)t * a.Hk * DK] = (T)dQ[ii][e];
-        dk[(size_t)t * a.Hk * DK] = (T)dK[ii][e];
-      }
-    }
+  for (int ii = 0; ii < NI; ++ii) {
+    DT::template put<1>(smem, 16 * jt + c, i0 + ii, g, dQ[ii]);
+    DT::template put<1>(smem + DT::bytes(1), 16 * jt + c, i0 + ii, g, dK[ii]);
+  }
+  __syncthreads();
+  for (int x = w; x < 8 * NP; x += 8) {
+    const int i = x & 3, p = (x >> 2) % NP, t = 16 * i + c;
+    const bool second = x >= 4 * NP;
+    f32x4 lo, hi;
+    DT::template eight<1>(smem + (second ? DT::bytes(1) : 0), i, 32 * p, g, c, lo, hi);
+    T* out = reinterpret_cast<T*>(second ? a.dk : a.dq) + ((row0 + t) * a.Hk + hk) * DK + 32 * p + 8 * g;
+    if (t < len) st_eight(out, lo, hi);
+  }
 }
 
 // dynamic LDS above 64 KB needs the attribute once per kernel and device

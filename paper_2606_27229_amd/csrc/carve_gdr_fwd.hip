@@ -657,13 +657,10 @@ int launch_fwd_t(const GdrArgs& a, hipStream_t s, void (*mark)(hipStream_t)) {
   int st = launch_prep_t<T, DK>(a, false, s);
   if (st) return st;
   mark(s);
-  if constexpr (DK == 32) {
-    st = launch_chain_t<T, DK, 2>(a, s);
-  } else {
-    constexpr bool four = sizeof(T) == 2 || DK < 128;   // (f32 rows of 128: four tiles' LDS does not fit)
-    if (!four || !gdr_many_tiles(a)) st = launch_pair_t<T, DK>(a, s);
-    else if constexpr (four) st = launch_chain_t<T, DK, 4>(a, s);
-  }
+  // (two waves a tile also where many tiles share the card: 8 x 1024 tokens of 32 heads of
+  // 128, 2048 tiles: 239 us; one wave a tile, four tiles a workgroup: 318 us)
+  if constexpr (DK == 32) st = launch_chain_t<T, DK, 2>(a, s);
+  else st = launch_pair_t<T, DK>(a, s);
   mark(s);
   return st;
 }
