@@ -602,7 +602,9 @@ struct GradLds {
   static constexpr int total = red + floats * 4;
 };
 
-template <typename T, int DK, int VB>
+// NB: blocks of VB value columns (with one, no product has to live through another block's
+// first part)
+template <typename T, int DK, int VB, int NB>
 __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
   typedef GradLds<T, DK, VB> L;
   typedef typename L::KR KR;
@@ -647,14 +649,18 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
     const size_t sh = (size_t)slot * a.Hv + hv;
     f32x4 aP[2], aA[2];                     // tile tasks w and w + 8 (of ten)
     f32x4 a1[NI], a2[NI], a3[NI];           // dO S, U dS, dR S
-#pragma unroll
-    for (int x = 0; x < 2; ++x) aP[x] = aA[x] = zero4();
-#pragma unroll
-    for (int i = 0; i < NI; ++i) a1[i] = a2[i] = a3[i] = zero4();
     float ss = 0.0f;
+    const auto clear = [&] {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) aP[x] = aA[x] = zero4();
+#pragma unroll
+      for (int i = 0; i < NI; ++i) a1[i] = a2[i] = a3[i] = zero4();
+    };
+    if (NB > 1) clear();
 
 #pragma unroll 1
-    for (int vb = 0; vb < a.Dv; vb += VB) {
+    for (int b = 0; b < NB; ++b) {
+      const int vb = b * VB;
       // ---- 1. U and dR of columns vb + 16 w ..
       renew(g, c);
       const T* dO = reinterpret_cast<const T*>(a.dO) + (row0 * a.Hv + hv) * a.Dv + vb;
@@ -719,7 +725,8 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
       __syncthreads();
       // ---- 2. products over these columns (queries on their way)
       renew(g, c);
-      if (vb + VB >= a.Dv) KR::template dma<8>(smem + L::Z, q, (int)(a.qs[1] * sizeof(T)), len, w, lane);
+      if (NB == 1) clear();
+      if (b + 1 == NB) KR::template dma<8>(smem + L::Z, q, (int)(a.qs[1] * sizeof(T)), len, w, lane);
       f32x4 sn[2], dn[2];   // S, dS of the next 32 value columns
       const auto columns = [&](int p) {
 #pragma unroll
@@ -770,7 +777,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
         const float be = scal[kScBeta * kGdrC + t];
         if (t < len) st_eight(reinterpret_cast<T*>(a.dv) + ((row0 + t) * a.Hv + hv) * a.Dv + vb + 32 * p + 8 * g, lo * be, hi * be);
       }
-      if (vb + VB >= a.Dv) vm_wait_all();
+      if (b + 1 == NB) vm_wait_all();
       __syncthreads();
     }
 
@@ -953,11 +960,11 @@ int launch_bpair_t(const GdrArgs& a, hipStream_t s) {
   hipLaunchKernelGGL(kern, dim3(gdr_chain_grid(heads, a.Dv / 32)), dim3(512), lds, s, a);
   return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
 }
-template <typename T, int DK, int VB>
+template <typename T, int DK, int VB, int NB>
 int launch_grad_t(const GdrArgs& a, hipStream_t s) {
   constexpr int lds = GradLds<T, DK, VB>::total;
   static_assert(lds <= 160 * 1024, "LDS");
-  const auto kern = carve_gdr_grad_kernel<T, DK, VB>;
+  const auto kern = carve_gdr_grad_kernel<T, DK, VB, NB>;
   const int st = allow_lds(kern, lds);
   if (st) return st;
   hipLaunchKernelGGL(kern, dim3(a.nslots, a.Hk), dim3(512), lds, s, a);
@@ -977,9 +984,10 @@ int launch_bwd_t(const GdrArgs& a, hipStream_t s, void (*mark)(hipStream_t)) {
   }
   if (st) return st;
   mark(s);
-  if (a.Dv == 32) st = launch_grad_t<T, DK, 32>(a, s);
-  else if (a.Dv == 64 || sizeof(T) == 4) st = launch_grad_t<T, DK, 64>(a, s);   // (f32 at 128 columns: 177 KB)
-  else st = launch_grad_t<T, DK, sizeof(T) == 4 ? 64 : 128>(a, s);
+  if (a.Dv == 32) st = launch_grad_t<T, DK, 32, 1>(a, s);
+  else if (a.Dv == 64) st = launch_grad_t<T, DK, 64, 1>(a, s);
+  else if constexpr (sizeof(T) == 2) st = a.Dv == 128 ? launch_grad_t<T, DK, 128, 1>(a, s) : launch_grad_t<T, DK, 128, 2>(a, s);
+  else st = a.Dv == 128 ? launch_grad_t<T, DK, 64, 2>(a, s) : launch_grad_t<T, DK, 64, 4>(a, s);   // (128 columns: 177 KB)
   mark(s);
   return st;
 }
