@@ -252,14 +252,20 @@ __device__ __forceinline__ float decay_exp(float x) { return exp2_f(x * kLog2e);
 // scalars [5][64] of a chunk: e^G, e^{G_C - G}, beta, and G as a sum of two floats
 enum : int { kScGam = 0, kScEnd = 1, kScBeta = 2, kScGh = 3, kScGl = 4 };
 
-// sum over the 16 lanes of a row, in every lane (group_sum<16> in forms that fold into the
-// additions: every lane has a source, so the bound control changes nothing)
-__device__ __forceinline__ float row_sum(float x) {
-  x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0xB1, 0xf, 0xf, true));
-  x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x4E, 0xf, 0xf, true));
-  x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x141, 0xf, 0xf, true));
-  x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x140, 0xf, 0xf, true));
-  return x;
+// Sums over the 16 lanes of a row of four values at once: lane c gets that of value
+// c mod 4.  Neighbouring lanes swap the values the other one keeps, twice, and the four
+// quads of the row are added up (11 operations; each value's butterfly on its own 16 to 24).
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float row_sum4(f32x4 v, int c) {
+  const bool b0 = c & 1, b1 = c & 2;
+  const float r0 = (b0 ? v[1] : v[0]) + dpp<0xB1>(b0 ? v[0] : v[1]);   // lane ^ 1
+  const float r1 = (b0 ? v[3] : v[2]) + dpp<0xB1>(b0 ? v[2] : v[3]);
+  float q = (b1 ? r1 : r0) + dpp<0x4E>(b1 ? r0 : r1);                  // lane ^ 2
+  q += dpp<0x128>(q);                                                  // the row turned by 8 lanes
+  return q + dpp<0x124>(q);                                            // and by 4
 }
 
 // lane coordinates the compiler takes as new: what is computed from them is computed

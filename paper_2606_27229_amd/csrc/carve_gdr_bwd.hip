@@ -645,6 +645,44 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
 #pragma unroll
   for (int i = 0; i < NI; ++i) dQ[i] = dK[i] = zero4();
 
+  // dbeta and dg of a value head, by one wave
+  const auto finish = [&](int hv) {
+    const int t = lane;
+    float rv1 = 0.0f, rk1 = 0.0f, s1 = 0.0f, s2 = 0.0f, sss = 0.0f, row = 0.0f, rb = 0.0f, col = 0.0f;
+    for (int x = 0; x < VB / 16; ++x) {
+      rv1 += rRV[x * kGdrC + t];
+      rk1 += rRK[x * kGdrC + t];
+    }
+    for (int x = 0; x < 8; ++x) sss += rSS[x];
+    for (int x = 0; x < NJ; ++x) {
+      s1 += rQ[x * kGdrC + t];
+      s2 += rUK[x * kGdrC + t];
+    }
+    for (int x = 0; x < 4; ++x) {
+      if (x <= t / 16) {
+        row += rRow[x * kGdrC + t];
+        rb += rBeta[x * kGdrC + t];
+      }
+      if (x >= t / 16) col += rCol[x * kGdrC + t];
+    }
+    const float be = scal[kScBeta * kGdrC + t];
+    float dG = s1 - be * rk1 - s2 + row - col;
+    float ends = t < len ? s2 : 0.0f;
+    if (t >= len) dG = 0.0f;
+    ends = group_sum<64>(ends);
+    ends += scal[kScGam * kGdrC + kGdrC - 1] * sss;
+    // suffix sums
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const float up = __shfl_down(dG, d);
+      if (t + d < 64) dG += up;
+    }
+    if (t < len) {
+      a.dg[(row0 + t) * a.Hv + hv] = dG + ends;
+      reinterpret_cast<T*>(a.dbeta)[(row0 + t) * a.Hv + hv] = (T)(rv1 + rb);
+    }
+  };
+
   for (int hv = hk * grp; hv < (hk + 1) * grp; ++hv) {
     const size_t sh = (size_t)slot * a.Hv + hv;
     f32x4 aP[2], aA[2];                     // tile tasks w and w + 8 (of ten)
@@ -700,14 +738,11 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
           x *= *reinterpret_cast<const f32x4*>(scal + kScGam * kGdrC + 16 * i + 4 * g);
           const f32x4 be = *reinterpret_cast<const f32x4*>(scal + kScBeta * kGdrC + 16 * i + 4 * g);
           vt[i] -= x;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int at = w * kGdrC + 16 * i + 4 * g + e;
-            const float s1 = row_sum(R[i][e] * vt[i][e]), s2 = row_sum(R[i][e] * x[e]);
-            if (c == 0) {
-              rRV[at] = vb ? rRV[at] + s1 : s1;
-              rRK[at] = vb ? rRK[at] + s2 : s2;
-            }
+          const float s1 = row_sum4(R[i] * vt[i], c), s2 = row_sum4(R[i] * x, c);
+          if (c < 4) {
+            const int at = w * kGdrC + 16 * i + 4 * g + c;
+            rRV[at] = vb ? rRV[at] + s1 : s1;
+            rRK[at] = vb ? rRK[at] + s2 : s2;
           }
           vt[i] *= be;
           UT::template put<kExact>(smem + L::R, 16 * w + c, i, g, R[i]);
@@ -750,6 +785,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
         if (p + 1 < NV) columns(p + 1);
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
+          __builtin_amdgcn_sched_barrier(0);   // (the tiles' operands one tile at a time: all do not fit)
           a1[i] = mma<T>(VR::nat(smem + L::O, i0 + i, p, g, c), fs, a1[i]);
           a2[i] = mma<T>(UT::template tok<kExact>(smem + L::U, i0 + i, 32 * p, g, c), fd, a2[i]);
           a3[i] = mma<T>(UT::template tok<kNear>(smem + L::R, i0 + i, 32 * p, g, c), first<kNear>(fs), a3[i]);
@@ -805,7 +841,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
           kk = mma<T>(KR::nat(smem + L::K, i, p, g, c), fb, kk);
         }
         const float Ghj = scal[kScGh * kGdrC + tj], Glj = scal[kScGl * kGdrC + tj];
-        f32x4 W, M;
+        f32x4 W, M, rows, betas;
         float col = 0.0f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -818,11 +854,13 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
           // (a token's product with itself is a row and a column term of one G: no change)
           const float pp = tj < ti ? W[e] * qk[e] : 0.0f, ab = D * dA * kk[e], sum = pp + be * ab;
           col += sum;
-          const float rs = row_sum(sum), rb = row_sum(ab);
-          if (c == 0) {
-            rRow[j * kGdrC + ti] = rs;
-            rBeta[j * kGdrC + ti] = rb;
-          }
+          rows[e] = sum;
+          betas[e] = ab;
+        }
+        const float rs = row_sum4(rows, c), rb = row_sum4(betas, c);
+        if (c < 4) {
+          rRow[j * kGdrC + 16 * i + 4 * g + c] = rs;
+          rBeta[j * kGdrC + 16 * i + 4 * g + c] = rb;
         }
         col += __shfl_xor(col, 16);
         col += __shfl_xor(col, 32);
@@ -844,13 +882,10 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
       const f32x4 x1 = a1[ii] * gam * a.scale, x2 = a2[ii] * end, x3 = a3[ii] * gam;
       const f32x4 kt = Quad<T>::f32(KR::tr(smem + L::K, 16 * i, jt, g, c));
       const f32x4 qt = Quad<T>::f32(KR::tr(smem + L::Z, 16 * i, jt, g, c));
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float s1 = row_sum(qt[e] * x1[e]), s2 = row_sum(kt[e] * x2[e]);
-        if (c == 0) {
-          rQ[jt * kGdrC + 16 * i + 4 * g + e] = s1;
-          rUK[jt * kGdrC + 16 * i + 4 * g + e] = s2;
-        }
+      const float s1 = row_sum4(qt * x1, c), s2 = row_sum4(kt * x2, c);
+      if (c < 4) {
+        rQ[jt * kGdrC + 16 * i + 4 * g + c] = s1;
+        rUK[jt * kGdrC + 16 * i + 4 * g + c] = s2;
       }
       dQ[ii] += x1;
       dK[ii] += x2 - be * x3;
@@ -869,50 +904,16 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
     }
     __syncthreads();
 
-    // ---- dbeta, dg
-    if (w == 0) {
-      const int t = lane;
-      float rv1 = 0.0f, rk1 = 0.0f, s1 = 0.0f, s2 = 0.0f, sss = 0.0f, row = 0.0f, rb = 0.0f, col = 0.0f;
-      for (int x = 0; x < VB / 16; ++x) {
-        rv1 += rRV[x * kGdrC + t];
-        rk1 += rRK[x * kGdrC + t];
-      }
-      for (int x = 0; x < 8; ++x) sss += rSS[x];
-      for (int x = 0; x < NJ; ++x) {
-        s1 += rQ[x * kGdrC + t];
-        s2 += rUK[x * kGdrC + t];
-      }
-      for (int x = 0; x < 4; ++x) {
-        if (x <= t / 16) {
-          row += rRow[x * kGdrC + t];
-          rb += rBeta[x * kGdrC + t];
-        }
-        if (x >= t / 16) col += rCol[x * kGdrC + t];
-      }
-      const float be = scal[kScBeta * kGdrC + t];
-      float dG = s1 - be * rk1 - s2 + row - col;
-      float ends = t < len ? s2 : 0.0f;
-      if (t >= len) dG = 0.0f;
-      ends = group_sum<64>(ends);
-      ends += scal[kScGam * kGdrC + kGdrC - 1] * sss;
-      // suffix sums
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) {
-        const float up = __shfl_down(dG, d);
-        if (t + d < 64) dG += up;
-      }
-      if (t < len) {
-        a.dg[(row0 + t) * a.Hv + hv] = dG + ends;
-        reinterpret_cast<T*>(a.dbeta)[(row0 + t) * a.Hv + hv] = (T)(rv1 + rb);
-      }
+    if (hv + 1 < (hk + 1) * grp) {
+      if (w == 0) finish(hv);
+      __syncthreads();
     }
-    __syncthreads();
   }
 
   // out through LDS, 16 bytes a lane (from the results' layout a store would cover 32
   // bytes of each of 4 rows)
   typedef InterT<T, DK> DT;
-  static_assert(2 * DT::bytes(1) <= L::total, "over what is no longer needed");
+  static_assert(2 * DT::bytes(1) <= L::scal, "over what is no longer needed");
 #pragma unroll
   for (int ii = 0; ii < NI; ++ii) {
     DT::template put<1>(smem, 16 * jt + c, i0 + ii, g, dQ[ii]);
@@ -927,6 +928,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
     T* out = reinterpret_cast<T*>(second ? a.dk : a.dq) + ((row0 + t) * a.Hk + hk) * DK + 32 * p + 8 * g;
     if (t < len) st_eight(out, lo, hi);
   }
+  if (w == 7) finish((hk + 1) * grp - 1);
 }
 
 // dynamic LDS above 64 KB needs the attribute once per kernel and device
