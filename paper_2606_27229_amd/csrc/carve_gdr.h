@@ -168,21 +168,6 @@ __device__ __forceinline__ f32x4 mma(const Fi<T, N>& a, const Fi<T, N>& b, f32x4
   return c;
 }
 
-// eight consecutive elements of a token row (16-byte aligned)
-template <typename T>
-__device__ __forceinline__ Fr<T> ld_fr(const T* p) {
-  Fr<T> f;
-  if constexpr (sizeof(T) == 2) {
-    const bf16x8 b = *reinterpret_cast<const bf16x8*>(p);
-    f.a = __builtin_shufflevector(b, b, 0, 1, 2, 3);
-    f.b = __builtin_shufflevector(b, b, 4, 5, 6, 7);
-  } else {
-    f.a = *reinterpret_cast<const f32x4*>(p);
-    f.b = *reinterpret_cast<const f32x4*>(p + 4);
-  }
-  return f;
-}
-
 template <typename T>
 __device__ __forceinline__ void st_eight(T* p, f32x4 lo, f32x4 hi) {
   if constexpr (sizeof(T) == 2) {

@@ -14,16 +14,32 @@ namespace {
 // blocks in one wave), the blocks below by T21 = -T22 A21 T11 with f32 matrix-core
 // products, twice.  f32 throughout: T multiplies every value of the chunk.  Bound by the
 // latency of these steps, so what counts is how many workgroups a compute unit holds:
-// A (below the diagonal) and T (transposed, above it) share 17 KB of LDS.
+// A (below the diagonal) and T (transposed, above it) share 17 KB of LDS, where the rows
+// were before.  The rows come through LDS because each wave needs most of them: loaded by
+// every wave for itself, 16 rows at a time, they took 38 of 86 us at 4096 chunks of 128.
 // G is summed in 64 bits and kept as two floats, so that a decay between two tokens
 // keeps its digits however strongly the tokens before them decay.
+template <typename T, int DK>
+struct PrepLds {
+  typedef GdrRows<T, DK> KR;
+  static constexpr int LD = kGdrC + 4;
+  static constexpr int K = 0, Q = KR::bytes, M = 0;   // M over the rows
+  static constexpr int rows = 2 * KR::bytes > kGdrC * LD * 4 ? 2 * KR::bytes : kGdrC * LD * 4;
+  static constexpr int total = rows + 3 * kGdrC * 4;
+};
+
 template <typename T, int DK, bool BWD>
 __global__ void __launch_bounds__(256, 4) carve_gdr_prep_kernel(GdrArgs a) {
   constexpr int NP = DK / 32;
-  constexpr int LD = kGdrC + 4;
+  typedef PrepLds<T, DK> L;
+  typedef typename L::KR KR;
   typedef GdrWs<T> WS;
-  __shared__ __attribute__((aligned(16))) float sM[kGdrC * LD];
-  __shared__ __attribute__((aligned(16))) float sGh[kGdrC], sGl[kGdrC], sB[kGdrC];
+  constexpr int LD = L::LD;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  float* sM = reinterpret_cast<float*>(smem + L::M);
+  float* sGh = reinterpret_cast<float*>(smem + L::rows);
+  float* sGl = sGh + kGdrC;
+  float* sB = sGl + kGdrC;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, c = lane & 15;
   const int slot = blockIdx.x, hv = blockIdx.y, hk = hv / (a.Hv / a.Hk);
@@ -31,8 +47,8 @@ __global__ void __launch_bounds__(256, 4) carve_gdr_prep_kernel(GdrArgs a) {
   int n, chunk;
   if (!gdr_find(a, slot, sq, n, chunk)) return;   // (uniform)
   const int t0 = sq.t0 + chunk * kGdrC, len = min(kGdrC, sq.len - chunk * kGdrC);
-  const T* q = reinterpret_cast<const T*>(a.q) + sq.batch * a.qs[0] + t0 * a.qs[1] + hk * a.qs[2] + 8 * g;
-  const T* k = reinterpret_cast<const T*>(a.k) + sq.batch * a.ks[0] + t0 * a.ks[1] + hk * a.ks[2] + 8 * g;
+  const T* q = reinterpret_cast<const T*>(a.q) + sq.batch * a.qs[0] + t0 * a.qs[1] + hk * a.qs[2];
+  const T* k = reinterpret_cast<const T*>(a.k) + sq.batch * a.ks[0] + t0 * a.ks[1] + hk * a.ks[2];
   const size_t row0 = ((size_t)sq.batch * a.T + t0) * a.Hv + hv;
   char* ws = a.ws + ((size_t)slot * a.Hv + hv) * a.per;
   float* scal = reinterpret_cast<float*>(ws + (BWD ? WS::bScal : WS::fScal));
@@ -41,15 +57,10 @@ __global__ void __launch_bounds__(256, 4) carve_gdr_prep_kernel(GdrArgs a) {
   // of token 16 w + c (forward), or queries 16 j + 4 g + e against key 16 w + c (backward)
   f32x4 KK[4], QK[4];
   {
-    Fr<T> fk[NP], fq[NP];
     // (rows behind the last token repeat it: beta is 0 there, and no token before them
     // sees them)
-    const int r = min(16 * w + c, len - 1);
-#pragma unroll
-    for (int p = 0; p < NP; ++p) {
-      fk[p] = ld_fr<T>(k + r * a.ks[1] + 32 * p);
-      if (!BWD) fq[p] = ld_fr<T>(q + r * a.qs[1] + 32 * p);
-    }
+    KR::template dma<4>(smem + L::K, k, (int)(a.ks[1] * sizeof(T)), len, w, lane);
+    KR::template dma<4>(smem + L::Q, q, (int)(a.qs[1] * sizeof(T)), len, w, lane);
     if (w == 0) {   // decays: prefix sums over the wave's lanes
       const size_t at = row0 + (size_t)lane * a.Hv;
       float gt = lane < len ? a.g[at] : 0.0f;
@@ -72,17 +83,24 @@ __global__ void __launch_bounds__(256, 4) carve_gdr_prep_kernel(GdrArgs a) {
       scal[kScGh * kGdrC + lane] = Gh;
       scal[kScGl * kGdrC + lane] = Gl;
     }
+    vm_wait_all();
+    __syncthreads();
+    Fr<T> fk[NP], fq[NP];
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      fk[p] = KR::nat(smem + L::K, w, p, g, c);
+      if (!BWD) fq[p] = KR::nat(smem + L::Q, w, p, g, c);
+    }
     // (all four tiles for every wave, masked below: branches by wave cost more than the
     // products they save)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       KK[j] = QK[j] = zero4();
-      const int ra = min(16 * j + c, len - 1);
 #pragma unroll
       for (int p = 0; p < NP; ++p) {
-        const Fr<T> fa = ld_fr<T>(k + ra * a.ks[1] + 32 * p);
+        const Fr<T> fa = KR::nat(smem + L::K, j, p, g, c);
         KK[j] = mma<T>(fa, fk[p], KK[j]);
-        if constexpr (BWD) QK[j] = mma<T>(ld_fr<T>(q + ra * a.qs[1] + 32 * p), fk[p], QK[j]);
+        if constexpr (BWD) QK[j] = mma<T>(KR::nat(smem + L::Q, j, p, g, c), fk[p], QK[j]);
         else QK[j] = mma<T>(fa, fq[p], QK[j]);
       }
     }
@@ -623,12 +641,18 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_pair_kernel(GdrArgs a) {
   if (nch > 0) store_o(nch - 1);
 }
 
+template <typename T, int DK, bool BWD>
+int launch_prep_b(const GdrArgs& a, hipStream_t s) {
+  constexpr int lds = PrepLds<T, DK>::total;
+  const auto kern = carve_gdr_prep_kernel<T, DK, BWD>;
+  if (hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
+    return CARVE_ERR_HIP;
+  hipLaunchKernelGGL(kern, dim3(a.nslots, a.Hv), dim3(256), lds, s, a);
+  return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
+}
 template <typename T, int DK>
 int launch_prep_t(const GdrArgs& a, bool bwd, hipStream_t s) {
-  const dim3 grid(a.nslots, a.Hv);
-  if (bwd) hipLaunchKernelGGL((carve_gdr_prep_kernel<T, DK, true>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((carve_gdr_prep_kernel<T, DK, false>), grid, dim3(256), 0, s, a);
-  return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
+  return bwd ? launch_prep_b<T, DK, true>(a, s) : launch_prep_b<T, DK, false>(a, s);
 }
 template <typename T, int DK, int NW>
 int launch_chain_t(const GdrArgs& a, hipStream_t s) {
