@@ -291,7 +291,7 @@ int carve_rmsnorm_bwd_noalloc(const carve_dims_t* d, const void* o, const float*
  *     they may be slices of a fused projection.  beta [B, T, Hv] (token dtype),
  *     g [B, T, Hv] (f32), o and dO [B, T, Hv, Dv] and every gradient are dense.
  *     The strides may not be negative; a stride of 0 is a broadcast input, whose
- *     gradient is still written per element.
+ *     gradient is still written per element.  A token's stride is less than 16 MB.
  *   - Packed sequences: with N > 0, B must be 1 and the T rows hold N sequences,
  *     sequence n being rows [offsets[n], offsets[n + 1]); offsets is a device
  *     array of N + 1 ints, non-decreasing from >= 0 to <= T.  Sequences may be
@@ -306,10 +306,12 @@ int carve_rmsnorm_bwd_noalloc(const carve_dims_t* d, const void* o, const float*
  *   - Supported: Dk in {32, 64, 128}; Dv in {32, 64, 128, 256}; Hv a multiple of
  *     Hk, at most 65535; dtype f32 or bf16.  scale is finite.  q, k, v and their
  *     strides are 16-byte aligned, like every other pointer.
- *   - Inputs are finite with g <= 0; g = -inf is a reset (decay 0).  With bf16
- *     tokens the chunk form carries f32 intermediates through the matrix cores as
- *     sums of two bf16 values (errors of states and of dg of some 1e-6 of their
- *     size); with f32 tokens all products are f32.
+ *   - Inputs are finite with g <= 0; g = -inf is a reset (decay 0).  NaN and
+ *     infinities propagate within their sequence, also to tokens before them in
+ *     the same chunk.  With bf16 tokens the chunk form carries f32 intermediates
+ *     through the matrix cores as sums of bf16 values, three towards f32 outputs
+ *     (states, dg: f32 accuracy) and two towards bf16 outputs; with f32 tokens
+ *     all products are f32.
  */
 typedef struct {
   int B, T;            /* dense: B sequences of T tokens; packed: B = 1, T rows */

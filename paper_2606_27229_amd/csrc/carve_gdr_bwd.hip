@@ -7,9 +7,8 @@
 //   dQ = e^G dO' S + (D dP) K
 //   dK = (D dP)^T Q + M K + M^T K + E U dS - beta e^G dR S
 //   dbeta_t = dR_t.V_t - e^{G_t} k_t.(dR S)_t + sum_j dA_tj D_tj k_t.k_j
-//   dG_t = q_t.(e^G dO' S)_t - k_t.(beta e^G dR S)_t - k_t.(E U dS)_t
-//          + row sums - column sums of dP P + dA A
-//   dG_C += e^{G_C} <dS, S> + sum_t k_t.(E U dS)_t,  dg_t = sum_{i >= t} dG_i
+//   dG_t = q_t.(e^G dO' S)_t - k_t.(beta e^G dR S)_t + row sums - column sums of dP P + dA A
+//   dg_t = sum_{i >= t} dG_i + sum_{j < t} k_j.(E U dS)_j + e^{G_C} <dS, S>
 // Three launches: the triangles (carve_gdr_prep_kernel), the chain of state
 // gradients, then every chunk's gradients at once.
 #include "carve_gdr.h"
@@ -666,19 +665,21 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
       if (x >= t / 16) col += rCol[x * kGdrC + t];
     }
     const float be = scal[kScBeta * kGdrC + t];
-    float dG = s1 - be * rk1 - s2 + row - col;
-    float ends = t < len ? s2 : 0.0f;
-    if (t >= len) dG = 0.0f;
-    ends = group_sum<64>(ends);
-    ends += scal[kScGam * kGdrC + kGdrC - 1] * sss;
-    // suffix sums
+    // dg_t: over i >= t what reaches G_i, and over j < t the writes that a decay at t
+    // takes from the end state (with - k.(E U dS) as a term of G_j and their sum as one of
+    // G_C the undecayed writes behind t would cancel: nothing would be left of a small dg)
+    float after = t < len ? s1 - be * rk1 + row - col : 0.0f;
+    float before = __shfl_up(s2, 1);
+    if (t == 0) before = 0.0f;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
-      const float up = __shfl_down(dG, d);
-      if (t + d < 64) dG += up;
+      const float x = __shfl_down(after, d), y = __shfl_up(before, d);
+      if (t + d < 64) after += x;
+      if (t >= d) before += y;
     }
+    const float ends = scal[kScGam * kGdrC + kGdrC - 1] * sss;
     if (t < len) {
-      a.dg[(row0 + t) * a.Hv + hv] = dG + ends;
+      a.dg[(row0 + t) * a.Hv + hv] = after + before + ends;
       reinterpret_cast<T*>(a.dbeta)[(row0 + t) * a.Hv + hv] = (T)(rv1 + rb);
     }
   };
