@@ -313,19 +313,35 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_bpair_kernel(GdrArgs a) {
         for (int p = 0; p < NP / 2; ++p) acc[y] = mma<T>(KR::nat(buf + L::K0, i, NP / 2 * h + p, g, c), Sf[p], acc[y]);
         if (y < 2) x[64 * (L::xP + 2 * h + y)] = acc[y];
       }
+      // (what a step needs besides the other wave's part is read before the two meet)
+      f32x4 end[2];
+      Fi<T, kExact> Tf[4];
+#pragma unroll
+      for (int y = 0; y < 2; ++y) end[y] = *reinterpret_cast<const f32x4*>(scal + kScEnd * kGdrC + 16 * (2 * h + y) + 4 * g);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i < 2 || h) Tf[i] = ld_img<T, kExact>(buf + L::I + kGdrScal, img_upper(i, h), lane);   // (uniform)
       pair_meet(flags, h, 2 * (nch - 1 - ch) + 1);   // (3)
 #pragma unroll
-      for (int y = 0; y < 2; ++y)
-        U[y] += (acc[2 + y] + x[64 * (L::xP + 2 * (1 - h) + y)]) *
-                *reinterpret_cast<const f32x4*>(scal + kScEnd * kGdrC + 16 * (2 * h + y) + 4 * g);
+      for (int y = 0; y < 2; ++y) U[y] += (acc[2 + y] + x[64 * (L::xP + 2 * (1 - h) + y)]) * end[y];
       const Fi<T, kExact> Uf = to_fi<T, kExact>(U[0], U[1]);
       f32x4 R[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (i >= 2 && !h) continue;   // (uniform)
-        R[i] = mma<T>(ld_img<T, kExact>(buf + L::I + kGdrScal, img_upper(i, h), lane), Uf, zero4());
+        R[i] = mma<T>(Tf[i], Uf, zero4());
         x[64 * (h ? L::xU + i : L::xV + i)] = R[i];
       }
+      f32x4 gb[4];
+      Fr<T> Kt[NP][2];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        gb[i] = *reinterpret_cast<const f32x4*>(scal + kScGam * kGdrC + 16 * i + 4 * g) *
+                *reinterpret_cast<const f32x4*>(scal + kScBeta * kGdrC + 16 * i + 4 * g);
+#pragma unroll
+      for (int j = 0; j < NP; ++j)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) Kt[j][s] = KR::tr32(buf + L::K0, s, NP * h + j, g, c);
       pair_meet(flags, h, 2 * (nch - 1 - ch) + 2);   // (4)
       // dR whole; tiles 2 h, 2 h + 1 of it go out
       float* keep = a.dR + (sh * (a.Dv / 16) + v0 / 16) * 1024 + 4 * lane + 512 * h;
@@ -343,14 +359,12 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_bpair_kernel(GdrArgs a) {
         *reinterpret_cast<f32x4*>(keep + 256) = R[1];
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        R[i] *= -(*reinterpret_cast<const f32x4*>(scal + kScGam * kGdrC + 16 * i + 4 * g) *
-                  *reinterpret_cast<const f32x4*>(scal + kScBeta * kGdrC + 16 * i + 4 * g));
+      for (int i = 0; i < 4; ++i) R[i] *= -gb[i];
       const Fi<T, kExact> Rf[2] = {to_fi<T, kExact>(R[0], R[1]), to_fi<T, kExact>(R[2], R[3])};
 #pragma unroll
       for (int j = 0; j < NP; ++j)
 #pragma unroll
-        for (int s = 0; s < 2; ++s) S[j] = mma<T>(KR::tr32(buf + L::K0, s, NP * h + j, g, c), Rf[s], S[j]);
+        for (int s = 0; s < 2; ++s) S[j] = mma<T>(Kt[j][s], Rf[s], S[j]);
     }
     if (a.dS0) {
       float* s = a.dS0 + (size_t)head * sm + soff;

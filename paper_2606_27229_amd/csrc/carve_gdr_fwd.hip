@@ -482,22 +482,38 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_pair_kernel(GdrArgs a) {
       const float gend = scal[kScGam * kGdrC + kGdrC - 1];
 #pragma unroll
       for (int j = 0; j < NP; ++j) S[j] *= gend;
-      pair_meet(flags, h, 2 * ch + 1);   // (3)
-      f32x4 R[2], U[4];
+      // (what a step needs besides the other wave's part is read before the two meet)
+      f32x4 gam[2], be[2], vt[2];
+      Fi<T, kExact> Tf[4];
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
         const int i = 2 * h + y;
-        const f32x4 gam = *reinterpret_cast<const f32x4*>(scal + kScGam * kGdrC + 16 * i + 4 * g);
-        const f32x4 be = *reinterpret_cast<const f32x4*>(scal + kScBeta * kGdrC + 16 * i + 4 * g);
-        R[y] = be * (Quad<T>::f32(VR::tr(buf + L::V, 16 * i, w, g, c)) - gam * (acc[2 + y] + x[64 * (L::xP + 2 * (1 - h) + y)]));
+        gam[y] = *reinterpret_cast<const f32x4*>(scal + kScGam * kGdrC + 16 * i + 4 * g);
+        be[y] = *reinterpret_cast<const f32x4*>(scal + kScBeta * kGdrC + 16 * i + 4 * g);
+        vt[y] = Quad<T>::f32(VR::tr(buf + L::V, 16 * i, w, g, c));
       }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i >= 2 || !h) Tf[i] = ld_img<T, kExact>(buf + L::I + WS::fT, img_lower(i, h), lane);   // (uniform)
+      pair_meet(flags, h, 2 * ch + 1);   // (3)
+      f32x4 R[2], U[4];
+#pragma unroll
+      for (int y = 0; y < 2; ++y) R[y] = be[y] * (vt[y] - gam[y] * (acc[2 + y] + x[64 * (L::xP + 2 * (1 - h) + y)]));
       const Fi<T, kExact> Rf = to_fi<T, kExact>(R[0], R[1]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (i < 2 && h) continue;   // (uniform)
-        U[i] = mma<T>(ld_img<T, kExact>(buf + L::I + WS::fT, img_lower(i, h), lane), Rf, zero4());
+        U[i] = mma<T>(Tf[i], Rf, zero4());
         x[64 * (h ? L::xV + i - 2 : L::xU + i)] = U[i];
       }
+      f32x4 end[4];
+      Fr<T> Kt[NP][2];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) end[i] = *reinterpret_cast<const f32x4*>(scal + kScEnd * kGdrC + 16 * i + 4 * g);
+#pragma unroll
+      for (int j = 0; j < NP; ++j)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) Kt[j][s] = KR::tr32(buf + L::K, s, NP * h + j, g, c);
       pair_meet(flags, h, 2 * ch + 2);   // (4)
       if (h == 0) {
         U[2] += x[64 * L::xV];
@@ -511,12 +527,12 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_pair_kernel(GdrArgs a) {
         x[64 * (L::xW + 1)] = U[3];
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) U[i] *= *reinterpret_cast<const f32x4*>(scal + kScEnd * kGdrC + 16 * i + 4 * g);
+      for (int i = 0; i < 4; ++i) U[i] *= end[i];
       const Fi<T, kExact> Ue[2] = {to_fi<T, kExact>(U[0], U[1]), to_fi<T, kExact>(U[2], U[3])};
 #pragma unroll
       for (int j = 0; j < NP; ++j) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) S[j] = mma<T>(KR::tr32(buf + L::K, s, NP * h + j, g, c), Ue[s], S[j]);
+        for (int s = 0; s < 2; ++s) S[j] = mma<T>(Kt[j][s], Ue[s], S[j]);
         x[64 * (L::xS + NP * h + j)] = S[j];
       }
     }
