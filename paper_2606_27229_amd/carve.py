@@ -488,17 +488,40 @@ def _same_device(device, **tensors):
             raise ValueError(f"{name} is on {t.device}, expected {device}")
 
 
+# the current stream's handle of a device (building a Stream object for it takes 2.5 us
+# of a 10 us call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _on_stream(call, device, stream):
     """call(stream handle) with the tensors' device current and, with ``stream``
     given, that stream current too, so that what the call allocates belongs to it."""
     if stream is None and device.index == torch.cuda.current_device():
-        return call(torch.cuda.current_stream().cuda_stream)
+        return call(_raw_stream(device.index))
     if stream is None:
         stream = torch.cuda.current_stream(device)
     if stream.device != device:
         raise ValueError(f"stream is on {stream.device}, the tensors are on {device}")
     with torch.cuda.stream(stream):
         return call(stream.cuda_stream)
+
+
+def _signature(*tensors):
+    """What the checks of a call look at: None, or the layout of each tensor."""
+    return tuple([None if t is None else (t.shape, t.stride(), t.dtype, t.device) for t in tensors])
+
+
+# layouts that passed a call's checks, and what follows from them alone (the C dims,
+# sizes): a call with the same layouts checks nothing else
+_checked = {}
+
+
+def _remember(key, value):
+    if len(_checked) >= 512:
+        _checked.clear()
+    _checked[key] = value
+    return value
 
 
 def _out(res, name, shape, dtype, device):
@@ -515,12 +538,12 @@ def _scratch(workspace, nbytes, device):
 
 @functools.lru_cache(maxsize=256)
 def _gdr_dims(B, T, N, Hk, Hv, Dk, Dv, dtype, scale, *strides):
-    """The C dims of a call (by sizes and strides alone), its chunk count and the
-    workspace sizes of its forward and backward."""
+    """A reference to the C dims of a call (by sizes and strides alone), its chunk count
+    and the workspace sizes of its forward and backward."""
     lib = load_library()
     d = GdrDims(B, T, N, Hk, Hv, Dk, Dv, CARVE_BF16 if dtype == torch.bfloat16 else CARVE_F32, scale, *strides)
     r = ctypes.byref(d)
-    return d, int(lib.carve_gdr_chunk_count(r)), int(lib.carve_gdr_workspace_size(r, 0)), int(lib.carve_gdr_workspace_size(r, 1))
+    return r, int(lib.carve_gdr_chunk_count(r)), int(lib.carve_gdr_workspace_size(r, 0)), int(lib.carve_gdr_workspace_size(r, 1))
 
 
 def _strides(t):
@@ -529,8 +552,15 @@ def _strides(t):
 
 
 def _gdr_call(q, k, v, g, beta, scale, offsets):
-    """Checks what every entry point takes; returns (dims, chunks, workspace sizes,
+    """Checks what every entry point takes; returns ((dims, chunks, workspace sizes),
     sequences, the pointers of q, k, v, g, beta)."""
+    try:
+        key = ("gdr", scale, _signature(q, k, v, g, beta, offsets))
+        hit = _checked.get(key)
+    except AttributeError:   # (something else than tensors: named below)
+        hit = None
+    if hit is not None:
+        return *hit, (q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr())
     for name, t, dims in (("q", q, 4), ("k", k, 4), ("v", v, 4), ("g", g, 3), ("beta", beta, 3)):
         if not isinstance(t, torch.Tensor) or not t.is_cuda:
             raise TypeError(f"{name} must be a GPU tensor")
@@ -561,7 +591,7 @@ def _gdr_call(q, k, v, g, beta, scale, offsets):
                      *_strides(k), *_strides(v))
     ptrs = (q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(g, "g", torch.float32, (B, T, Hv)),
             _ptr(beta, "beta", dt, (B, T, Hv)))
-    return dims, seqs, ptrs
+    return *_remember(key, (dims, seqs)), ptrs
 
 
 def gdr_chunk_fwd(q, k, v, g, beta, S0=None, *, scale=None, offsets=None, want_chunks=True, want_state=True, out=None,
@@ -592,7 +622,7 @@ def gdr_chunk_fwd(q, k, v, g, beta, S0=None, *, scale=None, offsets=None, want_c
         S_c = _out(res, "S_chunks", (chunks, Hv, Dv, Dk), f32, dev) if want_chunks or res.get("S_chunks") is not None else None
         ws, ws_ptr, ws_len = _scratch(workspace, ws_bytes, dev)
         return lib.carve_gdr_chunk_fwd(
-            ctypes.byref(dims), *ptrs, _ptr(S0, "S0", f32, (seqs, Hv, Dv, Dk)), _ptr(offsets, "offsets", torch.int32),
+            dims, *ptrs, _ptr(S0, "S0", f32, (seqs, Hv, Dv, Dk)), _ptr(offsets, "offsets", torch.int32),
             o, S_T, S_c, ws_ptr, ws_len, s)
 
     _check("carve_gdr_chunk_fwd", _on_stream(call, dev, stream))
@@ -619,7 +649,7 @@ def gdr_chunk_bwd(q, k, v, g, beta, S_chunks, dO, dS_T=None, *, scale=None, offs
         dS0 = _out(res, "dS0", (seqs, Hv, Dv, Dk), f32, dev) if want_dS0 or res.get("dS0") is not None else None
         ws, ws_ptr, ws_len = _scratch(workspace, ws_bytes, dev)
         return lib.carve_gdr_chunk_bwd(
-            ctypes.byref(dims), *ptrs, _ptr(S_chunks, "S_chunks", f32, (chunks, Hv, Dv, Dk)),
+            dims, *ptrs, _ptr(S_chunks, "S_chunks", f32, (chunks, Hv, Dv, Dk)),
             _ptr(offsets, "offsets", torch.int32), _ptr(dO, "dO", dt, (B, T, Hv, Dv)),
             _ptr(dS_T, "dS_T", f32, (seqs, Hv, Dv, Dk)), *outs, dS0, ws_ptr, ws_len, s)
 
@@ -635,21 +665,25 @@ def gdr_step(q, k, v, g, beta, state, slots=None, *, scale=None, out=None, strea
     pool (-1) marks a padding entry, whose output rows are left as they were.  No
     slot may appear twice.  The other arguments are those of ``gdr_chunk_fwd``.
     Returns o [B,T,Hv,Dv] (``out`` if given)."""
-    lib = load_library()
     (dims, *_), _, ptrs = _gdr_call(q, k, v, g, beta, scale, None)
-    B, T, Hv, Dv = v.shape
-    dt, dev = q.dtype, q.device
+    dev = q.device
     if not isinstance(state, torch.Tensor) or state.dim() != 4:
         raise ValueError("state must be [pool, Hv, Dv, Dk]")
-    pool = state.shape[0]
-    _same_device(dev, state=state, slots=slots, out=out)
-    res = {"o": out}
+    key = ("step", q.shape, v.shape, q.dtype, dev, _signature(state, slots, out))
+    if key not in _checked:
+        _same_device(dev, state=state, slots=slots, out=out)
+        _ptr(slots, "slots", torch.int32, (v.shape[0],))
+        _ptr(state, "state", torch.float32, (state.shape[0], v.shape[2], v.shape[3], q.shape[3]))
+        _ptr(out, "out", q.dtype, v.shape)
+        _remember(key, True)
 
     def call(s):
-        o = _out(res, "o", (B, T, Hv, Dv), dt, dev)
-        return lib.carve_gdr_step(ctypes.byref(dims), *ptrs, _ptr(slots, "slots", torch.int32, (B,)), pool,
-                                  _ptr(state, "state", torch.float32, (pool, Hv, Dv, q.shape[3])), o, s)
+        o = torch.empty(v.shape, dtype=q.dtype, device=dev) if out is None else out
+        res["o"] = o
+        return _lib.carve_gdr_step(dims, *ptrs, None if slots is None else slots.data_ptr(), state.shape[0],
+                                   state.data_ptr(), o.data_ptr(), s)
 
+    res = {}
     _check("carve_gdr_step", _on_stream(call, dev, stream))
     return res["o"]
 
@@ -660,7 +694,8 @@ GATE_ACTS = {"silu": 1, "sigmoid": 2}
 @functools.lru_cache(maxsize=256)
 def _block_norm_dims(rows, N, groups, dtype, act, eps, alpha, *strides):
     d = BlockNormDims(rows, N, groups, CARVE_BF16 if dtype == torch.bfloat16 else CARVE_F32, act, eps, alpha, *strides)
-    return d, int(load_library().carve_block_norm_workspace_size(ctypes.byref(d)))
+    r = ctypes.byref(d)
+    return r, int(load_library().carve_block_norm_workspace_size(r))
 
 
 def _rows(t, name, like=None):
@@ -685,6 +720,13 @@ def _rows(t, name, like=None):
 
 
 def _block_norm_call(y, weight, groups, gate, gate_act, residual, alpha, scale, next_weight, eps):
+    try:
+        key = ("norm", groups, gate_act, alpha, eps, _signature(y, weight, gate, residual, scale, next_weight))
+        hit = _checked.get(key)
+    except AttributeError:   # (something else than tensors: named below)
+        hit = None
+    if hit is not None:
+        return *hit, tuple([None if t is None else t.data_ptr() for t in (y, weight, gate, residual, scale, next_weight)])
     yr, ys = _rows(y, "y")
     if y.dtype not in (torch.bfloat16, torch.float32):
         raise TypeError(f"y must be bfloat16 or float32, got {y.dtype}")
@@ -701,7 +743,7 @@ def _block_norm_call(y, weight, groups, gate, gate_act, residual, alpha, scale, 
             _ptr(next_weight, "next_weight", torch.float32, (N,)))
     if weight is None:
         raise TypeError("weight must be a GPU tensor")
-    return dims, ws_bytes, ptrs
+    return *_remember(key, (dims, ws_bytes)), ptrs
 
 
 def block_norm_fwd(y, weight, *, groups=1, gate=None, gate_act="silu", residual=None, alpha=1.0, scale=None,
@@ -716,18 +758,25 @@ def block_norm_fwd(y, weight, *, groups=1, gate=None, gate_act="silu", residual=
     gate, residual (shape and dtype of y), scale, next_weight (f32 [N]) may be left
     out.  y, gate and residual may be slices of wider rows.  Returns (x, h), h None
     without next_weight.  ``out`` may hold preallocated {"x", "h"}."""
-    lib = load_library()
     dims, _, ptrs = _block_norm_call(y, weight, groups, gate, gate_act, residual, alpha, scale, next_weight, eps)
-    res = dict(out or {})
+    res = {"x": None, "h": None, **(out or {})}
     _same_device(y.device, **res)
 
     def call(s):
-        x = _out(res, "x", tuple(y.shape), y.dtype, y.device)
-        h = _out(res, "h", tuple(y.shape), y.dtype, y.device) if next_weight is not None else _ptr(res.get("h"), "h")
-        return lib.carve_block_norm_fwd(ctypes.byref(dims), *ptrs, x, h, s)
+        if out is None:
+            res["x"] = x = torch.empty(y.shape, dtype=y.dtype, device=y.device)
+            x = x.data_ptr()
+            h = None
+            if next_weight is not None:
+                res["h"] = torch.empty(y.shape, dtype=y.dtype, device=y.device)
+                h = res["h"].data_ptr()
+        else:
+            x = _out(res, "x", tuple(y.shape), y.dtype, y.device)
+            h = _out(res, "h", tuple(y.shape), y.dtype, y.device) if next_weight is not None else _ptr(res["h"], "h")
+        return _lib.carve_block_norm_fwd(dims, *ptrs, x, h, s)
 
     _check("carve_block_norm_fwd", _on_stream(call, y.device, stream))
-    return res["x"], res.get("h")
+    return res["x"], res["h"]
 
 
 def block_norm_bwd(y, weight, dx, dh=None, *, groups=1, gate=None, gate_act="silu", residual=None, alpha=1.0, scale=None,
@@ -746,7 +795,7 @@ def block_norm_bwd(y, weight, dx, dh=None, *, groups=1, gate=None, gate_act="sil
     def call(s):
         outs = [_out(res, name, sh, t, dev) if of is not None else _ptr(res.get(name), name) for name, of, sh, t in wanted]
         ws, ws_ptr, ws_len = _scratch(workspace, ws_bytes, dev)
-        return lib.carve_block_norm_bwd(ctypes.byref(dims), *ptrs, _ptr(dx, "dx", y.dtype, shape),
+        return lib.carve_block_norm_bwd(dims, *ptrs, _ptr(dx, "dx", y.dtype, shape),
                                         _ptr(dh, "dh", y.dtype, shape), *outs, ws_ptr, ws_len, s)
 
     _check("carve_block_norm_bwd", _on_stream(call, dev, stream))
