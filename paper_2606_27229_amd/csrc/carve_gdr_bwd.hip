@@ -772,11 +772,6 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
           UT::template put<kExact>(smem + L::U, 16 * w + c, i, g, x);
         }
       }
-      __syncthreads();
-      // ---- 2. products over these columns (queries on their way)
-      renew(g, c);
-      if (NB == 1) clear();
-      if (b + 1 == NB) KR::template dma<8>(smem + L::Z, q, (int)(a.qs[1] * sizeof(T)), len, w, lane);
       f32x4 sn[2], dn[2];   // S, dS of the next 32 value columns
       const auto columns = [&](int p) {
 #pragma unroll
@@ -789,6 +784,10 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
           }
       };
       columns(0);
+      __syncthreads();
+      // ---- 2. products over these columns (queries on their way)
+      if (NB == 1) clear();
+      if (b + 1 == NB) KR::template dma<8>(smem + L::Z, q, (int)(a.qs[1] * sizeof(T)), len, w, lane);
 #pragma unroll 1
       for (int p = 0; p < NV; ++p) {
         const Fi<T, kExact> fs = to_fi<T, kExact>(sn[0], sn[1]), fd = to_fi<T, kExact>(dn[0], dn[1]);
