@@ -304,7 +304,9 @@ int carve_rmsnorm_bwd_noalloc(const carve_dims_t* d, const void* o, const float*
  *     f32, the state at the start of every chunk, written by carve_gdr_chunk_fwd for
  *     carve_gdr_chunk_bwd (slots of no chunk are left as they were).
  *   - Supported: Dk in {32, 64, 128}; Dv in {32, 64, 128, 256}; Hv a multiple of
- *     Hk, at most 65535; dtype f32 or bf16.  scale is finite.  q, k, v and their
+ *     Hk, at most 65535; dtype f32 or bf16.  In the chunk form sequences * Hv *
+ *     Dv / 32 (sequences * Hv rounded up to eights) and the chunk count are less
+ *     than 2^23 each.  scale is finite.  q, k, v and their
  *     strides are 16-byte aligned, like every other pointer.
  *   - Inputs are finite with g <= 0; g = -inf is a reset (decay 0).  NaN and
  *     infinities propagate within their sequence, also to tokens before them in

@@ -609,7 +609,7 @@ int check_gdr(const carve_gdr_dims_t* d) {
   // (a chunk's rows are addressed with 32 bits)
   for (const long long s : {d->q_token, d->k_token, d->v_token, (long long)d->Hv * d->Dv})
     if (s >= (1LL << 24) / (long long)esize(d->dtype)) return CARVE_ERR_UNSUPPORTED;
-  // grids and row counts: B T rows, chunk slots and (sequence, head, slice) workgroups below 2^31
+  // (row and slot numbers are ints)
   if ((long long)d->B * d->T >= (1LL << 31)) return CARVE_ERR_UNSUPPORTED;
   if ((long long)d->B * ((d->T + kGdrC - 1) / kGdrC) + d->N >= (1LL << 31)) return CARVE_ERR_UNSUPPORTED;
   const long long seqs = d->N ? d->N : d->B;
@@ -619,6 +619,15 @@ int check_gdr(const carve_gdr_dims_t* d) {
 
 size_t gdr_chunks(const carve_gdr_dims_t* d) {
   return d->N ? (size_t)(d->T / kGdrC) + d->N : (size_t)d->B * ((d->T + kGdrC - 1) / kGdrC);
+}
+// the chunk form's: a launch has less than 2^32 threads, 512 a chunk slot and 512 a
+// (sequence, head, 32 value columns)
+int check_gdr_chunk(const carve_gdr_dims_t* d) {
+  const int st = check_gdr(d);
+  if (st) return st;
+  const long long heads = (d->N ? d->N : (long long)d->B) * d->Hv;
+  if ((heads + 7) / 8 * 8 * (d->Dv / 32) >= (1LL << 23) || gdr_chunks(d) >= (1u << 23)) return CARVE_ERR_UNSUPPORTED;
+  return CARVE_OK;
 }
 // workspace bytes of one (chunk slot, value head)
 size_t gdr_per(const carve_gdr_dims_t* d, bool bwd) {
@@ -658,10 +667,10 @@ int gdr_inputs(const carve_gdr_dims_t* d, const void* q, const void* k, const vo
 
 extern "C" {
 
-size_t carve_gdr_chunk_count(const carve_gdr_dims_t* d) { return check_gdr(d) == CARVE_OK ? gdr_chunks(d) : 0; }
+size_t carve_gdr_chunk_count(const carve_gdr_dims_t* d) { return check_gdr_chunk(d) == CARVE_OK ? gdr_chunks(d) : 0; }
 
 size_t carve_gdr_workspace_size(const carve_gdr_dims_t* d, int for_backward) {
-  if (check_gdr(d) != CARVE_OK) return 0;
+  if (check_gdr_chunk(d) != CARVE_OK) return 0;
   const size_t n = gdr_chunks(d);
   const size_t images = align256(n * d->Hv * gdr_per(d, for_backward != 0));
   return for_backward ? images + n * gdr_state(d) + n * d->Hv * d->Dv * kGdrC * 4 : images;
@@ -671,7 +680,7 @@ int carve_gdr_chunk_fwd(const carve_gdr_dims_t* d, const void* q, const void* k,
                   const void* beta, const float* S0, const int* offsets, void* o, float* S_T, float* S_chunks,
                   void* workspace, size_t workspace_bytes, hipStream_t stream) {
   ProfClear pc;
-  int st = check_gdr(d);
+  int st = check_gdr_chunk(d);
   if (st) return st;
   if (!q || !k || !v || !g || !beta || !o || (d->N > 0 && !offsets)) return CARVE_ERR_NULL;
   if (d->N == 0 && offsets) return CARVE_ERR_ARG;
@@ -702,7 +711,7 @@ int carve_gdr_chunk_bwd(const carve_gdr_dims_t* d, const void* q, const void* k,
                   void* dq, void* dk, void* dv, float* dg, void* dbeta, float* dS0, void* workspace,
                   size_t workspace_bytes, hipStream_t stream) {
   ProfClear pc;
-  int st = check_gdr(d);
+  int st = check_gdr_chunk(d);
   if (st) return st;
   if (!q || !k || !v || !g || !beta || !S_chunks || !dO || !dq || !dk || !dv || !dg || !dbeta ||
       (d->N > 0 && !offsets))

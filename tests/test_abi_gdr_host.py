@@ -57,6 +57,20 @@ def test_gdr_dims(kw, status):
     assert lib.carve_gdr_step(ctypes.byref(d), *ptrs[:6], 8, *ptrs[6:8], None) == status
 
 
+@pytest.mark.parametrize("kw", [dict(B=1 << 15, T=1, Hk=64, Hv=64, Dv=128), dict(B=1, N=1 << 20, T=64, Hk=2, Hv=4, Dv=64),
+                                dict(B=1 << 15, T=64 * 256, Hk=1, Hv=1, Dv=32), dict(B=1, N=1 << 23, T=1, Hk=1, Hv=1, Dv=32)])
+def test_chunk_calls_beyond_a_launch(kw):
+    """2^32 threads or more of a kernel are refused, not left to the launch; the step, which
+    spreads them over three dimensions, has no such bound."""
+    lib = carve.load_library()
+    d = gdims(**kw)
+    assert fwd(d, ws=1 << 62) == UNSUPPORTED
+    assert lib.carve_gdr_chunk_bwd(ctypes.byref(d), *far(16), 1 << 62, None) == UNSUPPORTED
+    assert lib.carve_gdr_chunk_count(ctypes.byref(d)) == 0 and lib.carve_gdr_workspace_size(ctypes.byref(d), 0) == 0
+    if not d.N:   # (past the sizes' checks: the missing tensors are what is refused)
+        assert lib.carve_gdr_step(ctypes.byref(d), *[None] * 6, 1 << 16, None, None, None) == NULL
+
+
 def test_gdr_sizes():
     lib = carve.load_library()
     count = lambda **kw: lib.carve_gdr_chunk_count(ctypes.byref(gdims(**kw)))
