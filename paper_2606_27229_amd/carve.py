@@ -554,6 +554,8 @@ def _strides(t):
 def _gdr_call(q, k, v, g, beta, scale, offsets):
     """Checks what every entry point takes; returns ((dims, chunks, workspace sizes),
     sequences, the pointers of q, k, v, g, beta)."""
+    if scale is not None:
+        scale = float(scale)
     try:
         key = ("gdr", scale, _signature(q, k, v, g, beta, offsets))
         hit = _checked.get(key)
@@ -587,7 +589,7 @@ def _gdr_call(q, k, v, g, beta, scale, offsets):
         seqs = offsets.numel() - 1
     if scale is None:
         scale = Dk ** -0.5
-    dims = _gdr_dims(B, T, seqs if offsets is not None else 0, Hk, Hv, Dk, Dv, dt, float(scale), *_strides(q),
+    dims = _gdr_dims(B, T, seqs if offsets is not None else 0, Hk, Hv, Dk, Dv, dt, scale, *_strides(q),
                      *_strides(k), *_strides(v))
     ptrs = (q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(g, "g", torch.float32, (B, T, Hv)),
             _ptr(beta, "beta", dt, (B, T, Hv)))
@@ -720,6 +722,7 @@ def _rows(t, name, like=None):
 
 
 def _block_norm_call(y, weight, groups, gate, gate_act, residual, alpha, scale, next_weight, eps):
+    groups, alpha, eps = int(groups), float(alpha), float(eps)
     try:
         key = ("norm", groups, gate_act, alpha, eps, _signature(y, weight, gate, residual, scale, next_weight))
         hit = _checked.get(key)
@@ -736,8 +739,8 @@ def _block_norm_call(y, weight, groups, gate, gate_act, residual, alpha, scale, 
     rr, rs = (None, 0) if residual is None else _rows(residual, "residual", y)
     _same_device(y.device, weight=weight, scale=scale, next_weight=next_weight)
     rows, N = yr.shape
-    dims, ws_bytes = _block_norm_dims(rows, N, int(groups), y.dtype, GATE_ACTS[gate_act] if gate is not None else 0,
-                                      float(eps), float(alpha), ys, zs, rs)
+    dims, ws_bytes = _block_norm_dims(rows, N, groups, y.dtype, GATE_ACTS[gate_act] if gate is not None else 0,
+                                      eps, alpha, ys, zs, rs)
     ptrs = (yr.data_ptr(), _ptr(weight, "weight", torch.float32, (N,)), None if gate is None else zr.data_ptr(),
             None if residual is None else rr.data_ptr(), _ptr(scale, "scale", torch.float32, (N,)),
             _ptr(next_weight, "next_weight", torch.float32, (N,)))

@@ -276,6 +276,15 @@ def test_step(B, T, Hk, Hv, Dk, Dv, dtype, pool):
     assert torch.equal(o2, o[:B]) and torch.equal(st2, st[order.cuda()])
 
 
+def test_scale_given_as_a_tensor_is_read_at_every_call():
+    x = cuda(gdr_inputs(2, 1, 2, 2, 64, 64, F32, seed=63))
+    scale = torch.tensor(1.0)
+    for value in (1.0, 0.5):
+        scale.fill_(value)
+        got, want = (carve.gdr_step(x["q"], x["k"], x["v"], x["g"], x["beta"], x["S0"].clone(), scale=s) for s in (scale, value))
+        assert torch.equal(got, want)
+
+
 def test_step_far_slot():
     """A slot whose state lies past 2^31 elements."""
     H, D = 32, 128
