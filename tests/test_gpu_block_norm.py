@@ -53,6 +53,27 @@ def test_rows_of_every_size(rows, N, dtype):
     compare(run(cuda(x)), norm_reference(x), dtype)
 
 
+@pytest.mark.parametrize("rows,N", [((1 << 26) + 1024, 8), ((1 << 22) + 1024, 1032)])
+def test_more_rows_than_one_grid_dimension(rows, N):
+    """The rows repeat after 1024, so every part of the result equals the first."""
+    print(f"case block norm {rows}x{N}", flush=True)
+    x = cuda(norm_inputs(1024, N, BF, seed=N, gate="", residual=False, scale=False, next=False))
+    first, _ = carve.block_norm_fwd(x["y"], x["weight"], eps=x["eps"])
+    many, _ = carve.block_norm_fwd(x["y"].repeat(rows // 1024, 1), x["weight"], eps=x["eps"])
+    for part in many.view(-1, 1024, N).split(1024):
+        assert torch.equal(part, first.expand_as(part))
+
+
+def test_numbers_given_as_tensors_are_read_at_every_call():
+    x = cuda(norm_inputs(4, 64, F32, seed=5, gate="", residual=True, scale=False, next=False))
+    alpha = torch.tensor(1.0)
+    for value in (1.0, 0.5):
+        alpha.fill_(value)
+        got, _ = carve.block_norm_fwd(x["y"], x["weight"], residual=x["residual"], alpha=alpha)
+        want, _ = carve.block_norm_fwd(x["y"], x["weight"], residual=x["residual"], alpha=value)
+        assert torch.equal(got, want)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF])
 @pytest.mark.parametrize("gate", ["", "silu", "sigmoid"])
 @pytest.mark.parametrize("residual,scale,next", [(False, False, False), (True, False, False), (False, True, True), (True, True, True)])
