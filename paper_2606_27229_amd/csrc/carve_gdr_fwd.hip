@@ -16,7 +16,9 @@ namespace {
 // latency of these steps, so what counts is how many workgroups a compute unit holds:
 // A (below the diagonal) and T (transposed, above it) share 17 KB of LDS, where the rows
 // were before.  The rows come through LDS because each wave needs most of them: loaded by
-// every wave for itself, 16 rows at a time, they took 38 of 86 us at 4096 chunks of 128.
+// every wave for itself, 16 rows at a time, they made it 86 us at 4096 chunks of 128 keys
+// (bf16; 270 MB in and out), where it takes 64 us now; the backward form, which writes
+// two more images, 83 us.
 // G is summed in 64 bits and kept as two floats, so that a decay between two tokens
 // keeps its digits however strongly the tokens before them decay.
 template <typename T, int DK>
@@ -193,9 +195,9 @@ __global__ void __launch_bounds__(256, 4) carve_gdr_prep_kernel(GdrArgs a) {
 }
 
 // ---------------------------------------------------------------------------------
-// The chain of states.  A workgroup runs one sequence and value head for 16 NW value
-// columns, NW tiles of 16: value rows of S are independent, so the tiles share nothing
-// but the chunk's rows.  Two waves a tile:
+// The chain of states, keys of 32.  A workgroup runs one sequence and value head for 32
+// value columns, two tiles of 16: value rows of S are independent, so the tiles share
+// nothing but the chunk's rows.  Two waves a tile:
 //   chain   R = beta (V - e^G K S^T), U = T R, S^T <- e^{G_C} S^T + K^T (e^{G_C - G} U)
 //   helper  o = scale (e^G Q S^T + P U), one chunk behind, and all global memory: the
 //           next chunk's keys, values, T and decays straight into LDS, its own queries
@@ -207,8 +209,10 @@ __global__ void __launch_bounds__(256, 4) carve_gdr_prep_kernel(GdrArgs a) {
 // pass to the helper through LDS as they lie in registers.  Barriers, two a chunk: (1)
 // the chunk's rows are there and the chain has left S(ch), U(ch - 1); (2) the helper has
 // taken them.
-template <typename T, int DK, int NW>
+constexpr int kChainNW = 2;   // value tiles of a workgroup
+template <typename T>
 struct ChainLds {
+  static constexpr int DK = 32, NW = kChainNW;
   typedef GdrRows<T, DK> KR;
   typedef GdrRows<T, 16 * NW> VR;
   static constexpr int K = 0, V = K + KR::bytes, I = V + VR::bytes;   // I: T, scalars
@@ -217,10 +221,10 @@ struct ChainLds {
   static constexpr int total = xU + NW * 4 * 1024;
 };
 
-template <typename T, int DK, int NW>
-__global__ void __launch_bounds__(128 * NW, 1) carve_gdr_chain_kernel(GdrArgs a) {
-  constexpr int NP = DK / 32;
-  typedef ChainLds<T, DK, NW> L;
+template <typename T>
+__global__ void __launch_bounds__(128 * kChainNW, 1) carve_gdr_chain_kernel(GdrArgs a) {
+  typedef ChainLds<T> L;
+  constexpr int DK = L::DK, NP = DK / 32, NW = L::NW;
   typedef typename L::KR KR;
   typedef typename L::VR VR;
   typedef GdrWs<T> WS;
@@ -337,8 +341,8 @@ __global__ void __launch_bounds__(128 * NW, 1) carve_gdr_chain_kernel(GdrArgs a)
     for (int i = 0; i < 4; ++i)
       m.gam[i] = reinterpret_cast<const float*>(img + WS::fScal)[kScGam * kGdrC + 16 * i + c];
   };
-  // with the registers for it (one wave a SIMD, bf16), loaded a chunk ahead
-  constexpr bool AHEAD = NW == 2 && sizeof(T) == 2;
+  // loaded a chunk ahead where they take few registers (bf16)
+  constexpr bool AHEAD = sizeof(T) == 2;
   Mine cur, nxt;
   f32x4 x[4];
   if (nch > 0) {
@@ -402,17 +406,21 @@ __global__ void __launch_bounds__(128 * NW, 1) carve_gdr_chain_kernel(GdrArgs a)
 }
 
 // ---------------------------------------------------------------------------------
-// The same chain with two waves a tile on it and two helpers (keys of 64 and 128), for
-// calls of few tiles, which wait for each chunk's chain: a wave issues an instruction
-// every 7 to 8 cycles on its own, so that the number of instructions between chunk and
-// chunk is what takes the time.  Chain wave h keeps the state of the keys' half h.  K S^T
+// The same chain with two waves a tile on it and two helpers (keys of 64 and 128): a call
+// waits for each chunk's chain, and a wave issues an instruction every 7 to 8 cycles on
+// its own, so that the number of instructions between chunk and chunk is what takes the
+// time.  Chain wave h keeps the state of the keys' half h.  K S^T
 // is the sum of both halves' products; each wave finishes two token tiles of it, makes
 // their R and multiplies by T's columns of these tokens; both then add up U and update
 // their half of the state.  Helper wave h takes the outputs of two token tiles.
 // Two barriers a chunk, (1) and (2) as above; the chain waves of a tile meet twice more,
 // by flags in LDS: (3) the halves of K S^T are there; (4) the parts of U.  With barriers
 // for these too the helpers, whose memory instructions wait for each other (some 45 cycles
-// a KB), held the chain up: 214 us a call of 64 chunks of 64 heads.
+// a KB), held the chain up: 214 us for 64 sequences and heads of 64 chunks (128 keys, 128
+// values, bf16), where it takes 190 us now, 3.0 us a chunk (240 us with the states at chunk
+// starts written out: 268 MB).  One chain wave a tile with four tiles in a workgroup, which
+// fits more tiles on the card, loses also where there are many: 8 x 1024 tokens of 32 heads
+// (2048 tiles) 318 us, this 239 us.
 template <typename T, int DK>
 struct PairLds {
   static constexpr int NW = 2;   // tiles
@@ -670,11 +678,11 @@ template <typename T, int DK>
 int launch_prep_t(const GdrArgs& a, bool bwd, hipStream_t s) {
   return bwd ? launch_prep_b<T, DK, true>(a, s) : launch_prep_b<T, DK, false>(a, s);
 }
-template <typename T, int DK, int NW>
+template <typename T>
 int launch_chain_t(const GdrArgs& a, hipStream_t s) {
-  constexpr int lds = ChainLds<T, DK, NW>::total;
+  constexpr int lds = ChainLds<T>::total, NW = kChainNW;
   static_assert(lds <= 160 * 1024, "LDS");
-  const auto kern = carve_gdr_chain_kernel<T, DK, NW>;
+  const auto kern = carve_gdr_chain_kernel<T>;
   if (hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
     return CARVE_ERR_HIP;
   const unsigned heads = (unsigned)a.nseq * a.Hv;
@@ -697,9 +705,7 @@ int launch_fwd_t(const GdrArgs& a, hipStream_t s, void (*mark)(hipStream_t)) {
   int st = launch_prep_t<T, DK>(a, false, s);
   if (st) return st;
   mark(s);
-  // (two waves a tile also where many tiles share the card: 8 x 1024 tokens of 32 heads of
-  // 128, 2048 tiles: 239 us; one wave a tile, four tiles a workgroup: 318 us)
-  if constexpr (DK == 32) st = launch_chain_t<T, DK, 2>(a, s);
+  if constexpr (DK == 32) st = launch_chain_t<T>(a, s);   // (one pair of key tiles: no halves)
   else st = launch_pair_t<T, DK>(a, s);
   mark(s);
   return st;

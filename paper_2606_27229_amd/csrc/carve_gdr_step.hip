@@ -4,9 +4,11 @@
 // state's read-out is that of the old one plus the write's:
 //   S_new q = e^g (S q) + u (k.q),  S k before the write = e^g (S k).
 //
-// Bound by HBM: every state is read and written once a call, whatever T.  A row of
+// Bound by HBM: every state is read and written once a call, whatever T (64 states of
+// 32 heads of 128 x 128 and their tokens, 270 MB: 55.8 us, 4.8 TB/s; one state of 16 heads:
+// 9.8 us with the call, which is the launch and its arguments).  A row of
 // S (Dk floats) is spread over Dk / 8 lanes, two 16-byte loads each, so that a wave
-// load covers whole rows; a lane holds kRows rows, 8 loads in flight; a row's two
+// load covers whole rows; a lane holds kStepRows rows, 8 loads in flight; a row's two
 // sums run over its lanes by DPP.
 #include "carve_gdr.h"
 
