@@ -409,14 +409,16 @@ int carve_block_norm_bwd(const carve_block_norm_dims_t* d, const void* y, const 
                          float* dnext_weight, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 /* Measurement hook (not part of the computation).  Arms the next
- * carve_chunk_*, carve_rmsnorm_*, carve_gdr_* or carve_block_norm_* call made on the calling thread to record
- * events[0] on its stream before its first kernel launch and events[i] after
+ * carve_chunk_*, carve_rmsnorm_*, carve_gdr_* or carve_block_norm_* call made
+ * on the calling thread to record events[0] on its stream before its first kernel launch and events[i] after
  * its i-th launch (the forward makes 1 launch; the backward 4: clear of the
  * chunk ready flags, chunk recompute fused with the adjoint, the partials of
  * d[Ub;Uw] and dVb/dVw, their fixed-order reductions; the gated backward
  * a 5th, the reduction of dA, dtau over the batch; the backward with the
  * input activations a 5th, the activation gradient of dq, dk; the norm's
- * forward 1, its backward 2),
+ * forward 1, its backward 2; the gated delta rule's forward 2, chunk triangles
+ * and chain, its backward 3, triangles, chain and gradients, its step 1; the
+ * block norm's forward 1, its backward 2),
  * up to `capacity` events.  `events` are hipEvent_t handles created by the
  * caller (hipEventCreate) and owned by the caller; the handles are copied
  * here (the array may be freed after this call) and the events are only
