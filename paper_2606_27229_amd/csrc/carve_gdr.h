@@ -358,14 +358,30 @@ __device__ __forceinline__ void pair_meet(lds_flag* flags, int me, int turn) {
 
 // ---- workgroups of the chains ---------------------------------------------------------
 // Workgroup -> (sequence, value head) and value slice (of ns).  Blocks 8 apart share an
-// XCD; each XCD takes a run of consecutive heads, all slices of a head one after another,
-// so that the slices, and the value heads of a key head, read the same rows from one L2.
+// XCD, which takes all slices of a head one after another: they read the same rows from
+// one L2.  Packed sequences come longest first: a call takes as long as its last chain,
+// and one that is long and starts late waits for a compute unit first.  Every wave ranks
+// the sequences' chunk counts for itself, a sequence a lane; beyond 64 sequences they come
+// as they are.
 __host__ __device__ inline unsigned gdr_chain_grid(unsigned heads, int ns) { return (heads + 7) / 8 * 8 * ns; }
-__device__ __forceinline__ bool gdr_chain_block(const GdrArgs& a, int ns, int& head, int& slice) {
-  const int heads = a.nseq * a.Hv, run = (heads + 7) / 8, at = blockIdx.x / 8;
-  head = (int)(blockIdx.x % 8) * run + at / ns;
+__device__ __forceinline__ bool gdr_chain_block(const GdrArgs& a, int ns, int& n, int& hv, int& slice) {
+  const int at = blockIdx.x / 8, head = at / ns * 8 + (int)(blockIdx.x % 8);
+  n = head / a.Hv;
+  hv = head % a.Hv;
   slice = at % ns;
-  return at / ns < run && head < heads;
+  if (n >= a.nseq) return false;
+  if (a.offsets && a.nseq > 1 && a.nseq <= 64) {
+    const int lane = threadIdx.x & 63;
+    const int len = lane < a.nseq ? (gdr_seq(a, lane).len + kGdrC - 1) / kGdrC : -1;
+    int rank = 0;
+    for (int i = 0; i < a.nseq; ++i) {
+      const int other = __builtin_amdgcn_readlane(len, i);
+      rank += other > len || (other == len && i < lane);
+    }
+    // (the lanes without a sequence rank behind all that have one)
+    n = __builtin_ctzll(__builtin_amdgcn_ballot_w64(rank == n));
+  }
+  return true;
 }
 
 // launches (carve_gdr_*.hip); mark: called after every launch

@@ -47,9 +47,9 @@ __global__ void __launch_bounds__(128 * NW, 1) carve_gdr_bchain_kernel(GdrArgs a
   const bool helper = wave >= NW;
   const int w = helper ? wave - NW : wave;
   const int g = lane >> 4, c = lane & 15;
-  int head, slice;
-  if (!gdr_chain_block(a, a.Dv / (16 * NW), head, slice)) return;
-  const int n = head / a.Hv, hv = head % a.Hv, hk = hv / (a.Hv / a.Hk);
+  int n, hv, slice;
+  if (!gdr_chain_block(a, a.Dv / (16 * NW), n, hv, slice)) return;
+  const int hk = hv / (a.Hv / a.Hk), head = n * a.Hv + hv;
   const int v0 = 16 * (NW * slice + w);
   const GdrSeq sq = gdr_seq(a, n);
   const size_t sm = (size_t)a.Dv * DK, soff = (size_t)(v0 + c) * DK + 4 * g;
@@ -266,9 +266,9 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_bpair_kernel(GdrArgs a) {
   const bool helper = wave >= 2 * NW;
   const int w = (wave >> 1) & (NW - 1), h = wave & 1;
   const int g = lane >> 4, c = lane & 15;
-  int head, slice;
-  if (!gdr_chain_block(a, a.Dv / (16 * NW), head, slice)) return;
-  const int n = head / a.Hv, hv = head % a.Hv, hk = hv / (a.Hv / a.Hk);
+  int n, hv, slice;
+  if (!gdr_chain_block(a, a.Dv / (16 * NW), n, hv, slice)) return;
+  const int hk = hv / (a.Hv / a.Hk), head = n * a.Hv + hv;
   const int v0 = 16 * (NW * slice + w);
   const GdrSeq sq = gdr_seq(a, n);
   const size_t sm = (size_t)a.Dv * DK, soff = (size_t)(v0 + c) * DK + 16 * NP * h + 4 * g;

@@ -233,9 +233,9 @@ __global__ void __launch_bounds__(128 * kChainNW, 1) carve_gdr_chain_kernel(GdrA
   const bool helper = wave >= NW;
   const int w = helper ? wave - NW : wave;   // tile
   const int g = lane >> 4, c = lane & 15;
-  int head, slice;
-  if (!gdr_chain_block(a, a.Dv / (16 * NW), head, slice)) return;
-  const int n = head / a.Hv, hv = head % a.Hv, hk = hv / (a.Hv / a.Hk);
+  int n, hv, slice;
+  if (!gdr_chain_block(a, a.Dv / (16 * NW), n, hv, slice)) return;
+  const int hk = hv / (a.Hv / a.Hk), head = n * a.Hv + hv;
   const int vs = 16 * NW * slice, v0 = vs + 16 * w;
   const GdrSeq sq = gdr_seq(a, n);
   const size_t sm = (size_t)a.Dv * DK;   // elements of a state
@@ -448,9 +448,9 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_pair_kernel(GdrArgs a) {
   const bool helper = wave >= 2 * NW;
   const int w = (wave >> 1) & (NW - 1), h = wave & 1;   // tile, half
   const int g = lane >> 4, c = lane & 15;
-  int head, slice;
-  if (!gdr_chain_block(a, a.Dv / (16 * NW), head, slice)) return;
-  const int n = head / a.Hv, hv = head % a.Hv, hk = hv / (a.Hv / a.Hk);
+  int n, hv, slice;
+  if (!gdr_chain_block(a, a.Dv / (16 * NW), n, hv, slice)) return;
+  const int hk = hv / (a.Hv / a.Hk), head = n * a.Hv + hv;
   const int vs = 16 * NW * slice, v0 = vs + 16 * w;
   const GdrSeq sq = gdr_seq(a, n);
   const size_t sm = (size_t)a.Dv * DK;
