@@ -388,10 +388,17 @@ __device__ __forceinline__ bool gdr_chain_block(const GdrArgs& a, int ns, int& n
 int launch_gdr_fwd(const GdrArgs& a, int dtype, hipStream_t s, void (*mark)(hipStream_t));
 int launch_gdr_bwd(const GdrArgs& a, int dtype, hipStream_t s, void (*mark)(hipStream_t));
 int launch_gdr_prep(const GdrArgs& a, int dtype, bool bwd, hipStream_t s);
-// Whether a call has more value tiles than the chains' workgroups of two can run at once
-// (512): then four tiles a workgroup, one chain wave each, give more per compute unit;
-// below it two chain waves a tile run a chunk faster.
-inline bool gdr_many_tiles(const GdrArgs& a) { return a.Dv % 64 == 0 && (long long)a.nseq * a.Hv * (a.Dv / 16) > 512; }
+// Whether a call of the backward's chain has more value tiles than workgroups of two can
+// run at once (512): then four tiles a workgroup, one chain wave each, give more per compute
+// unit; below it two chain waves a tile run a chunk faster.  Both sides (us, pairs / four;
+// 128 values, bf16): 512 tiles of 4 x 2048 tokens 149 / 189; 640 of 5 x 1024 116 / 93; 1024
+// of 8 x 1024 147 / 115, with keys of 64 105 / 83.  Packed sequences differ in length, so
+// that the call waits for the longest ones' chains far beyond that: 5 documents, 640 tiles,
+// 321 / 465, keys of 64 251 / 317; 11 documents, 1408 tiles 137 / 177, 2816 tiles 121 / 134;
+// 40 documents, 5120 tiles 198 / 149.
+inline bool gdr_many_tiles(const GdrArgs& a) {
+  return a.Dv % 64 == 0 && (long long)a.nseq * a.Hv * (a.Dv / 16) > (a.offsets ? 4096 : 512);
+}
 
 struct GdrStepArgs {
   const void *q, *k, *v, *beta;

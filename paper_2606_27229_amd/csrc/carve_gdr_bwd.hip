@@ -25,6 +25,7 @@ namespace {
 //           it loads the next chunk's rows
 // z and Y pass through LDS as they lie in registers.  Barriers, two a chunk: (1) z, Y and
 // the chunk's rows are there; (2) the chain has taken z and Y.
+// Two tiles a workgroup (keys of 32), or four where there are many (gdr_many_tiles).
 template <typename T, int DK, int NW>
 struct BChainLds {
   typedef GdrRows<T, DK> KR;
@@ -237,7 +238,9 @@ __global__ void __launch_bounds__(128 * NW, 1) carve_gdr_bchain_kernel(GdrArgs a
 // token tiles 2 h, 2 h + 1 and multiplies by T^T's columns of these tokens.  Helper wave
 // h forms z of the same token tiles and Y of the same keys.
 // Two barriers a chunk, (1) and (2) as above; the chain waves of a tile meet by flags: (3)
-// the halves of K dS^T are there; (4) the parts of dR.
+// the halves of K dS^T are there; (4) the parts of dR.  Bound by the chunks following each
+// other, 4.6 us each at 128 keys and values in bf16, where the 400 MB that go out (64
+// sequences and heads of 64 chunks: 295 us) alone take 80 us; one chain wave: 372 us.
 template <typename T, int DK>
 struct BPairLds {
   static constexpr int NW = 2;
@@ -508,6 +511,11 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_bpair_kernel(GdrArgs a) {
 // so that dR S itself only reaches dk and is taken in two.
 // LDS: U and dR in three pieces fill 96 KB at 128 columns, so the rest shares places:
 // the values lie where U goes, the queries where T was.
+// 4096 chunks and heads of 128 keys and values in bf16: 470 us for 1.1 GB, 2.3 TB/s.  Bound
+// by one workgroup a compute unit (158 KB): its loads, its LDS reads (three pieces an
+// operand) and its matrix products do not overlap beyond what two waves a SIMD give.  Taken
+// from memory without LDS, the token rows alone cost 63 cycles a load instruction, and the
+// kernel 5.4 ms.
 
 // [VB columns][64 tokens] of an f32 intermediate in LDS
 template <typename T, int VB>

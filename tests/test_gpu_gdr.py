@@ -113,6 +113,18 @@ def test_packed(lens, Hk, Hv, Dk, Dv, dtype, first, behind):
             assert torch.equal(got["S_T"][i], d["S0"][i]) and torch.equal(got["dS0"][i], d["dS_T"][i])
 
 
+@pytest.mark.parametrize("nseq,Hk,Hv,Dk,Dv,dtype", [(64, 1, 2, 64, 64, BF), (65, 1, 2, 64, 64, BF), (70, 2, 16, 64, 64, BF),
+                                                    (63, 17, 17, 64, 64, F32), (5, 32, 32, 128, 256, BF)])
+def test_many_sequences(nseq, Hk, Hv, Dk, Dv, dtype):
+    """Up to 64 sequences are taken longest first, more as they come; beyond 4096 value tiles
+    the backward runs four a workgroup.  Lengths of every order, many of them equal."""
+    print(f"case many sequences {nseq} Hk={Hk} Hv={Hv} Dk={Dk} Dv={Dv} {dtype}", flush=True)
+    lens = [(0, 1, 65, 5, 130, 2)[(5 * i * i + i) % 6] if i % 9 else 70 for i in range(nseq)]
+    x = gdr_inputs(1, sum(lens), Hk, Hv, Dk, Dv, dtype, seed=nseq, seqs=nseq)
+    off = torch.tensor([0] + lens).cumsum(0).to(torch.int32).cuda()
+    compare(run(cuda(x), off), gdr_reference(x, lens), dtype, ALL)
+
+
 def test_offsets_outside_the_contract_stay_inside_the_tensors():
     """Decreasing, negative and too large offsets: the call returns, and what lies around
     the outputs keeps its values."""
