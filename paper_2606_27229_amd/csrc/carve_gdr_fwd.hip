@@ -421,25 +421,27 @@ __global__ void __launch_bounds__(128 * kChainNW, 1) carve_gdr_chain_kernel(GdrA
 // starts written out: 268 MB).  One chain wave a tile with four tiles in a workgroup, which
 // fits more tiles on the card, loses also where there are many: 8 x 1024 tokens of 32 heads
 // (2048 tiles) 318 us, this 239 us.
-template <typename T, int DK>
+template <typename T, int DK, int NW>   // NW: tiles
 struct PairLds {
-  static constexpr int NW = 2;   // tiles
   typedef GdrRows<T, DK> KR;
-  typedef GdrRows<T, 16 * NW> VR;
+  typedef GdrRows<T, 32> VR;    // (with one tile, its neighbour's values too)
   static constexpr int K = 0, V = K + KR::bytes, I = V + VR::bytes;   // I: T, scalars
   static constexpr int one = I + GdrWs<T>::fP;
-  // KB of a tile: S, the halves of K S^T that the other wave takes, U (its last two
-  // tiles without the other wave's part), that part, U's last two tiles
-  static constexpr int xS = 0, xP = DK / 16, xU = xP + 4, xV = xU + 4, xW = xV + 2, kb = xW + 2;
+  // KB of a tile: S, U (its last two tiles without the other wave's part), U's last two
+  // tiles; with room for it once more, for the other parity of the chunk; the halves of
+  // K S^T that the other wave takes, its part of U
+  static constexpr int xS = 0, xU = DK / 16, xW = xU + 4, out = xW + 2;
   static constexpr bool q_lds = sizeof(T) == 2 || DK < 128;           // (f32 queries of 128: from memory)
-  static constexpr int Q = 2 * one, qone = q_lds ? KR::bytes : 0;
-  static constexpr int x = Q + 2 * qone, flags = x + NW * kb * 1024, total = flags + NW * 16;
+  static constexpr int Q = 2 * one, qone = q_lds ? KR::bytes : 0, x = Q + 2 * qone;
+  static constexpr bool twice = x + NW * ((2 * out + 6) * 1024 + 16) <= 160 * 1024;
+  static constexpr int other = twice ? out : 0, xP = out + other, xV = xP + 4, kb = xV + 2;
+  static constexpr int flags = x + NW * kb * 1024, total = flags + NW * 16;
 };
 
-template <typename T, int DK>
-__global__ void __launch_bounds__(512, 1) carve_gdr_pair_kernel(GdrArgs a) {
-  constexpr int NP = DK / 32, NW = 2;
-  typedef PairLds<T, DK> L;
+template <typename T, int DK, int NW>
+__global__ void __launch_bounds__(256 * NW, 1) carve_gdr_pair_kernel(GdrArgs a) {
+  constexpr int NP = DK / 32;
+  typedef PairLds<T, DK, NW> L;
   typedef typename L::KR KR;
   typedef typename L::VR VR;
   typedef GdrWs<T> WS;
@@ -451,7 +453,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_pair_kernel(GdrArgs a) {
   int n, hv, slice;
   if (!gdr_chain_block(a, a.Dv / (16 * NW), n, hv, slice)) return;
   const int hk = hv / (a.Hv / a.Hk), head = n * a.Hv + hv;
-  const int vs = 16 * NW * slice, v0 = vs + 16 * w;
+  const int v0 = 16 * (NW * slice + w), vs = v0 & ~31, vt0 = v0 & 16 ? 1 : 0;   // vt0: tile of the values' rows
   const GdrSeq sq = gdr_seq(a, n);
   const size_t sm = (size_t)a.Dv * DK;
   const size_t soff = (size_t)(v0 + c) * DK + 4 * g;
@@ -473,11 +475,13 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_pair_kernel(GdrArgs a) {
     for (int ch = 0; ch < nch; ++ch) {
       const char* buf = smem + (ch & 1) * L::one;
       const float* scal = reinterpret_cast<const float*>(buf + L::I + WS::fScal);
+      f32x4* const xu = x + 64 * L::other * (ch & 1);             // this chunk's U
+      f32x4* const xs = x + 64 * L::other * ((ch + 1) & 1);       // the state behind it
       __syncthreads();   // (1)
       Fi<T, kExact> Sf[NP / 2];
 #pragma unroll
       for (int p = 0; p < NP / 2; ++p) Sf[p] = to_fi<T, kExact>(S[2 * p], S[2 * p + 1]);
-      __syncthreads();   // (2)
+      if (!L::twice) __syncthreads();   // (2)
       f32x4 acc[4];      // the other wave's two token tiles, then this one's
 #pragma unroll
       for (int y = 0; y < 4; ++y) {
@@ -498,7 +502,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_pair_kernel(GdrArgs a) {
         const int i = 2 * h + y;
         gam[y] = *reinterpret_cast<const f32x4*>(scal + kScGam * kGdrC + 16 * i + 4 * g);
         be[y] = *reinterpret_cast<const f32x4*>(scal + kScBeta * kGdrC + 16 * i + 4 * g);
-        vt[y] = Quad<T>::f32(VR::tr(buf + L::V, 16 * i, w, g, c));
+        vt[y] = Quad<T>::f32(VR::tr(buf + L::V, 16 * i, vt0, g, c));
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -512,7 +516,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_pair_kernel(GdrArgs a) {
       for (int i = 0; i < 4; ++i) {
         if (i < 2 && h) continue;   // (uniform)
         U[i] = mma<T>(Tf[i], Rf, zero4());
-        x[64 * (h ? L::xV + i - 2 : L::xU + i)] = U[i];
+        (h ? x + 64 * (L::xV + i - 2) : xu + 64 * (L::xU + i))[0] = U[i];
       }
       f32x4 end[4];
       Fr<T> Kt[NP][2];
@@ -527,12 +531,12 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_pair_kernel(GdrArgs a) {
         U[2] += x[64 * L::xV];
         U[3] += x[64 * (L::xV + 1)];
       } else {
-        U[0] = x[64 * L::xU];
-        U[1] = x[64 * (L::xU + 1)];
-        U[2] += x[64 * (L::xU + 2)];
-        U[3] += x[64 * (L::xU + 3)];
-        x[64 * L::xW] = U[2];
-        x[64 * (L::xW + 1)] = U[3];
+        U[0] = xu[64 * L::xU];
+        U[1] = xu[64 * (L::xU + 1)];
+        U[2] += xu[64 * (L::xU + 2)];
+        U[3] += xu[64 * (L::xU + 3)];
+        xu[64 * L::xW] = U[2];
+        xu[64 * (L::xW + 1)] = U[3];
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) U[i] *= end[i];
@@ -541,7 +545,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_pair_kernel(GdrArgs a) {
       for (int j = 0; j < NP; ++j) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) S[j] = mma<T>(Kt[j][s], Ue[s], S[j]);
-        x[64 * (L::xS + NP * h + j)] = S[j];
+        xs[64 * (L::xS + NP * h + j)] = S[j];
       }
     }
     __syncthreads();
@@ -623,10 +627,10 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_pair_kernel(GdrArgs a) {
     __syncthreads();   // (1)
     f32x4 S[2 * NP], U[4];
 #pragma unroll
-    for (int j = 0; j < 2 * NP; ++j) S[j] = x[64 * (L::xS + j)];
+    for (int j = 0; j < 2 * NP; ++j) S[j] = x[64 * (L::other * (ch & 1) + L::xS + j)];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) U[i] = x[64 * (i < 2 ? L::xU + i : L::xW + i - 2)];
-    if (ch < nch) __syncthreads();   // (2)
+    for (int i = 0; i < 4; ++i) U[i] = x[64 * (L::other * ((ch + 1) & 1) + (i < 2 ? L::xU + i : L::xW + i - 2))];
+    if (!L::twice && ch < nch) __syncthreads();   // (2)
     if (ch > 1) store_o(ch - 2);
     if (ch + 1 < nch) {
       load_k(ch + 1);
@@ -689,15 +693,15 @@ int launch_chain_t(const GdrArgs& a, hipStream_t s) {
   hipLaunchKernelGGL(kern, dim3(gdr_chain_grid(heads, a.Dv / (16 * NW))), dim3(128 * NW), lds, s, a);
   return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
 }
-template <typename T, int DK>
+template <typename T, int DK, int NW>
 int launch_pair_t(const GdrArgs& a, hipStream_t s) {
-  constexpr int lds = PairLds<T, DK>::total;
+  constexpr int lds = PairLds<T, DK, NW>::total;
   static_assert(lds <= 160 * 1024, "LDS");
-  const auto kern = carve_gdr_pair_kernel<T, DK>;
+  const auto kern = carve_gdr_pair_kernel<T, DK, NW>;
   if (hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
     return CARVE_ERR_HIP;
   const unsigned heads = (unsigned)a.nseq * a.Hv;
-  hipLaunchKernelGGL(kern, dim3(gdr_chain_grid(heads, a.Dv / 32)), dim3(512), lds, s, a);
+  hipLaunchKernelGGL(kern, dim3(gdr_chain_grid(heads, a.Dv / (16 * NW))), dim3(256 * NW), lds, s, a);
   return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
 }
 template <typename T, int DK>
@@ -706,7 +710,7 @@ int launch_fwd_t(const GdrArgs& a, hipStream_t s, void (*mark)(hipStream_t)) {
   if (st) return st;
   mark(s);
   if constexpr (DK == 32) st = launch_chain_t<T>(a, s);   // (one pair of key tiles: no halves)
-  else st = launch_pair_t<T, DK>(a, s);
+  else st = (long long)a.nseq * a.Hv * (a.Dv / 16) <= 256 ? launch_pair_t<T, DK, 1>(a, s) : launch_pair_t<T, DK, 2>(a, s);
   mark(s);
   return st;
 }
