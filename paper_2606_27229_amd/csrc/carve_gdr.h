@@ -388,6 +388,11 @@ __device__ __forceinline__ bool gdr_chain_block(const GdrArgs& a, int ns, int& n
 int launch_gdr_fwd(const GdrArgs& a, int dtype, hipStream_t s, void (*mark)(hipStream_t));
 int launch_gdr_bwd(const GdrArgs& a, int dtype, hipStream_t s, void (*mark)(hipStream_t));
 int launch_gdr_prep(const GdrArgs& a, int dtype, bool bwd, hipStream_t s);
+// Whether a call has no more value tiles than the card compute units (256): then a tile a
+// workgroup runs a chunk faster than two, and beyond it they wait for each other (forward,
+// one / two, us: 128 tiles of 4096 tokens 146 / 153, 256 149 / 154, in f32 with 1024 tokens
+// 69 / 87; 320 tiles 271 / 166).
+inline bool gdr_few_tiles(const GdrArgs& a) { return (long long)a.nseq * a.Hv * (a.Dv / 16) <= 256; }
 // Whether a call of the backward's chain has more value tiles than workgroups of two can
 // run at once (512): then four tiles a workgroup, one chain wave each, give more per compute
 // unit; below it two chain waves a tile run a chunk faster.  Both sides (us, pairs / four;

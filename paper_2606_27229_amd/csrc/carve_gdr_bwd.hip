@@ -241,26 +241,28 @@ __global__ void __launch_bounds__(128 * NW, 1) carve_gdr_bchain_kernel(GdrArgs a
 // the halves of K dS^T are there; (4) the parts of dR.  Bound by the chunks following each
 // other, 4.6 us each at 128 keys and values in bf16, where the 400 MB that go out (64
 // sequences and heads of 64 chunks: 295 us) alone take 80 us; one chain wave: 372 us.
-template <typename T, int DK>
+template <typename T, int DK, int NW>   // NW: tiles
 struct BPairLds {
-  static constexpr int NW = 2;
   typedef GdrRows<T, DK> KR;
-  typedef GdrRows<T, 16 * NW> VR;
+  typedef GdrRows<T, 32> VR;    // (with one tile, its neighbour's columns too)
   static constexpr bool q_lds = sizeof(T) == 2 || DK < 128;       // (f32 queries of 128: from memory)
   static constexpr int K0 = 0, I = KR::bytes;                     // I: scalars, then T^T
   static constexpr int one = I + kGdrScal + GdrWs<T>::I3;
   static constexpr int Q = 2 * one, qone = q_lds ? KR::bytes : 0;
-  // KB of a tile: z, Y, the halves of K dS^T that the other wave takes, dR of wave 1 (its
-  // first two tiles without wave 0's part), that part
-  static constexpr int xz = 0, xY = 4, xP = xY + DK / 16, xU = xP + 4, xV = xU + 4, kb = xV + 2;
-  static constexpr int O = Q + 2 * qone;                          // dO of the workgroup's columns
-  static constexpr int x = O + 2 * VR::bytes, flags = x + NW * kb * 1024, total = flags + NW * 16;
+  static constexpr int O = Q + 2 * qone, x = O + 2 * VR::bytes;   // O: dO of the workgroup's columns
+  // KB of a tile: z, Y; with room for it once more, for the other parity of the chunk; the
+  // halves of K dS^T that the other wave takes, dR of wave 1 (its first two tiles without
+  // wave 0's part), that part
+  static constexpr int xz = 0, xY = 4, in = xY + DK / 16;
+  static constexpr bool twice = x + NW * ((2 * in + 10) * 1024 + 16) <= 160 * 1024;
+  static constexpr int other = twice ? in : 0, xP = in + other, xU = xP + 4, xV = xU + 4, kb = xV + 2;
+  static constexpr int flags = x + NW * kb * 1024, total = flags + NW * 16;
 };
 
-template <typename T, int DK>
-__global__ void __launch_bounds__(512, 1) carve_gdr_bpair_kernel(GdrArgs a) {
-  constexpr int NP = DK / 32, NW = 2;
-  typedef BPairLds<T, DK> L;
+template <typename T, int DK, int NW>
+__global__ void __launch_bounds__(256 * NW, 1) carve_gdr_bpair_kernel(GdrArgs a) {
+  constexpr int NP = DK / 32;
+  typedef BPairLds<T, DK, NW> L;
   typedef typename L::KR KR;
   typedef typename L::VR VR;
   typedef GdrWs<T> WS;
@@ -274,6 +276,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_bpair_kernel(GdrArgs a) {
   const int hk = hv / (a.Hv / a.Hk), head = n * a.Hv + hv;
   const int v0 = 16 * (NW * slice + w);
   const GdrSeq sq = gdr_seq(a, n);
+  const int vt0 = v0 & 16 ? 1 : 0;   // tile of dO's columns
   const size_t sm = (size_t)a.Dv * DK, soff = (size_t)(v0 + c) * DK + 16 * NP * h + 4 * g;
   const int nch = (sq.len + kGdrC - 1) / kGdrC;
   f32x4* x = reinterpret_cast<f32x4*>(smem + L::x + w * L::kb * 1024) + lane;
@@ -292,6 +295,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_bpair_kernel(GdrArgs a) {
       const char* buf = smem + (ch & 1) * L::one;
       const float* scal = reinterpret_cast<const float*>(buf + L::I);
       const size_t sh = (size_t)(sq.slot0 + ch) * a.Hv + hv;
+      const f32x4* const xi = x + 64 * L::other * (ch & 1);   // this chunk's z and Y
       __syncthreads();   // (1)
       const float gend = scal[kScGam * kGdrC + kGdrC - 1];
       float* out = a.dS_chunks + sh * sm + soff;
@@ -302,11 +306,11 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_bpair_kernel(GdrArgs a) {
 #pragma unroll
         for (int j = 2 * p; j < 2 * p + 2; ++j) {
           *reinterpret_cast<f32x4*>(out + 16 * j) = S[j];
-          S[j] = S[j] * gend + x[64 * (L::xY + NP * h + j)];
+          S[j] = S[j] * gend + xi[64 * (L::xY + NP * h + j)];
         }
       }
-      f32x4 U[2] = {x[64 * (L::xz + 2 * h)], x[64 * (L::xz + 2 * h + 1)]};
-      __syncthreads();   // (2)
+      f32x4 U[2] = {xi[64 * (L::xz + 2 * h)], xi[64 * (L::xz + 2 * h + 1)]};
+      if (!L::twice) __syncthreads();   // (2)
       f32x4 acc[4];      // the other wave's two token tiles, then this one's
 #pragma unroll
       for (int y = 0; y < 4; ++y) {
@@ -381,7 +385,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_bpair_kernel(GdrArgs a) {
   if (nch == 0) return;   // (no barriers then)
   const T* q = reinterpret_cast<const T*>(a.q) + sq.batch * a.qs[0] + sq.t0 * a.qs[1] + hk * a.qs[2];
   const T* k = reinterpret_cast<const T*>(a.k) + sq.batch * a.ks[0] + sq.t0 * a.ks[1] + hk * a.ks[2];
-  const T* dO = reinterpret_cast<const T*>(a.dO) + (((size_t)sq.batch * a.T + sq.t0) * a.Hv + hv) * a.Dv + 16 * NW * slice;
+  const T* dO = reinterpret_cast<const T*>(a.dO) + (((size_t)sq.batch * a.T + sq.t0) * a.Hv + hv) * a.Dv + (v0 & ~31);
   const size_t ors = (size_t)a.Hv * a.Dv;
   const int part = wave - 2 * NW;
   const auto ws_of = [&](int ch) { return a.ws + ((size_t)(sq.slot0 + ch) * a.Hv + hv) * a.per; };
@@ -420,7 +424,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_bpair_kernel(GdrArgs a) {
   const auto work_z = [&](Mine& m, int ch) {
     const int len = sq.len - ch * kGdrC;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) od[i] = VR::tr(smem + L::O + (ch & 1) * VR::bytes, 16 * i, w, g, c);
+    for (int i = 0; i < 4; ++i) od[i] = VR::tr(smem + L::O + (ch & 1) * VR::bytes, 16 * i, vt0, g, c);
     if (len < kGdrC)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -437,7 +441,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_bpair_kernel(GdrArgs a) {
         z = mma<T>(m.Pt[y][0], of[0], z);
         z = mma<T>(m.Pt[y][1], of[1], z);
       }
-      x[64 * (L::xz + 2 * h + y)] = z * a.scale;
+      x[64 * (L::other * (ch & 1) + L::xz + 2 * h + y)] = z * a.scale;
     }
   };
   const auto work_Y = [&](Mine& m, int ch) {
@@ -463,7 +467,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_bpair_kernel(GdrArgs a) {
         }
         y = mma<T>(f, Of[s], y);
       }
-      x[64 * (L::xY + NP * h + j)] = y;
+      x[64 * (L::other * (ch & 1) + L::xY + NP * h + j)] = y;
     }
   };
   Mine cur, nxt;
@@ -482,7 +486,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_bpair_kernel(GdrArgs a) {
   for (int ch = nch - 1; ch >= 0; --ch) {
     vm_wait_all();
     __syncthreads();   // (1)
-    __syncthreads();   // (2)
+    if (!L::twice) __syncthreads();   // (2)
     if (ch > 0) {
       load(ch - 1);
       cur = nxt;
@@ -973,15 +977,15 @@ int launch_bchain_t(const GdrArgs& a, hipStream_t s) {
   hipLaunchKernelGGL(kern, dim3(gdr_chain_grid(heads, a.Dv / (16 * NW))), dim3(128 * NW), lds, s, a);
   return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
 }
-template <typename T, int DK>
+template <typename T, int DK, int NW>
 int launch_bpair_t(const GdrArgs& a, hipStream_t s) {
-  constexpr int lds = BPairLds<T, DK>::total;
+  constexpr int lds = BPairLds<T, DK, NW>::total;
   static_assert(lds <= 160 * 1024, "LDS");
-  const auto kern = carve_gdr_bpair_kernel<T, DK>;
+  const auto kern = carve_gdr_bpair_kernel<T, DK, NW>;
   const int st = allow_lds(kern, lds);
   if (st) return st;
   const unsigned heads = (unsigned)a.nseq * a.Hv;
-  hipLaunchKernelGGL(kern, dim3(gdr_chain_grid(heads, a.Dv / 32)), dim3(512), lds, s, a);
+  hipLaunchKernelGGL(kern, dim3(gdr_chain_grid(heads, a.Dv / (16 * NW))), dim3(256 * NW), lds, s, a);
   return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
 }
 template <typename T, int DK, int VB, int NB>
@@ -1003,7 +1007,8 @@ int launch_bwd_t(const GdrArgs& a, hipStream_t s, void (*mark)(hipStream_t)) {
     st = launch_bchain_t<T, DK, 2>(a, s);
   } else {
     constexpr bool four = sizeof(T) == 2 || DK < 128;   // (f32 rows of 128: four tiles' LDS does not fit)
-    if (!four || !gdr_many_tiles(a)) st = launch_bpair_t<T, DK>(a, s);
+    if (gdr_few_tiles(a)) st = launch_bpair_t<T, DK, 1>(a, s);
+    else if (!four || !gdr_many_tiles(a)) st = launch_bpair_t<T, DK, 2>(a, s);
     else if constexpr (four) st = launch_bchain_t<T, DK, 4>(a, s);
   }
   if (st) return st;

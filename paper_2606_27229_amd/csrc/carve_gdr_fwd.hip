@@ -710,7 +710,7 @@ int launch_fwd_t(const GdrArgs& a, hipStream_t s, void (*mark)(hipStream_t)) {
   if (st) return st;
   mark(s);
   if constexpr (DK == 32) st = launch_chain_t<T>(a, s);   // (one pair of key tiles: no halves)
-  else st = (long long)a.nseq * a.Hv * (a.Dv / 16) <= 256 ? launch_pair_t<T, DK, 1>(a, s) : launch_pair_t<T, DK, 2>(a, s);
+  else st = gdr_few_tiles(a) ? launch_pair_t<T, DK, 1>(a, s) : launch_pair_t<T, DK, 2>(a, s);
   mark(s);
   return st;
 }

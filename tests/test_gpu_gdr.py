@@ -74,6 +74,15 @@ def test_many_heads(Hk, Hv, Dk, Dv, dtype):
     compare(run(cuda(x)), gdr_reference(x), dtype, ALL)
 
 
+@pytest.mark.parametrize("Hk,Hv,Dk,Dv,dtype", [(20, 20, 64, 256, F32), (40, 40, 64, 128, BF), (10, 20, 128, 256, BF), (33, 33, 128, 128, F32),
+                                               (16, 16, 128, 256, BF), (17, 17, 64, 256, F32)])
+def test_heads_between(Hk, Hv, Dk, Dv, dtype):
+    """256 value tiles, a tile a workgroup, and a few more, two."""
+    print(f"case heads Hk={Hk} Hv={Hv} Dk={Dk} Dv={Dv} {dtype}", flush=True)
+    x = gdr_inputs(1, 200, Hk, Hv, Dk, Dv, dtype, seed=Hk + Dk)
+    compare(run(cuda(x)), gdr_reference(x), dtype, ALL)
+
+
 LENGTHS = [[0, 1, 64, 0, 65, 130, 1], [63], [1, 0, 0], [128, 64, 7]]
 
 
