@@ -237,7 +237,8 @@ __global__ void __launch_bounds__(128 * NW, 1) carve_gdr_bchain_kernel(GdrArgs a
 // carve_gdr_pair_kernel.  Chain wave h keeps dS of the keys' half h, finishes dU of the
 // token tiles 2 h, 2 h + 1 and multiplies by T^T's columns of these tokens.  Helper wave
 // h forms z of the same token tiles and Y of the same keys.
-// Two barriers a chunk, (1) and (2) as above; the chain waves of a tile meet by flags: (3)
+// Barriers (1) and, without LDS for z and Y of two chunks in turn, (2) as above; the chain
+// waves of a tile meet by flags: (3)
 // the halves of K dS^T are there; (4) the parts of dR.  Bound by the chunks following each
 // other, 4.6 us each at 128 keys and values in bf16, where the 400 MB that go out (64
 // sequences and heads of 64 chunks: 295 us) alone take 80 us; one chain wave: 372 us.
