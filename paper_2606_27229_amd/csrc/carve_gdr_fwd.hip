@@ -59,14 +59,18 @@ __global__ void __launch_bounds__(256, 4) carve_gdr_prep_kernel(GdrArgs a) {
   // of token 16 w + c (forward), or queries 16 j + 4 g + e against key 16 w + c (backward)
   f32x4 KK[4], QK[4];
   {
+    // (the decays first: their sums form while the rows are on their way)
+    float gt = 0.0f, be = 0.0f, Gh, Gl, end;
+    if (w == 0 && lane < len) {
+      const size_t at = row0 + (size_t)lane * a.Hv;
+      gt = a.g[at];
+      be = (float)reinterpret_cast<const T*>(a.beta)[at];
+    }
     // (rows behind the last token repeat it: beta is 0 there, and no token before them
     // sees them)
     KR::template dma<4>(smem + L::K, k, (int)(a.ks[1] * sizeof(T)), len, w, lane);
     KR::template dma<4>(smem + L::Q, q, (int)(a.qs[1] * sizeof(T)), len, w, lane);
     if (w == 0) {   // decays: prefix sums over the wave's lanes
-      const size_t at = row0 + (size_t)lane * a.Hv;
-      float gt = lane < len ? a.g[at] : 0.0f;
-      const float be = lane < len ? (float)reinterpret_cast<const T*>(a.beta)[at] : 0.0f;
       gt = gt < kGdrMinG ? kGdrMinG : gt;
       double G = (double)gt;
 #pragma unroll
@@ -74,19 +78,22 @@ __global__ void __launch_bounds__(256, 4) carve_gdr_prep_kernel(GdrArgs a) {
         const double up = __shfl_up(G, d);
         if (lane >= d) G += up;
       }
-      const float Gh = (float)G, Gl = (float)(G - (double)Gh);
-      const double Ge = __shfl(G, 63);
+      Gh = (float)G;
+      Gl = (float)(G - (double)Gh);
+      end = (float)(__shfl(G, 63) - G);
       sGh[lane] = Gh;
       sGl[lane] = Gl;
       sB[lane] = be;
+    }
+    vm_wait_all();
+    __syncthreads();
+    if (w == 0) {   // (behind the wait, which would wait for these stores too)
       scal[kScGam * kGdrC + lane] = decay_exp(Gh) * (1.0f + Gl);
-      scal[kScEnd * kGdrC + lane] = decay_exp((float)(Ge - G));
+      scal[kScEnd * kGdrC + lane] = decay_exp(end);
       scal[kScBeta * kGdrC + lane] = be;
       scal[kScGh * kGdrC + lane] = Gh;
       scal[kScGl * kGdrC + lane] = Gl;
     }
-    vm_wait_all();
-    __syncthreads();
     Fr<T> fk[NP], fq[NP];
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
