@@ -10,8 +10,8 @@ namespace {
 // operand images, with the chunk's decay factors.  One workgroup of four waves each.
 // Wave w forms the products of token tile w (as columns of the result, so that a lane
 // holds four consecutive entries of a row of A and P: P's image needs no transposition).
-// The diagonal 16 x 16 blocks are inverted by substitution (one lane a column, all four
-// blocks in one wave), the blocks below by T21 = -T22 A21 T11 with f32 matrix-core
+// The diagonal 16 x 16 blocks are inverted by substitution (one lane a column, a block a
+// wave), the blocks below by T21 = -T22 A21 T11 with f32 matrix-core
 // products, twice.  f32 throughout: T multiplies every value of the chunk.  Bound by the
 // latency of these steps, so what counts is how many workgroups a compute unit holds:
 // A (below the diagonal) and T (transposed, above it) share 17 KB of LDS, where the rows
@@ -140,10 +140,11 @@ __global__ void __launch_bounds__(256, 4) carve_gdr_prep_kernel(GdrArgs a) {
       if (BWD && s >= w / 2) st_img<T, kExact>(ws + WS::bPt, img_upper(w, s), lane, QK[2 * s], QK[2 * s + 1]);
     }
   }
-  __syncthreads();
-  if (w == 0) {   // diagonal blocks: lane (g, c) column c of block g
-    const float* A = sM + 16 * g * LD + 16 * g;
-    float* Tt = sM + (16 * g + c) * LD + 16 * g;
+  // the wave's own diagonal block, lane (g, c) column c of its inverse; A's block is this
+  // wave's writes (LDS accesses of a wave are carried out in order) and is not read again
+  asm volatile("" ::: "memory");
+  {
+    const float* A = sM + 16 * w * (LD + 1);
     float col[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -152,27 +153,22 @@ __global__ void __launch_bounds__(256, 4) carve_gdr_prep_kernel(GdrArgs a) {
       for (int j = 0; j < i; ++j) x -= A[i * LD + j] * col[j];
       col[i] = x;
     }
+    asm volatile("" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (i >= c) Tt[i] = col[i];   // (above the diagonal and on it: A's entries stay)
+    for (int i = 0; i < 16; i += 4)   // (T transposed, zeros below its diagonal)
+      if (4 * g == i) *reinterpret_cast<f32x4*>(sM + (16 * w + c) * LD + 16 * w + i) = f32x4{col[i], col[i + 1], col[i + 2], col[i + 3]};
   }
   __syncthreads();
-  // 16 x 16 operands: A's rows; T's rows and columns, zero above T's diagonal
+  // 16 x 16 operands: A's rows; T's rows and columns, zero above T's diagonal blocks
   const auto opA = [&](int i, int j) { return *reinterpret_cast<const f32x4*>(sM + (16 * i + c) * LD + 16 * j + 4 * g); };
   const auto rowT = [&](int i, int j) {
     const float* r = sM + (16 * j + 4 * g) * LD + 16 * i + c;
-    f32x4 x = {r[0], r[LD], r[2 * LD], r[3 * LD]};
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (i < j || (i == j && 4 * g + e > c)) x[e] = 0.0f;
-    return x;
+    const f32x4 x = {r[0], r[LD], r[2 * LD], r[3 * LD]};
+    return i < j ? zero4() : x;
   };
   const auto colT = [&](int i, int j) {
-    f32x4 x = *reinterpret_cast<const f32x4*>(sM + (16 * j + c) * LD + 16 * i + 4 * g);
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (i < j || (i == j && 4 * g + e < c)) x[e] = 0.0f;
-    return x;
+    const f32x4 x = *reinterpret_cast<const f32x4*>(sM + (16 * j + c) * LD + 16 * i + 4 * g);
+    return i < j ? zero4() : x;
   };
   const auto put = [&](int i, int j, f32x4 x) { *reinterpret_cast<f32x4*>(sM + (16 * j + c) * LD + 16 * i + 4 * g) = -x; };
   typedef Quad<float> QF;
