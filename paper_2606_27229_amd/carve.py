@@ -672,27 +672,33 @@ def gdr_step(q, k, v, g, beta, state, slots=None, *, scale=None, out=None, strea
     pool (-1) marks a padding entry, whose output rows are left as they were.  No
     slot may appear twice.  The other arguments are those of ``gdr_chunk_fwd``.
     Returns o [B,T,Hv,Dv] (``out`` if given)."""
-    (dims, *_), _, ptrs = _gdr_call(q, k, v, g, beta, scale, None)
-    dev = q.device
-    if not isinstance(state, torch.Tensor) or state.dim() != 4:
-        raise ValueError("state must be [pool, Hv, Dv, Dk]")
-    key = ("step", q.shape, v.shape, q.dtype, dev, _layout(state), _layout(slots), _layout(out))
-    if key not in _checked:
-        _same_device(dev, state=state, slots=slots, out=out)
+    if scale is not None:
+        scale = float(scale)
+    try:
+        key = ("step", scale, _layout(q), _layout(k), _layout(v), _layout(g), _layout(beta), _layout(state),
+               _layout(slots), _layout(out))
+        dims = _checked.get(key)
+    except AttributeError:   # (something else than tensors: named below)
+        key = dims = None
+    if dims is None:
+        (dims, *_), _, _ = _gdr_call(q, k, v, g, beta, scale, None)
+        if not isinstance(state, torch.Tensor) or state.dim() != 4:
+            raise ValueError("state must be [pool, Hv, Dv, Dk]")
         _ptr(slots, "slots", torch.int32, (v.shape[0],))
         _ptr(state, "state", torch.float32, (state.shape[0], v.shape[2], v.shape[3], q.shape[3]))
         _ptr(out, "out", q.dtype, v.shape)
-        _remember(key, True)
+        _same_device(q.device, state=state, slots=slots, out=out)
+        _remember(key, dims)
 
     def call(s):
         o = _dense_like(v) if out is None else out
-        res["o"] = o
-        return _lib.carve_gdr_step(dims, *ptrs, None if slots is None else slots.data_ptr(), state.shape[0],
-                                   state.data_ptr(), o.data_ptr(), s)
+        return o, _lib.carve_gdr_step(
+            dims, q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(),
+            None if slots is None else slots.data_ptr(), state.shape[0], state.data_ptr(), o.data_ptr(), s)
 
-    res = {}
-    _check("carve_gdr_step", _on_stream(call, dev, stream))
-    return res["o"]
+    o, st = _on_stream(call, q.device, stream)
+    _check("carve_gdr_step", st)
+    return o
 
 
 GATE_ACTS = {"silu": 1, "sigmoid": 2}
@@ -768,24 +774,20 @@ def block_norm_fwd(y, weight, *, groups=1, gate=None, gate_act="silu", residual=
     out.  y, gate and residual may be slices of wider rows.  Returns (x, h), h None
     without next_weight.  ``out`` may hold preallocated {"x", "h"}."""
     dims, _, ptrs = _block_norm_call(y, weight, groups, gate, gate_act, residual, alpha, scale, next_weight, eps)
-    res = {"x": None, "h": None, **(out or {})}
-    _same_device(y.device, **res)
+    x, h = (out.get("x"), out.get("h")) if out else (None, None)
+    for name, t in (("x", x), ("h", h)):
+        if t is not None:
+            _ptr(t, name, y.dtype, y.shape)
+            _same_device(y.device, **{name: t})
 
     def call(s):
-        if out is None:
-            res["x"] = _dense_like(y)
-            x = res["x"].data_ptr()
-            h = None
-            if next_weight is not None:
-                res["h"] = _dense_like(y)
-                h = res["h"].data_ptr()
-        else:
-            x = _out(res, "x", tuple(y.shape), y.dtype, y.device)
-            h = _out(res, "h", tuple(y.shape), y.dtype, y.device) if next_weight is not None else _ptr(res["h"], "h")
-        return _lib.carve_block_norm_fwd(dims, *ptrs, x, h, s)
+        xo = _dense_like(y) if x is None else x
+        ho = _dense_like(y) if h is None and next_weight is not None else h
+        return xo, ho, _lib.carve_block_norm_fwd(dims, *ptrs, xo.data_ptr(), None if ho is None else ho.data_ptr(), s)
 
-    _check("carve_block_norm_fwd", _on_stream(call, y.device, stream))
-    return res["x"], res["h"]
+    x, h, st = _on_stream(call, y.device, stream)
+    _check("carve_block_norm_fwd", st)
+    return x, h
 
 
 def block_norm_bwd(y, weight, dx, dh=None, *, groups=1, gate=None, gate_act="silu", residual=None, alpha=1.0, scale=None,
