@@ -408,3 +408,90 @@ def test_captured_and_replayed():
         torch.cuda.synchronize()
         for n in want:
             assert torch.equal(got[n], want[n]), (turn, n)
+
+
+def test_replayed_on_other_sequences():
+    """Offsets, slots and states are read on the device: one graph serves batches that are
+    packed otherwise, a sequence longer than any it was captured with among them."""
+    x = cuda(gdr_inputs(1, 300, 2, 4, 128, 64, BF, seed=121, seqs=4))
+    offs = [[0, 100, 100, 164, 300], [0, 0, 0, 299, 300], [10, 11, 200, 290, 290], [0, 300, 300, 300, 300]]
+    off = torch.tensor(offs[0], dtype=torch.int32, device="cuda")
+    pool, slots = torch.zeros(5, 4, 64, 128, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    outs = {n: torch.zeros_like(x[m]) for n, m in (("o", "v"), ("dq", "q"), ("dk", "k"), ("dv", "v"), ("dg", "g"), ("dbeta", "beta"))}
+
+    def work():
+        for t in outs.values():
+            t.zero_()
+        o, S_T, S_c = carve.gdr_chunk_fwd(x["q"], x["k"], x["v"], x["g"], x["beta"], x["S0"], offsets=off, out={"o": outs["o"]})
+        r = carve.gdr_chunk_bwd(x["q"], x["k"], x["v"], x["g"], x["beta"], S_c, x["dO"], x["dS_T"], offsets=off,
+                                out={n: t for n, t in outs.items() if n != "o"})
+        pool.zero_()
+        r["step"] = carve.gdr_step(*(x[n][:, :1].contiguous() for n in ("q", "k", "v", "g", "beta")), pool, slots)
+        return dict(r, S_T=S_T, pool=pool, **outs)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        work()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        res = work()
+    for turn, now in enumerate(offs + offs[:1]):
+        off.copy_(torch.tensor(now, dtype=torch.int32))
+        slots.fill_(turn % 5)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = {n: t.clone() for n, t in res.items()}
+        want = {n: t.clone() for n, t in work().items()}
+        torch.cuda.synchronize()
+        assert got["pool"][turn % 5].any()
+        for n in want:
+            assert torch.equal(got[n], want[n]), (turn, n)
+
+
+def test_small_step_between_large_strides():
+    """A step on one token of a wide projection whose head and token strides differ from every
+    other call's, with padding entries, twice on the same pool."""
+    B, Hk, Hv, D = 3, 2, 4, 64
+    x = gdr_inputs(B, 2, Hk, Hv, D, D, F32, seed=131)
+    ref = gdr_reference(x, grads=False)
+    wide = torch.zeros(B, 2, 2 * Hk * D + Hv * D + 64, device="cuda")
+    q = wide[..., :Hk * D].view(B, 2, Hk, D)
+    k = wide[..., Hk * D:2 * Hk * D].view(B, 2, Hk, D)
+    v = wide[..., 2 * Hk * D:2 * Hk * D + Hv * D].view(B, 2, Hv, D)
+    for t, n in ((q, "q"), (k, "k"), (v, "v")):
+        t.copy_(x[n])
+    pool = torch.zeros(7, Hv, D, D, device="cuda")
+    slots = torch.tensor([6, 0, 3], dtype=torch.int32, device="cuda")
+    pool[slots.long()] = x["S0"].cuda()
+    for t in range(2):
+        cut = slice(t, t + 1)
+        o = carve.gdr_step(q[:, cut], k[:, cut], v[:, cut], x["g"][:, cut].contiguous().cuda(),
+                           x["beta"][:, cut].contiguous().cuda(), pool, slots, scale=x["scale"])
+        assert rel(o, ref["o"][:, cut]) <= 256 * 2.0 ** -24, t
+    assert rel(pool[slots.long()], ref["S_T"]) <= 256 * 2.0 ** -24
+
+
+def test_more_than_2_31_values():
+    """Values, outputs and value gradients past 2^31 elements: the end of a long sequence
+    against a call on that end alone, from the state that the long call had there."""
+    T, Hk, Hv, Dk, Dv, n = 66 * 1024, 4, 128, 32, 256, 128
+    assert T * Hv * Dv > 1 << 31
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    rnd = lambda *s: torch.randn(*s, generator=gen, device="cuda", dtype=BF)
+    q, k = rnd(1, T, Hk, Dk) / 6, rnd(1, T, Hk, Dk) / 6
+    v, dO = rnd(1, T, Hv, Dv), rnd(1, T, Hv, Dv)
+    g = -0.1 * torch.rand(1, T, Hv, generator=gen, device="cuda")
+    beta = torch.rand(1, T, Hv, generator=gen, device="cuda").to(BF)
+    o, S_T, S_c = carve.gdr_chunk_fwd(q, k, v, g, beta)
+    r = carve.gdr_chunk_bwd(q, k, v, g, beta, S_c, dO)
+    end = [t[:, T - n:].contiguous() for t in (q, k, v, g, beta)]
+    S0 = S_c[(T - n) // 64:(T - n) // 64 + 1].contiguous()
+    oe, Se, Sce = carve.gdr_chunk_fwd(*end, S0)
+    re = carve.gdr_chunk_bwd(*end, Sce, dO[:, T - n:].contiguous())
+    assert oe.float().abs().max() > 0.1
+    assert torch.equal(o[:, T - n:], oe) and torch.equal(S_T, Se)
+    for m in ("dq", "dk", "dv", "dg", "dbeta"):
+        assert torch.equal(r[m][:, T - n:], re[m]), m
+        assert torch.isfinite(r[m][:, :64]).all(), m
