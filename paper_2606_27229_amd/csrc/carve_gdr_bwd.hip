@@ -754,6 +754,18 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
         for (int i = 0; i < 4; ++i) vt[i] = Quad<T>::f32(VR::tr(smem + L::V, 16 * i, w, g, c));
       }
       __syncthreads();   // (U goes where the values were)
+      f32x4 sn[2], dn[2];   // S, dS of the next 32 value columns, on their way from here
+      const auto columns = [&](int p) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int at = (32 * p + 16 * h + 4 * g + e) * DK + 16 * jt + c;
+            sn[h][e] = S[at];
+            dn[h][e] = dS[at];
+          }
+      };
+      columns(0);
       if (mine) {
         Fi<T, kExact> Sf[NP];
 #pragma unroll
@@ -785,18 +797,6 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
           UT::template put<kExact>(smem + L::U, 16 * w + c, i, g, x);
         }
       }
-      f32x4 sn[2], dn[2];   // S, dS of the next 32 value columns
-      const auto columns = [&](int p) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int at = (32 * p + 16 * h + 4 * g + e) * DK + 16 * jt + c;
-            sn[h][e] = S[at];
-            dn[h][e] = dS[at];
-          }
-      };
-      columns(0);
       __syncthreads();
       // ---- 2. products over these columns (queries on their way)
       if (NB == 1) clear();
