@@ -529,10 +529,14 @@ def _dense_like(t):
     return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
-def _out(res, name, shape, dtype, device):
-    if res.get(name) is None:
-        res[name] = torch.empty(shape, dtype=dtype, device=device)
-    return _ptr(res[name], name, dtype, shape)
+def _out(res, name, like, shape, dtype, device):
+    """The pointer of res[name], which is allocated if missing; like: a tensor of its
+    shape and type, or None."""
+    t = res.get(name)
+    if t is not None:
+        return _ptr(t, name, dtype, shape)
+    res[name] = t = torch.empty(shape, dtype=dtype, device=device) if like is None else _dense_like(like)
+    return t.data_ptr()
 
 
 def _scratch(workspace, nbytes, device):
@@ -624,9 +628,9 @@ def gdr_chunk_fwd(q, k, v, g, beta, S0=None, *, scale=None, offsets=None, want_c
     _same_device(dev, S0=S0, workspace=workspace, **res)
 
     def call(s):
-        o = _out(res, "o", (B, T, Hv, Dv), dt, dev)
-        S_T = _out(res, "S_T", (seqs, Hv, Dv, Dk), f32, dev) if want_state or res.get("S_T") is not None else None
-        S_c = _out(res, "S_chunks", (chunks, Hv, Dv, Dk), f32, dev) if want_chunks or res.get("S_chunks") is not None else None
+        o = _out(res, "o", v, (B, T, Hv, Dv), dt, dev)
+        S_T = _out(res, "S_T", S0, (seqs, Hv, Dv, Dk), f32, dev) if want_state or res.get("S_T") is not None else None
+        S_c = _out(res, "S_chunks", None, (chunks, Hv, Dv, Dk), f32, dev) if want_chunks or res.get("S_chunks") is not None else None
         ws, ws_ptr, ws_len = _scratch(workspace, ws_bytes, dev)
         return lib.carve_gdr_chunk_fwd(
             dims, *ptrs, _ptr(S0, "S0", f32, (seqs, Hv, Dv, Dk)), _ptr(offsets, "offsets", torch.int32),
@@ -644,16 +648,14 @@ def gdr_chunk_bwd(q, k, v, g, beta, S_chunks, dO, dS_T=None, *, scale=None, offs
     lib = load_library()
     (dims, chunks, _, ws_bytes), seqs, ptrs = _gdr_call(q, k, v, g, beta, scale, offsets)
     B, T, Hv, Dv = v.shape
-    Hk, Dk = q.shape[2:]
-    dt, f32, dev = q.dtype, torch.float32, q.device
+    Dk, dt, f32, dev = q.shape[3], q.dtype, torch.float32, q.device
     res = dict(out or {})
     _same_device(dev, S_chunks=S_chunks, dO=dO, dS_T=dS_T, workspace=workspace, **res)
 
     def call(s):
-        outs = [_out(res, name, shape, t, dev)
-                for name, shape, t in (("dq", (B, T, Hk, Dk), dt), ("dk", (B, T, Hk, Dk), dt), ("dv", (B, T, Hv, Dv), dt),
-                                       ("dg", (B, T, Hv), f32), ("dbeta", (B, T, Hv), dt))]
-        dS0 = _out(res, "dS0", (seqs, Hv, Dv, Dk), f32, dev) if want_dS0 or res.get("dS0") is not None else None
+        outs = [_out(res, name, like, like.shape, like.dtype, dev)
+                for name, like in (("dq", q), ("dk", k), ("dv", v), ("dg", g), ("dbeta", beta))]
+        dS0 = _out(res, "dS0", dS_T, (seqs, Hv, Dv, Dk), f32, dev) if want_dS0 or res.get("dS0") is not None else None
         ws, ws_ptr, ws_len = _scratch(workspace, ws_bytes, dev)
         return lib.carve_gdr_chunk_bwd(
             dims, *ptrs, _ptr(S_chunks, "S_chunks", f32, (chunks, Hv, Dv, Dk)),
@@ -798,13 +800,14 @@ def block_norm_bwd(y, weight, dx, dh=None, *, groups=1, gate=None, gate_act="sil
     lib = load_library()
     dims, ws_bytes, ptrs = _block_norm_call(y, weight, groups, gate, gate_act, residual, alpha, scale, next_weight, eps)
     res = dict(out or {})
-    dev, shape, N, f32 = y.device, tuple(y.shape), y.shape[-1], torch.float32
+    dev, shape = y.device, y.shape
     _same_device(dev, dx=dx, dh=dh, workspace=workspace, **res)
-    wanted = [("dy", y, shape, y.dtype), ("dgate", gate, shape, y.dtype), ("dresidual", residual, shape, y.dtype),
-              ("dweight", weight, (N,), f32), ("dscale", scale, (N,), f32), ("dnext_weight", next_weight, (N,), f32)]
+    wanted = (("dy", y), ("dgate", gate), ("dresidual", residual), ("dweight", weight), ("dscale", scale),
+              ("dnext_weight", next_weight))
 
     def call(s):
-        outs = [_out(res, name, sh, t, dev) if of is not None else _ptr(res.get(name), name) for name, of, sh, t in wanted]
+        outs = [_out(res, name, of, of.shape, of.dtype, dev) if of is not None else _ptr(res.get(name), name)
+                for name, of in wanted]
         ws, ws_ptr, ws_len = _scratch(workspace, ws_bytes, dev)
         return lib.carve_block_norm_bwd(dims, *ptrs, _ptr(dx, "dx", y.dtype, shape),
                                         _ptr(dh, "dh", y.dtype, shape), *outs, ws_ptr, ws_len, s)
