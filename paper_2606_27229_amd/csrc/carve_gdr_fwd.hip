@@ -17,8 +17,8 @@ namespace {
 // A (below the diagonal) and T (transposed, above it) share 17 KB of LDS, where the rows
 // were before.  The rows come through LDS because each wave needs most of them: loaded by
 // every wave for itself, 16 rows at a time, they made it 86 us at 4096 chunks of 128 keys
-// (bf16; 270 MB in and out), where it takes 64 us now; the backward form, which writes
-// two more images, 83 us.
+// (bf16; 270 MB in and out), where it takes 56 us now; the backward form, which writes
+// two more images, 70 us.
 // G is summed in 64 bits and kept as two floats, so that a decay between two tokens
 // keeps its digits however strongly the tokens before them decay.
 template <typename T, int DK>

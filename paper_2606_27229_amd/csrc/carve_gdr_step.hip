@@ -5,8 +5,8 @@
 //   S_new q = e^g (S q) + u (k.q),  S k before the write = e^g (S k).
 //
 // Bound by HBM: every state is read and written once a call, whatever T (64 states of
-// 32 heads of 128 x 128 and their tokens, 270 MB: 54 us, 5.0 TB/s; one state of 16 heads:
-// 8.9 us with the call, which is the launch and its arguments).  A row of
+// 32 heads of 128 x 128 and their tokens, 270 MB: 56 us, 4.8 TB/s; one state of 16 heads:
+// 8.3 us with the call, which is the launch and its arguments).  A row of
 // S (Dk floats) is spread over Dk / 8 lanes, two 16-byte loads each, so that a wave
 // load covers whole rows; a lane holds kStepRows rows, 8 loads in flight; a row's two
 // sums run over its lanes by DPP.
