@@ -7,8 +7,9 @@
 //   dQ = e^G dO' S + (D dP) K
 //   dK = (D dP)^T Q + M K + M^T K + E U dS - beta e^G dR S
 //   dbeta_t = dR_t.V_t - e^{G_t} k_t.(dR S)_t + sum_j dA_tj D_tj k_t.k_j
-//   dG_t = q_t.(e^G dO' S)_t - k_t.(beta e^G dR S)_t + row sums - column sums of dP P + dA A
-//   dg_t = sum_{i >= t} dG_i + sum_{j < t} k_j.(E U dS)_j + e^{G_C} <dS, S>
+//   dg_t = sum_{i >= t} (q_i.(e^G dO' S)_i - k_i.(beta e^G dR S)_i) + sum_{i >= t > j} (dP P + dA A)_ij
+//          + sum_{j < t} k_j.(E U dS)_j + e^{G_C} <dS, S>
+// (each sum over what the decay at t multiplies, and nothing else: every term holds e^{g_t})
 // Three launches: the triangles (carve_gdr_prep_kernel), the chain of state
 // gradients, then every chunk's gradients at once.
 #include "carve_gdr.h"
@@ -623,7 +624,8 @@ struct GradLds {
   static constexpr int red = Z + (KR::bytes > GdrWs<T>::I3 ? KR::bytes : GdrWs<T>::I3);
   // sums over values, [wave][64]: dR.(V - e^G S k), dR.(e^G S k); over keys, [key tile]
   // [64]: q.(dO' S), k.(U dS); <dS, S> per wave; over tiles, [4][64]: rows of dP P + dA
-  // A, rows of dA A / beta, columns of dP P + dA A
+  // A (of the diagonal tiles, sums over i >= t > j), rows of dA A / beta, columns of dP P +
+  // dA A
   static constexpr int floats = 4 * 8 * kGdrC + 8 + 3 * 4 * kGdrC;
   static constexpr int total = red + floats * 4;
 };
@@ -686,18 +688,38 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
       s1 += rQ[x * kGdrC + t];
       s2 += rUK[x * kGdrC + t];
     }
+    // (read whole, so that the reads wait for each other once; upper tiles hold nothing)
+    f32x4 rows, betas, cols;
+#pragma unroll
     for (int x = 0; x < 4; ++x) {
-      if (x <= t / 16) {
-        row += rRow[x * kGdrC + t];
-        rb += rBeta[x * kGdrC + t];
-      }
-      if (x >= t / 16) col += rCol[x * kGdrC + t];
+      rows[x] = rRow[x * kGdrC + t];
+      betas[x] = rBeta[x * kGdrC + t];
+      cols[x] = rCol[x * kGdrC + t];
+    }
+    float diag = rows[0];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      rb += x <= t / 16 ? betas[x] : 0.0f;
+      row += x < t / 16 ? rows[x] : 0.0f;
+      col += x > t / 16 ? cols[x] : 0.0f;
+      if (x == t / 16) diag = rows[x];
     }
     const float be = scal[kScBeta * kGdrC + t];
-    // dg_t: over i >= t what reaches G_i, and over j < t the writes that a decay at t
-    // takes from the end state (with - k.(E U dS) as a term of G_j and their sum as one of
-    // G_C the undecayed writes behind t would cancel: nothing would be left of a small dg)
-    float after = t < len ? s1 - be * rk1 + row - col : 0.0f;
+    // dg_t: over i >= t what token i reads of the start state, over j < t the writes that
+    // the end state keeps, and the pairs i >= t > j.  (As a suffix sum of dG alone, with a
+    // pair a row term of G_i and a column term of G_j, the pairs that a decay at t leaves
+    // alone would only cancel up to their rounding: nothing would be left of a small dg.)
+    // The pairs by tiles (I, J): the diagonal tile's; I = t's, J before it, rows from t on;
+    // J = t's, I behind it, columns before t; and whole tiles around t's.
+    const float y0 = t >= 16 ? rows[0] : 0.0f, y1 = t >= 32 ? rows[1] : 0.0f;
+    const auto of_lane = [](float x, int l) {
+      return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), l));
+    };
+    const float z0 = row_suffix(y0), z1 = row_suffix(y1);   // (whole tiles at their first rows)
+    const float t30 = of_lane(z0, 48), in1 = of_lane(z0, 32) + t30, in2 = t30 + of_lane(z1, 48);
+    float pairs = diag + row_suffix(row) + dpp<0x111>(row_scan(col));   // (0x111: of the lane before)
+    pairs += t / 16 == 1 ? in1 : t / 16 == 2 ? in2 : 0.0f;
+    float after = t < len ? s1 - be * rk1 : 0.0f;
     float before = __shfl_up(s2, 1);
     if (t == 0) before = 0.0f;
 #pragma unroll
@@ -708,7 +730,7 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
     }
     const float ends = scal[kScGam * kGdrC + kGdrC - 1] * sss;
     if (t < len) {
-      a.dg[(row0 + t) * a.Hv + hv] = after + before + ends;
+      a.dg[(row0 + t) * a.Hv + hv] = after + before + ends + pairs;
       reinterpret_cast<T*>(a.dbeta)[(row0 + t) * a.Hv + hv] = (T)(rv1 + rb);
     }
   };
@@ -880,11 +902,20 @@ __global__ void __launch_bounds__(512, 1) carve_gdr_grad_kernel(GdrArgs a) {
           const float be = scal[kScBeta * kGdrC + ti], dA = tj < ti ? -aA[x][e] : 0.0f;
           W[e] = a.scale * (D * aP[x][e]);
           M[e] = be * (D * dA);
-          // (a token's product with itself is a row and a column term of one G: no change)
+          // (no decay lies between a token and itself)
           const float pp = tj < ti ? W[e] * qk[e] : 0.0f, ab = D * dA * kk[e], sum = pp + be * ab;
           col += sum;
           rows[e] = sum;
           betas[e] = ab;
+        }
+        if (i == j) {   // (uniform) the sums over i >= t > j for t = row: down the columns, then along t's row
+          rows[2] += rows[3];
+          rows[1] += rows[2];
+          rows[0] += rows[1];
+          const float d1 = __shfl_down(rows[0], 16), d2 = __shfl_down(rows[0], 32), d3 = __shfl_down(rows[0], 48);
+          const float below = (g < 3 ? d1 : 0.0f) + (g < 2 ? d2 : 0.0f) + (g < 1 ? d3 : 0.0f);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) rows[e] = c < 4 * g + e ? rows[e] + below : 0.0f;
         }
         const float rs = row_sum4(rows, c), rb = row_sum4(betas, c);
         if (c < 4) {
