@@ -373,6 +373,8 @@ int carve_gdr_step(const carve_gdr_dims_t* d, const void* q, const void* k, cons
  * y is a block's output; n its norm over `groups` equal groups of a row (1: the
  * row; H: per head, with N = H Dv); x the residual stream; h the next block's
  * input.  One pass: h is formed from x before x is rounded to its dtype.
+ * Rows of any finite size are normalised, also where their squares leave the
+ * range of f32 (and, with eps = 0, small ones): they are summed in another unit.
  * weight, scale, next_weight: [N] f32.  y, gate, residual have row strides (in
  * elements, >= 0, 16-byte aligned), every other tensor is dense.
  * Supported: N a multiple of 8 (bf16) or 4 (f32), at most 8192; with groups > 1,

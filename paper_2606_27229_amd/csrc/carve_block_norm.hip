@@ -86,33 +86,80 @@ __device__ __forceinline__ void row_sums(float& a, float& b, float* red) {
 
 __device__ __forceinline__ float sigmoid_x(float z) { return 1.0f / (1.0f + expf(-z)); }
 
-// r1 of every chunk: over the whole row, or over the lanes of the chunk's group
+// Squares of large values leave the range of f32 (from 2^64 on, sums of them earlier), and
+// with eps = 0 those of small ones lose their digits.  A row (or group) whose mean square
+// with eps lies outside 2^-90 .. 2^87 is taken in another unit, 2^72 times as large or as
+// small: its values are then at most 2^56 and their squares sum to less than 2^126.  A
+// factor of a power of two rounds nothing, and what underflows is below 2^-36 of the mean.
+// No row that models have is of that kind: it costs the others one comparison a sum.
+__device__ __forceinline__ bool other_unit(float mean_eps) {   // (one comparison: of bits, as of values >= 0)
+  constexpr unsigned lo = (127 - 90) << 23, hi = (127 + 87) << 23;
+  return __builtin_bit_cast(unsigned, mean_eps) - lo > hi - lo;
+}
+__device__ __forceinline__ int unit_of(float mean_eps) { return mean_eps < 1.0f ? 72 : -72; }
+__device__ __forceinline__ float pow2(int e) { return __builtin_bit_cast(float, (127 + e) << 23); }
+
+// y becomes y r1 and r1 is that of every chunk: over the whole row, or over the lanes of
+// the chunk's group
 template <typename T, int NT, int NCH>
-__device__ __forceinline__ void group_rstd(const float (*y)[Vec<T>::n], float* r1, const BlockNormArgs& a, float* red) {
+__device__ __forceinline__ void group_norm(float (*y)[Vec<T>::n], float* r1, const BlockNormArgs& a, float* red) {
   constexpr int V = Vec<T>::n;
-  float part[NCH];
+  const auto squares = [&](int ch) {
+    float s = 0.0f;
 #pragma unroll
-  for (int ch = 0; ch < NCH; ++ch) {
-    part[ch] = 0.0f;
+    for (int e = 0; e < V; ++e) s += y[ch][e] * y[ch][e];
+    return s;
+  };
+  const auto times = [&](int ch, float f) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) part[ch] += y[ch][e] * y[ch][e];
-  }
+    for (int e = 0; e < V; ++e) y[ch][e] *= f;
+  };
   const float inv = 1.0f / (float)(a.N / a.groups);
   if (a.groups == 1) {
     float s = 0.0f, z = 0.0f;
 #pragma unroll
-    for (int ch = 0; ch < NCH; ++ch) s += part[ch];
+    for (int ch = 0; ch < NCH; ++ch) s += squares(ch);
     row_sums<NT>(s, z, red);
+    const float mean_eps = s * inv + a.eps;
+    float r = 1.0f / sqrtf(mean_eps), f = 1.0f;
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(other_unit(mean_eps)) != 0, 0)) {   // (the row's: uniform)
+      f = pow2(unit_of(mean_eps));
+      s = 0.0f;
 #pragma unroll
-    for (int ch = 0; ch < NCH; ++ch) r1[ch] = 1.0f / sqrtf(s * inv + a.eps);
+      for (int ch = 0; ch < NCH; ++ch) {
+        times(ch, f);
+        s += squares(ch);
+      }
+      if (NT > 64) __syncthreads();   // (the first sums are read)
+      row_sums<NT>(s, z, red);
+      r = 1.0f / sqrtf(s * inv + a.eps * f * f);
+    }
+#pragma unroll
+    for (int ch = 0; ch < NCH; ++ch) {
+      times(ch, r);
+      r1[ch] = r * f;
+    }
   } else {
 #pragma unroll
-    for (int ch = 0; ch < NCH; ++ch) r1[ch] = 1.0f / sqrtf(lanes_sum(part[ch], a.lanes) * inv + a.eps);
+    for (int ch = 0; ch < NCH; ++ch) {
+      float s = lanes_sum(squares(ch), a.lanes), f = 1.0f;
+      const float mean_eps = s * inv + a.eps;
+      float r = 1.0f / sqrtf(mean_eps);
+      const bool other = other_unit(mean_eps);   // (the group's)
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(other) != 0, 0)) {
+        f = other ? pow2(unit_of(mean_eps)) : 1.0f;
+        times(ch, f);
+        s = lanes_sum(squares(ch), a.lanes);
+        r = 1.0f / sqrtf(s * inv + a.eps * f * f);
+      }
+      times(ch, r);
+      r1[ch] = r * f;
+    }
   }
 }
 
 template <typename T, int NT, int NCH>
-__global__ void __launch_bounds__(256) carve_block_norm_fwd_kernel(BlockNormArgs a) {
+__global__ void __launch_bounds__(256, NCH <= 2 ? 6 : 3) carve_block_norm_fwd_kernel(BlockNormArgs a) {
   constexpr int V = Vec<T>::n;
   __shared__ float red[16];
   const int tid = threadIdx.x % NT;
@@ -133,19 +180,32 @@ __global__ void __launch_bounds__(256) carve_block_norm_fwd_kernel(BlockNormArgs
       if (a.residual) ld_vec(rp + c0, rs[ch]);
     }
   }
+  // (with up to eight columns a thread the parameters are on their way before the sums)
+  constexpr bool AHEAD = NCH * V <= 8;
+  float pw[V], ps[V], pn[V];
+  if (AHEAD && tid * V < a.N) {
+    ld_f32(a.weight + tid * V, pw, V);
+    if (a.scale) ld_f32(a.scale + tid * V, ps, V);
+    if (a.next_weight) ld_f32(a.next_weight + tid * V, pn, V);
+  }
   float r1[NCH];
-  group_rstd<T, NT, NCH>(y, r1, a, red);
+  group_norm<T, NT, NCH>(y, r1, a, red);
   float ss = 0.0f, none = 0.0f;
 #pragma unroll
   for (int ch = 0; ch < NCH; ++ch) {
     const int c0 = (ch * NT + tid) * V;
     if (c0 >= a.N) continue;
     float wt[V], sc[V];
-    ld_f32(a.weight + c0, wt, V);
-    if (a.scale) ld_f32(a.scale + c0, sc, V);
+    if constexpr (AHEAD) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) wt[e] = pw[e], sc[e] = ps[e];
+    } else {
+      ld_f32(a.weight + c0, wt, V);
+      if (a.scale) ld_f32(a.scale + c0, sc, V);
+    }
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      float t = y[ch][e] * r1[ch] * wt[e];
+      float t = y[ch][e] * wt[e];
       if (a.gate) t *= a.act == CARVE_GATE_SILU ? z[ch][e] * sigmoid_x(z[ch][e]) : sigmoid_x(z[ch][e]);
       if (a.scale) t *= sc[e];
       y[ch][e] = a.residual ? a.alpha * rs[ch][e] + t : t;
@@ -155,13 +215,34 @@ __global__ void __launch_bounds__(256) carve_block_norm_fwd_kernel(BlockNormArgs
   }
   if (!a.next_weight) return;   // (uniform)
   row_sums<NT>(ss, none, red + 8);
-  const float r2 = 1.0f / sqrtf(ss / (float)a.N + a.eps);
+  const float mean_eps = ss / (float)a.N + a.eps;
+  float r2 = 1.0f / sqrtf(mean_eps);
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64(other_unit(mean_eps)) != 0, 0)) {   // (uniform)
+    const float f = pow2(unit_of(mean_eps));
+    ss = 0.0f;
+#pragma unroll
+    for (int ch = 0; ch < NCH; ++ch)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        if ((ch * NT + tid) * V >= a.N) continue;
+        y[ch][e] *= f;
+        ss += y[ch][e] * y[ch][e];
+      }
+    if (NT > 64) __syncthreads();   // (the first sums are read)
+    row_sums<NT>(ss, none, red + 8);
+    r2 = 1.0f / sqrtf(ss / (float)a.N + a.eps * f * f);
+  }
 #pragma unroll
   for (int ch = 0; ch < NCH; ++ch) {
     const int c0 = (ch * NT + tid) * V;
     if (c0 >= a.N) continue;
     float wt[V];
-    ld_f32(a.next_weight + c0, wt, V);
+    if constexpr (AHEAD) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) wt[e] = pn[e];
+    } else {
+      ld_f32(a.next_weight + c0, wt, V);
+    }
 #pragma unroll
     for (int e = 0; e < V; ++e) y[ch][e] *= r2 * wt[e];
     st_vec(reinterpret_cast<T*>(a.h) + row * a.N + c0, y[ch]);
@@ -254,7 +335,7 @@ __global__ void __launch_bounds__(256) carve_block_norm_bwd_kernel(BlockNormArgs
 #pragma unroll
         for (int e = 0; e < V; ++e) sg[ch][e] = sigmoid_x(z[ch][e]);
     float r1[NCH];
-    group_rstd<T, NT, NCH>(y, r1, a, red[turn]);
+    group_norm<T, NT, NCH>(y, r1, a, red[turn]);
     // through the next block's norm
     if (a.next_weight) {
       float ss = 0.0f, mx = 0.0f;
@@ -268,7 +349,7 @@ __global__ void __launch_bounds__(256) carve_block_norm_bwd_kernel(BlockNormArgs
         next_weight(ch, wn);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          float t = y[ch][e] * r1[ch] * wt[e];
+          float t = y[ch][e] * wt[e];
           if (a.gate) t *= a.act == CARVE_GATE_SILU ? z[ch][e] * sg[ch][e] : sg[ch][e];
           t *= sc[e];
           x[ch][e] = a.residual ? a.alpha * x[ch][e] + t : t;
@@ -277,7 +358,29 @@ __global__ void __launch_bounds__(256) carve_block_norm_bwd_kernel(BlockNormArgs
         }
       }
       row_sums<NT>(ss, mx, red[turn] + 8);
-      const float r2 = 1.0f / sqrtf(ss * invN + a.eps), m2 = r2 * r2 * (mx * invN);
+      const float mean_eps = ss * invN + a.eps;
+      float r2 = 1.0f / sqrtf(mean_eps), r2f = r2;
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(other_unit(mean_eps)) != 0, 0)) {   // (uniform)
+        const float f = pow2(unit_of(mean_eps));
+        ss = mx = 0.0f;
+#pragma unroll
+        for (int ch = 0; ch < NCH; ++ch) {
+          if ((ch * NT + tid) * V >= a.N) continue;
+          float wn[V];
+          next_weight(ch, wn);
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            x[ch][e] *= f;
+            ss += x[ch][e] * x[ch][e];
+            mx += dh[ch][e] * wn[e] * x[ch][e];
+          }
+        }
+        if (NT > 64) __syncthreads();   // (the first sums are read)
+        row_sums<NT>(ss, mx, red[turn] + 8);
+        r2 = 1.0f / sqrtf(ss * invN + a.eps * f * f);
+        r2f = r2 * f;
+      }
+      const float m2 = r2 * r2 * (mx * invN);
 #pragma unroll
       for (int ch = 0; ch < NCH; ++ch) {
         const int c0 = (ch * NT + tid) * V;
@@ -286,7 +389,7 @@ __global__ void __launch_bounds__(256) carve_block_norm_bwd_kernel(BlockNormArgs
         next_weight(ch, wn);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          dX[ch][e] += r2 * (dh[ch][e] * wn[e] - x[ch][e] * m2);
+          dX[ch][e] += r2f * (dh[ch][e] * wn[e] - x[ch][e] * m2);
           an[ch][e] += dh[ch][e] * (x[ch][e] * r2);
         }
       }
@@ -308,7 +411,7 @@ __global__ void __launch_bounds__(256) carve_block_norm_bwd_kernel(BlockNormArgs
       scale(ch, sc);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        const float yh = y[ch][e] * r1[ch], nv = yh * wt[e];
+        const float yh = y[ch][e], nv = yh * wt[e];
         float act = 1.0f, slope = 0.0f;
         if (a.gate) {
           const float s = sg[ch][e];
@@ -341,7 +444,7 @@ __global__ void __launch_bounds__(256) carve_block_norm_bwd_kernel(BlockNormArgs
       const int c0 = (ch * NT + tid) * V;
       if (c0 >= a.N) continue;
 #pragma unroll
-      for (int e = 0; e < V; ++e) dX[ch][e] = r1[ch] * (dX[ch][e] - y[ch][e] * r1[ch] * dot[ch]);
+      for (int e = 0; e < V; ++e) dX[ch][e] = r1[ch] * (dX[ch][e] - y[ch][e] * dot[ch]);
       st_vec(reinterpret_cast<T*>(a.dy) + row * a.N + c0, dX[ch]);
     }
   }
