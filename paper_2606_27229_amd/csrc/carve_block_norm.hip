@@ -180,8 +180,8 @@ __global__ void __launch_bounds__(256, NCH <= 2 ? 6 : 3) carve_block_norm_fwd_ke
       if (a.residual) ld_vec(rp + c0, rs[ch]);
     }
   }
-  // (with up to eight columns a thread the parameters are on their way before the sums)
-  constexpr bool AHEAD = NCH * V <= 8;
+  // (with one chunk a thread the parameters are on their way before the sums)
+  constexpr bool AHEAD = NCH == 1;
   float pw[V], ps[V], pn[V];
   if (AHEAD && tid * V < a.N) {
     ld_f32(a.weight + tid * V, pw, V);
