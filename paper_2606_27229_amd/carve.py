@@ -484,7 +484,11 @@ def rmsnorm_bwd_noalloc(o, weight, dy, d_o, dweight, *, eps=RMSNORM_EPS, stream=
 
 def _same_device(device, **tensors):
     for name, t in tensors.items():
-        if t is not None and t.device != device:
+        if t is None:
+            continue
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name} must be a GPU tensor")
+        if t.device != device:
             raise ValueError(f"{name} is on {t.device}, expected {device}")
 
 
