@@ -314,6 +314,9 @@ int carve_rmsnorm_bwd_noalloc(const carve_dims_t* d, const void* o, const float*
  *     through the matrix cores as sums of bf16 values, three towards f32 outputs
  *     (states, dg: f32 accuracy) and two towards bf16 outputs; with f32 tokens
  *     all products are f32.
+ *   - No output may overlap an input, another output or the workspace
+ *     (CARVE_ERR_UNSUPPORTED): S_T is not written over S0.  Only the pool of
+ *     carve_gdr_step is updated in place.
  */
 typedef struct {
   int B, T;            /* dense: B sequences of T tokens; packed: B = 1, T rows */
@@ -355,7 +358,7 @@ int carve_gdr_chunk_bwd(const carve_gdr_dims_t* d, const void* q, const void* k,
 /* T tokens for each of B sequences (d->N = 0), token by token in f32: state is a
  * pool of `pool` states [pool, Hv, Dv, Dk] f32, updated in place; sequence b's
  * state is state[slots[b]] (slots: [B] device ints), or state[b] with slots NULL
- * (then pool >= B).  A sequence whose slot is outside [0, pool) is a padding
+ * (then pool >= B).  The state left is that behind the last of the T tokens.  A sequence whose slot is outside [0, pool) is a padding
  * entry: its state and its rows of o are left as they were.  Two sequences of one
  * call may not have the same slot (their results are then unspecified).  B is at
  * most 65535.  One launch, no workspace. */
@@ -379,7 +382,8 @@ int carve_gdr_step(const carve_gdr_dims_t* d, const void* q, const void* k, cons
  * elements, >= 0, 16-byte aligned), every other tensor is dense.
  * Supported: N a multiple of 8 (bf16) or 4 (f32), at most 8192; with groups > 1,
  * N / groups must be 16 bytes times a power of two up to 64; eps finite and >= 0,
- * alpha finite. */
+ * alpha finite.  No output may overlap an input, another output or the workspace
+ * (CARVE_ERR_UNSUPPORTED): x is not written over residual. */
 enum { CARVE_GATE_SILU = 1, CARVE_GATE_SIGMOID = 2 };
 typedef struct {
   long long rows;

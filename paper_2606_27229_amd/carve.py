@@ -671,9 +671,11 @@ def gdr_chunk_bwd(q, k, v, g, beta, S_chunks, dO, dS_T=None, *, scale=None, offs
 
 
 def gdr_step(q, k, v, g, beta, state, slots=None, *, scale=None, out=None, stream=None):
-    """The gated delta rule token by token, for decoding: T tokens (one, or a few
-    drafted ones) for each of B sequences, whose states in the pool ``state``
-    [pool,Hv,Dv,Dk] f32 are updated in place.  Sequence b's state is
+    """The gated delta rule token by token, for decoding: T tokens (one, or several
+    at once) for each of B sequences, whose states in the pool ``state``
+    [pool,Hv,Dv,Dk] f32 are updated in place.  The state left is that behind the last
+    token: to keep only some of T proposed ones, copy the states before the call
+    (``state[slots]``), put them back and run the kept tokens again.  Sequence b's state is
     state[slots[b]] (int32 [B]), or state[b] without slots.  A slot outside the
     pool (-1) marks a padding entry, whose output rows are left as they were.  No
     slot may appear twice.  The other arguments are those of ``gdr_chunk_fwd``.
