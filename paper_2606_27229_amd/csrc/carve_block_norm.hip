@@ -10,12 +10,18 @@
 //   dy = r1 (dn weight - y r1 mean_group(dn weight y r1))
 //   dweight = sum dn y r1,  dscale = sum dX t,  dnext_weight = sum dh x r2
 //
-// Bound by HBM: every row tensor is read once and written once (16384 rows of 2048 in
-// bf16, everything given: forward 335 MB in 70 us, 4.8 TB/s; backward 537 MB in 127 us,
-// 4.2 TB/s, and 9 us for the parameters; norm and gate alone in 16 groups: 46 and 82 us
-// for 201 and 336 MB).  NT threads (one
-// wave, or four) hold a row in registers, NCH 16-byte chunks each; sums run over a
-// group's lanes by DPP and over the waves through LDS.  Statistics, x and the
+// Every row tensor is read once and written once.  16384 rows of 2048 in bf16, everything
+// given: forward 335 MB in 71 us, 4.7 TB/s, bound by HBM and to a lesser part by its vector
+// instructions (f32 rows of as many bytes, half as many values: 65 us; rows of 256 in bf16,
+// which leave half of a wave idle, 97 us, in f32 61); backward with the parameters' sums 537
+// MB in 129 us, 4.2 TB/s.  Norm and gate alone in 16 groups: 43 and 85 us for 201 and 336
+// MB.  Of the same size, 4096 columns: 75 and 150 us; 8192: 93 and 238 us, where the
+// registers of a row leave three waves a SIMD forward and one backward, which has no row
+// loaded ahead beyond eight columns a thread; in f32, 2048, 4096 and 8192 columns: 65, 70,
+// 79 and 117, 133, 198 us.
+//
+// NT threads (one wave, or four) hold a row in registers, NCH 16-byte chunks each; sums
+// run over a group's lanes by DPP and over the waves through LDS.  Statistics, x and the
 // gradients are f32 until they are stored; h comes from the unrounded x, and so
 // does the backward, which forms x again instead of reading the rounded one.
 #include "carve_kernels.h"

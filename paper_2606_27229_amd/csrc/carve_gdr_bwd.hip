@@ -241,8 +241,8 @@ __global__ void __launch_bounds__(128 * NW, 1) carve_gdr_bchain_kernel(GdrArgs a
 // Barriers (1) and, without LDS for z and Y of two chunks in turn, (2) as above; the chain
 // waves of a tile meet by flags: (3)
 // the halves of K dS^T are there; (4) the parts of dR.  Bound by the chunks following each
-// other, 4.6 us each at 128 keys and values in bf16, where the 400 MB that go out (64
-// sequences and heads of 64 chunks: 295 us) alone take 80 us; one chain wave: 372 us.
+// other, 4.7 us each at 128 keys and values in bf16, where the 400 MB that go out (64
+// sequences and heads of 64 chunks: 300 us) alone take 80 us; one chain wave: 372 us.
 template <typename T, int DK, int NW>   // NW: tiles
 struct BPairLds {
   typedef GdrRows<T, DK> KR;
@@ -517,11 +517,15 @@ __global__ void __launch_bounds__(256 * NW, 1) carve_gdr_bpair_kernel(GdrArgs a)
 // so that dR S itself only reaches dk and is taken in two.
 // LDS: U and dR in three pieces fill 96 KB at 128 columns, so the rest shares places:
 // the values lie where U goes, the queries where T was.
-// 4096 chunks and heads of 128 keys and values in bf16: 470 us for 1.1 GB, 2.3 TB/s.  Bound
+// 4096 chunks and heads of 128 keys and values in bf16: 475 us for 1.5 GB, 3.2 TB/s.  Bound
 // by one workgroup a compute unit (158 KB): its loads, its LDS reads (three pieces an
-// operand) and its matrix products do not overlap beyond what two waves a SIMD give.  Taken
-// from memory without LDS, the token rows alone cost 63 cycles a load instruction, and the
-// kernel 5.4 ms.
+// operand) and its matrix products do not overlap beyond what two waves a SIMD give (vector
+// units 38 %, matrix cores 17 % of the cycles).  0.4 GB of the traffic are registers that do
+// not fit, 21 a lane here, 17 to 91 at 128 keys: dQ and dK live across the loop over the
+// value heads.  With narrower keys none spill.  One workgroup a chunk and key head takes its
+// value heads one after another, so a call takes whole turns of 256 such workgroups (5
+// documents of 8191 tokens with 4 key heads: 528 of them, a third turn for 16).  Taken from
+// memory without LDS, the token rows made it 5.4 ms.
 
 // [VB columns][64 tokens] of an f32 intermediate in LDS
 template <typename T, int VB>

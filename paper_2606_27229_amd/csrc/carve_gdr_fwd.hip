@@ -17,8 +17,8 @@ namespace {
 // A (below the diagonal) and T (transposed, above it) share 17 KB of LDS, where the rows
 // were before.  The rows come through LDS because each wave needs most of them: loaded by
 // every wave for itself, 16 rows at a time, they made it 86 us at 4096 chunks of 128 keys
-// (bf16; 270 MB in and out), where it takes 56 us now; the backward form, which writes
-// two more images, 70 us.
+// (bf16; 270 MB in and out), where it takes 57 us now; the backward form, which writes
+// two more images, 72 us.
 // G is summed in 64 bits and kept as two floats, so that a decay between two tokens
 // keeps its digits however strongly the tokens before them decay.
 template <typename T, int DK>
@@ -410,9 +410,12 @@ __global__ void __launch_bounds__(128 * kChainNW, 1) carve_gdr_chain_kernel(GdrA
 
 // ---------------------------------------------------------------------------------
 // The same chain with two waves a tile on it and two helpers (keys of 64 and 128): a call
-// waits for each chunk's chain, and a wave issues an instruction every 7 to 8 cycles on
-// its own, so that the number of instructions between chunk and chunk is what takes the
-// time.  Chain wave h keeps the state of the keys' half h.  K S^T
+// waits for each chunk's chain, 500 to 600 instructions of a chain wave (128 keys, bf16)
+// that depend on each other in long rows: 5200 cycles a chunk with a tile a workgroup, 6600
+// with two, where the vector units issue in 14 and 37 % of them.  (With a tile a workgroup
+// some 90 of the instructions move accumulators between the register files: launch bounds
+// of one wave a SIMD leave the compiler that choice.)  Chain wave h keeps the state of the
+// keys' half h.  K S^T
 // is the sum of both halves' products; each wave finishes two token tiles of it, makes
 // their R and multiplies by T's columns of these tokens; both then add up U and update
 // their half of the state.  Helper wave h takes the outputs of two token tiles.
@@ -420,10 +423,10 @@ __global__ void __launch_bounds__(128 * kChainNW, 1) carve_gdr_chain_kernel(GdrA
 // taken one before the chain writes it again behind the next (1), and (2) is not needed (one
 // sequence of 256 chunks of 16 heads 588 -> 562 us).  The chain waves of a tile meet twice more,
 // by flags in LDS: (3) the halves of K S^T are there; (4) the parts of U.  With barriers
-// for these too the helpers, whose memory instructions wait for each other (some 45 cycles
-// a KB), held the chain up: 214 us for 64 sequences and heads of 64 chunks (128 keys, 128
-// values, bf16), where it takes 190 us now, 3.0 us a chunk (240 us with the states at chunk
-// starts written out: 268 MB).  One chain wave a tile with four tiles in a workgroup, which
+// for these too the helpers, whose memory instructions wait for each other, held the chain
+// up: 214 us for 64 sequences and heads of 64 chunks (128 keys, 128 values, bf16), where it
+// takes 180 us now, 2.8 us a chunk (230 us with the states at chunk starts written out:
+// 268 MB).  One chain wave a tile with four tiles in a workgroup, which
 // fits more tiles on the card, loses also where there are many: 8 x 1024 tokens of 32 heads
 // (2048 tiles) 318 us, this 239 us.
 template <typename T, int DK, int NW>   // NW: tiles
@@ -584,7 +587,7 @@ __global__ void __launch_bounds__(256 * NW, 1) carve_gdr_pair_kernel(GdrArgs a) 
     float gam[2];
   };
   // queries go through LDS like the keys: a wave that loads 16 rows' pieces of 8 bytes
-  // itself takes as long as all else together (63 cycles an instruction)
+  // itself takes as long as all else together (64 heads of 64 chunks 252 us, this 214)
   const auto load_q = [&](int ch) {
     if constexpr (L::q_lds) {
       const int t0 = ch * kGdrC, len = min(kGdrC, sq.len - t0);

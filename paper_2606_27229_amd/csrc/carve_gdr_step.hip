@@ -5,8 +5,10 @@
 //   S_new q = e^g (S q) + u (k.q),  S k before the write = e^g (S k).
 //
 // Bound by HBM: every state is read and written once a call, whatever T (64 states of
-// 32 heads of 128 x 128 and their tokens, 270 MB: 56 us, 4.8 TB/s; one state of 16 heads:
-// 8.3 us with the call, which is the launch and its arguments).  A row of
+// 32 heads of 128 x 128 and their tokens, 270 MB: 56 us, 4.8 TB/s; 43 us on the states of the
+// call before, which the last-level cache still holds).  One state of 16 heads takes 4.3 us,
+// 8.3 with the call.  A token's rows are loaded when the token before it is done, so that
+// several tokens wait for memory in turn (24 x 4 tokens of 8 f32 heads of 64: 6.3 us).  A row of
 // S (Dk floats) is spread over Dk / 8 lanes, two 16-byte loads each, so that a wave
 // load covers whole rows; a lane holds kStepRows rows, 8 loads in flight; a row's two
 // sums run over its lanes by DPP.

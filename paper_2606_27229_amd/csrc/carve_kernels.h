@@ -494,7 +494,10 @@ int launch_rmsnorm_bwd(const void* x, const float* wt, const void* dy, void* dx,
 
 // The norms around a block (carve_block_norm.hip): rows of N values.  The backward's
 // workgroups (at most kBlockNormGroups) each write three f32 partial rows, summed in
-// order by a second launch; mark is called after each.
+// order by a second launch; mark is called after each.  Backward of 33.5 M bf16 values with
+// 512 / 768 / 1024 / 1536 of them, us: rows of 256 195 / 177 / 181 / 174, of 512 113 / 117 /
+// 130 / 122, of 2048 114 / 117 / 129 / 126, of 4096 143 / 155 / 150 / 158, of 8192 215 / 225 /
+// 237 / 259; 16.8 M f32 ones, rows of 2048 113 / 122 / 116 / 123.
 constexpr int kBlockNormGroups = 1024;
 constexpr int kBlockNormMaxN = 8192;
 struct BlockNormArgs {
