@@ -414,9 +414,158 @@ int carve_block_norm_bwd(const carve_block_norm_dims_t* d, const void* y, const 
                          const void* dh, void* dy, void* dgate, void* dresidual, float* dweight, float* dscale,
                          float* dnext_weight, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
+/* ---- the short causal convolution -------------------------------------------------
+ *
+ * Every channel over its last W inputs, as it stands before a recurrent layer's
+ * queries, keys and values:
+ *     p_t = bias + sum_j weight[c][j] x_{t-W+1+j},   y_t = act(p_t)
+ *   - x [B, T, C] with strides of batch and token (in elements, >= 0, 16-byte
+ *     aligned; channels are contiguous), so that it may be a slice of a fused
+ *     projection; y, dy, dx [B, T, C] dense; weight [C, W], bias [C] f32.
+ *   - x0, x_T [sequences, W - 1, C] (token dtype): the inputs before a sequence's first
+ *     row, oldest first (NULL: zeros), and its last W - 1 inputs, those of x0 among them
+ *     where it is shorter.
+ *   - Packed sequences (N > 0, B = 1, offsets) as for the gated delta rule: rows of no
+ *     sequence are left as they were; offsets outside the contract stay within the
+ *     tensors, with unspecified results.
+ *   - Supported: W in {2, 3, 4}; C a multiple of 8 (bf16) or 4 (f32), below 2^20.
+ *   - NaN and infinities reach the W outputs that read them.  No output may overlap an
+ *     input, another output or the workspace (CARVE_ERR_UNSUPPORTED); only the step's
+ *     pool is updated in place. */
+enum { CARVE_CONV_LINEAR = 0, CARVE_CONV_SILU = 1 };
+typedef struct {
+  int B, T, N;         /* as in carve_gdr_dims_t */
+  int C, W;
+  carve_dtype_t dtype;
+  int activation;      /* CARVE_CONV_* */
+  long long x_batch, x_token;
+} carve_short_conv_dims_t;
+
+/* bias, x0, x_T may be NULL.  One launch. */
+int carve_short_conv_fwd(const carve_short_conv_dims_t* d, const void* x, const float* weight, const float* bias,
+                         const void* x0, const int* offsets, void* y, void* x_T, hipStream_t stream);
+
+/* Bytes of device workspace of carve_short_conv_bwd; 0 for invalid dims. */
+size_t carve_short_conv_workspace_size(const carve_short_conv_dims_t* d);
+
+/* Backward for loss <dy, y> + <dx_T, x_T> (dx_T may be NULL: zeros).  Out: dx, dx0 (token
+ * dtype; dx0 may be NULL), dweight [C, W] f32, dbias [C] f32 (exactly where bias is
+ * given), summed over the rows in a fixed order: reruns are bitwise identical.  Two
+ * launches. */
+int carve_short_conv_bwd(const carve_short_conv_dims_t* d, const void* x, const float* weight, const float* bias,
+                         const void* x0, const int* offsets, const void* dy, const void* dx_T, void* dx,
+                         float* dweight, float* dbias, void* dx0, void* workspace, size_t workspace_bytes,
+                         hipStream_t stream);
+
+/* T tokens for each of B sequences (d->N = 0) on the inputs kept in a pool [pool, W - 1,
+ * C] (token dtype), updated in place; slots as in carve_gdr_step.  B is at most 65535.
+ * One launch. */
+int carve_short_conv_step(const carve_short_conv_dims_t* d, const void* x, const float* weight, const float* bias,
+                          const int* slots, int pool, void* state, void* y, hipStream_t stream);
+
+/* ---- rotary positions ----------------------------------------------------------------
+ *
+ * The pairs (a, b) of the first `rot` values of every head of q [B, T, Hq, D] and k
+ * [B, T, Hk, D] become
+ *     m (a cos(z) - b sin(z)),  m (b cos(z) + a sin(z)),    z = position * freq[i]
+ * i the pair's number: values i and i + rot / 2, or (interleaved) 2 i and 2 i + 1.  The
+ * values behind `rot` are kept.  freq: [rot / 2] f64; m: amplitude.  Stretched contexts
+ * are a matter of freq and m alone.  Angles are formed in 64 bits.
+ *   - A row's position is positions[b][t]; with positions NULL, start[sequence] (or 0)
+ *     plus its row in the sequence (batch element, or packed sequence of offsets).  With
+ *     positions given, start and offsets must be NULL and N 0.
+ *   - All strides are in elements, >= 0 and multiples of 16 bytes.  q_out and k_out are
+ *     other memory than q and k, or (both) q and k themselves with the same strides; they
+ *     may be slices of one tensor's rows, and every element has a place of its own.  Rows
+ *     of no sequence are left as they were.  k and k_out may be NULL (then Hk = 0).
+ *   - backward: turned the other way, which takes dq, dk to the gradients of q, k.
+ *   - Supported: D a multiple of 8 (bf16) or 4 (f32), at most 1024; rot a positive
+ *     multiple of 16 (bf16) or 8 (f32), at most D; Hq + Hk at most 65535. */
+typedef struct {
+  int B, T, N;         /* as in carve_gdr_dims_t */
+  int Hq, Hk, D, rot;
+  carve_dtype_t dtype;
+  int interleaved;
+  float amplitude;     /* finite */
+  long long q_batch, q_token, q_head, k_batch, k_token, k_head;
+  long long qo_batch, qo_token, qo_head, ko_batch, ko_token, ko_head;
+} carve_rotary_dims_t;
+
+/* One launch. */
+int carve_rotary(const carve_rotary_dims_t* d, const void* q, const void* k, const double* freq, const int* positions,
+                 const int* start, const int* offsets, int backward, void* q_out, void* k_out, hipStream_t stream);
+
+/* ---- the selective state space scan -----------------------------------------------------
+ *
+ * Per sequence and head, with a state S in R^{P x S} (f32; S: state size), group
+ * head / (H / G) of B and C:
+ *     d_t = softplus(dt_t + dt_bias)     (softplus = 0: d_t = dt_t + dt_bias, >= 0)
+ *     S_t = e^{d_t A} S_{t-1} + d_t x_t B_t^T,   y_t = S_t C_t + D x_t
+ * with A <= 0, D, dt_bias one value a head.  carve_ssm_chunk_fwd and carve_ssm_chunk_bwd
+ * evaluate it in chunks of 64 tokens (any T), carve_ssm_step token by token.
+ *
+ *   - x [B, T, H, P], Bm, Cm [B, T, G, S], dt [B, T, H] (token dtype) with the strides of
+ *     carve_ssm_dims_t (in elements, >= 0; last dimensions contiguous; those of x, Bm and
+ *     Cm multiples of 16 bytes, a token's less than 16 MB), so that they may be slices of
+ *     what a projection or convolution left.  y, dy and every gradient are dense.
+ *     A, D, dt_bias [H] f32 (D, dt_bias may be NULL: 0).
+ *   - S0, S_T, dS_T, dS0 [sequences, H, P, S] f32; packed sequences (N > 0, offsets) as
+ *     for the gated delta rule.
+ *   - S_chunks: [carve_ssm_chunk_count(d), H, P, S] of 4 bytes each, written by
+ *     carve_ssm_chunk_fwd for carve_ssm_chunk_bwd, in a form of their own.
+ *   - Supported: S in {32, 64, 128}; P a multiple of 32, at most 256; H a multiple of G,
+ *     at most 65535; dtype f32 or bf16.  Chunk count, and spans * H * P / 32 rounded up
+ *     to eights, below 2^23 (a span is four chunks or more; sequences are at most
+ *     twice the rest).
+ *   - A decay of -inf (a reset) is taken as e^-10000; NaN and infinities propagate within
+ *     their sequence, also to tokens before them in the same chunk.  Precision as for the
+ *     gated delta rule: f32 outputs to f32 accuracy.
+ *   - No output may overlap an input, another output or the workspace
+ *     (CARVE_ERR_UNSUPPORTED); only the step's pool is updated in place. */
+typedef struct {
+  int B, T, N;         /* as in carve_gdr_dims_t */
+  int G, H, P, S;
+  carve_dtype_t dtype;
+  int softplus;
+  long long x_batch, x_token, x_head;
+  long long b_batch, b_token, b_group, c_batch, c_token, c_group;
+  long long dt_batch, dt_token;
+} carve_ssm_dims_t;
+
+/* Chunks that S_chunks has room for; 0 for invalid dims. */
+size_t carve_ssm_chunk_count(const carve_ssm_dims_t* d);
+
+/* Bytes of device workspace of carve_ssm_chunk_fwd (for_backward = 0; may be none) and
+ * carve_ssm_chunk_bwd (1); 0 for invalid dims.  Nothing in it is kept between calls. */
+size_t carve_ssm_workspace_size(const carve_ssm_dims_t* d, int for_backward);
+
+/* Forward.  S0, S_T, S_chunks may be NULL.  One launch, or three where long sequences are
+ * cut into spans. */
+int carve_ssm_chunk_fwd(const carve_ssm_dims_t* d, const void* x, const void* dt, const float* A, const void* Bm,
+                        const void* Cm, const float* D, const float* dt_bias, const float* S0, const int* offsets,
+                        void* y, float* S_T, float* S_chunks, void* workspace, size_t workspace_bytes,
+                        hipStream_t stream);
+
+/* Backward for loss <dy, y> + <dS_T, S_T> (dS_T may be NULL: zeros).  Out: dx [B,T,H,P], ddt
+ * [B,T,H], dBm, dCm [B,T,G,S] (token dtype), dA [H] f32, dD and ddt_bias [H] f32 (exactly
+ * where D and dt_bias are given), dS0 or NULL.  All sums are in a fixed order: reruns are
+ * bitwise identical.  Three to six launches. */
+int carve_ssm_chunk_bwd(const carve_ssm_dims_t* d, const void* x, const void* dt, const float* A, const void* Bm,
+                        const void* Cm, const float* D, const float* dt_bias, const float* S_chunks, const int* offsets,
+                        const void* dy, const float* dS_T, void* dx, void* ddt, float* dA, void* dBm, void* dCm,
+                        float* dD, float* ddt_bias, float* dS0, void* workspace, size_t workspace_bytes,
+                        hipStream_t stream);
+
+/* T tokens for each of B sequences (d->N = 0), token by token in f32, on a pool of states
+ * [pool, H, P, S] f32 updated in place; slots as in carve_gdr_step.  B is at most 65535.
+ * One launch, no workspace. */
+int carve_ssm_step(const carve_ssm_dims_t* d, const void* x, const void* dt, const float* A, const void* Bm,
+                   const void* Cm, const float* D, const float* dt_bias, const int* slots, int pool, float* state,
+                   void* y, hipStream_t stream);
+
 /* Measurement hook (not part of the computation).  Arms the next
- * carve_chunk_*, carve_rmsnorm_*, carve_gdr_* or carve_block_norm_* call made
- * on the calling thread to record events[0] on its stream before its first kernel launch and events[i] after
+ * carve_chunk_*, carve_rmsnorm_*, carve_gdr_*, carve_block_norm_*,
+ * carve_short_conv_*, carve_rotary or carve_ssm_* call made on the calling thread to record events[0] on its stream before its first kernel launch and events[i] after
  * its i-th launch (the forward makes 1 launch; the backward 4: clear of the
  * chunk ready flags, chunk recompute fused with the adjoint, the partials of
  * d[Ub;Uw] and dVb/dVw, their fixed-order reductions; the gated backward
@@ -424,7 +573,8 @@ int carve_block_norm_bwd(const carve_block_norm_dims_t* d, const void* y, const 
  * input activations a 5th, the activation gradient of dq, dk; the norm's
  * forward 1, its backward 2; the gated delta rule's forward 2, chunk triangles
  * and chain, its backward 3, triangles, chain and gradients, its step 1; the
- * block norm's forward 1, its backward 2),
+ * block norm's forward 1, its backward 2; the short convolution's forward and step 1,
+ * its backward 2; rotary positions 1; the state space scan's as stated there),
  * up to `capacity` events.  `events` are hipEvent_t handles created by the
  * caller (hipEventCreate) and owned by the caller; the handles are copied
  * here (the array may be freed after this call) and the events are only

@@ -21,7 +21,9 @@ SOURCES = [("carve_abi.hip", "carve_abi", []), ("carve_fwd_chain.hip", "carve_fw
            ("carve_bwd.hip", "carve_bwd", []), ("carve_norm.hip", "carve_norm", []),
            ("carve_gdr_fwd.hip", "carve_gdr_fwd", []), ("carve_gdr_bwd.hip", "carve_gdr_bwd", []),
            ("carve_gdr_step.hip", "carve_gdr_step", []),
-           ("carve_block_norm.hip", "carve_block_norm", [])] + [
+           ("carve_block_norm.hip", "carve_block_norm", []), ("carve_short_conv.hip", "carve_short_conv", []),
+           ("carve_rotary.hip", "carve_rotary", []), ("carve_ssm_fwd.hip", "carve_ssm_fwd", []),
+           ("carve_ssm_bwd.hip", "carve_ssm_bwd", []), ("carve_ssm_step.hip", "carve_ssm_step", [])] + [
     ("carve_variant.hip", f"carve_variant{v}", [f"-DCARVE_VARIANT={v}"]) for v in range(5)]
 
 BUILD = os.path.join(HERE, "_build")

@@ -25,7 +25,9 @@ SYMBOLS = ("carve_chunk_fwd", "carve_chunk_bwd", "carve_chunk_fwd_gated", "carve
            "carve_set_ready_wait_limit",
            "carve_gdr_chunk_fwd", "carve_gdr_chunk_bwd", "carve_gdr_step", "carve_gdr_chunk_count",
            "carve_gdr_workspace_size", "carve_block_norm_fwd", "carve_block_norm_bwd",
-           "carve_block_norm_workspace_size")
+           "carve_block_norm_workspace_size", "carve_short_conv_fwd", "carve_short_conv_bwd", "carve_short_conv_step",
+           "carve_short_conv_workspace_size", "carve_rotary", "carve_ssm_chunk_fwd", "carve_ssm_chunk_bwd",
+           "carve_ssm_step", "carve_ssm_chunk_count", "carve_ssm_workspace_size")
 
 
 class Dims(ctypes.Structure):
@@ -44,6 +46,23 @@ class BlockNormDims(ctypes.Structure):
     _fields_ = ([("rows", ctypes.c_longlong)] + [(n, ctypes.c_int) for n in ("N", "groups", "dtype", "gate_act")]
                 + [("eps", ctypes.c_float), ("alpha", ctypes.c_float)]
                 + [(n, ctypes.c_longlong) for n in ("y_stride", "gate_stride", "residual_stride")])
+
+
+class ShortConvDims(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int) for n in ("B", "T", "N", "C", "W", "dtype", "activation")]
+                + [(n, ctypes.c_longlong) for n in ("x_batch", "x_token")])
+
+
+class RotaryDims(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int) for n in ("B", "T", "N", "Hq", "Hk", "D", "rot", "dtype", "interleaved")]
+                + [("amplitude", ctypes.c_float)]
+                + [(t + n, ctypes.c_longlong) for t in ("q_", "k_", "qo_", "ko_") for n in ("batch", "token", "head")])
+
+
+class SsmDims(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int) for n in ("B", "T", "N", "G", "H", "P", "S", "dtype", "softplus")]
+                + [(n, ctypes.c_longlong) for n in ("x_batch", "x_token", "x_head", "b_batch", "b_token", "b_group",
+                                                    "c_batch", "c_token", "c_group", "dt_batch", "dt_token")])
 
 
 class CarveError(RuntimeError):
@@ -118,6 +137,22 @@ def load_library(path: str = LIB_PATH):
     lib.carve_block_norm_workspace_size.restype = sz
     lib.carve_block_norm_bwd.argtypes = [N] + [vp] * 15 + [sz, vp]
     lib.carve_block_norm_bwd.restype = ctypes.c_int
+    V, R, S = ctypes.POINTER(ShortConvDims), ctypes.POINTER(RotaryDims), ctypes.POINTER(SsmDims)
+    lib.carve_short_conv_fwd.argtypes = [V] + [vp] * 8
+    lib.carve_short_conv_bwd.argtypes = [V] + [vp] * 12 + [sz, vp]
+    lib.carve_short_conv_step.argtypes = [V] + [vp] * 4 + [ctypes.c_int] + [vp] * 3
+    lib.carve_short_conv_workspace_size.argtypes = [V]
+    lib.carve_short_conv_workspace_size.restype = sz
+    lib.carve_rotary.argtypes = [R] + [vp] * 6 + [ctypes.c_int] + [vp] * 3
+    lib.carve_ssm_chunk_count.argtypes = [S]
+    lib.carve_ssm_chunk_count.restype = sz
+    lib.carve_ssm_workspace_size.argtypes = [S, ctypes.c_int]
+    lib.carve_ssm_workspace_size.restype = sz
+    lib.carve_ssm_chunk_fwd.argtypes = [S] + [vp] * 13 + [sz, vp]
+    lib.carve_ssm_chunk_bwd.argtypes = [S] + [vp] * 20 + [sz, vp]
+    lib.carve_ssm_step.argtypes = [S] + [vp] * 8 + [ctypes.c_int] + [vp] * 3
+    for name in ("short_conv_fwd", "short_conv_bwd", "short_conv_step", "rotary", "ssm_chunk_fwd", "ssm_chunk_bwd", "ssm_step"):
+        getattr(lib, "carve_" + name).restype = ctypes.c_int
     if path == LIB_PATH:
         _lib = lib
     return lib
@@ -820,3 +855,389 @@ def block_norm_bwd(y, weight, dx, dh=None, *, groups=1, gate=None, gate_act="sil
 
     _check("carve_block_norm_bwd", _on_stream(call, dev, stream))
     return res
+
+
+# ---- the short causal convolution, rotary positions and the selective state space scan --
+
+
+def _pointer(t):
+    return None if t is None else t.data_ptr()
+
+
+def _gpu(t, name, dims, dtype=None, device=None):
+    """Checks a required tensor by its number of dimensions, type and device."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a GPU tensor")
+    if t.dim() != dims:
+        raise ValueError(f"{name} has {t.dim()} dimensions, expected {dims}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+
+
+def _tokens(t, name):
+    if t.dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"{name} must be bfloat16 or float32, got {t.dtype}")
+    return CARVE_BF16 if t.dtype == torch.bfloat16 else CARVE_F32
+
+
+def _last(t, name):
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must be contiguous in its last dimension")
+
+
+def _count(offsets, B):
+    """Sequences, and the N of the C dims."""
+    if offsets is None:
+        return B, 0
+    if not isinstance(offsets, torch.Tensor):
+        raise TypeError("offsets must be a GPU tensor")
+    if offsets.dim() != 1 or offsets.numel() < 2:
+        raise ValueError("offsets must be one-dimensional, the number of sequences and one")
+    return offsets.numel() - 1, offsets.numel() - 1
+
+
+def _steps(t, dims):
+    # (a dimension of one element may have any stride; none is taken)
+    return [t.stride(i) if t.shape[i] > 1 else 0 for i in range(dims)]
+
+
+CONV_ACTS = {None: 0, "silu": 1}
+
+
+def _conv_key(kind, x, weight, bias, past, offsets, activation):
+    """The key of a call with these layouts, or None where something is no tensor."""
+    try:
+        return (kind, activation, _layout(x), _layout(weight), _layout(bias), _layout(past), _layout(offsets))
+    except (AttributeError, TypeError):
+        return None
+
+
+def _conv_check(x, weight, bias, past, offsets, activation, past_name, pool=None):
+    """Checks what every entry point takes; (reference to the C dims, sequences, workspace bytes)."""
+    _gpu(x, "x", 3)
+    dt = _tokens(x, "x")
+    _last(x, "x")
+    B, T, C = x.shape
+    _gpu(weight, "weight", 2, torch.float32, x.device)
+    W = weight.shape[1]
+    _ptr(weight, "weight", torch.float32, (C, W))
+    _same_device(x.device, bias=bias, offsets=offsets, **{past_name: past})
+    _ptr(bias, "bias", torch.float32, (C,))
+    _ptr(offsets, "offsets", torch.int32)
+    if activation not in CONV_ACTS:
+        raise ValueError(f"activation must be None or 'silu', got {activation!r}")
+    seqs, N = _count(offsets, B)
+    _ptr(past, past_name, x.dtype, (seqs if pool is None else pool, W - 1, C))
+    d = ShortConvDims(B, T, N, C, W, dt, CONV_ACTS[activation], *_steps(x, 2))
+    r = ctypes.byref(d)
+    return r, seqs, int(load_library().carve_short_conv_workspace_size(r))
+
+
+def short_conv_fwd(x, weight, x0=None, *, bias=None, activation="silu", offsets=None, want_state=True, out=None, stream=None):
+    """The short causal convolution of every channel over its last W inputs:
+
+        y_t = act(bias + sum_j weight[:, j] * x_{t-W+1+j}),   act: "silu" or None
+
+    x [B,T,C] (channels contiguous; it may be a slice of wider rows), weight [C,W] and
+    bias [C] f32, W 2 to 4; x0 [B,W-1,C] (x's dtype) or None: the inputs before the first
+    row, oldest first.  offsets (int32 [n + 1]): the T rows of B = 1 hold n packed
+    sequences, and x0 is [n,W-1,C]; rows of no sequence are left as they were in a given
+    ``out["y"]``.  Returns (y, x_T), x_T the last W - 1 inputs.  ``out`` may hold
+    preallocated {"y", "x_T"}."""
+    lib = load_library()
+    key = _conv_key("conv", x, weight, bias, x0, offsets, activation)
+    hit = _checked.get(key) or _remember(key, _conv_check(x, weight, bias, x0, offsets, activation, "x0"))
+    dims, seqs, _ = hit
+    y, x_T = (out.get("y"), out.get("x_T")) if out else (None, None)
+    kept = (seqs, weight.shape[1] - 1, x.shape[2])
+    for name, t, shape in (("y", y, x.shape), ("x_T", x_T, kept)):
+        if t is not None:
+            _ptr(t, name, x.dtype, shape)
+            _same_device(x.device, **{name: t})
+
+    def call(s):
+        yo = _dense_like(x) if y is None else y
+        xo = torch.empty(kept, dtype=x.dtype, device=x.device) if x_T is None and want_state else x_T
+        return yo, xo, lib.carve_short_conv_fwd(dims, x.data_ptr(), weight.data_ptr(), _pointer(bias), _pointer(x0),
+                                                _pointer(offsets), yo.data_ptr(), _pointer(xo), s)
+
+    y, x_T, st = _on_stream(call, x.device, stream)
+    _check("carve_short_conv_fwd", st)
+    return y, x_T
+
+
+def short_conv_bwd(x, weight, dy, x0=None, dx_T=None, *, bias=None, activation="silu", offsets=None, want_dx0=None, out=None,
+                   workspace=None, stream=None):
+    """Backward of ``short_conv_fwd`` for loss <dy, y> + <dx_T, x_T>: a dict with dx,
+    dweight (f32), dbias (where bias is given) and dx0 (want_dx0; by default where x0 is
+    given)."""
+    lib = load_library()
+    key = _conv_key("conv", x, weight, bias, x0, offsets, activation)
+    hit = _checked.get(key) or _remember(key, _conv_check(x, weight, bias, x0, offsets, activation, "x0"))
+    dims, seqs, ws_bytes = hit
+    res = dict(out or {})
+    dev, kept = x.device, (seqs, weight.shape[1] - 1, x.shape[2])
+    _same_device(dev, dy=dy, dx_T=dx_T, workspace=workspace, **res)
+    _ptr(dy, "dy", x.dtype, x.shape)
+    _ptr(dx_T, "dx_T", x.dtype, kept)
+    want = (x0 is not None if want_dx0 is None else want_dx0) or res.get("dx0") is not None
+
+    def call(s):
+        dx = _out(res, "dx", x, x.shape, x.dtype, dev)
+        dw = _out(res, "dweight", weight, weight.shape, torch.float32, dev)
+        db = _out(res, "dbias", bias, bias.shape, torch.float32, dev) if bias is not None else _ptr(res.get("dbias"), "dbias")
+        d0 = _out(res, "dx0", x0, kept, x.dtype, dev) if want else None
+        ws, ws_ptr, ws_len = _scratch(workspace, ws_bytes, dev)
+        return lib.carve_short_conv_bwd(dims, x.data_ptr(), weight.data_ptr(), _pointer(bias), _pointer(x0), _pointer(offsets),
+                                        _pointer(dy), _pointer(dx_T), dx, dw, db, d0, ws_ptr, ws_len, s)
+
+    _check("carve_short_conv_bwd", _on_stream(call, dev, stream))
+    return res
+
+
+def short_conv_step(x, weight, state, slots=None, *, bias=None, activation="silu", out=None, stream=None):
+    """The short convolution for decoding: T tokens (x [B,T,C]) for each of B sequences,
+    whose last inputs in the pool ``state`` [pool,W-1,C] (x's dtype) are updated in place.
+    slots as in ``gdr_step``: a slot outside the pool (-1) marks a padding entry, whose
+    output rows are left as they were, and no slot may appear twice.  Returns y ("out" if given)."""
+    key = _conv_key("conv_step", x, weight, bias, state, slots, activation)
+    key = None if key is None else key + (_layout(out) if isinstance(out, torch.Tensor) else out,)
+    try:
+        hit = _checked.get(key)
+    except TypeError:   # (something else than tensors: named below)
+        hit = None
+    if hit is None:
+        load_library()
+        if not isinstance(state, torch.Tensor) or state.dim() != 3:
+            raise ValueError("state must be [pool, W - 1, C]")
+        hit = _conv_check(x, weight, bias, state, None, activation, "state", pool=state.shape[0])
+        _ptr(slots, "slots", torch.int32, (x.shape[0],))
+        _ptr(out, "out", x.dtype, x.shape)
+        _same_device(x.device, slots=slots, out=out)
+        _remember(key, hit)
+
+    def call(s):
+        y = _dense_like(x) if out is None else out
+        return y, _lib.carve_short_conv_step(hit[0], x.data_ptr(), weight.data_ptr(), _pointer(bias), _pointer(slots),
+                                             state.shape[0], state.data_ptr(), y.data_ptr(), s)
+
+    y, st = _on_stream(call, x.device, stream)
+    _check("carve_short_conv_step", st)
+    return y
+
+
+def rotary_frequencies(rot, base=10000.0, *, stretch=1.0, low=None, high=None, length=None, device="cuda"):
+    """Angles a position of the rot / 2 pairs, base^(-2 i / rot), in 64 bits, as
+    ``rotary_fwd`` takes them.  stretch: a context ``stretch`` times as long as trained;
+    all frequencies are divided by it, or, with length (of the trained context), low and
+    high: those that turn less than ``low`` times in it, none that turn more than ``high``
+    times, and those between by a part that is linear in their turns."""
+    if rot <= 0 or rot % 2:
+        raise ValueError(f"rot must be a positive even number, got {rot}")
+    if (low is None) != (high is None) or (low is None) != (length is None):
+        raise ValueError("low, high and length are given together")
+    freq = torch.tensor(float(base), dtype=torch.float64) ** (torch.arange(rot // 2, dtype=torch.float64) * (-2.0 / rot))
+    part = torch.ones_like(freq)
+    if low is not None:
+        if not low < high:
+            raise ValueError(f"low must be below high, got {low} and {high}")
+        turns = freq * (float(length) / 6.283185307179586)
+        part = 1 - ((turns - low) / (high - low)).clamp(0, 1)
+    return (freq * (1 - part) + freq / float(stretch) * part).to(device)
+
+
+def _rotary(q, k, freq, positions, start, offsets, interleaved, amplitude, out, stream, backward, names):
+    lib = load_library()
+    amplitude, interleaved = float(amplitude), bool(interleaved)
+    oq, ok = (out.get("q"), out.get("k")) if out else (None, None)
+    try:
+        key = ("rotary", interleaved, amplitude, _layout(q), _layout(k), _layout(freq), _layout(positions), _layout(start),
+               _layout(offsets), _layout(oq), _layout(ok))
+        dims = _checked.get(key)
+    except AttributeError:   # (something else than tensors: named below)
+        key = dims = None
+    if dims is None:
+        _gpu(q, names[0], 4)
+        dt, dev = _tokens(q, names[0]), q.device
+        B, T, Hq, D = q.shape
+        if k is not None:
+            _gpu(k, names[1], 4, q.dtype, dev)
+            if k.shape[:2] != q.shape[:2] or k.shape[3] != D:
+                raise ValueError(f"{names[1]} has shape {tuple(k.shape)}, expected {(B, T, 'heads', D)}")
+        elif ok is not None:
+            raise ValueError(f"out holds k, {names[1]} is not given")
+        _gpu(freq, "freq", 1, torch.float64, dev)
+        _same_device(dev, positions=positions, start=start, offsets=offsets, freq=freq, **{"out q": oq, "out k": ok})
+        seqs, N = _count(offsets, B)
+        _ptr(freq, "freq")
+        _ptr(positions, "positions", torch.int32, (B, T))
+        _ptr(start, "start", torch.int32, (seqs,))
+        _ptr(offsets, "offsets", torch.int32)
+        strides = []
+        for name, t, like in ((names[0], q, None), (names[1], k, None), ("out q", oq, q), ("out k", ok, k)):
+            if t is None:
+                # (a new tensor: dense)
+                n, d = (0, 0) if like is None else like.shape[2:]
+                strides += [T * n * d if B > 1 else 0, n * d if T > 1 else 0, d if n > 1 else 0]
+                continue
+            if like is not None and (t.dtype != like.dtype or t.shape != like.shape):
+                raise ValueError(f"{name} must be {tuple(like.shape)} of {like.dtype}")
+            _last(t, name)
+            strides += _steps(t, 3)
+        d = RotaryDims(B, T, N, Hq, 0 if k is None else k.shape[2], D, 2 * freq.numel(), dt, interleaved, amplitude, *strides)
+        dims = ctypes.byref(d)
+        _remember(key, dims)
+
+    def call(s):
+        qo = _dense_like(q) if oq is None else oq
+        ko = _dense_like(k) if ok is None and k is not None else ok
+        return qo, ko, lib.carve_rotary(dims, q.data_ptr(), _pointer(k), freq.data_ptr(), _pointer(positions), _pointer(start),
+                                        _pointer(offsets), backward, qo.data_ptr(), _pointer(ko), s)
+
+    qo, ko, st = _on_stream(call, q.device, stream)
+    _check("carve_rotary", st)
+    return qo, ko
+
+
+def rotary_fwd(q, k, freq, *, positions=None, start=None, offsets=None, interleaved=False, amplitude=1.0, out=None, stream=None):
+    """Rotary positions of q [B,T,Hq,D] and k [B,T,Hk,D] (k may be None): the pairs of the
+    first rot = 2 len(freq) values of every head are turned by position * freq (f64
+    [rot / 2], see ``rotary_frequencies``) and multiplied by ``amplitude``; the others are
+    kept.  Pairs are values i and i + rot / 2, or with interleaved 2 i and 2 i + 1.
+
+    A row's position is positions[b, t] (int32 [B,T]), or start (int32 [sequences], 0 if
+    None) plus its row in its sequence; offsets (int32 [n + 1]) as in ``gdr_chunk_fwd``.
+    Returns (q, k) turned.  ``out`` may hold {"q", "k"} to write to, strided or q and k
+    themselves (in place)."""
+    return _rotary(q, k, freq, positions, start, offsets, interleaved, amplitude, out, stream, 0, ("q", "k"))
+
+
+def rotary_bwd(dq, dk, freq, *, positions=None, start=None, offsets=None, interleaved=False, amplitude=1.0, out=None, stream=None):
+    """Backward of ``rotary_fwd``: from the gradients of its outputs to those of q and k
+    (turned the other way).  ``out`` {"q", "k"} as there."""
+    return _rotary(dq, dk, freq, positions, start, offsets, interleaved, amplitude, out, stream, 1, ("dq", "dk"))
+
+
+def _ssm_call(x, dt, A, Bm, Cm, D, dt_bias, softplus, offsets):
+    """Checks what every entry point takes; returns (dims, chunks, workspace bytes of
+    forward and backward, sequences, the pointers of x, dt, A, Bm, Cm, D, dt_bias)."""
+    try:
+        key = ("ssm", softplus, _layout(x), _layout(dt), _layout(A), _layout(Bm), _layout(Cm), _layout(D), _layout(dt_bias),
+               _layout(offsets))
+        hit = _checked.get(key)
+    except (AttributeError, TypeError):   # (something else than tensors: named below)
+        key = hit = None
+    if hit is None:
+        lib = load_library()
+        _gpu(x, "x", 4)
+        code, dev = _tokens(x, "x"), x.device
+        B, T, H, P = x.shape
+        _gpu(dt, "dt", 3, x.dtype, dev)
+        if tuple(dt.shape) != (B, T, H):
+            raise ValueError(f"dt has shape {tuple(dt.shape)}, expected {(B, T, H)}")
+        for name, t in (("Bm", Bm), ("Cm", Cm)):
+            _gpu(t, name, 4, x.dtype, dev)
+            if t.shape[:2] != x.shape[:2] or t.shape != Bm.shape:
+                raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(B, T, 'groups', 'state')}")
+        for name, t in (("x", x), ("dt", dt), ("Bm", Bm), ("Cm", Cm)):
+            _last(t, name)
+        _gpu(A, "A", 1, torch.float32, dev)
+        _same_device(dev, D=D, dt_bias=dt_bias, offsets=offsets)
+        for name, t in (("A", A), ("D", D), ("dt_bias", dt_bias)):
+            _ptr(t, name, torch.float32, (H,))
+        _ptr(offsets, "offsets", torch.int32)
+        seqs, N = _count(offsets, B)
+        d = SsmDims(B, T, N, Bm.shape[2], H, P, Bm.shape[3], code, bool(softplus), *_steps(x, 3), *_steps(Bm, 3), *_steps(Cm, 3),
+                    *_steps(dt, 2))
+        r = ctypes.byref(d)
+        hit = _remember(key, (r, int(lib.carve_ssm_chunk_count(r)), int(lib.carve_ssm_workspace_size(r, 0)),
+                              int(lib.carve_ssm_workspace_size(r, 1)), seqs))
+    return *hit, (x.data_ptr(), dt.data_ptr(), A.data_ptr(), Bm.data_ptr(), Cm.data_ptr(), _pointer(D), _pointer(dt_bias))
+
+
+def ssm_chunk_fwd(x, dt, A, Bm, Cm, S0=None, *, D=None, dt_bias=None, softplus=True, offsets=None, want_chunks=True,
+                  want_state=True, out=None, workspace=None, stream=None):
+    """Forward of the selective state space scan with a matrix state a head, in chunks of
+    64 tokens:
+
+        d_t = softplus(dt_t + dt_bias);  S = e^(d_t A) S + d_t x_t B_t^T;  y_t = S C_t + D x_t
+
+    x [B,T,H,P], Bm, Cm [B,T,G,N] (last dimension contiguous, any strides that are
+    multiples of 16 bytes), dt [B,T,H]; A (<= 0), D, dt_bias f32 [H], D and dt_bias may be
+    None; head h reads group h // (H // G) of Bm and Cm; S0 [B,H,P,N] f32 or None.
+    softplus=False: d_t = dt_t + dt_bias.  offsets (int32 [n + 1]): packed sequences as in
+    ``gdr_chunk_fwd``.  Returns (y, S_T, S_chunks); S_chunks (of its own form) is what
+    ``ssm_chunk_bwd`` needs.  ``out`` may hold preallocated {"y", "S_T", "S_chunks"}."""
+    lib = load_library()
+    dims, chunks, ws_bytes, _, seqs, ptrs = _ssm_call(x, dt, A, Bm, Cm, D, dt_bias, softplus, offsets)
+    H, P, N, f32, dev = x.shape[2], x.shape[3], Bm.shape[3], torch.float32, x.device
+    res = dict(out or {})
+    _same_device(dev, S0=S0, workspace=workspace, **res)
+
+    def call(s):
+        y = _out(res, "y", x, x.shape, x.dtype, dev)
+        S_T = _out(res, "S_T", S0, (seqs, H, P, N), f32, dev) if want_state or res.get("S_T") is not None else None
+        S_c = _out(res, "S_chunks", None, (chunks, H, P, N), f32, dev) if want_chunks or res.get("S_chunks") is not None else None
+        ws, ws_ptr, ws_len = _scratch(workspace, ws_bytes, dev) if ws_bytes or workspace is not None else (None, None, 0)
+        return lib.carve_ssm_chunk_fwd(dims, *ptrs, _ptr(S0, "S0", f32, (seqs, H, P, N)), _pointer(offsets), y, S_T, S_c,
+                                       ws_ptr, ws_len, s)
+
+    _check("carve_ssm_chunk_fwd", _on_stream(call, dev, stream))
+    return res["y"], res.get("S_T"), res.get("S_chunks")
+
+
+def ssm_chunk_bwd(x, dt, A, Bm, Cm, S_chunks, dy, dS_T=None, *, D=None, dt_bias=None, softplus=True, offsets=None,
+                  want_dS0=True, out=None, workspace=None, stream=None):
+    """Backward of ``ssm_chunk_fwd`` for loss <dy, y> + <dS_T, S_T>: a dict with dx, ddt, dA
+    (f32), dBm, dCm and, where they are given, dD, ddt_bias (f32), and with want_dS0 dS0.
+    dBm and dCm are sums over the heads of a group."""
+    lib = load_library()
+    dims, chunks, _, ws_bytes, seqs, ptrs = _ssm_call(x, dt, A, Bm, Cm, D, dt_bias, softplus, offsets)
+    H, P, N, f32, dev = x.shape[2], x.shape[3], Bm.shape[3], torch.float32, x.device
+    res = dict(out or {})
+    _same_device(dev, S_chunks=S_chunks, dy=dy, dS_T=dS_T, workspace=workspace, **res)
+
+    def call(s):
+        o = {name: _out(res, name, like, like.shape, like.dtype, dev) if like is not None else _ptr(res.get(name), name)
+             for name, like in (("dx", x), ("ddt", dt), ("dA", A), ("dBm", Bm), ("dCm", Cm), ("dD", D), ("ddt_bias", dt_bias))}
+        dS0 = _out(res, "dS0", dS_T, (seqs, H, P, N), f32, dev) if want_dS0 or res.get("dS0") is not None else None
+        ws, ws_ptr, ws_len = _scratch(workspace, ws_bytes, dev)
+        return lib.carve_ssm_chunk_bwd(dims, *ptrs, _ptr(S_chunks, "S_chunks", f32, (chunks, H, P, N)), _pointer(offsets),
+                                       _ptr(dy, "dy", x.dtype, x.shape), _ptr(dS_T, "dS_T", f32, (seqs, H, P, N)),
+                                       *o.values(), dS0, ws_ptr, ws_len, s)
+
+    _check("carve_ssm_chunk_bwd", _on_stream(call, dev, stream))
+    return res
+
+
+def ssm_step(x, dt, A, Bm, Cm, state, slots=None, *, D=None, dt_bias=None, softplus=True, out=None, stream=None):
+    """The scan token by token, for decoding: T tokens (one, or several at once) for each
+    of B sequences, whose states in the pool ``state`` [pool,H,P,N] f32 are updated in
+    place; slots as in ``gdr_step``.  The other arguments are those of ``ssm_chunk_fwd``.
+    Returns y [B,T,H,P] (``out`` if given)."""
+    try:
+        key = ("ssm_step", softplus, _layout(x), _layout(dt), _layout(A), _layout(Bm), _layout(Cm), _layout(D), _layout(dt_bias),
+               _layout(state), _layout(slots), _layout(out))
+        dims = _checked.get(key)
+    except (AttributeError, TypeError):   # (something else than tensors: named below)
+        key = dims = None
+    if dims is None:
+        dims, *_ = _ssm_call(x, dt, A, Bm, Cm, D, dt_bias, softplus, None)
+        if not isinstance(state, torch.Tensor) or state.dim() != 4:
+            raise ValueError("state must be [pool, H, P, N]")
+        _ptr(slots, "slots", torch.int32, (x.shape[0],))
+        _ptr(state, "state", torch.float32, (state.shape[0], x.shape[2], x.shape[3], Bm.shape[3]))
+        _ptr(out, "out", x.dtype, x.shape)
+        _same_device(x.device, state=state, slots=slots, out=out)
+        _remember(key, dims)
+
+    def call(s):
+        y = _dense_like(x) if out is None else out
+        return y, _lib.carve_ssm_step(dims, x.data_ptr(), dt.data_ptr(), A.data_ptr(), Bm.data_ptr(), Cm.data_ptr(), _pointer(D),
+                                      _pointer(dt_bias), _pointer(slots), state.shape[0], state.data_ptr(), y.data_ptr(), s)
+
+    y, st = _on_stream(call, x.device, stream)
+    _check("carve_ssm_step", st)
+    return y

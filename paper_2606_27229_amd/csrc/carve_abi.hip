@@ -2,8 +2,11 @@
 // sizing, kernel selection and launch.  No allocation, no synchronisation.
 #include <stdint.h>
 
+#include <utility>
+
 #include "carve_gdr.h"
 #include "carve_kernels.h"
+#include "carve_ssm.h"
 
 using namespace carve;
 
@@ -888,6 +891,467 @@ int carve_block_norm_bwd(const carve_block_norm_dims_t* d, const void* y, const 
   a.partial = static_cast<float*>(workspace);
   prof_mark(stream);
   return launch_block_norm_bwd(a, d->dtype, stream, prof_mark);
+}
+
+}  // extern "C"
+
+// ---- the short causal convolution --------------------------------------------------
+
+namespace {
+
+// sizes that packed and dense rows share: B, T, N of every operator beside the layer
+int check_rows(int B, int T, int N, carve_dtype_t dtype) {
+  if (B <= 0 || T <= 0 || N < 0) return CARVE_ERR_SHAPE;
+  if (N > 0 && B != 1) return CARVE_ERR_SHAPE;
+  if (dtype != CARVE_F32 && dtype != CARVE_BF16) return CARVE_ERR_UNSUPPORTED;
+  if ((long long)B * T >= (1LL << 31)) return CARVE_ERR_UNSUPPORTED;   // (row numbers are ints)
+  return CARVE_OK;
+}
+// a stride of `count` steps: not negative, whole pieces of 16 bytes (vec elements)
+int check_stride(long long stride, int count, long long vec) {
+  if (stride < 0) return CARVE_ERR_ARG;
+  if (stride % vec) return CARVE_ERR_ALIGN;
+  // (no tensor reaches 2^45 elements: spans stay within 64 bits)
+  if ((double)stride * (count - 1) >= 3.5e13) return CARVE_ERR_UNSUPPORTED;
+  return CARVE_OK;
+}
+
+int check_conv(const carve_short_conv_dims_t* d) {
+  if (!d) return CARVE_ERR_NULL;
+  if (d->C <= 0 || d->W <= 0) return CARVE_ERR_SHAPE;
+  int st = check_rows(d->B, d->T, d->N, d->dtype);
+  if (st) return st;
+  const long long vec = 16 / (long long)esize(d->dtype);
+  if (d->W < 2 || d->W > 4 || d->C % vec || d->C >= (1 << 20)) return CARVE_ERR_UNSUPPORTED;
+  if (d->activation != CARVE_CONV_LINEAR && d->activation != CARVE_CONV_SILU) return CARVE_ERR_ARG;
+  st = check_stride(d->x_batch, d->B, vec);
+  return st ? st : check_stride(d->x_token, d->T, vec);
+}
+size_t conv_seqs(const carve_short_conv_dims_t* d) { return d->N ? d->N : d->B; }
+size_t conv_kept(const carve_short_conv_dims_t* d) { return (size_t)(d->W - 1) * d->C * esize(d->dtype); }
+Range conv_x(const carve_short_conv_dims_t* d, const void* x) {
+  return {x, ((size_t)(d->B - 1) * d->x_batch + (size_t)(d->T - 1) * d->x_token + d->C) * esize(d->dtype)};
+}
+void conv_args(ConvArgs& a, const carve_short_conv_dims_t* d, const void* x, const float* weight, const float* bias,
+               const void* x0, const int* offsets) {
+  a = ConvArgs{};
+  a.x = x, a.weight = weight, a.bias = bias, a.x0 = x0, a.offsets = offsets;
+  a.x_batch = d->x_batch, a.x_token = d->x_token;
+  a.T = d->T, a.C = d->C, a.nseq = (int)conv_seqs(d), a.act = d->activation;
+}
+
+}  // namespace
+
+extern "C" {
+
+int carve_short_conv_fwd(const carve_short_conv_dims_t* d, const void* x, const float* weight, const float* bias,
+                         const void* x0, const int* offsets, void* y, void* x_T, hipStream_t stream) {
+  ProfClear pc;
+  int st = check_conv(d);
+  if (st) return st;
+  if (!x || !weight || !y || (d->N > 0 && !offsets)) return CARVE_ERR_NULL;
+  if (d->N == 0 && offsets) return CARVE_ERR_ARG;
+  const void* ptrs[] = {x, weight, bias, x0, offsets, y, x_T};
+  for (const void* p : ptrs)
+    if (!aligned16(p)) return CARVE_ERR_ALIGN;
+  const size_t kept = conv_seqs(d) * conv_kept(d);
+  const Range ins[] = {conv_x(d, x), {weight, (size_t)d->C * d->W * 4}, {bias, (size_t)d->C * 4}, {x0, kept}, {offsets, (size_t)(d->N + 1) * 4}};
+  const Range outs[] = {{y, (size_t)d->B * d->T * d->C * esize(d->dtype)}, {x_T, kept}};
+  if (any_overlap(outs, 2, ins, 5)) return CARVE_ERR_UNSUPPORTED;
+  ConvArgs a;
+  conv_args(a, d, x, weight, bias, x0, offsets);
+  a.y = y, a.x_T = x_T;
+  prof_mark(stream);
+  st = launch_short_conv_fwd(a, d->W, d->dtype, stream);
+  prof_mark(stream);
+  return st;
+}
+
+size_t carve_short_conv_workspace_size(const carve_short_conv_dims_t* d) {
+  if (check_conv(d) != CARVE_OK) return 0;
+  return align256((size_t)conv_parts(d->T, d->B, d->C, d->dtype) * (d->W + 1) * d->C * 4);
+}
+
+int carve_short_conv_bwd(const carve_short_conv_dims_t* d, const void* x, const float* weight, const float* bias,
+                         const void* x0, const int* offsets, const void* dy, const void* dx_T, void* dx,
+                         float* dweight, float* dbias, void* dx0, void* workspace, size_t workspace_bytes,
+                         hipStream_t stream) {
+  ProfClear pc;
+  int st = check_conv(d);
+  if (st) return st;
+  if (!x || !weight || !dy || !dx || !dweight || (d->N > 0 && !offsets)) return CARVE_ERR_NULL;
+  if ((d->N == 0 && offsets) || !bias != !dbias) return CARVE_ERR_ARG;
+  const void* ptrs[] = {x, weight, bias, x0, offsets, dy, dx_T, dx, dweight, dbias, dx0, workspace};
+  for (const void* p : ptrs)
+    if (!aligned16(p)) return CARVE_ERR_ALIGN;
+  const size_t need = carve_short_conv_workspace_size(d);
+  if (!workspace || workspace_bytes < need) return CARVE_ERR_WORKSPACE;
+  const size_t kept = conv_seqs(d) * conv_kept(d), rows = (size_t)d->B * d->T * d->C * esize(d->dtype);
+  const size_t nw = (size_t)d->C * d->W * 4, nb = (size_t)d->C * 4;
+  const Range ins[] = {conv_x(d, x), {weight, nw}, {bias, nb}, {x0, kept}, {offsets, (size_t)(d->N + 1) * 4}, {dy, rows}, {dx_T, kept}};
+  const Range outs[] = {{dx, rows}, {dweight, nw}, {dbias, nb}, {dx0, kept}, {workspace, need}};
+  if (any_overlap(outs, 5, ins, 7)) return CARVE_ERR_UNSUPPORTED;
+  ConvArgs a;
+  conv_args(a, d, x, weight, bias, x0, offsets);
+  a.dy = dy, a.dx_T = dx_T, a.dx = dx, a.dweight = dweight, a.dbias = dbias, a.dx0 = dx0;
+  a.partial = static_cast<float*>(workspace);
+  prof_mark(stream);
+  return launch_short_conv_bwd(a, d->W, d->dtype, stream, prof_mark);
+}
+
+int carve_short_conv_step(const carve_short_conv_dims_t* d, const void* x, const float* weight, const float* bias,
+                          const int* slots, int pool, void* state, void* y, hipStream_t stream) {
+  ProfClear pc;
+  int st = check_conv(d);
+  if (st) return st;
+  if (d->N != 0 || pool <= 0 || (!slots && pool < d->B)) return CARVE_ERR_SHAPE;
+  if (d->B > 65535) return CARVE_ERR_UNSUPPORTED;
+  if (!x || !weight || !state || !y) return CARVE_ERR_NULL;
+  const void* ptrs[] = {x, weight, bias, state, y};
+  for (const void* p : ptrs)
+    if (!aligned16(p)) return CARVE_ERR_ALIGN;
+  if ((uintptr_t)slots & 3u) return CARVE_ERR_ALIGN;
+  const Range ins[] = {conv_x(d, x), {weight, (size_t)d->C * d->W * 4}, {bias, (size_t)d->C * 4}, {slots, (size_t)d->B * 4}};
+  const Range outs[] = {{y, (size_t)d->B * d->T * d->C * esize(d->dtype)}, {state, pool * conv_kept(d)}};
+  if (any_overlap(outs, 2, ins, 4)) return CARVE_ERR_UNSUPPORTED;
+  ConvStepArgs a = {};
+  a.x = x, a.weight = weight, a.bias = bias, a.slots = slots, a.state = state, a.y = y;
+  a.x_batch = d->x_batch, a.x_token = d->x_token;
+  a.B = d->B, a.T = d->T, a.C = d->C, a.pool = pool, a.act = d->activation;
+  prof_mark(stream);
+  st = launch_short_conv_step(a, d->W, d->dtype, stream);
+  prof_mark(stream);
+  return st;
+}
+
+}  // extern "C"
+
+// ---- rotary positions ------------------------------------------------------------------
+
+namespace {
+
+// whether every element of a strided [.., D] tensor has a place of its own (st, n: strides
+// and counts of its three outer dimensions)
+bool places_apart(const long long* st, const int* n, int D) {
+  int order[3] = {0, 1, 2};
+  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2 - i; ++j)
+      if (st[order[j]] > st[order[j + 1]]) std::swap(order[j], order[j + 1]);
+  long long extent = D;
+  for (const int i : order) {
+    if (n[i] <= 1) continue;
+    if (st[i] < extent) return false;
+    extent += st[i] * (n[i] - 1);
+  }
+  return true;
+}
+// whether the heads of two such tensors lie in one row of a fused tensor without meeting
+bool rows_apart(const void* p, const long long* sp, int hp, const void* r, const long long* sr, int hr, const int* n, int D,
+                size_t es) {
+  if ((uintptr_t)p > (uintptr_t)r) return rows_apart(r, sr, hr, p, sp, hp, n, D, es);
+  const size_t off = (uintptr_t)r - (uintptr_t)p;
+  if (((size_t)(hp - 1) * sp[2] + D) * es > off) return false;
+  const size_t end = off + ((size_t)(hr - 1) * sr[2] + D) * es;
+  for (int i = 0; i < 2; ++i)
+    if (n[i] > 1 && (sp[i] != sr[i] || end > (size_t)sp[i] * es)) return false;
+  return true;
+}
+
+}  // namespace
+
+extern "C" {
+
+int carve_rotary(const carve_rotary_dims_t* d, const void* q, const void* k, const double* freq, const int* positions,
+                 const int* start, const int* offsets, int backward, void* q_out, void* k_out, hipStream_t stream) {
+  ProfClear pc;
+  if (!d) return CARVE_ERR_NULL;
+  if (d->Hq <= 0 || d->Hk < 0 || d->D <= 0 || d->rot <= 0 || d->rot > d->D) return CARVE_ERR_SHAPE;
+  int st = check_rows(d->B, d->T, d->N, d->dtype);
+  if (st) return st;
+  const size_t es = esize(d->dtype);
+  const int vec = (int)(16 / es);
+  if (d->D % vec || d->D > 1024 || d->rot % (2 * vec) || (long long)d->Hq + d->Hk > 65535) return CARVE_ERR_UNSUPPORTED;
+  if (!(d->amplitude >= -3.0e38f && d->amplitude <= 3.0e38f)) return CARVE_ERR_ARG;
+  const long long strides[] = {d->q_batch,  d->q_token,  d->q_head,  d->k_batch,  d->k_token,  d->k_head,
+                               d->qo_batch, d->qo_token, d->qo_head, d->ko_batch, d->ko_token, d->ko_head};
+  const int counts[] = {d->B, d->T, d->Hq, d->B, d->T, d->Hk > 0 ? d->Hk : 1};
+  for (int i = 0; i < 12; ++i) {
+    st = check_stride(strides[i], counts[i % 6], vec);
+    if (st) return st;
+  }
+  if (!q || !freq || !q_out || (d->Hk > 0 && (!k || !k_out)) || (d->N > 0 && !offsets)) return CARVE_ERR_NULL;
+  if (d->Hk == 0 && (k || k_out)) return CARVE_ERR_ARG;
+  if ((d->N == 0 && offsets) || (positions && (start || offsets))) return CARVE_ERR_ARG;
+  const void* ptrs[] = {q, k, freq, q_out, k_out};
+  for (const void* p : ptrs)
+    if (!aligned16(p)) return CARVE_ERR_ALIGN;
+  for (const int* p : {positions, start, offsets})
+    if ((uintptr_t)p & 3u) return CARVE_ERR_ALIGN;
+  const size_t nq = span(d->q_batch, d->q_token, d->q_head, d->B, d->T, d->Hq, d->D, es);
+  const size_t nqo = span(d->qo_batch, d->qo_token, d->qo_head, d->B, d->T, d->Hq, d->D, es);
+  const size_t nk = d->Hk ? span(d->k_batch, d->k_token, d->k_head, d->B, d->T, d->Hk, d->D, es) : 0;
+  const size_t nko = d->Hk ? span(d->ko_batch, d->ko_token, d->ko_head, d->B, d->T, d->Hk, d->D, es) : 0;
+  const int nqd[] = {d->B, d->T, d->Hq}, nkd[] = {d->B, d->T, d->Hk};
+  if (!places_apart(strides + 6, nqd, d->D) || (d->Hk > 0 && !places_apart(strides + 9, nkd, d->D))) return CARVE_ERR_ARG;
+  const bool in_place = q_out == q;
+  if (d->Hk > 0 && in_place != (k_out == k)) return CARVE_ERR_ARG;
+  if (in_place)
+    for (int i = 0; i < 6; ++i)
+      if ((i < 3 ? nqd[i] : nkd[i - 3]) > 1 && strides[i] != strides[6 + i]) return CARVE_ERR_ARG;
+  const Range others[] = {{freq, (size_t)(d->rot / 2) * 8}, {positions, (size_t)d->B * d->T * 4},
+                          {start, (size_t)(d->N ? d->N : d->B) * 4}, {offsets, (size_t)(d->N + 1) * 4},
+                          {q, in_place ? 0 : nq}, {k, in_place ? 0 : nk}};
+  const Range qo = {q_out, nqo}, ko = {k_out, nko};
+  if (any_overlap(&qo, 1, others, 6) || any_overlap(&ko, 1, others, 6)) return CARVE_ERR_UNSUPPORTED;
+  // (both may be slices of one tensor)
+  if (overlap(qo, ko) && !rows_apart(q_out, strides + 6, d->Hq, k_out, strides + 9, d->Hk, nqd, d->D, es))
+    return CARVE_ERR_UNSUPPORTED;
+  RotaryArgs a = {};
+  a.q = q, a.k = k, a.freq = freq, a.positions = positions, a.start = start, a.offsets = offsets, a.qo = q_out, a.ko = k_out;
+  for (int i = 0; i < 3; ++i) a.qs[i] = strides[i], a.ks[i] = strides[3 + i], a.qos[i] = strides[6 + i], a.kos[i] = strides[9 + i];
+  a.B = d->B, a.T = d->T, a.Hq = d->Hq, a.Hk = d->Hk, a.D = d->D, a.rot = d->rot, a.nseq = d->N ? d->N : d->B;
+  a.interleaved = d->interleaved, a.amplitude = d->amplitude, a.sign = backward ? -1.0f : 1.0f, a.copy = !in_place;
+  prof_mark(stream);
+  st = launch_rotary(a, d->dtype, stream);
+  prof_mark(stream);
+  return st;
+}
+
+}  // extern "C"
+
+// ---- the selective state space scan -------------------------------------------------------
+
+namespace {
+
+int check_ssm(const carve_ssm_dims_t* d) {
+  if (!d) return CARVE_ERR_NULL;
+  if (d->G <= 0 || d->H <= 0 || d->P <= 0 || d->S <= 0) return CARVE_ERR_SHAPE;
+  int st = check_rows(d->B, d->T, d->N, d->dtype);
+  if (st) return st;
+  if (d->S != 32 && d->S != 64 && d->S != 128) return CARVE_ERR_UNSUPPORTED;
+  if (d->P % 32 || d->P > 256 || d->H % d->G || d->H > 65535) return CARVE_ERR_UNSUPPORTED;
+  const long long vec = 16 / (long long)esize(d->dtype);
+  const struct {
+    long long s;
+    int n;
+    long long vec;
+  } strides[] = {{d->x_batch, d->B, vec}, {d->x_token, d->T, vec},  {d->x_head, d->H, vec},   {d->b_batch, d->B, vec},
+                 {d->b_token, d->T, vec}, {d->b_group, d->G, vec},  {d->c_batch, d->B, vec},  {d->c_token, d->T, vec},
+                 {d->c_group, d->G, vec}, {d->dt_batch, d->B, 1}, {d->dt_token, d->T, 1}};
+  for (const auto& x : strides) {
+    st = check_stride(x.s, x.n, x.vec);
+    if (st) return st;
+  }
+  // (a chunk's rows are addressed with 32 bits)
+  for (const long long s : {d->x_token, d->b_token, d->c_token, (long long)d->H * d->P})
+    if (s >= (1LL << 24) / (long long)esize(d->dtype)) return CARVE_ERR_UNSUPPORTED;
+  return CARVE_OK;
+}
+
+// chunks of a span, spans (slots of them) and shares of a group's heads
+struct SsmPlan {
+  size_t chunks, spans;
+  int span, splits;
+};
+constexpr long long kSsmGroups = 1024;   // workgroups that spans are cut for
+constexpr int kSsmMinSpan = 4;
+SsmPlan ssm_plan(const carve_ssm_dims_t* d) {
+  SsmPlan p;
+  const long long units = (d->T + (long long)kSsmC - 1) / kSsmC;
+  p.chunks = d->N ? (size_t)(d->T / kSsmC) + d->N : (size_t)(d->B * units);
+  const long long per = (long long)d->H * (d->P % 64 ? d->P / 32 : d->P / 64);
+  long long span = ((d->N ? 1 : d->B) * units * per + kSsmGroups - 1) / kSsmGroups;
+  if (span < kSsmMinSpan) span = kSsmMinSpan;
+  if (span > units) span = units;
+  // (equal ones)
+  const long long n = (units + span - 1) / span;
+  p.span = (int)((units + n - 1) / n);
+  const long long L = (long long)p.span * kSsmC;
+  p.spans = d->N ? (size_t)(d->T / L) + d->N : (size_t)(d->B * ((d->T + L - 1) / L));
+  const long long rep = d->H / d->G, want = (long long)(512 + p.chunks * d->G - 1) / (long long)(p.chunks * d->G);
+  p.splits = (int)(want < rep ? want : rep);
+  if (p.splits < 1) p.splits = 1;
+  return p;
+}
+// the chunk form's: a launch has less than 2^32 threads of each dimension
+int check_ssm_chunk(const carve_ssm_dims_t* d) {
+  const int st = check_ssm(d);
+  if (st) return st;
+  if ((long long)(d->T / kSsmC) + d->N >= (1LL << 23) || (long long)d->B * ((d->T + kSsmC - 1) / kSsmC) >= (1LL << 23))
+    return CARVE_ERR_UNSUPPORTED;
+  const SsmPlan p = ssm_plan(d);
+  if ((long long)(p.spans + 8) * d->H * (d->P / 32) >= (1LL << 23) || d->G > 65535) return CARVE_ERR_UNSUPPORTED;
+  return CARVE_OK;
+}
+size_t ssm_state(const carve_ssm_dims_t* d) { return (size_t)d->H * d->P * d->S * 4; }   // bytes, all heads
+bool ssm_split(const carve_ssm_dims_t* d, const SsmPlan& p) { return (long long)d->T > (long long)p.span * kSsmC; }
+
+// workspace: spans' states and decays | state gradients | shares of the head sums | of dB, dC
+struct SsmWs {
+  size_t Z, Zg, E, part, dBp, total;
+};
+SsmWs ssm_ws(const carve_ssm_dims_t* d, bool bwd) {
+  const SsmPlan p = ssm_plan(d);
+  SsmWs w{};
+  size_t off = 0;
+  const bool split = ssm_split(d, p);
+  w.Z = off, off += split ? align256(p.spans * ssm_state(d)) : 0;
+  w.Zg = off, off += split ? align256(p.spans * d->H * 4) : 0;
+  if (bwd) {
+    w.E = off, off += align256(p.chunks * ssm_state(d));
+    w.part = off, off += align256(p.chunks * d->H * 16);
+    w.dBp = off, off += p.splits > 1 ? align256((size_t)p.splits * 2 * d->B * d->T * d->G * d->S * 4) : 0;
+  }
+  w.total = off;
+  return w;
+}
+void ssm_args(SsmArgs& a, const carve_ssm_dims_t* d, const void* x, const void* dt, const float* A, const void* Bm,
+              const void* Cm, const float* D, const float* dt_bias, const int* offsets, void* workspace, bool bwd) {
+  a = SsmArgs{};
+  a.x = x, a.dt = dt, a.A = A, a.Bm = Bm, a.Cm = Cm, a.D = D, a.dt_bias = dt_bias, a.offsets = offsets;
+  a.xs[0] = d->x_batch, a.xs[1] = d->x_token, a.xs[2] = d->x_head;
+  a.bs[0] = d->b_batch, a.bs[1] = d->b_token, a.bs[2] = d->b_group;
+  a.cs[0] = d->c_batch, a.cs[1] = d->c_token, a.cs[2] = d->c_group;
+  a.ds[0] = d->dt_batch, a.ds[1] = d->dt_token;
+  a.T = d->T, a.G = d->G, a.H = d->H, a.P = d->P, a.N = d->S, a.softplus = d->softplus;
+  const SsmPlan p = ssm_plan(d);
+  a.nseq = d->N ? d->N : d->B;
+  a.nslots = (int)p.chunks, a.nspans = (int)p.spans, a.span = p.span, a.splits = p.splits;
+  const SsmWs w = ssm_ws(d, bwd);
+  char* ws = static_cast<char*>(workspace);
+  a.Z = reinterpret_cast<float*>(ws + w.Z), a.Zg = reinterpret_cast<float*>(ws + w.Zg);
+  a.E_chunks = ws + w.E, a.part = reinterpret_cast<float*>(ws + w.part), a.dBp = reinterpret_cast<float*>(ws + w.dBp);
+}
+int ssm_inputs(const carve_ssm_dims_t* d, const void* x, const void* dt, const float* A, const void* Bm, const void* Cm,
+               const float* D, const float* dt_bias, Range* r) {
+  const size_t es = esize(d->dtype), nh = (size_t)d->H * 4;
+  r[0] = {x, span(d->x_batch, d->x_token, d->x_head, d->B, d->T, d->H, d->P, es)};
+  r[1] = {dt, span(d->dt_batch, d->dt_token, 0, d->B, d->T, 1, d->H, es)};
+  r[2] = {Bm, span(d->b_batch, d->b_token, d->b_group, d->B, d->T, d->G, d->S, es)};
+  r[3] = {Cm, span(d->c_batch, d->c_token, d->c_group, d->B, d->T, d->G, d->S, es)};
+  r[4] = {A, nh}, r[5] = {D, nh}, r[6] = {dt_bias, nh};
+  return 7;
+}
+// pointers every entry point takes: whole pieces of 16 bytes, but the scalars a head and dt
+int ssm_aligned(const carve_ssm_dims_t* d, const void* x, const void* dt, const float* A, const void* Bm, const void* Cm,
+                const float* D, const float* dt_bias) {
+  if (!aligned16(x) || !aligned16(Bm) || !aligned16(Cm) || (uintptr_t)dt % esize(d->dtype)) return CARVE_ERR_ALIGN;
+  for (const float* p : {A, D, dt_bias})
+    if ((uintptr_t)p & 3u) return CARVE_ERR_ALIGN;
+  return CARVE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t carve_ssm_chunk_count(const carve_ssm_dims_t* d) { return check_ssm_chunk(d) == CARVE_OK ? ssm_plan(d).chunks : 0; }
+
+size_t carve_ssm_workspace_size(const carve_ssm_dims_t* d, int for_backward) {
+  return check_ssm_chunk(d) == CARVE_OK ? ssm_ws(d, for_backward != 0).total : 0;
+}
+
+int carve_ssm_chunk_fwd(const carve_ssm_dims_t* d, const void* x, const void* dt, const float* A, const void* Bm,
+                        const void* Cm, const float* D, const float* dt_bias, const float* S0, const int* offsets,
+                        void* y, float* S_T, float* S_chunks, void* workspace, size_t workspace_bytes,
+                        hipStream_t stream) {
+  ProfClear pc;
+  int st = check_ssm_chunk(d);
+  if (st) return st;
+  if (!x || !dt || !A || !Bm || !Cm || !y || (d->N > 0 && !offsets)) return CARVE_ERR_NULL;
+  if (d->N == 0 && offsets) return CARVE_ERR_ARG;
+  st = ssm_aligned(d, x, dt, A, Bm, Cm, D, dt_bias);
+  if (st) return st;
+  const void* ptrs[] = {S0, offsets, y, S_T, S_chunks, workspace};
+  for (const void* p : ptrs)
+    if (!aligned16(p)) return CARVE_ERR_ALIGN;
+  const size_t need = carve_ssm_workspace_size(d, 0);
+  if (need && (!workspace || workspace_bytes < need)) return CARVE_ERR_WORKSPACE;
+  const size_t seqs = d->N ? d->N : d->B, state = ssm_state(d);
+  Range ins[9];
+  int nin = ssm_inputs(d, x, dt, A, Bm, Cm, D, dt_bias, ins);
+  ins[nin++] = {S0, seqs * state};
+  ins[nin++] = {offsets, (size_t)(d->N + 1) * 4};
+  const Range outs[] = {{y, (size_t)d->B * d->T * d->H * d->P * esize(d->dtype)},
+                        {S_T, seqs * state},
+                        {S_chunks, ssm_plan(d).chunks * state},
+                        {workspace, need}};
+  if (any_overlap(outs, 4, ins, nin)) return CARVE_ERR_UNSUPPORTED;
+  SsmArgs a;
+  ssm_args(a, d, x, dt, A, Bm, Cm, D, dt_bias, offsets, workspace, false);
+  a.S0 = S0, a.y = y, a.S_T = S_T, a.S_chunks = reinterpret_cast<char*>(S_chunks);
+  prof_mark(stream);
+  return launch_ssm_fwd(a, d->dtype, stream, prof_mark);
+}
+
+int carve_ssm_chunk_bwd(const carve_ssm_dims_t* d, const void* x, const void* dt, const float* A, const void* Bm,
+                        const void* Cm, const float* D, const float* dt_bias, const float* S_chunks, const int* offsets,
+                        const void* dy, const float* dS_T, void* dx, void* ddt, float* dA, void* dBm, void* dCm,
+                        float* dD, float* ddt_bias, float* dS0, void* workspace, size_t workspace_bytes,
+                        hipStream_t stream) {
+  ProfClear pc;
+  int st = check_ssm_chunk(d);
+  if (st) return st;
+  if (!x || !dt || !A || !Bm || !Cm || !S_chunks || !dy || !dx || !ddt || !dA || !dBm || !dCm || (d->N > 0 && !offsets))
+    return CARVE_ERR_NULL;
+  if ((d->N == 0 && offsets) || !D != !dD || !dt_bias != !ddt_bias) return CARVE_ERR_ARG;
+  st = ssm_aligned(d, x, dt, A, Bm, Cm, D, dt_bias);
+  if (st) return st;
+  const void* ptrs[] = {S_chunks, offsets, dy, dS_T, dx, ddt, dBm, dCm, dS0, workspace};
+  for (const void* p : ptrs)
+    if (!aligned16(p)) return CARVE_ERR_ALIGN;
+  for (const float* p : {dA, dD, ddt_bias})
+    if ((uintptr_t)p & 3u) return CARVE_ERR_ALIGN;
+  const size_t need = carve_ssm_workspace_size(d, 1);
+  if (!workspace || workspace_bytes < need) return CARVE_ERR_WORKSPACE;
+  const size_t es = esize(d->dtype), rows = (size_t)d->B * d->T, seqs = d->N ? d->N : d->B, state = ssm_state(d);
+  Range ins[11];
+  int nin = ssm_inputs(d, x, dt, A, Bm, Cm, D, dt_bias, ins);
+  ins[nin++] = {S_chunks, ssm_plan(d).chunks * state};
+  ins[nin++] = {offsets, (size_t)(d->N + 1) * 4};
+  ins[nin++] = {dy, rows * d->H * d->P * es};
+  ins[nin++] = {dS_T, seqs * state};
+  const size_t nb = rows * d->G * d->S * es, nh = (size_t)d->H * 4;
+  const Range outs[] = {{dx, rows * d->H * d->P * es}, {ddt, rows * d->H * es}, {dA, nh}, {dBm, nb}, {dCm, nb},
+                        {dD, nh}, {ddt_bias, nh}, {dS0, seqs * state}, {workspace, need}};
+  if (any_overlap(outs, 9, ins, nin)) return CARVE_ERR_UNSUPPORTED;
+  SsmArgs a;
+  ssm_args(a, d, x, dt, A, Bm, Cm, D, dt_bias, offsets, workspace, true);
+  a.S_chunks = const_cast<char*>(reinterpret_cast<const char*>(S_chunks));   // (read only)
+  a.dy = dy, a.dS_T = dS_T, a.dx = dx, a.ddt = ddt, a.dA = dA, a.dBm = dBm, a.dCm = dCm, a.dD = dD;
+  a.ddt_bias = ddt_bias, a.dS0 = dS0;
+  prof_mark(stream);
+  return launch_ssm_bwd(a, d->dtype, stream, prof_mark);
+}
+
+int carve_ssm_step(const carve_ssm_dims_t* d, const void* x, const void* dt, const float* A, const void* Bm,
+                   const void* Cm, const float* D, const float* dt_bias, const int* slots, int pool, float* state,
+                   void* y, hipStream_t stream) {
+  ProfClear pc;
+  int st = check_ssm(d);
+  if (st) return st;
+  if (d->N != 0 || pool <= 0 || (!slots && pool < d->B)) return CARVE_ERR_SHAPE;
+  if (d->B > 65535) return CARVE_ERR_UNSUPPORTED;
+  if (!x || !dt || !A || !Bm || !Cm || !state || !y) return CARVE_ERR_NULL;
+  st = ssm_aligned(d, x, dt, A, Bm, Cm, D, dt_bias);
+  if (st) return st;
+  if (!aligned16(state) || !aligned16(y) || ((uintptr_t)slots & 3u)) return CARVE_ERR_ALIGN;
+  Range ins[8];
+  int nin = ssm_inputs(d, x, dt, A, Bm, Cm, D, dt_bias, ins);
+  ins[nin++] = {slots, (size_t)d->B * 4};
+  const Range outs[] = {{y, (size_t)d->B * d->T * d->H * d->P * esize(d->dtype)}, {state, (size_t)pool * ssm_state(d)}};
+  if (any_overlap(outs, 2, ins, nin)) return CARVE_ERR_UNSUPPORTED;
+  SsmStepArgs a = {};
+  a.x = x, a.dt = dt, a.Bm = Bm, a.Cm = Cm, a.A = A, a.D = D, a.dt_bias = dt_bias, a.slots = slots, a.state = state, a.y = y;
+  a.xs[0] = d->x_batch, a.xs[1] = d->x_token, a.xs[2] = d->x_head;
+  a.bs[0] = d->b_batch, a.bs[1] = d->b_token, a.bs[2] = d->b_group;
+  a.cs[0] = d->c_batch, a.cs[1] = d->c_token, a.cs[2] = d->c_group;
+  a.ds[0] = d->dt_batch, a.ds[1] = d->dt_token;
+  a.B = d->B, a.T = d->T, a.G = d->G, a.H = d->H, a.P = d->P, a.pool = pool, a.softplus = d->softplus;
+  prof_mark(stream);
+  st = launch_ssm_step(a, d->S, d->dtype, stream);
+  prof_mark(stream);
+  return st;
 }
 
 }  // extern "C"

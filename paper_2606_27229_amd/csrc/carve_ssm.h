@@ -1,0 +1,206 @@
+// carve_ssm.h -- shared pieces of the selective state space scan (a matrix state a head,
+// one decay a token and head):
+//   d_t = softplus(dt_t + dt_bias),  a_t = d_t A,
+//   S_t = e^{a_t} S_{t-1} + d_t x_t B_t^T  (P x N),  y_t = S_t C_t + D x_t
+// Chunk form over C = 64 tokens, G = prefix sums of a inside the chunk, L_ij = e^{G_i - G_j}
+// for j <= i:
+//   Y = e^G C S^T + (L d_j C B^T) X + D X
+//   S <- e^{G_C} S + X^T (e^{G_C - G} d B)
+// Unlike a delta rule's, a chunk's writes do not depend on the state, so spans of chunks
+// run side by side: each adds up what it writes, one pass joins them along the sequence,
+// and each then makes its outputs from its start state.  A span keeps its state in
+// registers; only spans' states go through memory.
+//
+// Precision as in the gated delta rule (carve_gdr.h): decays and steps multiply f32 values;
+// with bf16 tokens the f32 intermediates enter the matrix cores as sums of bf16 values,
+// three towards f32 results and two towards bf16 ones; with f32 tokens every product is
+// f32.  G is summed in 64 bits and kept as two floats.
+#pragma once
+#include "carve_gdr.h"
+#include "carve_ops.h"
+
+namespace carve {
+
+constexpr int kSsmC = kGdrC;              // tokens of a chunk
+
+struct SsmArgs {
+  const void *x, *dt, *Bm, *Cm, *dy;
+  const float *A, *D, *dt_bias, *S0, *dS_T;
+  const int* offsets;      // packed sequences: [nseq + 1]; dense: NULL
+  void *y, *dx, *ddt, *dBm, *dCm;
+  float *S_T, *dA, *dD, *ddt_bias, *dS0;
+  char *S_chunks, *E_chunks;   // states at chunk starts, state gradients at chunk ends: see SsmState
+  float* Z;                // [nspans][H][P][N]: what a span adds, then the state it starts from
+  float* Zg;               // [nspans][H]: its decay
+  float* part;             // [nslots][H][4]: a chunk's share of dA, ddt_bias, dD
+  float* dBp;              // [splits][rows][G][N], dCp behind it: shares of dB, dC
+  long long xs[3], bs[3], cs[3], ds[2];   // strides of batch, token, head (or group)
+  int T, G, H, P, N, nseq, nslots, nspans, span, splits;   // span: chunks of a span
+  int softplus;
+};
+
+// ---- sequences, chunk slots and spans --------------------------------------------------
+// As for the gated delta rule: a sequence's units of L rows are slots floor(first / L) +
+// sequence + unit where sequences are packed, sequence * units + unit else.
+struct SsmSeq {
+  int n, batch, first, len;
+};
+__device__ __forceinline__ SsmSeq ssm_seq(const SsmArgs& a, int n) {
+  SsmSeq s;
+  s.n = n;
+  if (!a.offsets) {
+    s.batch = n, s.first = 0, s.len = a.T;
+  } else {
+    int end;
+    packed_seq(a.offsets, n, a.T, s.first, end);
+    s.batch = 0, s.len = end - s.first;
+  }
+  return s;
+}
+__device__ __forceinline__ int ssm_units(int len, int L) { return (int)(((long long)len + L - 1) / L); }
+__device__ __forceinline__ int ssm_slot0(const SsmArgs& a, const SsmSeq& s, int L) {
+  return a.offsets ? s.first / L + s.n : s.n * ssm_units(a.T, L);
+}
+// sequence of a slot; its unit there may lie behind the sequence's last
+__device__ __forceinline__ SsmSeq ssm_find(const SsmArgs& a, int slot, int L) {
+  if (!a.offsets) return ssm_seq(a, slot / ssm_units(a.T, L));
+  int lo = 0, hi = a.nseq - 1;   // the last n whose first slot is not behind this one
+  while (lo < hi) {
+    const int m = (lo + hi + 1) >> 1;
+    if (min(max(a.offsets[m], 0), a.T) / L + m <= slot) lo = m;
+    else hi = m - 1;
+  }
+  return ssm_seq(a, lo);
+}
+
+// ---- scalars of a chunk ---------------------------------------------------------------
+// d, G as two floats, e^G (0 behind the last token), e^{G_C - G}; then e^{G_C}
+enum : int { kSmD = 0, kSmGh = 1, kSmGl = 2, kSmGam = 3, kSmEnd = 4, kSmWhole = 5 * kSsmC, kSmFloats = 5 * kSsmC + 4 };
+
+__device__ __forceinline__ float ssm_step_of(float z, int softplus) {
+  return softplus ? fmaxf(z, 0.0f) + log1pf(expf(-fabsf(z))) : z;
+}
+// by one wave, a token a lane; raw: its dt
+__device__ __forceinline__ void ssm_scalars(float raw, bool in, float bias, float A, int softplus, int lane, float* out) {
+  const float d = in ? ssm_step_of(raw + bias, softplus) : 0.0f;
+  float ga = in ? d * A : 0.0f;
+  ga = ga < kGdrMinG ? kGdrMinG : ga;
+  double G = (double)ga;
+#pragma unroll
+  for (int s = 1; s < 64; s *= 2) {
+    const double up = __shfl_up(G, s);
+    if (lane >= s) G += up;
+  }
+  const double all = __shfl(G, 63);
+  const float Gh = (float)G, Gl = (float)(G - (double)Gh);
+  out[kSmD * kSsmC + lane] = d;
+  out[kSmGh * kSsmC + lane] = Gh;
+  out[kSmGl * kSsmC + lane] = Gl;
+  out[kSmGam * kSsmC + lane] = in ? decay_exp(Gh) * (1.0f + Gl) : 0.0f;
+  out[kSmEnd * kSsmC + lane] = decay_exp((float)(all - G));
+  if (lane == 0) out[kSmWhole] = decay_exp((float)all);
+}
+
+// ---- LDS tiles -------------------------------------------------------------------------
+// GdrRows of ROWS rows (its layout and operand reads); rows behind the last of `len`
+// repeat it.
+template <typename T, int COLS, int ROWS>
+struct SsmRows : GdrRows<T, COLS> {
+  typedef GdrRows<T, COLS> R;
+  static constexpr int bytes = ROWS * R::RB;
+  static_assert(bytes % 1024 == 0, "whole pieces of 1 KB");
+  template <int NW>
+  static __device__ __forceinline__ void dma(char* lds, const void* base, int stride, int len, int w, int lane) {
+    const __amdgpu_buffer_rsrc_t r =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (len - 1) * stride + R::RB, 0x00027000);
+    constexpr int RPI = 1024 / R::RB;   // rows of a piece
+#pragma unroll
+    for (int u = 0; u < (bytes / 1024 + NW - 1) / NW; ++u) {
+      const int i = w + NW * u;
+      if ((bytes / 1024) % NW != 0 && i >= bytes / 1024) break;   // (uniform)
+      const int row = i * RPI + lane / R::NCH, x = (lane % R::NCH) ^ R::swz(row);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, lds_at(lds + 1024 * i), 16, (int)__umul24(min(row, len - 1), stride) + 16 * x, 0, 0, 0);
+    }
+  }
+  // lane (g, c): row 16 i + c, columns 16 j + 4 g + e
+  static __device__ __forceinline__ typename Quad<T>::q quad(const char* lds, int i, int j, int g, int c) {
+    int o;
+    if constexpr (sizeof(T) == 2) o = (((2 * j + (g >> 1)) ^ R::swz(c)) << 4) + ((g & 1) << 3);
+    else o = ((4 * j + g) ^ R::swz(c)) << 4;
+    return Quad<T>::ld(reinterpret_cast<const T*>(lds + (16 * i + c) * R::RB + o));
+  }
+};
+
+// States kept for the backward, a head's [P][N]: f32, or with bf16 tokens two planes of
+// bf16, the upper and the lower half of the significand's first 16 bits (as many bytes).
+// They only enter products towards bf16 results, and matrix cores take the planes as they
+// are: the gradients' kernel needs no conversion of them (its LDS holds them as loaded).
+template <typename T>
+struct SsmState {
+  static constexpr int planes = sizeof(T) == 2 ? 2 : 1;
+  // lane's four neighbouring n of row p
+  static __device__ __forceinline__ void st(char* head, size_t pn, size_t at, f32x4 v) {
+    if constexpr (sizeof(T) == 2) {
+      const bf16x4 hi = Quad<T>::cvt(v);
+      *reinterpret_cast<bf16x4*>(head + 2 * at) = hi;
+      *reinterpret_cast<bf16x4*>(head + 2 * pn + 2 * at) = Quad<T>::cvt(bf16_rest(v, hi));
+    } else {
+      *reinterpret_cast<f32x4*>(head + 4 * at) = v;
+    }
+  }
+};
+
+// ---- workgroups of the scans -------------------------------------------------------------
+// Workgroup -> (span, head, slice of PW value rows).  Blocks 8 apart share an XCD: with many
+// spans each goes to one XCD with all its heads, which read the same B and C from one L2;
+// with few the heads are spread.
+constexpr int kSsmManySpans = 32;
+__host__ __device__ inline unsigned ssm_grid(int nspans, int per) {
+  return nspans >= kSsmManySpans ? (unsigned)((nspans + 7) / 8 * 8) * per : (unsigned)nspans * per;
+}
+struct SsmSpan {
+  SsmSeq q;
+  int slot, s, nspan;      // span slot; the span's number in its sequence, of nspan (at least 1)
+  int first, len, nch;     // rows (of the sequence's batch) and chunks of the span
+  int slot0;               // its first chunk's slot
+};
+__device__ __forceinline__ bool ssm_block(const SsmArgs& a, int per, SsmSpan& p, int& rest) {
+  int b = blockIdx.x;
+  if (a.nspans >= kSsmManySpans) {
+    const int at = b / 8;
+    p.slot = at / per * 8 + b % 8;
+    rest = at % per;
+  } else {
+    p.slot = b / per;
+    rest = b % per;
+  }
+  if (p.slot >= a.nspans) return false;
+  const int L = a.span * kSsmC;
+  p.q = ssm_find(a, p.slot, L);
+  p.s = p.slot - ssm_slot0(a, p.q, L);
+  p.nspan = max(ssm_units(p.q.len, L), 1);
+  if (p.s < 0 || p.s >= p.nspan) return false;
+  p.first = p.q.first + p.s * L;
+  p.len = min(p.q.len - p.s * L, L);
+  p.nch = (p.len + kSsmC - 1) / kSsmC;
+  p.slot0 = ssm_slot0(a, p.q, kSsmC) + p.s * a.span;
+  return true;
+}
+
+struct SsmStepArgs {
+  const void *x, *dt, *Bm, *Cm;
+  const float *A, *D, *dt_bias;
+  const int* slots;
+  float* state;
+  void* y;
+  long long xs[3], bs[3], cs[3], ds[2];
+  int B, T, G, H, P, pool, softplus;
+};
+
+int launch_ssm_fwd(const SsmArgs& a, int dtype, hipStream_t s, void (*mark)(hipStream_t));
+int launch_ssm_bwd(const SsmArgs& a, int dtype, hipStream_t s, void (*mark)(hipStream_t));
+int launch_ssm_step(const SsmStepArgs& a, int N, int dtype, hipStream_t s);
+// the chain of state gradients: spans' sums and their joining, then E of every chunk, dS0
+int launch_ssm_spans_rev(const SsmArgs& a, int dtype, hipStream_t s, void (*mark)(hipStream_t));
+
+}  // namespace carve
