@@ -41,6 +41,10 @@ struct Tile {
 
 __device__ __forceinline__ f32x4 four(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
 
+// Behind a loop whose last instructions are products: the stores that follow read their
+// results, and the compiler leaves them a wait state short there.
+__device__ __forceinline__ void settle() { asm volatile("s_nop 7" ::: "memory"); }
+
 // The steps of a span's chunks, a chunk ahead: one wave holds the next chunk's dt and makes
 // its scalars while the others' rows are on their way.
 template <typename T>
@@ -139,6 +143,7 @@ __global__ void __launch_bounds__(64 * NW) carve_ssm_state_kernel(SsmArgs a, int
     }, sc[kSmWhole], g, c);
     decay *= sc[kSmWhole];
   }
+  settle();
   if (!full) {
     t.store(zs);
     if (tid == 0 && p0 == 0) a.Zg[(size_t)p.slot * a.H + h] = decay;
@@ -296,6 +301,7 @@ __global__ void __launch_bounds__(64 * NW) carve_ssm_out_kernel(SsmArgs a) {
     t.template add<KR>(smem + L::B, fx, [&](int at) { return four(sc + kSmEnd * kSsmC + at) * four(sc + kSmD * kSsmC + at); },
                        sc[kSmWhole], g, c);
   }
+  settle();
   if (a.S_T && p.s == p.nspan - 1) t.store(a.S_T + ((size_t)p.q.n * a.H + h) * pn + row);
 }
 
