@@ -150,6 +150,11 @@ struct SsmState {
   }
 };
 
+// ---- odds and ends ------------------------------------------------------------------------
+// Behind a loop whose last instructions are products: the stores that follow read their
+// results, and the compiler leaves them a wait state short there.
+__device__ __forceinline__ void settle() { asm volatile("s_nop 7" ::: "memory"); }
+
 // ---- workgroups of the scans -------------------------------------------------------------
 // Workgroup -> (span, head, slice of PW value rows).  Blocks 8 apart share an XCD: with many
 // spans each goes to one XCD with all its heads, which read the same B and C from one L2;

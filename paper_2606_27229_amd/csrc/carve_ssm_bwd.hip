@@ -20,22 +20,26 @@ namespace {
 constexpr int kPw = 32;   // value columns of a turn
 constexpr int kPart = 4;  // floats of a (chunk, head) in SsmArgs::part
 
-// One workgroup a chunk, group and share of the group's heads; wave w owns token tile w, as
-// i of dC and as j of dB and dx (their work adds up to the same for every wave).  dB and dC
-// stay in registers over the heads; a head comes in turns of 32 value columns, in which
-// everything but L is linear: x, dy and the rows of S and E, loaded straight into LDS.
-// Bound by HBM, the states S and E above all (N x P floats each, a chunk and head); two
-// workgroups a compute unit load and compute by turns (bf16).
+// One workgroup a chunk, group and share of the group's heads.  Waves 0 to 3 make dC and
+// what a decay multiplies from before, waves 4 to 7 dB, dx and the rest; wave w of each side
+// owns token tile w, as i of dC and as j of dB and dx.  dB and dC stay in registers over the
+// heads; a head comes in turns of 32 value columns, in which everything but L is linear: x,
+// dy and the rows of S and E, loaded straight into LDS a turn ahead.
+// Bound by HBM, the states S and E above all (N x P floats each, a chunk and head).
 template <typename T, int N>
 struct GradLds {
   typedef SsmRows<T, N, kSsmC> KR;     // B, C
   typedef SsmRows<T, kPw, kSsmC> VR;   // x, dy
   typedef SsmRows<T, N, kPw> SR;       // a plane of S or E
   static constexpr int state = SR::bytes * SsmState<T>::planes;
-  static constexpr int B = 0, C = KR::bytes, X = 2 * KR::bytes, dY = X + VR::bytes, S = dY + VR::bytes, E = S + state;
-  static constexpr int scal = E + state, sum = scal + kSmFloats * 4;
-  // r_t, d_t E_t x.EB, their column sums, da's rectangles by wave, dy.x; <E, S> by wave
-  static constexpr int total = sum + (8 * kSsmC + 4) * 4;
+  static constexpr int B = 0, C = KR::bytes, turn = 2 * KR::bytes;
+  static constexpr int X = 0, dY = VR::bytes, S = dY + VR::bytes, E = S + state, one = E + state;   // of a turn
+  // r_t, E_t x.EB, their column sums, dy.x, da's rectangles by wave; <E, S> by wave
+  static constexpr int sums = 8 * kSsmC + 4, small = 2 * (kSmFloats + sums) * 4;
+  // two turns' rows where they fit (else a turn's rows are waited for)
+  static constexpr bool ahead = turn + 2 * one + small <= 160 * 1024;
+  static constexpr int scal = turn + (ahead ? 2 : 1) * one, sum = scal + 2 * kSmFloats * 4;
+  static constexpr int total = scal + small;
 };
 
 template <typename T, int N>
@@ -63,247 +67,277 @@ __device__ __forceinline__ float col_sum(float x) {
 }
 
 template <typename T, int N>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) carve_ssm_grad_kernel(SsmArgs a) {
+__global__ void __launch_bounds__(512, 2) carve_ssm_grad_kernel(SsmArgs a) {
   typedef GradLds<T, N> L;
   typedef typename L::KR KR;
   typedef typename L::VR VR;
   typedef typename L::SR SR;
   constexpr int NP = N / 32, NT = N / 16;
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  float* sc = reinterpret_cast<float*>(smem + L::scal);
-  float* sR = reinterpret_cast<float*>(smem + L::sum);
-  float *sE = sR + kSsmC, *sM = sE + kSsmC, *sRect = sM + kSsmC, *sDiag = sRect + 4 * kSsmC, *sES = sDiag + kSsmC;
-  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int g = lane >> 4, c = lane & 15;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const bool back = wave >= 4;   // (uniform) dB and dx
+  const int w = wave & 3;
+  int g = lane >> 4, c = lane & 15;
   const int slot = blockIdx.x, grp = blockIdx.y, part = blockIdx.z;
   const int rep = a.H / a.G, h0 = grp * rep + (int)((long long)rep * part / a.splits),
             h1 = grp * rep + (int)((long long)rep * (part + 1) / a.splits);
   const SsmSeq q = ssm_find(a, slot, kSsmC);
   const int ch = slot - ssm_slot0(a, q, kSsmC);
   if (ch < 0 || (long long)ch * kSsmC >= q.len) {   // a slot of no chunk
-    for (int i = tid; i < (h1 - h0) * kPart; i += 256) a.part[((size_t)slot * a.H + h0) * kPart + i] = 0.0f;
+    for (int i = tid; i < (h1 - h0) * kPart; i += 512) a.part[((size_t)slot * a.H + h0) * kPart + i] = 0.0f;
     return;
   }
   const int first = q.first + ch * kSsmC, len = min(kSsmC, q.len - ch * kSsmC);
   const size_t row0 = (size_t)q.batch * a.T + first, pn = (size_t)a.P * N;
   const int tok = 16 * w + c;
-  f32x4 dB[NT], dC[NT], CB[4];
+  const int turns = a.P / kPw;
+  const auto scal = [&](int h) { return reinterpret_cast<float*>(smem + L::scal) + (h & 1) * kSmFloats; };
+  const auto sums = [&](int h) { return reinterpret_cast<float*>(smem + L::sum) + (h & 1) * L::sums; };
+  const auto issue = [&](int h, int t, char* buf) {
+    const T* x = reinterpret_cast<const T*>(a.x) + q.batch * a.xs[0] + first * a.xs[1] + h * a.xs[2] + t * kPw;
+    const T* dy = reinterpret_cast<const T*>(a.dy) + (row0 * a.H + h) * a.P + t * kPw;
+    const size_t at = ((size_t)slot * a.H + h) * pn * 4;
+    VR::template dma<8>(buf + L::X, x, (int)(a.xs[1] * sizeof(T)), len, wave, lane);
+    VR::template dma<8>(buf + L::dY, dy, (int)((long long)a.H * a.P * sizeof(T)), len, wave, lane);
 #pragma unroll
-  for (int j = 0; j < NT; ++j) dB[j] = dC[j] = zero4();
+    for (int u = 0; u < SsmState<T>::planes; ++u) {
+      const size_t pl = at + (u * pn + (size_t)t * kPw * N) * sizeof(T);
+      SR::template dma<8>(buf + L::S + u * SR::bytes, a.S_chunks + pl, SR::RB, kPw, wave, lane);
+      SR::template dma<8>(buf + L::E + u * SR::bytes, a.E_chunks + pl, SR::RB, kPw, wave, lane);
+    }
+  };
+  // dt and the scalars of a head, by wave 0
+  const auto dt_of = [&](int h) {
+    return lane < len ? (float)(reinterpret_cast<const T*>(a.dt) + q.batch * a.ds[0] + h)[(first + lane) * a.ds[1]] : 0.0f;
+  };
+  const auto bias_of = [&](int h) { return a.dt_bias ? a.dt_bias[h] : 0.0f; };
+  // what remains of a head when all its sums are there, by wave 0
+  const auto finish = [&](int h, float raw) {
+    const float *sc = scal(h), *sR = sums(h), *sE = sR + kSsmC, *sM = sE + kSsmC, *sDiag = sM + kSsmC, *sRect = sDiag + kSsmC,
+                *sES = sRect + 4 * kSsmC;
+    const bool in = lane < len;
+    const float d = sc[kSmD * kSsmC + lane], e = sE[lane], A = a.A[h];
+    float suf = in ? sR[lane] : 0.0f, pre = in ? d * e : 0.0f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) CB[i] = zero4();
-  KR::template dma<4>(smem + L::B, reinterpret_cast<const T*>(a.Bm) + q.batch * a.bs[0] + first * a.bs[1] + grp * a.bs[2],
-                      (int)(a.bs[1] * sizeof(T)), len, w, lane);
-  KR::template dma<4>(smem + L::C, reinterpret_cast<const T*>(a.Cm) + q.batch * a.cs[0] + first * a.cs[1] + grp * a.cs[2],
-                      (int)(a.cs[1] * sizeof(T)), len, w, lane);
+    for (int s = 1; s < 64; s *= 2) {
+      const float dn = __shfl_down(suf, s), up = __shfl_up(pre, s);
+      if (lane + s < 64) suf += dn;
+      if (lane >= s) pre += up;
+    }
+    const float before = __shfl_up(pre, 1);
+    const float es = sc[kSmWhole] * ((sES[0] + sES[1]) + (sES[2] + sES[3]));
+    const float rect = (sRect[lane] + sRect[kSsmC + lane]) + (sRect[2 * kSsmC + lane] + sRect[3 * kSsmC + lane]);
+    const float da = suf + (lane > 0 ? before : 0.0f) + rect + es;
+    float dd = A * da + (sM[lane] + e);
+    if (a.softplus) {
+      const float z = raw + bias_of(h), ez = expf(-fabsf(z));
+      dd *= (z >= 0.0f ? 1.0f : ez) / (1.0f + ez);
+    }
+    if (in) reinterpret_cast<T*>(a.ddt)[(row0 + lane) * a.H + h] = (T)dd;
+    const float sa = group_sum<64>(in ? d * da : 0.0f), sb = group_sum<64>(in ? dd : 0.0f), sd = group_sum<64>(in ? sDiag[lane] : 0.0f);
+    if (lane == 0) *reinterpret_cast<f32x4*>(a.part + ((size_t)slot * a.H + h) * kPart) = f32x4{sa, sb, sd, 0.0f};
+  };
+  KR::template dma<8>(smem + L::B, reinterpret_cast<const T*>(a.Bm) + q.batch * a.bs[0] + first * a.bs[1] + grp * a.bs[2],
+                      (int)(a.bs[1] * sizeof(T)), len, wave, lane);
+  KR::template dma<8>(smem + L::C, reinterpret_cast<const T*>(a.Cm) + q.batch * a.cs[0] + first * a.cs[1] + grp * a.cs[2],
+                      (int)(a.cs[1] * sizeof(T)), len, wave, lane);
+  if (L::ahead) issue(h0, 0, smem + L::turn);
+  float raw = 0.0f, was = 0.0f;
+  if (wave == 0) {
+    raw = dt_of(h0);
+    ssm_scalars(raw, lane < len, bias_of(h0), a.A[h0], a.softplus, lane, scal(h0));
+  }
+  f32x4 acc[NT];   // dC^T or dB^T: rows n, the tile's tokens
+#pragma unroll
+  for (int j = 0; j < NT; ++j) acc[j] = zero4();
+  int parity = 0;
 #pragma unroll 1
   for (int h = h0; h < h1; ++h) {
-    const T* x = reinterpret_cast<const T*>(a.x) + q.batch * a.xs[0] + first * a.xs[1] + h * a.xs[2];
-    const T* dy = reinterpret_cast<const T*>(a.dy) + (row0 * a.H + h) * a.P;
-    T* dx = reinterpret_cast<T*>(a.dx) + (row0 * a.H + h) * a.P;
-    const char* S = a.S_chunks + ((size_t)slot * a.H + h) * pn * 4;
-    const char* E = a.E_chunks + ((size_t)slot * a.H + h) * pn * 4;
-    const float skip = a.D ? a.D[h] : 0.0f, bias = a.dt_bias ? a.dt_bias[h] : 0.0f, A = a.A[h];
-    float raw = 0.0f;
-    if (w == 0 && lane < len) raw = (float)(reinterpret_cast<const T*>(a.dt) + q.batch * a.ds[0] + h)[(first + lane) * a.ds[1]];
-    f32x4 QT[4], Q[4];       // Q of tile w's dy (columns) and of its x
-    Fi<T, kNear> Lf[2];      // L C B^T, rows i, columns j of tile w
-    f32x4 LC[4];
-    float r = 0.0f, ex = 0.0f, es = 0.0f, dj = 0.0f, endj = 0.0f, gami = 0.0f;
+    // Q against the wave's tile: x (rows j) against its dy, or dy (rows i) against its x;
+    // L C B^T, rows i, columns j of the tile
+    f32x4 Q[4], LC[4];
+    float r = 0.0f, es = 0.0f, mine = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) QT[i] = Q[i] = LC[i] = zero4();
+    for (int i = 0; i < 4; ++i) Q[i] = LC[i] = zero4();
+    const float* sc = scal(h);
 #pragma unroll 1
-    for (int p0 = 0; p0 < a.P; p0 += kPw) {
-      __syncthreads();   // what the turn before read may be overwritten
-      VR::template dma<4>(smem + L::X, x + p0, (int)(a.xs[1] * sizeof(T)), len, w, lane);
-      VR::template dma<4>(smem + L::dY, dy + p0, (int)((long long)a.H * a.P * sizeof(T)), len, w, lane);
-#pragma unroll
-      for (int u = 0; u < SsmState<T>::planes; ++u) {
-        const size_t at = (u * pn + (size_t)p0 * N) * sizeof(T);
-        SR::template dma<4>(smem + L::S + u * SR::bytes, S + at, SR::RB, kPw, w, lane);
-        SR::template dma<4>(smem + L::E + u * SR::bytes, E + at, SR::RB, kPw, w, lane);
+    for (int t = 0; t < turns; ++t) {
+      char* buf = smem + L::turn + parity * L::one;
+      if (L::ahead) {
+        vm_wait_all();
+        __syncthreads();   // this turn's rows are there, the other buffer's are no longer read
+        parity ^= 1;
+        if (t + 1 < turns) issue(h, t + 1, smem + L::turn + parity * L::one);
+        else if (h + 1 < h1) issue(h + 1, 0, smem + L::turn + parity * L::one);
+      } else {
+        __syncthreads();
+        issue(h, t, buf);
+        vm_wait_all();
+        __syncthreads();
       }
-      if (p0 == 0 && w == 0) ssm_scalars(raw, lane < len, bias, A, a.softplus, lane, sc);
-      vm_wait_all();
-      __syncthreads();
-      if (p0 == 0) {
-        dj = sc[kSmD * kSsmC + tok], endj = sc[kSmEnd * kSsmC + tok], gami = sc[kSmGam * kSsmC + tok];
-        if (h == h0) {
+      renew(g, c);
+      if (t == 0 && wave == 0) {
+        if (h > h0) finish(h - 1, was);
+        was = raw;
+        if (h + 1 < h1) raw = dt_of(h + 1);
+      }
+      if (!back) {
+        const Fr<T> fy = VR::nat(buf + L::dY, w, 0, g, c);
+        const float gam = sc[kSmGam * kSsmC + tok];
 #pragma unroll
-          for (int p = 0; p < NP; ++p) {
-            const Fr<T> fb = KR::nat(smem + L::B, w, p, g, c);
+        for (int i = 0; i < 4; ++i) Q[i] = mma<T>(VR::nat(buf + L::X, i, 0, g, c), fy, Q[i]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (i >= w) CB[i] = mma<T>(KR::nat(smem + L::C, i, p, g, c), fb, CB[i]);
-          }
+        for (int j = 0; j < NT; ++j) {
+          const f32x4 u = mma<T>(state_tr<T, N>(buf + L::S, j, g, c), fy, zero4()) * gam;
+          acc[j] += u;
+          r += dot4(u, Quad<T>::f32(KR::quad(smem + L::C, w, j, g, c)));
         }
-        // L C B^T below the diagonal
-        const float Gh = sc[kSmGh * kSsmC + tok], Gl = sc[kSmGl * kSsmC + tok];
+        // <E, S>, by pieces of 16 bytes (both lie alike in LDS)
+        for (int i = tid; i < SR::bytes / 16; i += 256) {
+          float e[Chunk16<T>::N], s[Chunk16<T>::N];
+#pragma unroll
+          for (int u = 0; u < Chunk16<T>::N; ++u) e[u] = s[u] = 0.0f;
+#pragma unroll
+          for (int pl = SsmState<T>::planes - 1; pl >= 0; --pl) {
+            float fe[Chunk16<T>::N], fs[Chunk16<T>::N];
+            Chunk16<T>::unpack(*reinterpret_cast<const u32x4_t*>(buf + L::E + pl * SR::bytes + 16 * i), fe);
+            Chunk16<T>::unpack(*reinterpret_cast<const u32x4_t*>(buf + L::S + pl * SR::bytes + 16 * i), fs);
+#pragma unroll
+            for (int u = 0; u < Chunk16<T>::N; ++u) e[u] += fe[u], s[u] += fs[u];
+          }
+#pragma unroll
+          for (int u = 0; u < Chunk16<T>::N; ++u) es += e[u] * s[u];
+        }
+        continue;
+      }
+      const float Gh = sc[kSmGh * kSsmC + tok], Gl = sc[kSmGl * kSsmC + tok];
+      const float dj = sc[kSmD * kSsmC + tok], endj = sc[kSmEnd * kSsmC + tok];
+      if (t == 0) {
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+          const Fr<T> fb = KR::nat(smem + L::B, w, p, g, c);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) LC[i] = mma<T>(KR::nat(smem + L::C, i, p, g, c), fb, LC[i]);
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if (i < w) continue;   // (uniform)
           const f32x4 gh = four(sc + kSmGh * kSsmC + 16 * i + 4 * g), gl = four(sc + kSmGl * kSsmC + 16 * i + 4 * g);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int t = 16 * i + 4 * g + e;
-            LC[i][e] = t >= tok && t < len ? decay_exp((gh[e] - Gh) + (gl[e] - Gl)) * CB[i][e] : 0.0f;
+            const int i1 = 16 * i + 4 * g + e;
+            LC[i][e] = i1 >= tok && i1 < len ? decay_exp((gh[e] - Gh) + (gl[e] - Gl)) * LC[i][e] : 0.0f;
           }
         }
-#pragma unroll
-        for (int s = 0; s < 2; ++s) Lf[s] = to_fi<T, kNear>(LC[2 * s], LC[2 * s + 1]);
       }
-      const Fr<T> fx = VR::nat(smem + L::X, w, 0, g, c), fy = VR::nat(smem + L::dY, w, 0, g, c);
+      const Fr<T> fx = VR::nat(buf + L::X, w, 0, g, c);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (i >= w) Q[i] = mma<T>(VR::nat(smem + L::dY, i, 0, g, c), fx, Q[i]);
-        if (i <= w) QT[i] = mma<T>(VR::nat(smem + L::X, i, 0, g, c), fy, QT[i]);
-      }
-      // dC and dB of the states, a tile of n at a time
+      for (int i = 0; i < 4; ++i) Q[i] = mma<T>(VR::nat(buf + L::dY, i, 0, g, c), fx, Q[i]);
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const f32x4 u = mma<T>(state_tr<T, N>(smem + L::S, j, g, c), fy, zero4()) * gami;
-        dC[j] += u;
-        r += dot4(u, Quad<T>::f32(KR::quad(smem + L::C, w, j, g, c)));
-        const f32x4 v = mma<T>(state_tr<T, N>(smem + L::E, j, g, c), fx, zero4());
-        dB[j] += v * (dj * endj);
-      }
+      for (int j = 0; j < NT; ++j) acc[j] += mma<T>(state_tr<T, N>(buf + L::E, j, g, c), fx, zero4()) * (dj * endj);
       // dx: two tiles of p
+      T* dx = reinterpret_cast<T*>(a.dx) + (row0 * a.H + h) * a.P + t * kPw;
+      const float skip = a.D ? a.D[h] : 0.0f;
+      const Fi<T, kNear> Lf[2] = {to_fi<T, kNear>(LC[0], LC[1]), to_fi<T, kNear>(LC[2], LC[3])};
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
+      for (int v = 0; v < 2; ++v) {
         f32x4 u = zero4(), z = zero4();
 #pragma unroll
-        for (int p = 0; p < NP; ++p) u = mma<T>(state_nat<T, N>(smem + L::E, t, p, g, c), KR::nat(smem + L::B, w, p, g, c), u);
+        for (int p = 0; p < NP; ++p) u = mma<T>(state_nat<T, N>(buf + L::E, v, p, g, c), KR::nat(smem + L::B, w, p, g, c), u);
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
-          if (s >= w / 2) z = mma<T>(VR::tr32(smem + L::dY, s, t, g, c), Lf[s], z);
+        for (int s = 0; s < 2; ++s) z = mma<T>(VR::tr32(buf + L::dY, s, v, g, c), Lf[s], z);
         u *= endj;
-        ex += dot4(u, Quad<T>::f32(VR::quad(smem + L::X, w, t, g, c)));
-        const f32x4 o = (u + z) * dj + Quad<T>::f32(VR::quad(smem + L::dY, w, t, g, c)) * skip;
-        if (tok < len) Quad<T>::st(dx + (size_t)tok * a.H * a.P + p0 + 16 * t + 4 * g, Quad<T>::cvt(o));
-      }
-      // <E, S>, by pieces of 16 bytes (both lie alike in LDS)
-      for (int i = tid; i < SR::bytes / 16; i += 256) {
-        float e[Chunk16<T>::N], s[Chunk16<T>::N];
-#pragma unroll
-        for (int u = 0; u < Chunk16<T>::N; ++u) e[u] = s[u] = 0.0f;
-#pragma unroll
-        for (int pl = SsmState<T>::planes - 1; pl >= 0; --pl) {
-          float fe[Chunk16<T>::N], fs[Chunk16<T>::N];
-          Chunk16<T>::unpack(*reinterpret_cast<const u32x4_t*>(smem + L::E + pl * SR::bytes + 16 * i), fe);
-          Chunk16<T>::unpack(*reinterpret_cast<const u32x4_t*>(smem + L::S + pl * SR::bytes + 16 * i), fs);
-#pragma unroll
-          for (int u = 0; u < Chunk16<T>::N; ++u) e[u] += fe[u], s[u] += fs[u];
-        }
-#pragma unroll
-        for (int u = 0; u < Chunk16<T>::N; ++u) es += e[u] * s[u];
+        r += dot4(u, Quad<T>::f32(VR::quad(buf + L::X, w, v, g, c)));
+        const f32x4 o = (u + z) * dj + Quad<T>::f32(VR::quad(buf + L::dY, w, v, g, c)) * skip;
+        if (tok < len) Quad<T>::st(dx + (size_t)tok * a.H * a.P + 16 * v + 4 * g, Quad<T>::cvt(o));
       }
     }
-    // what pairs of tokens add: rows j (dC) and rows i (dB) against the wave's tile
-    {
-      const float Gh = sc[kSmGh * kSsmC + tok], Gl = sc[kSmGl * kSsmC + tok];
-      f32x4 V[4], M[4];
-      float cm = 0.0f, diag = 0.0f;
+    // what pairs of tokens add
+    const float Gh = sc[kSmGh * kSsmC + tok], Gl = sc[kSmGl * kSsmC + tok], dj = sc[kSmD * kSsmC + tok];
+    float* sum = sums(h);
+    renew(g, c);
+    if (!back) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        V[i] = M[i] = zero4();
         const f32x4 gh = four(sc + kSmGh * kSsmC + 16 * i + 4 * g), gl = four(sc + kSmGl * kSsmC + 16 * i + 4 * g);
         const f32x4 d = four(sc + kSmD * kSsmC + 16 * i + 4 * g);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int t = 16 * i + 4 * g + e;
-          if (i >= w) {
-            const bool on = t >= tok && t < len;
-            V[i][e] = on ? decay_exp((gh[e] - Gh) + (gl[e] - Gl)) * dj * Q[i][e] : 0.0f;
-            M[i][e] = on ? LC[i][e] * Q[i][e] : 0.0f;
-            cm += M[i][e];
-            M[i][e] *= dj;
-            if (t == tok) diag = Q[i][e];
-          }
-          if (i <= w) QT[i][e] = t <= tok ? decay_exp((Gh - gh[e]) + (Gl - gl[e])) * d[e] * QT[i][e] : 0.0f;
-        }
+        for (int e = 0; e < 4; ++e)
+          Q[i][e] = 16 * i + 4 * g + e <= tok ? decay_exp((Gh - gh[e]) + (Gl - gl[e])) * d[e] * Q[i][e] : 0.0f;
       }
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        if (s <= w / 2) {
-          const Fi<T, kNear> f = to_fi<T, kNear>(QT[2 * s], QT[2 * s + 1]);
+        if (s > w / 2) continue;   // (uniform)
+        const Fi<T, kNear> f = to_fi<T, kNear>(Q[2 * s], Q[2 * s + 1]);
 #pragma unroll
-          for (int j = 0; j < NT; ++j) dC[j] = mma<T>(KR::tr32(smem + L::B, s, j, g, c), f, dC[j]);
-        }
-        if (s >= w / 2) {
-          const Fi<T, kNear> f = to_fi<T, kNear>(V[2 * s], V[2 * s + 1]);
-#pragma unroll
-          for (int j = 0; j < NT; ++j) dB[j] = mma<T>(KR::tr32(smem + L::C, s, j, g, c), f, dB[j]);
-        }
+        for (int j = 0; j < NT; ++j) acc[j] = mma<T>(KR::tr32(smem + L::B, s, j, g, c), f, acc[j]);
       }
-      // sums of M over i >= t and j < t: suffix sums down each column, then along rows
-      float carry = 0.0f;
-#pragma unroll
-      for (int i = 3; i >= 0; --i) {
-        f32x4 suf = zero4();
-        if (i >= w) {   // (uniform)
-          suf[3] = M[i][3];
-#pragma unroll
-          for (int e = 2; e >= 0; --e) suf[e] = M[i][e] + suf[e + 1];
-          float in = suf[0];
-          const float n1 = __shfl(in, (lane + 16) & 63);
-          in += g < 3 ? n1 : 0.0f;
-          const float n2 = __shfl(in, (lane + 32) & 63);
-          in += g < 2 ? n2 : 0.0f;
-          const float behind = __shfl(in, (lane + 16) & 63), whole = __shfl(in, c);
-          const float more = carry + (g < 3 ? behind : 0.0f);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) suf[e] = 16 * i + 4 * g + e > tok ? suf[e] + more : 0.0f;
-          carry += whole;
-        }
-        const float rect = row_sum4(suf, c);
-        if (c < 4) sRect[w * kSsmC + 16 * i + 4 * g + c] = rect;
-      }
-      r = col_sum(r), ex = col_sum(ex), cm = col_sum(cm), diag = col_sum(diag);
+      r = col_sum(r);
       es = group_sum<64>(es);
-      if (g == 0) sR[tok] = r, sE[tok] = ex, sM[tok] = cm, sDiag[tok] = diag;
-      if (lane == 0) sES[w] = es;
+      if (g == 0) sum[tok] = r;
+      if (lane == 0) sum[8 * kSsmC + w] = es;
+      if (wave == 0 && h + 1 < h1) ssm_scalars(raw, lane < len, bias_of(h + 1), a.A[h + 1], a.softplus, lane, scal(h + 1));
+      continue;
     }
-    __syncthreads();
-    if (w == 0) {   // (the next head's turns write these places behind their first barriers)
-      const bool in = lane < len;
-      const float d = sc[kSmD * kSsmC + lane], e = sE[lane];
-      float suf = in ? sR[lane] : 0.0f, pre = in ? d * e : 0.0f;
+    float cm = 0.0f;
 #pragma unroll
-      for (int s = 1; s < 64; s *= 2) {
-        const float dn = __shfl_down(suf, s), up = __shfl_up(pre, s);
-        if (lane + s < 64) suf += dn;
-        if (lane >= s) pre += up;
+    for (int i = 0; i < 4; ++i) {
+      const f32x4 gh = four(sc + kSmGh * kSsmC + 16 * i + 4 * g), gl = four(sc + kSmGl * kSsmC + 16 * i + 4 * g);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int i1 = 16 * i + 4 * g + e;
+        const bool on = i1 >= tok && i1 < len;
+        LC[i][e] = on ? LC[i][e] * Q[i][e] : 0.0f;   // M
+        cm += LC[i][e];
+        LC[i][e] *= dj;
+        mine = i1 == tok ? Q[i][e] : mine;
+        Q[i][e] = on ? decay_exp((gh[e] - Gh) + (gl[e] - Gl)) * dj * Q[i][e] : 0.0f;
       }
-      const float before = __shfl_up(pre, 1);
-      const float es4 = sc[kSmWhole] * ((sES[0] + sES[1]) + (sES[2] + sES[3]));
-      const float rect = (sRect[lane] + sRect[kSsmC + lane]) + (sRect[2 * kSsmC + lane] + sRect[3 * kSsmC + lane]);
-      const float da = suf + (lane > 0 ? before : 0.0f) + rect + es4;
-      float dd = A * da + (sM[lane] + e);
-      if (a.softplus) {
-        const float z = raw + bias, ez = expf(-fabsf(z));
-        dd *= (z >= 0.0f ? 1.0f : ez) / (1.0f + ez);
-      }
-      if (in) reinterpret_cast<T*>(a.ddt)[(row0 + lane) * a.H + h] = (T)dd;
-      const float sa = group_sum<64>(in ? d * da : 0.0f), sb = group_sum<64>(in ? dd : 0.0f), sd = group_sum<64>(in ? sDiag[lane] : 0.0f);
-      if (lane == 0) *reinterpret_cast<f32x4*>(a.part + ((size_t)slot * a.H + h) * kPart) = f32x4{sa, sb, sd, 0.0f};
     }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      if (s < w / 2) continue;   // (uniform)
+      const Fi<T, kNear> f = to_fi<T, kNear>(Q[2 * s], Q[2 * s + 1]);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) acc[j] = mma<T>(KR::tr32(smem + L::C, s, j, g, c), f, acc[j]);
+    }
+    // sums of M over i >= t and j < t: suffix sums down each column, then along rows
+    float carry = 0.0f;
+#pragma unroll
+    for (int i = 3; i >= 0; --i) {
+      f32x4 suf;
+      suf[3] = LC[i][3];
+#pragma unroll
+      for (int e = 2; e >= 0; --e) suf[e] = LC[i][e] + suf[e + 1];
+      float in = suf[0];
+      const float n1 = __shfl(in, (lane + 16) & 63);
+      in += g < 3 ? n1 : 0.0f;
+      const float n2 = __shfl(in, (lane + 32) & 63);
+      in += g < 2 ? n2 : 0.0f;
+      const float behind = __shfl(in, (lane + 16) & 63), whole = __shfl(in, c);
+      const float more = carry + (g < 3 ? behind : 0.0f);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) suf[e] = 16 * i + 4 * g + e > tok ? suf[e] + more : 0.0f;
+      carry += whole;
+      const float rect = row_sum4(suf, c);
+      if (c < 4) sum[(4 + w) * kSsmC + 16 * i + 4 * g + c] = rect;
+    }
+    r = col_sum(r), cm = col_sum(cm), mine = col_sum(mine);
+    if (g == 0) sum[kSsmC + tok] = r, sum[2 * kSsmC + tok] = cm, sum[3 * kSsmC + tok] = mine;
   }
+  __syncthreads();
+  if (wave == 0) finish(h1 - 1, was);
+  settle();
   if (tok < len) {
     const size_t at = ((row0 + tok) * a.G + grp) * N + 4 * g;
     if (a.splits == 1) {
+      T* out = reinterpret_cast<T*>(back ? a.dBm : a.dCm) + at;
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        Quad<T>::st(reinterpret_cast<T*>(a.dBm) + at + 16 * j, Quad<T>::cvt(dB[j]));
-        Quad<T>::st(reinterpret_cast<T*>(a.dCm) + at + 16 * j, Quad<T>::cvt(dC[j]));
-      }
+      for (int j = 0; j < NT; ++j) Quad<T>::st(out + 16 * j, Quad<T>::cvt(acc[j]));
     } else {
       const size_t all = (size_t)(a.offsets ? 1 : a.nseq) * a.T * a.G * N;
-      float* out = a.dBp + (size_t)part * 2 * all + at;
+      float* out = a.dBp + ((size_t)part * 2 + (back ? 0 : 1)) * all + at;
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        *reinterpret_cast<f32x4*>(out + 16 * j) = dB[j];
-        *reinterpret_cast<f32x4*>(out + all + 16 * j) = dC[j];
-      }
+      for (int j = 0; j < NT; ++j) *reinterpret_cast<f32x4*>(out + 16 * j) = acc[j];
     }
   }
 }
@@ -363,7 +397,7 @@ int launch_t(const SsmArgs& a, hipStream_t s, void (*mark)(hipStream_t)) {
   const auto kern = carve_ssm_grad_kernel<T, N>;
   if (hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
     return CARVE_ERR_HIP;
-  hipLaunchKernelGGL(kern, dim3(a.nslots, a.G, a.splits), dim3(256), lds, s, a);
+  hipLaunchKernelGGL(kern, dim3(a.nslots, a.G, a.splits), dim3(512), lds, s, a);
   int st = launched();
   if (st) return st;
   mark(s);

@@ -41,10 +41,6 @@ struct Tile {
 
 __device__ __forceinline__ f32x4 four(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
 
-// Behind a loop whose last instructions are products: the stores that follow read their
-// results, and the compiler leaves them a wait state short there.
-__device__ __forceinline__ void settle() { asm volatile("s_nop 7" ::: "memory"); }
-
 // The steps of a span's chunks, a chunk ahead: one wave holds the next chunk's dt and makes
 // its scalars while the others' rows are on their way.
 template <typename T>
