@@ -151,6 +151,12 @@ struct SsmState {
 };
 
 // ---- odds and ends ------------------------------------------------------------------------
+// v where `on`, else 0, without a branch around what v takes (the compiler makes one of a
+// plain choice: sixteen of them cost more than the exponentials that they skip)
+__device__ __forceinline__ float masked(bool on, float v) {
+  asm("" : "+v"(v));
+  return on ? v : 0.0f;
+}
 // Behind a loop whose last instructions are products: the stores that follow read their
 // results, and the compiler leaves them a wait state short there.
 __device__ __forceinline__ void settle() { asm volatile("s_nop 7" ::: "memory"); }

@@ -74,10 +74,16 @@ __global__ void __launch_bounds__(512, 2) carve_ssm_grad_kernel(SsmArgs a) {
   typedef typename L::SR SR;
   constexpr int NP = N / 32, NT = N / 16;
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const bool back = wave >= 4;   // (uniform) dB and dx
   const int w = wave & 3;
-  int g = lane >> 4, c = lane & 15;
+  int lane = tid & 63, g = lane >> 4, c = lane & 15, tok = 16 * w + c;
+  // (coordinates the compiler takes as new: addresses are formed where they are used, not
+  // all of them ahead of the loops and kept)
+  const auto anew = [&]() {
+    asm volatile("" : "+v"(lane));
+    g = lane >> 4, c = lane & 15, tok = 16 * w + c;
+  };
   const int slot = blockIdx.x, grp = blockIdx.y, part = blockIdx.z;
   const int rep = a.H / a.G, h0 = grp * rep + (int)((long long)rep * part / a.splits),
             h1 = grp * rep + (int)((long long)rep * (part + 1) / a.splits);
@@ -89,7 +95,6 @@ __global__ void __launch_bounds__(512, 2) carve_ssm_grad_kernel(SsmArgs a) {
   }
   const int first = q.first + ch * kSsmC, len = min(kSsmC, q.len - ch * kSsmC);
   const size_t row0 = (size_t)q.batch * a.T + first, pn = (size_t)a.P * N;
-  const int tok = 16 * w + c;
   const int turns = a.P / kPw;
   const auto scal = [&](int h) { return reinterpret_cast<float*>(smem + L::scal) + (h & 1) * kSmFloats; };
   const auto sums = [&](int h) { return reinterpret_cast<float*>(smem + L::sum) + (h & 1) * L::sums; };
@@ -163,6 +168,7 @@ __global__ void __launch_bounds__(512, 2) carve_ssm_grad_kernel(SsmArgs a) {
 #pragma unroll 1
     for (int t = 0; t < turns; ++t) {
       char* buf = smem + L::turn + parity * L::one;
+      anew();
       if (L::ahead) {
         vm_wait_all();
         __syncthreads();   // this turn's rows are there, the other buffer's are no longer read
@@ -175,7 +181,7 @@ __global__ void __launch_bounds__(512, 2) carve_ssm_grad_kernel(SsmArgs a) {
         vm_wait_all();
         __syncthreads();
       }
-      renew(g, c);
+      anew();
       if (t == 0 && wave == 0) {
         if (h > h0) finish(h - 1, was);
         was = raw;
@@ -193,7 +199,7 @@ __global__ void __launch_bounds__(512, 2) carve_ssm_grad_kernel(SsmArgs a) {
           r += dot4(u, Quad<T>::f32(KR::quad(smem + L::C, w, j, g, c)));
         }
         // <E, S>, by pieces of 16 bytes (both lie alike in LDS)
-        for (int i = tid; i < SR::bytes / 16; i += 256) {
+        for (int i = 64 * w + lane; i < SR::bytes / 16; i += 256) {
           float e[Chunk16<T>::N], s[Chunk16<T>::N];
 #pragma unroll
           for (int u = 0; u < Chunk16<T>::N; ++u) e[u] = s[u] = 0.0f;
@@ -225,7 +231,7 @@ __global__ void __launch_bounds__(512, 2) carve_ssm_grad_kernel(SsmArgs a) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int i1 = 16 * i + 4 * g + e;
-            LC[i][e] = i1 >= tok && i1 < len ? decay_exp((gh[e] - Gh) + (gl[e] - Gl)) * LC[i][e] : 0.0f;
+            LC[i][e] = masked((i1 >= tok) & (i1 < len), decay_exp((gh[e] - Gh) + (gl[e] - Gl)) * LC[i][e]);
           }
         }
       }
@@ -252,9 +258,9 @@ __global__ void __launch_bounds__(512, 2) carve_ssm_grad_kernel(SsmArgs a) {
       }
     }
     // what pairs of tokens add
+    anew();
     const float Gh = sc[kSmGh * kSsmC + tok], Gl = sc[kSmGl * kSsmC + tok], dj = sc[kSmD * kSsmC + tok];
     float* sum = sums(h);
-    renew(g, c);
     if (!back) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -262,7 +268,7 @@ __global__ void __launch_bounds__(512, 2) carve_ssm_grad_kernel(SsmArgs a) {
         const f32x4 d = four(sc + kSmD * kSsmC + 16 * i + 4 * g);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          Q[i][e] = 16 * i + 4 * g + e <= tok ? decay_exp((Gh - gh[e]) + (Gl - gl[e])) * d[e] * Q[i][e] : 0.0f;
+          Q[i][e] = masked(16 * i + 4 * g + e <= tok, decay_exp((Gh - gh[e]) + (Gl - gl[e])) * d[e] * Q[i][e]);
       }
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
@@ -285,12 +291,12 @@ __global__ void __launch_bounds__(512, 2) carve_ssm_grad_kernel(SsmArgs a) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int i1 = 16 * i + 4 * g + e;
-        const bool on = i1 >= tok && i1 < len;
-        LC[i][e] = on ? LC[i][e] * Q[i][e] : 0.0f;   // M
+        const bool on = (i1 >= tok) & (i1 < len);
+        LC[i][e] = masked(on, LC[i][e] * Q[i][e]);   // M
         cm += LC[i][e];
         LC[i][e] *= dj;
-        mine = i1 == tok ? Q[i][e] : mine;
-        Q[i][e] = on ? decay_exp((gh[e] - Gh) + (gl[e] - Gl)) * dj * Q[i][e] : 0.0f;
+        mine += masked(i1 == tok, Q[i][e]);
+        Q[i][e] = masked(on, decay_exp((gh[e] - Gh) + (gl[e] - Gl)) * dj * Q[i][e]);
       }
     }
 #pragma unroll
@@ -316,7 +322,7 @@ __global__ void __launch_bounds__(512, 2) carve_ssm_grad_kernel(SsmArgs a) {
       const float behind = __shfl(in, (lane + 16) & 63), whole = __shfl(in, c);
       const float more = carry + (g < 3 ? behind : 0.0f);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) suf[e] = 16 * i + 4 * g + e > tok ? suf[e] + more : 0.0f;
+      for (int e = 0; e < 4; ++e) suf[e] = masked(16 * i + 4 * g + e > tok, suf[e] + more);
       carry += whole;
       const float rect = row_sum4(suf, c);
       if (c < 4) sum[(4 + w) * kSsmC + 16 * i + 4 * g + c] = rect;
@@ -325,6 +331,7 @@ __global__ void __launch_bounds__(512, 2) carve_ssm_grad_kernel(SsmArgs a) {
     if (g == 0) sum[kSsmC + tok] = r, sum[2 * kSsmC + tok] = cm, sum[3 * kSsmC + tok] = mine;
   }
   __syncthreads();
+  anew();
   if (wave == 0) finish(h1 - 1, was);
   settle();
   if (tok < len) {

@@ -269,8 +269,7 @@ __global__ void __launch_bounds__(64 * NW) carve_ssm_out_kernel(SsmArgs a) {
         const f32x4 d = four(sc + kSmD * kSsmC + 16 * j + 4 * g);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const bool on = j < i || 4 * g + e <= c;
-          M[j][e] = on ? decay_exp((Gh - gh[e]) + (Gl - gl[e])) * d[e] * M[j][e] : 0.0f;
+          M[j][e] = masked((j < i) | (4 * g + e <= c), decay_exp((Gh - gh[e]) + (Gl - gl[e])) * d[e] * M[j][e]);
         }
       }
 #pragma unroll
