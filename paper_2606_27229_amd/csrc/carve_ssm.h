@@ -74,8 +74,11 @@ __device__ __forceinline__ SsmSeq ssm_find(const SsmArgs& a, int slot, int L) {
 }
 
 // ---- scalars of a chunk ---------------------------------------------------------------
-// d, G as two floats, e^G (0 behind the last token), e^{G_C - G}; then e^{G_C}
-enum : int { kSmD = 0, kSmGh = 1, kSmGl = 2, kSmGam = 3, kSmEnd = 4, kSmWhole = 5 * kSsmC, kSmFloats = 5 * kSsmC + 4 };
+// Of every token: d; G / log 2 as two floats (far below any other behind the last token, so
+// that what decays from a token before to one there is 0); e^G (0 there); E = e^{G_C - G};
+// E d.  Then e^{G_C}.
+enum : int { kSmD = 0, kSmGh = 1, kSmGl = 2, kSmGam = 3, kSmEnd = 4, kSmEndD = 5, kSmWhole = 6 * kSsmC, kSmFloats = 6 * kSsmC + 4 };
+constexpr float kSmNever = -1e5f;
 
 __device__ __forceinline__ float ssm_step_of(float z, int softplus) {
   return softplus ? fmaxf(z, 0.0f) + log1pf(expf(-fabsf(z))) : z;
@@ -85,21 +88,24 @@ __device__ __forceinline__ void ssm_scalars(float raw, bool in, float bias, floa
   const float d = in ? ssm_step_of(raw + bias, softplus) : 0.0f;
   float ga = in ? d * A : 0.0f;
   ga = ga < kGdrMinG ? kGdrMinG : ga;
-  double G = (double)ga;
+  double G = (double)ga * 1.4426950408889634;
 #pragma unroll
   for (int s = 1; s < 64; s *= 2) {
     const double up = __shfl_up(G, s);
     if (lane >= s) G += up;
   }
   const double all = __shfl(G, 63);
-  const float Gh = (float)G, Gl = (float)(G - (double)Gh);
+  const float Gh = (float)G, Gl = (float)(G - (double)Gh), end = exp2_f((float)(all - G));
   out[kSmD * kSsmC + lane] = d;
-  out[kSmGh * kSsmC + lane] = Gh;
-  out[kSmGl * kSsmC + lane] = Gl;
-  out[kSmGam * kSsmC + lane] = in ? decay_exp(Gh) * (1.0f + Gl) : 0.0f;
-  out[kSmEnd * kSsmC + lane] = decay_exp((float)(all - G));
-  if (lane == 0) out[kSmWhole] = decay_exp((float)all);
+  out[kSmGh * kSsmC + lane] = in ? Gh : kSmNever;
+  out[kSmGl * kSsmC + lane] = in ? Gl : 0.0f;
+  out[kSmGam * kSsmC + lane] = in ? exp2_f(Gh) * (1.0f + Gl * 0.69314718f) : 0.0f;
+  out[kSmEnd * kSsmC + lane] = end;
+  out[kSmEndD * kSsmC + lane] = end * d;
+  if (lane == 0) out[kSmWhole] = exp2_f((float)all);
 }
+// e^{G_i - G_j}
+__device__ __forceinline__ float decay_between(float ih, float il, float jh, float jl) { return exp2_f((ih - jh) + (il - jl)); }
 
 // ---- LDS tiles -------------------------------------------------------------------------
 // GdrRows of ROWS rows (its layout and operand reads); rows behind the last of `len`

@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(512, 2) carve_ssm_grad_kernel(SsmArgs a) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int i1 = 16 * i + 4 * g + e;
-            LC[i][e] = masked((i1 >= tok) & (i1 < len), decay_exp((gh[e] - Gh) + (gl[e] - Gl)) * LC[i][e]);
+            LC[i][e] = masked((i1 >= tok) & (i1 < len), decay_between(gh[e], gl[e], Gh, Gl) * LC[i][e]);
           }
         }
       }
@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(512, 2) carve_ssm_grad_kernel(SsmArgs a) {
         const f32x4 d = four(sc + kSmD * kSsmC + 16 * i + 4 * g);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          Q[i][e] = masked(16 * i + 4 * g + e <= tok, decay_exp((Gh - gh[e]) + (Gl - gl[e])) * d[e] * Q[i][e]);
+          Q[i][e] = masked(16 * i + 4 * g + e <= tok, decay_between(Gh, Gl, gh[e], gl[e]) * d[e] * Q[i][e]);
       }
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
@@ -296,7 +296,7 @@ __global__ void __launch_bounds__(512, 2) carve_ssm_grad_kernel(SsmArgs a) {
         cm += LC[i][e];
         LC[i][e] *= dj;
         mine += masked(i1 == tok, Q[i][e]);
-        Q[i][e] = masked(on, decay_exp((gh[e] - Gh) + (gl[e] - Gl)) * dj * Q[i][e]);
+        Q[i][e] = masked(on, decay_between(gh[e], gl[e], Gh, Gl) * dj * Q[i][e]);
       }
     }
 #pragma unroll

@@ -81,7 +81,7 @@ struct StateLds {
   static constexpr int K = 0, V = KR::bytes, S = V + VR::bytes, total = S + 2 * kSmFloats * 4;
 };
 template <typename T, int N, int NW, bool REV>
-__global__ void __launch_bounds__(64 * NW) carve_ssm_state_kernel(SsmArgs a, int full) {
+__global__ void __launch_bounds__(64 * NW, 2) carve_ssm_state_kernel(SsmArgs a, int full) {
   typedef StateLds<T, N, NW> L;
   typedef typename L::KR KR;
   typedef typename L::VR VR;
@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(64 * NW) carve_ssm_state_kernel(SsmArgs a, int
     __syncthreads();
     const Fr<T> v[2] = {VR::tr32(smem + L::V, 0, w, g, c), VR::tr32(smem + L::V, 1, w, g, c)};
     t.template add<KR>(smem + L::K, v, [&](int at) {
-      return REV ? four(sc + kSmGam * kSsmC + at) : four(sc + kSmEnd * kSsmC + at) * four(sc + kSmD * kSsmC + at);
+      return four(sc + (REV ? kSmGam : kSmEndD) * kSsmC + at);
     }, sc[kSmWhole], g, c);
     decay *= sc[kSmWhole];
   }
@@ -199,7 +199,7 @@ struct OutLds {
   static constexpr int S = P + img_bytes<T>(kNear), total = S + 2 * kSmFloats * 4;
 };
 template <typename T, int N, int NW>
-__global__ void __launch_bounds__(64 * NW) carve_ssm_out_kernel(SsmArgs a) {
+__global__ void __launch_bounds__(64 * NW, 2) carve_ssm_out_kernel(SsmArgs a) {
   typedef OutLds<T, N, NW> L;
   typedef typename L::KR KR;
   typedef typename L::VR VR;
@@ -269,7 +269,8 @@ __global__ void __launch_bounds__(64 * NW) carve_ssm_out_kernel(SsmArgs a) {
         const f32x4 d = four(sc + kSmD * kSsmC + 16 * j + 4 * g);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          M[j][e] = masked((j < i) | (4 * g + e <= c), decay_exp((Gh - gh[e]) + (Gl - gl[e])) * d[e] * M[j][e]);
+          M[j][e] *= decay_between(Gh, Gl, gh[e], gl[e]) * d[e];
+          if (j == i) M[j][e] = masked(4 * g + e <= c, M[j][e]);   // (uniform)
         }
       }
 #pragma unroll
@@ -293,7 +294,7 @@ __global__ void __launch_bounds__(64 * NW) carve_ssm_out_kernel(SsmArgs a) {
       o = o * sc[kSmGam * kSsmC + tok] + z + xv * skip;
       if (tok < len) Quad<T>::st(y + (size_t)(ch * kSsmC + tok) * yrow, Quad<T>::cvt(o));
     }
-    t.template add<KR>(smem + L::B, fx, [&](int at) { return four(sc + kSmEnd * kSsmC + at) * four(sc + kSmD * kSsmC + at); },
+    t.template add<KR>(smem + L::B, fx, [&](int at) { return four(sc + kSmEndD * kSsmC + at); },
                        sc[kSmWhole], g, c);
   }
   settle();
