@@ -1148,23 +1148,26 @@ int check_ssm(const carve_ssm_dims_t* d) {
   return CARVE_OK;
 }
 
+// value rows of a unit: 64, or 32 where P is no multiple of it or they would not fit the registers
+bool ssm_wide(const carve_ssm_dims_t* d) { return d->P % 64 == 0 && !(d->dtype == CARVE_F32 && d->S == 128); }
+
 // chunks of a span, spans (slots of them) and shares of a group's heads
 struct SsmPlan {
   size_t chunks, spans;
   int span, splits;
 };
-constexpr long long kSsmGroups = 1024;   // workgroups that spans are cut for
+// Spans: as many as let every compute unit hold one workgroup of the outputs (a pair of
+// units, see carve_ssm_fwd.hip), none shorter than kSsmMinSpan chunks.
+constexpr long long kSsmGroups = 256;
 constexpr int kSsmMinSpan = 4;
 SsmPlan ssm_plan(const carve_ssm_dims_t* d) {
   SsmPlan p;
   const long long units = (d->T + (long long)kSsmC - 1) / kSsmC;
   p.chunks = d->N ? (size_t)(d->T / kSsmC) + d->N : (size_t)(d->B * units);
-  const long long per = (long long)d->H * (d->P % 64 ? d->P / 32 : d->P / 64);
-  long long span = ((d->N ? 1 : d->B) * units * per + kSsmGroups - 1) / kSsmGroups;
-  if (span < kSsmMinSpan) span = kSsmMinSpan;
-  if (span > units) span = units;
-  // (equal ones)
-  const long long n = (units + span - 1) / span;
+  const long long per = (long long)d->G * ((d->H / d->G * (d->P / (ssm_wide(d) ? 64 : 32)) + 1) / 2) * d->B;
+  long long n = kSsmGroups / per;
+  if (n > (units + kSsmMinSpan - 1) / kSsmMinSpan) n = (units + kSsmMinSpan - 1) / kSsmMinSpan;
+  if (n < 1) n = 1;
   p.span = (int)((units + n - 1) / n);
   const long long L = (long long)p.span * kSsmC;
   p.spans = d->N ? (size_t)(d->T / L) + d->N : (size_t)(d->B * ((d->T + L - 1) / L));

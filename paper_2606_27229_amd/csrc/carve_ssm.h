@@ -137,21 +137,62 @@ struct SsmRows : GdrRows<T, COLS> {
   }
 };
 
-// States kept for the backward, a head's [P][N]: f32, or with bf16 tokens two planes of
-// bf16, the upper and the lower half of the significand's first 16 bits (as many bytes).
-// They only enter products towards bf16 results, and matrix cores take the planes as they
-// are: the gradients' kernel needs no conversion of them (its LDS holds them as loaded).
-template <typename T>
+// States kept for the backward, a head's P x N values of 4 bytes in blocks of 16 rows p by
+// 64 bytes of n, so that a wave's store is 1 KB in one piece: f32, or with bf16 tokens two
+// planes of bf16, the upper and the lower half of the significand's first 16 bits (as many
+// bytes).  They only enter products towards bf16 results and the sums of dA, and matrix
+// cores take the planes as they are: the gradients' kernel needs no conversion of them (its
+// LDS holds them as loaded).
+template <typename T, int N>
 struct SsmState {
   static constexpr int planes = sizeof(T) == 2 ? 2 : 1;
-  // lane's four neighbouring n of row p
-  static __device__ __forceinline__ void st(char* head, size_t pn, size_t at, f32x4 v) {
+  static constexpr int BN = 64 / (int)sizeof(T);       // n of a block
+  // bytes of 16-byte piece x of row p
+  static __device__ __forceinline__ unsigned at(int p, int x) {
+    return (unsigned)(((p >> 4) * (N / BN) + (x >> 2)) * 1024 + (p & 15) * 64 + (x & 3) * 16);
+  }
+  // the values of 16 rows from p0 as they lie in registers (lane (g, c): n = 16 j + 4 g + e,
+  // row p0 + c); head: the head's values, of pn elements
+  static __device__ __forceinline__ void st(char* head, size_t pn, int p0, const f32x4 (&S)[N / 16], int lane) {
     if constexpr (sizeof(T) == 2) {
-      const bf16x4 hi = Quad<T>::cvt(v);
-      *reinterpret_cast<bf16x4*>(head + 2 * at) = hi;
-      *reinterpret_cast<bf16x4*>(head + 2 * pn + 2 * at) = Quad<T>::cvt(bf16_rest(v, hi));
+      char* to = head + (p0 >> 4) * (N / BN) * 1024;
+      const int g = lane >> 4, c = lane & 15;
+      // tile 2 u's values go to even rows of lanes, tile 2 u + 1's to odd ones: eight
+      // neighbouring n a lane
+      const unsigned off = (unsigned)(c * 64 + (g & 1) * 32 + (g >> 1) * 16);
+#pragma unroll
+      for (int u = 0; u < N / 32; ++u) {
+        f32x4 a = S[2 * u], b = S[2 * u + 1];
+#pragma unroll
+        for (int pl = 0; pl < 2; ++pl) {
+          const bf16x4 ha = Quad<bf16_t>::cvt(a), hb = Quad<bf16_t>::cvt(b);
+          const u32x2_t ua = __builtin_bit_cast(u32x2_t, ha), ub = __builtin_bit_cast(u32x2_t, hb);
+          const auto r0 = __builtin_amdgcn_permlane16_swap(ua[0], ub[0], false, false);
+          const auto r1 = __builtin_amdgcn_permlane16_swap(ua[1], ub[1], false, false);
+          const u32x4_t v = {r0[0], r1[0], r0[1], r1[1]};
+          *reinterpret_cast<u32x4_t*>(to + pl * 2 * pn + u * 1024 + off) = v;
+          if (pl == 0) a = bf16_rest(a, ha), b = bf16_rest(b, hb);
+        }
+      }
     } else {
-      *reinterpret_cast<f32x4*>(head + 4 * at) = v;
+      char* to = head + (p0 >> 4) * (N / BN) * 1024 + (lane & 15) * 64 + (lane >> 4) * 16;
+#pragma unroll
+      for (int j = 0; j < N / 16; ++j) *reinterpret_cast<f32x4*>(to + j * 1024) = S[j];
+    }
+  }
+  // rows p0 .. p0 + ROWS - 1 of a plane into LDS as SsmRows<T, N, ROWS> lies there
+  template <int ROWS, int NW>
+  static __device__ __forceinline__ void dma(char* lds, const char* plane, int p0, int w, int lane) {
+    typedef SsmRows<T, N, ROWS> R;
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<char*>(plane) + (p0 >> 4) * (N / BN) * 1024, 0, R::bytes, 0x00027000);
+    constexpr int RPI = 1024 / R::RB;
+#pragma unroll
+    for (int u = 0; u < (R::bytes / 1024 + NW - 1) / NW; ++u) {
+      const int i = w + NW * u;
+      if ((R::bytes / 1024) % NW != 0 && i >= R::bytes / 1024) break;   // (uniform)
+      const int row = i * RPI + lane / R::NCH, x = (lane % R::NCH) ^ R::swz(row);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, lds_at(lds + 1024 * i), 16, (int)at(row, x), 0, 0, 0);
     }
   }
 };

@@ -31,7 +31,7 @@ struct GradLds {
   typedef SsmRows<T, N, kSsmC> KR;     // B, C
   typedef SsmRows<T, kPw, kSsmC> VR;   // x, dy
   typedef SsmRows<T, N, kPw> SR;       // a plane of S or E
-  static constexpr int state = SR::bytes * SsmState<T>::planes;
+  static constexpr int state = SR::bytes * SsmState<T, N>::planes;
   static constexpr int B = 0, C = KR::bytes, turn = 2 * KR::bytes;
   static constexpr int X = 0, dY = VR::bytes, S = dY + VR::bytes, E = S + state, one = E + state;   // of a turn
   // r_t, E_t x.EB, their column sums, dy.x, da's rectangles by wave; <E, S> by wave
@@ -47,7 +47,7 @@ __device__ __forceinline__ Fi<T, kNear> state_tr(const char* lds, int j, int g, 
   typedef typename GradLds<T, N>::SR SR;
   Fi<T, kNear> f;
 #pragma unroll
-  for (int i = 0; i < SsmState<T>::planes; ++i) f.x[i] = SR::tr32(lds + i * SR::bytes, 0, j, g, c);
+  for (int i = 0; i < SsmState<T, N>::planes; ++i) f.x[i] = SR::tr32(lds + i * SR::bytes, 0, j, g, c);
   return f;
 }
 template <typename T, int N>
@@ -55,7 +55,7 @@ __device__ __forceinline__ Fi<T, kNear> state_nat(const char* lds, int i, int p,
   typedef typename GradLds<T, N>::SR SR;
   Fi<T, kNear> f;
 #pragma unroll
-  for (int u = 0; u < SsmState<T>::planes; ++u) f.x[u] = SR::nat(lds + u * SR::bytes, i, p, g, c);
+  for (int u = 0; u < SsmState<T, N>::planes; ++u) f.x[u] = SR::nat(lds + u * SR::bytes, i, p, g, c);
   return f;
 }
 __device__ __forceinline__ float dot4(f32x4 a, f32x4 b) { return a[0] * b[0] + a[1] * b[1] + a[2] * b[2] + a[3] * b[3]; }
@@ -105,10 +105,10 @@ __global__ void __launch_bounds__(512, 2) carve_ssm_grad_kernel(SsmArgs a) {
     VR::template dma<8>(buf + L::X, x, (int)(a.xs[1] * sizeof(T)), len, wave, lane);
     VR::template dma<8>(buf + L::dY, dy, (int)((long long)a.H * a.P * sizeof(T)), len, wave, lane);
 #pragma unroll
-    for (int u = 0; u < SsmState<T>::planes; ++u) {
-      const size_t pl = at + (u * pn + (size_t)t * kPw * N) * sizeof(T);
-      SR::template dma<8>(buf + L::S + u * SR::bytes, a.S_chunks + pl, SR::RB, kPw, wave, lane);
-      SR::template dma<8>(buf + L::E + u * SR::bytes, a.E_chunks + pl, SR::RB, kPw, wave, lane);
+    for (int u = 0; u < SsmState<T, N>::planes; ++u) {
+      const size_t pl = at + u * pn * sizeof(T);
+      SsmState<T, N>::template dma<kPw, 8>(buf + L::S + u * SR::bytes, a.S_chunks + pl, t * kPw, wave, lane);
+      SsmState<T, N>::template dma<kPw, 8>(buf + L::E + u * SR::bytes, a.E_chunks + pl, t * kPw, wave, lane);
     }
   };
   // dt and the scalars of a head, by wave 0
@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(512, 2) carve_ssm_grad_kernel(SsmArgs a) {
 #pragma unroll
           for (int u = 0; u < Chunk16<T>::N; ++u) e[u] = s[u] = 0.0f;
 #pragma unroll
-          for (int pl = SsmState<T>::planes - 1; pl >= 0; --pl) {
+          for (int pl = SsmState<T, N>::planes - 1; pl >= 0; --pl) {
             float fe[Chunk16<T>::N], fs[Chunk16<T>::N];
             Chunk16<T>::unpack(*reinterpret_cast<const u32x4_t*>(buf + L::E + pl * SR::bytes + 16 * i), fe);
             Chunk16<T>::unpack(*reinterpret_cast<const u32x4_t*>(buf + L::S + pl * SR::bytes + 16 * i), fs);

@@ -127,9 +127,7 @@ __global__ void __launch_bounds__(64 * NW, 2) carve_ssm_state_kernel(SsmArgs a, 
       if (i + 2 < p.nch) st.fetch(chunk(i + 2));
     }
     if (REV && full) {   // the gradient of the state behind this chunk
-      char* e = a.E_chunks + ((size_t)(p.slot0 + ch) * a.H + h) * pn * 4;
-#pragma unroll
-      for (int j = 0; j < N / 16; ++j) SsmState<T>::st(e, pn, row + 16 * j, t.S[j]);
+      SsmState<T, N>::st(a.E_chunks + ((size_t)(p.slot0 + ch) * a.H + h) * pn * 4, pn, p0 + 16 * w, t.S, lane);
     }
     vm_wait_all();
     __syncthreads();
@@ -187,118 +185,156 @@ __global__ void __launch_bounds__(256) carve_ssm_join_kernel(SsmArgs a) {
   }
 }
 
-// Outputs of a span: its chunks one after another, the state in registers.  Waves hold 16
-// value rows each.  A chunk: the wave forms its tokens' share of L d C B^T (an operand
-// image in LDS, for all waves), then
-//   Y^T = S (e^G C)^T + X^T (L d C B^T)^T + D X^T,   S as above.
+// Outputs of a span: its chunks one after another, the state in registers.  A workgroup
+// takes two units (a head's 16 NW value rows) of one group, which share B and C; waves hold
+// 16 value rows each.  A chunk:
+//   all waves   L d C B^T of both units, a pair of tiles a wave: operand images in LDS
+//   its waves   Y^T = S (e^G C)^T + X^T (L d C B^T)^T + D X^T, then S as above
+// Four more waves bring the next chunk's rows into LDS and make its scalars: a wave that
+// reads LDS waits for all the LDS loads it has under way, so the loads are others'.
 template <typename T, int N, int NW>
 struct OutLds {
   typedef SsmRows<T, N, kSsmC> KR;
   typedef SsmRows<T, 16 * NW, kSsmC> VR;
-  static constexpr int B = 0, C = KR::bytes, X = C + KR::bytes, P = X + VR::bytes;
-  static constexpr int S = P + img_bytes<T>(kNear), total = S + 2 * kSmFloats * 4;
+  static constexpr int B = 0, C = KR::bytes, X = 2 * KR::bytes, one = X + 2 * VR::bytes;
+  static constexpr int image = img_bytes<T>(kNear), small = 2 * image + 4 * kSmFloats * 4;
+  static constexpr int bufs = 2 * one + small <= 160 * 1024 ? 2 : 1;
+  static constexpr int P = bufs * one, S = P + 2 * image, total = S + 4 * kSmFloats * 4;
 };
 template <typename T, int N, int NW>
-__global__ void __launch_bounds__(64 * NW, 2) carve_ssm_out_kernel(SsmArgs a) {
+__global__ void __launch_bounds__(128 * NW + 256, NW == 4 ? 3 : 2) carve_ssm_out_kernel(SsmArgs a) {
   typedef OutLds<T, N, NW> L;
   typedef typename L::KR KR;
   typedef typename L::VR VR;
   constexpr int NP = N / 32;
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  float* scal = reinterpret_cast<float*>(smem + L::S);
-  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int g = lane >> 4, c = lane & 15;
-  const int slices = a.P / (16 * NW);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int slices = a.P / (16 * NW), rep = a.H / a.G, units = rep * slices, pairs = (units + 1) / 2;
   SsmSpan p;
   int rest;
-  if (!ssm_block(a, a.H * slices, p, rest)) return;
-  const int h = rest / slices, p0 = rest % slices * 16 * NW, grp = h / (a.H / a.G);
-  const size_t pn = (size_t)a.P * N, row = (size_t)(p0 + 16 * w + c) * N + 4 * g;
+  if (!ssm_block(a, a.G * pairs, p, rest)) return;
+  const int grp = rest / pairs, u0 = 2 * (rest % pairs);   // the workgroup's first unit of the group
+  const int have = min(2, units - u0);
+  const auto scal = [&](int u, int ch) { return reinterpret_cast<float*>(smem + L::S) + (2 * u + (ch & 1)) * kSmFloats; };
+  const auto rows = [&](int ch) { return smem + (L::bufs == 2 ? (ch & 1) * L::one : 0); };
+
+  if (wave >= 2 * NW) {   // ---- rows and scalars
+    const int k = wave - 2 * NW;
+    const int h0 = grp * rep + u0 / slices, h1 = grp * rep + (u0 + have - 1) / slices;   // heads of the units
+    const T* Bm = reinterpret_cast<const T*>(a.Bm) + p.q.batch * a.bs[0] + p.first * a.bs[1] + grp * a.bs[2];
+    const T* Cm = reinterpret_cast<const T*>(a.Cm) + p.q.batch * a.cs[0] + p.first * a.cs[1] + grp * a.cs[2];
+    const T* x = reinterpret_cast<const T*>(a.x) + p.q.batch * a.xs[0] + p.first * a.xs[1];
+    const T* x0 = x + h0 * a.xs[2] + u0 % slices * 16 * NW;
+    const T* x1 = x + h1 * a.xs[2] + (u0 + have - 1) % slices * 16 * NW;
+    const auto issue = [&](int ch) {
+      const int len = min(kSsmC, p.len - ch * kSsmC);
+      char* to = rows(ch);
+      if (k == 0) KR::template dma<1>(to + L::B, Bm + (long long)ch * kSsmC * a.bs[1], (int)(a.bs[1] * sizeof(T)), len, 0, lane);
+      if (k == 1) KR::template dma<1>(to + L::C, Cm + (long long)ch * kSsmC * a.cs[1], (int)(a.cs[1] * sizeof(T)), len, 0, lane);
+      if (k >= 2) VR::template dma<1>(to + L::X + (k - 2) * VR::bytes, (k == 2 ? x0 : x1) + (long long)ch * kSsmC * a.xs[1],
+                                      (int)(a.xs[1] * sizeof(T)), len, 0, lane);
+    };
+    const int hs = k == 2 ? h0 : h1;   // waves 2 and 3: scalars of a unit
+    Steps<T> st = steps_of<T>(a, p, hs, lane);
+    if (k >= 2 && p.nch > 0) {
+      st.fetch(0);
+      st.make(0, scal(k - 2, 0));
+      if (p.nch > 1) st.fetch(1);
+    }
+    if (L::bufs == 2 && p.nch > 0) issue(0);
+#pragma unroll 1
+    for (int ch = 0; ch < p.nch; ++ch) {
+      if (L::bufs == 1) {
+        __syncthreads();   // (0) the rows of the chunk before are no longer read
+        issue(ch);
+      }
+      vm_wait_all();
+      __syncthreads();     // (1)
+      if (L::bufs == 2 && ch + 1 < p.nch) issue(ch + 1);
+      if (k >= 2 && ch + 1 < p.nch) {
+        st.make(ch + 1, scal(k - 2, ch + 1));
+        if (ch + 2 < p.nch) st.fetch(ch + 2);
+      }
+      __syncthreads();     // (2)
+    }
+    return;
+  }
+
+  // ---- outputs and states
+  const int g = lane >> 4, c = lane & 15, un = wave / NW, w = wave % NW;
+  const bool mine = un < have;
+  const int unit = min(u0 + un, units - 1), h = grp * rep + unit / slices, p0 = unit % slices * 16 * NW + 16 * w;
+  const size_t pn = (size_t)a.P * N, row = (size_t)(p0 + c) * N + 4 * g;
   Tile<T, N> t;
   if (p.s > 0) t.load(a.Z + ((size_t)p.slot * a.H + h) * pn + row);
   else if (a.S0) t.load(a.S0 + ((size_t)p.q.n * a.H + h) * pn + row);
   else t.zero();
-  const T* Bm = reinterpret_cast<const T*>(a.Bm) + p.q.batch * a.bs[0] + p.first * a.bs[1] + grp * a.bs[2];
-  const T* Cm = reinterpret_cast<const T*>(a.Cm) + p.q.batch * a.cs[0] + p.first * a.cs[1] + grp * a.cs[2];
-  const T* x = reinterpret_cast<const T*>(a.x) + p.q.batch * a.xs[0] + p.first * a.xs[1] + h * a.xs[2] + p0;
-  T* y = reinterpret_cast<T*>(a.y) + (((size_t)p.q.batch * a.T + p.first) * a.H + h) * a.P + p0 + 16 * w + 4 * g;
+  T* y = reinterpret_cast<T*>(a.y) + (((size_t)p.q.batch * a.T + p.first) * a.H + h) * a.P + p0 + 4 * g;
   const size_t yrow = (size_t)a.H * a.P;
   const float skip = a.D ? a.D[h] : 0.0f;
-  Steps<T> st = steps_of<T>(a, p, h, lane);
-  if (w == 0 && p.nch > 0) {
-    st.fetch(0);
-    st.make(0, scal);
-    if (p.nch > 1) st.fetch(1);
-  }
 #pragma unroll 1
   for (int ch = 0; ch < p.nch; ++ch) {
     const int len = min(kSsmC, p.len - ch * kSsmC);
-    const float* sc = scal + (ch & 1) * kSmFloats;
-    if (ch > 0) __syncthreads();   // the rows of the chunk before are no longer read
-    KR::template dma<NW>(smem + L::B, Bm + (long long)ch * kSsmC * a.bs[1], (int)(a.bs[1] * sizeof(T)), len, w, lane);
-    KR::template dma<NW>(smem + L::C, Cm + (long long)ch * kSsmC * a.cs[1], (int)(a.cs[1] * sizeof(T)), len, w, lane);
-    VR::template dma<NW>(smem + L::X, x + (long long)ch * kSsmC * a.xs[1], (int)(a.xs[1] * sizeof(T)), len, w, lane);
-    if (w == 0 && ch + 1 < p.nch) {
-      st.make(ch + 1, scal + ((ch + 1) & 1) * kSmFloats);
-      if (ch + 2 < p.nch) st.fetch(ch + 2);
-    }
-    if (a.S_chunks) {
-      char* out = a.S_chunks + ((size_t)(p.slot0 + ch) * a.H + h) * pn * 4;
+    const char* buf = rows(ch);
+    if (L::bufs == 1) __syncthreads();   // (0)
+    if (a.S_chunks && mine) SsmState<T, N>::st(a.S_chunks + ((size_t)(p.slot0 + ch) * a.H + h) * pn * 4, pn, p0, t.S, lane);
+    __syncthreads();   // (1) the chunk's rows and scalars are there, the images no longer read
+    // L d C B^T: rows j of the result (tiles 2 s, 2 s + 1), columns the tokens i of a tile
+    {
+      constexpr int PER = 8 / (2 * NW);   // (i, s) of a wave: i = 0 .. 3, s = 0, 1
 #pragma unroll
-      for (int j = 0; j < N / 16; ++j) SsmState<T>::st(out, pn, row + 16 * j, t.S[j]);
-    }
-    vm_wait_all();
-    __syncthreads();
-    // L d C B^T: rows j of the result, columns the tokens i of tile w (and 3 - w of two waves)
+      for (int v = 0; v < PER; ++v) {
+        const int id = wave + 2 * NW * v, i = id & 3, s = id >> 2;
+        if (s > i / 2) continue;   // (uniform)
+        f32x4 M[2] = {zero4(), zero4()};
 #pragma unroll
-    for (int u = 0; u < 4 / NW; ++u) {
-      const int i = u == 0 ? w : 3 - w;
-      Fr<T> fc[NP];
+        for (int q = 0; q < NP; ++q) {
+          const Fr<T> fc = KR::nat(buf + L::C, i, q, g, c);
 #pragma unroll
-      for (int q = 0; q < NP; ++q) fc[q] = KR::nat(smem + L::C, i, q, g, c);
-      const float Gh = sc[kSmGh * kSsmC + 16 * i + c], Gl = sc[kSmGl * kSsmC + 16 * i + c];
-      f32x4 M[4];
+          for (int b = 0; b < 2; ++b) M[b] = mma<T>(KR::nat(buf + L::B, 2 * s + b, q, g, c), fc, M[b]);
+        }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        M[j] = zero4();
-        if (j > i) continue;   // (uniform)
+        for (int u = 0; u < 2; ++u) {
+          if (u >= have) break;   // (uniform)
+          const float* sc = scal(u, ch);
+          const float Gh = sc[kSmGh * kSsmC + 16 * i + c], Gl = sc[kSmGl * kSsmC + 16 * i + c];
+          f32x4 W[2];
 #pragma unroll
-        for (int q = 0; q < NP; ++q) M[j] = mma<T>(KR::nat(smem + L::B, j, q, g, c), fc[q], M[j]);
-        const f32x4 gh = four(sc + kSmGh * kSsmC + 16 * j + 4 * g);
-        const f32x4 gl = four(sc + kSmGl * kSsmC + 16 * j + 4 * g);
-        const f32x4 d = four(sc + kSmD * kSsmC + 16 * j + 4 * g);
+          for (int b = 0; b < 2; ++b) {
+            const int at = 32 * s + 16 * b + 4 * g;
+            const f32x4 gh = four(sc + kSmGh * kSsmC + at), gl = four(sc + kSmGl * kSsmC + at), d = four(sc + kSmD * kSsmC + at);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          M[j][e] *= decay_between(Gh, Gl, gh[e], gl[e]) * d[e];
-          if (j == i) M[j][e] = masked(4 * g + e <= c, M[j][e]);   // (uniform)
+            for (int e = 0; e < 4; ++e)
+              W[b][e] = masked(at + e <= 16 * i + c, M[b][e] * (decay_between(Gh, Gl, gh[e], gl[e]) * d[e]));
+          }
+          st_img<T, kNear>(smem + L::P + u * L::image, img_lower(i, s), lane, W[0], W[1]);
         }
       }
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-        if (s <= i / 2) st_img<T, kNear>(smem + L::P, img_lower(i, s), lane, M[2 * s], M[2 * s + 1]);
     }
     Fi<T, kNear> Sf[NP];
 #pragma unroll
     for (int q = 0; q < NP; ++q) Sf[q] = to_fi<T, kNear>(t.S[2 * q], t.S[2 * q + 1]);
-    __syncthreads();
-    const Fr<T> fx[2] = {VR::tr32(smem + L::X, 0, w, g, c), VR::tr32(smem + L::X, 1, w, g, c)};
+    __syncthreads();   // (2)
+    if (!mine) continue;
+    const float* sc = scal(un, ch);
+    const char* xb = buf + L::X + un * VR::bytes;
+    const Fr<T> fx[2] = {VR::tr32(xb, 0, w, g, c), VR::tr32(xb, 1, w, g, c)};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       f32x4 o = zero4(), z = zero4();
 #pragma unroll
-      for (int q = 0; q < NP; ++q) o = mma<T>(Sf[q], KR::nat(smem + L::C, i, q, g, c), o);
+      for (int q = 0; q < NP; ++q) o = mma<T>(Sf[q], KR::nat(buf + L::C, i, q, g, c), o);
 #pragma unroll
-      for (int s = 0; s <= i / 2; ++s) z = mma<T>(fx[s], ld_img<T, kNear>(smem + L::P, img_lower(i, s), lane), z);
+      for (int s = 0; s <= i / 2; ++s) z = mma<T>(fx[s], ld_img<T, kNear>(smem + L::P + un * L::image, img_lower(i, s), lane), z);
       const int tok = 16 * i + c;
-      const f32x4 xv = Quad<T>::f32(VR::quad(smem + L::X, i, w, g, c));
+      const f32x4 xv = Quad<T>::f32(VR::quad(xb, i, w, g, c));
       o = o * sc[kSmGam * kSsmC + tok] + z + xv * skip;
       if (tok < len) Quad<T>::st(y + (size_t)(ch * kSsmC + tok) * yrow, Quad<T>::cvt(o));
     }
-    t.template add<KR>(smem + L::B, fx, [&](int at) { return four(sc + kSmEndD * kSsmC + at); },
-                       sc[kSmWhole], g, c);
+    t.template add<KR>(buf + L::B, fx, [&](int at) { return four(sc + kSmEndD * kSsmC + at); }, sc[kSmWhole], g, c);
   }
   settle();
-  if (a.S_T && p.s == p.nspan - 1) t.store(a.S_T + ((size_t)p.q.n * a.H + h) * pn + row);
+  if (mine && a.S_T && p.s == p.nspan - 1) t.store(a.S_T + ((size_t)p.q.n * a.H + h) * pn + row);
 }
 
 template <typename K>
@@ -349,7 +385,8 @@ int launch_fwd_t(const SsmArgs& a, hipStream_t s, void (*mark)(hipStream_t)) {
   static_assert(lds <= 160 * 1024, "LDS");
   const auto kern = carve_ssm_out_kernel<T, N, NW>;
   if (!lds_attr(kern, lds)) return CARVE_ERR_HIP;
-  hipLaunchKernelGGL(kern, dim3(ssm_grid(a.nspans, a.H * (a.P / (16 * NW)))), dim3(64 * NW), lds, s, a);
+  const int pairs = (a.H / a.G * (a.P / (16 * NW)) + 1) / 2;
+  hipLaunchKernelGGL(kern, dim3(ssm_grid(a.nspans, a.G * pairs)), dim3(128 * NW + 256), lds, s, a);
   st = launched();
   mark(s);
   return st;
@@ -357,7 +394,8 @@ int launch_fwd_t(const SsmArgs& a, hipStream_t s, void (*mark)(hipStream_t)) {
 
 }  // namespace
 
-// value rows of a workgroup: 64, or 32 where P is no multiple of it
+// value rows of a unit: 64, or 32 where P is no multiple of it, and with f32 keys of 128,
+// whose products of 64 rows do not fit the registers (as in the C entry points' plan)
 #define CARVE_SSM_BY(call)                                                      \
   const bool wide = a.P % 64 == 0;                                              \
   if (dtype == CARVE_BF16) {                                                    \
@@ -370,7 +408,7 @@ int launch_fwd_t(const SsmArgs& a, hipStream_t s, void (*mark)(hipStream_t)) {
     switch (a.N) {                                                              \
       case 32: return wide ? call(float, 32, 4) : call(float, 32, 2);           \
       case 64: return wide ? call(float, 64, 4) : call(float, 64, 2);           \
-      case 128: return wide ? call(float, 128, 4) : call(float, 128, 2);        \
+      case 128: return call(float, 128, 2);                                     \
     }                                                                           \
   }                                                                             \
   return CARVE_ERR_UNSUPPORTED;
