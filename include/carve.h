@@ -535,11 +535,11 @@ typedef struct {
 /* Chunks that S_chunks has room for; 0 for invalid dims. */
 size_t carve_ssm_chunk_count(const carve_ssm_dims_t* d);
 
-/* Bytes of device workspace of carve_ssm_chunk_fwd (for_backward = 0; may be none) and
+/* Bytes of device workspace of carve_ssm_chunk_fwd (for_backward = 0) and
  * carve_ssm_chunk_bwd (1); 0 for invalid dims.  Nothing in it is kept between calls. */
 size_t carve_ssm_workspace_size(const carve_ssm_dims_t* d, int for_backward);
 
-/* Forward.  S0, S_T, S_chunks may be NULL.  One launch, or three where long sequences are
+/* Forward.  S0, S_T, S_chunks may be NULL.  Two launches, or four where long sequences are
  * cut into spans. */
 int carve_ssm_chunk_fwd(const carve_ssm_dims_t* d, const void* x, const void* dt, const float* A, const void* Bm,
                         const void* Cm, const float* D, const float* dt_bias, const float* S0, const int* offsets,
@@ -549,7 +549,7 @@ int carve_ssm_chunk_fwd(const carve_ssm_dims_t* d, const void* x, const void* dt
 /* Backward for loss <dy, y> + <dS_T, S_T> (dS_T may be NULL: zeros).  Out: dx [B,T,H,P], ddt
  * [B,T,H], dBm, dCm [B,T,G,S] (token dtype), dA [H] f32, dD and ddt_bias [H] f32 (exactly
  * where D and dt_bias are given), dS0 or NULL.  All sums are in a fixed order: reruns are
- * bitwise identical.  Three to six launches. */
+ * bitwise identical.  Four to seven launches. */
 int carve_ssm_chunk_bwd(const carve_ssm_dims_t* d, const void* x, const void* dt, const float* A, const void* Bm,
                         const void* Cm, const float* D, const float* dt_bias, const float* S_chunks, const int* offsets,
                         const void* dy, const float* dS_T, void* dx, void* ddt, float* dA, void* dBm, void* dCm,

@@ -1180,7 +1180,7 @@ def ssm_chunk_fwd(x, dt, A, Bm, Cm, S0=None, *, D=None, dt_bias=None, softplus=T
         y = _out(res, "y", x, x.shape, x.dtype, dev)
         S_T = _out(res, "S_T", S0, (seqs, H, P, N), f32, dev) if want_state or res.get("S_T") is not None else None
         S_c = _out(res, "S_chunks", None, (chunks, H, P, N), f32, dev) if want_chunks or res.get("S_chunks") is not None else None
-        ws, ws_ptr, ws_len = _scratch(workspace, ws_bytes, dev) if ws_bytes or workspace is not None else (None, None, 0)
+        ws, ws_ptr, ws_len = _scratch(workspace, ws_bytes, dev)
         return lib.carve_ssm_chunk_fwd(dims, *ptrs, _ptr(S0, "S0", f32, (seqs, H, P, N)), _pointer(offsets), y, S_T, S_c,
                                        ws_ptr, ws_len, s)
 

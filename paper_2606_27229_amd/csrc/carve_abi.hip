@@ -1156,9 +1156,9 @@ struct SsmPlan {
   size_t chunks, spans;
   int span, splits;
 };
-// Spans: as many as let every compute unit hold one workgroup of the outputs (a pair of
-// units, see carve_ssm_fwd.hip), none shorter than kSsmMinSpan chunks.
-constexpr long long kSsmGroups = 256;
+// Spans: as many as let every compute unit hold two workgroups of the outputs (a pair of
+// units each, see carve_ssm_fwd.hip), none shorter than kSsmMinSpan chunks.
+constexpr long long kSsmGroups = 512;
 constexpr int kSsmMinSpan = 4;
 SsmPlan ssm_plan(const carve_ssm_dims_t* d) {
   SsmPlan p;
@@ -1183,21 +1183,23 @@ int check_ssm_chunk(const carve_ssm_dims_t* d) {
   if ((long long)(d->T / kSsmC) + d->N >= (1LL << 23) || (long long)d->B * ((d->T + kSsmC - 1) / kSsmC) >= (1LL << 23))
     return CARVE_ERR_UNSUPPORTED;
   const SsmPlan p = ssm_plan(d);
-  if ((long long)(p.spans + 8) * d->H * (d->P / 32) >= (1LL << 23) || d->G > 65535) return CARVE_ERR_UNSUPPORTED;
+  if ((long long)(p.spans + 8) * d->H * (d->P / 32) >= (1LL << 23) || d->G > 61000) return CARVE_ERR_UNSUPPORTED;
   return CARVE_OK;
 }
 size_t ssm_state(const carve_ssm_dims_t* d) { return (size_t)d->H * d->P * d->S * 4; }   // bytes, all heads
 bool ssm_split(const carve_ssm_dims_t* d, const SsmPlan& p) { return (long long)d->T > (long long)p.span * kSsmC; }
 
-// workspace: spans' states and decays | state gradients | shares of the head sums | of dB, dC
+// workspace: scalars and C B^T of the chunks | spans' states and decays | state gradients | shares of the head sums | of dB, dC
 struct SsmWs {
-  size_t Z, Zg, E, part, dBp, total;
+  size_t scal, cb, Z, Zg, E, part, dBp, total;
 };
 SsmWs ssm_ws(const carve_ssm_dims_t* d, bool bwd) {
   const SsmPlan p = ssm_plan(d);
   SsmWs w{};
   size_t off = 0;
   const bool split = ssm_split(d, p);
+  w.scal = off, off += align256(p.chunks * d->H * (bwd ? kSmBwd : kSmFwd) * 4);
+  w.cb = off, off += align256(p.chunks * d->G * kSsmCB);
   w.Z = off, off += split ? align256(p.spans * ssm_state(d)) : 0;
   w.Zg = off, off += split ? align256(p.spans * d->H * 4) : 0;
   if (bwd) {
@@ -1223,6 +1225,7 @@ void ssm_args(SsmArgs& a, const carve_ssm_dims_t* d, const void* x, const void* 
   const SsmWs w = ssm_ws(d, bwd);
   char* ws = static_cast<char*>(workspace);
   a.Z = reinterpret_cast<float*>(ws + w.Z), a.Zg = reinterpret_cast<float*>(ws + w.Zg);
+  a.scal = ws + w.scal, a.cb = ws + w.cb;
   a.E_chunks = ws + w.E, a.part = reinterpret_cast<float*>(ws + w.part), a.dBp = reinterpret_cast<float*>(ws + w.dBp);
 }
 int ssm_inputs(const carve_ssm_dims_t* d, const void* x, const void* dt, const float* A, const void* Bm, const void* Cm,
@@ -1269,7 +1272,7 @@ int carve_ssm_chunk_fwd(const carve_ssm_dims_t* d, const void* x, const void* dt
   for (const void* p : ptrs)
     if (!aligned16(p)) return CARVE_ERR_ALIGN;
   const size_t need = carve_ssm_workspace_size(d, 0);
-  if (need && (!workspace || workspace_bytes < need)) return CARVE_ERR_WORKSPACE;
+  if (!workspace || workspace_bytes < need) return CARVE_ERR_WORKSPACE;
   const size_t seqs = d->N ? d->N : d->B, state = ssm_state(d);
   Range ins[9];
   int nin = ssm_inputs(d, x, dt, A, Bm, Cm, D, dt_bias, ins);

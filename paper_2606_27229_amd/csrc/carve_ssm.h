@@ -32,6 +32,8 @@ struct SsmArgs {
   char *S_chunks, *E_chunks;   // states at chunk starts, state gradients at chunk ends: see SsmState
   float* Z;                // [nspans][H][P][N]: what a span adds, then the state it starts from
   float* Zg;               // [nspans][H]: its decay
+  char* scal;              // [nslots][H]: scalars; cb: [nslots][G], C B^T
+  char* cb;
   float* part;             // [nslots][H][4]: a chunk's share of dA, ddt_bias, dD
   float* dBp;              // [splits][rows][G][N], dCp behind it: shares of dB, dC
   long long xs[3], bs[3], cs[3], ds[2];   // strides of batch, token, head (or group)
@@ -73,17 +75,27 @@ __device__ __forceinline__ SsmSeq ssm_find(const SsmArgs& a, int slot, int L) {
   return ssm_seq(a, lo);
 }
 
-// ---- scalars of a chunk ---------------------------------------------------------------
-// Of every token: d; G / log 2 as two floats (far below any other behind the last token, so
-// that what decays from a token before to one there is 0); e^G (0 there); E = e^{G_C - G};
-// E d.  Then e^{G_C}.
-enum : int { kSmD = 0, kSmGh = 1, kSmGl = 2, kSmGam = 3, kSmEnd = 4, kSmEndD = 5, kSmWhole = 6 * kSsmC, kSmFloats = 6 * kSsmC + 4 };
-constexpr float kSmNever = -1e5f;
+// ---- what chunks are made from: scalars of the heads, products of the groups -----------------
+// Made once a call by carve_ssm_prep_kernel, as several kernels need them.
+// Scalars of a (slot, head), floats.  Of every token: d; G / log 2 as two floats (far below
+// any other behind the last token, so that what decays from a token before to one there is
+// 0); e^G (0 there); E = e^{G_C - G}; E d; F d with F = e^{g - G}, g being G at the end of
+// the token's tile of 16.  Then g / log 2 of every tile as two floats, and e^{G_C}; for the
+// backward also F, and e^{G - g} of tiles 0, 1 and 2 at the tokens behind them.
+enum : int { kSmD = 0, kSmGh = 1, kSmGl = 2, kSmGam = 3, kSmEnd = 4, kSmEndD = 5, kSmFD = 6, kSmTile = 7 * kSsmC,
+             kSmWhole = kSmTile + 8, kSmFwd = 8 * kSsmC, kSmF = 8, kSmDown = 9, kSmBwd = 12 * kSsmC };
+constexpr float kSmNever = -1e7f;   // (64 tokens reach -10^6)
+// C B^T of a (slot, group): its ten tiles on and below the diagonal, 1 KB each as result
+// tiles; tile (i, j) at ssm_tile(i, j).  Forward: rows j, columns i; backward: rows i,
+// columns j.
+constexpr int kSsmCB = 10 * 1024;
+__host__ __device__ constexpr int ssm_tile(int i, int j) { return (i * (i + 1) / 2 + j) * 1024; }
 
 __device__ __forceinline__ float ssm_step_of(float z, int softplus) {
   return softplus ? fmaxf(z, 0.0f) + log1pf(expf(-fabsf(z))) : z;
 }
 // by one wave, a token a lane; raw: its dt
+template <bool BWD>
 __device__ __forceinline__ void ssm_scalars(float raw, bool in, float bias, float A, int softplus, int lane, float* out) {
   const float d = in ? ssm_step_of(raw + bias, softplus) : 0.0f;
   float ga = in ? d * A : 0.0f;
@@ -94,15 +106,25 @@ __device__ __forceinline__ void ssm_scalars(float raw, bool in, float bias, floa
     const double up = __shfl_up(G, s);
     if (lane >= s) G += up;
   }
-  const double all = __shfl(G, 63);
-  const float Gh = (float)G, Gl = (float)(G - (double)Gh), end = exp2_f((float)(all - G));
+  const double all = __shfl(G, 63), tile = __shfl(G, lane | 15);
+  const float Gh = (float)G, Gl = (float)(G - (double)Gh), end = exp2_f((float)(all - G)), f = exp2_f((float)(tile - G));
   out[kSmD * kSsmC + lane] = d;
   out[kSmGh * kSsmC + lane] = in ? Gh : kSmNever;
   out[kSmGl * kSsmC + lane] = in ? Gl : 0.0f;
   out[kSmGam * kSsmC + lane] = in ? exp2_f(Gh) * (1.0f + Gl * 0.69314718f) : 0.0f;
   out[kSmEnd * kSsmC + lane] = end;
   out[kSmEndD * kSsmC + lane] = end * d;
+  out[kSmFD * kSsmC + lane] = f * d;
+  if ((lane & 15) == 15) out[kSmTile + lane / 16] = Gh, out[kSmTile + 4 + lane / 16] = Gl;
   if (lane == 0) out[kSmWhole] = exp2_f((float)all);
+  if (BWD) {
+    out[kSmF * kSsmC + lane] = f;
+#pragma unroll
+    for (int t = 0; t < 3; ++t) {
+      const double gt = __shfl(G, 16 * t + 15);
+      out[(kSmDown + t) * kSsmC + lane] = in && lane / 16 > t ? exp2_f((float)(G - gt)) : 0.0f;
+    }
+  }
 }
 // e^{G_i - G_j}
 __device__ __forceinline__ float decay_between(float ih, float il, float jh, float jl) { return exp2_f((ih - jh) + (il - jl)); }
@@ -208,6 +230,26 @@ __device__ __forceinline__ float masked(bool on, float v) {
 // results, and the compiler leaves them a wait state short there.
 __device__ __forceinline__ void settle() { asm volatile("s_nop 7" ::: "memory"); }
 
+// Rows of a chunk to memory, four values a lane, without a branch around the store (which
+// would part what the compiler may reorder): a buffer of the rows there are, behind which
+// stores are dropped.  base: the chunk's first row (uniform); row: values of a row; cols:
+// values from a row's base that lanes write at most.
+template <typename T>
+struct RowStore {
+  __amdgpu_buffer_rsrc_t r;
+  unsigned bytes;          // of a row
+  __device__ __forceinline__ RowStore(T* base, size_t row, int len, int cols)
+      : r(__builtin_amdgcn_make_buffer_rsrc(base, 0, (int)((unsigned)(len - 1) * (unsigned)(row * sizeof(T)) + cols * (unsigned)sizeof(T)), 0x00027000)),
+        bytes((unsigned)(row * sizeof(T))) {}
+  __device__ __forceinline__ void st(int tok, int col, f32x4 v) const {
+    const int off = (int)((unsigned)tok * bytes + (unsigned)col * (unsigned)sizeof(T));
+    if constexpr (sizeof(T) == 2)
+      __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2_t, Quad<T>::cvt(v)), r, off, 0, 0);
+    else
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_g, v), r, off, 0, 0);
+  }
+};
+
 // ---- workgroups of the scans -------------------------------------------------------------
 // Workgroup -> (span, head, slice of PW value rows).  Blocks 8 apart share an XCD: with many
 // spans each goes to one XCD with all its heads, which read the same B and C from one L2;
@@ -258,7 +300,8 @@ struct SsmStepArgs {
 int launch_ssm_fwd(const SsmArgs& a, int dtype, hipStream_t s, void (*mark)(hipStream_t));
 int launch_ssm_bwd(const SsmArgs& a, int dtype, hipStream_t s, void (*mark)(hipStream_t));
 int launch_ssm_step(const SsmStepArgs& a, int N, int dtype, hipStream_t s);
-// the chain of state gradients: spans' sums and their joining, then E of every chunk, dS0
+// scalars and C B^T for the backward, then the chain of state gradients: spans' sums and
+// their joining, E of every chunk, dS0
 int launch_ssm_spans_rev(const SsmArgs& a, int dtype, hipStream_t s, void (*mark)(hipStream_t));
 
 }  // namespace carve

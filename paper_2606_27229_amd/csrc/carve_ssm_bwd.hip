@@ -24,8 +24,11 @@ constexpr int kPart = 4;  // floats of a (chunk, head) in SsmArgs::part
 // what a decay multiplies from before, waves 4 to 7 dB, dx and the rest; wave w of each side
 // owns token tile w, as i of dC and as j of dB and dx.  dB and dC stay in registers over the
 // heads; a head comes in turns of 32 value columns, in which everything but L is linear: x,
-// dy and the rows of S and E, loaded straight into LDS a turn ahead.
-// Bound by HBM, the states S and E above all (N x P floats each, a chunk and head).
+// dy and the rows of S and E.  Waves 8 to 10 bring them straight into LDS, a turn ahead (a
+// wave that reads LDS waits for all the LDS loads it has under way, so the loads are
+// others'); wave 11 makes a head's ddt and its sums when the others have gone on.
+// Bound by HBM, the states S and E above all (N x P floats each, a chunk and head), and by
+// the latency of a turn's steps.
 template <typename T, int N>
 struct GradLds {
   typedef SsmRows<T, N, kSsmC> KR;     // B, C
@@ -34,13 +37,14 @@ struct GradLds {
   static constexpr int state = SR::bytes * SsmState<T, N>::planes;
   static constexpr int B = 0, C = KR::bytes, turn = 2 * KR::bytes;
   static constexpr int X = 0, dY = VR::bytes, S = dY + VR::bytes, E = S + state, one = E + state;   // of a turn
-  // r_t, E_t x.EB, their column sums, dy.x, da's rectangles by wave; <E, S> by wave
-  static constexpr int sums = 8 * kSsmC + 4, small = 2 * (kSmFloats + sums) * 4;
+  // of a head: r_t, E_t x.EB, their column sums, dy.x, d_t, da's rectangles by wave; <E, S> by
+  // wave, e^{G_C}
+  static constexpr int sums = 9 * kSsmC + 8, small = 2 * (kSmBwd + sums) * 4;
   // two turns' rows where they fit (else a turn's rows are waited for)
-  static constexpr bool ahead = turn + 2 * one + small <= 160 * 1024;
-  static constexpr int scal = turn + (ahead ? 2 : 1) * one, sum = scal + 2 * kSmFloats * 4;
-  static constexpr int total = scal + small;
+  static constexpr int bufs = turn + 2 * one + small <= 160 * 1024 ? 2 : 1;
+  static constexpr int scal = turn + bufs * one, sum = scal + 2 * kSmBwd * 4, total = scal + small;
 };
+enum : int { kSuR = 0, kSuE = 1, kSuM = 2, kSuDiag = 3, kSuD = 4, kSuRect = 5, kSuES = 9 * kSsmC, kSuWhole = kSuES + 4 };
 
 template <typename T, int N>
 __device__ __forceinline__ Fi<T, kNear> state_tr(const char* lds, int j, int g, int c) {
@@ -67,7 +71,7 @@ __device__ __forceinline__ float col_sum(float x) {
 }
 
 template <typename T, int N>
-__global__ void __launch_bounds__(512, 2) carve_ssm_grad_kernel(SsmArgs a) {
+__global__ void __launch_bounds__(768, 3) carve_ssm_grad_kernel(SsmArgs a) {
   typedef GradLds<T, N> L;
   typedef typename L::KR KR;
   typedef typename L::VR VR;
@@ -75,7 +79,6 @@ __global__ void __launch_bounds__(512, 2) carve_ssm_grad_kernel(SsmArgs a) {
   constexpr int NP = N / 32, NT = N / 16;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const bool back = wave >= 4;   // (uniform) dB and dx
   const int w = wave & 3;
   int lane = tid & 63, g = lane >> 4, c = lane & 15, tok = 16 * w + c;
   // (coordinates the compiler takes as new: addresses are formed where they are used, not
@@ -90,185 +93,144 @@ __global__ void __launch_bounds__(512, 2) carve_ssm_grad_kernel(SsmArgs a) {
   const SsmSeq q = ssm_find(a, slot, kSsmC);
   const int ch = slot - ssm_slot0(a, q, kSsmC);
   if (ch < 0 || (long long)ch * kSsmC >= q.len) {   // a slot of no chunk
-    for (int i = tid; i < (h1 - h0) * kPart; i += 512) a.part[((size_t)slot * a.H + h0) * kPart + i] = 0.0f;
+    for (int i = tid; i < (h1 - h0) * kPart; i += 768) a.part[((size_t)slot * a.H + h0) * kPart + i] = 0.0f;
     return;
   }
   const int first = q.first + ch * kSsmC, len = min(kSsmC, q.len - ch * kSsmC);
   const size_t row0 = (size_t)q.batch * a.T + first, pn = (size_t)a.P * N;
-  const int turns = a.P / kPw;
-  const auto scal = [&](int h) { return reinterpret_cast<float*>(smem + L::scal) + (h & 1) * kSmFloats; };
+  const int turns = a.P / kPw, total = (h1 - h0) * turns;
+  const auto rows = [&](int n) { return smem + L::turn + (L::bufs == 2 ? (n & 1) * L::one : 0); };
+  const auto scal = [&](int h) { return reinterpret_cast<float*>(smem + L::scal) + (h & 1) * kSmBwd; };
   const auto sums = [&](int h) { return reinterpret_cast<float*>(smem + L::sum) + (h & 1) * L::sums; };
-  const auto issue = [&](int h, int t, char* buf) {
-    const T* x = reinterpret_cast<const T*>(a.x) + q.batch * a.xs[0] + first * a.xs[1] + h * a.xs[2] + t * kPw;
-    const T* dy = reinterpret_cast<const T*>(a.dy) + (row0 * a.H + h) * a.P + t * kPw;
-    const size_t at = ((size_t)slot * a.H + h) * pn * 4;
-    VR::template dma<8>(buf + L::X, x, (int)(a.xs[1] * sizeof(T)), len, wave, lane);
-    VR::template dma<8>(buf + L::dY, dy, (int)((long long)a.H * a.P * sizeof(T)), len, wave, lane);
+
+  if (wave >= 8 && wave < 11) {   // ---- rows
+    if (w == 0)
+      KR::template dma<1>(smem + L::B, reinterpret_cast<const T*>(a.Bm) + q.batch * a.bs[0] + first * a.bs[1] + grp * a.bs[2],
+                          (int)(a.bs[1] * sizeof(T)), len, 0, lane);
+    if (w == 1)
+      KR::template dma<1>(smem + L::C, reinterpret_cast<const T*>(a.Cm) + q.batch * a.cs[0] + first * a.cs[1] + grp * a.cs[2],
+                          (int)(a.cs[1] * sizeof(T)), len, 0, lane);
+    const T* x = reinterpret_cast<const T*>(a.x) + q.batch * a.xs[0] + first * a.xs[1];
+    const T* dy = reinterpret_cast<const T*>(a.dy) + row0 * a.H * a.P;
+    const auto issue = [&](int n) {
+      const int h = h0 + n / turns, p0 = n % turns * kPw;
+      char* buf = rows(n);
+      if (w == 0) {
+        VR::template dma<1>(buf + L::X, x + h * a.xs[2] + p0, (int)(a.xs[1] * sizeof(T)), len, 0, lane);
+        VR::template dma<1>(buf + L::dY, dy + h * a.P + p0, (int)((long long)a.H * a.P * sizeof(T)), len, 0, lane);
+        if (p0 == 0) dma_flat<1, 3>(reinterpret_cast<char*>(scal(h)), a.scal + ((size_t)slot * a.H + h) * kSmBwd * 4, 0, lane);
+      } else {
+        const char* from = (w == 1 ? a.S_chunks : a.E_chunks) + ((size_t)slot * a.H + h) * pn * 4;
+        char* to = buf + (w == 1 ? L::S : L::E);
 #pragma unroll
-    for (int u = 0; u < SsmState<T, N>::planes; ++u) {
-      const size_t pl = at + u * pn * sizeof(T);
-      SsmState<T, N>::template dma<kPw, 8>(buf + L::S + u * SR::bytes, a.S_chunks + pl, t * kPw, wave, lane);
-      SsmState<T, N>::template dma<kPw, 8>(buf + L::E + u * SR::bytes, a.E_chunks + pl, t * kPw, wave, lane);
+        for (int u = 0; u < SsmState<T, N>::planes; ++u)
+          SsmState<T, N>::template dma<kPw, 1>(to + u * SR::bytes, from + u * pn * sizeof(T), p0, 0, lane);
+      }
+    };
+    if (L::bufs == 2) issue(0);
+#pragma unroll 1
+    for (int n = 0; n < total; ++n) {
+      if (L::bufs == 1) {
+        __syncthreads();   // (0) the rows of the turn before are no longer read
+        issue(n);
+      }
+      vm_wait_all();
+      __syncthreads();     // (1)
+      if (L::bufs == 2 && n + 1 < total) issue(n + 1);
     }
-  };
-  // dt and the scalars of a head, by wave 0
-  const auto dt_of = [&](int h) {
-    return lane < len ? (float)(reinterpret_cast<const T*>(a.dt) + q.batch * a.ds[0] + h)[(first + lane) * a.ds[1]] : 0.0f;
-  };
-  const auto bias_of = [&](int h) { return a.dt_bias ? a.dt_bias[h] : 0.0f; };
-  // what remains of a head when all its sums are there, by wave 0
-  const auto finish = [&](int h, float raw) {
-    const float *sc = scal(h), *sR = sums(h), *sE = sR + kSsmC, *sM = sE + kSsmC, *sDiag = sM + kSsmC, *sRect = sDiag + kSsmC,
-                *sES = sRect + 4 * kSsmC;
-    const bool in = lane < len;
-    const float d = sc[kSmD * kSsmC + lane], e = sE[lane], A = a.A[h];
-    float suf = in ? sR[lane] : 0.0f, pre = in ? d * e : 0.0f;
-#pragma unroll
-    for (int s = 1; s < 64; s *= 2) {
-      const float dn = __shfl_down(suf, s), up = __shfl_up(pre, s);
-      if (lane + s < 64) suf += dn;
-      if (lane >= s) pre += up;
-    }
-    const float before = __shfl_up(pre, 1);
-    const float es = sc[kSmWhole] * ((sES[0] + sES[1]) + (sES[2] + sES[3]));
-    const float rect = (sRect[lane] + sRect[kSsmC + lane]) + (sRect[2 * kSsmC + lane] + sRect[3 * kSsmC + lane]);
-    const float da = suf + (lane > 0 ? before : 0.0f) + rect + es;
-    float dd = A * da + (sM[lane] + e);
-    if (a.softplus) {
-      const float z = raw + bias_of(h), ez = expf(-fabsf(z));
-      dd *= (z >= 0.0f ? 1.0f : ez) / (1.0f + ez);
-    }
-    if (in) reinterpret_cast<T*>(a.ddt)[(row0 + lane) * a.H + h] = (T)dd;
-    const float sa = group_sum<64>(in ? d * da : 0.0f), sb = group_sum<64>(in ? dd : 0.0f), sd = group_sum<64>(in ? sDiag[lane] : 0.0f);
-    if (lane == 0) *reinterpret_cast<f32x4*>(a.part + ((size_t)slot * a.H + h) * kPart) = f32x4{sa, sb, sd, 0.0f};
-  };
-  KR::template dma<8>(smem + L::B, reinterpret_cast<const T*>(a.Bm) + q.batch * a.bs[0] + first * a.bs[1] + grp * a.bs[2],
-                      (int)(a.bs[1] * sizeof(T)), len, wave, lane);
-  KR::template dma<8>(smem + L::C, reinterpret_cast<const T*>(a.Cm) + q.batch * a.cs[0] + first * a.cs[1] + grp * a.cs[2],
-                      (int)(a.cs[1] * sizeof(T)), len, wave, lane);
-  if (L::ahead) issue(h0, 0, smem + L::turn);
-  float raw = 0.0f, was = 0.0f;
-  if (wave == 0) {
-    raw = dt_of(h0);
-    ssm_scalars(raw, lane < len, bias_of(h0), a.A[h0], a.softplus, lane, scal(h0));
+    __syncthreads();       // (2)
+    return;
   }
-  f32x4 acc[NT];   // dC^T or dB^T: rows n, the tile's tokens
+  if (wave == 11) {   // ---- what remains of a head when all its sums are there
+    const auto finish = [&](int h) {
+      const float* su = sums(h);
+      const bool in = lane < len;
+      const float bias = a.dt_bias ? a.dt_bias[h] : 0.0f, A = a.A[h];
+      const float raw = (float)(reinterpret_cast<const T*>(a.dt) + q.batch * a.ds[0] + h)[(first + min(lane, len - 1)) * a.ds[1]];
+      const float d = su[kSuD * kSsmC + lane], e = su[kSuE * kSsmC + lane];
+      float suf = in ? su[kSuR * kSsmC + lane] : 0.0f, pre = in ? d * e : 0.0f;
+#pragma unroll
+      for (int s = 1; s < 64; s *= 2) {
+        const float dn = __shfl_down(suf, s), up = __shfl_up(pre, s);
+        if (lane + s < 64) suf += dn;
+        if (lane >= s) pre += up;
+      }
+      const float before = __shfl_up(pre, 1);
+      const float es = su[kSuWhole] * ((su[kSuES] + su[kSuES + 1]) + (su[kSuES + 2] + su[kSuES + 3]));
+      const float* rect = su + kSuRect * kSsmC + lane;
+      const float da = suf + (lane > 0 ? before : 0.0f) + ((rect[0] + rect[kSsmC]) + (rect[2 * kSsmC] + rect[3 * kSsmC])) + es;
+      float dd = A * da + (su[kSuM * kSsmC + lane] + e);
+      if (a.softplus) {
+        const float z = raw + bias, ez = expf(-fabsf(z));
+        dd *= (z >= 0.0f ? 1.0f : ez) / (1.0f + ez);
+      }
+      if (in) reinterpret_cast<T*>(a.ddt)[(row0 + lane) * a.H + h] = (T)dd;
+      const float sa = group_sum<64>(in ? d * da : 0.0f), sb = group_sum<64>(in ? dd : 0.0f),
+                  sd = group_sum<64>(in ? su[kSuDiag * kSsmC + lane] : 0.0f);
+      if (lane == 0) *reinterpret_cast<f32x4*>(a.part + ((size_t)slot * a.H + h) * kPart) = f32x4{sa, sb, sd, 0.0f};
+    };
+#pragma unroll 1
+    for (int h = h0; h < h1; ++h)
+#pragma unroll 1
+      for (int t = 0; t < turns; ++t) {
+        if (L::bufs == 1) __syncthreads();   // (0)
+        __syncthreads();                     // (1)
+        if (t == 0 && h > h0) finish(h - 1);
+      }
+    __syncthreads();   // (2)
+    finish(h1 - 1);
+    return;
+  }
+
+  const bool back = wave >= 4;   // (uniform) dB and dx
+  f32x4 acc[NT];                 // dC^T or dB^T: rows n, the tile's tokens
 #pragma unroll
   for (int j = 0; j < NT; ++j) acc[j] = zero4();
-  int parity = 0;
+  int n = 0;
+  if (!back) {   // ---- dC
 #pragma unroll 1
-  for (int h = h0; h < h1; ++h) {
-    // Q against the wave's tile: x (rows j) against its dy, or dy (rows i) against its x;
-    // L C B^T, rows i, columns j of the tile
-    f32x4 Q[4], LC[4];
-    float r = 0.0f, es = 0.0f, mine = 0.0f;
+    for (int h = h0; h < h1; ++h) {
+      f32x4 Q[4], ES = zero4();   // x (rows j) against the tile's dy; S against E
+      float r = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) Q[i] = LC[i] = zero4();
-    const float* sc = scal(h);
+      for (int i = 0; i < 4; ++i) Q[i] = zero4();
+      const float* sc = scal(h);
 #pragma unroll 1
-    for (int t = 0; t < turns; ++t) {
-      char* buf = smem + L::turn + parity * L::one;
-      anew();
-      if (L::ahead) {
-        vm_wait_all();
-        __syncthreads();   // this turn's rows are there, the other buffer's are no longer read
-        parity ^= 1;
-        if (t + 1 < turns) issue(h, t + 1, smem + L::turn + parity * L::one);
-        else if (h + 1 < h1) issue(h + 1, 0, smem + L::turn + parity * L::one);
-      } else {
-        __syncthreads();
-        issue(h, t, buf);
-        vm_wait_all();
-        __syncthreads();
-      }
-      anew();
-      if (t == 0 && wave == 0) {
-        if (h > h0) finish(h - 1, was);
-        was = raw;
-        if (h + 1 < h1) raw = dt_of(h + 1);
-      }
-      if (!back) {
+      for (int t = 0; t < turns; ++t, ++n) {
+        const char* buf = rows(n);
+        if (L::bufs == 1) __syncthreads();   // (0)
+        __syncthreads();                     // (1)
+        anew();
         const Fr<T> fy = VR::nat(buf + L::dY, w, 0, g, c);
         const float gam = sc[kSmGam * kSsmC + tok];
 #pragma unroll
         for (int i = 0; i < 4; ++i) Q[i] = mma<T>(VR::nat(buf + L::X, i, 0, g, c), fy, Q[i]);
+        if (w < NP) {   // (uniform) <E, S> of 32 n: the diagonal of their product
+#pragma unroll
+          for (int v = 0; v < 2; ++v)
+            ES = mma<T>(state_nat<T, N>(buf + L::S, v, w, g, c), state_nat<T, N>(buf + L::E, v, w, g, c), ES);
+        }
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-          const f32x4 u = mma<T>(state_tr<T, N>(buf + L::S, j, g, c), fy, zero4()) * gam;
-          acc[j] += u;
+          const f32x4 u = mma<T>(state_tr<T, N>(buf + L::S, j, g, c), fy, zero4());
+          acc[j] += u * gam;
           r += dot4(u, Quad<T>::f32(KR::quad(smem + L::C, w, j, g, c)));
         }
-        // <E, S>, by pieces of 16 bytes (both lie alike in LDS)
-        for (int i = 64 * w + lane; i < SR::bytes / 16; i += 256) {
-          float e[Chunk16<T>::N], s[Chunk16<T>::N];
-#pragma unroll
-          for (int u = 0; u < Chunk16<T>::N; ++u) e[u] = s[u] = 0.0f;
-#pragma unroll
-          for (int pl = SsmState<T, N>::planes - 1; pl >= 0; --pl) {
-            float fe[Chunk16<T>::N], fs[Chunk16<T>::N];
-            Chunk16<T>::unpack(*reinterpret_cast<const u32x4_t*>(buf + L::E + pl * SR::bytes + 16 * i), fe);
-            Chunk16<T>::unpack(*reinterpret_cast<const u32x4_t*>(buf + L::S + pl * SR::bytes + 16 * i), fs);
-#pragma unroll
-            for (int u = 0; u < Chunk16<T>::N; ++u) e[u] += fe[u], s[u] += fs[u];
-          }
-#pragma unroll
-          for (int u = 0; u < Chunk16<T>::N; ++u) es += e[u] * s[u];
-        }
-        continue;
       }
+      anew();
       const float Gh = sc[kSmGh * kSsmC + tok], Gl = sc[kSmGl * kSsmC + tok];
-      const float dj = sc[kSmD * kSsmC + tok], endj = sc[kSmEnd * kSsmC + tok];
-      if (t == 0) {
-#pragma unroll
-        for (int p = 0; p < NP; ++p) {
-          const Fr<T> fb = KR::nat(smem + L::B, w, p, g, c);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) LC[i] = mma<T>(KR::nat(smem + L::C, i, p, g, c), fb, LC[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x4 gh = four(sc + kSmGh * kSsmC + 16 * i + 4 * g), gl = four(sc + kSmGl * kSsmC + 16 * i + 4 * g);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int i1 = 16 * i + 4 * g + e;
-            LC[i][e] = masked((i1 >= tok) & (i1 < len), decay_between(gh[e], gl[e], Gh, Gl) * LC[i][e]);
-          }
-        }
-      }
-      const Fr<T> fx = VR::nat(buf + L::X, w, 0, g, c);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) Q[i] = mma<T>(VR::nat(buf + L::dY, i, 0, g, c), fx, Q[i]);
-#pragma unroll
-      for (int j = 0; j < NT; ++j) acc[j] += mma<T>(state_tr<T, N>(buf + L::E, j, g, c), fx, zero4()) * (dj * endj);
-      // dx: two tiles of p
-      T* dx = reinterpret_cast<T*>(a.dx) + (row0 * a.H + h) * a.P + t * kPw;
-      const float skip = a.D ? a.D[h] : 0.0f;
-      const Fi<T, kNear> Lf[2] = {to_fi<T, kNear>(LC[0], LC[1]), to_fi<T, kNear>(LC[2], LC[3])};
-#pragma unroll
-      for (int v = 0; v < 2; ++v) {
-        f32x4 u = zero4(), z = zero4();
-#pragma unroll
-        for (int p = 0; p < NP; ++p) u = mma<T>(state_nat<T, N>(buf + L::E, v, p, g, c), KR::nat(smem + L::B, w, p, g, c), u);
-#pragma unroll
-        for (int s = 0; s < 2; ++s) z = mma<T>(VR::tr32(buf + L::dY, s, v, g, c), Lf[s], z);
-        u *= endj;
-        r += dot4(u, Quad<T>::f32(VR::quad(buf + L::X, w, v, g, c)));
-        const f32x4 o = (u + z) * dj + Quad<T>::f32(VR::quad(buf + L::dY, w, v, g, c)) * skip;
-        if (tok < len) Quad<T>::st(dx + (size_t)tok * a.H * a.P + 16 * v + 4 * g, Quad<T>::cvt(o));
-      }
-    }
-    // what pairs of tokens add
-    anew();
-    const float Gh = sc[kSmGh * kSsmC + tok], Gl = sc[kSmGl * kSsmC + tok], dj = sc[kSmD * kSsmC + tok];
-    float* sum = sums(h);
-    if (!back) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const f32x4 gh = four(sc + kSmGh * kSsmC + 16 * i + 4 * g), gl = four(sc + kSmGl * kSsmC + 16 * i + 4 * g);
-        const f32x4 d = four(sc + kSmD * kSsmC + 16 * i + 4 * g);
+        if (i < w) {          // (uniform) from a tile before
+          Q[i] *= four(sc + kSmFD * kSsmC + 16 * i + 4 * g) * decay_between(Gh, Gl, sc[kSmTile + i], sc[kSmTile + 4 + i]);
+        } else if (i == w) {
+          const f32x4 gh = four(sc + kSmGh * kSsmC + 16 * i + 4 * g), gl = four(sc + kSmGl * kSsmC + 16 * i + 4 * g);
+          const f32x4 d = four(sc + kSmD * kSsmC + 16 * i + 4 * g);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          Q[i][e] = masked(16 * i + 4 * g + e <= tok, decay_between(Gh, Gl, gh[e], gl[e]) * d[e] * Q[i][e]);
+          for (int e = 0; e < 4; ++e) Q[i][e] = masked(4 * g + e <= c, decay_between(Gh, Gl, gh[e], gl[e]) * d[e] * Q[i][e]);
+        } else {
+          Q[i] = zero4();
+        }
       }
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
@@ -277,62 +239,124 @@ __global__ void __launch_bounds__(512, 2) carve_ssm_grad_kernel(SsmArgs a) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[j] = mma<T>(KR::tr32(smem + L::B, s, j, g, c), f, acc[j]);
       }
-      r = col_sum(r);
-      es = group_sum<64>(es);
-      if (g == 0) sum[tok] = r;
-      if (lane == 0) sum[8 * kSsmC + w] = es;
-      if (wave == 0 && h + 1 < h1) ssm_scalars(raw, lane < len, bias_of(h + 1), a.A[h + 1], a.softplus, lane, scal(h + 1));
-      continue;
-    }
-    float cm = 0.0f;
+      float* su = sums(h);
+      r = col_sum(r) * sc[kSmGam * kSsmC + tok];
+      float es = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const f32x4 gh = four(sc + kSmGh * kSsmC + 16 * i + 4 * g), gl = four(sc + kSmGl * kSsmC + 16 * i + 4 * g);
+      for (int e = 0; e < 4; ++e) es += masked(4 * g + e == c, ES[e]);
+      es = group_sum<64>(es);
+      if (g == 0) su[kSuR * kSsmC + tok] = r, su[kSuD * kSsmC + tok] = sc[kSmD * kSsmC + tok];
+      if (lane == 0) su[kSuES + w] = es, su[kSuWhole] = sc[kSmWhole];
+    }
+  } else {   // ---- dB, dx
+    f32x4 CB[4];   // C B^T: rows i, the tile's columns j
+    const char* cb = a.cb + ((size_t)slot * a.G + grp) * kSsmCB + 16 * lane;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) CB[i] = i >= w ? *reinterpret_cast<const f32x4*>(cb + ssm_tile(i, w)) : zero4();
+#pragma unroll 1
+    for (int h = h0; h < h1; ++h) {
+      f32x4 Q[4], D[4];   // dy (rows i) against the tile's x; L
+      float ex = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) Q[i] = D[i] = zero4();
+      const float* sc = scal(h);
+#pragma unroll 1
+      for (int t = 0; t < turns; ++t, ++n) {
+        const char* buf = rows(n);
+        if (L::bufs == 1) __syncthreads();   // (0)
+        __syncthreads();                     // (1)
+        anew();
+        if (t == 0) {
+          const float f = sc[kSmF * kSsmC + tok], Gh = sc[kSmGh * kSsmC + tok], Gl = sc[kSmGl * kSsmC + tok];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (i > w) {          // (uniform) to a tile behind
+              D[i] = four(sc + (kSmDown + w) * kSsmC + 16 * i + 4 * g) * f;
+            } else if (i == w) {
+              const f32x4 gh = four(sc + kSmGh * kSsmC + 16 * i + 4 * g), gl = four(sc + kSmGl * kSsmC + 16 * i + 4 * g);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) D[i][e] = masked(4 * g + e >= c, decay_between(gh[e], gl[e], Gh, Gl));
+            }
+          }
+        }
+        const Fr<T> fx = VR::nat(buf + L::X, w, 0, g, c);
+        const float dj = sc[kSmD * kSsmC + tok], endj = sc[kSmEnd * kSsmC + tok], endd = sc[kSmEndD * kSsmC + tok];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) Q[i] = mma<T>(VR::nat(buf + L::dY, i, 0, g, c), fx, Q[i]);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[j] += mma<T>(state_tr<T, N>(buf + L::E, j, g, c), fx, zero4()) * endd;
+        // dx: two tiles of p
+        const RowStore<T> dx(reinterpret_cast<T*>(a.dx) + (row0 * a.H + h) * a.P + t * kPw, (size_t)a.H * a.P, len, kPw);
+        const float skip = a.D ? a.D[h] : 0.0f;
+        const Fi<T, kNear> Lf[2] = {to_fi<T, kNear>(D[0] * CB[0], D[1] * CB[1]), to_fi<T, kNear>(D[2] * CB[2], D[3] * CB[3])};
+        f32x4 u[2] = {zero4(), zero4()}, z[2] = {zero4(), zero4()};
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+          const Fr<T> fb = KR::nat(smem + L::B, w, p, g, c);
+#pragma unroll
+          for (int v = 0; v < 2; ++v) u[v] = mma<T>(state_nat<T, N>(buf + L::E, v, p, g, c), fb, u[v]);
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int v = 0; v < 2; ++v) z[v] = mma<T>(VR::tr32(buf + L::dY, s, v, g, c), Lf[s], z[v]);
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          u[v] *= endj;
+          ex += dot4(u[v], Quad<T>::f32(VR::quad(buf + L::X, w, v, g, c)));
+          dx.st(tok, 16 * v + 4 * g, (u[v] + z[v]) * dj + Quad<T>::f32(VR::quad(buf + L::dY, w, v, g, c)) * skip);
+        }
+      }
+      anew();
+      // M = L C B^T Q and what it adds, tile after tile; Q becomes L d Q
+      const float dj = sc[kSmD * kSsmC + tok];
+      float* su = sums(h);
+      float cm = 0.0f, mine = 0.0f, carry = 0.0f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int i1 = 16 * i + 4 * g + e;
-        const bool on = (i1 >= tok) & (i1 < len);
-        LC[i][e] = masked(on, LC[i][e] * Q[i][e]);   // M
-        cm += LC[i][e];
-        LC[i][e] *= dj;
-        mine += masked(i1 == tok, Q[i][e]);
-        Q[i][e] = masked(on, decay_between(gh[e], gl[e], Gh, Gl) * dj * Q[i][e]);
+        float q4 = Q[0][e];
+#pragma unroll
+        for (int i = 1; i < 4; ++i) q4 = i == w ? Q[i][e] : q4;   // (uniform)
+        mine += masked(4 * g + e == c, q4);
       }
+      // sums of M over i >= t and j < t: suffix sums down each column, then along rows
+#pragma unroll
+      for (int i = 3; i >= 0; --i) {
+        f32x4 suf = zero4();
+        if (i >= w) {   // (uniform)
+          Q[i] *= D[i];
+          suf = CB[i] * Q[i];
+          cm += (suf[0] + suf[1]) + (suf[2] + suf[3]);
+          Q[i] *= dj;
+          suf *= dj;
+#pragma unroll
+          for (int e = 2; e >= 0; --e) suf[e] += suf[e + 1];
+          float in = suf[0];
+          const float n1 = __shfl(in, (lane + 16) & 63);
+          in += g < 3 ? n1 : 0.0f;
+          const float n2 = __shfl(in, (lane + 32) & 63);
+          in += g < 2 ? n2 : 0.0f;
+          const float behind = __shfl(in, (lane + 16) & 63), whole = __shfl(in, c);
+          const float more = carry + (g < 3 ? behind : 0.0f);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) suf[e] = masked(16 * i + 4 * g + e > tok, suf[e] + more);
+          carry += whole;
+        }
+        const float rect = row_sum4(suf, c);
+        if (c < 4) su[(kSuRect + w) * kSsmC + 16 * i + 4 * g + c] = rect;
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        if (s < w / 2) continue;   // (uniform)
+        const Fi<T, kNear> f = to_fi<T, kNear>(2 * s >= w ? Q[2 * s] : zero4(), Q[2 * s + 1]);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[j] = mma<T>(KR::tr32(smem + L::C, s, j, g, c), f, acc[j]);
+      }
+      ex = col_sum(ex), cm = col_sum(cm), mine = col_sum(mine);
+      if (g == 0) su[kSuE * kSsmC + tok] = ex, su[kSuM * kSsmC + tok] = cm, su[kSuDiag * kSsmC + tok] = mine;
     }
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      if (s < w / 2) continue;   // (uniform)
-      const Fi<T, kNear> f = to_fi<T, kNear>(Q[2 * s], Q[2 * s + 1]);
-#pragma unroll
-      for (int j = 0; j < NT; ++j) acc[j] = mma<T>(KR::tr32(smem + L::C, s, j, g, c), f, acc[j]);
-    }
-    // sums of M over i >= t and j < t: suffix sums down each column, then along rows
-    float carry = 0.0f;
-#pragma unroll
-    for (int i = 3; i >= 0; --i) {
-      f32x4 suf;
-      suf[3] = LC[i][3];
-#pragma unroll
-      for (int e = 2; e >= 0; --e) suf[e] = LC[i][e] + suf[e + 1];
-      float in = suf[0];
-      const float n1 = __shfl(in, (lane + 16) & 63);
-      in += g < 3 ? n1 : 0.0f;
-      const float n2 = __shfl(in, (lane + 32) & 63);
-      in += g < 2 ? n2 : 0.0f;
-      const float behind = __shfl(in, (lane + 16) & 63), whole = __shfl(in, c);
-      const float more = carry + (g < 3 ? behind : 0.0f);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) suf[e] = masked(16 * i + 4 * g + e > tok, suf[e] + more);
-      carry += whole;
-      const float rect = row_sum4(suf, c);
-      if (c < 4) sum[(4 + w) * kSsmC + 16 * i + 4 * g + c] = rect;
-    }
-    r = col_sum(r), cm = col_sum(cm), mine = col_sum(mine);
-    if (g == 0) sum[kSsmC + tok] = r, sum[2 * kSsmC + tok] = cm, sum[3 * kSsmC + tok] = mine;
   }
-  __syncthreads();
-  anew();
-  if (wave == 0) finish(h1 - 1, was);
+  __syncthreads();   // (2)
   settle();
   if (tok < len) {
     const size_t at = ((row0 + tok) * a.G + grp) * N + 4 * g;
@@ -404,7 +428,7 @@ int launch_t(const SsmArgs& a, hipStream_t s, void (*mark)(hipStream_t)) {
   const auto kern = carve_ssm_grad_kernel<T, N>;
   if (hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
     return CARVE_ERR_HIP;
-  hipLaunchKernelGGL(kern, dim3(a.nslots, a.G, a.splits), dim3(512), lds, s, a);
+  hipLaunchKernelGGL(kern, dim3(a.nslots, a.G, a.splits), dim3(768), lds, s, a);
   int st = launched();
   if (st) return st;
   mark(s);

@@ -41,33 +41,57 @@ struct Tile {
 
 __device__ __forceinline__ f32x4 four(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
 
-// The steps of a span's chunks, a chunk ahead: one wave holds the next chunk's dt and makes
-// its scalars while the others' rows are on their way.
-template <typename T>
-struct Steps {
-  const T* dt;             // of the span's first row
-  long long stride;
-  float A, bias;
-  int softplus, len, lane;
-  float raw;
-  __device__ __forceinline__ void fetch(int ch) {
-    const int t = ch * kSsmC + lane;
-    raw = ch >= 0 && t < len ? (float)dt[t * stride] : 0.0f;
+// Scalars and C B^T of every chunk slot: blockIdx.y < G a group's products, wave w making
+// its column tile w; behind them the scalars of 16 heads, four a wave.
+constexpr int kPrepHeads = 16;
+template <typename T, int N, bool BWD>
+__global__ void __launch_bounds__(256) carve_ssm_prep_kernel(SsmArgs a) {
+  typedef SsmRows<T, N, kSsmC> KR;
+  constexpr int NP = N / 32;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int slot = blockIdx.x;
+  const SsmSeq q = ssm_find(a, slot, kSsmC);
+  const int ch = slot - ssm_slot0(a, q, kSsmC);
+  if (ch < 0 || (long long)ch * kSsmC >= q.len) return;   // a slot of no chunk
+  const int first = q.first + ch * kSsmC, len = min(kSsmC, q.len - ch * kSsmC);
+  if ((int)blockIdx.y >= a.G) {
+    const int h0 = ((int)blockIdx.y - a.G) * kPrepHeads + w;
+    const T* dt = reinterpret_cast<const T*>(a.dt) + q.batch * a.ds[0] + (first + min(lane, len - 1)) * a.ds[1];
+    float raw[kPrepHeads / 4];
+#pragma unroll
+    for (int u = 0; u < kPrepHeads / 4; ++u) raw[u] = (float)dt[min(h0 + 4 * u, a.H - 1)];
+#pragma unroll
+    for (int u = 0; u < kPrepHeads / 4; ++u) {
+      const int h = h0 + 4 * u;
+      if (h >= a.H) return;
+      float* out = reinterpret_cast<float*>(a.scal) + ((size_t)slot * a.H + h) * (BWD ? kSmBwd : kSmFwd);
+      ssm_scalars<BWD>(raw[u], lane < len, a.dt_bias ? a.dt_bias[h] : 0.0f, a.A[h], a.softplus, lane, out);
+    }
+    return;
   }
-  __device__ __forceinline__ void make(int ch, float* out) const {
-    ssm_scalars(raw, ch * kSsmC + lane < len, bias, A, softplus, lane, out);
+  const int grp = blockIdx.y, g = lane >> 4, c = lane & 15;
+  KR::template dma<4>(smem, reinterpret_cast<const T*>(a.Bm) + q.batch * a.bs[0] + first * a.bs[1] + grp * a.bs[2],
+                      (int)(a.bs[1] * sizeof(T)), len, w, lane);
+  KR::template dma<4>(smem + KR::bytes, reinterpret_cast<const T*>(a.Cm) + q.batch * a.cs[0] + first * a.cs[1] + grp * a.cs[2],
+                      (int)(a.cs[1] * sizeof(T)), len, w, lane);
+  vm_wait_all();
+  __syncthreads();
+  const char *rows = smem + (BWD ? KR::bytes : 0), *cols = smem + (BWD ? 0 : KR::bytes);
+  f32x4 M[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) M[i] = zero4();
+#pragma unroll
+  for (int p = 0; p < NP; ++p) {
+    const Fr<T> f = KR::nat(cols, w, p, g, c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) M[i] = mma<T>(KR::nat(rows, i, p, g, c), f, M[i]);
   }
-};
-
-template <typename T>
-__device__ __forceinline__ Steps<T> steps_of(const SsmArgs& a, const SsmSpan& p, int h, int lane) {
-  Steps<T> s;
-  s.dt = reinterpret_cast<const T*>(a.dt) + p.q.batch * a.ds[0] + p.first * a.ds[1] + h;
-  s.stride = a.ds[1];
-  s.A = a.A[h];
-  s.bias = a.dt_bias ? a.dt_bias[h] : 0.0f;
-  s.softplus = a.softplus, s.len = p.len, s.lane = lane;
-  return s;
+  char* out = a.cb + ((size_t)slot * a.G + grp) * kSsmCB + 16 * lane;
+  settle();
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (BWD ? i >= w : i <= w) *reinterpret_cast<f32x4*>(out + (BWD ? ssm_tile(i, w) : ssm_tile(w, i))) = M[i];
 }
 
 // Chains of states without outputs.  Forward (REV false): what each span but a sequence's
@@ -78,7 +102,7 @@ template <typename T, int N, int NW>
 struct StateLds {
   typedef SsmRows<T, N, kSsmC> KR;
   typedef SsmRows<T, 16 * NW, kSsmC> VR;
-  static constexpr int K = 0, V = KR::bytes, S = V + VR::bytes, total = S + 2 * kSmFloats * 4;
+  static constexpr int K = 0, V = KR::bytes, S = V + VR::bytes, total = S + kSmFwd * 4;
 };
 template <typename T, int N, int NW, bool REV>
 __global__ void __launch_bounds__(64 * NW, 2) carve_ssm_state_kernel(SsmArgs a, int full) {
@@ -86,7 +110,7 @@ __global__ void __launch_bounds__(64 * NW, 2) carve_ssm_state_kernel(SsmArgs a, 
   typedef typename L::KR KR;
   typedef typename L::VR VR;
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  float* scal = reinterpret_cast<float*>(smem + L::S);
+  const float* sc = reinterpret_cast<const float*>(smem + L::S);
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, c = lane & 15;
   const int slices = a.P / (16 * NW);
@@ -107,25 +131,14 @@ __global__ void __launch_bounds__(64 * NW, 2) carve_ssm_state_kernel(SsmArgs a, 
   const long long ks = REV ? a.cs[1] : a.bs[1], vs = REV ? (long long)a.H * a.P : a.xs[1];
   const T* vb = REV ? reinterpret_cast<const T*>(a.dy) + (((size_t)p.q.batch * a.T + p.first) * a.H + h) * a.P + p0
                     : reinterpret_cast<const T*>(a.x) + p.q.batch * a.xs[0] + p.first * a.xs[1] + h * a.xs[2] + p0;
-  Steps<T> st = steps_of<T>(a, p, h, lane);
-  const auto chunk = [&](int i) { return REV ? p.nch - 1 - i : i; };
   float decay = 1.0f;
-  if (w == 0 && p.nch > 0) {
-    st.fetch(chunk(0));
-    st.make(chunk(0), scal);
-    if (p.nch > 1) st.fetch(chunk(1));
-  }
 #pragma unroll 1
   for (int i = 0; i < p.nch; ++i) {
-    const int ch = chunk(i), len = min(kSsmC, p.len - ch * kSsmC);
-    const float* sc = scal + (i & 1) * kSmFloats;
+    const int ch = REV ? p.nch - 1 - i : i, len = min(kSsmC, p.len - ch * kSsmC);
     if (i > 0) __syncthreads();   // the rows of the chunk before are no longer read
     KR::template dma<NW>(smem + L::K, kb + (long long)ch * kSsmC * ks, (int)(ks * sizeof(T)), len, w, lane);
     VR::template dma<NW>(smem + L::V, vb + (long long)ch * kSsmC * vs, (int)(vs * sizeof(T)), len, w, lane);
-    if (w == 0 && i + 1 < p.nch) {
-      st.make(chunk(i + 1), scal + ((i + 1) & 1) * kSmFloats);
-      if (i + 2 < p.nch) st.fetch(chunk(i + 2));
-    }
+    dma_flat<NW, 2>(smem + L::S, a.scal + ((size_t)(p.slot0 + ch) * a.H + h) * (REV ? kSmBwd : kSmFwd) * 4, w, lane);
     if (REV && full) {   // the gradient of the state behind this chunk
       SsmState<T, N>::st(a.E_chunks + ((size_t)(p.slot0 + ch) * a.H + h) * pn * 4, pn, p0 + 16 * w, t.S, lane);
     }
@@ -188,150 +201,120 @@ __global__ void __launch_bounds__(256) carve_ssm_join_kernel(SsmArgs a) {
 // Outputs of a span: its chunks one after another, the state in registers.  A workgroup
 // takes two units (a head's 16 NW value rows) of one group, which share B and C; waves hold
 // 16 value rows each.  A chunk:
-//   all waves   L d C B^T of both units, a pair of tiles a wave: operand images in LDS
+//   all waves   L d C B^T of both units from C B^T, a pair of tiles a wave: operand images in LDS
 //   its waves   Y^T = S (e^G C)^T + X^T (L d C B^T)^T + D X^T, then S as above
-// Four more waves bring the next chunk's rows into LDS and make its scalars: a wave that
-// reads LDS waits for all the LDS loads it has under way, so the loads are others'.
+// Bound by the latency of these steps: two workgroups a compute unit take turns with loads
+// and products.
 template <typename T, int N, int NW>
 struct OutLds {
   typedef SsmRows<T, N, kSsmC> KR;
   typedef SsmRows<T, 16 * NW, kSsmC> VR;
-  static constexpr int B = 0, C = KR::bytes, X = 2 * KR::bytes, one = X + 2 * VR::bytes;
-  static constexpr int image = img_bytes<T>(kNear), small = 2 * image + 4 * kSmFloats * 4;
-  static constexpr int bufs = 2 * one + small <= 160 * 1024 ? 2 : 1;
-  static constexpr int P = bufs * one, S = P + 2 * image, total = S + 4 * kSmFloats * 4;
+  static constexpr int B = 0, C = KR::bytes, X = 2 * KR::bytes;
+  static constexpr int image = img_bytes<T>(kNear), P = X + 2 * VR::bytes, S = P + 2 * image, total = S + 2 * kSmFwd * 4;
 };
 template <typename T, int N, int NW>
-__global__ void __launch_bounds__(128 * NW + 256, NW == 4 ? 3 : 2) carve_ssm_out_kernel(SsmArgs a) {
+__global__ void __launch_bounds__(128 * NW, sizeof(T) == 2 && NW == 4 ? 4 : 2) carve_ssm_out_kernel(SsmArgs a) {
   typedef OutLds<T, N, NW> L;
   typedef typename L::KR KR;
   typedef typename L::VR VR;
-  constexpr int NP = N / 32;
+  constexpr int NP = N / 32, WAVES = 2 * NW, PER = 8 / WAVES;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = lane >> 4, c = lane & 15, un = wave / NW, w = wave % NW;
   const int slices = a.P / (16 * NW), rep = a.H / a.G, units = rep * slices, pairs = (units + 1) / 2;
   SsmSpan p;
   int rest;
   if (!ssm_block(a, a.G * pairs, p, rest)) return;
   const int grp = rest / pairs, u0 = 2 * (rest % pairs);   // the workgroup's first unit of the group
   const int have = min(2, units - u0);
-  const auto scal = [&](int u, int ch) { return reinterpret_cast<float*>(smem + L::S) + (2 * u + (ch & 1)) * kSmFloats; };
-  const auto rows = [&](int ch) { return smem + (L::bufs == 2 ? (ch & 1) * L::one : 0); };
-
-  if (wave >= 2 * NW) {   // ---- rows and scalars
-    const int k = wave - 2 * NW;
-    const int h0 = grp * rep + u0 / slices, h1 = grp * rep + (u0 + have - 1) / slices;   // heads of the units
-    const T* Bm = reinterpret_cast<const T*>(a.Bm) + p.q.batch * a.bs[0] + p.first * a.bs[1] + grp * a.bs[2];
-    const T* Cm = reinterpret_cast<const T*>(a.Cm) + p.q.batch * a.cs[0] + p.first * a.cs[1] + grp * a.cs[2];
-    const T* x = reinterpret_cast<const T*>(a.x) + p.q.batch * a.xs[0] + p.first * a.xs[1];
-    const T* x0 = x + h0 * a.xs[2] + u0 % slices * 16 * NW;
-    const T* x1 = x + h1 * a.xs[2] + (u0 + have - 1) % slices * 16 * NW;
-    const auto issue = [&](int ch) {
-      const int len = min(kSsmC, p.len - ch * kSsmC);
-      char* to = rows(ch);
-      if (k == 0) KR::template dma<1>(to + L::B, Bm + (long long)ch * kSsmC * a.bs[1], (int)(a.bs[1] * sizeof(T)), len, 0, lane);
-      if (k == 1) KR::template dma<1>(to + L::C, Cm + (long long)ch * kSsmC * a.cs[1], (int)(a.cs[1] * sizeof(T)), len, 0, lane);
-      if (k >= 2) VR::template dma<1>(to + L::X + (k - 2) * VR::bytes, (k == 2 ? x0 : x1) + (long long)ch * kSsmC * a.xs[1],
-                                      (int)(a.xs[1] * sizeof(T)), len, 0, lane);
-    };
-    const int hs = k == 2 ? h0 : h1;   // waves 2 and 3: scalars of a unit
-    Steps<T> st = steps_of<T>(a, p, hs, lane);
-    if (k >= 2 && p.nch > 0) {
-      st.fetch(0);
-      st.make(0, scal(k - 2, 0));
-      if (p.nch > 1) st.fetch(1);
-    }
-    if (L::bufs == 2 && p.nch > 0) issue(0);
-#pragma unroll 1
-    for (int ch = 0; ch < p.nch; ++ch) {
-      if (L::bufs == 1) {
-        __syncthreads();   // (0) the rows of the chunk before are no longer read
-        issue(ch);
-      }
-      vm_wait_all();
-      __syncthreads();     // (1)
-      if (L::bufs == 2 && ch + 1 < p.nch) issue(ch + 1);
-      if (k >= 2 && ch + 1 < p.nch) {
-        st.make(ch + 1, scal(k - 2, ch + 1));
-        if (ch + 2 < p.nch) st.fetch(ch + 2);
-      }
-      __syncthreads();     // (2)
-    }
-    return;
-  }
-
-  // ---- outputs and states
-  const int g = lane >> 4, c = lane & 15, un = wave / NW, w = wave % NW;
   const bool mine = un < have;
-  const int unit = min(u0 + un, units - 1), h = grp * rep + unit / slices, p0 = unit % slices * 16 * NW + 16 * w;
+  // (waves of a unit that is not there do the other's work and write nothing)
+  const int unit = u0 + min(un, have - 1), h = grp * rep + unit / slices, slice0 = unit % slices * 16 * NW, p0 = slice0 + 16 * w;
   const size_t pn = (size_t)a.P * N, row = (size_t)(p0 + c) * N + 4 * g;
+  const float* scal = reinterpret_cast<const float*>(smem + L::S);
+  const float* sc = scal + un * kSmFwd;
   Tile<T, N> t;
   if (p.s > 0) t.load(a.Z + ((size_t)p.slot * a.H + h) * pn + row);
   else if (a.S0) t.load(a.S0 + ((size_t)p.q.n * a.H + h) * pn + row);
   else t.zero();
-  T* y = reinterpret_cast<T*>(a.y) + (((size_t)p.q.batch * a.T + p.first) * a.H + h) * a.P + p0 + 4 * g;
+  const T* Bm = reinterpret_cast<const T*>(a.Bm) + p.q.batch * a.bs[0] + p.first * a.bs[1] + grp * a.bs[2];
+  const T* Cm = reinterpret_cast<const T*>(a.Cm) + p.q.batch * a.cs[0] + p.first * a.cs[1] + grp * a.cs[2];
+  const T* x = reinterpret_cast<const T*>(a.x) + p.q.batch * a.xs[0] + p.first * a.xs[1] + h * a.xs[2] + slice0;
+  T* y = reinterpret_cast<T*>(a.y) + (((size_t)p.q.batch * a.T + p.first) * a.H + h) * a.P + p0;
   const size_t yrow = (size_t)a.H * a.P;
   const float skip = a.D ? a.D[h] : 0.0f;
+  const char* xb = smem + L::X + un * VR::bytes;
 #pragma unroll 1
   for (int ch = 0; ch < p.nch; ++ch) {
     const int len = min(kSsmC, p.len - ch * kSsmC);
-    const char* buf = rows(ch);
-    if (L::bufs == 1) __syncthreads();   // (0)
+    if (ch > 0) __syncthreads();   // (0) the chunk before is done with
+    KR::template dma<WAVES>(smem + L::B, Bm + (long long)ch * kSsmC * a.bs[1], (int)(a.bs[1] * sizeof(T)), len, wave, lane);
+    KR::template dma<WAVES>(smem + L::C, Cm + (long long)ch * kSsmC * a.cs[1], (int)(a.cs[1] * sizeof(T)), len, wave, lane);
+    VR::template dma<NW>(smem + L::X + un * VR::bytes, x + (long long)ch * kSsmC * a.xs[1], (int)(a.xs[1] * sizeof(T)), len, w, lane);
+    dma_flat<NW, 2>(smem + L::S + un * kSmFwd * 4, a.scal + ((size_t)(p.slot0 + ch) * a.H + h) * kSmFwd * 4, w, lane);
+    // C B^T of the wave's tiles (i, j = 2 s, 2 s + 1), i = 0 .. 3, s = 0, 1
+    f32x4 M[PER][2];
+#pragma unroll
+    for (int v = 0; v < PER; ++v) {
+      const int id = wave + WAVES * v, i = id & 3, s = id >> 2;
+      const char* cb = a.cb + ((size_t)(p.slot0 + ch) * a.G + grp) * kSsmCB + 16 * lane;
+#pragma unroll
+      for (int b = 0; b < 2; ++b) M[v][b] = 2 * s + b <= i ? *reinterpret_cast<const f32x4*>(cb + ssm_tile(i, 2 * s + b)) : zero4();
+    }
     if (a.S_chunks && mine) SsmState<T, N>::st(a.S_chunks + ((size_t)(p.slot0 + ch) * a.H + h) * pn * 4, pn, p0, t.S, lane);
-    __syncthreads();   // (1) the chunk's rows and scalars are there, the images no longer read
+    vm_wait_all();
+    __syncthreads();   // (1) its rows and scalars are there
     // L d C B^T: rows j of the result (tiles 2 s, 2 s + 1), columns the tokens i of a tile
-    {
-      constexpr int PER = 8 / (2 * NW);   // (i, s) of a wave: i = 0 .. 3, s = 0, 1
 #pragma unroll
-      for (int v = 0; v < PER; ++v) {
-        const int id = wave + 2 * NW * v, i = id & 3, s = id >> 2;
-        if (s > i / 2) continue;   // (uniform)
-        f32x4 M[2] = {zero4(), zero4()};
+    for (int v = 0; v < PER; ++v) {
+      const int id = wave + WAVES * v, i = id & 3, s = id >> 2;
+      if (s > i / 2) continue;   // (uniform)
 #pragma unroll
-        for (int q = 0; q < NP; ++q) {
-          const Fr<T> fc = KR::nat(buf + L::C, i, q, g, c);
+      for (int u = 0; u < 2; ++u) {
+        const float* su = scal + u * kSmFwd;
+        const float Gh = su[kSmGh * kSsmC + 16 * i + c], Gl = su[kSmGl * kSsmC + 16 * i + c];
+        f32x4 W[2];
 #pragma unroll
-          for (int b = 0; b < 2; ++b) M[b] = mma<T>(KR::nat(buf + L::B, 2 * s + b, q, g, c), fc, M[b]);
-        }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          if (u >= have) break;   // (uniform)
-          const float* sc = scal(u, ch);
-          const float Gh = sc[kSmGh * kSsmC + 16 * i + c], Gl = sc[kSmGl * kSsmC + 16 * i + c];
-          f32x4 W[2];
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            const int at = 32 * s + 16 * b + 4 * g;
-            const f32x4 gh = four(sc + kSmGh * kSsmC + at), gl = four(sc + kSmGl * kSsmC + at), d = four(sc + kSmD * kSsmC + at);
+        for (int b = 0; b < 2; ++b) {
+          const int j = 2 * s + b, at = 16 * j + 4 * g;
+          if (j < i) {   // (uniform) from a tile before: one exponential a token, F d of the other
+            const float down = decay_between(Gh, Gl, su[kSmTile + j], su[kSmTile + 4 + j]);
+            W[b] = M[v][b] * (four(su + kSmFD * kSsmC + at) * down);
+          } else {       // within the tile, and nothing from behind it
+            const f32x4 gh = four(su + kSmGh * kSsmC + at), gl = four(su + kSmGl * kSsmC + at), d = four(su + kSmD * kSsmC + at);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              W[b][e] = masked(at + e <= 16 * i + c, M[b][e] * (decay_between(Gh, Gl, gh[e], gl[e]) * d[e]));
+              W[b][e] = masked(at + e <= 16 * i + c, M[v][b][e] * (decay_between(Gh, Gl, gh[e], gl[e]) * d[e]));
           }
-          st_img<T, kNear>(smem + L::P + u * L::image, img_lower(i, s), lane, W[0], W[1]);
         }
+        st_img<T, kNear>(smem + L::P + u * L::image, img_lower(i, s), lane, W[0], W[1]);
       }
     }
-    Fi<T, kNear> Sf[NP];
-#pragma unroll
-    for (int q = 0; q < NP; ++q) Sf[q] = to_fi<T, kNear>(t.S[2 * q], t.S[2 * q + 1]);
-    __syncthreads();   // (2)
-    if (!mine) continue;
-    const float* sc = scal(un, ch);
-    const char* xb = buf + L::X + un * VR::bytes;
+    __syncthreads();   // (2) the images are there
     const Fr<T> fx[2] = {VR::tr32(xb, 0, w, g, c), VR::tr32(xb, 1, w, g, c)};
+    // (four token tiles side by side: a tile's products follow each other)
+    f32x4 o[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f32x4 o = zero4(), z = zero4();
+    for (int i = 0; i < 4; ++i) o[i] = zero4();
 #pragma unroll
-      for (int q = 0; q < NP; ++q) o = mma<T>(Sf[q], KR::nat(buf + L::C, i, q, g, c), o);
+    for (int q = 0; q < NP; ++q) {
+      const Fi<T, kNear> Sf = to_fi<T, kNear>(t.S[2 * q], t.S[2 * q + 1]);
 #pragma unroll
-      for (int s = 0; s <= i / 2; ++s) z = mma<T>(fx[s], ld_img<T, kNear>(smem + L::P + un * L::image, img_lower(i, s), lane), z);
-      const int tok = 16 * i + c;
-      const f32x4 xv = Quad<T>::f32(VR::quad(xb, i, w, g, c));
-      o = o * sc[kSmGam * kSsmC + tok] + z + xv * skip;
-      if (tok < len) Quad<T>::st(y + (size_t)(ch * kSsmC + tok) * yrow, Quad<T>::cvt(o));
+      for (int i = 0; i < 4; ++i) o[i] = mma<T>(Sf, KR::nat(smem + L::C, i, q, g, c), o[i]);
     }
-    t.template add<KR>(buf + L::B, fx, [&](int at) { return four(sc + kSmEndD * kSsmC + at); }, sc[kSmWhole], g, c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] *= sc[kSmGam * kSsmC + 16 * i + c];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+#pragma unroll
+      for (int i = 2 * s; i < 4; ++i) o[i] = mma<T>(fx[s], ld_img<T, kNear>(smem + L::P + un * L::image, img_lower(i, s), lane), o[i]);
+    }
+    if (mine) {
+      const RowStore<T> out(y + (size_t)ch * kSsmC * yrow, yrow, len, 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) out.st(16 * i + c, 4 * g, o[i] + Quad<T>::f32(VR::quad(xb, i, w, g, c)) * skip);
+    }
+    t.template add<KR>(smem + L::B, fx, [&](int at) { return four(sc + kSmEndD * kSsmC + at); }, sc[kSmWhole], g, c);
   }
   settle();
   if (mine && a.S_T && p.s == p.nspan - 1) t.store(a.S_T + ((size_t)p.q.n * a.H + h) * pn + row);
@@ -360,8 +343,21 @@ int launch_join(const SsmArgs& a, hipStream_t s) {
 // Whether any sequence can have more than one span (packed lengths are not known here)
 bool split(const SsmArgs& a) { return a.T > a.span * kSsmC; }
 
+template <typename T, int N, bool BWD>
+int launch_prep(const SsmArgs& a, hipStream_t s) {
+  constexpr int lds = 2 * SsmRows<T, N, kSsmC>::bytes;
+  const auto kern = carve_ssm_prep_kernel<T, N, BWD>;
+  if (!lds_attr(kern, lds)) return CARVE_ERR_HIP;
+  hipLaunchKernelGGL(kern, dim3(a.nslots, a.G + (a.H + kPrepHeads - 1) / kPrepHeads), dim3(256), lds, s, a);
+  return launched();
+}
 template <typename T, int N, int NW, bool REV>
 int launch_spans(const SsmArgs& a, hipStream_t s, void (*mark)(hipStream_t)) {
+  {
+    const int st = launch_prep<T, N, REV>(a, s);
+    if (st) return st;
+    mark(s);
+  }
   if (split(a)) {
     int st = launch_state<T, N, NW, REV>(a, 0, s);
     if (st) return st;
@@ -386,7 +382,7 @@ int launch_fwd_t(const SsmArgs& a, hipStream_t s, void (*mark)(hipStream_t)) {
   const auto kern = carve_ssm_out_kernel<T, N, NW>;
   if (!lds_attr(kern, lds)) return CARVE_ERR_HIP;
   const int pairs = (a.H / a.G * (a.P / (16 * NW)) + 1) / 2;
-  hipLaunchKernelGGL(kern, dim3(ssm_grid(a.nspans, a.G * pairs)), dim3(128 * NW + 256), lds, s, a);
+  hipLaunchKernelGGL(kern, dim3(ssm_grid(a.nspans, a.G * pairs)), dim3(128 * NW), lds, s, a);
   st = launched();
   mark(s);
   return st;
