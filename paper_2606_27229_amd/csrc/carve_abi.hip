@@ -1171,9 +1171,15 @@ SsmPlan ssm_plan(const carve_ssm_dims_t* d) {
   p.span = (int)((units + n - 1) / n);
   const long long L = (long long)p.span * kSsmC;
   p.spans = d->N ? (size_t)(d->T / L) + d->N : (size_t)(d->B * ((d->T + L - 1) / L));
-  const long long rep = d->H / d->G, want = (long long)(512 + p.chunks * d->G - 1) / (long long)(p.chunks * d->G);
-  p.splits = (int)(want < rep ? want : rep);
-  if (p.splits < 1) p.splits = 1;
+  // Shares of a group's heads: the gradients run one workgroup a compute unit, in turns of
+  // 256, each of which takes its heads and about as long as one more to begin and end.
+  const long long rep = d->H / d->G, wgs = (long long)p.chunks * d->G;
+  double best = 0.0;
+  p.splits = 1;
+  for (long long s = 1; s <= rep && s <= 64; s *= 2) {
+    const double cost = (double)((wgs * s + 255) / 256) * ((double)((rep + s - 1) / s) + 1.0);
+    if (s == 1 || cost < 0.95 * best) best = cost, p.splits = (int)s;
+  }
   return p;
 }
 // the chunk form's: a launch has less than 2^32 threads of each dimension

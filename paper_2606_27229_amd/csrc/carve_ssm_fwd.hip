@@ -58,16 +58,17 @@ __global__ void __launch_bounds__(256) carve_ssm_prep_kernel(SsmArgs a) {
   if ((int)blockIdx.y >= a.G) {
     const int h0 = ((int)blockIdx.y - a.G) * kPrepHeads + w;
     const T* dt = reinterpret_cast<const T*>(a.dt) + q.batch * a.ds[0] + (first + min(lane, len - 1)) * a.ds[1];
-    float raw[kPrepHeads / 4];
-#pragma unroll
-    for (int u = 0; u < kPrepHeads / 4; ++u) raw[u] = (float)dt[min(h0 + 4 * u, a.H - 1)];
+    float raw[kPrepHeads / 4], bias[kPrepHeads / 4], A[kPrepHeads / 4];
 #pragma unroll
     for (int u = 0; u < kPrepHeads / 4; ++u) {
-      const int h = h0 + 4 * u;
-      if (h >= a.H) return;
-      float* out = reinterpret_cast<float*>(a.scal) + ((size_t)slot * a.H + h) * (BWD ? kSmBwd : kSmFwd);
-      ssm_scalars<BWD>(raw[u], lane < len, a.dt_bias ? a.dt_bias[h] : 0.0f, a.A[h], a.softplus, lane, out);
+      const int h = min(h0 + 4 * u, a.H - 1);
+      raw[u] = (float)dt[h], bias[u] = a.dt_bias ? a.dt_bias[h] : 0.0f, A[u] = a.A[h];
     }
+    // (heads behind the last repeat it, so that the four of a wave run side by side)
+#pragma unroll
+    for (int u = 0; u < kPrepHeads / 4; ++u)
+      ssm_scalars<BWD>(raw[u], lane < len, bias[u], A[u], a.softplus, lane,
+                       reinterpret_cast<float*>(a.scal) + ((size_t)slot * a.H + min(h0 + 4 * u, a.H - 1)) * (BWD ? kSmBwd : kSmFwd));
     return;
   }
   const int grp = blockIdx.y, g = lane >> 4, c = lane & 15;
