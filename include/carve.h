@@ -511,8 +511,9 @@ int carve_rotary(const carve_rotary_dims_t* d, const void* q, const void* k, con
  *     A, D, dt_bias [H] f32 (D, dt_bias may be NULL: 0).
  *   - S0, S_T, dS_T, dS0 [sequences, H, P, S] f32; packed sequences (N > 0, offsets) as
  *     for the gated delta rule.
- *   - S_chunks: [carve_ssm_chunk_count(d), H, P, S] of 4 bytes each, written by
- *     carve_ssm_chunk_fwd for carve_ssm_chunk_bwd, in a form of their own.
+ *   - S_chunks: [carve_ssm_chunk_count(d), H, P, S] f32, the state at the start of every
+ *     chunk, written by carve_ssm_chunk_fwd for carve_ssm_chunk_bwd (slots of no chunk are
+ *     left as they were).
  *   - Supported: S in {32, 64, 128}; P a multiple of 32, at most 256; H a multiple of G,
  *     at most 65535; dtype f32 or bf16.  Chunk count, and spans * H * P / 32 rounded up
  *     to eights, below 2^23 (a span is four chunks or more; sequences are at most

@@ -1168,8 +1168,8 @@ def ssm_chunk_fwd(x, dt, A, Bm, Cm, S0=None, *, D=None, dt_bias=None, softplus=T
     multiples of 16 bytes), dt [B,T,H]; A (<= 0), D, dt_bias f32 [H], D and dt_bias may be
     None; head h reads group h // (H // G) of Bm and Cm; S0 [B,H,P,N] f32 or None.
     softplus=False: d_t = dt_t + dt_bias.  offsets (int32 [n + 1]): packed sequences as in
-    ``gdr_chunk_fwd``.  Returns (y, S_T, S_chunks); S_chunks (of its own form) is what
-    ``ssm_chunk_bwd`` needs.  ``out`` may hold preallocated {"y", "S_T", "S_chunks"}."""
+    ``gdr_chunk_fwd``.  Returns (y, S_T, S_chunks); S_chunks is what ``ssm_chunk_bwd``
+    needs.  ``out`` may hold preallocated {"y", "S_T", "S_chunks"}."""
     lib = load_library()
     dims, chunks, ws_bytes, _, seqs, ptrs = _ssm_call(x, dt, A, Bm, Cm, D, dt_bias, softplus, offsets)
     H, P, N, f32, dev = x.shape[2], x.shape[3], Bm.shape[3], torch.float32, x.device

@@ -1205,7 +1205,7 @@ SsmWs ssm_ws(const carve_ssm_dims_t* d, bool bwd) {
   size_t off = 0;
   const bool split = ssm_split(d, p);
   w.scal = off, off += align256(p.chunks * d->H * (bwd ? kSmBwd : kSmFwd) * 4);
-  w.cb = off, off += align256(p.chunks * d->G * kSsmCB);
+  w.cb = off, off += align256(p.chunks * d->G * (bwd ? 2 : 1) * kSsmCB);
   w.Z = off, off += split ? align256(p.spans * ssm_state(d)) : 0;
   w.Zg = off, off += split ? align256(p.spans * d->H * 4) : 0;
   if (bwd) {
@@ -1232,7 +1232,7 @@ void ssm_args(SsmArgs& a, const carve_ssm_dims_t* d, const void* x, const void* 
   char* ws = static_cast<char*>(workspace);
   a.Z = reinterpret_cast<float*>(ws + w.Z), a.Zg = reinterpret_cast<float*>(ws + w.Zg);
   a.scal = ws + w.scal, a.cb = ws + w.cb;
-  a.E_chunks = ws + w.E, a.part = reinterpret_cast<float*>(ws + w.part), a.dBp = reinterpret_cast<float*>(ws + w.dBp);
+  a.E_chunks = reinterpret_cast<float*>(ws + w.E), a.part = reinterpret_cast<float*>(ws + w.part), a.dBp = reinterpret_cast<float*>(ws + w.dBp);
 }
 int ssm_inputs(const carve_ssm_dims_t* d, const void* x, const void* dt, const float* A, const void* Bm, const void* Cm,
                const float* D, const float* dt_bias, Range* r) {
@@ -1291,7 +1291,7 @@ int carve_ssm_chunk_fwd(const carve_ssm_dims_t* d, const void* x, const void* dt
   if (any_overlap(outs, 4, ins, nin)) return CARVE_ERR_UNSUPPORTED;
   SsmArgs a;
   ssm_args(a, d, x, dt, A, Bm, Cm, D, dt_bias, offsets, workspace, false);
-  a.S0 = S0, a.y = y, a.S_T = S_T, a.S_chunks = reinterpret_cast<char*>(S_chunks);
+  a.S0 = S0, a.y = y, a.S_T = S_T, a.S_chunks = S_chunks;
   prof_mark(stream);
   return launch_ssm_fwd(a, d->dtype, stream, prof_mark);
 }
@@ -1329,7 +1329,7 @@ int carve_ssm_chunk_bwd(const carve_ssm_dims_t* d, const void* x, const void* dt
   if (any_overlap(outs, 9, ins, nin)) return CARVE_ERR_UNSUPPORTED;
   SsmArgs a;
   ssm_args(a, d, x, dt, A, Bm, Cm, D, dt_bias, offsets, workspace, true);
-  a.S_chunks = const_cast<char*>(reinterpret_cast<const char*>(S_chunks));   // (read only)
+  a.S_chunks = const_cast<float*>(S_chunks);   // (read only)
   a.dy = dy, a.dS_T = dS_T, a.dx = dx, a.ddt = ddt, a.dA = dA, a.dBm = dBm, a.dCm = dCm, a.dD = dD;
   a.ddt_bias = ddt_bias, a.dS0 = dS0;
   prof_mark(stream);

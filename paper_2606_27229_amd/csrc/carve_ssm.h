@@ -29,10 +29,10 @@ struct SsmArgs {
   const int* offsets;      // packed sequences: [nseq + 1]; dense: NULL
   void *y, *dx, *ddt, *dBm, *dCm;
   float *S_T, *dA, *dD, *ddt_bias, *dS0;
-  char *S_chunks, *E_chunks;   // states at chunk starts, state gradients at chunk ends: see SsmState
+  float *S_chunks, *E_chunks;   // [nslots][H][P][N]: states at chunk starts, state gradients at chunk ends
   float* Z;                // [nspans][H][P][N]: what a span adds, then the state it starts from
   float* Zg;               // [nspans][H]: its decay
-  char* scal;              // [nslots][H]: scalars; cb: [nslots][G], C B^T
+  char* scal;              // [nslots][H]: scalars; cb: [nslots][G], C B^T (backward: twice)
   char* cb;
   float* part;             // [nslots][H][4]: a chunk's share of dA, ddt_bias, dD
   float* dBp;              // [splits][rows][G][N], dCp behind it: shares of dB, dC
@@ -86,8 +86,8 @@ enum : int { kSmD = 0, kSmGh = 1, kSmGl = 2, kSmGam = 3, kSmEnd = 4, kSmEndD = 5
              kSmWhole = kSmTile + 8, kSmFwd = 8 * kSsmC, kSmF = 8, kSmDown = 9, kSmBwd = 12 * kSsmC };
 constexpr float kSmNever = -1e7f;   // (64 tokens reach -10^6)
 // C B^T of a (slot, group): its ten tiles on and below the diagonal, 1 KB each as result
-// tiles; tile (i, j) at ssm_tile(i, j).  Forward: rows j, columns i; backward: rows i,
-// columns j.
+// tiles (rows j, columns i); tile (i, j) at ssm_tile(i, j).  For the backward the same with
+// rows i, columns j behind them.
 constexpr int kSsmCB = 10 * 1024;
 __host__ __device__ constexpr int ssm_tile(int i, int j) { return (i * (i + 1) / 2 + j) * 1024; }
 
@@ -150,72 +150,26 @@ struct SsmRows : GdrRows<T, COLS> {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(r, lds_at(lds + 1024 * i), 16, (int)__umul24(min(row, len - 1), stride) + 16 * x, 0, 0, 0);
     }
   }
+  // lane (g, c): row 16 i + c, columns 32 p + 8 g + e, e < 8: for products both of whose
+  // operands are read so (16 bytes at once, where nat's order is that of result tiles)
+  static __device__ __forceinline__ Fr<T> nat8(const char* lds, int i, int p, int g, int c) {
+    Fr<T> f;
+    if constexpr (sizeof(T) == 2) {
+      const bf16x8 v = *reinterpret_cast<const bf16x8*>(lds + (16 * i + c) * R::RB + (((4 * p + g) ^ R::swz(c)) << 4));
+      f.a = __builtin_shufflevector(v, v, 0, 1, 2, 3);
+      f.b = __builtin_shufflevector(v, v, 4, 5, 6, 7);
+    } else {
+      f.a = Quad<T>::ld(reinterpret_cast<const T*>(lds + (16 * i + c) * R::RB + (((8 * p + 2 * g) ^ R::swz(c)) << 4)));
+      f.b = Quad<T>::ld(reinterpret_cast<const T*>(lds + (16 * i + c) * R::RB + (((8 * p + 2 * g + 1) ^ R::swz(c)) << 4)));
+    }
+    return f;
+  }
   // lane (g, c): row 16 i + c, columns 16 j + 4 g + e
   static __device__ __forceinline__ typename Quad<T>::q quad(const char* lds, int i, int j, int g, int c) {
     int o;
     if constexpr (sizeof(T) == 2) o = (((2 * j + (g >> 1)) ^ R::swz(c)) << 4) + ((g & 1) << 3);
     else o = ((4 * j + g) ^ R::swz(c)) << 4;
     return Quad<T>::ld(reinterpret_cast<const T*>(lds + (16 * i + c) * R::RB + o));
-  }
-};
-
-// States kept for the backward, a head's P x N values of 4 bytes in blocks of 16 rows p by
-// 64 bytes of n, so that a wave's store is 1 KB in one piece: f32, or with bf16 tokens two
-// planes of bf16, the upper and the lower half of the significand's first 16 bits (as many
-// bytes).  They only enter products towards bf16 results and the sums of dA, and matrix
-// cores take the planes as they are: the gradients' kernel needs no conversion of them (its
-// LDS holds them as loaded).
-template <typename T, int N>
-struct SsmState {
-  static constexpr int planes = sizeof(T) == 2 ? 2 : 1;
-  static constexpr int BN = 64 / (int)sizeof(T);       // n of a block
-  // bytes of 16-byte piece x of row p
-  static __device__ __forceinline__ unsigned at(int p, int x) {
-    return (unsigned)(((p >> 4) * (N / BN) + (x >> 2)) * 1024 + (p & 15) * 64 + (x & 3) * 16);
-  }
-  // the values of 16 rows from p0 as they lie in registers (lane (g, c): n = 16 j + 4 g + e,
-  // row p0 + c); head: the head's values, of pn elements
-  static __device__ __forceinline__ void st(char* head, size_t pn, int p0, const f32x4 (&S)[N / 16], int lane) {
-    if constexpr (sizeof(T) == 2) {
-      char* to = head + (p0 >> 4) * (N / BN) * 1024;
-      const int g = lane >> 4, c = lane & 15;
-      // tile 2 u's values go to even rows of lanes, tile 2 u + 1's to odd ones: eight
-      // neighbouring n a lane
-      const unsigned off = (unsigned)(c * 64 + (g & 1) * 32 + (g >> 1) * 16);
-#pragma unroll
-      for (int u = 0; u < N / 32; ++u) {
-        f32x4 a = S[2 * u], b = S[2 * u + 1];
-#pragma unroll
-        for (int pl = 0; pl < 2; ++pl) {
-          const bf16x4 ha = Quad<bf16_t>::cvt(a), hb = Quad<bf16_t>::cvt(b);
-          const u32x2_t ua = __builtin_bit_cast(u32x2_t, ha), ub = __builtin_bit_cast(u32x2_t, hb);
-          const auto r0 = __builtin_amdgcn_permlane16_swap(ua[0], ub[0], false, false);
-          const auto r1 = __builtin_amdgcn_permlane16_swap(ua[1], ub[1], false, false);
-          const u32x4_t v = {r0[0], r1[0], r0[1], r1[1]};
-          *reinterpret_cast<u32x4_t*>(to + pl * 2 * pn + u * 1024 + off) = v;
-          if (pl == 0) a = bf16_rest(a, ha), b = bf16_rest(b, hb);
-        }
-      }
-    } else {
-      char* to = head + (p0 >> 4) * (N / BN) * 1024 + (lane & 15) * 64 + (lane >> 4) * 16;
-#pragma unroll
-      for (int j = 0; j < N / 16; ++j) *reinterpret_cast<f32x4*>(to + j * 1024) = S[j];
-    }
-  }
-  // rows p0 .. p0 + ROWS - 1 of a plane into LDS as SsmRows<T, N, ROWS> lies there
-  template <int ROWS, int NW>
-  static __device__ __forceinline__ void dma(char* lds, const char* plane, int p0, int w, int lane) {
-    typedef SsmRows<T, N, ROWS> R;
-    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<char*>(plane) + (p0 >> 4) * (N / BN) * 1024, 0, R::bytes, 0x00027000);
-    constexpr int RPI = 1024 / R::RB;
-#pragma unroll
-    for (int u = 0; u < (R::bytes / 1024 + NW - 1) / NW; ++u) {
-      const int i = w + NW * u;
-      if ((R::bytes / 1024) % NW != 0 && i >= R::bytes / 1024) break;   // (uniform)
-      const int row = i * RPI + lane / R::NCH, x = (lane % R::NCH) ^ R::swz(row);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, lds_at(lds + 1024 * i), 16, (int)at(row, x), 0, 0, 0);
-    }
   }
 };
 

@@ -21,12 +21,14 @@ constexpr int kPw = 32;   // value columns of a turn
 constexpr int kPart = 4;  // floats of a (chunk, head) in SsmArgs::part
 
 // One workgroup a chunk, group and share of the group's heads.  Waves 0 to 3 make dC and
-// what a decay multiplies from before, waves 4 to 7 dB, dx and the rest; wave w of each side
-// owns token tile w, as i of dC and as j of dB and dx.  dB and dC stay in registers over the
-// heads; a head comes in turns of 32 value columns, in which everything but L is linear: x,
-// dy and the rows of S and E.  Waves 8 to 10 bring them straight into LDS, a turn ahead (a
+// what pairs of tokens add to da, waves 4 to 7 dB and dx; wave w of each side owns token tile
+// w, as i of dC and as j of dB and dx.  dB and dC stay in registers over the heads; a head
+// comes in turns of 32 value columns, in which everything but L is linear: x, dy and the
+// rows of S and E.  The other waves bring them a turn ahead: wave 8 rows straight into LDS (a
 // wave that reads LDS waits for all the LDS loads it has under way, so the loads are
-// others'); wave 11 makes a head's ddt and its sums when the others have gone on.
+// others'); waves 9 and 10 the states, which pass their registers and become the matrix
+// cores' operands on the way (with bf16 tokens three bf16 values each, SsmPlanes); wave 11
+// makes a head's ddt and its sums when the others have gone on.
 // Bound by HBM, the states S and E above all (N x P floats each, a chunk and head), and by
 // the latency of a turn's steps.
 template <typename T, int N>
@@ -34,32 +36,64 @@ struct GradLds {
   typedef SsmRows<T, N, kSsmC> KR;     // B, C
   typedef SsmRows<T, kPw, kSsmC> VR;   // x, dy
   typedef SsmRows<T, N, kPw> SR;       // a plane of S or E
-  static constexpr int state = SR::bytes * SsmState<T, N>::planes;
+  static constexpr int planes = sizeof(T) == 2 ? kExact : 1, state = SR::bytes * planes;
   static constexpr int B = 0, C = KR::bytes, turn = 2 * KR::bytes;
   static constexpr int X = 0, dY = VR::bytes, S = dY + VR::bytes, E = S + state, one = E + state;   // of a turn
-  // of a head: r_t, E_t x.EB, their column sums, dy.x, d_t, da's rectangles by wave; <E, S> by
-  // wave, e^{G_C}
-  static constexpr int sums = 9 * kSsmC + 8, small = 2 * (kSmBwd + sums) * 4;
+  // of a head: r_t, E_t x.EB, dy.x, d_t, sums of M over i and da's rectangles by wave; <E, S>
+  // by wave, e^{G_C}
+  static constexpr int sums = 12 * kSsmC + 8, small = 2 * (kSmBwd + sums) * 4;
   // two turns' rows where they fit (else a turn's rows are waited for)
   static constexpr int bufs = turn + 2 * one + small <= 160 * 1024 ? 2 : 1;
   static constexpr int scal = turn + bufs * one, sum = scal + 2 * kSmBwd * 4, total = scal + small;
 };
-enum : int { kSuR = 0, kSuE = 1, kSuM = 2, kSuDiag = 3, kSuD = 4, kSuRect = 5, kSuES = 9 * kSsmC, kSuWhole = kSuES + 4 };
+enum : int { kSuR = 0, kSuE = 1, kSuDiag = 2, kSuD = 3, kSuM = 4, kSuRect = 8, kSuES = 12 * kSsmC, kSuWhole = kSuES + 4 };
 
+// The 32 rows of a turn's state, f32 in memory, by one wave: into its registers, then as
+// planes into LDS (SsmRows' layout).
 template <typename T, int N>
-__device__ __forceinline__ Fi<T, kNear> state_tr(const char* lds, int j, int g, int c) {
-  typedef typename GradLds<T, N>::SR SR;
-  Fi<T, kNear> f;
+struct StateRows {
+  typedef GradLds<T, N> L;
+  typedef typename L::SR SR;
+  static constexpr int n = kPw * N / 256;   // quads of a lane
+  f32x4 v[n];
+  __device__ __forceinline__ void load(const float* from, int lane) {
 #pragma unroll
-  for (int i = 0; i < SsmState<T, N>::planes; ++i) f.x[i] = SR::tr32(lds + i * SR::bytes, 0, j, g, c);
+    for (int k = 0; k < n; ++k) v[k] = *reinterpret_cast<const f32x4*>(from + 4 * (64 * k + lane));
+  }
+  __device__ __forceinline__ void put(char* lds, int lane) const {
+#pragma unroll
+    for (int k = 0; k < n; ++k) {
+      const int at = 64 * k + lane, row = at / (N / 4), q = at % (N / 4);
+      if constexpr (sizeof(T) == 2) {
+        char* to = lds + row * SR::RB + (((q >> 1) ^ SR::swz(row)) << 4) + ((q & 1) << 3);
+        f32x4 x = v[k];
+#pragma unroll
+        for (int i = 0; i < L::planes; ++i) {
+          const bf16x4 h = Quad<bf16_t>::cvt(x);
+          *reinterpret_cast<bf16x4*>(to + i * SR::bytes) = h;
+          if (i + 1 < L::planes) x = bf16_rest(x, h);
+        }
+      } else {
+        *reinterpret_cast<f32x4*>(lds + row * SR::RB + ((q ^ SR::swz(row)) << 4)) = v[k];
+      }
+    }
+  }
+};
+// operands from the first M planes: columns n (rows p), and rows p in nat8's order
+template <typename T, int N, int M>
+__device__ __forceinline__ Fi<T, M> state_tr(const char* lds, int j, int g, int c) {
+  typedef typename GradLds<T, N>::SR SR;
+  Fi<T, M> f;
+#pragma unroll
+  for (int i = 0; i < (sizeof(T) == 2 ? M : 1); ++i) f.x[i] = SR::tr32(lds + i * SR::bytes, 0, j, g, c);
   return f;
 }
 template <typename T, int N>
-__device__ __forceinline__ Fi<T, kNear> state_nat(const char* lds, int i, int p, int g, int c) {
+__device__ __forceinline__ Fi<T, kExact> state_nat8(const char* lds, int i, int p, int g, int c) {
   typedef typename GradLds<T, N>::SR SR;
-  Fi<T, kNear> f;
+  Fi<T, kExact> f;
 #pragma unroll
-  for (int u = 0; u < SsmState<T, N>::planes; ++u) f.x[u] = SR::nat(lds + u * SR::bytes, i, p, g, c);
+  for (int u = 0; u < GradLds<T, N>::planes; ++u) f.x[u] = SR::nat8(lds + u * SR::bytes, i, p, g, c);
   return f;
 }
 __device__ __forceinline__ float dot4(f32x4 a, f32x4 b) { return a[0] * b[0] + a[1] * b[1] + a[2] * b[2] + a[3] * b[3]; }
@@ -75,7 +109,6 @@ __global__ void __launch_bounds__(768, 3) carve_ssm_grad_kernel(SsmArgs a) {
   typedef GradLds<T, N> L;
   typedef typename L::KR KR;
   typedef typename L::VR VR;
-  typedef typename L::SR SR;
   constexpr int NP = N / 32, NT = N / 16;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -103,29 +136,19 @@ __global__ void __launch_bounds__(768, 3) carve_ssm_grad_kernel(SsmArgs a) {
   const auto scal = [&](int h) { return reinterpret_cast<float*>(smem + L::scal) + (h & 1) * kSmBwd; };
   const auto sums = [&](int h) { return reinterpret_cast<float*>(smem + L::sum) + (h & 1) * L::sums; };
 
-  if (wave >= 8 && wave < 11) {   // ---- rows
-    if (w == 0)
-      KR::template dma<1>(smem + L::B, reinterpret_cast<const T*>(a.Bm) + q.batch * a.bs[0] + first * a.bs[1] + grp * a.bs[2],
-                          (int)(a.bs[1] * sizeof(T)), len, 0, lane);
-    if (w == 1)
-      KR::template dma<1>(smem + L::C, reinterpret_cast<const T*>(a.Cm) + q.batch * a.cs[0] + first * a.cs[1] + grp * a.cs[2],
-                          (int)(a.cs[1] * sizeof(T)), len, 0, lane);
+  if (wave == 8) {   // ---- rows
+    KR::template dma<1>(smem + L::B, reinterpret_cast<const T*>(a.Bm) + q.batch * a.bs[0] + first * a.bs[1] + grp * a.bs[2],
+                        (int)(a.bs[1] * sizeof(T)), len, 0, lane);
+    KR::template dma<1>(smem + L::C, reinterpret_cast<const T*>(a.Cm) + q.batch * a.cs[0] + first * a.cs[1] + grp * a.cs[2],
+                        (int)(a.cs[1] * sizeof(T)), len, 0, lane);
     const T* x = reinterpret_cast<const T*>(a.x) + q.batch * a.xs[0] + first * a.xs[1];
     const T* dy = reinterpret_cast<const T*>(a.dy) + row0 * a.H * a.P;
     const auto issue = [&](int n) {
       const int h = h0 + n / turns, p0 = n % turns * kPw;
       char* buf = rows(n);
-      if (w == 0) {
-        VR::template dma<1>(buf + L::X, x + h * a.xs[2] + p0, (int)(a.xs[1] * sizeof(T)), len, 0, lane);
-        VR::template dma<1>(buf + L::dY, dy + h * a.P + p0, (int)((long long)a.H * a.P * sizeof(T)), len, 0, lane);
-        if (p0 == 0) dma_flat<1, 3>(reinterpret_cast<char*>(scal(h)), a.scal + ((size_t)slot * a.H + h) * kSmBwd * 4, 0, lane);
-      } else {
-        const char* from = (w == 1 ? a.S_chunks : a.E_chunks) + ((size_t)slot * a.H + h) * pn * 4;
-        char* to = buf + (w == 1 ? L::S : L::E);
-#pragma unroll
-        for (int u = 0; u < SsmState<T, N>::planes; ++u)
-          SsmState<T, N>::template dma<kPw, 1>(to + u * SR::bytes, from + u * pn * sizeof(T), p0, 0, lane);
-      }
+      VR::template dma<1>(buf + L::X, x + h * a.xs[2] + p0, (int)(a.xs[1] * sizeof(T)), len, 0, lane);
+      VR::template dma<1>(buf + L::dY, dy + h * a.P + p0, (int)((long long)a.H * a.P * sizeof(T)), len, 0, lane);
+      if (p0 == 0) dma_flat<1, 3>(reinterpret_cast<char*>(scal(h)), a.scal + ((size_t)slot * a.H + h) * kSmBwd * 4, 0, lane);
     };
     if (L::bufs == 2) issue(0);
 #pragma unroll 1
@@ -137,6 +160,33 @@ __global__ void __launch_bounds__(768, 3) carve_ssm_grad_kernel(SsmArgs a) {
       vm_wait_all();
       __syncthreads();     // (1)
       if (L::bufs == 2 && n + 1 < total) issue(n + 1);
+    }
+    __syncthreads();       // (2)
+    return;
+  }
+  if (wave == 9 || wave == 10) {   // ---- states
+    const float* from = (wave == 9 ? a.S_chunks : a.E_chunks) + ((size_t)slot * a.H + h0) * pn;
+    const int to = wave == 9 ? L::S : L::E;
+    StateRows<T, N> st;
+    // (a head's turns are one after another in memory)
+    const auto at = [&](int n) { return from + (size_t)n * kPw * N; };
+    st.load(at(0), lane);
+    if (L::bufs == 2) {
+      st.put(rows(0) + to, lane);
+      if (total > 1) st.load(at(1), lane);
+    }
+#pragma unroll 1
+    for (int n = 0; n < total; ++n) {
+      if (L::bufs == 1) {
+        __syncthreads();   // (0)
+        st.put(rows(n) + to, lane);
+        if (n + 1 < total) st.load(at(n + 1), lane);
+      }
+      __syncthreads();     // (1)
+      if (L::bufs == 2 && n + 1 < total) {
+        st.put(rows(n + 1) + to, lane);
+        if (n + 2 < total) st.load(at(n + 2), lane);
+      }
     }
     __syncthreads();       // (2)
     return;
@@ -157,9 +207,12 @@ __global__ void __launch_bounds__(768, 3) carve_ssm_grad_kernel(SsmArgs a) {
       }
       const float before = __shfl_up(pre, 1);
       const float es = su[kSuWhole] * ((su[kSuES] + su[kSuES + 1]) + (su[kSuES + 2] + su[kSuES + 3]));
-      const float* rect = su + kSuRect * kSsmC + lane;
-      const float da = suf + (lane > 0 ? before : 0.0f) + ((rect[0] + rect[kSsmC]) + (rect[2 * kSsmC] + rect[3 * kSsmC])) + es;
-      float dd = A * da + (su[kSuM * kSsmC + lane] + e);
+      const auto waves = [&](int k) {
+        const float* p = su + k * kSsmC + lane;
+        return (p[0] + p[kSsmC]) + (p[2 * kSsmC] + p[3 * kSsmC]);
+      };
+      const float da = suf + (lane > 0 ? before : 0.0f) + waves(kSuRect) + es;
+      float dd = A * da + (waves(kSuM) + e);
       if (a.softplus) {
         const float z = raw + bias, ez = expf(-fabsf(z));
         dd *= (z >= 0.0f ? 1.0f : ez) / (1.0f + ez);
@@ -187,13 +240,18 @@ __global__ void __launch_bounds__(768, 3) carve_ssm_grad_kernel(SsmArgs a) {
 #pragma unroll
   for (int j = 0; j < NT; ++j) acc[j] = zero4();
   int n = 0;
-  if (!back) {   // ---- dC
+  const char* cb = a.cb + ((size_t)slot * a.G + grp) * 2 * kSsmCB + 16 * lane;
+  if (!back) {   // ---- dC, and what pairs of tokens add to da
+    f32x4 CB[4];   // C B^T: rows j, the tile's columns i
+#pragma unroll
+    for (int i = 0; i < 4; ++i) CB[i] = i <= w ? *reinterpret_cast<const f32x4*>(cb + ssm_tile(w, i)) : zero4();
 #pragma unroll 1
     for (int h = h0; h < h1; ++h) {
-      f32x4 Q[4], ES = zero4();   // x (rows j) against the tile's dy; S against E
-      float r = 0.0f;
+      f32x4 Q[4], ES = zero4(), U[NT];   // x (rows j) against the tile's dy; S against E; S^T dy
 #pragma unroll
       for (int i = 0; i < 4; ++i) Q[i] = zero4();
+#pragma unroll
+      for (int j = 0; j < NT; ++j) U[j] = zero4();
       const float* sc = scal(h);
 #pragma unroll 1
       for (int t = 0; t < turns; ++t, ++n) {
@@ -201,58 +259,85 @@ __global__ void __launch_bounds__(768, 3) carve_ssm_grad_kernel(SsmArgs a) {
         if (L::bufs == 1) __syncthreads();   // (0)
         __syncthreads();                     // (1)
         anew();
-        const Fr<T> fy = VR::nat(buf + L::dY, w, 0, g, c);
-        const float gam = sc[kSmGam * kSsmC + tok];
+        const Fr<T> fy = VR::nat(buf + L::dY, w, 0, g, c), fy8 = VR::nat8(buf + L::dY, w, 0, g, c);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) Q[i] = mma<T>(VR::nat(buf + L::X, i, 0, g, c), fy, Q[i]);
+        for (int i = 0; i < 4; ++i) Q[i] = mma<T>(VR::nat8(buf + L::X, i, 0, g, c), fy8, Q[i]);
         if (w < NP) {   // (uniform) <E, S> of 32 n: the diagonal of their product
 #pragma unroll
           for (int v = 0; v < 2; ++v)
-            ES = mma<T>(state_nat<T, N>(buf + L::S, v, w, g, c), state_nat<T, N>(buf + L::E, v, w, g, c), ES);
+            ES = mma<T>(state_nat8<T, N>(buf + L::S, v, w, g, c), state_nat8<T, N>(buf + L::E, v, w, g, c), ES);
         }
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          const f32x4 u = mma<T>(state_tr<T, N>(buf + L::S, j, g, c), fy, zero4());
-          acc[j] += u * gam;
-          r += dot4(u, Quad<T>::f32(KR::quad(smem + L::C, w, j, g, c)));
-        }
+        for (int j = 0; j < NT; ++j) U[j] = mma<T>(state_tr<T, N, kExact>(buf + L::S, j, g, c), fy, U[j]);
       }
       anew();
-      const float Gh = sc[kSmGh * kSsmC + tok], Gl = sc[kSmGl * kSsmC + tok];
+      const float Gh = sc[kSmGh * kSsmC + tok], Gl = sc[kSmGl * kSsmC + tok], gam = sc[kSmGam * kSsmC + tok];
+      float* su = sums(h);
+      float r = 0.0f, mine = 0.0f, carry = 0.0f;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        r += dot4(U[j], Quad<T>::f32(KR::quad(smem + L::C, w, j, g, c)));
+        acc[j] += U[j] * gam;
+      }
+      // Q becomes L d Q.  M = L C B^T Q, summed over i (the tile's columns) for each j, and
+      // d_j M over j < t and i >= t: prefix sums down each column, then along rows
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (i < w) {          // (uniform) from a tile before
-          Q[i] *= four(sc + kSmFD * kSsmC + 16 * i + 4 * g) * decay_between(Gh, Gl, sc[kSmTile + i], sc[kSmTile + 4 + i]);
-        } else if (i == w) {
-          const f32x4 gh = four(sc + kSmGh * kSsmC + 16 * i + 4 * g), gl = four(sc + kSmGl * kSsmC + 16 * i + 4 * g);
+        f32x4 pre = zero4(), ms = zero4();
+        if (i <= w) {   // (uniform)
           const f32x4 d = four(sc + kSmD * kSsmC + 16 * i + 4 * g);
+          if (i < w) {  // (uniform) from a tile before
+            Q[i] *= four(sc + kSmF * kSsmC + 16 * i + 4 * g) * decay_between(Gh, Gl, sc[kSmTile + i], sc[kSmTile + 4 + i]);
+          } else {
+            const f32x4 gh = four(sc + kSmGh * kSsmC + 16 * i + 4 * g), gl = four(sc + kSmGl * kSsmC + 16 * i + 4 * g);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) Q[i][e] = masked(4 * g + e <= c, decay_between(Gh, Gl, gh[e], gl[e]) * d[e] * Q[i][e]);
-        } else {
-          Q[i] = zero4();
+            for (int e = 0; e < 4; ++e) {
+              mine += masked(4 * g + e == c, Q[i][e]);
+              Q[i][e] = masked(4 * g + e <= c, decay_between(Gh, Gl, gh[e], gl[e]) * Q[i][e]);
+            }
+          }
+          ms = CB[i] * Q[i];
+          Q[i] *= d;
+          const f32x4 m = ms * d;
+          // (before each row of the quad, of the quads before it, of the tiles before it)
+          pre[1] = m[0];
+          pre[2] = m[0] + m[1];
+          pre[3] = pre[2] + m[2];
+          float in = pre[3] + m[3];
+          const float p1 = __shfl(in, (lane - 16) & 63);
+          in += g > 0 ? p1 : 0.0f;
+          const float p2 = __shfl(in, (lane - 32) & 63);
+          in += g > 1 ? p2 : 0.0f;
+          const float ahead = __shfl(in, (lane - 16) & 63), whole = __shfl(in, 48 + c);
+          const float more = carry + (g > 0 ? ahead : 0.0f);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) pre[e] = masked((16 * i + 4 * g + e <= tok) & (tok < len), pre[e] + more);
+          carry += whole;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) ms[e] = masked(tok < len, ms[e]);
         }
+        const float rect = row_sum4(pre, c), col = row_sum4(ms, c);
+        if (c < 4) su[(kSuRect + w) * kSsmC + 16 * i + 4 * g + c] = rect, su[(kSuM + w) * kSsmC + 16 * i + 4 * g + c] = col;
       }
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         if (s > w / 2) continue;   // (uniform)
-        const Fi<T, kNear> f = to_fi<T, kNear>(Q[2 * s], Q[2 * s + 1]);
+        const Fi<T, kNear> f = to_fi<T, kNear>(Q[2 * s], 2 * s + 1 <= w ? Q[2 * s + 1] : zero4());
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[j] = mma<T>(KR::tr32(smem + L::B, s, j, g, c), f, acc[j]);
       }
-      float* su = sums(h);
-      r = col_sum(r) * sc[kSmGam * kSsmC + tok];
+      r = col_sum(r) * gam, mine = col_sum(mine);
       float es = 0.0f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) es += masked(4 * g + e == c, ES[e]);
       es = group_sum<64>(es);
-      if (g == 0) su[kSuR * kSsmC + tok] = r, su[kSuD * kSsmC + tok] = sc[kSmD * kSsmC + tok];
+      if (g == 0) su[kSuR * kSsmC + tok] = r, su[kSuDiag * kSsmC + tok] = mine, su[kSuD * kSsmC + tok] = sc[kSmD * kSsmC + tok];
       if (lane == 0) su[kSuES + w] = es, su[kSuWhole] = sc[kSmWhole];
     }
   } else {   // ---- dB, dx
     f32x4 CB[4];   // C B^T: rows i, the tile's columns j
-    const char* cb = a.cb + ((size_t)slot * a.G + grp) * kSsmCB + 16 * lane;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) CB[i] = i >= w ? *reinterpret_cast<const f32x4*>(cb + ssm_tile(i, w)) : zero4();
+    for (int i = 0; i < 4; ++i) CB[i] = i >= w ? *reinterpret_cast<const f32x4*>(cb + kSsmCB + ssm_tile(i, w)) : zero4();
 #pragma unroll 1
     for (int h = h0; h < h1; ++h) {
       f32x4 Q[4], D[4];   // dy (rows i) against the tile's x; L
@@ -279,12 +364,12 @@ __global__ void __launch_bounds__(768, 3) carve_ssm_grad_kernel(SsmArgs a) {
             }
           }
         }
-        const Fr<T> fx = VR::nat(buf + L::X, w, 0, g, c);
+        const Fr<T> fx = VR::nat(buf + L::X, w, 0, g, c), fx8 = VR::nat8(buf + L::X, w, 0, g, c);
         const float dj = sc[kSmD * kSsmC + tok], endj = sc[kSmEnd * kSsmC + tok], endd = sc[kSmEndD * kSsmC + tok];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) Q[i] = mma<T>(VR::nat(buf + L::dY, i, 0, g, c), fx, Q[i]);
+        for (int i = 0; i < 4; ++i) Q[i] = mma<T>(VR::nat8(buf + L::dY, i, 0, g, c), fx8, Q[i]);
 #pragma unroll
-        for (int j = 0; j < NT; ++j) acc[j] += mma<T>(state_tr<T, N>(buf + L::E, j, g, c), fx, zero4()) * endd;
+        for (int j = 0; j < NT; ++j) acc[j] += mma<T>(state_tr<T, N, kNear>(buf + L::E, j, g, c), fx, zero4()) * endd;
         // dx: two tiles of p
         const RowStore<T> dx(reinterpret_cast<T*>(a.dx) + (row0 * a.H + h) * a.P + t * kPw, (size_t)a.H * a.P, len, kPw);
         const float skip = a.D ? a.D[h] : 0.0f;
@@ -292,9 +377,9 @@ __global__ void __launch_bounds__(768, 3) carve_ssm_grad_kernel(SsmArgs a) {
         f32x4 u[2] = {zero4(), zero4()}, z[2] = {zero4(), zero4()};
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
-          const Fr<T> fb = KR::nat(smem + L::B, w, p, g, c);
+          const Fr<T> fb = KR::nat8(smem + L::B, w, p, g, c);
 #pragma unroll
-          for (int v = 0; v < 2; ++v) u[v] = mma<T>(state_nat<T, N>(buf + L::E, v, p, g, c), fb, u[v]);
+          for (int v = 0; v < 2; ++v) u[v] = mma<T>(state_nat8<T, N>(buf + L::E, v, p, g, c), fb, u[v]);
         }
 #pragma unroll
         for (int s = 0; s < 2; ++s)
@@ -308,52 +393,18 @@ __global__ void __launch_bounds__(768, 3) carve_ssm_grad_kernel(SsmArgs a) {
         }
       }
       anew();
-      // M = L C B^T Q and what it adds, tile after tile; Q becomes L d Q
       const float dj = sc[kSmD * kSsmC + tok];
-      float* su = sums(h);
-      float cm = 0.0f, mine = 0.0f, carry = 0.0f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float q4 = Q[0][e];
-#pragma unroll
-        for (int i = 1; i < 4; ++i) q4 = i == w ? Q[i][e] : q4;   // (uniform)
-        mine += masked(4 * g + e == c, q4);
-      }
-      // sums of M over i >= t and j < t: suffix sums down each column, then along rows
-#pragma unroll
-      for (int i = 3; i >= 0; --i) {
-        f32x4 suf = zero4();
-        if (i >= w) {   // (uniform)
-          Q[i] *= D[i];
-          suf = CB[i] * Q[i];
-          cm += (suf[0] + suf[1]) + (suf[2] + suf[3]);
-          Q[i] *= dj;
-          suf *= dj;
-#pragma unroll
-          for (int e = 2; e >= 0; --e) suf[e] += suf[e + 1];
-          float in = suf[0];
-          const float n1 = __shfl(in, (lane + 16) & 63);
-          in += g < 3 ? n1 : 0.0f;
-          const float n2 = __shfl(in, (lane + 32) & 63);
-          in += g < 2 ? n2 : 0.0f;
-          const float behind = __shfl(in, (lane + 16) & 63), whole = __shfl(in, c);
-          const float more = carry + (g < 3 ? behind : 0.0f);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) suf[e] = masked(16 * i + 4 * g + e > tok, suf[e] + more);
-          carry += whole;
-        }
-        const float rect = row_sum4(suf, c);
-        if (c < 4) su[(kSuRect + w) * kSsmC + 16 * i + 4 * g + c] = rect;
-      }
+      for (int i = 0; i < 4; ++i) Q[i] *= D[i] * dj;
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         if (s < w / 2) continue;   // (uniform)
-        const Fi<T, kNear> f = to_fi<T, kNear>(2 * s >= w ? Q[2 * s] : zero4(), Q[2 * s + 1]);
+        const Fi<T, kNear> f = to_fi<T, kNear>(Q[2 * s], Q[2 * s + 1]);
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[j] = mma<T>(KR::tr32(smem + L::C, s, j, g, c), f, acc[j]);
       }
-      ex = col_sum(ex), cm = col_sum(cm), mine = col_sum(mine);
-      if (g == 0) su[kSuE * kSsmC + tok] = ex, su[kSuM * kSsmC + tok] = cm, su[kSuDiag * kSsmC + tok] = mine;
+      ex = col_sum(ex);
+      if (g == 0) sums(h)[kSuE * kSsmC + tok] = ex;
     }
   }
   __syncthreads();   // (2)

@@ -78,21 +78,24 @@ __global__ void __launch_bounds__(256) carve_ssm_prep_kernel(SsmArgs a) {
                       (int)(a.cs[1] * sizeof(T)), len, w, lane);
   vm_wait_all();
   __syncthreads();
-  const char *rows = smem + (BWD ? KR::bytes : 0), *cols = smem + (BWD ? 0 : KR::bytes);
-  f32x4 M[4];
+  char* out = a.cb + ((size_t)slot * a.G + grp) * (BWD ? 2 : 1) * kSsmCB + 16 * lane;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) M[i] = zero4();
+  for (int way = 0; way < (BWD ? 2 : 1); ++way) {   // rows j of B, then rows i of C
+    const char *rows = smem + way * KR::bytes, *cols = smem + (1 - way) * KR::bytes;
+    f32x4 M[4];
 #pragma unroll
-  for (int p = 0; p < NP; ++p) {
-    const Fr<T> f = KR::nat(cols, w, p, g, c);
+    for (int i = 0; i < 4; ++i) M[i] = zero4();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) M[i] = mma<T>(KR::nat(rows, i, p, g, c), f, M[i]);
+    for (int p = 0; p < NP; ++p) {
+      const Fr<T> f = KR::nat8(cols, w, p, g, c);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) M[i] = mma<T>(KR::nat8(rows, i, p, g, c), f, M[i]);
+    }
+    settle();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (way ? i >= w : i <= w) *reinterpret_cast<f32x4*>(out + (way ? kSsmCB + ssm_tile(i, w) : ssm_tile(w, i))) = M[i];
   }
-  char* out = a.cb + ((size_t)slot * a.G + grp) * kSsmCB + 16 * lane;
-  settle();
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (BWD ? i >= w : i <= w) *reinterpret_cast<f32x4*>(out + (BWD ? ssm_tile(i, w) : ssm_tile(w, i))) = M[i];
 }
 
 // Chains of states without outputs.  Forward (REV false): what each span but a sequence's
@@ -141,7 +144,7 @@ __global__ void __launch_bounds__(64 * NW, 2) carve_ssm_state_kernel(SsmArgs a, 
     VR::template dma<NW>(smem + L::V, vb + (long long)ch * kSsmC * vs, (int)(vs * sizeof(T)), len, w, lane);
     dma_flat<NW, 2>(smem + L::S, a.scal + ((size_t)(p.slot0 + ch) * a.H + h) * (REV ? kSmBwd : kSmFwd) * 4, w, lane);
     if (REV && full) {   // the gradient of the state behind this chunk
-      SsmState<T, N>::st(a.E_chunks + ((size_t)(p.slot0 + ch) * a.H + h) * pn * 4, pn, p0 + 16 * w, t.S, lane);
+      t.store(a.E_chunks + ((size_t)(p.slot0 + ch) * a.H + h) * pn + row);
     }
     vm_wait_all();
     __syncthreads();
@@ -262,7 +265,7 @@ __global__ void __launch_bounds__(128 * NW, sizeof(T) == 2 && NW == 4 ? 4 : 2) c
 #pragma unroll
       for (int b = 0; b < 2; ++b) M[v][b] = 2 * s + b <= i ? *reinterpret_cast<const f32x4*>(cb + ssm_tile(i, 2 * s + b)) : zero4();
     }
-    if (a.S_chunks && mine) SsmState<T, N>::st(a.S_chunks + ((size_t)(p.slot0 + ch) * a.H + h) * pn * 4, pn, p0, t.S, lane);
+    if (a.S_chunks && mine) t.store(a.S_chunks + ((size_t)(p.slot0 + ch) * a.H + h) * pn + row);
     vm_wait_all();
     __syncthreads();   // (1) its rows and scalars are there
     // L d C B^T: rows j of the result (tiles 2 s, 2 s + 1), columns the tokens i of a tile
