@@ -100,16 +100,16 @@ __global__ void __launch_bounds__(256) carve_ssm_prep_kernel(SsmArgs a) {
 
 // Chains of states without outputs.  Forward (REV false): what each span but a sequence's
 // last adds to the state.  Reverse: E <- e^{G_C} E + dY^T (e^G C) from the last chunk to the
-// first: what each span but the first adds (full = 0), or, from the span's own end, E of
-// every chunk's end (full = 1), then dS0.
+// first: what each span but the first adds, or (FULL), from the span's own end, E of every
+// chunk's end, then dS0.
 template <typename T, int N, int NW>
 struct StateLds {
   typedef SsmRows<T, N, kSsmC> KR;
   typedef SsmRows<T, 16 * NW, kSsmC> VR;
   static constexpr int K = 0, V = KR::bytes, S = V + VR::bytes, total = S + kSmFwd * 4;
 };
-template <typename T, int N, int NW, bool REV>
-__global__ void __launch_bounds__(64 * NW, 2) carve_ssm_state_kernel(SsmArgs a, int full) {
+template <typename T, int N, int NW, bool REV, bool FULL>
+__global__ void __launch_bounds__(64 * NW, 2) carve_ssm_state_kernel(SsmArgs a) {
   typedef StateLds<T, N, NW> L;
   typedef typename L::KR KR;
   typedef typename L::VR VR;
@@ -122,11 +122,11 @@ __global__ void __launch_bounds__(64 * NW, 2) carve_ssm_state_kernel(SsmArgs a, 
   int rest;
   if (!ssm_block(a, a.H * slices, p, rest)) return;
   const int h = rest / slices, p0 = rest % slices * 16 * NW, grp = h / (a.H / a.G);
-  if (!full && p.s == (REV ? 0 : p.nspan - 1)) return;
+  if (!FULL && p.s == (REV ? 0 : p.nspan - 1)) return;
   const size_t pn = (size_t)a.P * N, row = (size_t)(p0 + 16 * w + c) * N + 4 * g;
   float* zs = a.Z + ((size_t)p.slot * a.H + h) * pn + row;
   Tile<T, N> t;
-  if (!full) t.zero();
+  if (!FULL) t.zero();
   else if (p.s < p.nspan - 1) t.load(zs);
   else if (a.dS_T) t.load(a.dS_T + ((size_t)p.q.n * a.H + h) * pn + row);
   else t.zero();
@@ -143,10 +143,12 @@ __global__ void __launch_bounds__(64 * NW, 2) carve_ssm_state_kernel(SsmArgs a, 
     KR::template dma<NW>(smem + L::K, kb + (long long)ch * kSsmC * ks, (int)(ks * sizeof(T)), len, w, lane);
     VR::template dma<NW>(smem + L::V, vb + (long long)ch * kSsmC * vs, (int)(vs * sizeof(T)), len, w, lane);
     dma_flat<NW, 2>(smem + L::S, a.scal + ((size_t)(p.slot0 + ch) * a.H + h) * (REV ? kSmBwd : kSmFwd) * 4, w, lane);
-    if (REV && full) {   // the gradient of the state behind this chunk
+    if (FULL) {   // the gradient of the state behind this chunk
       t.store(a.E_chunks + ((size_t)(p.slot0 + ch) * a.H + h) * pn + row);
+      vm_wait_but<N / 16>();   // (the loads: the stores may be under way)
+    } else {
+      vm_wait_all();
     }
-    vm_wait_all();
     __syncthreads();
     const Fr<T> v[2] = {VR::tr32(smem + L::V, 0, w, g, c), VR::tr32(smem + L::V, 1, w, g, c)};
     t.template add<KR>(smem + L::K, v, [&](int at) {
@@ -155,7 +157,7 @@ __global__ void __launch_bounds__(64 * NW, 2) carve_ssm_state_kernel(SsmArgs a, 
     decay *= sc[kSmWhole];
   }
   settle();
-  if (!full) {
+  if (!FULL) {
     t.store(zs);
     if (tid == 0 && p0 == 0) a.Zg[(size_t)p.slot * a.H + h] = decay;
   } else if (p.s == 0 && a.dS0) {
@@ -216,7 +218,7 @@ struct OutLds {
   static constexpr int B = 0, C = KR::bytes, X = 2 * KR::bytes;
   static constexpr int image = img_bytes<T>(kNear), P = X + 2 * VR::bytes, S = P + 2 * image, total = S + 2 * kSmFwd * 4;
 };
-template <typename T, int N, int NW>
+template <typename T, int N, int NW, bool KEEP>
 __global__ void __launch_bounds__(128 * NW, sizeof(T) == 2 && NW == 4 ? 4 : 2) carve_ssm_out_kernel(SsmArgs a) {
   typedef OutLds<T, N, NW> L;
   typedef typename L::KR KR;
@@ -265,8 +267,12 @@ __global__ void __launch_bounds__(128 * NW, sizeof(T) == 2 && NW == 4 ? 4 : 2) c
 #pragma unroll
       for (int b = 0; b < 2; ++b) M[v][b] = 2 * s + b <= i ? *reinterpret_cast<const f32x4*>(cb + ssm_tile(i, 2 * s + b)) : zero4();
     }
-    if (a.S_chunks && mine) t.store(a.S_chunks + ((size_t)(p.slot0 + ch) * a.H + h) * pn + row);
-    vm_wait_all();
+    if (KEEP) {   // (a unit that is not there writes the other's states, which are its own)
+      t.store(a.S_chunks + ((size_t)(p.slot0 + ch) * a.H + h) * pn + row);
+      vm_wait_but<N / 16>();   // (the loads: the stores may be under way)
+    } else {
+      vm_wait_all();
+    }
     __syncthreads();   // (1) its rows and scalars are there
     // L d C B^T: rows j of the result (tiles 2 s, 2 s + 1), columns the tokens i of a tile
 #pragma unroll
@@ -330,13 +336,13 @@ bool lds_attr(K kern, int lds) {
 }
 int launched() { return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP; }
 
-template <typename T, int N, int NW, bool REV>
-int launch_state(const SsmArgs& a, int full, hipStream_t s) {
+template <typename T, int N, int NW, bool REV, bool FULL>
+int launch_state(const SsmArgs& a, hipStream_t s) {
   constexpr int lds = StateLds<T, N, NW>::total;
   static_assert(lds <= 160 * 1024, "LDS");
-  const auto kern = carve_ssm_state_kernel<T, N, NW, REV>;
+  const auto kern = carve_ssm_state_kernel<T, N, NW, REV, FULL>;
   if (!lds_attr(kern, lds)) return CARVE_ERR_HIP;
-  hipLaunchKernelGGL(kern, dim3(ssm_grid(a.nspans, a.H * (a.P / (16 * NW)))), dim3(64 * NW), lds, s, a, full);
+  hipLaunchKernelGGL(kern, dim3(ssm_grid(a.nspans, a.H * (a.P / (16 * NW)))), dim3(64 * NW), lds, s, a);
   return launched();
 }
 template <bool REV>
@@ -363,31 +369,35 @@ int launch_spans(const SsmArgs& a, hipStream_t s, void (*mark)(hipStream_t)) {
     mark(s);
   }
   if (split(a)) {
-    int st = launch_state<T, N, NW, REV>(a, 0, s);
+    int st = launch_state<T, N, NW, REV, false>(a, s);
     if (st) return st;
     mark(s);
     st = launch_join<REV>(a, s);
     if (st) return st;
     mark(s);
   }
-  if (REV) {
-    const int st = launch_state<T, N, NW, REV>(a, 1, s);
+  if constexpr (REV) {
+    const int st = launch_state<T, N, NW, true, true>(a, s);
     if (st) return st;
     mark(s);
   }
   return CARVE_OK;
 }
+template <typename T, int N, int NW, bool KEEP>
+int launch_out(const SsmArgs& a, hipStream_t s) {
+  constexpr int lds = OutLds<T, N, NW>::total;
+  static_assert(lds <= 160 * 1024, "LDS");
+  const auto kern = carve_ssm_out_kernel<T, N, NW, KEEP>;
+  if (!lds_attr(kern, lds)) return CARVE_ERR_HIP;
+  const int pairs = (a.H / a.G * (a.P / (16 * NW)) + 1) / 2;
+  hipLaunchKernelGGL(kern, dim3(ssm_grid(a.nspans, a.G * pairs)), dim3(128 * NW), lds, s, a);
+  return launched();
+}
 template <typename T, int N, int NW>
 int launch_fwd_t(const SsmArgs& a, hipStream_t s, void (*mark)(hipStream_t)) {
   int st = launch_spans<T, N, NW, false>(a, s, mark);
   if (st) return st;
-  constexpr int lds = OutLds<T, N, NW>::total;
-  static_assert(lds <= 160 * 1024, "LDS");
-  const auto kern = carve_ssm_out_kernel<T, N, NW>;
-  if (!lds_attr(kern, lds)) return CARVE_ERR_HIP;
-  const int pairs = (a.H / a.G * (a.P / (16 * NW)) + 1) / 2;
-  hipLaunchKernelGGL(kern, dim3(ssm_grid(a.nspans, a.G * pairs)), dim3(128 * NW), lds, s, a);
-  st = launched();
+  st = a.S_chunks ? launch_out<T, N, NW, true>(a, s) : launch_out<T, N, NW, false>(a, s);
   mark(s);
   return st;
 }
