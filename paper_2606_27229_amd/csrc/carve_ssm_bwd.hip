@@ -60,7 +60,8 @@ struct StateRows {
 #pragma unroll
     for (int k = 0; k < n; ++k) v[k] = *reinterpret_cast<const f32x4*>(from + 4 * (64 * k + lane));
   }
-  __device__ __forceinline__ void put(char* lds, int lane) const {
+  // next: the rows that take the registers as they become free
+  __device__ __forceinline__ void put(char* lds, int lane, const float* next) {
 #pragma unroll
     for (int k = 0; k < n; ++k) {
       const int at = 64 * k + lane, row = at / (N / 4), q = at % (N / 4);
@@ -76,6 +77,7 @@ struct StateRows {
       } else {
         *reinterpret_cast<f32x4*>(lds + row * SR::RB + ((q ^ SR::swz(row)) << 4)) = v[k];
       }
+      v[k] = *reinterpret_cast<const f32x4*>(next + 4 * (64 * k + lane));
     }
   }
 };
@@ -169,24 +171,17 @@ __global__ void __launch_bounds__(768, 3) carve_ssm_grad_kernel(SsmArgs a) {
     const int to = wave == 9 ? L::S : L::E;
     StateRows<T, N> st;
     // (a head's turns are one after another in memory)
-    const auto at = [&](int n) { return from + (size_t)n * kPw * N; };
+    const auto at = [&](int n) { return from + (size_t)min(n, total - 1) * kPw * N; };   // (the last one again behind it)
     st.load(at(0), lane);
-    if (L::bufs == 2) {
-      st.put(rows(0) + to, lane);
-      if (total > 1) st.load(at(1), lane);
-    }
+    if (L::bufs == 2) st.put(rows(0) + to, lane, at(1));
 #pragma unroll 1
     for (int n = 0; n < total; ++n) {
       if (L::bufs == 1) {
         __syncthreads();   // (0)
-        st.put(rows(n) + to, lane);
-        if (n + 1 < total) st.load(at(n + 1), lane);
+        st.put(rows(n) + to, lane, at(n + 1));
       }
       __syncthreads();     // (1)
-      if (L::bufs == 2 && n + 1 < total) {
-        st.put(rows(n + 1) + to, lane);
-        if (n + 2 < total) st.load(at(n + 2), lane);
-      }
+      if (L::bufs == 2 && n + 1 < total) st.put(rows(n + 1) + to, lane, at(n + 2));
     }
     __syncthreads();       // (2)
     return;
@@ -340,11 +335,22 @@ __global__ void __launch_bounds__(768, 3) carve_ssm_grad_kernel(SsmArgs a) {
     for (int i = 0; i < 4; ++i) CB[i] = i >= w ? *reinterpret_cast<const f32x4*>(cb + kSsmCB + ssm_tile(i, w)) : zero4();
 #pragma unroll 1
     for (int h = h0; h < h1; ++h) {
-      f32x4 Q[4], D[4];   // dy (rows i) against the tile's x; L
+      f32x4 Q[4];          // dy (rows i) against the tile's x
+      Fi<T, kNear> Lf[2];  // L C B^T
       float ex = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) Q[i] = D[i] = zero4();
+      for (int i = 0; i < 4; ++i) Q[i] = zero4();
       const float* sc = scal(h);
+      // L of the tile's columns, applied to tile i
+      const auto decayed = [&](int i, f32x4 v) {
+        if (i < w) return zero4();   // (uniform)
+        if (i > w) return v * (four(sc + (kSmDown + w) * kSsmC + 16 * i + 4 * g) * sc[kSmF * kSsmC + tok]);
+        const float Gh = sc[kSmGh * kSsmC + tok], Gl = sc[kSmGl * kSsmC + tok];
+        const f32x4 gh = four(sc + kSmGh * kSsmC + 16 * i + 4 * g), gl = four(sc + kSmGl * kSsmC + 16 * i + 4 * g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = masked(4 * g + e >= c, decay_between(gh[e], gl[e], Gh, Gl) * v[e]);
+        return v;
+      };
 #pragma unroll 1
       for (int t = 0; t < turns; ++t, ++n) {
         const char* buf = rows(n);
@@ -352,17 +358,8 @@ __global__ void __launch_bounds__(768, 3) carve_ssm_grad_kernel(SsmArgs a) {
         __syncthreads();                     // (1)
         anew();
         if (t == 0) {
-          const float f = sc[kSmF * kSsmC + tok], Gh = sc[kSmGh * kSsmC + tok], Gl = sc[kSmGl * kSsmC + tok];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (i > w) {          // (uniform) to a tile behind
-              D[i] = four(sc + (kSmDown + w) * kSsmC + 16 * i + 4 * g) * f;
-            } else if (i == w) {
-              const f32x4 gh = four(sc + kSmGh * kSsmC + 16 * i + 4 * g), gl = four(sc + kSmGl * kSsmC + 16 * i + 4 * g);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) D[i][e] = masked(4 * g + e >= c, decay_between(gh[e], gl[e], Gh, Gl));
-            }
-          }
+          for (int s = 0; s < 2; ++s) Lf[s] = to_fi<T, kNear>(decayed(2 * s, CB[2 * s]), decayed(2 * s + 1, CB[2 * s + 1]));
         }
         const Fr<T> fx = VR::nat(buf + L::X, w, 0, g, c), fx8 = VR::nat8(buf + L::X, w, 0, g, c);
         const float dj = sc[kSmD * kSsmC + tok], endj = sc[kSmEnd * kSsmC + tok], endd = sc[kSmEndD * kSsmC + tok];
@@ -373,7 +370,6 @@ __global__ void __launch_bounds__(768, 3) carve_ssm_grad_kernel(SsmArgs a) {
         // dx: two tiles of p
         const RowStore<T> dx(reinterpret_cast<T*>(a.dx) + (row0 * a.H + h) * a.P + t * kPw, (size_t)a.H * a.P, len, kPw);
         const float skip = a.D ? a.D[h] : 0.0f;
-        const Fi<T, kNear> Lf[2] = {to_fi<T, kNear>(D[0] * CB[0], D[1] * CB[1]), to_fi<T, kNear>(D[2] * CB[2], D[3] * CB[3])};
         f32x4 u[2] = {zero4(), zero4()}, z[2] = {zero4(), zero4()};
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
@@ -395,7 +391,7 @@ __global__ void __launch_bounds__(768, 3) carve_ssm_grad_kernel(SsmArgs a) {
       anew();
       const float dj = sc[kSmD * kSsmC + tok];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) Q[i] *= D[i] * dj;
+      for (int i = 0; i < 4; ++i) Q[i] = decayed(i, Q[i] * dj);
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         if (s < w / 2) continue;   // (uniform)
