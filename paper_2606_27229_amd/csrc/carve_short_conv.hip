@@ -19,14 +19,47 @@ namespace carve {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kBwdV = 4;   // channels of a thread in the backward
 
-template <typename T>
-__device__ __forceinline__ void ld16(const T* p, float (&f)[Chunk16<T>::N]) {
-  Chunk16<T>::unpack(*reinterpret_cast<const u32x4_t*>(p), f);
-}
-template <typename T>
-__device__ __forceinline__ void st16(T* p, const float (&f)[Chunk16<T>::N]) {
-  *reinterpret_cast<u32x4_t*>(p) = Chunk16<T>::pack(f);
+// V channels of a row (16 bytes, or 8 with V = 4 of bf16) and their values
+template <typename T, int V>
+struct Piece {
+  static constexpr int words = V * (int)sizeof(T) / 4;
+  typedef unsigned raw __attribute__((ext_vector_type(words)));
+  static __device__ __forceinline__ raw ld(const T* p) { return *reinterpret_cast<const raw*>(p); }
+  static __device__ __forceinline__ void unpack(raw r, float (&f)[V]) {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < words; ++i) {
+        f[2 * i] = __builtin_bit_cast(float, r[i] << 16);
+        f[2 * i + 1] = __builtin_bit_cast(float, r[i] & 0xffff0000u);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const unsigned u = r[i];   // (of an element itself the cast takes the first one)
+        f[i] = __builtin_bit_cast(float, u);
+      }
+    }
+  }
+  static __device__ __forceinline__ void st(T* p, const float (&f)[V]) {
+    raw r;
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < words; ++i) {
+        const f32x2 v = {f[2 * i], f[2 * i + 1]};
+        r[i] = __builtin_bit_cast(unsigned, __builtin_convertvector(v, bf16x2));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) r[i] = __builtin_bit_cast(unsigned, f[i]);
+    }
+    *reinterpret_cast<raw*>(p) = r;
+  }
+};
+template <typename T, int V>
+__device__ __forceinline__ void ld_row(const T* p, float (&f)[V]) {
+  Piece<T, V>::unpack(Piece<T, V>::ld(p), f);
 }
 
 // weights of a thread's channels, by tap
@@ -77,16 +110,15 @@ struct Where {
 };
 
 // Input of a sequence at position p of it, from x0 where p < 0.
-template <typename T, int W>
-__device__ __forceinline__ void ld_past(const ConvArgs& a, const T* x, int n, int first, int p, int c0,
-                                        float (&f)[Chunk16<T>::N]) {
+template <typename T, int W, int V>
+__device__ __forceinline__ void ld_past(const ConvArgs& a, const T* x, int n, int first, int p, int c0, float (&f)[V]) {
   if (p >= 0) {
-    ld16(x + (size_t)(first + p) * a.x_token + c0, f);
+    ld_row<T, V>(x + (size_t)(first + p) * a.x_token + c0, f);
   } else if (a.x0) {
-    ld16(reinterpret_cast<const T*>(a.x0) + ((size_t)n * (W - 1) + (W - 1 + p)) * a.C + c0, f);
+    ld_row<T, V>(reinterpret_cast<const T*>(a.x0) + ((size_t)n * (W - 1) + (W - 1 + p)) * a.C + c0, f);
   } else {
 #pragma unroll
-    for (int e = 0; e < Chunk16<T>::N; ++e) f[e] = 0.0f;
+    for (int e = 0; e < V; ++e) f[e] = 0.0f;
   }
 }
 
@@ -118,9 +150,13 @@ __device__ __forceinline__ bool place(const ConvArgs& a, int R, int lw, int rows
 
 __device__ __forceinline__ float act_of(float p, int act) { return act ? silu_f(p) : p; }
 
+// The rows of a run in ascending order.  Where all of a wave's runs lie within a sequence
+// (but for its start), rows come by fours with the window in a ring of four, so that no
+// value moves and no lane branches, and the next four are under way; else row by row.
 template <typename T, int W>
 __global__ void __launch_bounds__(kThreads) carve_short_conv_fwd_kernel(ConvArgs a, int R, int lw, int rows_blocks, int batches) {
-  constexpr int V = Chunk16<T>::N, AHEAD = 4;
+  constexpr int V = Chunk16<T>::N;
+  typedef Piece<T, V> P;
   Place pl;
   if (!place<V>(a, R, lw, rows_blocks, batches, pl)) return;
   const int c0 = pl.c0;
@@ -132,8 +168,8 @@ __global__ void __launch_bounds__(kThreads) carve_short_conv_fwd_kernel(ConvArgs
     if (a.offsets) packed_seq(a.offsets, (int)n, a.T, first, end);
     const T* x = reinterpret_cast<const T*>(a.x) + (a.offsets ? 0 : n * a.x_batch);
     float f[V];
-    ld_past<T, W>(a, x, (int)n, first, end - first - (W - 1) + j, c0, f);
-    st16(reinterpret_cast<T*>(a.x_T) + ((size_t)n * (W - 1) + j) * a.C + c0, f);
+    ld_past<T, W, V>(a, x, (int)n, first, end - first - (W - 1) + j, c0, f);
+    P::st(reinterpret_cast<T*>(a.x_T) + ((size_t)n * (W - 1) + j) * a.C + c0, f);
     return;
   }
   const int row0 = pl.row0, rows = min(R, a.T - row0);
@@ -146,44 +182,71 @@ __global__ void __launch_bounds__(kThreads) carve_short_conv_fwd_kernel(ConvArgs
   at.at(a, pl.batch, row0);
   if (at.in) {
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) ld_past<T, W>(a, x, at.n, at.first, row0 - at.first - (W - 1) + j, c0, past[j]);
+    for (int j = 0; j < W - 1; ++j) ld_past<T, W, V>(a, x, at.n, at.first, row0 - at.first - (W - 1) + j, c0, past[j]);
   }
+  const T* xr = x + (size_t)row0 * a.x_token + c0;
+  if (__all(at.in && rows == R && row0 + R <= at.end)) {   // (R is a multiple of four)
+    float ring[4][V];   // row r at r mod 4
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+      for (int e = 0; e < V; ++e) ring[(j + 5 - W) & 3][e] = past[j][e];
+    typename P::raw next[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) next[i] = P::ld(xr + (size_t)i * a.x_token);
 #pragma unroll 1
-  for (int i0 = 0; i0 < rows; i0 += AHEAD) {
-    u32x4_t raw[AHEAD];
+    for (int i0 = 0; i0 < R; i0 += 4) {
+      typename P::raw now[4];
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i)
-      raw[i] = *reinterpret_cast<const u32x4_t*>(x + (size_t)min(row0 + i0 + i, a.T - 1) * a.x_token + c0);
+      for (int i = 0; i < 4; ++i) now[i] = next[i];
+      xr += 4 * a.x_token;
+      if (i0 + 4 < R) {
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      const int row = row0 + i0 + i;
-      if (i0 + i >= rows) break;
-      if (i0 + i > 0) {
-        at.next(a, pl.batch, row);
-        if (at.in && row == at.first) {
-#pragma unroll
-          for (int j = 0; j < W - 1; ++j) ld_past<T, W>(a, x, at.n, at.first, j - (W - 1), c0, past[j]);
-        }
+        for (int i = 0; i < 4; ++i) next[i] = P::ld(xr + (size_t)i * a.x_token);
       }
-      if (at.in) {   // (a row of no sequence is left as it was)
-        float cur[V], o[V];
-        Chunk16<T>::unpack(raw[i], cur);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        P::unpack(now[i], ring[i]);
+        float o[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          float p = b[e] + w[W - 1][e] * cur[e];
+          float p = b[e];
 #pragma unroll
-          for (int j = 0; j < W - 1; ++j) p += w[j][e] * past[j][e];
+          for (int j = 0; j < W; ++j) p += w[j][e] * ring[(i + 5 - W + j) & 3][e];
           o[e] = act_of(p, a.act);
         }
-        st16(y + (size_t)(i0 + i) * a.C, o);
-#pragma unroll
-        for (int j = 0; j + 1 < W - 1; ++j)
-#pragma unroll
-          for (int e = 0; e < V; ++e) past[j][e] = past[j + 1][e];
-#pragma unroll
-        for (int e = 0; e < V; ++e) past[W - 2][e] = cur[e];
+        P::st(y + (size_t)(i0 + i) * a.C, o);
       }
     }
+    return;
+  }
+#pragma unroll 1
+  for (int i = 0; i < rows; ++i) {
+    const int row = row0 + i;
+    if (i > 0) {
+      at.next(a, pl.batch, row);
+      if (at.in && row == at.first) {
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) ld_past<T, W, V>(a, x, at.n, at.first, j - (W - 1), c0, past[j]);
+      }
+    }
+    if (!at.in) continue;   // (a row of no sequence is left as it was)
+    float cur[V], o[V];
+    ld_row<T, V>(x + (size_t)row * a.x_token + c0, cur);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      float p = b[e] + w[W - 1][e] * cur[e];
+#pragma unroll
+      for (int j = 0; j < W - 1; ++j) p += w[j][e] * past[j][e];
+      o[e] = act_of(p, a.act);
+    }
+    P::st(y + (size_t)i * a.C, o);
+#pragma unroll
+    for (int j = 0; j + 1 < W - 1; ++j)
+#pragma unroll
+      for (int e = 0; e < V; ++e) past[j][e] = past[j + 1][e];
+#pragma unroll
+    for (int e = 0; e < V; ++e) past[W - 2][e] = cur[e];
   }
 }
 
@@ -205,11 +268,15 @@ __device__ __forceinline__ void row_dp(const float (&w)[W][V], const float (&b)[
 
 // The rows of a run in ascending order, and W - 1 more that follow it (for dx alone): row
 // u's dp goes to dx of rows u, u - 1, .. u - W + 1 of its sequence, of which acc[k] is that
-// of row u - k; acc[W - 1] is then complete.  The sums of dweight and dbias over a
-// workgroup's runs are added up in LDS in a fixed order and leave as one row of partials.
+// of row u - k; acc[W - 1] is then complete.  As in the forward, by fours with rings where
+// all of a wave's runs and what follows them lie within a sequence and before its last
+// W - 1 rows.  The sums of dweight and dbias over a workgroup's runs are added up in LDS in
+// a fixed order and leave as one row of partials.  Four channels a thread: with eight the
+// rings, weights and sums take 210 registers, and two waves a SIMD do not hide the loads.
 template <typename T, int W>
 __global__ void __launch_bounds__(kThreads) carve_short_conv_bwd_kernel(ConvArgs a, int lw, int rows_blocks, int batches) {
-  constexpr int V = Chunk16<T>::N, R = kConvBwdRows, AHEAD = 4;
+  constexpr int V = kBwdV, R = kConvBwdRows;
+  typedef Piece<T, V> P;
   __shared__ float red[kThreads * (V + 1)];
   Place pl;
   const bool mine = place<V>(a, R, lw, rows_blocks, batches, pl);
@@ -229,15 +296,15 @@ __global__ void __launch_bounds__(kThreads) carve_short_conv_bwd_kernel(ConvArgs
     float d[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) d[e] = 0.0f;
-    if (a.dx_T && i >= len) ld16(reinterpret_cast<const T*>(a.dx_T) + ((size_t)n * (W - 1) + i - len) * a.C + c0, d);
+    if (a.dx_T && i >= len) ld_row<T, V>(reinterpret_cast<const T*>(a.dx_T) + ((size_t)n * (W - 1) + i - len) * a.C + c0, d);
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) ld_past<T, W>(a, x, (int)n, first, j - (W - 1), c0, past[j]);
+    for (int j = 0; j < W - 1; ++j) ld_past<T, W, V>(a, x, (int)n, first, j - (W - 1), c0, past[j]);
 #pragma unroll
     for (int u = 0; u < W - 1; ++u) {
       if (u >= len) break;
       float cur[V], g[V], dp[V];
-      ld16(x + (size_t)(first + u) * a.x_token + c0, cur);
-      ld16(dy + (size_t)(first + u) * a.C, g);
+      ld_row<T, V>(x + (size_t)(first + u) * a.x_token + c0, cur);
+      ld_row<T, V>(dy + (size_t)(first + u) * a.C, g);
       row_dp<V, W>(w, b, past, cur, g, a.act, dp);
       // weight j of row u reads position u - (W - 1) + j
 #pragma unroll
@@ -252,93 +319,150 @@ __global__ void __launch_bounds__(kThreads) carve_short_conv_bwd_kernel(ConvArgs
 #pragma unroll
       for (int e = 0; e < V; ++e) past[W - 2][e] = cur[e];
     }
-    st16(reinterpret_cast<T*>(a.dx0) + ((size_t)n * (W - 1) + i) * a.C + c0, d);
+    P::st(reinterpret_cast<T*>(a.dx0) + ((size_t)n * (W - 1) + i) * a.C + c0, d);
     return;
   }
   const int row0 = pl.row0, rows = min(R, a.T - row0);
   const T* x = reinterpret_cast<const T*>(a.x) + pl.batch * a.x_batch + c0;
   const T* dy = reinterpret_cast<const T*>(a.dy) + (size_t)pl.batch * a.T * a.C + c0;
   T* dx = reinterpret_cast<T*>(a.dx) + (size_t)pl.batch * a.T * a.C + c0;
-  float aw[W][V], ab[V], acc[W][V];
+  float aw[W][V], ab[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) {
     ab[e] = 0.0f;
 #pragma unroll
-    for (int j = 0; j < W; ++j) aw[j][e] = acc[j][e] = 0.0f;
+    for (int j = 0; j < W; ++j) aw[j][e] = 0.0f;
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) past[j][e] = 0.0f;
   }
+  Where at;
+  at.in = false;
   if (rows > 0) {
-    Where at;
     at.at(a, pl.batch, row0);
     if (at.in) {
 #pragma unroll
-      for (int j = 0; j < W - 1; ++j)
-        ld_past<T, W>(a, reinterpret_cast<const T*>(a.x) + pl.batch * a.x_batch, at.n, at.first, row0 - at.first - (W - 1) + j, c0, past[j]);
-    }
-    unsigned ins = 0;   // bit k: whether row u - k belongs to a sequence and to this run
-    const int last = row0 + rows + W - 1;   // (rows behind the tensor are of no sequence)
-    for (int u0 = row0; u0 < last; u0 += AHEAD) {
-      u32x4_t rx[AHEAD], rd[AHEAD];
-#pragma unroll
-      for (int i = 0; i < AHEAD; ++i) {
-        const size_t r = min(u0 + i, a.T - 1);
-        rx[i] = *reinterpret_cast<const u32x4_t*>(x + r * a.x_token);
-        rd[i] = *reinterpret_cast<const u32x4_t*>(dy + r * a.C);
-      }
-#pragma unroll
-      for (int i = 0; i < AHEAD; ++i) {
-        const int u = u0 + i;
-        if (u >= last) break;
-        if (u > row0) {
-          at.next(a, pl.batch, u);
-          if (at.in && u == at.first) {
-#pragma unroll
-            for (int j = 0; j < W - 1; ++j)
-              ld_past<T, W>(a, reinterpret_cast<const T*>(a.x) + pl.batch * a.x_batch, at.n, at.first, j - (W - 1), c0, past[j]);
-          }
-        }
-        const bool own = u < row0 + rows;
-        ins = ins << 1 | (at.in && own);
-        if (at.in) {
-          float cur[V], g[V], dp[V];
-          Chunk16<T>::unpack(rx[i], cur);
-          Chunk16<T>::unpack(rd[i], g);
-          row_dp<V, W>(w, b, past, cur, g, a.act, dp);
-          if (own) {
-            const int j = u - at.end + W - 1;   // (one of the sequence's last W - 1 rows)
-            if (a.dx_T && j >= 0) ld16(reinterpret_cast<const T*>(a.dx_T) + ((size_t)at.n * (W - 1) + j) * a.C + c0, acc[0]);
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-              ab[e] += dp[e];
-              aw[W - 1][e] += dp[e] * cur[e];
-#pragma unroll
-              for (int j = 0; j < W - 1; ++j) aw[j][e] += dp[e] * past[j][e];
-            }
-          }
-#pragma unroll
-          for (int k = 0; k < W; ++k)
-            if (u - k >= at.first)   // (rows before the run take it too and are not written)
-#pragma unroll
-              for (int e = 0; e < V; ++e) acc[k][e] += w[W - 1 - k][e] * dp[e];
-#pragma unroll
-          for (int j = 0; j + 1 < W - 1; ++j)
-#pragma unroll
-            for (int e = 0; e < V; ++e) past[j][e] = past[j + 1][e];
-#pragma unroll
-          for (int e = 0; e < V; ++e) past[W - 2][e] = cur[e];
-        }
-        if ((ins >> (W - 1) & 1) && mine) st16(dx + (size_t)(u - (W - 1)) * a.C, acc[W - 1]);
-#pragma unroll
-        for (int k = W - 1; k > 0; --k)
-#pragma unroll
-          for (int e = 0; e < V; ++e) acc[k][e] = acc[k - 1][e];
-#pragma unroll
-        for (int e = 0; e < V; ++e) acc[0][e] = 0.0f;
-      }
+      for (int j = 0; j < W - 1; ++j) ld_past<T, W, V>(a, x - c0, at.n, at.first, row0 - at.first - (W - 1) + j, c0, past[j]);
     }
   }
-  // the workgroup's sums, a tap at a time: thread (lane, run 0 .. ) adds the runs in order
+  if (__all(at.in && rows == R && row0 + R + W - 1 <= at.end)) {
+    float ring[4][V], acc[4][V];   // rows r's input and dx at r mod 4
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < V; ++e) acc[j][e] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+      for (int e = 0; e < V; ++e) ring[(j + 5 - W) & 3][e] = past[j][e];
+    const T *xr = x + (size_t)row0 * a.x_token, *gr = dy + (size_t)row0 * a.C;
+    T* dr = dx + (size_t)row0 * a.C;
+    typename P::raw nx[4], ng[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) nx[i] = P::ld(xr + (size_t)i * a.x_token), ng[i] = P::ld(gr + (size_t)i * a.C);
+    // row u0 + i, the run's (own) or behind it
+    const auto row = [&](int i, typename P::raw rx, typename P::raw rg, bool own) {
+      float g[V];
+      P::unpack(rx, ring[i]);
+      P::unpack(rg, g);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        float dp = g[e];
+        if (a.act) {
+          float p = b[e];
+#pragma unroll
+          for (int j = 0; j < W; ++j) p += w[j][e] * ring[(i + 5 - W + j) & 3][e];
+          dp *= silu_grad_f(p);
+        }
+        if (own) {
+          ab[e] += dp;
+#pragma unroll
+          for (int j = 0; j < W; ++j) aw[j][e] += dp * ring[(i + 5 - W + j) & 3][e];
+          acc[i][e] = 0.0f;
+        }
+#pragma unroll
+        for (int k = own ? 0 : 1; k < W; ++k) acc[(i - k) & 3][e] += w[W - 1 - k][e] * dp;
+      }
+    };
+#pragma unroll 1
+    for (int u0 = 0; u0 < R; u0 += 4) {
+      typename P::raw rx[4], rg[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) rx[i] = nx[i], rg[i] = ng[i];
+      xr += 4 * a.x_token, gr += 4 * a.C;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        // (behind the run only W - 1 rows are there)
+        const int r = i < W - 1 ? i : u0 + 4 < R ? i : 0;
+        nx[i] = P::ld(xr + (size_t)r * a.x_token), ng[i] = P::ld(gr + (size_t)r * a.C);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        row(i, rx[i], rg[i], true);
+        if ((u0 > 0 || i >= W - 1) && mine) P::st(dr + ((ptrdiff_t)u0 + i - (W - 1)) * a.C, acc[(i - (W - 1)) & 3]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < W - 1; ++i) {
+      row(i, nx[i], ng[i], false);
+      if (mine) P::st(dr + ((ptrdiff_t)R + i - (W - 1)) * a.C, acc[(i - (W - 1)) & 3]);
+    }
+  } else if (rows > 0) {
+    float acc[W][V];
+#pragma unroll
+    for (int j = 0; j < W; ++j)
+#pragma unroll
+      for (int e = 0; e < V; ++e) acc[j][e] = 0.0f;
+    unsigned ins = 0;   // bit k: whether row u - k belongs to a sequence and to this run
+    const int last = row0 + rows + W - 1;   // (rows behind the tensor are of no sequence)
+#pragma unroll 1
+    for (int u = row0; u < last; ++u) {
+      if (u > row0) {
+        at.next(a, pl.batch, u);
+        if (at.in && u == at.first) {
+#pragma unroll
+          for (int j = 0; j < W - 1; ++j) ld_past<T, W, V>(a, x - c0, at.n, at.first, j - (W - 1), c0, past[j]);
+        }
+      }
+      const bool own = u < row0 + rows;
+      ins = ins << 1 | (at.in && own);
+      if (at.in) {
+        float cur[V], g[V], dp[V];
+        ld_row<T, V>(x + (size_t)u * a.x_token, cur);
+        ld_row<T, V>(dy + (size_t)u * a.C, g);
+        row_dp<V, W>(w, b, past, cur, g, a.act, dp);
+        if (own) {
+          const int j = u - at.end + W - 1;   // (one of the sequence's last W - 1 rows)
+          if (a.dx_T && j >= 0) ld_row<T, V>(reinterpret_cast<const T*>(a.dx_T) + ((size_t)at.n * (W - 1) + j) * a.C + c0, acc[0]);
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            ab[e] += dp[e];
+            aw[W - 1][e] += dp[e] * cur[e];
+#pragma unroll
+            for (int j = 0; j < W - 1; ++j) aw[j][e] += dp[e] * past[j][e];
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < W; ++k)
+          if (u - k >= at.first)   // (rows before the run take it too and are not written)
+#pragma unroll
+            for (int e = 0; e < V; ++e) acc[k][e] += w[W - 1 - k][e] * dp[e];
+#pragma unroll
+        for (int j = 0; j + 1 < W - 1; ++j)
+#pragma unroll
+          for (int e = 0; e < V; ++e) past[j][e] = past[j + 1][e];
+#pragma unroll
+        for (int e = 0; e < V; ++e) past[W - 2][e] = cur[e];
+      }
+      if ((ins >> (W - 1) & 1) && mine) P::st(dx + (size_t)(u - (W - 1)) * a.C, acc[W - 1]);
+#pragma unroll
+      for (int k = W - 1; k > 0; --k)
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[k][e] = acc[k - 1][e];
+#pragma unroll
+      for (int e = 0; e < V; ++e) acc[0][e] = 0.0f;
+    }
+  }
+  // the workgroup's sums, a tap at a time: a thread adds its channel's runs in order
   const int lane = threadIdx.x & (lw - 1), runs = kThreads / lw;
   const int cblocks = (a.C / V + lw - 1) / lw;
   const long long part = ((long long)blockIdx.y * gridDim.x + blockIdx.x) / cblocks;
@@ -399,40 +523,41 @@ __global__ void __launch_bounds__(64) carve_short_conv_step_kernel(ConvStepArgs 
   T* st = reinterpret_cast<T*>(a.state) + (size_t)slot * (W - 1) * a.C + c0;
   const T* x = reinterpret_cast<const T*>(a.x) + b * a.x_batch + c0;
   T* y = reinterpret_cast<T*>(a.y) + (size_t)b * a.T * a.C + c0;
-  u32x4_t keep[W - 1], raw = *reinterpret_cast<const u32x4_t*>(x);
+  typedef Piece<T, V> P;
+  typename P::raw keep[W - 1], raw = P::ld(x);
 #pragma unroll
-  for (int j = 0; j < W - 1; ++j) keep[j] = *reinterpret_cast<const u32x4_t*>(st + (size_t)j * a.C);
+  for (int j = 0; j < W - 1; ++j) keep[j] = P::ld(st + (size_t)j * a.C);
   float w[W][V], bi[V];
   ld_weights<V, W>(a.weight, a.bias, c0, w, bi);
   for (int t = 0; t < a.T; ++t) {
-    const u32x4_t now = raw;
-    if (t + 1 < a.T) raw = *reinterpret_cast<const u32x4_t*>(x + (size_t)(t + 1) * a.x_token);
+    const typename P::raw now = raw;
+    if (t + 1 < a.T) raw = P::ld(x + (size_t)(t + 1) * a.x_token);
     float cur[V], o[V];
-    Chunk16<T>::unpack(now, cur);
+    P::unpack(now, cur);
 #pragma unroll
     for (int e = 0; e < V; ++e) o[e] = bi[e] + w[W - 1][e] * cur[e];
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) {
       float f[V];
-      Chunk16<T>::unpack(keep[j], f);
+      P::unpack(keep[j], f);
 #pragma unroll
       for (int e = 0; e < V; ++e) o[e] += w[j][e] * f[e];
     }
 #pragma unroll
     for (int e = 0; e < V; ++e) o[e] = act_of(o[e], a.act);
-    st16(y + (size_t)t * a.C, o);
+    P::st(y + (size_t)t * a.C, o);
 #pragma unroll
     for (int j = 0; j + 1 < W - 1; ++j) keep[j] = keep[j + 1];
     keep[W - 2] = now;
   }
 #pragma unroll
-  for (int j = 0; j < W - 1; ++j) *reinterpret_cast<u32x4_t*>(st + (size_t)j * a.C) = keep[j];
+  for (int j = 0; j < W - 1; ++j) *reinterpret_cast<typename P::raw*>(st + (size_t)j * a.C) = keep[j];
 }
 
-// threads side by side on a row: a power of two up to 16
-int lanes_of(int C, size_t esize) {
+// threads side by side on a row, V channels each: a power of two, up to 256 bytes of it
+int lanes_of(int C, int V, size_t esize) {
   int lw = 1;
-  while (lw < 16 && lw < C * (int)esize / 16) lw *= 2;
+  while (lw * V * (int)esize < 256 && lw * V < C) lw *= 2;
   return lw;
 }
 
@@ -452,7 +577,7 @@ constexpr long long kConvFewBlocks = 1024;
 template <typename T, int W>
 int launch_fwd(const ConvArgs& a, hipStream_t s) {
   constexpr int V = Chunk16<T>::N;
-  const int lw = lanes_of(a.C, sizeof(T)), runs = kThreads / lw, cb = (a.C / V + lw - 1) / lw;
+  const int lw = lanes_of(a.C, V, sizeof(T)), runs = kThreads / lw, cb = (a.C / V + lw - 1) / lw;
   const int batches = a.offsets ? 1 : a.nseq;
   const auto blocks = [&](int R) { return (a.T + (long long)runs * R - 1) / (runs * R); };
   const int R = blocks(kConvRows) * batches * cb < kConvFewBlocks ? kConvFewRows : kConvRows;
@@ -465,8 +590,8 @@ int launch_fwd(const ConvArgs& a, hipStream_t s) {
 }
 template <typename T, int W>
 int launch_bwd(const ConvArgs& a, hipStream_t s, void (*mark)(hipStream_t)) {
-  constexpr int V = Chunk16<T>::N;
-  const int lw = lanes_of(a.C, sizeof(T)), runs = kThreads / lw;
+  constexpr int V = kBwdV;
+  const int lw = lanes_of(a.C, V, sizeof(T)), runs = kThreads / lw;
   const int batches = a.offsets ? 1 : a.nseq, rows = runs * kConvBwdRows;
   const int rb = (int)((a.T + (long long)rows - 1) / rows), cb = (a.C / V + lw - 1) / lw;
   const long long tail = a.dx0 ? ((long long)a.nseq * (W - 1) + runs - 1) / runs : 0;
@@ -490,7 +615,7 @@ int launch_step(const ConvStepArgs& a, hipStream_t s) {
 
 }  // namespace
 
-int conv_bwd_block_rows(int C, int dtype) { return kThreads / lanes_of(C, dtype == CARVE_BF16 ? 2 : 4) * kConvBwdRows; }
+int conv_bwd_block_rows(int C, int dtype) { return kThreads / lanes_of(C, kBwdV, dtype == CARVE_BF16 ? 2 : 4) * kConvBwdRows; }
 long long conv_parts(long long T, int batches, int C, int dtype) {
   const int rows = conv_bwd_block_rows(C, dtype);
   return (T + rows - 1) / rows * batches;
