@@ -23,6 +23,27 @@ __device__ __forceinline__ int packed_find(const int* offsets, int nseq, int T, 
   return lo;
 }
 
+// The same for every lane of a wave at once, with the sequence's rows: up to 63 sequences
+// come with one load, and each row (the same in runs of lw lanes) is counted by a ballot,
+// where the search waits for memory at every step.  All lanes take part.
+__device__ __forceinline__ void packed_find_wave(const int* offsets, int nseq, int T, int row, int lw, int& n, int& first, int& end) {
+  if (nseq > 63) {
+    n = packed_find(offsets, nseq, T, row);
+    packed_seq(offsets, n, T, first, end);
+    return;
+  }
+  const int lane = threadIdx.x & 63;
+  const int v = min(max(offsets[min(lane, nseq)], 0), T);
+  n = 0;
+  for (int r = 0; r < 64; r += lw) {
+    const int at = __builtin_amdgcn_readlane(row, r);
+    const int count = __popcll(__builtin_amdgcn_ballot_w64(lane < nseq && v <= at));
+    if ((lane & ~(lw - 1)) == r) n = max(count - 1, 0);
+  }
+  first = __shfl(v, n);
+  end = max(__shfl(v, n + 1), first);
+}
+
 struct ConvArgs {
   const void *x, *x0, *dy, *dx_T;
   const float *weight, *bias;
@@ -40,7 +61,7 @@ struct ConvStepArgs {
   long long x_batch, x_token;
   int B, T, C, pool, act;
 };
-constexpr int kConvBwdRows = 16;   // rows of a thread in the backward
+constexpr int kConvBwdRows = 24;   // rows of a thread in the backward (16384 x 2304: 62 us; 16 rows 69, 32 rows 75)
 // rows of a workgroup of the backward, which leaves one row of partial sums for them
 int conv_bwd_block_rows(int C, int dtype);
 long long conv_parts(long long rows_of_a_batch, int batches, int C, int dtype);

@@ -102,6 +102,12 @@ struct Where {
     }
     in = row >= first && row < end;
   }
+  // the first row of a wave's runs of lw lanes (all lanes take part)
+  __device__ __forceinline__ void start(const ConvArgs& a, int batch, int row, int lw) {
+    if (!a.offsets) n = batch, first = 0, end = a.T;
+    else packed_find_wave(a.offsets, a.nseq, a.T, row, lw, n, first, end);
+    in = row >= first && row < end;
+  }
   // the next row
   __device__ __forceinline__ void next(const ConvArgs& a, int batch, int row) {
     if (a.offsets && row >= end) at(a, batch, row);
@@ -129,12 +135,18 @@ struct Place {
   long long item;          // the blocks of x_T or dx0, and any behind them: which row of them; else -1
 };
 template <int V>
-__device__ __forceinline__ bool place(const ConvArgs& a, int R, int lw, int rows_blocks, int batches, Place& p) {
+__device__ __forceinline__ void place(const ConvArgs& a, int R, int lw, int rows_blocks, int batches, Place& p) {
   const int lane = threadIdx.x & (lw - 1), run = threadIdx.x / lw, runs = kThreads / lw;
   const int cblocks = (a.C / V + lw - 1) / lw;
-  const long long b = (long long)blockIdx.y * gridDim.x + blockIdx.x;
-  const int cb = (int)(b % cblocks);
-  const long long rb = b / cblocks, main = (long long)rows_blocks * batches;
+  long long rb;
+  int cb;
+  if (gridDim.y == 1) {   // (a division of 32 bits)
+    cb = blockIdx.x % (unsigned)cblocks, rb = blockIdx.x / (unsigned)cblocks;
+  } else {
+    const long long b = (long long)blockIdx.y * gridDim.x + blockIdx.x;
+    cb = (int)(b % cblocks), rb = b / cblocks;
+  }
+  const long long main = (long long)rows_blocks * batches;
   p.c0 = (cb * lw + lane) * V;
   p.item = -1;
   p.batch = p.row0 = 0;
@@ -145,7 +157,6 @@ __device__ __forceinline__ bool place(const ConvArgs& a, int R, int lw, int rows
   } else {
     p.item = (rb - main) * runs + run;
   }
-  return p.c0 < a.C;
 }
 
 __device__ __forceinline__ float act_of(float p, int act) { return act ? silu_f(p) : p; }
@@ -158,8 +169,8 @@ __global__ void __launch_bounds__(kThreads) carve_short_conv_fwd_kernel(ConvArgs
   constexpr int V = Chunk16<T>::N;
   typedef Piece<T, V> P;
   Place pl;
-  if (!place<V>(a, R, lw, rows_blocks, batches, pl)) return;
-  const int c0 = pl.c0;
+  place<V>(a, R, lw, rows_blocks, batches, pl);
+  const int c0 = min(pl.c0, a.C - V);   // (lanes behind the channels do and write what the last one does)
   if (pl.item >= 0) {   // x_T[n][j]: the input at position len - (W - 1) + j
     const long long n = pl.item / (W - 1);
     const int j = (int)(pl.item % (W - 1));
@@ -172,28 +183,28 @@ __global__ void __launch_bounds__(kThreads) carve_short_conv_fwd_kernel(ConvArgs
     P::st(reinterpret_cast<T*>(a.x_T) + ((size_t)n * (W - 1) + j) * a.C + c0, f);
     return;
   }
-  const int row0 = pl.row0, rows = min(R, a.T - row0);
-  if (rows <= 0) return;
+  const int row0 = pl.row0, rows = min(R, a.T - row0);   // (no rows: behind the tensor)
   const T* x = reinterpret_cast<const T*>(a.x) + pl.batch * a.x_batch;
   T* y = reinterpret_cast<T*>(a.y) + ((size_t)pl.batch * a.T + row0) * a.C + c0;
+  // (the first rows on their way before the sequence is known)
+  const T* xr = x + (size_t)row0 * a.x_token + c0;
+  typename P::raw next[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) next[i] = P::ld(x + (size_t)min(row0 + i, a.T - 1) * a.x_token + c0);
   float w[W][V], b[V], past[W - 1][V];
   ld_weights<V, W>(a.weight, a.bias, c0, w, b);
   Where at;
-  at.at(a, pl.batch, row0);
+  at.start(a, pl.batch, row0, min(lw, 64));
   if (at.in) {
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) ld_past<T, W, V>(a, x, at.n, at.first, row0 - at.first - (W - 1) + j, c0, past[j]);
   }
-  const T* xr = x + (size_t)row0 * a.x_token + c0;
   if (__all(at.in && rows == R && row0 + R <= at.end)) {   // (R is a multiple of four)
     float ring[4][V];   // row r at r mod 4
 #pragma unroll
     for (int j = 0; j < W - 1; ++j)
 #pragma unroll
       for (int e = 0; e < V; ++e) ring[(j + 5 - W) & 3][e] = past[j][e];
-    typename P::raw next[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) next[i] = P::ld(xr + (size_t)i * a.x_token);
 #pragma unroll 1
     for (int i0 = 0; i0 < R; i0 += 4) {
       typename P::raw now[4];
@@ -279,14 +290,14 @@ __global__ void __launch_bounds__(kThreads) carve_short_conv_bwd_kernel(ConvArgs
   typedef Piece<T, V> P;
   __shared__ float red[kThreads * (V + 1)];
   Place pl;
-  const bool mine = place<V>(a, R, lw, rows_blocks, batches, pl);
-  const int c0 = min(pl.c0, a.C - V);   // (lanes behind the channels work on the last ones and write nothing)
+  place<V>(a, R, lw, rows_blocks, batches, pl);
+  const int c0 = min(pl.c0, a.C - V);   // (lanes behind the channels do and write what the last one does)
   float w[W][V], b[V], past[W - 1][V];
   ld_weights<V, W>(a.weight, a.bias, c0, w, b);
   if (pl.item >= 0) {   // dx0[n][i], the input at position i - (W - 1)
     const long long n = pl.item / (W - 1);
     const int i = (int)(pl.item % (W - 1));
-    if (!mine || n >= a.nseq || !a.dx0) return;
+    if (n >= a.nseq || !a.dx0) return;
     int first = 0, end = a.T;
     if (a.offsets) packed_seq(a.offsets, (int)n, a.T, first, end);
     const long long batch = a.offsets ? 0 : n;
@@ -336,13 +347,10 @@ __global__ void __launch_bounds__(kThreads) carve_short_conv_bwd_kernel(ConvArgs
     for (int j = 0; j < W - 1; ++j) past[j][e] = 0.0f;
   }
   Where at;
-  at.in = false;
-  if (rows > 0) {
-    at.at(a, pl.batch, row0);
-    if (at.in) {
+  at.start(a, pl.batch, row0, min(lw, 64));
+  if (at.in) {
 #pragma unroll
-      for (int j = 0; j < W - 1; ++j) ld_past<T, W, V>(a, x - c0, at.n, at.first, row0 - at.first - (W - 1) + j, c0, past[j]);
-    }
+    for (int j = 0; j < W - 1; ++j) ld_past<T, W, V>(a, x - c0, at.n, at.first, row0 - at.first - (W - 1) + j, c0, past[j]);
   }
   if (__all(at.in && rows == R && row0 + R + W - 1 <= at.end)) {
     float ring[4][V], acc[4][V];   // rows r's input and dx at r mod 4
@@ -398,13 +406,13 @@ __global__ void __launch_bounds__(kThreads) carve_short_conv_bwd_kernel(ConvArgs
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         row(i, rx[i], rg[i], true);
-        if ((u0 > 0 || i >= W - 1) && mine) P::st(dr + ((ptrdiff_t)u0 + i - (W - 1)) * a.C, acc[(i - (W - 1)) & 3]);
+        if (u0 > 0 || i >= W - 1) P::st(dr + ((ptrdiff_t)u0 + i - (W - 1)) * a.C, acc[(i - (W - 1)) & 3]);
       }
     }
 #pragma unroll
     for (int i = 0; i < W - 1; ++i) {
       row(i, nx[i], ng[i], false);
-      if (mine) P::st(dr + ((ptrdiff_t)R + i - (W - 1)) * a.C, acc[(i - (W - 1)) & 3]);
+      P::st(dr + ((ptrdiff_t)R + i - (W - 1)) * a.C, acc[(i - (W - 1)) & 3]);
     }
   } else if (rows > 0) {
     float acc[W][V];
@@ -453,7 +461,7 @@ __global__ void __launch_bounds__(kThreads) carve_short_conv_bwd_kernel(ConvArgs
 #pragma unroll
         for (int e = 0; e < V; ++e) past[W - 2][e] = cur[e];
       }
-      if ((ins >> (W - 1) & 1) && mine) P::st(dx + (size_t)(u - (W - 1)) * a.C, acc[W - 1]);
+      if (ins >> (W - 1) & 1) P::st(dx + (size_t)(u - (W - 1)) * a.C, acc[W - 1]);
 #pragma unroll
       for (int k = W - 1; k > 0; --k)
 #pragma unroll
