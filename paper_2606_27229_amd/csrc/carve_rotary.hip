@@ -30,7 +30,7 @@ __global__ void __launch_bounds__(kThreads) carve_rotary_kernel(RotaryArgs a, in
   const int in_row = off % per, group = in_row / chunks, piece = in_row % chunks;
   if (row >= (long long)a.B * a.T) return;
   const int batch = (int)(row / a.T), t = (int)(row % a.T);
-  int pos = 0;
+  long long pos = 0;   // (a start and a row together may pass 32 bits)
   if (a.positions) {
     pos = a.positions[row];
   } else if (a.offsets) {
@@ -38,9 +38,9 @@ __global__ void __launch_bounds__(kThreads) carve_rotary_kernel(RotaryArgs a, in
     int first, end;
     packed_seq(a.offsets, n, a.T, first, end);
     if (t < first || t >= end) return;   // a row of no sequence
-    pos = t - first + (a.start ? a.start[n] : 0);
+    pos = (long long)(t - first) + (a.start ? a.start[n] : 0);
   } else {
-    pos = t + (a.start ? a.start[batch] : 0);
+    pos = (long long)t + (a.start ? a.start[batch] : 0);
   }
   const bool turn = piece < turns;
   // first values of the thread's two 16-byte pieces
