@@ -29,7 +29,7 @@ struct SsmArgs {
   const int* offsets;      // packed sequences: [nseq + 1]; dense: NULL
   void *y, *dx, *ddt, *dBm, *dCm;
   float *S_T, *dA, *dD, *ddt_bias, *dS0;
-  float *S_chunks, *E_chunks;   // [nslots][H][P][N]: states at chunk starts, state gradients at chunk ends
+  float *S_chunks, *E_chunks;   // [nslots][H][P][N]: states at chunk starts, state gradients at chunk ends (ssm_sign)
   float* Z;                // [nspans][H][P][N]: what a span adds, then the state it starts from
   float* Zg;               // [nspans][H]: its decay
   char* scal;              // [nslots][H]: scalars; cb: [nslots][G], C B^T (backward: twice)
@@ -126,6 +126,12 @@ __device__ __forceinline__ void ssm_scalars(float raw, bool in, float bias, floa
     }
   }
 }
+// The matrix cores leave sums of bf16 products a little low (by up to a step of f32, whatever
+// their sign).  x, B and C have means, so that all tokens' da would be low together, and dA,
+// which adds them up, off by ten times what rounding leaves: in the backward every other
+// chunk's E is kept, and its products with dy are made, negated.  (At 4 x 4096 tokens of 32
+// heads dA is 8e-7 to 2e-6 off without, 5e-8 to 2e-7 with.)
+__device__ __forceinline__ float ssm_sign(int slot) { return slot & 1 ? -1.0f : 1.0f; }
 // e^{G_i - G_j}
 __device__ __forceinline__ float decay_between(float ih, float il, float jh, float jl) { return exp2_f((ih - jh) + (il - jl)); }
 

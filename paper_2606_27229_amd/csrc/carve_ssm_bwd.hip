@@ -98,6 +98,18 @@ __device__ __forceinline__ Fi<T, kExact> state_nat8(const char* lds, int i, int 
   for (int u = 0; u < GradLds<T, N>::planes; ++u) f.x[u] = SR::nat8(lds + u * SR::bytes, i, p, g, c);
   return f;
 }
+// f where sign is 1, -f where it is -1 (uniform)
+template <typename T>
+__device__ __forceinline__ Fr<T> with_sign(Fr<T> f, float sign) {
+  if constexpr (sizeof(T) == 2) {
+    const unsigned m = sign < 0.0f ? 0x80008000u : 0u;
+    f.a = __builtin_bit_cast(bf16x4, __builtin_bit_cast(u32x2_t, f.a) ^ m);
+    f.b = __builtin_bit_cast(bf16x4, __builtin_bit_cast(u32x2_t, f.b) ^ m);
+  } else {
+    f.a *= sign, f.b *= sign;
+  }
+  return f;
+}
 __device__ __forceinline__ float dot4(f32x4 a, f32x4 b) { return a[0] * b[0] + a[1] * b[1] + a[2] * b[2] + a[3] * b[3]; }
 __device__ __forceinline__ f32x4 four(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
 // over the four lanes of a column
@@ -132,6 +144,7 @@ __global__ void __launch_bounds__(768, 3) carve_ssm_grad_kernel(SsmArgs a) {
     return;
   }
   const int first = q.first + ch * kSsmC, len = min(kSsmC, q.len - ch * kSsmC);
+  const float sign = ssm_sign(slot);   // of E, and of dy where its products are summed into da
   const size_t row0 = (size_t)q.batch * a.T + first, pn = (size_t)a.P * N;
   const int turns = a.P / kPw, total = (h1 - h0) * turns;
   const auto rows = [&](int n) { return smem + L::turn + (L::bufs == 2 ? (n & 1) * L::one : 0); };
@@ -254,7 +267,8 @@ __global__ void __launch_bounds__(768, 3) carve_ssm_grad_kernel(SsmArgs a) {
         if (L::bufs == 1) __syncthreads();   // (0)
         __syncthreads();                     // (1)
         anew();
-        const Fr<T> fy = VR::nat(buf + L::dY, w, 0, g, c), fy8 = VR::nat8(buf + L::dY, w, 0, g, c);
+        const Fr<T> fy = with_sign<T>(VR::nat(buf + L::dY, w, 0, g, c), sign),
+                    fy8 = with_sign<T>(VR::nat8(buf + L::dY, w, 0, g, c), sign);
 #pragma unroll
         for (int i = 0; i < 4; ++i) Q[i] = mma<T>(VR::nat8(buf + L::X, i, 0, g, c), fy8, Q[i]);
         if (w < NP) {   // (uniform) <E, S> of 32 n: the diagonal of their product
@@ -266,7 +280,7 @@ __global__ void __launch_bounds__(768, 3) carve_ssm_grad_kernel(SsmArgs a) {
         for (int j = 0; j < NT; ++j) U[j] = mma<T>(state_tr<T, N, kExact>(buf + L::S, j, g, c), fy, U[j]);
       }
       anew();
-      const float Gh = sc[kSmGh * kSsmC + tok], Gl = sc[kSmGl * kSsmC + tok], gam = sc[kSmGam * kSsmC + tok];
+      const float Gh = sc[kSmGh * kSsmC + tok], Gl = sc[kSmGl * kSsmC + tok], gam = sc[kSmGam * kSsmC + tok] * sign;
       float* su = sums(h);
       float r = 0.0f, mine = 0.0f, carry = 0.0f;
 #pragma unroll
@@ -281,6 +295,7 @@ __global__ void __launch_bounds__(768, 3) carve_ssm_grad_kernel(SsmArgs a) {
         f32x4 pre = zero4(), ms = zero4();
         if (i <= w) {   // (uniform)
           const f32x4 d = four(sc + kSmD * kSsmC + 16 * i + 4 * g);
+          Q[i] *= sign;
           if (i < w) {  // (uniform) from a tile before
             Q[i] *= four(sc + kSmF * kSsmC + 16 * i + 4 * g) * decay_between(Gh, Gl, sc[kSmTile + i], sc[kSmTile + 4 + i]);
           } else {
@@ -327,7 +342,7 @@ __global__ void __launch_bounds__(768, 3) carve_ssm_grad_kernel(SsmArgs a) {
       for (int e = 0; e < 4; ++e) es += masked(4 * g + e == c, ES[e]);
       es = group_sum<64>(es);
       if (g == 0) su[kSuR * kSsmC + tok] = r, su[kSuDiag * kSsmC + tok] = mine, su[kSuD * kSsmC + tok] = sc[kSmD * kSsmC + tok];
-      if (lane == 0) su[kSuES + w] = es, su[kSuWhole] = sc[kSmWhole];
+      if (lane == 0) su[kSuES + w] = es, su[kSuWhole] = sc[kSmWhole] * sign;
     }
   } else {   // ---- dB, dx
     f32x4 CB[4];   // C B^T: rows i, the tile's columns j
@@ -362,7 +377,7 @@ __global__ void __launch_bounds__(768, 3) carve_ssm_grad_kernel(SsmArgs a) {
           for (int s = 0; s < 2; ++s) Lf[s] = to_fi<T, kNear>(decayed(2 * s, CB[2 * s]), decayed(2 * s + 1, CB[2 * s + 1]));
         }
         const Fr<T> fx = VR::nat(buf + L::X, w, 0, g, c), fx8 = VR::nat8(buf + L::X, w, 0, g, c);
-        const float dj = sc[kSmD * kSsmC + tok], endj = sc[kSmEnd * kSsmC + tok], endd = sc[kSmEndD * kSsmC + tok];
+        const float dj = sc[kSmD * kSsmC + tok], endj = sc[kSmEnd * kSsmC + tok] * sign, endd = sc[kSmEndD * kSsmC + tok] * sign;
 #pragma unroll
         for (int i = 0; i < 4; ++i) Q[i] = mma<T>(VR::nat8(buf + L::dY, i, 0, g, c), fx8, Q[i]);
 #pragma unroll

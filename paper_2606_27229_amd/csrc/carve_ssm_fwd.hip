@@ -22,6 +22,10 @@ struct Tile {
 #pragma unroll
     for (int j = 0; j < N / 16; ++j) *reinterpret_cast<f32x4*>(row + 16 * j) = S[j];
   }
+  __device__ __forceinline__ void scale(float by) {
+#pragma unroll
+    for (int j = 0; j < N / 16; ++j) S[j] *= by;
+  }
   // S <- whole S + sum_t k_t (f_t v_t)^T over the chunk's rows k (N wide); v: the wave's 16
   // columns of the rows v, f(t): the factors of four tokens from t
   template <typename KR, typename F>
@@ -135,7 +139,9 @@ __global__ void __launch_bounds__(64 * NW, 2) carve_ssm_state_kernel(SsmArgs a) 
   const long long ks = REV ? a.cs[1] : a.bs[1], vs = REV ? (long long)a.H * a.P : a.xs[1];
   const T* vb = REV ? reinterpret_cast<const T*>(a.dy) + (((size_t)p.q.batch * a.T + p.first) * a.H + h) * a.P + p0
                     : reinterpret_cast<const T*>(a.x) + p.q.batch * a.xs[0] + p.first * a.xs[1] + h * a.xs[2] + p0;
-  float decay = 1.0f;
+  // (in reverse the state has the sign of the chunk that it is the gradient behind)
+  float decay = 1.0f, sign = REV ? ssm_sign(p.slot0 + p.nch - 1) : 1.0f;
+  if (FULL) t.scale(sign);
 #pragma unroll 1
   for (int i = 0; i < p.nch; ++i) {
     const int ch = REV ? p.nch - 1 - i : i, len = min(kSsmC, p.len - ch * kSsmC);
@@ -151,12 +157,14 @@ __global__ void __launch_bounds__(64 * NW, 2) carve_ssm_state_kernel(SsmArgs a) 
     }
     __syncthreads();
     const Fr<T> v[2] = {VR::tr32(smem + L::V, 0, w, g, c), VR::tr32(smem + L::V, 1, w, g, c)};
+    if (REV) sign = -sign;
     t.template add<KR>(smem + L::K, v, [&](int at) {
-      return four(sc + (REV ? kSmGam : kSmEndD) * kSsmC + at);
-    }, sc[kSmWhole], g, c);
+      return REV ? four(sc + kSmGam * kSsmC + at) * sign : four(sc + kSmEndD * kSsmC + at);
+    }, REV ? -sc[kSmWhole] : sc[kSmWhole], g, c);
     decay *= sc[kSmWhole];
   }
   settle();
+  if (REV) t.scale(sign);
   if (!FULL) {
     t.store(zs);
     if (tid == 0 && p0 == 0) a.Zg[(size_t)p.slot * a.H + h] = decay;
