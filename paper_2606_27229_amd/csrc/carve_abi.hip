@@ -1157,9 +1157,12 @@ struct SsmPlan {
   int span, splits;
 };
 // Spans: as many as let every compute unit hold two workgroups of the outputs (a pair of
-// units each, see carve_ssm_fwd.hip), none shorter than kSsmMinSpan chunks.
+// units each, see carve_ssm_fwd.hip), none shorter than kSsmMinSpan chunks.  (For 512
+// workgroups, 256 and 1024: 119, 128 and 136 us at 4 x 4096 tokens of 32 heads, 122, 140 and
+// 139 at 16384 tokens.  For spans of at least 2 chunks, 1 and 4: 30, 28 and 40 us at 1024
+// tokens of 8 heads, 45, 52 and 49 at 4096 of 16; training, 129, 150 and 136 at 2048 of 32.)
 constexpr long long kSsmGroups = 512;
-constexpr int kSsmMinSpan = 4;
+constexpr int kSsmMinSpan = 2;
 SsmPlan ssm_plan(const carve_ssm_dims_t* d) {
   SsmPlan p;
   const long long units = (d->T + (long long)kSsmC - 1) / kSsmC;
@@ -1172,7 +1175,8 @@ SsmPlan ssm_plan(const carve_ssm_dims_t* d) {
   const long long L = (long long)p.span * kSsmC;
   p.spans = d->N ? (size_t)(d->T / L) + d->N : (size_t)(d->B * ((d->T + L - 1) / L));
   // Shares of a group's heads: the gradients run one workgroup a compute unit, in turns of
-  // 256, each of which takes its heads and about as long as one more to begin and end.
+  // 256, each of which takes its heads and about as long as one more to begin and end (2048
+  // tokens of 32 heads, forward and backward: 129 us, 300 undivided).
   const long long rep = d->H / d->G, wgs = (long long)p.chunks * d->G;
   double best = 0.0;
   p.splits = 1;

@@ -7,17 +7,24 @@
 //
 // Angles are formed and brought to one turn in 64 bits: position * freq reaches 10^6, of
 // which f32 keeps a sixteenth; sines and cosines, of less than half a turn, are f32.
-// Bound by HBM: every value is read and written once.  A thread makes the sines of one
-// row's 8 (bf16) or 4 (f32) pairs once and turns those pairs of several heads, of the
-// queries and the keys alike; 16-byte accesses.
+// Bound by HBM: every value is read and written once (and by the call for few tokens: 4 us of
+// the kernel, 9 to 10 with the call).  A thread makes the sines of one row's 8 (bf16) or 4
+// (f32) pairs once and turns those pairs of two heads, of the queries and the keys alike;
+// 16-byte accesses.
 #include "carve_ops.h"
 
 namespace carve {
 namespace {
 
 constexpr int kThreads = 256;
+// Heads of a thread.  The sines are about 300 operations, but threads that load more than two
+// heads' pairs one after another keep fewer loads under way than the memory has room for:
+// 4 x 4096 tokens of 16 + 16 bf16 heads of 128 (268 MB) take 48 us with 2 heads (5.5 TB/s),
+// 59 with 1, 53 with 3, 55 with 4 and 59 with 8; 8191 rows of 16 + 4 f32 heads 28 us with 2,
+// 29 with 1 or 4; one token a sequence the same with any.
+constexpr int kHeads = 2;
 
-template <typename T, int HPT>
+template <typename T>
 __global__ void __launch_bounds__(kThreads) carve_rotary_kernel(RotaryArgs a, int chunks, int turns, int groups) {
   constexpr int V = Chunk16<T>::N;
   const long long b64 = (long long)blockIdx.y * gridDim.x + blockIdx.x;
@@ -104,34 +111,24 @@ __global__ void __launch_bounds__(kThreads) carve_rotary_kernel(RotaryArgs a, in
   T* ko = reinterpret_cast<T*>(a.ko) + batch * a.kos[0] + t * a.kos[1];
   // heads, the keys' behind the queries'
 #pragma unroll
-  for (int i = 0; i < HPT; ++i) {
-    const int h = group * HPT + i;
+  for (int i = 0; i < kHeads; ++i) {
+    const int h = group * kHeads + i;
     if (h < a.Hq) one(q + h * a.qs[2], qo + h * a.qos[2]);
     else if (h < a.Hq + a.Hk) one(k + (h - a.Hq) * a.ks[2], ko + (h - a.Hq) * a.kos[2]);
   }
 }
 
-template <typename T, int HPT>
-int launch_h(const RotaryArgs& a, hipStream_t s) {
+template <typename T>
+int launch_t(const RotaryArgs& a, hipStream_t s) {
   constexpr int V = Chunk16<T>::N;
   const int turns = a.rot / 2 / V, chunks = turns + (a.copy ? ((a.D - a.rot) / V + 1) / 2 : 0);
-  const int groups = (a.Hq + a.Hk + HPT - 1) / HPT;
+  const int groups = (a.Hq + a.Hk + kHeads - 1) / kHeads;
   const long long threads = (long long)a.B * a.T * chunks * groups, blocks = (threads + kThreads - 1) / kThreads;
   const long long gx = blocks < (1 << 20) ? blocks : 1 << 20, gy = (blocks + gx - 1) / gx;
   if (gy > 65535) return CARVE_ERR_UNSUPPORTED;
-  hipLaunchKernelGGL((carve_rotary_kernel<T, HPT>), dim3((unsigned)gx, (unsigned)gy), dim3(kThreads), 0, s, a, chunks, turns, groups);
+  hipLaunchKernelGGL(carve_rotary_kernel<T>, dim3((unsigned)gx, (unsigned)gy), dim3(kThreads), 0, s, a, chunks, turns, groups);
   return hipGetLastError() == hipSuccess ? CARVE_OK : CARVE_ERR_HIP;
 }
-// Heads of a thread: eight, so that the sines (about 300 operations) are a third of its
-// work; fewer where that would leave less than four workgroups a compute unit.
-template <typename T>
-int launch_t(const RotaryArgs& a, hipStream_t s) {
-  const long long all = (long long)a.B * a.T * (a.Hq + a.Hk) * (a.rot / 2 / Chunk16<T>::N);
-  if (all >= 8ll * 4 * 256 * kThreads) return launch_h<T, 8>(a, s);
-  if (all >= 2ll * 4 * 256 * kThreads) return launch_h<T, 2>(a, s);
-  return launch_h<T, 1>(a, s);
-}
-
 }  // namespace
 
 int launch_rotary(const RotaryArgs& a, int dtype, hipStream_t s) {

@@ -577,10 +577,11 @@ bool grid_of(long long blocks, dim3& g) {
   return true;
 }
 
-// Rows of a thread in the forward: runs of 16, but of 4 where those are fewer workgroups
-// than would fill the card.
+// Rows of a thread in the forward: runs of 16, but of 4 where those would be fewer workgroups
+// than compute units (16384 x 2304: 37 us by 16, 49 by 4; 16384 x 1024, 512 workgroups: 22.4
+// and 24.0; 8192 x 1024, 256: 16.2 and 16.6; 2048 x 512, 32: 13.7 and 11.9 with the call).
 constexpr int kConvRows = 16, kConvFewRows = 4;
-constexpr long long kConvFewBlocks = 1024;
+constexpr long long kConvFewBlocks = 256;
 
 template <typename T, int W>
 int launch_fwd(const ConvArgs& a, hipStream_t s) {

@@ -219,7 +219,7 @@ struct RowStore {
 // ---- workgroups of the scans -------------------------------------------------------------
 // Workgroup -> (span, head, slice of PW value rows).  Blocks 8 apart share an XCD: with many
 // spans each goes to one XCD with all its heads, which read the same B and C from one L2;
-// with few the heads are spread.
+// with few the heads are spread (64 spans of 16384 tokens of 32 heads: 122 us, 128 spread).
 constexpr int kSsmManySpans = 32;
 __host__ __device__ inline unsigned ssm_grid(int nspans, int per) {
   return nspans >= kSsmManySpans ? (unsigned)((nspans + 7) / 8 * 8) * per : (unsigned)nspans * per;
