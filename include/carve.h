@@ -515,9 +515,10 @@ int carve_rotary(const carve_rotary_dims_t* d, const void* q, const void* k, con
  *     chunk, written by carve_ssm_chunk_fwd for carve_ssm_chunk_bwd (slots of no chunk are
  *     left as they were).
  *   - Supported: S in {32, 64, 128}; P a multiple of 32, at most 256; H a multiple of G,
- *     at most 65535; dtype f32 or bf16.  Chunk count, and spans * H * P / 32 rounded up
- *     to eights, below 2^23 (a span is four chunks or more; sequences are at most
- *     twice the rest).
+ *     at most 65535; G at most 61000; dtype f32 or bf16.  T / 64 + N, and B times T / 64
+ *     rounded up, below 2^23.  A call works in spans of two chunks or more, and spans + 8
+ *     times H * P / 32 is below 2^23: T / 128 + N spans at most where sequences are packed,
+ *     B times T / 128 rounded up else.
  *   - A decay of -inf (a reset) is taken as e^-10000; NaN and infinities propagate within
  *     their sequence, also to tokens before them in the same chunk.  Precision as for the
  *     gated delta rule: f32 outputs to f32 accuracy.
@@ -566,8 +567,9 @@ int carve_ssm_step(const carve_ssm_dims_t* d, const void* x, const void* dt, con
 
 /* Measurement hook (not part of the computation).  Arms the next
  * carve_chunk_*, carve_rmsnorm_*, carve_gdr_*, carve_block_norm_*,
- * carve_short_conv_*, carve_rotary or carve_ssm_* call made on the calling thread to record events[0] on its stream before its first kernel launch and events[i] after
- * its i-th launch (the forward makes 1 launch; the backward 4: clear of the
+ * carve_short_conv_*, carve_rotary or carve_ssm_* call made on the calling thread to
+ * record events[0] on its stream before its first kernel launch and events[i] after its
+ * i-th launch (the forward makes 1 launch; the backward 4: clear of the
  * chunk ready flags, chunk recompute fused with the adjoint, the partials of
  * d[Ub;Uw] and dVb/dVw, their fixed-order reductions; the gated backward
  * a 5th, the reduction of dA, dtau over the batch; the backward with the
