@@ -186,12 +186,6 @@ __device__ __forceinline__ float masked(bool on, float v) {
   asm("" : "+v"(v));
   return on ? v : 0.0f;
 }
-// wait for all but the wave's last N vector memory operations (stores that follow loads)
-template <int N>
-__device__ __forceinline__ void vm_wait_but() {
-  static_assert(N < 16, "the low bits of the count");
-  __builtin_amdgcn_s_waitcnt(0x0F70 | N);
-}
 // Behind a loop whose last instructions are products: the stores that follow read their
 // results, and the compiler leaves them a wait state short there.
 __device__ __forceinline__ void settle() { asm volatile("s_nop 7" ::: "memory"); }
