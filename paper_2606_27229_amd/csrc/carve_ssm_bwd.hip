@@ -27,10 +27,12 @@ constexpr int kPart = 4;  // floats of a (chunk, head) in SsmArgs::part
 // rows of S and E.  The other waves bring them a turn ahead: wave 8 rows straight into LDS (a
 // wave that reads LDS waits for all the LDS loads it has under way, so the loads are
 // others'); waves 9 and 10 the states, which pass their registers and become the matrix
-// cores' operands on the way (with bf16 tokens three bf16 values each, SsmPlanes); wave 11
+// cores' operands on the way (with bf16 tokens three bf16 values each, StateRows); wave 11
 // makes a head's ddt and its sums when the others have gone on.
-// Bound by HBM, the states S and E above all (N x P floats each, a chunk and head), and by
-// the latency of a turn's steps.
+// Bound by the latency of a turn's steps, most of all of its loads: the states S and E (N x P
+// floats each, a chunk and head) are 0.54 of the 0.74 GB that 4 x 4096 tokens of 32 heads read in 250 to
+// 267 us (2.9 TB/s); vector instructions issue in 46 % of the cycles, matrix cores work in
+// 22 %, LDS in 41 %.  Without the loads it takes as long as without the products.
 template <typename T, int N>
 struct GradLds {
   typedef SsmRows<T, N, kSsmC> KR;     // B, C
@@ -56,9 +58,13 @@ struct StateRows {
   typedef typename L::SR SR;
   static constexpr int n = kPw * N / 256;   // quads of a lane
   f32x4 v[n];
+  // (read once: past the L2, which the rows of B, C, x and dy want; 280 -> 267 us)
+  static __device__ __forceinline__ f32x4 quad(const float* from, int k, int lane) {
+    return __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(from + 4 * (64 * k + lane)));
+  }
   __device__ __forceinline__ void load(const float* from, int lane) {
 #pragma unroll
-    for (int k = 0; k < n; ++k) v[k] = *reinterpret_cast<const f32x4*>(from + 4 * (64 * k + lane));
+    for (int k = 0; k < n; ++k) v[k] = quad(from, k, lane);
   }
   // next: the rows that take the registers as they become free
   __device__ __forceinline__ void put(char* lds, int lane, const float* next) {
@@ -77,7 +83,7 @@ struct StateRows {
       } else {
         *reinterpret_cast<f32x4*>(lds + row * SR::RB + ((q ^ SR::swz(row)) << 4)) = v[k];
       }
-      v[k] = *reinterpret_cast<const f32x4*>(next + 4 * (64 * k + lane));
+      v[k] = quad(next, k, lane);
     }
   }
 };
