@@ -46,7 +46,8 @@ struct Tile {
 __device__ __forceinline__ f32x4 four(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
 
 // Scalars and C B^T of every chunk slot: blockIdx.y < G a group's products, wave w making
-// its column tile w; behind them the scalars of 16 heads, four a wave.
+// its column tile w; behind them the scalars of 16 heads, four a wave (4 x 4096 tokens of 32
+// heads: 10 us, one after another of loads, sums by shuffles and stores; 6 of a few chunks).
 constexpr int kPrepHeads = 16;
 template <typename T, int N, bool BWD>
 __global__ void __launch_bounds__(256) carve_ssm_prep_kernel(SsmArgs a) {
@@ -106,6 +107,8 @@ __global__ void __launch_bounds__(256) carve_ssm_prep_kernel(SsmArgs a) {
 // last adds to the state.  Reverse: E <- e^{G_C} E + dY^T (e^G C) from the last chunk to the
 // first: what each span but the first adds, or (FULL), from the span's own end, E of every
 // chunk's end, then dS0.
+// (4 x 4096 tokens of 32 heads: 37 us for the spans' sums; 99 for every chunk's E, whose 268 MB a
+// fill of memory takes 39 for.)
 template <typename T, int N, int NW>
 struct StateLds {
   typedef SsmRows<T, N, kSsmC> KR;
@@ -172,7 +175,8 @@ __global__ void __launch_bounds__(64 * NW, 2) carve_ssm_state_kernel(SsmArgs a) 
 
 // Joins the spans of every sequence: Z becomes the state each span starts from (REV: the
 // gradient of the state it ends with).  Elementwise along the sequence: four values a
-// thread; the spans next to come are loaded ahead of the sum that waits for them.
+// thread; the spans next to come are loaded ahead of the sum that waits for them (8 spans of
+// 4 sequences, 32 heads: 11 us, 67 MB).
 template <bool REV>
 __global__ void __launch_bounds__(256) carve_ssm_join_kernel(SsmArgs a) {
   const size_t pn = (size_t)a.P * a.N;
@@ -215,7 +219,9 @@ __global__ void __launch_bounds__(256) carve_ssm_join_kernel(SsmArgs a) {
 //   all waves   L d C B^T of both units from C B^T, a pair of tiles a wave: operand images in LDS
 //   its waves   Y^T = S (e^G C)^T + X^T (L d C B^T)^T + D X^T, then S as above
 // Bound by the latency of these steps: two workgroups a compute unit take turns with loads
-// and products.
+// and products (4 x 4096 tokens of 32 heads: 82 us; without loads and stores 67; vector
+// instructions issue in 30 % of the cycles, matrix cores work in 20 %, LDS in 27 %).  One
+// workgroup a compute unit with waves that load a chunk ahead took 97, one unit a workgroup 113.
 template <typename T, int N, int NW>
 struct OutLds {
   typedef SsmRows<T, N, kSsmC> KR;
