@@ -516,7 +516,7 @@ int carve_rotary(const carve_rotary_dims_t* d, const void* q, const void* k, con
  *     left as they were).
  *   - Supported: S in {32, 64, 128}; P a multiple of 32, at most 256; H a multiple of G,
  *     at most 65535; G at most 61000; dtype f32 or bf16.  T / 64 + N, and B times T / 64
- *     rounded up, below 2^23.  A call works in spans of two chunks or more, and spans + 8
+ *     rounded up, below 5 * 2^20.  A call works in spans of two chunks or more, and spans + 8
  *     times H * P / 32 is below 2^23: T / 128 + N spans at most where sequences are packed,
  *     B times T / 128 rounded up else.
  *   - A decay of -inf (a reset) is taken as e^-10000; NaN and infinities propagate within

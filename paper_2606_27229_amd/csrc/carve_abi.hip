@@ -1186,11 +1186,12 @@ SsmPlan ssm_plan(const carve_ssm_dims_t* d) {
   }
   return p;
 }
-// the chunk form's: a launch has less than 2^32 threads of each dimension
+// the chunk form's: a launch has less than 2^32 threads of each dimension (the gradients 768 a chunk)
+constexpr long long kSsmMaxChunks = 5LL << 20;
 int check_ssm_chunk(const carve_ssm_dims_t* d) {
   const int st = check_ssm(d);
   if (st) return st;
-  if ((long long)(d->T / kSsmC) + d->N >= (1LL << 23) || (long long)d->B * ((d->T + kSsmC - 1) / kSsmC) >= (1LL << 23))
+  if ((long long)(d->T / kSsmC) + d->N >= kSsmMaxChunks || (long long)d->B * ((d->T + kSsmC - 1) / kSsmC) >= kSsmMaxChunks)
     return CARVE_ERR_UNSUPPORTED;
   const SsmPlan p = ssm_plan(d);
   if ((long long)(p.spans + 8) * d->H * (d->P / 32) >= (1LL << 23) || d->G > 61000) return CARVE_ERR_UNSUPPORTED;

@@ -244,6 +244,16 @@ def test_ssm_calls_beyond_a_launch():
         assert ssm(d) == UNSUPPORTED and ssm(d, "bwd") == UNSUPPORTED
 
 
+def test_ssm_most_chunks():
+    """The gradients run 768 threads a chunk: at most 5 * 2^20 of them."""
+    lib, one = carve.load_library(), dict(B=1, T=64, G=1, H=1, P=32, S=32)
+    for n, fits in (((5 << 20) - 2, True), (5 << 20, False), (6 << 20, False)):
+        d = sdims(N=n, **one)
+        assert (lib.carve_ssm_chunk_count(ctypes.byref(d)) > 0) == fits
+        if not fits:
+            assert ssm(d) == UNSUPPORTED and ssm(d, "bwd") == UNSUPPORTED
+
+
 def test_ssm_sizes():
     lib = carve.load_library()
     count = lambda **kw: lib.carve_ssm_chunk_count(ctypes.byref(sdims(**kw)))
