@@ -222,6 +222,8 @@ __global__ void __launch_bounds__(256) carve_ssm_join_kernel(SsmArgs a) {
 // and products (4 x 4096 tokens of 32 heads: 82 us; without loads and stores 67; vector
 // instructions issue in 30 % of the cycles, matrix cores work in 20 %, LDS in 27 %).  One
 // workgroup a compute unit with waves that load a chunk ahead took 97, one unit a workgroup 113.
+// Of two waves the one that is further on in its chunk goes first, so that its workgroup's loads
+// begin (the whole forward 126 -> 121 us).
 template <typename T, int N, int NW>
 struct OutLds {
   typedef SsmRows<T, N, kSsmC> KR;
@@ -280,6 +282,7 @@ __global__ void __launch_bounds__(128 * NW, sizeof(T) == 2 && NW == 4 ? 4 : 2) c
     }
     vm_wait_all();
     __syncthreads();   // (1) its rows and scalars are there
+    __builtin_amdgcn_s_setprio(1);
     // (stores behind the barrier: ahead of it the loads, or what waits for them, take 159 us at 4 x
     // 4096 tokens of 32 heads, here 142; a unit that is not there writes the other's states, which are its own)
     if (KEEP) t.store(a.S_chunks + ((size_t)(p.slot0 + ch) * a.H + h) * pn + row);
@@ -310,6 +313,7 @@ __global__ void __launch_bounds__(128 * NW, sizeof(T) == 2 && NW == 4 ? 4 : 2) c
       }
     }
     __syncthreads();   // (2) the images are there
+    __builtin_amdgcn_s_setprio(2);
     const Fr<T> fx[2] = {VR::tr32(xb, 0, w, g, c), VR::tr32(xb, 1, w, g, c)};
     // (four token tiles side by side: a tile's products follow each other)
     f32x4 o[4];
@@ -334,6 +338,7 @@ __global__ void __launch_bounds__(128 * NW, sizeof(T) == 2 && NW == 4 ? 4 : 2) c
       for (int i = 0; i < 4; ++i) out.st(16 * i + c, 4 * g, o[i] + Quad<T>::f32(VR::quad(xb, i, w, g, c)) * skip);
     }
     t.template add<KR>(smem + L::B, fx, [&](int at) { return four(sc + kSmEndD * kSsmC + at); }, sc[kSmWhole], g, c);
+    __builtin_amdgcn_s_setprio(0);
   }
   settle();
   if (mine && a.S_T && p.s == p.nspan - 1) t.store(a.S_T + ((size_t)p.q.n * a.H + h) * pn + row);
