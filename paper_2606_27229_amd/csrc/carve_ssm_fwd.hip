@@ -219,11 +219,11 @@ __global__ void __launch_bounds__(256) carve_ssm_join_kernel(SsmArgs a) {
 //   all waves   L d C B^T of both units from C B^T, a pair of tiles a wave: operand images in LDS
 //   its waves   Y^T = S (e^G C)^T + X^T (L d C B^T)^T + D X^T, then S as above
 // Bound by the latency of these steps: two workgroups a compute unit take turns with loads
-// and products (4 x 4096 tokens of 32 heads: 82 us; without loads and stores 67; vector
-// instructions issue in 30 % of the cycles, matrix cores work in 20 %, LDS in 27 %).  One
+// and products (4 x 4096 tokens of 32 heads: 79 us, 130 with every chunk's state; without loads
+// and stores 67 of 82; vector instructions issue in 32 % of the cycles, matrix cores work in 21 %).  One
 // workgroup a compute unit with waves that load a chunk ahead took 97, one unit a workgroup 113.
 // Of two waves the one that is further on in its chunk goes first, so that its workgroup's loads
-// begin (the whole forward 126 -> 121 us).
+// begin (82 -> 79 us, with states 142 -> 130).
 template <typename T, int N, int NW>
 struct OutLds {
   typedef SsmRows<T, N, kSsmC> KR;
