@@ -1032,7 +1032,7 @@ namespace {
 
 // whether every element of a strided [.., D] tensor has a place of its own (st, n: strides
 // and counts of its three outer dimensions)
-bool places_apart(const long long* st, const int* n, int D) {
+bool places_apart(const long long* st, const int* n, long long D) {
   int order[3] = {0, 1, 2};
   for (int i = 0; i < 2; ++i)
     for (int j = 0; j < 2 - i; ++j)
@@ -1045,16 +1045,19 @@ bool places_apart(const long long* st, const int* n, int D) {
   }
   return true;
 }
-// whether the heads of two such tensors lie in one row of a fused tensor without meeting
+// whether two such tensors are slices of one fused tensor's rows without meeting: their
+// heads one after another, and what lies from the first head to the last one of them apart
+// from every other row's
 bool rows_apart(const void* p, const long long* sp, int hp, const void* r, const long long* sr, int hr, const int* n, int D,
                 size_t es) {
   if ((uintptr_t)p > (uintptr_t)r) return rows_apart(r, sr, hr, p, sp, hp, n, D, es);
-  const size_t off = (uintptr_t)r - (uintptr_t)p;
-  if (((size_t)(hp - 1) * sp[2] + D) * es > off) return false;
-  const size_t end = off + ((size_t)(hr - 1) * sr[2] + D) * es;
+  const size_t off = ((uintptr_t)r - (uintptr_t)p) / es;   // (whole elements: both are 16-byte aligned)
+  if ((size_t)(hp - 1) * sp[2] + D > off) return false;
   for (int i = 0; i < 2; ++i)
-    if (n[i] > 1 && (sp[i] != sr[i] || end > (size_t)sp[i] * es)) return false;
-  return true;
+    if (n[i] > 1 && sp[i] != sr[i]) return false;
+  const long long rows[] = {sp[0], sp[1], 0};
+  const int counts[] = {n[0], n[1], 1};
+  return places_apart(rows, counts, (long long)off + (long long)(hr - 1) * sr[2] + D);
 }
 
 }  // namespace
