@@ -428,7 +428,8 @@ int carve_block_norm_bwd(const carve_block_norm_dims_t* d, const void* y, const 
  *   - Packed sequences (N > 0, B = 1, offsets) as for the gated delta rule: rows of no
  *     sequence are left as they were; offsets outside the contract stay within the
  *     tensors, with unspecified results.
- *   - Supported: W in {2, 3, 4}; C a multiple of 8 (bf16) or 4 (f32), below 2^20.
+ *   - Supported: W in {2, 3, 4}; C a multiple of 8 (bf16) or 4 (f32), below 2^20; B T below
+ *     2^31, T at most 2^31 - 64.
  *   - NaN and infinities reach the W outputs that read them.  No output may overlap an
  *     input, another output or the workspace (CARVE_ERR_UNSUPPORTED); only the step's
  *     pool is updated in place. */

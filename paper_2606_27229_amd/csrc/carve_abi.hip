@@ -923,6 +923,8 @@ int check_conv(const carve_short_conv_dims_t* d) {
   if (st) return st;
   const long long vec = 16 / (long long)esize(d->dtype);
   if (d->W < 2 || d->W > 4 || d->C % vec || d->C >= (1 << 20)) return CARVE_ERR_UNSUPPORTED;
+  // (the kernels count up to a run's rows and W - 1 more behind the last one, in ints)
+  if ((long long)d->T > (1LL << 31) - 64) return CARVE_ERR_UNSUPPORTED;
   if (d->activation != CARVE_CONV_LINEAR && d->activation != CARVE_CONV_SILU) return CARVE_ERR_ARG;
   st = check_stride(d->x_batch, d->B, vec);
   return st ? st : check_stride(d->x_token, d->T, vec);
