@@ -1123,6 +1123,7 @@ def rotary_bwd(dq, dk, freq, *, positions=None, start=None, offsets=None, interl
 def _ssm_call(x, dt, A, Bm, Cm, D, dt_bias, softplus, offsets):
     """Checks what every entry point takes; returns (dims, chunks, workspace bytes of
     forward and backward, sequences, the pointers of x, dt, A, Bm, Cm, D, dt_bias)."""
+    softplus = bool(softplus)   # (a tensor is read at every call)
     try:
         key = ("ssm", softplus, _layout(x), _layout(dt), _layout(A), _layout(Bm), _layout(Cm), _layout(D), _layout(dt_bias),
                _layout(offsets))
@@ -1149,7 +1150,7 @@ def _ssm_call(x, dt, A, Bm, Cm, D, dt_bias, softplus, offsets):
             _ptr(t, name, torch.float32, (H,))
         _ptr(offsets, "offsets", torch.int32)
         seqs, N = _count(offsets, B)
-        d = SsmDims(B, T, N, Bm.shape[2], H, P, Bm.shape[3], code, bool(softplus), *_steps(x, 3), *_steps(Bm, 3), *_steps(Cm, 3),
+        d = SsmDims(B, T, N, Bm.shape[2], H, P, Bm.shape[3], code, softplus, *_steps(x, 3), *_steps(Bm, 3), *_steps(Cm, 3),
                     *_steps(dt, 2))
         r = ctypes.byref(d)
         hit = _remember(key, (r, int(lib.carve_ssm_chunk_count(r)), int(lib.carve_ssm_workspace_size(r, 0)),
@@ -1217,6 +1218,7 @@ def ssm_step(x, dt, A, Bm, Cm, state, slots=None, *, D=None, dt_bias=None, softp
     of B sequences, whose states in the pool ``state`` [pool,H,P,N] f32 are updated in
     place; slots as in ``gdr_step``.  The other arguments are those of ``ssm_chunk_fwd``.
     Returns y [B,T,H,P] (``out`` if given)."""
+    softplus = bool(softplus)
     try:
         key = ("ssm_step", softplus, _layout(x), _layout(dt), _layout(A), _layout(Bm), _layout(Cm), _layout(D), _layout(dt_bias),
                _layout(state), _layout(slots), _layout(out))
