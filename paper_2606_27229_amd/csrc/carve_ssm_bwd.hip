@@ -226,7 +226,8 @@ __global__ void __launch_bounds__(768, 3) carve_ssm_grad_kernel(SsmArgs a) {
         return (p[0] + p[kSsmC]) + (p[2 * kSsmC] + p[3 * kSsmC]);
       };
       const float da = suf + (lane > 0 ? before : 0.0f) + waves(kSuRect) + es;
-      float dd = A * da + (waves(kSuM) + e);
+      // (A may be -inf: nothing comes through decays of 0)
+      float dd = (da != 0.0f ? A * da : 0.0f) + (waves(kSuM) + e);
       if (a.softplus) {
         const float z = raw + bias, ez = expf(-fabsf(z));
         dd *= (z >= 0.0f ? 1.0f : ez) / (1.0f + ez);
