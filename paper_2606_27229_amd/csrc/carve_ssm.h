@@ -186,9 +186,19 @@ __device__ __forceinline__ float masked(bool on, float v) {
   asm("" : "+v"(v));
   return on ? v : 0.0f;
 }
-// Behind a loop whose last instructions are products: the stores that follow read their
-// results, and the compiler leaves them a wait state short there.
-__device__ __forceinline__ void settle() { asm volatile("s_nop 7" ::: "memory"); }
+// Eight wait states between products and the stores that follow and read their results, where
+// the compiler has left one too few behind a loop.  The results pass through: the products
+// cannot sink below the wait, nor what reads them rise above it.
+template <int n>
+__device__ __forceinline__ void settle(f32x4 (&v)[n]) {
+  static_assert(n == 2 || n == 4 || n == 8, "accumulators of a wave");
+  if constexpr (n == 2)
+    asm volatile("s_nop 7" : "+v"(v[0]), "+v"(v[1]));
+  else if constexpr (n == 4)
+    asm volatile("s_nop 7" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]));
+  else
+    asm volatile("s_nop 7" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]), "+v"(v[4]), "+v"(v[5]), "+v"(v[6]), "+v"(v[7]));
+}
 
 // Rows of a chunk to memory, four values a lane, without a branch around the store (which
 // would part what the compiler may reorder): a buffer of the rows there are, behind which

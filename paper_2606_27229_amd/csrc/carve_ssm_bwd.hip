@@ -426,7 +426,7 @@ __global__ void __launch_bounds__(768, 3) carve_ssm_grad_kernel(SsmArgs a) {
     }
   }
   __syncthreads();   // (2)
-  settle();
+  settle(acc);
   if (tok < len) {
     const size_t at = ((row0 + tok) * a.G + grp) * N + 4 * g;
     if (a.splits == 1) {

@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(256) carve_ssm_prep_kernel(SsmArgs a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) M[i] = mma<T>(KR::nat8(rows, i, p, g, c), f, M[i]);
     }
-    settle();
+    settle(M);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (way ? i >= w : i <= w) *reinterpret_cast<f32x4*>(out + (way ? kSsmCB + ssm_tile(i, w) : ssm_tile(w, i))) = M[i];
@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(64 * NW, 2) carve_ssm_state_kernel(SsmArgs a) 
     }, REV ? -sc[kSmWhole] : sc[kSmWhole], g, c);
     decay *= sc[kSmWhole];
   }
-  settle();
+  settle(t.S);
   if (REV) t.scale(sign);
   if (!FULL) {
     t.store(zs);
@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(128 * NW, sizeof(T) == 2 && NW == 4 ? 4 : 2) c
     t.template add<KR>(smem + L::B, fx, [&](int at) { return four(sc + kSmEndD * kSsmC + at); }, sc[kSmWhole], g, c);
     __builtin_amdgcn_s_setprio(0);
   }
-  settle();
+  settle(t.S);
   if (mine && a.S_T && p.s == p.nspan - 1) t.store(a.S_T + ((size_t)p.q.n * a.H + h) * pn + row);
 }
 
