@@ -1153,7 +1153,10 @@ int check_ssm(const carve_ssm_dims_t* d) {
   return CARVE_OK;
 }
 
-// value rows of a unit: 64, or 32 where P is no multiple of it or they would not fit the registers
+// Value rows of a unit: 64, or 32 where P is no multiple of it and with f32 states of 128.  (By
+// 64 rows and by 32, outputs of 32 heads of 64: bf16, 4 x 4096 tokens, 112 and 125 us with
+// states of 128, 82 and 101 of 64, 73 and 90 of 32; f32, 4 x 1024 tokens, 71 and 66 with states
+// of 64, 51 and 51 of 32, 107 and 114 of 128: f32 is within a tenth either way.)
 bool ssm_wide(const carve_ssm_dims_t* d) { return d->P % 64 == 0 && !(d->dtype == CARVE_F32 && d->S == 128); }
 
 // chunks of a span, spans (slots of them) and shares of a group's heads
@@ -1162,10 +1165,13 @@ struct SsmPlan {
   int span, splits;
 };
 // Spans: as many as let every compute unit hold two workgroups of the outputs (a pair of
-// units each, see carve_ssm_fwd.hip), none shorter than kSsmMinSpan chunks.  (For 512
-// workgroups, 256 and 1024: 119, 128 and 136 us at 4 x 4096 tokens of 32 heads, 122, 140 and
-// 139 at 16384 tokens.  For spans of at least 2 chunks, 1 and 4: 30, 28 and 40 us at 1024
-// tokens of 8 heads, 45, 52 and 49 at 4096 of 16; training, 129, 150 and 136 at 2048 of 32.)
+// units each, see carve_ssm_fwd.hip), none shorter than kSsmMinSpan chunks.  (Replayed from a
+// graph, for 512 workgroups, 256 and 1024: 115, 129 and 135 us at 4 x 4096 tokens of 32 heads,
+// training 571, 584 and 598; 116, 132 and 134 at 16381 tokens.  For spans of at least 2 chunks,
+// 1 and 4: 19, 22 and 19 us at 128 tokens of 8 heads, 28, 23 and 27 at 256, 30, 28 and 39 at
+// 1024; 45, 52 and 49 at 4096 of 16, 47, 51 and 48 for 9 prompts of 1777 tokens; training, 74,
+// 64 and 72 at 256 of 8, 131, 145 and 138 at 2048 of 32: a chunk a span is a little better for
+// the smallest calls alone.)
 constexpr long long kSsmGroups = 512;
 constexpr int kSsmMinSpan = 2;
 SsmPlan ssm_plan(const carve_ssm_dims_t* d) {
@@ -1180,8 +1186,8 @@ SsmPlan ssm_plan(const carve_ssm_dims_t* d) {
   const long long L = (long long)p.span * kSsmC;
   p.spans = d->N ? (size_t)(d->T / L) + d->N : (size_t)(d->B * ((d->T + L - 1) / L));
   // Shares of a group's heads: the gradients run one workgroup a compute unit, in turns of
-  // 256, each of which takes its heads and about as long as one more to begin and end (2048
-  // tokens of 32 heads, forward and backward: 129 us, 300 undivided).
+  // 256, each of which takes its heads and about as long as one more to begin and end (32
+  // heads, forward and backward: 2048 tokens 134 us, 295 undivided; 8192 tokens 307 and 384).
   const long long rep = d->H / d->G, wgs = (long long)p.chunks * d->G;
   double best = 0.0;
   p.splits = 1;

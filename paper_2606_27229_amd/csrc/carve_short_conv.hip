@@ -15,7 +15,8 @@
 // next four are on their way.  A workgroup is LW threads of channels by 256 / LW runs, LW up
 // to 16, 32 in the backward (256 neighbouring bytes a row).  16384 rows of 2304 bf16 channels
 // take 37 us (151 MB, 4.1 TB/s), their backward 61 (226 MB, 3.7 TB/s) and 5 for the weights'
-// sums; row by row, with the window moved along, they took 44 and 84.  A step of a sequence
+// sums; row by row, with the window moved along, they took 44 and 84.  8192 rows of 2304 f32
+// channels take 27 us forward and 99 in both directions (378 MB).  A step of a sequence
 // takes 3 us, 8 with the call: its loads wait for one another (slot, inputs), no more.
 #include "carve_ops.h"
 
@@ -584,8 +585,9 @@ bool grid_of(long long blocks, dim3& g) {
 }
 
 // Rows of a thread in the forward: runs of 16, but of 4 where those would be fewer workgroups
-// than compute units (16384 x 2304: 37 us by 16, 49 by 4; 16384 x 1024, 512 workgroups: 22.4
-// and 24.0; 8192 x 1024, 256: 16.2 and 16.6; 2048 x 512, 32: 13.7 and 11.9 with the call).
+// than compute units.  (By 16 and by 4, on one input again and again, replayed from a graph:
+// 16384 x 2304, 1152 workgroups by 16, 30 and 43 us; 16384 x 1024, 512: 15.8 and 21.8; 256: 10.0
+// and 13.4; 192: 9.6 and 10.5; 128: 9.2 and 7.9; 64: 8.6 and 5.8; 2048 x 512, 32: 8.3 and 5.6.)
 constexpr int kConvRows = 16, kConvFewRows = 4;
 constexpr long long kConvFewBlocks = 256;
 

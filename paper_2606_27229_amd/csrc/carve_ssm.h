@@ -223,7 +223,8 @@ struct RowStore {
 // ---- workgroups of the scans -------------------------------------------------------------
 // Workgroup -> (span, head, slice of PW value rows).  Blocks 8 apart share an XCD: with many
 // spans each goes to one XCD with all its heads, which read the same B and C from one L2;
-// with few the heads are spread (64 spans of 16384 tokens of 32 heads: 122 us, 128 spread).
+// with few the heads are spread (by one XCD and spread: 32 spans of 4 x 4096 tokens of 32 heads
+// 114 and 113 us, of 16381 tokens in two groups 119 and 123; 22 spans of 9 prompts 48 and 46).
 constexpr int kSsmManySpans = 32;
 __host__ __device__ inline unsigned ssm_grid(int nspans, int per) {
   return nspans >= kSsmManySpans ? (unsigned)((nspans + 7) / 8 * 8) * per : (unsigned)nspans * per;

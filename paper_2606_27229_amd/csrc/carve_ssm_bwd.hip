@@ -30,9 +30,9 @@ constexpr int kPart = 4;  // floats of a (chunk, head) in SsmArgs::part
 // cores' operands on the way (with bf16 tokens three bf16 values each, StateRows); wave 11
 // makes a head's ddt and its sums when the others have gone on.
 // Bound by the latency of a turn's steps, most of all of its loads: the states S and E (N x P
-// floats each, a chunk and head) are 0.54 of the 0.74 GB that 4 x 4096 tokens of 32 heads read in 250 to
-// 267 us (2.9 TB/s); vector instructions issue in 46 % of the cycles, matrix cores work in
-// 22 %, LDS in 41 %.  Without the loads it takes as long as without the products.
+// floats each, a chunk and head) are 0.54 of the 0.72 GB that 4 x 4096 tokens of 32 heads read in 248
+// to 283 us, 264 on average (2.7 TB/s); vector instructions issue in 47 % of the cycles, matrix
+// cores work in 22 %, LDS in 41 %.  Without the loads it takes as long as without the products.
 template <typename T, int N>
 struct GradLds {
   typedef SsmRows<T, N, kSsmC> KR;     // B, C

@@ -418,8 +418,8 @@ int launch_fwd_t(const SsmArgs& a, hipStream_t s, void (*mark)(hipStream_t)) {
 
 }  // namespace
 
-// value rows of a unit: 64, or 32 where P is no multiple of it, and with f32 keys of 128,
-// whose products of 64 rows do not fit the registers (as in the C entry points' plan)
+// value rows of a unit: 64, or 32 where P is no multiple of it, and with f32 states of 128 (as
+// in the C entry points' plan, which has the figures)
 #define CARVE_SSM_BY(call)                                                      \
   const bool wide = a.P % 64 == 0;                                              \
   if (dtype == CARVE_BF16) {                                                    \

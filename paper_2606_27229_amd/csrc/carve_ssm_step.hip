@@ -4,7 +4,9 @@
 // S (N floats) is spread over N / 8 lanes, two 16-byte loads each, so that a wave load
 // covers whole rows; a lane holds kRows rows, 8 loads in flight; a row's sum runs over its
 // lanes by DPP.  One token for each of 64 sequences of 32 heads of 64 x 128 (135 MB): 24 us,
-// 5.7 TB/s, part of the states in the last-level cache.
+// 5.7 TB/s, part of the states in the last-level cache.  Small states wait longer for what they
+// move: 64 x 64 (68 MB) 14 us, 64 x 32 (34 MB) 11, 32 x 32 (17 MB) 9, with rows for one of a
+// workgroup's four waves.
 #include "carve_ssm.h"
 
 namespace carve {
