@@ -32,11 +32,12 @@ def check_plan(x, N, span, splits):
     L, state = 64 * span, H * P * S * 4
     chunks = T // 64 + N if N else B * -(-T // 64)
     spans = T // L + N if N else B * -(-T // L)
+    token, tiles = 64 * 4, 10 * 1024   # a scalar of every token; C B^T of a chunk
     z = up(spans * state) + up(spans * H * 4) if T > L else 0
     assert lib.carve_ssm_chunk_count(r) == chunks
-    assert lib.carve_ssm_workspace_size(r, 0) == up(chunks * H * 2048) + up(chunks * G * 10240) + z
+    assert lib.carve_ssm_workspace_size(r, 0) == up(chunks * H * 8 * token) + up(chunks * G * tiles) + z
     shares = up(splits * 2 * B * T * G * S * 4) if splits > 1 else 0
-    assert lib.carve_ssm_workspace_size(r, 1) == (up(chunks * H * 3072) + up(chunks * G * 20480) + z + up(chunks * state)
+    assert lib.carve_ssm_workspace_size(r, 1) == (up(chunks * H * 12 * token) + up(chunks * G * 2 * tiles) + z + up(chunks * state)
                                                   + up(chunks * H * 16) + shares)
 
 
